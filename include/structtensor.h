@@ -71,7 +71,8 @@ typedef enum { ST_TRI_UPPER = 0, ST_TET = 1, ST_BAND = 2, ST_BLOCKDIAG = 3, ST_F
                ST_SIMPLEX4 = 6 } st_kind;
 typedef enum { ST_FILL_ZERO = 0, ST_FILL_SYMMETRIC = 1 } st_fill;
 typedef enum { ST_OP_SYM_MOMENT2 = 0, ST_OP_SYM_MOMENT3 = 1, ST_OP_MTTKRP_TRI = 2,
-               ST_OP_TTM_BLOCKDIAG = 3, ST_OP_SYM_MOMENT4 = 4, ST_OP_MTTKRP_SLICE = 5 } st_op;
+               ST_OP_TTM_BLOCKDIAG = 3, ST_OP_SYM_MOMENT4 = 4, ST_OP_MTTKRP_SLICE = 5, ST_OP_ATTN_WINDOW = 6,
+               ST_OP_ATTN_WINDOW_GRAD = 7, ST_OP_ATTN_WINDOW_STEP = 8, ST_OP_ATTN_DECAY = 9, ST_OP_ATTN_DECAY_GRAD = 10 } st_op;
 
 /* flags (bit mask) */
 #define ST_FLAG_DENSE_CONTROL 1u /* run the same kernel over the dense, unstructured iteration
@@ -128,6 +129,9 @@ st_status st_unpack(const st_layout *layout, st_dtype dtype, const void *packed,
  *   ST_OP_MTTKRP_TRI    a=I, b=K, c=R (flags as for the call: they change the size)
  *   ST_OP_MTTKRP_SLICE  a=I, b=J, c=K, e=R (enough for any fixed_i / fixed_j; flags as for the call)
  *   ST_OP_TTM_BLOCKDIAG a=nblocks, b=bs, c=K, e=R
+ *   ST_OP_ATTN_WINDOW   unused: the header alone;  ST_OP_ATTN_WINDOW_STEP likewise
+ *   ST_OP_ATTN_WINDOW_GRAD a=nq, b=heads
+ *   ST_OP_ATTN_DECAY, ST_OP_ATTN_DECAY_GRAD  a=nq, b=nseq, c=heads, e=max(d, dv)
  * Returns 0 for an invalid request (the call itself reports the error).  The current
  * device is queried for its SM count. */
 size_t st_workspace_bytes(st_op op, int64_t a, int64_t b, int64_t c, int64_t e, unsigned flags);
@@ -296,6 +300,96 @@ st_status st_thp(const st_layout *layout, const float *Bp, const float *C_dense,
 st_status st_packed_axpby(int64_t n, float alpha, const float *a, float beta, const float *b,
                           float *out, void *stream);
 st_status st_packed_mul(int64_t n, const float *a, const float *b, float *out, void *stream);
+
+/* ---- contractions over pairs (query token, key token) -----------------------------------------
+ * Attention is a contraction of three tables of tokens over the unique set of a structured matrix of pairs
+ * (t, s), query t and key s <= t:  a band with the first columns (st_attn_window, weights by softmax), or the
+ * whole triangle with weights that fade with t - s (st_attn_decay).  The paper has no counterpart: its
+ * structures are what is used here -- triangle, band and single columns as unique sets, their union for a sum --
+ * and the sum of outer products of Section 3, which st_attn_decay takes causally.
+ *
+ * Tables: row = token, all sequences behind one another; sequence b holds the rows offsets[b] .. offsets[b+1]-1
+ * (int32, nseq+1 of them, device memory; NULL = one sequence of all rows).  A row that lies in no sequence is
+ * neither read nor written.  Offsets that decrease or leave the table are cut to it and reported: st_check_status returns
+ * ST_ERR_DEV_BOUNDS.  The values of one head are contiguous; rows and heads have strides (in elements, a multiple
+ * of 8, at least the head's extent), so that slices of one projection's output need no copy.  out, lse, dout and the
+ * gradients are contiguous.  A key's or value's infinity or NaN may reach rows of its own sequence that do not see it
+ * (its weight 0 times it); nothing of another sequence, of rows of no sequence or behind a cache's length does. */
+typedef struct {
+    int32_t dtype;            /* st_dtype of q, k, v, out, dout and the gradients: ST_BF16 */
+    int32_t reserved;         /* must be 0 */
+    int64_t nseq;             /* sequences */
+    int64_t nq, nk;           /* rows of q, out, dout, dq; rows of k, v, dk, dv */
+    int64_t heads, kv_heads;  /* query head h reads key head h / (heads / kv_heads) */
+    int64_t d, dv;            /* extent of a query and a key, extent of a value: multiples of 8 up to 128 */
+    int64_t q_row, q_head;    /* strides */
+    int64_t k_row, k_head;
+    int64_t v_row, v_head;
+} st_tokens;
+
+/* Softmax attention over the union of a causal band and the first columns:
+ *     visible(t, s) = s <= t  and  (s > t - window  or  s < sinks)
+ *     x[t,s] = scale q[t].k[s];  lse[t] = log sum_s exp x[t,s];  out[t] = sum_s exp(x[t,s] - lse[t]) v[s]
+ * Positions count within a sequence; where it has more keys (Lk, k_offsets) than queries (Lq, q_offsets), the
+ * queries are its last tokens: query i stands at t = Lk - Lq + i.  A query that sees nothing (t < 0) gets out = 0 and
+ * lse = -inf.  q: [nq, heads, d]; k, v: [nk, kv_heads, d]; dv must equal d.  window >= 1 (as large as you like: the whole
+ * triangle), sinks >= 0, scale > 0.  out: bf16 [nq, heads, d]; lse: fp32 [nq, heads].  Scores, maxima and sums are fp32; the weights are
+ * rounded to bf16 (relative to the row's largest) for the product with v. */
+st_status st_attn_window(const st_tokens *tokens, const void *q, const void *k, const void *v, const int32_t *q_offsets,
+                         const int32_t *k_offsets, int64_t window, int64_t sinks, float scale, void *out, float *lse,
+                         void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of st_attn_window.  With p = exp(x - lse), delta[t] = dout[t].out[t], ds = p (dout[t].v[s] - delta[t]):
+ *     dq[t] = scale sum_s ds[t,s] k[s];   dk[s] = scale sum_t ds[t,s] q[t];   dv[s] = sum_t p[t,s] dout[t]
+ * dk and dv sum over the query heads that read the key head.  out and lse are what st_attn_window gave.  dq: [nq, heads, d];
+ * dk, dv: [nk, kv_heads, d].  p and ds are rounded to bf16 for the products; fixed order of sums, no atomics. */
+st_status st_attn_window_grad(const st_tokens *tokens, const void *q, const void *k, const void *v, const void *out,
+                              const float *lse, const void *dout, const int32_t *q_offsets, const int32_t *k_offsets,
+                              int64_t window, int64_t sinks, float scale, void *dq, void *dk, void *dv, void *ws,
+                              size_t ws_bytes, void *stream);
+
+/* A cache of keys and values in pages: token s of sequence b lies in page table[b*table_cols + s/page], place s % page. */
+typedef struct {
+    int32_t dtype;            /* ST_BF16 */
+    int32_t reserved;         /* must be 0 */
+    int64_t nseq, heads, kv_heads, d;
+    int64_t pages, page;      /* pages of the cache, tokens of a page */
+    int64_t table_cols;       /* page numbers in a row of the table */
+    int64_t page_stride, token_stride, head_stride;   /* of k_pages and v_pages, in elements, multiples of 8 */
+} st_cache;
+
+/* st_attn_window for one new token of every sequence: lens[b] counts the tokens of sequence b with the new one, whose
+ * key and value (k, v: [nseq, kv_heads, d]) are written to the cache at position lens[b]-1; out = attention of q
+ * ([nseq, heads, d], position lens[b]-1) over the cache and the new token.  All contiguous but the cache.  lens[b] = 0: out = 0,
+ * nothing written.  A length beyond the table's row, and a page number outside the cache, are reported (ST_ERR_DEV_BOUNDS); the
+ * tokens concerned are left out.  Two sequences may share pages that neither writes. */
+st_status st_attn_window_step(const st_cache *cache, const void *q, const void *k, const void *v, void *k_pages,
+                              void *v_pages, const int32_t *table, const int32_t *lens, int64_t window, int64_t sinks,
+                              float scale, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Linear attention with one decay per head, a sum of outer products that fades (log_decay[h] = a <= 0, fp32 [heads]):
+ *     S[t] = exp(a) S[t-1] + k[t] (x) v[t];    out[t] = scale S[t]^T q[t],    S[-1] = state_in (or 0)
+ * q, k: [n, heads, d]; v: [n, heads, dv]; one offsets array, nq = nk, kv_heads = heads.  state_in, state_out: fp32
+ * [nseq, heads, d, dv], both may be NULL; out: bf16 [n, heads, dv].  An empty sequence hands its state on.
+ * Sums and states are fp32; where they enter a product on the tensor cores they are the sum of two bf16 numbers, the
+ * weighted scores of a chunk of tokens are rounded to bf16 once. */
+st_status st_attn_decay(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
+                        const int32_t *offsets, const float *state_in, float scale, void *out, float *state_out,
+                        void *ws, size_t ws_bytes, void *stream);
+
+/* Gradient of st_attn_decay in q, k, v and state_in (the decay is a constant of the layer):
+ *     dq[t] = scale S[t] dout[t];   R[t] = scale q[t] (x) dout[t] + exp(a) R[t+1], R[n] = exp(-a) dstate_out (or 0);
+ *     dk[t] = R[t] v[t];   dv[t] = R[t]^T k[t];   dstate_in = exp(a) R[0]
+ * state_in, dstate_out and dstate_in may be NULL. */
+st_status st_attn_decay_grad(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
+                             const void *dout, const int32_t *offsets, const float *state_in, const float *dstate_out,
+                             float scale, void *dq, void *dk, void *dv, float *dstate_in, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* st_attn_decay for one new token of every sequence (nq = nk = nseq), all arrays contiguous: state
+ * ([nseq, heads, d, dv] fp32) is updated in place. */
+st_status st_attn_decay_step(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
+                             float *state, float scale, void *out, void *stream);
 
 /* Synchronises `stream`, then reads the status word a kernel may have written into the
  * workspace (a bounded wait that ran out, a failed consistency check).  ws may be NULL. */

@@ -34,7 +34,8 @@ ST_TRI_UPPER, ST_TET, ST_BAND, ST_BLOCKDIAG, ST_FIXED_ROW, ST_FIXED_COL, ST_SIMP
 ST_FILL_ZERO, ST_FILL_SYMMETRIC = 0, 1
 # st_op
 ST_OP_SYM_MOMENT2, ST_OP_SYM_MOMENT3, ST_OP_MTTKRP_TRI, ST_OP_TTM_BLOCKDIAG, ST_OP_SYM_MOMENT4, \
-    ST_OP_MTTKRP_SLICE = 0, 1, 2, 3, 4, 5
+    ST_OP_MTTKRP_SLICE, ST_OP_ATTN_WINDOW, ST_OP_ATTN_WINDOW_GRAD, ST_OP_ATTN_WINDOW_STEP, ST_OP_ATTN_DECAY, \
+    ST_OP_ATTN_DECAY_GRAD = range(11)
 # flags
 ST_FLAG_DENSE_CONTROL = 1
 ST_FLAG_TC_TF32 = 2
@@ -44,7 +45,8 @@ ST_FLAG_TC_SPLIT = 8
 EXPORTS = [
     "st_packed_elems", "st_dense_elems", "st_pack", "st_unpack", "st_workspace_bytes", "st_sym_moment2",
     "st_sym_moment3", "st_sym_moment3_static", "st_sym_moment4", "st_mttkrp_tri", "st_mttkrp_slice", "st_ttm_blockdiag", "st_ttm_packed",
-    "st_thp", "st_packed_axpby", "st_packed_mul", "st_check_status", "st_status_string",
+    "st_thp", "st_packed_axpby", "st_packed_mul", "st_attn_window", "st_attn_window_grad", "st_attn_window_step",
+    "st_attn_decay", "st_attn_decay_grad", "st_attn_decay_step", "st_check_status", "st_status_string",
     "st_abi_version", "st_bounds_checked_build", "st_bounds_self_test",
 ]
 
@@ -53,6 +55,16 @@ class StLayout(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("reserved", ctypes.c_int32), ("d", ctypes.c_int64),
                 ("inner", ctypes.c_int64), ("kl", ctypes.c_int64), ("ku", ctypes.c_int64),
                 ("nblocks", ctypes.c_int64), ("bs", ctypes.c_int64)]
+
+
+class StTokens(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in (
+        "nseq", "nq", "nk", "heads", "kv_heads", "d", "dv", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head")]
+
+
+class StCache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in (
+        "nseq", "heads", "kv_heads", "d", "pages", "page", "table_cols", "page_stride", "token_stride", "head_stride")]
 
 
 @dataclass(frozen=True)
@@ -109,12 +121,20 @@ def lib() -> ctypes.CDLL:
         L.st_thp.argtypes = [LP, vp, vp, vp, vp]
         L.st_packed_axpby.argtypes = [i64, ctypes.c_float, vp, ctypes.c_float, vp, vp, vp]
         L.st_packed_mul.argtypes = [i64, vp, vp, vp, vp]
+        TP, cf = ctypes.POINTER(StTokens), ctypes.c_float
+        L.st_attn_window.argtypes = [TP, vp, vp, vp, vp, vp, i64, i64, cf, vp, vp, vp, sz, vp]
+        L.st_attn_window_grad.argtypes = [TP, vp, vp, vp, vp, vp, vp, vp, vp, i64, i64, cf, vp, vp, vp, vp, sz, vp]
+        L.st_attn_window_step.argtypes = [ctypes.POINTER(StCache), vp, vp, vp, vp, vp, vp, vp, i64, i64, cf, vp, vp, sz, vp]
+        L.st_attn_decay.argtypes = [TP, vp, vp, vp, vp, vp, vp, cf, vp, vp, vp, sz, vp]
+        L.st_attn_decay_grad.argtypes = [TP, vp, vp, vp, vp, vp, vp, vp, vp, cf, vp, vp, vp, vp, vp, sz, vp]
+        L.st_attn_decay_step.argtypes = [TP, vp, vp, vp, vp, vp, cf, vp, vp]
         L.st_check_status.argtypes = [vp, vp]
         L.st_status_string.argtypes = [ci]
         L.st_status_string.restype = ctypes.c_char_p
         L.st_abi_version.restype = ci
         for name in ("st_pack", "st_unpack", "st_sym_moment2", "st_sym_moment3", "st_sym_moment3_static", "st_sym_moment4", "st_mttkrp_tri",
-                     "st_mttkrp_slice", "st_ttm_blockdiag", "st_ttm_packed", "st_thp", "st_packed_axpby", "st_packed_mul", "st_check_status"):
+                     "st_mttkrp_slice", "st_ttm_blockdiag", "st_ttm_packed", "st_thp", "st_packed_axpby", "st_packed_mul", "st_attn_window",
+                     "st_attn_window_grad", "st_attn_window_step", "st_attn_decay", "st_attn_decay_grad", "st_attn_decay_step", "st_check_status"):
             getattr(L, name).restype = ci
         _lib = L
     return _lib
@@ -278,6 +298,62 @@ def st_packed_axpby(alpha: float, a: torch.Tensor, beta: float, b: torch.Tensor,
 def st_packed_mul(a: torch.Tensor, b: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """out = a * b for two packed float32 arrays of the same layout (out may be a or b)."""
     return (_native or _bind()).mul(a, b, out)
+
+
+def st_attn_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0,
+                   q_offsets: torch.Tensor | None = None, k_offsets: torch.Tensor | None = None, scale: float | None = None,
+                   out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                   ws: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Softmax attention of every token over the ``window`` last tokens (itself among them) and the first ``sinks`` tokens of
+    its sequence.  q [nq, heads, d], k and v [nk, kv_heads, d] bfloat16, the last dimension contiguous; int32 offsets say where
+    the sequences begin (None: one sequence); a sequence with more keys than queries has its queries at its end.
+    scale: 1/sqrt(d) unless given.  Returns (out, lse): bfloat16 [nq, heads, d], float32 [nq, heads]."""
+    return (_native or _bind()).attn_window(q, k, v, window, sinks, q_offsets, k_offsets, scale, out, lse, ws)
+
+
+def st_attn_window_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                        dout: torch.Tensor, window: int, sinks: int = 0, q_offsets: torch.Tensor | None = None,
+                        k_offsets: torch.Tensor | None = None, scale: float | None = None, dq: torch.Tensor | None = None,
+                        dk: torch.Tensor | None = None, dv: torch.Tensor | None = None,
+                        ws: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dq, dk, dv) of st_attn_window, from its arguments, what it returned, and the gradient of out."""
+    return (_native or _bind()).attn_window_grad(q, k, v, out, lse, dout, window, sinks, q_offsets, k_offsets, scale, dq, dk, dv, ws)
+
+
+def st_attn_window_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                        table: torch.Tensor, lens: torch.Tensor, window: int, sinks: int = 0, scale: float | None = None,
+                        out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """st_attn_window for one new token of every sequence, on a cache in pages.  q [n, heads, d], k and v [n, kv_heads, d];
+    k_pages and v_pages [pages, page, kv_heads, d]; table int32 [n, cols]: the pages of each sequence; lens int32 [n]: its
+    tokens, the new one among them, whose k and v are written to the cache at lens - 1."""
+    return (_native or _bind()).attn_window_step(q, k, v, k_pages, v_pages, table, lens, window, sinks, scale, out, ws)
+
+
+def st_attn_decay(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor,
+                  offsets: torch.Tensor | None = None, state: torch.Tensor | None = None, scale: float | None = None,
+                  out: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                  ws: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """Linear attention with one decay per head: S[t] = exp(log_decay) S[t-1] + k[t] (x) v[t], out[t] = scale S[t]^T q[t].
+    q and k [n, heads, d], v [n, heads, dv] bfloat16; log_decay float32 [heads], at most 0; state float32
+    [sequences, heads, d, dv]: S before the first token (None: 0).  Returns (out, state after the last token)."""
+    return (_native or _bind()).attn_decay(q, k, v, log_decay, offsets, state, scale, out, state_out, ws)
+
+
+def st_attn_decay_grad(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, dout: torch.Tensor,
+                       offsets: torch.Tensor | None = None, state: torch.Tensor | None = None,
+                       dstate_out: torch.Tensor | None = None, scale: float | None = None, dq: torch.Tensor | None = None,
+                       dk: torch.Tensor | None = None, dv: torch.Tensor | None = None, dstate: torch.Tensor | None = None,
+                       ws: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor | None]:
+    """(dq, dk, dv, dstate) of st_attn_decay, from the gradients of out and of the last state (None: 0).  dstate is
+    the gradient of ``state``: None where neither is passed.  The decay has no gradient."""
+    return (_native or _bind()).attn_decay_grad(q, k, v, log_decay, dout, offsets, state, dstate_out, scale, dq, dk, dv, dstate, ws)
+
+
+def st_attn_decay_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,
+                       scale: float | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """st_attn_decay for one new token of every sequence: q and k [n, heads, d], v [n, heads, dv]; state [n, heads, d, dv]
+    is updated in place."""
+    return (_native or _bind()).attn_decay_step(q, k, v, log_decay, state, scale, out)
 
 
 def st_check_status(ws: torch.Tensor | None = None) -> int:

@@ -5,9 +5,12 @@
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <exception>
@@ -36,6 +39,12 @@ struct Api {
     decltype(&st_mttkrp_slice) mttkrp_slice;
     decltype(&st_ttm_blockdiag) ttm_blockdiag;
     decltype(&st_ttm_packed) ttm_packed;
+    decltype(&st_attn_window) attn_window;
+    decltype(&st_attn_window_grad) attn_window_grad;
+    decltype(&st_attn_window_step) attn_window_step;
+    decltype(&st_attn_decay) attn_decay;
+    decltype(&st_attn_decay_grad) attn_decay_grad;
+    decltype(&st_attn_decay_step) attn_decay_step;
 } api;
 
 PyObject *error_class, *allocator;             // StError; callable or null
@@ -493,6 +502,322 @@ PyObject *py_ttm_packed(PyObject *const *v)              // Bp, U, layout, out, 
     return out.release();
 }
 
+// ---- attention ------------------------------------------------------------------------
+
+typedef c10::cuda::CUDAGuard Guard;            // the tensors' device is the current one for the call, its stream the call's
+
+const at::Tensor &cuda_tensor(PyObject *o, const char *name)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda()) {
+        PyErr_Format(PyExc_ValueError, "%s must be a CUDA tensor", name);
+        throw Failed();
+    }
+    return t;
+}
+
+void want_bf16(const at::Tensor &t, const char *name)
+{
+    if (t.scalar_type() != at::kBFloat16) {
+        PyErr_Format(PyExc_TypeError, "%s must be bfloat16", name);
+        throw Failed();
+    }
+}
+
+void want_shape(const at::Tensor &t, at::IntArrayRef shape, const char *name)
+{
+    if (t.sizes() != shape) {
+        PyErr_Format(PyExc_ValueError, "%s has the wrong shape", name);
+        throw Failed();
+    }
+}
+
+// A bf16 table of `dims` dimensions whose last one is contiguous; the others may have any strides.
+const at::Tensor &table(const at::Tensor &x, PyObject *o, const char *name, int64_t dims)
+{
+    const at::Tensor &t = cuda_tensor(o, name);
+    want_device_of(x, t, name);
+    want_bf16(t, name);
+    if (t.dim() != dims) {
+        PyErr_Format(PyExc_ValueError, "%s must have %lld dimensions", name, (long long)dims);
+        throw Failed();
+    }
+    if (t.size(dims - 1) != 1 && t.stride(dims - 1) != 1) {
+        PyErr_Format(PyExc_ValueError, "the last dimension of %s must be contiguous", name);
+        throw Failed();
+    }
+    return t;
+}
+
+const at::Tensor &contiguous(const at::Tensor &x, PyObject *o, at::ScalarType type, const char *name)
+{
+    const at::Tensor &t = cuda_tensor(o, name);
+    want_device_of(x, t, name);
+    if (t.scalar_type() != type) {
+        PyErr_Format(PyExc_TypeError, "%s must be %s", name,
+                     type == at::kFloat ? "float32" : type == at::kInt ? "int32" : type == at::kLong ? "int64" : "bfloat16");
+        throw Failed();
+    }
+    (void)device_ptr(t, name);
+    return t;
+}
+
+// One offset more than there are sequences, or None for one sequence of all rows.
+const int32_t *offsets_of(const at::Tensor &x, PyObject *o, const char *name, int64_t *nseq)
+{
+    if (o == Py_None) {
+        *nseq = 1;
+        return nullptr;
+    }
+    const at::Tensor &t = contiguous(x, o, at::kInt, name);
+    if (t.dim() != 1 || t.size(0) < 2) {
+        PyErr_Format(PyExc_ValueError, "%s must be one-dimensional, with one entry more than there are sequences", name);
+        throw Failed();
+    }
+    *nseq = t.size(0) - 1;
+    return (const int32_t *)t.data_ptr();
+}
+
+// The caller's result or a new one.
+PyObject *result(PyObject *given, PyObject *like, const at::Tensor &x, at::IntArrayRef shape, at::ScalarType type, const char *name)
+{
+    if (given != Py_None) {
+        want_shape(contiguous(x, given, type, name), shape, name);
+        Py_INCREF(given);
+        return given;
+    }
+    Ref bf16_type(PyObject_GetAttr(like, s_dtype));
+    return allocate(like, x, shape, type, type == at::kFloat ? dtype_f32 : bf16_type.o);
+}
+void *data(const Ref &r) { return THPVariable_Unpack(r.o).data_ptr(); }
+
+float scale_of(PyObject *o, int64_t d) { return o == Py_None ? (float)(1.0 / std::sqrt((double)d)) : real(o); }
+
+// Window or sinks: as many as the kernels count to, where the caller's number is larger.
+int64_t count_of(PyObject *o)
+{
+    int overflow = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
+    if (overflow) return overflow > 0 ? INT64_MAX : -1;
+    if (v == -1 && PyErr_Occurred()) throw Failed();
+    return v;
+}
+
+struct Qkv {
+    const at::Tensor &q, &k, &v;
+    st_tokens t;
+};
+
+Qkv qkv(PyObject *pq, PyObject *pk, PyObject *pv)
+{
+    const at::Tensor &q = cuda_tensor(pq, "q");
+    table(q, pq, "q", 3);
+    const at::Tensor &k = table(q, pk, "k", 3), &v = table(q, pv, "v", 3);
+    if (k.size(0) != v.size(0) || k.size(1) != v.size(1) || k.size(2) != q.size(2)) fail(PyExc_ValueError, "shape mismatch");
+    st_tokens t;
+    t.dtype = ST_BF16;
+    t.reserved = 0;
+    t.nseq = 1;
+    t.nq = q.size(0);
+    t.nk = k.size(0);
+    t.heads = q.size(1);
+    t.kv_heads = k.size(1);
+    t.d = q.size(2);
+    t.dv = v.size(2);
+    t.q_row = q.stride(0);
+    t.q_head = q.stride(1);
+    t.k_row = k.stride(0);
+    t.k_head = k.stride(1);
+    t.v_row = v.stride(0);
+    t.v_head = v.stride(1);
+    return {q, k, v, t};
+}
+
+struct Offsets {
+    const int32_t *q, *k;
+};
+Offsets two_offsets(Qkv &x, PyObject *oq, PyObject *ok)
+{
+    if (oq == Py_None && ok != Py_None) fail(PyExc_ValueError, "k_offsets without q_offsets");
+    Offsets o;
+    int64_t keys = 1;
+    o.q = offsets_of(x.q, oq, "q_offsets", &x.t.nseq);
+    o.k = ok == Py_None ? o.q : offsets_of(x.q, ok, "k_offsets", &keys);
+    if (ok != Py_None && keys != x.t.nseq) fail(PyExc_ValueError, "q_offsets and k_offsets must have the same length");
+    if (oq != Py_None && ok == Py_None && x.t.nq != x.t.nk) fail(PyExc_ValueError, "k_offsets are needed where k has not the rows of q");
+    return o;
+}
+
+PyObject *pair(Ref a, Ref b)
+{
+    PyObject *r = PyTuple_New(2);
+    if (!r) throw Failed();
+    PyTuple_SET_ITEM(r, 0, a.release());
+    PyTuple_SET_ITEM(r, 1, b.release());
+    return r;
+}
+
+PyObject *py_attn_window(PyObject *const *v)             // q, k, v, window, sinks, q_offsets, k_offsets, scale, out, lse, ws
+{
+    Qkv x = qkv(v[0], v[1], v[2]);
+    const Guard guard(x.q.device());
+    const int64_t window = count_of(v[3]), sinks = count_of(v[4]);
+    const Offsets o = two_offsets(x, v[5], v[6]);
+    const float scale = scale_of(v[7], x.t.d);
+    Ref out(result(v[8], v[0], x.q, {x.t.nq, x.t.heads, x.t.d}, at::kBFloat16, "out"));
+    Ref lse(result(v[9], v[0], x.q, {x.t.nq, x.t.heads}, at::kFloat, "lse"));
+    const Workspace w = workspace(v[10], v[0], x.q, ST_OP_ATTN_WINDOW, 0, 0, 0, 0, 0);
+    void *po = data(out);
+    float *pl = (float *)data(lse);
+    const void *q = x.q.data_ptr(), *k = x.k.data_ptr(), *vv = x.v.data_ptr();
+    call("st_attn_window", [&](void *s) { return api.attn_window(&x.t, q, k, vv, o.q, o.k, window, sinks, scale, po, pl, w.ptr, w.bytes, s); });
+    return pair(std::move(out), std::move(lse));
+}
+
+// q, k, v, out, lse, dout, window, sinks, q_offsets, k_offsets, scale, dq, dk, dv, ws
+PyObject *py_attn_window_grad(PyObject *const *v)
+{
+    Qkv x = qkv(v[0], v[1], v[2]);
+    const Guard guard(x.q.device());
+    const st_tokens &t = x.t;
+    const at::Tensor &out = contiguous(x.q, v[3], at::kBFloat16, "out"), &lse = contiguous(x.q, v[4], at::kFloat, "lse"),
+                     &dout = contiguous(x.q, v[5], at::kBFloat16, "dout");
+    want_shape(out, {t.nq, t.heads, t.d}, "out");
+    want_shape(lse, {t.nq, t.heads}, "lse");
+    want_shape(dout, {t.nq, t.heads, t.d}, "dout");
+    const int64_t window = count_of(v[6]), sinks = count_of(v[7]);
+    const Offsets o = two_offsets(x, v[8], v[9]);
+    const float scale = scale_of(v[10], t.d);
+    Ref dq(result(v[11], v[0], x.q, {t.nq, t.heads, t.d}, at::kBFloat16, "dq"));
+    Ref dk(result(v[12], v[0], x.q, {t.nk, t.kv_heads, t.d}, at::kBFloat16, "dk"));
+    Ref dv(result(v[13], v[0], x.q, {t.nk, t.kv_heads, t.d}, at::kBFloat16, "dv"));
+    const Workspace w = workspace(v[14], v[0], x.q, ST_OP_ATTN_WINDOW_GRAD, t.nq, t.heads, 0, 0, 0);
+    const void *q = x.q.data_ptr(), *k = x.k.data_ptr(), *vv = x.v.data_ptr(), *po = out.data_ptr(), *pd = dout.data_ptr();
+    const float *pl = (const float *)lse.data_ptr();
+    void *pq = data(dq), *pk = data(dk), *pv = data(dv);
+    call("st_attn_window_grad", [&](void *s) {
+        return api.attn_window_grad(&t, q, k, vv, po, pl, pd, o.q, o.k, window, sinks, scale, pq, pk, pv, w.ptr, w.bytes, s);
+    });
+    return PyTuple_Pack(3, dq.o, dk.o, dv.o);
+}
+
+// q, k, v, k_pages, v_pages, table, lens, window, sinks, scale, out, ws
+PyObject *py_attn_window_step(PyObject *const *v)
+{
+    const at::Tensor &q = cuda_tensor(v[0], "q");
+    const Guard guard(q.device());
+    contiguous(q, v[0], at::kBFloat16, "q");
+    const at::Tensor &k = contiguous(q, v[1], at::kBFloat16, "k"), &vv = contiguous(q, v[2], at::kBFloat16, "v");
+    const at::Tensor &kp = table(q, v[3], "k_pages", 4), &vp = table(q, v[4], "v_pages", 4);
+    const at::Tensor &tab = contiguous(q, v[5], at::kInt, "table"), &lens = contiguous(q, v[6], at::kInt, "lens");
+    if (q.dim() != 3 || k.dim() != 3) fail(PyExc_ValueError, "q and k must have three dimensions");
+    const int64_t n = q.size(0), d = q.size(2), kv_heads = k.size(1);
+    want_shape(k, {n, kv_heads, d}, "k");
+    want_shape(vv, {n, kv_heads, d}, "v");
+    want_shape(kp, {kp.size(0), kp.size(1), kv_heads, d}, "k_pages");
+    want_shape(vp, kp.sizes(), "v_pages");
+    if (kp.strides() != vp.strides()) fail(PyExc_ValueError, "k_pages and v_pages must have the same strides");
+    if (tab.dim() != 2 || tab.size(0) != n) fail(PyExc_ValueError, "table must have one row for every sequence");
+    want_shape(lens, {n}, "lens");
+    st_cache c;
+    c.dtype = ST_BF16;
+    c.reserved = 0;
+    c.nseq = n;
+    c.heads = q.size(1);
+    c.kv_heads = kv_heads;
+    c.d = d;
+    c.pages = kp.size(0);
+    c.page = kp.size(1);
+    c.table_cols = tab.size(1);
+    c.page_stride = kp.stride(0);
+    c.token_stride = kp.stride(1);
+    c.head_stride = kp.stride(2);
+    const int64_t window = count_of(v[7]), sinks = count_of(v[8]);
+    const float scale = scale_of(v[9], d);
+    Ref out(result(v[10], v[0], q, q.sizes(), at::kBFloat16, "out"));
+    const Workspace w = workspace(v[11], v[0], q, ST_OP_ATTN_WINDOW_STEP, 0, 0, 0, 0, 0);
+    const void *pq = q.data_ptr(), *pk = k.data_ptr(), *pv = vv.data_ptr();
+    void *pkp = kp.data_ptr(), *pvp = vp.data_ptr(), *po = data(out);
+    const int32_t *pt = (const int32_t *)tab.data_ptr(), *pl = (const int32_t *)lens.data_ptr();
+    call("st_attn_window_step", [&](void *s) { return api.attn_window_step(&c, pq, pk, pv, pkp, pvp, pt, pl, window, sinks, scale, po, w.ptr, w.bytes, s); });
+    return out.release();
+}
+
+const float *decay_of(const Qkv &x, PyObject *o)
+{
+    const at::Tensor &a = contiguous(x.q, o, at::kFloat, "log_decay");
+    want_shape(a, {x.t.heads}, "log_decay");
+    return (const float *)a.data_ptr();
+}
+const float *state_of(const Qkv &x, PyObject *o, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &s = contiguous(x.q, o, at::kFloat, name);
+    want_shape(s, {x.t.nseq, x.t.heads, x.t.d, x.t.dv}, name);
+    return (const float *)s.data_ptr();
+}
+
+PyObject *py_attn_decay(PyObject *const *v)              // q, k, v, log_decay, offsets, state, scale, out, state_out, ws
+{
+    Qkv x = qkv(v[0], v[1], v[2]);
+    const Guard guard(x.q.device());
+    st_tokens &t = x.t;
+    const float *a = decay_of(x, v[3]);
+    const int32_t *at = offsets_of(x.q, v[4], "offsets", &t.nseq);
+    const float *in = state_of(x, v[5], "state"), scale = scale_of(v[6], t.d);
+    Ref out(result(v[7], v[0], x.q, {t.nq, t.heads, t.dv}, at::kBFloat16, "out"));
+    Ref last(result(v[8], v[0], x.q, {t.nseq, t.heads, t.d, t.dv}, at::kFloat, "state_out"));
+    const Workspace w = workspace(v[9], v[0], x.q, ST_OP_ATTN_DECAY, t.nq, t.nseq, t.heads, std::max(t.d, t.dv), 0);
+    const void *q = x.q.data_ptr(), *k = x.k.data_ptr(), *vv = x.v.data_ptr();
+    void *po = data(out);
+    float *pl = (float *)data(last);
+    call("st_attn_decay", [&](void *s) { return api.attn_decay(&t, q, k, vv, a, at, in, scale, po, pl, w.ptr, w.bytes, s); });
+    return pair(std::move(out), std::move(last));
+}
+
+// q, k, v, log_decay, dout, offsets, state, dstate_out, scale, dq, dk, dv, dstate, ws
+PyObject *py_attn_decay_grad(PyObject *const *v)
+{
+    Qkv x = qkv(v[0], v[1], v[2]);
+    const Guard guard(x.q.device());
+    st_tokens &t = x.t;
+    const float *a = decay_of(x, v[3]);
+    const at::Tensor &dout = contiguous(x.q, v[4], at::kBFloat16, "dout");
+    want_shape(dout, {t.nq, t.heads, t.dv}, "dout");
+    const int32_t *at = offsets_of(x.q, v[5], "offsets", &t.nseq);
+    const float *in = state_of(x, v[6], "state"), *dlast = state_of(x, v[7], "dstate_out"), scale = scale_of(v[8], t.d);
+    Ref dq(result(v[9], v[0], x.q, {t.nq, t.heads, t.d}, at::kBFloat16, "dq"));
+    Ref dk(result(v[10], v[0], x.q, {t.nk, t.heads, t.d}, at::kBFloat16, "dk"));
+    Ref dv(result(v[11], v[0], x.q, {t.nk, t.heads, t.dv}, at::kBFloat16, "dv"));
+    const bool wanted = in || v[12] != Py_None;
+    Ref first(wanted ? result(v[12], v[0], x.q, {t.nseq, t.heads, t.d, t.dv}, at::kFloat, "dstate") : (Py_INCREF(Py_None), Py_None));
+    const Workspace w = workspace(v[13], v[0], x.q, ST_OP_ATTN_DECAY_GRAD, t.nq, t.nseq, t.heads, std::max(t.d, t.dv), 0);
+    const void *q = x.q.data_ptr(), *k = x.k.data_ptr(), *vv = x.v.data_ptr(), *pd = dout.data_ptr();
+    void *pq = data(dq), *pk = data(dk), *pv = data(dv);
+    float *pf = wanted ? (float *)data(first) : nullptr;
+    call("st_attn_decay_grad", [&](void *s) { return api.attn_decay_grad(&t, q, k, vv, a, pd, at, in, dlast, scale, pq, pk, pv, pf, w.ptr, w.bytes, s); });
+    return PyTuple_Pack(4, dq.o, dk.o, dv.o, first.o);
+}
+
+PyObject *py_attn_decay_step(PyObject *const *v)         // q, k, v, log_decay, state, scale, out
+{
+    Qkv x = qkv(v[0], v[1], v[2]);
+    const Guard guard(x.q.device());
+    st_tokens &t = x.t;
+    (void)device_ptr(x.q, "q");
+    (void)device_ptr(x.k, "k");
+    (void)device_ptr(x.v, "v");
+    const float *a = decay_of(x, v[3]), scale = scale_of(v[5], t.d);
+    t.nseq = t.nq;
+    if (v[4] == Py_None) fail(PyExc_TypeError, "state must be a tensor");
+    float *state = const_cast<float *>(state_of(x, v[4], "state"));
+    Ref out(result(v[6], v[0], x.q, {t.nq, t.heads, t.dv}, at::kBFloat16, "out"));
+    const void *q = x.q.data_ptr(), *k = x.k.data_ptr(), *vv = x.v.data_ptr();
+    void *po = data(out);
+    call("st_attn_decay_step", [&](void *s) { return api.attn_decay_step(&t, q, k, vv, a, state, scale, po, s); });
+    return out.release();
+}
+
 // Argument count, and C++ errors as Python ones.
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -525,7 +850,9 @@ PyObject *py_bind(PyObject *, PyObject *args)
         {"st_pack", &a.pack}, {"st_unpack", &a.unpack}, {"st_thp", &a.thp}, {"st_packed_axpby", &a.packed_axpby},
         {"st_packed_mul", &a.packed_mul}, {"st_sym_moment2", &a.sym_moment2}, {"st_sym_moment3", &a.sym_moment3},
         {"st_sym_moment4", &a.sym_moment4}, {"st_mttkrp_tri", &a.mttkrp_tri}, {"st_mttkrp_slice", &a.mttkrp_slice},
-        {"st_ttm_blockdiag", &a.ttm_blockdiag}, {"st_ttm_packed", &a.ttm_packed}};
+        {"st_ttm_blockdiag", &a.ttm_blockdiag}, {"st_ttm_packed", &a.ttm_packed}, {"st_attn_window", &a.attn_window},
+        {"st_attn_window_grad", &a.attn_window_grad}, {"st_attn_window_step", &a.attn_window_step}, {"st_attn_decay", &a.attn_decay},
+        {"st_attn_decay_grad", &a.attn_decay_grad}, {"st_attn_decay_step", &a.attn_decay_step}};
     for (const auto &w : want) {
         PyObject *v = PyDict_GetItemString(table, w.name);
         void *p = v ? PyLong_AsVoidPtr(v) : nullptr;
@@ -558,6 +885,8 @@ PyMethodDef methods[] = {
     {"set_allocator", py_set_allocator, METH_O, nullptr},
     ENTRY(pack, 3), ENTRY(unpack, 4), ENTRY(thp, 4), ENTRY(axpby, 5), ENTRY(mul, 3), ENTRY(moment2, 4), ENTRY(moment3, 4),
     ENTRY(moment4, 4), ENTRY(mttkrp_tri, 6), ENTRY(mttkrp_slice, 9), ENTRY(ttm_blockdiag, 7), ENTRY(ttm_packed, 6),
+    ENTRY(attn_window, 11), ENTRY(attn_window_grad, 15), ENTRY(attn_window_step, 12), ENTRY(attn_decay, 10), ENTRY(attn_decay_grad, 14),
+    ENTRY(attn_decay_step, 7),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,625 @@
+"""Attention over structured pairs on the GPU: every call against its definition in 64 bits (attn_reference.py, which derives the
+tolerances), sequence by sequence, at the sizes and masks where tiles, chunks and pages end."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import attn_reference as ref
+import paper_2211_10482_b200 as st
+from test_gpu_parity import GuardAllocator
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture(autouse=True)
+def guard_bands_and_device_status():
+    """Nothing writes outside its buffers, and the last call left no error in its workspace."""
+    guard = GuardAllocator()
+    st.set_allocator(guard)
+    yield
+    st.set_allocator(None)
+    guard.check()
+
+
+def ok():
+    assert st.st_check_status() == st.ST_OK
+
+
+def normal(seed, *shape):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(BF16)
+
+
+def floats(seed, *shape):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda")
+
+
+def offsets(lens, at=0):
+    return torch.tensor([at] + [at + sum(lens[: i + 1]) for i in range(len(lens))], dtype=torch.int32, device="cuda")
+
+
+def spans(lens, at=0):
+    return [(at + sum(lens[:i]), at + sum(lens[: i + 1])) for i in range(len(lens))]
+
+
+def near(got, want, tol, what):
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    got, finite = got.double(), torch.isfinite(want)
+    assert bool((torch.isfinite(got) == finite).all()), "%s: not finite in other places" % what
+    assert bool((got[~finite] == want[~finite]).all()), what
+    over = ((got - want).abs() / (tol + 1e-30))[finite]
+    assert not over.numel() or float(over.max()) <= 1.0, "%s: %.3g of the tolerance" % (what, float(over.max()))
+
+
+# ------------------------------------------------------------------------------------- window
+
+WINDOWS = [
+    # query lengths, key lengths, heads, key heads, d, window, sinks
+    ([1], [1], 1, 1, 8, 1, 0),
+    ([197], [197], 8, 8, 64, 64, 4),
+    ([1, 2, 127, 128, 129, 0, 255, 257], None, 4, 2, 64, 100, 4),
+    ([300, 0, 31], None, 3, 3, 128, 1, 0),
+    ([513], None, 8, 1, 128, 128, 130),
+    ([640, 5], None, 4, 4, 128, 129, 1),
+    ([384], None, 2, 2, 128, 1 << 40, 0),
+    ([700, 33], None, 6, 2, 80, 65, 16),
+    ([260, 130], None, 2, 1, 32, 1000, 2),
+    ([400], None, 2, 2, 96, 37, 300),
+    ([333], None, 2, 1, 128, 127, 1 << 35),
+    ([5, 1, 200, 70], [45, 778, 240, 70], 4, 2, 64, 50, 4),
+    ([1, 100, 129], [1000, 515, 1300], 4, 1, 128, 300, 130),
+    ([50, 300, 8, 260], [20, 150, 0, 260], 2, 2, 64, 40, 3),       # fewer keys than queries: the first rows see nothing
+    ([1500], [1500], 2, 2, 64, 600, 10),
+    ([17] * 40, None, 2, 2, 64, 8, 1),
+]
+
+
+def window_inputs(seed, lq, lk, H, Hk, d):
+    lk = lq if lk is None else lk
+    return lk, normal(seed, sum(lq), H, d), normal(seed + 1, sum(lk), Hk, d), normal(seed + 2, sum(lk), Hk, d), offsets(lq), offsets(lk)
+
+
+@pytest.mark.parametrize("lq,lk,H,Hk,d,window,sinks", WINDOWS)
+def test_window_against_the_definition(lq, lk, H, Hk, d, window, sinks):
+    lk, q, k, v, qo, ko = window_inputs(1, lq, lk, H, Hk, d)
+    out, lse = st.st_attn_window(q, k, v, window, sinks, qo, ko)
+    ok()
+    for (a, b), (c, e) in zip(spans(lq), spans(lk)):
+        o, l, ot, lt = ref.window(q[a:b], k[c:e], v[c:e], window, sinks)
+        near(out[a:b], o, ot, "out")
+        near(lse[a:b], l, lt, "lse")
+
+
+@pytest.mark.parametrize("lq,lk,H,Hk,d,window,sinks", WINDOWS)
+def test_window_gradient_against_the_definition(lq, lk, H, Hk, d, window, sinks):
+    lk, q, k, v, qo, ko = window_inputs(11, lq, lk, H, Hk, d)
+    dout = normal(14, *q.shape)
+    out, lse = st.st_attn_window(q, k, v, window, sinks, qo, ko)
+    got = st.st_attn_window_grad(q, k, v, out, lse, dout, window, sinks, qo, ko)
+    ok()
+    for (a, b), (c, e) in zip(spans(lq), spans(lk)):
+        want = ref.window_grad(q[a:b], k[c:e], v[c:e], out[a:b], dout[a:b], window, sinks)
+        for g, rows, (w, tol), name in zip(got, ((a, b), (c, e), (c, e)), want, ("dq", "dk", "dv")):
+            near(g[rows[0] : rows[1]], w, tol, name)
+
+
+def test_window_gradient_against_differences():
+    H, Hk, d, n, window, sinks = 2, 1, 16, 40, 9, 3
+    lk, q, k, v, qo, ko = window_inputs(21, [n], None, H, Hk, d)
+    dout = normal(24, n, H, d)
+    out, lse = st.st_attn_window(q, k, v, window, sinks)
+    grads = st.st_attn_window_grad(q, k, v, out, lse, dout, window, sinks)
+    tols = [t for _, t in ref.window_grad(q, k, v, out, dout, window, sinks)]
+    loss = lambda *x: float((ref.window(*x, window, sinks)[0] * dout.double()).sum())
+    base = [x.double() for x in (q, k, v)]
+    # delta comes from the rounded out: off by half a step of every value of out
+    delta_off = (dout.double().abs() * out.double().abs()).sum(-1).max() * ref.B
+    for i, (g, tol) in enumerate(zip(grads, tols)):
+        direction = floats(30 + i, *g.shape).double()
+        h = 1e-5
+        x0, x1 = list(base), list(base)
+        x0[i], x1[i] = base[i] - h * direction, base[i] + h * direction
+        slope = (loss(*x1) - loss(*x0)) / (2 * h)
+        # a row's ds moves by p delta_off scale in all: against |k| or |q| of the largest
+        slack = float((tol * direction.abs()).sum()) + float(delta_off) * d ** -0.5 * H * n * float(direction.abs().max()) * float(max(base[0].abs().max(), base[1].abs().max())) * d
+        assert abs(float((g.double() * direction).sum()) - slope) <= slack
+
+
+def test_window_takes_strided_slices_and_head_major_tables():
+    n, H, Hk, d = 300, 6, 2, 80
+    qkv = normal(41, n, H + 2 * Hk, d)
+    q, k, v = qkv.split([H, Hk, Hk], 1)
+    want = st.st_attn_window(q.contiguous(), k.contiguous(), v.contiguous(), 77, 5)
+    got = st.st_attn_window(q, k, v, 77, 5)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    hq, hk, hv = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v))
+    got = st.st_attn_window(hq, hk, hv, 77, 5)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    dout = normal(42, n, H, d)
+    a = st.st_attn_window_grad(q, k, v, *want, dout, 77, 5)
+    b = st.st_attn_window_grad(hq, hk, hv, *want, dout, 77, 5)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+    r = st.st_attn_window(q, k, v, 77, 5, out=out, lse=lse, scale=d ** -0.5)
+    assert r[0] is out and r[1] is lse and torch.equal(out, want[0])
+    ok()
+
+
+def test_window_other_scale():
+    q, k, v = (normal(50 + i, 200, 2, 64) for i in range(3))
+    scale = 0.5
+    out, lse = st.st_attn_window(q, k, v, 90, 2, scale=scale)
+    o, l, ot, lt = ref.window(q, k, v, 90, 2, scale)
+    # scores are scale sqrt(d) times larger than at the usual scale, and so are their errors
+    wide = scale * 8
+    near(out, o, ot * wide, "out")
+    near(lse, l, lt * wide, "lse")
+    dout = normal(54, 200, 2, 64)
+    for g, (w, tol) in zip(st.st_attn_window_grad(q, k, v, out, lse, dout, 90, 2, scale=scale), ref.window_grad(q, k, v, out, dout, 90, 2, scale)):
+        near(g, w, tol * wide, "gradient")
+    for scale in (0.0, -0.2, math.nan, math.inf):
+        with pytest.raises(st.StError) as e:
+            st.st_attn_window(q, k, v, 90, 2, scale=scale)
+        assert e.value.status == st.ST_ERR_UNSUPPORTED
+
+
+def test_large_scores_do_not_overflow():
+    q, k, v = normal(55, 300, 2, 64) * 30, normal(56, 300, 2, 64) * 30, normal(57, 300, 2, 64)
+    out, lse = st.st_attn_window(q, k, v, 100, 4)
+    o, l, ot, lt = ref.window(q, k, v, 100, 4)
+    # the scores reach some 5000: their fp32 errors, 64 products of up to 10^4 at 2^-24 each times scale, are up to 64*1e4*6e-8/8 = 5e-3
+    near(lse, l, lt + 5e-3, "lse")
+    assert bool(torch.isfinite(out).all())
+    see = ref.visible(300, 300, 100, 4, "cuda")
+    V = ref.heads_first(v)
+    p = torch.exp((ref.heads_first(q) @ ref.heads_first(k).transpose(1, 2) / 8).masked_fill(~see, -math.inf) - l.transpose(0, 1)[..., None])
+    near(out, o, ot + 1.1e-2 * (p @ V.abs()).transpose(0, 1), "out")
+
+
+def test_rows_of_no_sequence_are_neither_read_nor_written():
+    """Rows before, between and behind the sequences hold NaN; so do the other sequences, one at a time."""
+    lq, H, Hk, d = [70, 130, 200], 4, 2, 64
+    total = 30 + sum(lq) + 100
+    base = [normal(60 + i, total, h, d) for i, h in enumerate((H, Hk, Hk))]
+    dout = normal(64, total, H, d)
+    at = offsets(lq, 30)
+    sp = spans(lq, 30)
+    clean = st.st_attn_window(*base, 60, 3, at)
+    cleang = st.st_attn_window_grad(*base, *clean, dout, 60, 3, at)
+    for keep in range(3):
+        a, b = sp[keep]
+        live = torch.zeros(total, dtype=torch.bool, device="cuda")
+        live[a:b] = True
+        q, k, v, do = (torch.where(live[:, None, None], x, torch.full_like(x, math.nan)) for x in (*base, dout))
+        out, lse = torch.full_like(base[0], 7.0), torch.full((total, H), 7.0, device="cuda")
+        st.st_attn_window(q, k, v, 60, 3, at, out=out, lse=lse)
+        assert torch.equal(out[a:b], clean[0][a:b]) and torch.equal(lse[a:b], clean[1][a:b])
+        inside = torch.zeros_like(live)
+        inside[sp[0][0] : sp[-1][1]] = True
+        assert bool((out[~inside] == 7.0).all()) and bool((lse[~inside] == 7.0).all())
+        grads = [torch.full_like(x, 7.0) for x in base]
+        st.st_attn_window_grad(q, k, v, out, lse, do, 60, 3, at, dq=grads[0], dk=grads[1], dv=grads[2])
+        for g, c in zip(grads, cleang):
+            assert torch.equal(g[a:b], c[a:b])
+            assert bool((g[~inside] == 7.0).all())
+    ok()
+
+
+@pytest.mark.parametrize("bad", [[0, 50, 40, 100], [0, 50, 60, 101], [-1, 50, 60, 100], [0, 1 << 30, 5, 100]])
+def test_bad_offsets_are_reported_and_touch_nothing_outside(bad):
+    q, k, v = (normal(70 + i, 100, 2, 64) for i in range(3))
+    at = torch.tensor(bad, dtype=torch.int32, device="cuda")
+    good = offsets([50, 10, 40])
+    out, lse = st.st_attn_window(q, k, v, 20, 2, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_window(q, k, v, 20, 2, good, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_window_grad(q, k, v, q, torch.zeros(100, 2, device="cuda"), q, 20, 2, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    a = -torch.ones(2, device="cuda")
+    st.st_attn_decay(q, k, v, a, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_decay_grad(q, k, v, a, q, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_window(q, k, v, 20, 2, good)
+    ok()
+
+
+# --------------------------------------------------------------------------------- window: step
+
+STEPS = [
+    # lengths with the new token, heads, key heads, d, page, window, sinks
+    ([1], 1, 1, 8, 1, 1, 0),
+    ([1, 2, 16, 17, 33, 0], 4, 2, 64, 16, 10, 0),
+    ([300, 1, 77], 8, 8, 128, 64, 1 << 33, 0),
+    ([1000, 999, 31, 128], 8, 2, 128, 100, 250, 4),
+    ([4000], 8, 1, 128, 7, 3000, 130),
+    ([2500, 65], 32, 2, 80, 256, 700, 16),
+    ([513] * 5, 6, 3, 96, 64, 64, 1000),
+    ([20000], 4, 4, 32, 1000, 16000, 1),
+    ([129, 5], 20, 1, 64, 32, 128, 2),
+]
+
+
+def cache_of(seed, lens, Hk, d, page, spare=2):
+    used = [-(-n // page) for n in lens]
+    pages = sum(used) + spare
+    g = torch.Generator().manual_seed(seed)
+    order = torch.randperm(pages, generator=g).to(torch.int32)
+    table = torch.full((len(lens), max(1, max(used))), -1, dtype=torch.int32)
+    for b, u in enumerate(used):
+        table[b, :u] = order[sum(used[:b]) : sum(used[:b]) + u]
+    return normal(seed, pages, page, Hk, d), normal(seed + 1, pages, page, Hk, d), table.cuda()
+
+
+def gathered(pages, table, b, n):
+    page = pages.shape[1]
+    i = torch.arange(n, device="cuda")
+    return pages[table[b, i // page].long(), i % page]
+
+
+@pytest.mark.parametrize("lens,H,Hk,d,page,window,sinks", STEPS)
+def test_window_step_against_the_definition(lens, H, Hk, d, page, window, sinks):
+    kp, vp, table = cache_of(80, lens, Hk, d, page)
+    q, k, v = normal(82, len(lens), H, d), normal(83, len(lens), Hk, d), normal(84, len(lens), Hk, d)
+    # what lies behind a sequence's length, and pages of nobody, may hold anything
+    live = torch.zeros(kp.shape[:2], dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens):
+        i = torch.arange(max(0, n - 1), device="cuda")
+        live[table[b, i // page].long(), i % page] = True
+    kp, vp = (torch.where(live[..., None, None], x, torch.full_like(x, math.nan)) for x in (kp, vp))
+    before = kp.clone(), vp.clone()
+    out = st.st_attn_window_step(q, k, v, kp, vp, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), window, sinks)
+    ok()
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert bool((out[b] == 0).all())
+            continue
+        K, V = gathered(kp, table, b, n), gathered(vp, table, b, n)
+        assert torch.equal(K[-1], k[b]) and torch.equal(V[-1], v[b])
+        o, _, ot, _ = ref.window(q[b : b + 1], K, V, window, sinks)
+        near(out[b : b + 1], o, ot, "out")
+        last = table[b, (n - 1) // page].long(), (n - 1) % page
+        before[0][last], before[1][last] = k[b], v[b]
+    # nothing else in the cache moved
+    for x, y in zip((kp, vp), before):
+        assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+
+
+def test_step_takes_interleaved_and_head_major_caches():
+    lens, H, Hk, d, page = [200, 90], 4, 2, 64, 32
+    kp, vp, table = cache_of(90, lens, Hk, d, page)
+    q, k, v = normal(92, 2, H, d), normal(93, 2, Hk, d), normal(94, 2, Hk, d)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want = st.st_attn_window_step(q, k, v, kp.clone(), vp.clone(), table, n, 100, 4)
+    both = torch.stack([kp, vp], 1)                                    # [pages, 2, page, Hk, d]
+    assert torch.equal(st.st_attn_window_step(q, k, v, both[:, 0], both[:, 1], table, n, 100, 4), want)
+    major = torch.stack([kp.transpose(1, 2), vp.transpose(1, 2)], 1)   # [pages, 2, Hk, page, d]
+    assert torch.equal(st.st_attn_window_step(q, k, v, major[:, 0].transpose(1, 2), major[:, 1].transpose(1, 2), table, n, 100, 4), want)
+    assert torch.equal(gathered(major[:, 1].transpose(1, 2), table, 0, 200)[-1], v[0])
+    ok()
+
+
+def test_step_leaves_out_bad_pages_and_reports_them():
+    lens, H, Hk, d, page = [100, 64], 4, 2, 64, 16
+    kp, vp, table = cache_of(95, lens, Hk, d, page)
+    q, k, v = normal(97, 2, H, d), normal(98, 2, Hk, d), normal(99, 2, Hk, d)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    want = st.st_attn_window_step(q, k, v, kp, vp, table, n, 1000, 0)
+    ok()
+    for wrong in (-1, kp.shape[0], 1 << 30):
+        bad = table.clone()
+        bad[0, 2] = wrong
+        out = st.st_attn_window_step(q, k, v, kp, vp, bad, n, 1000, 0)
+        assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+        assert torch.equal(out[1], want[1])
+        keep = torch.cat([torch.arange(32), torch.arange(48, 100)]).cuda()
+        o, _, ot, _ = ref.window(q[:1], gathered(kp, table, 0, 100)[keep], gathered(vp, table, 0, 100)[keep], 1000, 0)
+        near(out[:1], o, ot, "out")
+    long = torch.tensor([100, 7 * 16 + 1], dtype=torch.int32, device="cuda")
+    st.st_attn_window_step(q, k, v, kp, vp, table.clamp(min=0), long, 1000, 0)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_window_step(q, k, v, kp, vp, table, torch.tensor([100, -5], dtype=torch.int32, device="cuda"), 1000, 0)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_window_step(q, k, v, kp, vp, table, n, 1000, 0)
+    ok()
+
+
+def test_step_on_a_cache_whose_offsets_pass_32_bits():
+    page, Hk, d = 64, 8, 128
+    pages = (1 << 31) // (page * Hk * d) + 40                          # elements: beyond 2^31
+    kp, vp = torch.zeros(pages, page, Hk, d, dtype=BF16, device="cuda"), torch.zeros(pages, page, Hk, d, dtype=BF16, device="cuda")
+    last = torch.arange(pages - 3, pages, device="cuda")
+    kp[last], vp[last] = normal(100, 3, page, Hk, d), normal(101, 3, page, Hk, d)
+    table = last.to(torch.int32)[None]
+    q, k, v = normal(102, 1, 8, d), normal(103, 1, Hk, d), normal(104, 1, Hk, d)
+    out = st.st_attn_window_step(q, k, v, kp, vp, table, torch.tensor([190], dtype=torch.int32, device="cuda"), 150, 4)
+    o, _, ot, _ = ref.window(q, gathered(kp, table, 0, 190), gathered(vp, table, 0, 190), 150, 4)
+    near(out, o, ot, "out")
+    ok()
+
+
+# -------------------------------------------------------------------------------------- decay
+
+DECAYS = [
+    # lengths, heads, d, dv, log decays, state
+    ([1], 1, 8, 8, [-0.1], True),
+    ([1, 2, 127, 128, 129, 0, 255, 257], 2, 64, 64, [-0.5, -0.004], True),
+    ([700], 3, 128, 128, [-0.02, 0.0, -3.0], False),
+    ([700, 0, 31], 2, 128, 128, [-0.02, -0.3], True),
+    ([300, 77], 2, 80, 32, [-0.1, -0.001], True),
+    ([130], 2, 32, 96, [-math.inf, -20.0], True),
+    ([1100], 1, 64, 128, [-0.003], True),
+    ([1100], 1, 128, 40, [-0.003], False),
+    ([16] * 30, 2, 64, 64, [-0.05, -0.7], True),
+    ([6000], 1, 128, 128, [-0.0005], True),
+]
+
+
+def decay_inputs(seed, lens, H, d, dv, a, state):
+    n = sum(lens)
+    s = floats(seed + 3, len(lens), H, d, dv) if state else None
+    return normal(seed, n, H, d), normal(seed + 1, n, H, d), normal(seed + 2, n, H, dv), torch.tensor(a, device="cuda"), s, offsets(lens)
+
+
+def one(x, b):
+    return None if x is None else x[b]
+
+
+@pytest.mark.parametrize("lens,H,d,dv,a,state", DECAYS)
+def test_decay_against_the_definition(lens, H, d, dv, a, state):
+    q, k, v, a, s, at = decay_inputs(110, lens, H, d, dv, a, state)
+    out, last = st.st_attn_decay(q, k, v, a, at, s)
+    ok()
+    for b, (x, y) in enumerate(spans(lens)):
+        o, l, ot, lt = ref.decay(q[x:y], k[x:y], v[x:y], a, one(s, b))
+        near(out[x:y], o, ot, "out")
+        near(last[b], l, lt, "state")
+
+
+@pytest.mark.parametrize("lens,H,d,dv,a,state", DECAYS)
+def test_decay_gradient_against_the_definition(lens, H, d, dv, a, state):
+    q, k, v, a, s, at = decay_inputs(120, lens, H, d, dv, a, state)
+    dout = normal(124, *v.shape)
+    dlast = floats(125, len(lens), H, d, dv) if state else None
+    got = st.st_attn_decay_grad(q, k, v, a, dout, at, s, dlast)
+    ok()
+    assert (got[3] is None) == (not state)
+    for b, (x, y) in enumerate(spans(lens)):
+        want = ref.decay_grad(q[x:y], k[x:y], v[x:y], a, dout[x:y], one(s, b), one(dlast, b))
+        for g, (w, tol), name in zip(got, want, ("dq", "dk", "dv")):
+            near(g[x:y], w, tol, name)
+        if state:
+            near(got[3][b], *want[3], "dstate")
+
+
+def test_decay_gradient_against_differences():
+    q, k, v, a, s, at = decay_inputs(130, [50], 2, 16, 24, [-0.2, -0.01], True)
+    dout, dlast = normal(134, *v.shape), floats(135, 1, 2, 16, 24)
+    got = st.st_attn_decay_grad(q, k, v, a, dout, None, s, dlast)
+    want = ref.decay_grad(q, k, v, a, dout, s[0], dlast[0])
+
+    def loss(q, k, v, s):
+        out, last, _, _ = ref.decay(q, k, v, a, s[0])
+        return float((out * dout.double()).sum() + (last * dlast[0].double()).sum())
+
+    base = [x.double() for x in (q, k, v, s)]
+    for i, g in enumerate(got):
+        direction = floats(140 + i, *g.shape).double()
+        x0, x1 = list(base), list(base)
+        x0[i], x1[i] = base[i] - 1e-4 * direction, base[i] + 1e-4 * direction
+        slope = (loss(*x1) - loss(*x0)) / 2e-4
+        tol = want[i][1] if i < 3 else want[i][1][None]
+        # the differences themselves: sums of some 10^5 terms of a few units in 64 bits over 2e-4
+        assert abs(float((g.double() * direction).sum()) - slope) <= float((tol * direction.abs()).sum()) + 1e-5
+
+
+def test_decay_takes_strided_tables_and_results_that_the_caller_has():
+    n, H, d = 300, 2, 64
+    qkv = normal(150, n, 3 * H, d)
+    q, k, v = qkv.split(H, 1)
+    a = torch.tensor([-0.1, -0.01], device="cuda")
+    want = st.st_attn_decay(q.contiguous(), k.contiguous(), v.contiguous(), a)
+    out, last = torch.empty_like(want[0]), torch.empty_like(want[1])
+    got = st.st_attn_decay(q, k, v, a, out=out, state_out=last, scale=d ** -0.5)
+    assert got[0] is out and got[1] is last and torch.equal(out, want[0]) and torch.equal(last, want[1])
+    hq, hk, hv = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v))
+    assert torch.equal(st.st_attn_decay(hq, hk, hv, a)[0], out)
+    dout = normal(151, n, H, d)
+    x, y = st.st_attn_decay_grad(q, k, v, a, dout), st.st_attn_decay_grad(hq, hk, hv, a, dout)
+    assert all(torch.equal(i, j) for i, j in zip(x[:3], y[:3]))
+    # the last state may replace the first
+    s = floats(152, 1, H, d, d)
+    w = st.st_attn_decay(q, k, v, a, None, s.clone())
+    got = st.st_attn_decay(q, k, v, a, None, s, state_out=s)
+    assert got[1] is s and torch.equal(s, w[1]) and torch.equal(got[0], w[0])
+    ok()
+
+
+def test_decay_rows_of_no_sequence_are_neither_read_nor_written():
+    lens, H, d = [70, 130, 200], 2, 64
+    total = 30 + sum(lens) + 100
+    base = [normal(160 + i, total, H, d) for i in range(4)]
+    a, at, sp = torch.tensor([-0.1, -0.01], device="cuda"), offsets(lens, 30), spans(lens, 30)
+    clean, last = st.st_attn_decay(*base[:3], a, at)
+    cleang = st.st_attn_decay_grad(*base[:3], a, base[3], at)
+    for keep in range(3):
+        x, y = sp[keep]
+        live = torch.zeros(total, dtype=torch.bool, device="cuda")
+        live[x:y] = True
+        q, k, v, do = (torch.where(live[:, None, None], t, torch.full_like(t, math.nan)) for t in base)
+        out = torch.full_like(base[0], 7.0)
+        _, l = st.st_attn_decay(q, k, v, a, at, out=out)
+        inside = torch.zeros_like(live)
+        inside[sp[0][0] : sp[-1][1]] = True
+        assert torch.equal(out[x:y], clean[x:y]) and torch.equal(l[keep], last[keep]) and bool((out[~inside] == 7.0).all())
+        grads = [torch.full_like(base[0], 7.0) for _ in range(3)]
+        st.st_attn_decay_grad(q, k, v, a, do, at, dq=grads[0], dk=grads[1], dv=grads[2])
+        for g, c in zip(grads, cleang):
+            assert torch.equal(g[x:y], c[x:y]) and bool((g[~inside] == 7.0).all())
+    ok()
+
+
+@pytest.mark.parametrize("n,H,d,dv", [(1, 1, 8, 8), (3, 2, 64, 64), (70, 4, 128, 128), (5, 3, 80, 40), (300, 2, 32, 128)])
+def test_decay_step_against_the_definition(n, H, d, dv):
+    q, k, v, s = normal(170, n, H, d), normal(171, n, H, d), normal(172, n, H, dv), floats(173, n, H, d, dv)
+    a = torch.linspace(-2.0, -0.001, H, device="cuda")
+    state = s.clone()
+    out = st.st_attn_decay_step(q, k, v, a, state)
+    kept = s.double() * torch.exp(a.double()).view(-1, 1, 1)
+    want = kept + k.double()[..., None] * v.double()[:, :, None]
+    # two products and a sum in fp32, the decay's exponential within a few steps of it
+    near(state, want, 2.0 ** -20 * (kept.abs() + (k.double()[..., None] * v.double()[:, :, None]).abs()), "state")
+    o = torch.einsum("nhd,nhde->nhe", q.double(), want) * d ** -0.5
+    near(out, o, ref.B * o.abs() + ref.F * torch.einsum("nhd,nhde->nhe", q.double().abs(), want.abs()) * d ** -0.5, "out")
+
+
+# --------------------------------------------------------------------------- used together, and otherwise
+
+def test_a_prompt_and_its_steps_are_the_whole_sequence():
+    """Two layers, one of each kind: a prompt of 150 tokens, then 20 single steps, against one pass over all 170."""
+    n, p, H, Hk, d, window, sinks, page = 170, 150, 4, 2, 64, 48, 3, 16
+    q, k, v = normal(180, n, H, d), normal(181, n, Hk, d), normal(182, n, Hk, d)
+    whole, _ = st.st_attn_window(q, k, v, window, sinks)
+    kp, vp = torch.full((12, page, Hk, d), math.nan, dtype=BF16, device="cuda"), torch.full((12, page, Hk, d), math.nan, dtype=BF16, device="cuda")
+    table = torch.tensor([[7, 2, 9, 0, 4, 11, 1, 3, 10, 5, 8]], dtype=torch.int32, device="cuda")
+    i = torch.arange(p, device="cuda")
+    kp[table[0, i // page].long(), i % page], vp[table[0, i // page].long(), i % page] = k[:p], v[:p]
+    rows = [st.st_attn_window(q[:p], k[:p], v[:p], window, sinks)[0]]
+    for t in range(p, n):
+        rows.append(st.st_attn_window_step(q[t : t + 1], k[t : t + 1], v[t : t + 1], kp, vp, table, torch.tensor([t + 1], dtype=torch.int32, device="cuda"), window, sinks))
+    want, _, tol, _ = ref.window(q, k, v, window, sinks)
+    near(torch.cat(rows), want, tol, "window")
+    near(whole, want, tol, "window")
+    a = torch.tensor([-0.3, -0.05, -0.01, 0.0], device="cuda")
+    k4, v4 = whole, q
+    whole2, last = st.st_attn_decay(q, k4, v4, a)
+    out, state = st.st_attn_decay(q[:p], k4[:p], v4[:p], a)
+    rows = [out]
+    for t in range(p, n):
+        rows.append(st.st_attn_decay_step(q[t : t + 1], k4[t : t + 1], v4[t : t + 1], a, state))
+    want, wl, tol, lt = ref.decay(q, k4, v4, a, None)
+    near(torch.cat(rows), want, tol, "decay")
+    near(whole2, want, tol, "decay")
+    near(state[0], wl, 2 * lt, "state")
+    near(last[0], wl, lt, "state")
+    ok()
+
+
+def everything(seed, H=2, d=64, lens=(150, 40, 300)):
+    """One call of each kind, as a list of (inputs to overwrite, function)."""
+    lens = list(lens)
+    n = sum(lens)
+    q, k, v, do = (normal(seed + i, n, H, d) for i in range(4))
+    a, at = -torch.rand(H, device="cuda"), offsets(lens)
+    kp, vp, table = cache_of(seed + 5, lens, H, d, 16)
+    ns = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q1, k1, v1 = (normal(seed + 7 + i, len(lens), H, d) for i in range(3))
+    s = floats(seed + 11, len(lens), H, d, d)
+
+    def run():
+        out, lse = st.st_attn_window(q, k, v, 60, 4, at)
+        g = st.st_attn_window_grad(q, k, v, out, lse, do, 60, 4, at)
+        o1 = st.st_attn_window_step(q1, k1, v1, kp, vp, table, ns, 100, 4)
+        o2, last = st.st_attn_decay(q, k, v, a, at, s)
+        g2 = st.st_attn_decay_grad(q, k, v, a, do, at, s, last)
+        s1 = s.clone()
+        o3 = st.st_attn_decay_step(q1, k1, v1, a, s1)
+        return [out, lse, *g, o1, o2, last, *g2, o3, s1]
+    return (q, k, v, do, a, q1, k1, v1, s), at, run
+
+
+def test_the_same_bits_twenty_times():
+    _, _, run = everything(200)
+    first = [x.clone() for x in run()]
+    for _ in range(20):
+        assert all(torch.equal(x, y) for x, y in zip(run(), first))
+    ok()
+
+
+def test_captured_graphs_replay_with_new_inputs_and_offsets():
+    """Two graphs, each with its own workspaces, replayed in turn; an eager call between them."""
+    st.set_allocator(None)
+    made = []
+    side = torch.cuda.Stream()
+    for seed in (210, 230):
+        inputs, at, run = everything(seed)
+        with torch.cuda.stream(side):
+            run()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            results = run()
+        made.append((inputs, at, run, graph, results))
+    for step, lens in enumerate(([150, 40, 300], [1, 488, 1], [200, 0, 290])):
+        for inputs, at, run, graph, results in made:
+            for x in inputs:
+                x.mul_(0.75 if step == 1 else 1.0)
+            at.copy_(offsets(lens))
+            want = [x.clone() for x in run()]
+            for r in results:
+                r.fill_(3.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(results, want))
+
+
+def test_calls_on_two_streams_at_once():
+    st.set_allocator(None)
+    runs = [everything(seed, lens=(700, 20, 900))[2] for seed in (250, 270)]
+    want = [[x.clone() for x in run()] for run in runs]
+    streams = [torch.cuda.Stream() for _ in runs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, (run, s) in enumerate(zip(runs, streams)):
+            with torch.cuda.stream(s):
+                got[i].append(run())
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for r in g:
+            assert all(torch.equal(x, y) for x, y in zip(r, w))
+
+
+def test_wrong_tensors_are_refused():
+    q, k = normal(290, 10, 4, 64), normal(291, 10, 2, 64)
+    a, at = torch.zeros(4, device="cuda"), offsets([4, 6])
+    with pytest.raises(TypeError, match="k must be bfloat16"):
+        st.st_attn_window(q, k.float(), k, 4)
+    with pytest.raises(ValueError, match="shape mismatch"):
+        st.st_attn_window(q, k, k[:9], 4)
+    with pytest.raises(ValueError, match="last dimension of q"):
+        st.st_attn_window(q.transpose(1, 2), k, k, 4)
+    with pytest.raises(ValueError, match="k_offsets are needed"):
+        st.st_attn_window(q, k[:9], k[:9], 4, 0, at)
+    with pytest.raises(ValueError, match="same length"):
+        st.st_attn_window(q, k, k, 4, 0, at, offsets([10]))
+    with pytest.raises(TypeError, match="q_offsets must be int32"):
+        st.st_attn_window(q, k, k, 4, 0, at.long())
+    with pytest.raises(ValueError, match="out has the wrong shape"):
+        st.st_attn_window(q, k, k, 4, out=q[:5].clone())
+    with pytest.raises(st.StError) as e:
+        st.st_attn_window(q, k, k, 0)
+    assert e.value.status == st.ST_ERR_SHAPE
+    with pytest.raises(st.StError) as e:
+        st.st_attn_window(q[:0], k, k, 3)
+    assert e.value.status == st.ST_ERR_SHAPE
+    with pytest.raises(st.StError) as e:
+        st.st_attn_decay(q, k, k, a)
+    assert e.value.status == st.ST_ERR_SHAPE
+    with pytest.raises(ValueError, match="state has the wrong shape"):
+        st.st_attn_decay(q, q, q, a, at, torch.zeros(1, 4, 64, 64, device="cuda"))
+    with pytest.raises(ValueError, match="dout has the wrong shape"):
+        st.st_attn_decay_grad(q, q, q, a, q[:4], at)
+    with pytest.raises(ValueError, match="k must be contiguous"):
+        st.st_attn_decay_step(q, torch.cat([q, q], 2)[..., :64], q, a, torch.zeros(10, 4, 64, 64, device="cuda"))
+    with pytest.raises(ValueError, match="same strides"):
+        kp = normal(292, 3, 8, 2, 64)
+        st.st_attn_window_step(q, k, k, kp, kp.transpose(1, 2).contiguous().transpose(1, 2), torch.zeros(10, 1, dtype=torch.int32, device="cuda"),
+                               torch.ones(10, dtype=torch.int32, device="cuda"), 4)
