@@ -1,0 +1,156 @@
+// Building blocks of the tensor-core attention kernels: tiles of 128 tokens in shared memory and tensor memory, and which
+// tiles of keys a tile of queries sees.
+#pragma once
+#include "attn_common.cuh"
+#include "tc_common.cuh"
+
+namespace st {
+namespace attn {
+
+constexpr int TILE = 128;                     // tokens of a tile
+constexpr int SLAB = TILE * 128;              // bytes of 64 columns of a tile: rows of 128 bytes, 128-byte swizzle
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// A table as a tensor map {column, head, row}, boxes of 64 columns x 1 head x `rows` rows; what lies outside reads as zero.
+inline bool make_tmap_table(CUtensorMap *m, const Table &t, int64_t rows, int64_t heads, int64_t cols, uint32_t box_rows = TILE)
+{
+    const tc::EncodeTiledFn fn = tc::encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)heads, (cuuint64_t)rows};
+    cuuint64_t strides[2] = {(cuuint64_t)t.head * 2, (cuuint64_t)t.row * 2};
+    cuuint32_t box[3] = {64, 1, box_rows}, estr[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<bf16 *>(t.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+#if defined(__CUDACC__)
+
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *m, uint64_t *bar, int x, int y, int z)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
+// 128 rows from `row` of one head, COLS columns, as slabs of 64 columns; the copy's bytes are counted on `bar`.
+template <int COLS>
+__device__ __forceinline__ void load_tile(unsigned char *dst, const CUtensorMap *m, uint64_t *bar, int head, int row)
+{
+#pragma unroll
+    for (int c = 0; c < COLS / 64; ++c) tma_load_3d(dst + c * SLAB, m, bar, c * 64, head, row);
+}
+
+// The A operand from tensor memory: 128 lanes, two bf16 of consecutive k to a column.
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// D[128, N] = A B^T over COLS columns of two K-major tiles (rows of A are lanes of D, rows of B are columns of D).
+template <int COLS>
+__device__ __forceinline__ void mma_rows(uint32_t d_tmem, const unsigned char *A, const unsigned char *B, uint32_t idesc, bool add = false)
+{
+    const uint64_t a = tc::make_smem_desc(tc::smem_u32(A), 16, 1024), b = tc::make_smem_desc(tc::smem_u32(B), 16, 1024);
+#pragma unroll
+    for (int k = 0; k < COLS / 16; ++k) {
+        const uint64_t off = (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4);
+        tc::mma_bf16(d_tmem, a + off, b + off, idesc, add || k > 0 ? 1u : 0u);
+    }
+}
+
+// D[128, N] (+)= A B over the 128 tokens of a tile: A[128, 128 tokens] bf16 in tensor memory, B a tile whose rows are the tokens.
+__device__ __forceinline__ void mma_tokens(uint32_t d_tmem, uint32_t a_tmem, const unsigned char *B, uint32_t idesc, bool add)
+{
+    const uint64_t b = tc::make_smem_desc(tc::smem_u32(B), SLAB, 1024);
+#pragma unroll
+    for (int k = 0; k < TILE / 16; ++k) mma_bf16_ts(d_tmem, a_tmem + k * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0 ? 1u : 0u);
+}
+
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+          "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Tile number `index` of the tiles of ROWS tokens that the sequences are cut into, by a whole warp.  seq = -1: there is none.
+struct TileOf {
+    int seq, tile;
+};
+template <int ROWS>
+__device__ __forceinline__ TileOf tile_of(const int *offsets, int nseq, int n, int index, int lane)
+{
+    if (!offsets) return {index < (n + ROWS - 1) / ROWS ? 0 : -1, index};
+    for (int b0 = 0; b0 < nseq; b0 += 32) {
+        const int b = b0 + lane;
+        const int mine = b < nseq ? (rows_of(offsets, b, n).len + ROWS - 1) / ROWS : 0;
+        int sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += x;
+        }
+        const unsigned behind = __ballot_sync(~0u, index < sum);
+        if (behind) {
+            const int l = __ffs(behind) - 1;
+            return {b0 + l, index - __shfl_sync(~0u, sum - mine, l)};
+        }
+        index -= __shfl_sync(~0u, sum, 31);
+    }
+    return {-1, 0};
+}
+// A table of n rows in nseq sequences has at most this many tiles.
+#endif
+inline int64_t most_tiles(int64_t n, int64_t nseq, int64_t rows) { return n / rows + nseq; }
+#if defined(__CUDACC__)
+
+// Which pairs of positions the window and the first columns leave.
+struct Mask {
+    int window, sinks;
+    __device__ __forceinline__ bool sees(int t, int s) const { return s <= t && (s > t - window || s < sinks); }
+    // whether any of the queries t0..t1 sees any of the keys s0..s1, or each of them every one
+    __device__ __forceinline__ bool any(int t0, int t1, int s0, int s1) const { return s0 <= t1 && (s1 > t0 - window || s0 < sinks) && t1 >= t0; }
+    __device__ __forceinline__ bool all(int t0, int t1, int s0, int s1) const { return s1 <= t0 && (s0 > t1 - window || s1 < sinks); }
+};
+
+// Rows [valid, 128) of a tile in shared memory, whatever they are, become zero; by a whole warp, before the tensor cores read the tile.
+template <int COLS>
+__device__ __forceinline__ void clear_rows(unsigned char *tile, int valid, int lane)
+{
+#pragma unroll
+    for (int c = 0; c < COLS / 64; ++c)
+        for (int i = valid * 8 + lane; i < TILE * 8; i += 32) *reinterpret_cast<uint4 *>(tile + c * SLAB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    tc::fence_proxy_async();
+    __syncwarp();
+}
+
+#endif
+
+}  // namespace attn
+}  // namespace st

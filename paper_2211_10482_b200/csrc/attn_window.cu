@@ -1,296 +1,350 @@
-// st_attn_window: one warp per (query, head), the formula as it stands.
-#include "attn_common.cuh"
+// st_attn_window: softmax attention over a causal band and the first columns, on the tensor cores.
+//
+// A block owns 256 queries of one head as two tiles of 128.  For every tile of 128 keys that a tile of queries sees
+//     S = Q K^T  (tcgen05, fp32 in tensor memory);   P = exp2(c S - c m)  (one thread per query row);   O += P V
+// with c = scale log2 e and m a running row maximum.  P goes back to tensor memory as bf16, over S, and is the A operand of the
+// second product; O stays in tensor memory.  While one tile's rows are in the exponential, the tensor cores work for the
+// other.  m moves only when a row's maximum has grown by more than 8 / c: any m gives the same quotient O / l, and P up to 2^8
+// loses nothing in bf16 or fp32, so that O is read and rescaled for the first tiles only.  P is rounded to bf16 once,
+// for the tensor cores; the row sum l is taken from the fp32 values.
+//
+// Only tiles with a visible pair are loaded and multiplied (the sinks' tiles, then the band's), and only tiles that the mask
+// cuts are masked.  Values behind a sequence's last key may be anything: their weight is 0, and their rows of V are
+// cleared in shared memory, as 0 times NaN would be NaN.
+//
+// Warps: 0..3 and 4..7 one row per thread of the first and second tile of queries, 8 copies (TMA), 9 issues the products.
+#include "attn_window.cuh"
 
 namespace st {
 namespace attn {
 
-struct WindowArgs {
-    Table q, k, v;
-    const int *q_offsets, *k_offsets;
-    int nseq, nq, nk, group, d, window, sinks;
-    float scale;
-    bf16 *out;
-    float *lse;
-    unsigned *status;
-    int heads;
+namespace wfwd {
+constexpr int THREADS = 320;
+constexpr int STAGES = 2;
+template <int DP> struct Shape {
+    static constexpr int TILE_BYTES = DP / 64 * SLAB;
+    static constexpr size_t SMEM = 1024 + (size_t)TILE_BYTES * (2 + 2 * STAGES) + 256;
 };
+}  // namespace wfwd
 
-__device__ __forceinline__ int sequence_of(const int *offsets, int nseq, int row, int n)
+// The tiles of keys that the queries at positions t0..t1 see: [0, first) with the sinks and [lo, hi).
+struct KeyTiles {
+    int first, lo, hi;
+    __device__ __forceinline__ int count() const { return first + max(0, hi - lo); }
+    __device__ __forceinline__ int at(int i) const { return i < first ? i : lo + i - first; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const Mask &m, int t0, int t1)
 {
-    if (!offsets) return row < n ? 0 : -1;
-    for (int b = 0; b < nseq; ++b) {
-        const Rows r = rows_of(offsets, b, n);
-        if (row >= r.first && row < r.first + r.len) return b;
-    }
-    return -1;
+    KeyTiles k;
+    k.hi = t1 < 0 ? 0 : t1 / TILE + 1;
+    k.lo = min(max(0, t0 - m.window + 1) / TILE, k.hi);
+    k.first = min((min(m.sinks, 1 << 29) + TILE - 1) / TILE, k.lo);
+    return k;
 }
 
-__device__ __forceinline__ float dot(const bf16 *a, const bf16 *b, int d)
+template <int DP>
+__global__ void __launch_bounds__(wfwd::THREADS, 1)
+window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+              const WindowArgs a)
 {
-    float s = 0.f;
-    for (int i = 0; i < d; ++i) s += __bfloat162float(a[i]) * __bfloat162float(b[i]);
-    return s;
-}
+    using namespace wfwd;
+    using namespace tc;
+    using S = Shape<DP>;
+    extern __shared__ unsigned char raw[];
+    unsigned char *smem = align_smem(raw);
+    unsigned char *Q = smem, *K = Q + 2 * S::TILE_BYTES, *V = K + STAGES * S::TILE_BYTES;
+    uint64_t *bars = (uint64_t *)(V + STAGES * S::TILE_BYTES);
+    uint64_t *q_full = bars, *k_full = bars + 2, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES,
+             *v_copied = v_empty + STAGES, *s_full = v_copied + STAGES, *p_full = s_full + 2, *o_full = p_full + 2;
+    uint32_t *tmem_slot = (uint32_t *)(o_full + 2);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
 
-__global__ void window_kernel(const WindowArgs a)
-{
     pdl_wait();
-    pdl_trigger();
     if (blockIdx.x == 0 && blockIdx.y == 0) {
-        const bool fine = offsets_fine(a.q_offsets, a.nseq, a.nq, threadIdx.x, blockDim.x) && offsets_fine(a.k_offsets, a.nseq, a.nk, threadIdx.x, blockDim.x);
+        const bool fine = offsets_fine(a.q_offsets, a.nseq, a.nq, threadIdx.x, THREADS) && offsets_fine(a.k_offsets, a.nseq, a.nk, threadIdx.x, THREADS);
         const int all = __syncthreads_and(fine);
         if (threadIdx.x == 0) {
             a.status[kWsStatusWord] = all ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
             a.status[kWsDetailWord] = 0u;
         }
     }
-    const int row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, h = blockIdx.y;
-    if (row >= a.nq) return;
-    const int b = sequence_of(a.q_offsets, a.nseq, row, a.nq);
-    if (b < 0) return;
-    const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
-    const int t = row - rq.first + rk.len - rq.len;
-    const bf16 *q = a.q.p + row * a.q.row + h * a.q.head;
-    float most = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 <= t; s0 += 32) {
-        if (s0 + 31 <= t - a.window && s0 >= a.sinks) continue;
-        const int s = s0 + lane;
-        const bool seen = s <= t && (s > t - a.window || s < a.sinks);
-        float x = -INFINITY;
-        if (seen) x = a.scale * dot(q, a.k.p + (rk.first + s) * a.k.row + (h / a.group) * a.k.head, a.d);
-        float m = x;
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-        m = fmaxf(m, most);
-        if (m == -INFINITY) continue;
-        const float old = expf(most - m), p = expf(x - m);
-        float ps = p;
-        for (int o = 16; o; o >>= 1) ps += __shfl_xor_sync(~0u, ps, o);
-        sum = sum * old + ps;
-        most = m;
-        for (int c = 0; c < 4; ++c) acc[c] *= old;
-        for (int j = 0; j < 32; ++j) {
-            const float pj = __shfl_sync(~0u, p, j);
-            if (pj == 0.f) continue;
-            const bf16 *v = a.v.p + (rk.first + s0 + j) * a.v.row + (h / a.group) * a.v.head;
-            for (int c = 0; c < 4; ++c)
-                if (lane + 32 * c < a.d) acc[c] += pj * __bfloat162float(v[lane + 32 * c]);
+    const TileOf at = tile_of<2 * TILE>(a.q_offsets, a.nseq, a.nq, blockIdx.x, lane);
+    if (at.seq < 0) return;
+    const Rows rq = rows_of(a.q_offsets, at.seq, a.nq), rk = rows_of(a.k_offsets, at.seq, a.nk);
+    const int i0 = at.tile * 2 * TILE, left = min(rq.len - i0, 2 * TILE), t0 = i0 + rk.len - rq.len;
+    const Mask mask{a.window, a.sinks};
+    const KeyTiles tiles = key_tiles(mask, t0, t0 + left - 1);
+    const int n = tiles.count();
+    // positions of the rows of a tile of queries (none: t1 < t0), and whether it sees a tile of keys
+    auto sees = [&](int w, int kt) {
+        const int first = t0 + w * TILE;
+        return mask.any(first, min(first + TILE, t0 + left) - 1, kt * TILE, kt * TILE + TILE - 1);
+    };
+
+    if (threadIdx.x == 0) {
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(&q_full[w], 1);
+            mbar_init(&s_full[w], 1);
+            mbar_init(&p_full[w], 4);
+            mbar_init(&o_full[w], 1);
         }
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&k_full[s], 1);
+            mbar_init(&k_empty[s], 1);
+            mbar_init(&v_full[s], 1);
+            mbar_init(&v_empty[s], 1);
+            mbar_init(&v_copied[s], 1);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) a.out[((int64_t)row * a.heads + h) * a.d + lane + 32 * c] = __float2bfloat16(acc[c] * inv);
-    if (lane == 0) a.lse[(int64_t)row * a.heads + h] = sum > 0.f ? most + logf(sum) : -INFINITY;
-}
-
-struct WindowGradArgs {
-    WindowArgs w;
-    const bf16 *o, *dout;
-    bf16 *dq, *dk, *dv;
-};
-
-// dq: one warp per (query, head)
-__global__ void window_dq_kernel(const WindowGradArgs g)
-{
-    const WindowArgs &a = g.w;
-    pdl_wait();
+    if (warp == 9) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
     pdl_trigger();
-    if (blockIdx.x == 0 && blockIdx.y == 0) {
-        const bool fine = offsets_fine(a.q_offsets, a.nseq, a.nq, threadIdx.x, blockDim.x) && offsets_fine(a.k_offsets, a.nseq, a.nk, threadIdx.x, blockDim.x);
-        const int all = __syncthreads_and(fine);
-        if (threadIdx.x == 0) {
-            a.status[kWsStatusWord] = all ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
-            a.status[kWsDetailWord] = 0u;
-        }
-    }
-    const int row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, h = blockIdx.y;
-    if (row >= a.nq) return;
-    const int b = sequence_of(a.q_offsets, a.nseq, row, a.nq);
-    if (b < 0) return;
-    const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
-    const int t = row - rq.first + rk.len - rq.len;
-    const int64_t at = ((int64_t)row * a.heads + h) * a.d;
-    const bf16 *q = a.q.p + row * a.q.row + h * a.q.head;
-    const float delta = dot(g.o + at, g.dout + at, a.d), lse = a.lse[(int64_t)row * a.heads + h];
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s <= t; ++s) {
-        if (!(s > t - a.window || s < a.sinks)) continue;
-        const bf16 *k = a.k.p + (rk.first + s) * a.k.row + (h / a.group) * a.k.head, *v = a.v.p + (rk.first + s) * a.v.row + (h / a.group) * a.v.head;
-        float x = 0.f, dp = 0.f;
-        for (int i = lane; i < a.d; i += 32) {
-            x += __bfloat162float(q[i]) * __bfloat162float(k[i]);
-            dp += __bfloat162float(g.dout[at + i]) * __bfloat162float(v[i]);
-        }
-        for (int o = 16; o; o >>= 1) {
-            x += __shfl_xor_sync(~0u, x, o);
-            dp += __shfl_xor_sync(~0u, dp, o);
-        }
-        const float ds = expf(a.scale * x - lse) * (dp - delta) * a.scale;
-        for (int c = 0; c < 4; ++c)
-            if (lane + 32 * c < a.d) acc[c] += ds * __bfloat162float(k[lane + 32 * c]);
-    }
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) g.dq[at + lane + 32 * c] = __float2bfloat16(acc[c]);
-}
 
-// dk, dv: one warp per (key, key head)
-__global__ void window_dkv_kernel(const WindowGradArgs g)
-{
-    const WindowArgs &a = g.w;
-    pdl_wait();
-    pdl_trigger();
-    const int row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, hk = blockIdx.y;
-    if (row >= a.nk) return;
-    const int b = sequence_of(a.k_offsets, a.nseq, row, a.nk);
-    if (b < 0) return;
-    const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
-    const int s = row - rk.first;
-    const bf16 *k = a.k.p + row * a.k.row + hk * a.k.head, *v = a.v.p + row * a.v.row + hk * a.v.head;
-    float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < rq.len; ++i) {
-        const int t = i + rk.len - rq.len;
-        if (!(s <= t && (s > t - a.window || s < a.sinks))) continue;
-        for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
-            const int qr = rq.first + i;
-            const int64_t at = ((int64_t)qr * a.heads + h) * a.d;
-            const bf16 *q = a.q.p + qr * a.q.row + h * a.q.head;
-            float x = 0.f, dp = 0.f, delta = 0.f;
-            for (int c = lane; c < a.d; c += 32) {
-                x += __bfloat162float(q[c]) * __bfloat162float(k[c]);
-                dp += __bfloat162float(g.dout[at + c]) * __bfloat162float(v[c]);
-                delta += __bfloat162float(g.dout[at + c]) * __bfloat162float(g.o[at + c]);
-            }
-            for (int o = 16; o; o >>= 1) {
-                x += __shfl_xor_sync(~0u, x, o);
-                dp += __shfl_xor_sync(~0u, dp, o);
-                delta += __shfl_xor_sync(~0u, delta, o);
-            }
-            const float p = expf(a.scale * x - a.lse[(int64_t)qr * a.heads + h]), ds = p * (dp - delta) * a.scale;
-            for (int c = 0; c < 4; ++c)
-                if (lane + 32 * c < a.d) {
-                    dk[c] += ds * __bfloat162float(q[lane + 32 * c]);
-                    dv[c] += p * __bfloat162float(g.dout[at + lane + 32 * c]);
+    if (warp == 8) {
+        const int hk = h / a.group;
+        if (lane == 0) {
+            for (int w = 0; w < 2; ++w)
+                if (w * TILE < left) {
+                    mbar_expect_tx(&q_full[w], S::TILE_BYTES);
+                    load_tile<DP>(Q + w * S::TILE_BYTES, &qmap, &q_full[w], h, rq.first + i0 + w * TILE);
                 }
         }
-    }
-    const int64_t at = ((int64_t)row * (a.heads / a.group) + hk) * a.d;
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) {
-            g.dk[at + lane + 32 * c] = __float2bfloat16(dk[c]);
-            g.dv[at + lane + 32 * c] = __float2bfloat16(dv[c]);
-        }
-}
-
-struct StepArgs {
-    const bf16 *q, *k, *v;
-    bf16 *k_pages, *v_pages;
-    const int *table, *lens;
-    int nseq, heads, group, d, pages, page, cols, window, sinks;
-    int64_t page_stride, token_stride, head_stride;
-    float scale;
-    bf16 *out;
-    unsigned *status;
-};
-
-__global__ void window_step_kernel(const StepArgs a)
-{
-    pdl_wait();
-    pdl_trigger();
-    const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x, hk = h / a.group, hkn = a.heads / a.group;
-    if (h == 0 && b == 0) {
-        bool fine = true;
-        for (int i = 0; i < a.nseq; ++i) {
-            const int n = a.lens[i];
-            fine = fine && n >= 0 && (int64_t)n <= (int64_t)a.cols * a.page;
-            for (int c = lane; c < min(a.cols, (n + a.page - 1) / a.page); c += 32) fine = fine && (unsigned)a.table[(int64_t)i * a.cols + c] < (unsigned)a.pages;
-        }
-        fine = __all_sync(~0u, fine);
-        if (lane == 0) {
-            a.status[kWsStatusWord] = fine ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
-            a.status[kWsDetailWord] = 0u;
-        }
-    }
-    const int len = (int)min((int64_t)max(a.lens[b], 0), (int64_t)a.cols * a.page), t = len - 1;
-    const bf16 *q = a.q + ((int64_t)b * a.heads + h) * a.d;
-    const bf16 *kn = a.k + ((int64_t)b * hkn + hk) * a.d, *vn = a.v + ((int64_t)b * hkn + hk) * a.d;
-    float most = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s <= t; ++s) {
-        if (!(s > t - a.window || s < a.sinks)) continue;
-        const int p = a.table[(int64_t)b * a.cols + s / a.page];
-        if ((unsigned)p >= (unsigned)a.pages) continue;
-        const int64_t at = p * a.page_stride + (s % a.page) * a.token_stride + hk * a.head_stride;
-        const bf16 *k = s == t ? kn : a.k_pages + at, *v = s == t ? vn : a.v_pages + at;
-        if (s == t && h % a.group == 0)
-            for (int c = lane; c < a.d; c += 32) {
-                a.k_pages[at + c] = kn[c];
-                a.v_pages[at + c] = vn[c];
+        int use = 0;
+        uint32_t copied = 0;                    // parity of v_copied, by stage
+        bool ok = true;
+        for (int i = 0; i < n && ok; ++i) {
+            const int kt = tiles.at(i);
+            if (!sees(0, kt) && !sees(1, kt)) continue;
+            const int s = use % STAGES, row = rk.first + kt * TILE;
+            const uint32_t parity = (uint32_t)((use / STAGES + 1) & 1);
+            const bool edge = kt * TILE + TILE > rk.len;
+            if (lane == 0) {
+                ok = mbar_wait(&k_empty[s], parity, abort_flag, a.status, 1);
+                if (ok) {
+                    mbar_expect_tx(&k_full[s], S::TILE_BYTES);
+                    load_tile<DP>(K + s * S::TILE_BYTES, &kmap, &k_full[s], hk, row);
+                    ok = mbar_wait(&v_empty[s], parity, abort_flag, a.status, 2);
+                }
+                if (ok) {
+                    uint64_t *bar = edge ? &v_copied[s] : &v_full[s];
+                    mbar_expect_tx(bar, S::TILE_BYTES);
+                    load_tile<DP>(V + s * S::TILE_BYTES, &vmap, bar, hk, row);
+                }
             }
-        float x = 0.f;
-        for (int c = lane; c < a.d; c += 32) x += __bfloat162float(q[c]) * __bfloat162float(k[c]);
-        for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-        x *= a.scale;
-        const float m = fmaxf(most, x), old = expf(most - m), w = expf(x - m);
-        sum = sum * old + w;
-        most = m;
-        for (int c = 0; c < 4; ++c)
-            if (lane + 32 * c < a.d) acc[c] = acc[c] * old + w * __bfloat162float(v[lane + 32 * c]);
+            ok = __shfl_sync(~0u, ok, 0);
+            if (edge && ok) {
+                ok = __all_sync(~0u, mbar_wait(&v_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
+                copied ^= 1u << s;
+                if (ok) {
+                    clear_rows<DP>(V + s * S::TILE_BYTES, rk.len - kt * TILE, lane);
+                    if (lane == 0) mbar_arrive(&v_full[s]);
+                }
+            }
+            ++use;
+        }
+    } else if (warp == 9) {
+        if (elect_one()) {
+            const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
+            // products are issued in the order S0 S1 | O0 S0' O1 S1' | O0' S0'' ..: one tile's rows are in the exponential while
+            // the other's products run
+            int next = 0, use = 0, k_seen = 0, v_seen = 0;       // next tile of keys for S; stages used by S
+            bool q_seen[2] = {false, false}, started[2] = {false, false}, ok = true;
+            uint32_t p_parity[2] = {0, 0};
+            int kt_prev = -1;
+            auto score = [&](int w, int kt, int u) {
+                if (!ok || !sees(w, kt)) return;
+                if (!q_seen[w]) {
+                    ok = mbar_wait(&q_full[w], 0, abort_flag, a.status, 4);
+                    q_seen[w] = true;
+                }
+                if (ok && k_seen <= u) {
+                    ok = mbar_wait(&k_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 5);
+                    k_seen = u + 1;
+                }
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows<DP>(tmem + w * TILE, Q + w * S::TILE_BYTES, K + (u % STAGES) * S::TILE_BYTES, s_idesc);
+                tc_commit(&s_full[w]);
+            };
+            auto weigh = [&](int w, int kt, int u) {
+                if (!ok || !sees(w, kt)) return;
+                if (v_seen <= u) {
+                    ok = mbar_wait(&v_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 6);
+                    v_seen = u + 1;
+                }
+                if (ok) ok = mbar_wait(&p_full[w], p_parity[w], abort_flag, a.status, 7);
+                if (!ok) return;
+                p_parity[w] ^= 1u;
+                tc_fence_after();
+                mma_tokens(tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, started[w]);
+                started[w] = true;
+            };
+            for (int i = 0; i <= n && ok; ++i) {
+                int kt = -1;
+                while (next < n) {                               // the next tile that either sees
+                    kt = tiles.at(next++);
+                    if (sees(0, kt) || sees(1, kt)) break;
+                    kt = -1;
+                }
+                if (kt_prev >= 0) weigh(0, kt_prev, use - 1);
+                if (kt >= 0) score(0, kt, use);
+                if (kt_prev >= 0) {
+                    weigh(1, kt_prev, use - 1);
+                    if (ok) tc_commit(&v_empty[(use - 1) % STAGES]);
+                }
+                if (kt >= 0) {
+                    score(1, kt, use);
+                    if (ok) tc_commit(&k_empty[use % STAGES]);
+                }
+                if (kt < 0) break;
+                kt_prev = kt;
+                ++use;
+            }
+            for (int w = 0; w < 2; ++w)                          // a copy that no product waited for ends before the block does
+                if (!q_seen[w] && w * TILE < left) (void)mbar_wait(&q_full[w], 0, abort_flag, a.status, 10);
+            if (ok) {
+                tc_commit(&o_full[0]);
+                tc_commit(&o_full[1]);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int w = warp >> 2, r = (warp & 3) * 32 + lane, t = t0 + w * TILE + r;      // this thread's row and its position
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + w * TILE, o_addr = tmem + lanes + 2 * TILE + w * DP;
+        const float c = a.scale * LOG2E;
+        float m = -INFINITY, l = 0.f;
+        uint32_t parity = 0;
+        bool ok = true, started = false;
+        for (int i = 0; i < n; ++i) {
+            const int kt = tiles.at(i);
+            if (!sees(w, kt)) continue;
+            ok = __all_sync(~0u, mbar_wait(&s_full[w], parity, abort_flag, a.status, 8));
+            if (!ok) break;
+            parity ^= 1u;
+            tc_fence_after();
+            uint32_t x[4][32];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tmem_ld_32x32(s_addr + j * 32, x[j]);
+            tmem_ld_wait();
+            const int s0 = kt * TILE;
+            if (!mask.all(t0 + w * TILE, t0 + w * TILE + TILE - 1, s0, s0 + TILE - 1)) {
+#pragma unroll
+                for (int j = 0; j < 128; ++j)
+                    if (!mask.sees(t, s0 + j)) x[j / 32][j % 32] = __float_as_uint(-INFINITY);
+            }
+            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int j = 0; j < 128; ++j) most[j & 3] = fmaxf(most[j & 3], __uint_as_float(x[j / 32][j % 32]));
+            const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            // the reference moves: 8 is the factor 2^8 that P may exceed 1 by
+            if (__any_sync(~0u, c * (top - m) > 8.f)) {
+                const float now = fmaxf(top, m), f = now == -INFINITY ? 1.f : ex2(c * (m - now));
+                m = now;
+                l *= f;
+                if (started) {
+#pragma unroll
+                    for (int j = 0; j < DP / 32; ++j) {
+                        uint32_t o[32];
+                        tmem_ld_32x32(o_addr + j * 32, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st_32x32(o_addr + j * 32, o);
+                    }
+                }
+            }
+            started = true;
+            const float mc = m == -INFINITY ? 0.f : m * c;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const int k0 = j * 64 + 2 * e;
+                    const float y0 = ex2(fmaf(__uint_as_float(x[k0 / 32][k0 % 32]), c, -mc)), y1 = ex2(fmaf(__uint_as_float(x[k0 / 32][k0 % 32 + 1]), c, -mc));
+                    sum[(e & 1) * 2] += y0;
+                    sum[(e & 1) * 2 + 1] += y1;
+                    p[e] = pack_bf16(y0, y1);
+                }
+                tmem_st_32x32(s_addr + j * 32, p);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[w]);
+        }
+        if (ok && n > 0) ok = __all_sync(~0u, mbar_wait(&o_full[w], 0, abort_flag, a.status, 9));
+        if (ok) {
+            tc_fence_after();
+            const int row = rq.first + i0 + w * TILE + r;
+            const bool mine = w * TILE + r < left;
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            bf16 *out = a.out + ((int64_t)row * a.heads + h) * a.d;
+#pragma unroll
+            for (int j = 0; j < DP / 32; ++j) {
+                uint32_t o[32];
+                if (started) {
+                    tmem_ld_32x32(o_addr + j * 32, o);
+                    tmem_ld_wait();
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (mine && j * 32 + e * 8 < a.d) {
+                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                        if (l > 0.f) {
+                            uint32_t *u = &v.x;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) u[k] = pack_bf16(__uint_as_float(o[e * 8 + 2 * k]) * inv, __uint_as_float(o[e * 8 + 2 * k + 1]) * inv);
+                        }
+                        *reinterpret_cast<uint4 *>(out + j * 32 + e * 8) = v;
+                    }
+                }
+            }
+            if (mine) a.lse[(int64_t)row * a.heads + h] = l > 0.f ? (m * c + log2f(l)) * LN2 : -INFINITY;
+        }
     }
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) a.out[((int64_t)b * a.heads + h) * a.d + lane + 32 * c] = __float2bfloat16(sum > 0.f ? acc[c] / sum : 0.f);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
 }
 
-static WindowArgs window_args(const st_tokens *t, const void *q, const void *k, const void *v, const int *qo, const int *ko, int64_t window,
-                              int64_t sinks, float scale, void *ws)
+template <int DP>
+static st_status run_window(const WindowArgs &a, const st_tokens *t, cudaStream_t stream)
 {
-    WindowArgs a = {};
-    a.q = {(const bf16 *)q, stride_of(t->nq, t->q_row), stride_of(t->heads, t->q_head)};
-    a.k = {(const bf16 *)k, stride_of(t->nk, t->k_row), stride_of(t->kv_heads, t->k_head)};
-    a.v = {(const bf16 *)v, stride_of(t->nk, t->v_row), stride_of(t->kv_heads, t->v_head)};
-    a.q_offsets = qo;
-    a.k_offsets = ko;
-    a.nseq = (int)t->nseq;
-    a.nq = (int)t->nq;
-    a.nk = (int)t->nk;
-    a.heads = (int)t->heads;
-    a.group = (int)(t->heads / t->kv_heads);
-    a.d = (int)t->d;
-    a.window = clamp_int(window);
-    a.sinks = clamp_int(sinks);
-    a.scale = scale;
-    a.status = (unsigned *)ws;
-    return a;
+    CUtensorMap qm, km, vm;
+    if (!make_tmap_table(&qm, a.q, t->nq, t->heads, t->d) || !make_tmap_table(&km, a.k, t->nk, t->kv_heads, t->d) ||
+        !make_tmap_table(&vm, a.v, t->nk, t->kv_heads, t->d))
+        return ST_ERR_CUDA;
+    if (!ensure_dynamic_smem(window_kernel<DP>, wfwd::Shape<DP>::SMEM)) return ST_ERR_CUDA;
+    const dim3 grid((unsigned)most_tiles(t->nq, t->nseq, 2 * TILE), (unsigned)t->heads);
+    return launch(window_kernel<DP>, grid, wfwd::THREADS, wfwd::Shape<DP>::SMEM, stream, qm, km, vm, a);
 }
 
 }  // namespace attn
-
-size_t attn_window_grad_workspace(int64_t nq, int64_t heads)
-{
-    if (nq <= 0 || heads <= 0 || nq > (1 << 30) || heads > 65535) return 0;
-    return kWsHeaderBytes + (size_t)nq * heads * sizeof(float);
-}
-
 }  // namespace st
 
 using namespace st;
 using namespace st::attn;
 
-static st_status check_window(const st_tokens *t, const int32_t *qo, const int32_t *ko, int64_t window, int64_t sinks, float scale)
+extern "C" st_status st_attn_window(const st_tokens *tokens, const void *q, const void *k, const void *v, const int32_t *q_offsets,
+                                    const int32_t *k_offsets, int64_t window, int64_t sinks, float scale, void *out, float *lse,
+                                    void *ws, size_t ws_bytes, void *stream)
 {
-    const st_status rc = check_tokens(t);
-    if (rc != ST_OK) return rc;
-    if (t->d != t->dv || window < 1 || sinks < 0) return ST_ERR_SHAPE;
-    if (!(scale > 0.f && scale < INFINITY)) return ST_ERR_UNSUPPORTED;
-    if (!qo != !ko) return ST_ERR_NULL;
-    if (!qo && t->nseq != 1) return ST_ERR_NULL;
-    return ST_OK;
-}
-
-extern "C" {
-
-st_status st_attn_window(const st_tokens *tokens, const void *q, const void *k, const void *v, const int32_t *q_offsets,
-                         const int32_t *k_offsets, int64_t window, int64_t sinks, float scale, void *out, float *lse,
-                         void *ws, size_t ws_bytes, void *stream)
-{
-    st_status rc = check_window(tokens, q_offsets, k_offsets, window, sinks, scale);
+    const st_status rc = check_window(tokens, q_offsets, k_offsets, window, sinks, scale);
     if (rc != ST_OK) return rc;
     if (!q || !k || !v || !out || !lse) return ST_ERR_NULL;
     for (const void *p : {q, k, v, (const void *)out, (const void *)lse, (const void *)q_offsets, (const void *)k_offsets})
@@ -300,79 +354,5 @@ st_status st_attn_window(const st_tokens *tokens, const void *q, const void *k, 
     WindowArgs a = window_args(tokens, q, k, v, q_offsets, k_offsets, window, sinks, scale, ws);
     a.out = (bf16 *)out;
     a.lse = lse;
-    return launch(window_kernel, dim3((a.nq + 3) / 4, a.heads), 128, 0, (cudaStream_t)stream, a);
+    return a.d <= 64 ? run_window<64>(a, tokens, (cudaStream_t)stream) : run_window<128>(a, tokens, (cudaStream_t)stream);
 }
-
-st_status st_attn_window_grad(const st_tokens *tokens, const void *q, const void *k, const void *v, const void *out,
-                              const float *lse, const void *dout, const int32_t *q_offsets, const int32_t *k_offsets,
-                              int64_t window, int64_t sinks, float scale, void *dq, void *dk, void *dv, void *ws,
-                              size_t ws_bytes, void *stream)
-{
-    st_status rc = check_window(tokens, q_offsets, k_offsets, window, sinks, scale);
-    if (rc != ST_OK) return rc;
-    if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv) return ST_ERR_NULL;
-    for (const void *p : {q, k, v, out, (const void *)lse, dout, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)q_offsets, (const void *)k_offsets})
-        if (!aligned16(p)) return ST_ERR_ALIGN;
-    if (!ws || ws_bytes < attn_window_grad_workspace(tokens->nq, tokens->heads)) return ST_ERR_WORKSPACE;
-    if (!aligned256(ws)) return ST_ERR_ALIGN;
-    WindowGradArgs g = {};
-    g.w = window_args(tokens, q, k, v, q_offsets, k_offsets, window, sinks, scale, ws);
-    g.w.lse = const_cast<float *>(lse);
-    g.o = (const bf16 *)out;
-    g.dout = (const bf16 *)dout;
-    g.dq = (bf16 *)dq;
-    g.dk = (bf16 *)dk;
-    g.dv = (bf16 *)dv;
-    rc = launch(window_dq_kernel, dim3((g.w.nq + 3) / 4, g.w.heads), 128, 0, (cudaStream_t)stream, g);
-    if (rc != ST_OK) return rc;
-    return launch(window_dkv_kernel, dim3((g.w.nk + 3) / 4, g.w.heads / g.w.group), 128, 0, (cudaStream_t)stream, g);
-}
-
-st_status st_attn_window_step(const st_cache *c, const void *q, const void *k, const void *v, void *k_pages,
-                              void *v_pages, const int32_t *table, const int32_t *lens, int64_t window, int64_t sinks,
-                              float scale, void *out, void *ws, size_t ws_bytes, void *stream)
-{
-    if (!c) return ST_ERR_NULL;
-    if (c->dtype != ST_BF16) return ST_ERR_DTYPE;
-    if (c->reserved != 0 || c->nseq <= 0 || c->heads <= 0 || c->kv_heads <= 0 || c->d <= 0 || c->pages <= 0 || c->page <= 0 || c->table_cols <= 0 ||
-        c->heads % c->kv_heads != 0 || window < 1 || sinks < 0)
-        return ST_ERR_SHAPE;
-    if (c->nseq > 65535 || c->heads > 65535 || c->d % 8 != 0 || c->d > 128 || c->pages > (1 << 30) || c->page > (1 << 30) || c->table_cols > (1 << 30))
-        return ST_ERR_UNSUPPORTED;
-    if (!stride_ok(c->pages, c->page_stride, c->d) || !stride_ok(c->page, c->token_stride, c->d) || !stride_ok(c->kv_heads, c->head_stride, c->d))
-        return ST_ERR_SHAPE;
-    if ((c->pages > 1 && c->page_stride % 8 != 0) || (c->page > 1 && c->token_stride % 8 != 0) || (c->kv_heads > 1 && c->head_stride % 8 != 0))
-        return ST_ERR_ALIGN;
-    if (!(scale > 0.f && scale < INFINITY)) return ST_ERR_UNSUPPORTED;
-    if (!q || !k || !v || !k_pages || !v_pages || !table || !lens || !out) return ST_ERR_NULL;
-    for (const void *p : {q, k, v, (const void *)k_pages, (const void *)v_pages, (const void *)table, (const void *)lens, (const void *)out})
-        if (!aligned16(p)) return ST_ERR_ALIGN;
-    if (!ws || ws_bytes < kWsHeaderBytes) return ST_ERR_WORKSPACE;
-    if (!aligned256(ws)) return ST_ERR_ALIGN;
-    StepArgs a = {};
-    a.q = (const bf16 *)q;
-    a.k = (const bf16 *)k;
-    a.v = (const bf16 *)v;
-    a.k_pages = (bf16 *)k_pages;
-    a.v_pages = (bf16 *)v_pages;
-    a.table = table;
-    a.lens = lens;
-    a.nseq = (int)c->nseq;
-    a.heads = (int)c->heads;
-    a.group = (int)(c->heads / c->kv_heads);
-    a.d = (int)c->d;
-    a.pages = (int)c->pages;
-    a.page = (int)c->page;
-    a.cols = (int)c->table_cols;
-    a.window = clamp_int(window);
-    a.sinks = clamp_int(sinks);
-    a.page_stride = stride_of(c->pages, c->page_stride);
-    a.token_stride = stride_of(c->page, c->token_stride);
-    a.head_stride = stride_of(c->kv_heads, c->head_stride);
-    a.scale = scale;
-    a.out = (bf16 *)out;
-    a.status = (unsigned *)ws;
-    return launch(window_step_kernel, dim3(a.heads, a.nseq), 32, 0, (cudaStream_t)stream, a);
-}
-
-}  // extern "C"
