@@ -130,7 +130,7 @@ st_status st_unpack(const st_layout *layout, st_dtype dtype, const void *packed,
  *   ST_OP_MTTKRP_SLICE  a=I, b=J, c=K, e=R (enough for any fixed_i / fixed_j; flags as for the call)
  *   ST_OP_TTM_BLOCKDIAG a=nblocks, b=bs, c=K, e=R
  *   ST_OP_ATTN_WINDOW   unused: the header alone;  ST_OP_ATTN_WINDOW_STEP likewise
- *   ST_OP_ATTN_WINDOW_GRAD a=nq, b=heads
+ *   ST_OP_ATTN_WINDOW_GRAD a=nq, b=heads, c=kv_heads, e=sinks
  *   ST_OP_ATTN_DECAY, ST_OP_ATTN_DECAY_GRAD  a=nq, b=nseq, c=heads, e=max(d, dv)
  * Returns 0 for an invalid request (the call itself reports the error).  The current
  * device is queried for its SM count. */

@@ -64,12 +64,14 @@ __device__ __forceinline__ void mma_rows(uint32_t d_tmem, const unsigned char *A
     }
 }
 
-// D[128, N] (+)= A B over the 128 tokens of a tile: A[128, 128 tokens] bf16 in tensor memory, B a tile whose rows are the tokens.
+// D[128, N] (+)= A B over the 128 tokens of a tile: A[128, 128 tokens] bf16 in tensor memory, its second 64 tokens HALF columns behind
+// the first, B a tile whose rows are the tokens.
+template <int HALF = 32>
 __device__ __forceinline__ void mma_tokens(uint32_t d_tmem, uint32_t a_tmem, const unsigned char *B, uint32_t idesc, bool add)
 {
     const uint64_t b = tc::make_smem_desc(tc::smem_u32(B), SLAB, 1024);
 #pragma unroll
-    for (int k = 0; k < TILE / 16; ++k) mma_bf16_ts(d_tmem, a_tmem + k * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0 ? 1u : 0u);
+    for (int k = 0; k < TILE / 16; ++k) mma_bf16_ts(d_tmem, a_tmem + (k >> 2) * HALF + (k & 3) * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0 ? 1u : 0u);
 }
 
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32])
@@ -82,6 +84,14 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r
           "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
           "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
           "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -139,13 +149,28 @@ struct Mask {
     __device__ __forceinline__ bool all(int t0, int t1, int s0, int s1) const { return s1 <= t0 && (s0 > t1 - window || s1 < sinks); }
 };
 
+// The tiles of keys that the queries at positions t0..t1 see: [0, first) with the sinks and [lo, hi).
+struct KeyTiles {
+    int first, lo, hi;
+    __device__ __forceinline__ int count() const { return first + max(0, hi - lo); }
+    __device__ __forceinline__ int at(int i) const { return i < first ? i : lo + i - first; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const Mask &m, int t0, int t1)
+{
+    KeyTiles k;
+    k.hi = t1 < 0 ? 0 : t1 / TILE + 1;
+    k.lo = min(max(0, t0 - m.window + 1) / TILE, k.hi);
+    k.first = min((min(m.sinks, 1 << 29) + TILE - 1) / TILE, k.lo);
+    return k;
+}
+
 // Rows [valid, 128) of a tile in shared memory, whatever they are, become zero; by a whole warp, before the tensor cores read the tile.
 template <int COLS>
 __device__ __forceinline__ void clear_rows(unsigned char *tile, int valid, int lane)
 {
 #pragma unroll
     for (int c = 0; c < COLS / 64; ++c)
-        for (int i = valid * 8 + lane; i < TILE * 8; i += 32) *reinterpret_cast<uint4 *>(tile + c * SLAB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = max(valid, 0) * 8 + lane; i < TILE * 8; i += 32) *reinterpret_cast<uint4 *>(tile + c * SLAB + i * 16) = make_uint4(0u, 0u, 0u, 0u);
     tc::fence_proxy_async();
     __syncwarp();
 }

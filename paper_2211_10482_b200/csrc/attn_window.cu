@@ -27,21 +27,6 @@ template <int DP> struct Shape {
 };
 }  // namespace wfwd
 
-// The tiles of keys that the queries at positions t0..t1 see: [0, first) with the sinks and [lo, hi).
-struct KeyTiles {
-    int first, lo, hi;
-    __device__ __forceinline__ int count() const { return first + max(0, hi - lo); }
-    __device__ __forceinline__ int at(int i) const { return i < first ? i : lo + i - first; }
-};
-__device__ __forceinline__ KeyTiles key_tiles(const Mask &m, int t0, int t1)
-{
-    KeyTiles k;
-    k.hi = t1 < 0 ? 0 : t1 / TILE + 1;
-    k.lo = min(max(0, t0 - m.window + 1) / TILE, k.hi);
-    k.first = min((min(m.sinks, 1 << 29) + TILE - 1) / TILE, k.lo);
-    return k;
-}
-
 template <int DP>
 __global__ void __launch_bounds__(wfwd::THREADS, 1)
 window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,

@@ -1,130 +1,714 @@
-// st_attn_window_grad: one warp per (query, head) for dq and per (key, key head) for dk and dv, the formulas as they stand.
+// st_attn_window_grad on the tensor cores, without atomics: one kernel for dq, one for dk and dv, both from the saved log-sum-exp.
+//
+//   window_dq_kernel   a block owns 128 queries of one head and passes over the tiles of keys that they see:
+//                      S = Q K^T, dP = dO V^T, dS = exp(scale S - lse) (dP - delta), dQ += dS K
+//                      delta = dO.O is taken on the way in and kept for the second kernel.
+//   window_dkv_kernel  a block owns 128 keys of one key head and passes over the heads that share it and the tiles of queries that see it,
+//                      everything transposed:  S^T = K Q^T, dP^T = V dO^T, dV += P^T dO, dK += dS^T Q
+//
+// Seven products instead of the five of one pass over both, in exchange for sums in a fixed order: no atomics on dq, and the sum over the
+// heads that share keys stays in the accumulator.  P and dS go to tensor memory as bf16, each in the place of the fp32
+// scores it was made from, and are A operands there; a thread holds one row and half of a tile's columns, and writes where it has read.
+// Products and exponentials overlap: while a tile's dS is made the tensor cores work on the next tile's S.
+//
+// The first columns (sinks) are seen by every later query, so that their tiles of keys would take as long as the whole sequence:
+// queries beyond the window are cut into parts of 1024 for blocks of their own, which leave fp32 sums of the sinks' rows in the
+// workspace; window_sinks_kernel adds them in the order of the parts.
+//
+// Rows behind a sequence may hold anything: where they would be multiplied by weights of 0 they are cleared in shared memory.
 #include "attn_window.cuh"
 
 namespace st {
 namespace attn {
 
-__device__ __forceinline__ int sequence_of(const int *offsets, int nseq, int row, int n)
-{
-    if (!offsets) return row < n ? 0 : -1;
-    for (int b = 0; b < nseq; ++b) {
-        const Rows r = rows_of(offsets, b, n);
-        if (row >= r.first && row < r.first + r.len) return b;
-    }
-    return -1;
-}
-
-__device__ __forceinline__ float dot(const bf16 *a, const bf16 *b, int d)
-{
-    float s = 0.f;
-    for (int i = 0; i < d; ++i) s += __bfloat162float(a[i]) * __bfloat162float(b[i]);
-    return s;
-}
+namespace wgrad {
+constexpr int THREADS = 320;
+constexpr int PART_TILES = 8, PART = PART_TILES * TILE;      // queries of a part beyond the window
+constexpr int MAX_SPLIT_SINKS = 2 * TILE;                    // with more first columns they are no small share of the work any more
+template <int DP> struct Shape {
+    static constexpr int TILE_BYTES = DP / 64 * SLAB;
+    static constexpr size_t DQ_SMEM = 1024 + (size_t)TILE_BYTES * 7 + 2 * TILE * sizeof(float) + 256;
+    static constexpr size_t DKV_SMEM = 1024 + (size_t)TILE_BYTES * 6 + 4 * TILE * sizeof(float) + 256;
+};
+}  // namespace wgrad
 
 struct WindowGradArgs {
     WindowArgs w;
     const bf16 *o, *dout;
+    const float *lse;
     bf16 *dq, *dk, *dv;
+    float *delta;                  // [nq, heads]
+    float *parts;                  // sums of the sinks' rows: [2: near, far][tile of keys][slot][key head][2: dk, dv][rows][d]
+    int nslots, sink_tiles, sink_rows;   // 0 sink_tiles: nothing is split
 };
 
-// dq: one warp per (query, head)
-__global__ void window_dq_kernel(const WindowGradArgs g)
+__device__ __forceinline__ float *part_of(const WindowGradArgs &g, int far, int kt, int slot, int hk)
 {
+    const int kv_heads = g.w.heads / g.w.group;
+    return g.parts + ((((int64_t)far * g.sink_tiles + kt) * g.nslots + slot) * kv_heads + hk) * 2 * g.sink_rows * g.w.d;
+}
+
+// The tiles of queries that see the keys s0.. of a tile: [a, near) through the window, [near, all) through the first columns only.
+struct QueryTiles {
+    int a, near, all;
+};
+__device__ __forceinline__ QueryTiles query_tiles(const Mask &m, const Rows &rq, const Rows &rk, int s0)
+{
+    const int64_t off = rk.len - rq.len, last = min(s0 + TILE, rk.len) - 1;
+    const int n = (rq.len + TILE - 1) / TILE;
+    QueryTiles q;
+    q.a = (int)(max((int64_t)0, s0 - off) / TILE);
+    const int64_t end = last + m.window - 1 - off;         // the last query that sees the last key through the window
+    q.near = end < 0 ? 0 : (int)min((int64_t)n, end / TILE + 1);
+    q.near = max(q.near, min(q.a, n));
+    q.a = min(q.a, n);
+    q.all = s0 < m.sinks ? n : q.near;
+    return q;
+}
+// First query tile that is left to the parts, where a tile of keys is split.
+__device__ __forceinline__ int first_part(const QueryTiles &q) { return q.near + wgrad::PART_TILES; }
+
+// The sequence one of whose parts begins in rows [slot * PART, slot * PART + PART), and that part; by a whole warp.  Parts begin PART rows
+// apart and the first of a sequence more than PART rows behind its beginning, so that there is one at most.
+struct PartOf {
+    int seq, part;
+};
+__device__ __forceinline__ PartOf part_at(const WindowArgs &a, const Mask &m, int kt, int slot, int lane)
+{
+    for (int b0 = 0; b0 < a.nseq; b0 += 32) {
+        const int b = b0 + lane;
+        int part = -1;
+        if (b < a.nseq) {
+            const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
+            if (kt * TILE < rk.len) {
+                const QueryTiles q = query_tiles(m, rq, rk, kt * TILE);
+                const int begin = rq.first + first_part(q) * TILE, p = max(0, (slot * wgrad::PART - begin + wgrad::PART - 1) / wgrad::PART);
+                const int row = begin + p * wgrad::PART;
+                if (first_part(q) + p * wgrad::PART_TILES < q.all && row / wgrad::PART == slot) part = p;
+            }
+        }
+        const unsigned found = __ballot_sync(~0u, part >= 0);
+        if (found) {
+            const int l = __ffs(found) - 1;
+            return {b0 + l, __shfl_sync(~0u, part, l)};
+        }
+    }
+    return {-1, 0};
+}
+
+// 8 values of a row, products of which are summed in fp32
+__device__ __forceinline__ float dot8(uint4 x, uint4 y)
+{
+    const __nv_bfloat162 *a = reinterpret_cast<const __nv_bfloat162 *>(&x), *b = reinterpret_cast<const __nv_bfloat162 *>(&y);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 u = __bfloat1622float2(a[i]), v = __bfloat1622float2(b[i]);
+        s = fmaf(u.x, v.x, fmaf(u.y, v.y, s));
+    }
+    return s;
+}
+
+// Columns [c0, c0 + N) of a thread's row of an accumulator, scaled, as bf16 where `dst` is not null (dst: the row's first column, d columns).
+template <int N>
+__device__ __forceinline__ void store_row(uint32_t taddr, int c0, bf16 *dst, int d, float scale, bool zero)
+{
+#pragma unroll
+    for (int j = 0; j < N / 32; ++j) {
+        uint32_t o[32];
+        tc::tmem_ld_32x32(taddr + c0 + j * 32, o);
+        tc::tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = c0 + j * 32 + e * 8;
+            if (dst && c < d) {
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                uint32_t *u = &v.x;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (!zero) u[k] = pack_bf16(__uint_as_float(o[e * 8 + 2 * k]) * scale, __uint_as_float(o[e * 8 + 2 * k + 1]) * scale);
+                *reinterpret_cast<uint4 *>(dst + c) = v;
+            }
+        }
+    }
+}
+
+template <int DP>
+__global__ void __launch_bounds__(wgrad::THREADS, 1)
+window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+                 const __grid_constant__ CUtensorMap domap, const WindowGradArgs g)
+{
+    using namespace wgrad;
+    using namespace tc;
+    constexpr int BYTES = Shape<DP>::TILE_BYTES, KS = 3, VS = 2;
     const WindowArgs &a = g.w;
+    extern __shared__ unsigned char raw[];
+    unsigned char *smem = align_smem(raw);
+    unsigned char *Q = smem, *DO = Q + BYTES, *K = DO + BYTES, *V = K + KS * BYTES;
+    float *halves = (float *)(V + VS * BYTES);
+    uint64_t *bars = (uint64_t *)(halves + 2 * TILE);
+    uint64_t *q_full = bars, *do_full = bars + 1, *k_full = bars + 2, *k_copied = k_full + KS, *k_empty = k_copied + KS, *v_full = k_empty + KS,
+             *v_empty = v_full + VS, *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_full = dp_full + 1, *done = ds_full + 1;
+    uint32_t *tmem_slot = (uint32_t *)(done + 1);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
+
     pdl_wait();
-    pdl_trigger();
     if (blockIdx.x == 0 && blockIdx.y == 0) {
-        const bool fine = offsets_fine(a.q_offsets, a.nseq, a.nq, threadIdx.x, blockDim.x) && offsets_fine(a.k_offsets, a.nseq, a.nk, threadIdx.x, blockDim.x);
+        const bool fine = offsets_fine(a.q_offsets, a.nseq, a.nq, threadIdx.x, THREADS) && offsets_fine(a.k_offsets, a.nseq, a.nk, threadIdx.x, THREADS);
         const int all = __syncthreads_and(fine);
         if (threadIdx.x == 0) {
             a.status[kWsStatusWord] = all ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
             a.status[kWsDetailWord] = 0u;
         }
     }
-    const int row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, h = blockIdx.y;
-    if (row >= a.nq) return;
-    const int b = sequence_of(a.q_offsets, a.nseq, row, a.nq);
-    if (b < 0) return;
-    const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
-    const int t = row - rq.first + rk.len - rq.len;
-    const int64_t at = ((int64_t)row * a.heads + h) * a.d;
-    const bf16 *q = a.q.p + row * a.q.row + h * a.q.head;
-    const float delta = dot(g.o + at, g.dout + at, a.d), lse = a.lse[(int64_t)row * a.heads + h];
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s <= t; ++s) {
-        if (!(s > t - a.window || s < a.sinks)) continue;
-        const bf16 *k = a.k.p + (rk.first + s) * a.k.row + (h / a.group) * a.k.head, *v = a.v.p + (rk.first + s) * a.v.row + (h / a.group) * a.v.head;
-        float x = 0.f, dp = 0.f;
-        for (int i = lane; i < a.d; i += 32) {
-            x += __bfloat162float(q[i]) * __bfloat162float(k[i]);
-            dp += __bfloat162float(g.dout[at + i]) * __bfloat162float(v[i]);
+    const TileOf at = tile_of<TILE>(a.q_offsets, a.nseq, a.nq, blockIdx.x, lane);
+    if (at.seq < 0) return;
+    const Rows rq = rows_of(a.q_offsets, at.seq, a.nq), rk = rows_of(a.k_offsets, at.seq, a.nk);
+    const int i0 = at.tile * TILE, left = min(rq.len - i0, TILE), t0 = i0 + rk.len - rq.len;
+    const Mask mask{a.window, a.sinks};
+    const KeyTiles tiles = key_tiles(mask, t0, t0 + left - 1);
+    const int n = tiles.count();
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        mbar_init(do_full, 1);
+        for (int s = 0; s < KS; ++s) {
+            mbar_init(&k_full[s], 1);
+            mbar_init(&k_copied[s], 1);
+            mbar_init(&k_empty[s], 1);
         }
-        for (int o = 16; o; o >>= 1) {
-            x += __shfl_xor_sync(~0u, x, o);
-            dp += __shfl_xor_sync(~0u, dp, o);
+        for (int s = 0; s < VS; ++s) {
+            mbar_init(&v_full[s], 1);
+            mbar_init(&v_empty[s], 1);
         }
-        const float ds = expf(a.scale * x - lse) * (dp - delta) * a.scale;
-        for (int c = 0; c < 4; ++c)
-            if (lane + 32 * c < a.d) acc[c] += ds * __bfloat162float(k[lane + 32 * c]);
+        mbar_init(&s_full[0], 1);
+        mbar_init(&s_full[1], 1);
+        mbar_init(dp_full, 1);
+        mbar_init(ds_full, 8);
+        mbar_init(done, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
     }
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) g.dq[at + lane + 32 * c] = __float2bfloat16(acc[c]);
+    if (warp == 9) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot, dp_col = tmem + 2 * TILE, dq_col = tmem + 3 * TILE;
+    pdl_trigger();
+
+    if (warp == 8) {
+        const int hk = h / a.group;
+        if (lane == 0 && n > 0) {
+            mbar_expect_tx(q_full, BYTES);
+            load_tile<DP>(Q, &qmap, q_full, h, rq.first + i0);
+            mbar_expect_tx(do_full, BYTES);
+            load_tile<DP>(DO, &domap, do_full, h, rq.first + i0);
+        }
+        bool ok = true;
+        uint32_t copied = 0;
+        for (int i = 0; i < n && ok; ++i) {
+            const int kt = tiles.at(i), row = rk.first + kt * TILE, s = i % KS, sv = i % VS;
+            const bool edge = kt * TILE + TILE > rk.len;
+            if (lane == 0) {
+                ok = mbar_wait(&k_empty[s], (uint32_t)((i / KS + 1) & 1), abort_flag, a.status, 1);
+                if (ok) {
+                    uint64_t *bar = edge ? &k_copied[s] : &k_full[s];
+                    mbar_expect_tx(bar, BYTES);
+                    load_tile<DP>(K + s * BYTES, &kmap, bar, hk, row);
+                    ok = mbar_wait(&v_empty[sv], (uint32_t)((i / VS + 1) & 1), abort_flag, a.status, 2);
+                }
+                if (ok) {
+                    mbar_expect_tx(&v_full[sv], BYTES);
+                    load_tile<DP>(V + sv * BYTES, &vmap, &v_full[sv], hk, row);
+                }
+            }
+            ok = __shfl_sync(~0u, ok, 0);
+            if (edge && ok) {
+                ok = __all_sync(~0u, mbar_wait(&k_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
+                copied ^= 1u << s;
+                if (ok) {
+                    clear_rows<DP>(K + s * BYTES, rk.len - kt * TILE, lane);
+                    if (lane == 0) mbar_arrive(&k_full[s]);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (n > 0 && elect_one()) {
+            const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
+            bool ok = true;
+            auto score = [&](int j) {
+                if (!ok || j >= n) return;
+                ok = mbar_wait(&k_full[j % KS], (uint32_t)((j / KS) & 1), abort_flag, a.status, 4);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows<DP>(tmem + (j & 1) * TILE, Q, K + (j % KS) * BYTES, s_idesc);
+                tc_commit(&s_full[j & 1]);
+            };
+            auto dprob = [&](int j) {
+                if (!ok || j >= n) return;
+                ok = mbar_wait(&v_full[j % VS], (uint32_t)((j / VS) & 1), abort_flag, a.status, 5);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows<DP>(dp_col, DO, V + (j % VS) * BYTES, s_idesc);
+                tc_commit(dp_full);
+                tc_commit(&v_empty[j % VS]);
+            };
+            ok = mbar_wait(q_full, 0, abort_flag, a.status, 6);
+            score(0);
+            if (ok) ok = mbar_wait(do_full, 0, abort_flag, a.status, 7);
+            dprob(0);
+            score(1);
+            for (int j = 0; j < n && ok; ++j) {
+                ok = mbar_wait(ds_full, (uint32_t)(j & 1), abort_flag, a.status, 8);
+                if (!ok) break;
+                tc_fence_after();
+                dprob(j + 1);
+                if (!ok) break;
+                mma_tokens<64>(dq_col, tmem + (j & 1) * TILE, K + (j % KS) * BYTES, o_idesc, j > 0);
+                tc_commit(&k_empty[j % KS]);
+                score(j + 2);
+            }
+            if (ok) tc_commit(done);
+        }
+        __syncwarp();
+    } else {
+        // thread: row r, columns 64 half .. 64 half + 63
+        const int half = warp >> 2, r = (warp & 3) * 32 + lane, t = t0 + r;
+        const int64_t row = rq.first + i0 + r;
+        const bool mine = r < left;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        float lse2 = 0.f, delta = 0.f;
+        if (mine) {
+            const float lse = g.lse[row * a.heads + h];
+            lse2 = lse == -INFINITY ? 0.f : lse * LOG2E;
+            const int64_t base = (row * a.heads + h) * a.d;
+            for (int c = half * 8; c < a.d; c += 16)
+                delta += dot8(*reinterpret_cast<const uint4 *>(g.o + base + c), *reinterpret_cast<const uint4 *>(g.dout + base + c));
+        }
+        halves[half * TILE + r] = delta;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        delta = halves[r] + halves[TILE + r];
+        if (mine && half == 0) g.delta[row * a.heads + h] = delta;
+        const float c = a.scale * LOG2E;
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            const uint32_t s_addr = tmem + lanes + (j & 1) * TILE + half * 64, dp_addr = dp_col + lanes + half * 64;
+            const int s0 = tiles.at(j) * TILE;
+            const bool cut = !mask.all(t0, t0 + TILE - 1, s0, s0 + TILE - 1);
+            ok = __all_sync(~0u, mbar_wait(&s_full[j & 1], (uint32_t)((j >> 1) & 1), abort_flag, a.status, 9));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t x[2][32];
+            tmem_ld_32x32(s_addr, x[0]);
+            tmem_ld_32x32(s_addr + 32, x[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 64; ++e) {
+                float p = ex2(fmaf(__uint_as_float(x[e / 32][e % 32]), c, -lse2));
+                if (cut && !mask.sees(t, s0 + half * 64 + e)) p = 0.f;
+                x[e / 32][e % 32] = __float_as_uint(p);
+            }
+            ok = __all_sync(~0u, mbar_wait(dp_full, (uint32_t)(j & 1), abort_flag, a.status, 10));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t dp[32], ds[16];
+                tmem_ld_32x32(dp_addr + b * 32, dp);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float y[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float p = __uint_as_float(x[b][2 * e + k]);
+                        // a masked weight is 0 whatever its dP is
+                        y[k] = cut && p == 0.f ? 0.f : p * (__uint_as_float(dp[2 * e + k]) - delta);
+                    }
+                    ds[e] = pack_bf16(y[0], y[1]);
+                }
+                tmem_st_32x16(s_addr + b * 16, ds);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+        }
+        if (ok && n > 0) ok = __all_sync(~0u, mbar_wait(done, 0, abort_flag, a.status, 11));
+        if (ok) {
+            tc_fence_after();
+            store_row<DP / 2>(dq_col + lanes, half * (DP / 2), mine ? g.dq + (row * a.heads + h) * a.d : nullptr, a.d, a.scale, n == 0);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
 }
 
-// dk, dv: one warp per (key, key head)
-__global__ void window_dkv_kernel(const WindowGradArgs g)
+template <int DP>
+__global__ void __launch_bounds__(wgrad::THREADS, 1)
+window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+                  const __grid_constant__ CUtensorMap domap, const WindowGradArgs g)
+{
+    using namespace wgrad;
+    using namespace tc;
+    constexpr int BYTES = Shape<DP>::TILE_BYTES, ST = 2;
+    const WindowArgs &a = g.w;
+    extern __shared__ unsigned char raw[];
+    unsigned char *smem = align_smem(raw);
+    unsigned char *K = smem, *V = K + BYTES, *Q = V + BYTES, *DO = Q + ST * BYTES;
+    float *stats = (float *)(DO + ST * BYTES);             // [stage][2: lse log2 e, delta][128]
+    uint64_t *bars = (uint64_t *)(stats + ST * 2 * TILE);
+    uint64_t *k_full = bars, *v_full = bars + 1, *q_full = bars + 2, *q_copied = q_full + ST, *q_empty = q_copied + ST, *do_full = q_empty + ST,
+             *do_copied = do_full + ST, *do_empty = do_copied + ST, *s_full = do_empty + ST, *dp_full = s_full + 1, *p_full = dp_full + 1,
+             *ds_full = p_full + 1, *done = ds_full + 1;
+    uint32_t *tmem_slot = (uint32_t *)(done + 1);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y;
+
+    pdl_wait();
+    const Mask mask{a.window, a.sinks};
+    const int far_blocks = g.sink_tiles * g.nslots;
+    const bool far = (int)blockIdx.x < far_blocks;
+    int seq, kt, slot = 0;
+    QueryTiles qt;
+    Rows rq, rk;
+    if (far) {
+        kt = blockIdx.x / g.nslots;
+        slot = blockIdx.x % g.nslots;
+        const PartOf p = part_at(a, mask, kt, slot, lane);
+        if (p.seq < 0) return;
+        seq = p.seq;
+        rq = rows_of(a.q_offsets, seq, a.nq);
+        rk = rows_of(a.k_offsets, seq, a.nk);
+        qt = query_tiles(mask, rq, rk, kt * TILE);
+        qt.a = first_part(qt) + p.part * PART_TILES;
+        qt.all = min(qt.all, qt.a + PART_TILES);
+    } else {
+        const TileOf at = tile_of<TILE>(a.k_offsets, a.nseq, a.nk, blockIdx.x - far_blocks, lane);
+        if (at.seq < 0) return;
+        seq = at.seq;
+        kt = at.tile;
+        rq = rows_of(a.q_offsets, seq, a.nq);
+        rk = rows_of(a.k_offsets, seq, a.nk);
+        qt = query_tiles(mask, rq, rk, kt * TILE);
+    }
+    // rows whose sums are finished elsewhere: the sinks', where parts of the queries are left to other blocks
+    int partial_rows = 0;
+    if (far) {
+        partial_rows = min(a.sinks - kt * TILE, TILE);
+    } else if (kt < g.sink_tiles && first_part(qt) < qt.all) {
+        partial_rows = min(a.sinks - kt * TILE, TILE);
+        slot = (rq.first + first_part(qt) * TILE) / PART;
+        qt.all = first_part(qt);
+    }
+    const int s0 = kt * TILE, per_head = max(0, qt.all - qt.a), n = per_head * a.group, off = rk.len - rq.len;
+
+    if (threadIdx.x == 0) {
+        mbar_init(k_full, 1);
+        mbar_init(v_full, 1);
+        for (int s = 0; s < ST; ++s) {
+            mbar_init(&q_full[s], 1);
+            mbar_init(&q_copied[s], 1);
+            mbar_init(&q_empty[s], 1);
+            mbar_init(&do_full[s], 1);
+            mbar_init(&do_copied[s], 1);
+            mbar_init(&do_empty[s], 1);
+        }
+        mbar_init(s_full, 1);
+        mbar_init(dp_full, 1);
+        mbar_init(p_full, 8);
+        mbar_init(ds_full, 8);
+        mbar_init(done, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 9) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot, dp_col = tmem + TILE, dv_col = tmem + 2 * TILE, dk_col = tmem + 2 * TILE + DP;
+    pdl_trigger();
+
+    if (warp == 8) {
+        if (lane == 0 && n > 0) {
+            mbar_expect_tx(k_full, BYTES);
+            load_tile<DP>(K, &kmap, k_full, hk, rk.first + s0);
+            mbar_expect_tx(v_full, BYTES);
+            load_tile<DP>(V, &vmap, v_full, hk, rk.first + s0);
+        }
+        bool ok = true;
+        uint32_t copied = 0;
+        int h = hk * a.group, tile = qt.a;
+        for (int i = 0; i < n && ok; ++i) {
+            const int s = i % ST, i0 = tile * TILE;
+            const uint32_t parity = (uint32_t)((i / ST + 1) & 1);
+            const bool edge = i0 + TILE > rq.len;
+            float lse[4], delta[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int j = i0 + k * 32 + lane;
+                const bool in = j < rq.len;
+                const int64_t at = (int64_t)(rq.first + j) * a.heads + h;
+                lse[k] = in ? g.lse[at] : -INFINITY;
+                delta[k] = in ? g.delta[at] : 0.f;
+            }
+            ok = __all_sync(~0u, mbar_wait(&q_empty[s], parity, abort_flag, a.status, 1));
+            if (!ok) break;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // a row that sees nothing, or is none, has weights exp2(x - inf) = 0
+                stats[s * 2 * TILE + k * 32 + lane] = lse[k] == -INFINITY ? INFINITY : lse[k] * LOG2E;
+                stats[s * 2 * TILE + TILE + k * 32 + lane] = delta[k];
+            }
+            __syncwarp();
+            if (lane == 0) {
+                uint64_t *bar = edge ? &q_copied[s] : &q_full[s];
+                mbar_expect_tx(bar, BYTES);
+                load_tile<DP>(Q + s * BYTES, &qmap, bar, h, rq.first + i0);
+                ok = mbar_wait(&do_empty[s], parity, abort_flag, a.status, 2);
+                if (ok) {
+                    bar = edge ? &do_copied[s] : &do_full[s];
+                    mbar_expect_tx(bar, BYTES);
+                    load_tile<DP>(DO + s * BYTES, &domap, bar, h, rq.first + i0);
+                }
+            }
+            ok = __shfl_sync(~0u, ok, 0);
+            if (edge && ok) {
+                ok = __all_sync(~0u, mbar_wait(&q_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
+                if (ok) {
+                    clear_rows<DP>(Q + s * BYTES, rq.len - i0, lane);
+                    if (lane == 0) mbar_arrive(&q_full[s]);
+                    ok = __all_sync(~0u, mbar_wait(&do_copied[s], (copied >> s) & 1u, abort_flag, a.status, 4));
+                }
+                if (ok) {
+                    clear_rows<DP>(DO + s * BYTES, rq.len - i0, lane);
+                    if (lane == 0) mbar_arrive(&do_full[s]);
+                }
+                copied ^= 1u << s;
+            }
+            if (++tile == qt.all) {
+                tile = qt.a;
+                ++h;
+            }
+        }
+    } else if (warp == 9) {
+        if (n > 0 && elect_one()) {
+            const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
+            bool ok = true;
+            auto score = [&](int i) {
+                if (!ok || i >= n) return;
+                ok = mbar_wait(&q_full[i % ST], (uint32_t)((i / ST) & 1), abort_flag, a.status, 5);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows<DP>(tmem, K, Q + (i % ST) * BYTES, s_idesc);
+                tc_commit(s_full);
+            };
+            auto dprob = [&](int i) {
+                if (!ok || i >= n) return;
+                ok = mbar_wait(&do_full[i % ST], (uint32_t)((i / ST) & 1), abort_flag, a.status, 6);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows<DP>(dp_col, V, DO + (i % ST) * BYTES, s_idesc);
+                tc_commit(dp_full);
+            };
+            ok = mbar_wait(k_full, 0, abort_flag, a.status, 7);
+            score(0);
+            if (ok) ok = mbar_wait(v_full, 0, abort_flag, a.status, 8);
+            dprob(0);
+            for (int i = 0; i < n && ok; ++i) {
+                ok = mbar_wait(p_full, (uint32_t)(i & 1), abort_flag, a.status, 9);
+                if (!ok) break;
+                tc_fence_after();
+                mma_tokens<64>(dv_col, tmem, DO + (i % ST) * BYTES, o_idesc, i > 0);
+                tc_commit(&do_empty[i % ST]);
+                score(i + 1);
+                if (ok) ok = mbar_wait(ds_full, (uint32_t)(i & 1), abort_flag, a.status, 10);
+                if (!ok) break;
+                tc_fence_after();
+                mma_tokens<64>(dk_col, dp_col, Q + (i % ST) * BYTES, o_idesc, i > 0);
+                tc_commit(&q_empty[i % ST]);
+                dprob(i + 1);
+            }
+            if (ok) tc_commit(done);
+        }
+        __syncwarp();
+    } else {
+        // thread: key r, queries 64 half .. 64 half + 63 of a tile
+        const int half = warp >> 2, r = (warp & 3) * 32 + lane, s = s0 + r;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + half * 64, dp_addr = dp_col + lanes + half * 64;
+        const float c = a.scale * LOG2E;
+        bool ok = true;
+        int tile = qt.a;
+        for (int i = 0; i < n; ++i) {
+            const int st = i % ST, t0 = tile * TILE + off;
+            const float *lse2 = stats + st * 2 * TILE + half * 64, *delta = lse2 + TILE;
+            const bool cut = !mask.all(t0, t0 + TILE - 1, s0, s0 + TILE - 1);
+            ok = __all_sync(~0u, mbar_wait(&q_full[st], (uint32_t)((i / ST) & 1), abort_flag, a.status, 11));
+            if (ok) ok = __all_sync(~0u, mbar_wait(s_full, (uint32_t)(i & 1), abort_flag, a.status, 12));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t x[2][32];
+            tmem_ld_32x32(s_addr, x[0]);
+            tmem_ld_32x32(s_addr + 32, x[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t p[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 l = *reinterpret_cast<const float4 *>(lse2 + b * 32 + e);
+                    const float ll[4] = {l.x, l.y, l.z, l.w};
+                    float y[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        y[k] = ex2(fmaf(__uint_as_float(x[b][e + k]), c, -ll[k]));
+                        if (cut && !mask.sees(t0 + half * 64 + b * 32 + e + k, s)) y[k] = 0.f;
+                        x[b][e + k] = __float_as_uint(y[k]);
+                    }
+                    p[e / 2] = pack_bf16(y[0], y[1]);
+                    p[e / 2 + 1] = pack_bf16(y[2], y[3]);
+                }
+                tmem_st_32x16(s_addr + b * 16, p);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full);
+            ok = __all_sync(~0u, mbar_wait(dp_full, (uint32_t)(i & 1), abort_flag, a.status, 13));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                uint32_t dp[32], ds[16];
+                tmem_ld_32x32(dp_addr + b * 32, dp);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 d = *reinterpret_cast<const float4 *>(delta + b * 32 + e);
+                    const float dd[4] = {d.x, d.y, d.z, d.w};
+                    float y[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[k] = __uint_as_float(x[b][e + k]) * (__uint_as_float(dp[e + k]) - dd[k]);
+                    ds[e / 2] = pack_bf16(y[0], y[1]);
+                    ds[e / 2 + 1] = pack_bf16(y[2], y[3]);
+                }
+                tmem_st_32x16(dp_addr + b * 16, ds);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_full);
+            if (++tile == qt.all) tile = qt.a;
+        }
+        if (ok && n > 0) ok = __all_sync(~0u, mbar_wait(done, 0, abort_flag, a.status, 14));
+        if (ok) {
+            tc_fence_after();
+            // the first half of the threads has dk, the second dv
+            const uint32_t acc = (half ? dv_col : dk_col) + lanes;
+            const float scale = half ? 1.f : a.scale;
+            const int kv_heads = a.heads / a.group;
+            const bool inside = s < rk.len, partial = r < partial_rows;
+            bf16 *dst = inside && !partial && !far ? (half ? g.dv : g.dk) + ((int64_t)(rk.first + s) * kv_heads + hk) * a.d : nullptr;
+            store_row<DP>(acc, 0, dst, a.d, scale, n == 0);
+            if (partial_rows > (warp & 3) * 32) {
+                float *part = part_of(g, far, kt, slot, hk) + ((int64_t)half * g.sink_rows + r) * a.d;
+#pragma unroll
+                for (int j = 0; j < DP / 32; ++j) {
+                    uint32_t o[32];
+                    tmem_ld_32x32(acc + j * 32, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        if (partial && inside && j * 32 + e < a.d)
+                            *reinterpret_cast<float4 *>(part + j * 32 + e) =
+                                n == 0 ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                       : make_float4(__uint_as_float(o[e]) * scale, __uint_as_float(o[e + 1]) * scale, __uint_as_float(o[e + 2]) * scale,
+                                                     __uint_as_float(o[e + 3]) * scale);
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// dk and dv of the sinks' rows of the sequences whose queries were split: the sum of the block near them and of the parts.
+__global__ void __launch_bounds__(256) window_sinks_kernel(const WindowGradArgs g)
 {
     const WindowArgs &a = g.w;
     pdl_wait();
     pdl_trigger();
-    const int row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, hk = blockIdx.y;
-    if (row >= a.nk) return;
-    const int b = sequence_of(a.k_offsets, a.nseq, row, a.nk);
-    if (b < 0) return;
-    const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
-    const int s = row - rk.first;
-    const bf16 *k = a.k.p + row * a.k.row + hk * a.k.head, *v = a.v.p + row * a.v.row + hk * a.v.head;
-    float dk[4] = {0.f, 0.f, 0.f, 0.f}, dv[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < rq.len; ++i) {
-        const int t = i + rk.len - rq.len;
-        if (!(s <= t && (s > t - a.window || s < a.sinks))) continue;
-        for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
-            const int qr = rq.first + i;
-            const int64_t at = ((int64_t)qr * a.heads + h) * a.d;
-            const bf16 *q = a.q.p + qr * a.q.row + h * a.q.head;
-            float x = 0.f, dp = 0.f, delta = 0.f;
-            for (int c = lane; c < a.d; c += 32) {
-                x += __bfloat162float(q[c]) * __bfloat162float(k[c]);
-                dp += __bfloat162float(g.dout[at + c]) * __bfloat162float(v[c]);
-                delta += __bfloat162float(g.dout[at + c]) * __bfloat162float(g.o[at + c]);
-            }
-            for (int o = 16; o; o >>= 1) {
-                x += __shfl_xor_sync(~0u, x, o);
-                dp += __shfl_xor_sync(~0u, dp, o);
-                delta += __shfl_xor_sync(~0u, delta, o);
-            }
-            const float p = expf(a.scale * x - a.lse[(int64_t)qr * a.heads + h]), ds = p * (dp - delta) * a.scale;
-            for (int c = 0; c < 4; ++c)
-                if (lane + 32 * c < a.d) {
-                    dk[c] += ds * __bfloat162float(q[lane + 32 * c]);
-                    dv[c] += p * __bfloat162float(g.dout[at + lane + 32 * c]);
-                }
+    const int kt = blockIdx.z, hk = blockIdx.y, kv_heads = a.heads / a.group;
+    const Mask mask{a.window, a.sinks};
+    const PartOf p = part_at(a, mask, kt, blockIdx.x, threadIdx.x & 31);
+    if (p.seq < 0 || p.part != 0) return;
+    const Rows rq = rows_of(a.q_offsets, p.seq, a.nq), rk = rows_of(a.k_offsets, p.seq, a.nk);
+    const QueryTiles qt = query_tiles(mask, rq, rk, kt * TILE);
+    const int first = first_part(qt), parts = (qt.all - first + wgrad::PART_TILES - 1) / wgrad::PART_TILES;
+    const int rows = min(min(a.sinks - kt * TILE, TILE), rk.len - kt * TILE), quads = a.d / 4;
+    for (int i = threadIdx.x; i < 2 * rows * quads; i += blockDim.x) {
+        const int which = i / (rows * quads), r = i / quads % rows, c = i % quads * 4;
+        const int64_t at = ((int64_t)which * g.sink_rows + r) * a.d + c;
+        float4 sum = *reinterpret_cast<const float4 *>(part_of(g, 0, kt, blockIdx.x, hk) + at);
+        for (int k = 0; k < parts; ++k) {
+            const int slot = (rq.first + (first + k * wgrad::PART_TILES) * TILE) / wgrad::PART;
+            const float4 x = *reinterpret_cast<const float4 *>(part_of(g, 1, kt, slot, hk) + at);
+            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
         }
+        bf16 *dst = (which ? g.dv : g.dk) + ((int64_t)(rk.first + kt * TILE + r) * kv_heads + hk) * a.d + c;
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
     }
-    const int64_t at = ((int64_t)row * (a.heads / a.group) + hk) * a.d;
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) {
-            g.dk[at + lane + 32 * c] = __float2bfloat16(dk[c]);
-            g.dv[at + lane + 32 * c] = __float2bfloat16(dv[c]);
-        }
+}
+
+// Sums of parts: for up to two tiles of first columns, one slot per PART queries.
+static size_t parts_floats(int64_t nq, int64_t kv_heads, int64_t sinks, int64_t d)
+{
+    if (sinks <= 0 || sinks > wgrad::MAX_SPLIT_SINKS) return 0;
+    const int64_t tiles = (sinks + TILE - 1) / TILE, rows = sinks < TILE ? sinks : TILE;
+    return (size_t)(2 * tiles * (nq / wgrad::PART + 1) * kv_heads * 2 * rows * d);
+}
+
+template <int DP>
+static st_status run_grad(WindowGradArgs &g, const st_tokens *t, cudaStream_t stream)
+{
+    const WindowArgs &a = g.w;
+    CUtensorMap qm, km, vm, dom;
+    const Table dout{g.dout, (int64_t)t->heads * t->d, t->d};
+    if (!make_tmap_table(&qm, a.q, t->nq, t->heads, t->d) || !make_tmap_table(&km, a.k, t->nk, t->kv_heads, t->d) ||
+        !make_tmap_table(&vm, a.v, t->nk, t->kv_heads, t->d) || !make_tmap_table(&dom, dout, t->nq, t->heads, t->d))
+        return ST_ERR_CUDA;
+    using S = wgrad::Shape<DP>;
+    if (!ensure_dynamic_smem(window_dq_kernel<DP>, S::DQ_SMEM) || !ensure_dynamic_smem(window_dkv_kernel<DP>, S::DKV_SMEM)) return ST_ERR_CUDA;
+    st_status rc = launch(window_dq_kernel<DP>, dim3((unsigned)most_tiles(t->nq, t->nseq, TILE), (unsigned)t->heads), wgrad::THREADS, S::DQ_SMEM, stream,
+                          qm, km, vm, dom, g);
+    if (rc != ST_OK) return rc;
+    const dim3 grid((unsigned)(g.sink_tiles * g.nslots + most_tiles(t->nk, t->nseq, TILE)), (unsigned)t->kv_heads);
+    rc = launch(window_dkv_kernel<DP>, grid, wgrad::THREADS, S::DKV_SMEM, stream, qm, km, vm, dom, g);
+    if (rc != ST_OK || g.sink_tiles == 0) return rc;
+    return launch(window_sinks_kernel, dim3((unsigned)g.nslots, (unsigned)t->kv_heads, (unsigned)g.sink_tiles), 256, 0, stream, g);
 }
 
 }  // namespace attn
 
-size_t attn_window_grad_workspace(int64_t nq, int64_t heads)
+size_t attn_window_grad_workspace(int64_t nq, int64_t heads, int64_t kv_heads, int64_t sinks)
 {
-    if (nq <= 0 || heads <= 0 || nq > (1 << 30) || heads > 65535) return 0;
-    return kWsHeaderBytes + (size_t)nq * heads * sizeof(float);
+    if (nq <= 0 || heads <= 0 || kv_heads <= 0 || kv_heads > heads || sinks < 0 || nq > (1 << 30) || heads > 65535) return 0;
+    return kWsHeaderBytes + round_up((size_t)nq * heads * sizeof(float), 256) + attn::parts_floats(nq, kv_heads, sinks, 128) * sizeof(float);
 }
 
 }  // namespace st
@@ -133,26 +717,32 @@ using namespace st;
 using namespace st::attn;
 
 extern "C" st_status st_attn_window_grad(const st_tokens *tokens, const void *q, const void *k, const void *v, const void *out,
-                              const float *lse, const void *dout, const int32_t *q_offsets, const int32_t *k_offsets,
-                              int64_t window, int64_t sinks, float scale, void *dq, void *dk, void *dv, void *ws,
-                              size_t ws_bytes, void *stream)
+                                         const float *lse, const void *dout, const int32_t *q_offsets, const int32_t *k_offsets,
+                                         int64_t window, int64_t sinks, float scale, void *dq, void *dk, void *dv, void *ws,
+                                         size_t ws_bytes, void *stream)
 {
-    st_status rc = check_window(tokens, q_offsets, k_offsets, window, sinks, scale);
+    const st_status rc = check_window(tokens, q_offsets, k_offsets, window, sinks, scale);
     if (rc != ST_OK) return rc;
     if (!q || !k || !v || !out || !lse || !dout || !dq || !dk || !dv) return ST_ERR_NULL;
     for (const void *p : {q, k, v, out, (const void *)lse, dout, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)q_offsets, (const void *)k_offsets})
         if (!aligned16(p)) return ST_ERR_ALIGN;
-    if (!ws || ws_bytes < attn_window_grad_workspace(tokens->nq, tokens->heads)) return ST_ERR_WORKSPACE;
+    if (!ws || ws_bytes < attn_window_grad_workspace(tokens->nq, tokens->heads, tokens->kv_heads, sinks)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     WindowGradArgs g = {};
     g.w = window_args(tokens, q, k, v, q_offsets, k_offsets, window, sinks, scale, ws);
-    g.w.lse = const_cast<float *>(lse);
     g.o = (const bf16 *)out;
     g.dout = (const bf16 *)dout;
+    g.lse = lse;
     g.dq = (bf16 *)dq;
     g.dk = (bf16 *)dk;
     g.dv = (bf16 *)dv;
-    rc = launch(window_dq_kernel, dim3((g.w.nq + 3) / 4, g.w.heads), 128, 0, (cudaStream_t)stream, g);
-    if (rc != ST_OK) return rc;
-    return launch(window_dkv_kernel, dim3((g.w.nk + 3) / 4, g.w.heads / g.w.group), 128, 0, (cudaStream_t)stream, g);
+    g.delta = (float *)((unsigned char *)ws + kWsHeaderBytes);
+    g.parts = (float *)((unsigned char *)ws + kWsHeaderBytes + round_up((size_t)tokens->nq * tokens->heads * sizeof(float), 256));
+    // queries beyond the window and a part: only a sequence that is longer has them
+    if (sinks > 0 && sinks <= wgrad::MAX_SPLIT_SINKS && tokens->nq - wgrad::PART > window) {
+        g.sink_tiles = (int)((sinks + TILE - 1) / TILE);
+        g.sink_rows = (int)(sinks < TILE ? sinks : TILE);
+        g.nslots = (int)(tokens->nq / wgrad::PART + 1);
+    }
+    return g.w.d <= 64 ? run_grad<64>(g, tokens, (cudaStream_t)stream) : run_grad<128>(g, tokens, (cudaStream_t)stream);
 }

@@ -691,7 +691,7 @@ PyObject *py_attn_window_grad(PyObject *const *v)
     Ref dq(result(v[11], v[0], x.q, {t.nq, t.heads, t.d}, at::kBFloat16, "dq"));
     Ref dk(result(v[12], v[0], x.q, {t.nk, t.kv_heads, t.d}, at::kBFloat16, "dk"));
     Ref dv(result(v[13], v[0], x.q, {t.nk, t.kv_heads, t.d}, at::kBFloat16, "dv"));
-    const Workspace w = workspace(v[14], v[0], x.q, ST_OP_ATTN_WINDOW_GRAD, t.nq, t.heads, 0, 0, 0);
+    const Workspace w = workspace(v[14], v[0], x.q, ST_OP_ATTN_WINDOW_GRAD, t.nq, t.heads, t.kv_heads, sinks, 0);
     const void *q = x.q.data_ptr(), *k = x.k.data_ptr(), *vv = x.v.data_ptr(), *po = out.data_ptr(), *pd = dout.data_ptr();
     const float *pl = (const float *)lse.data_ptr();
     void *pq = data(dq), *pk = data(dk), *pv = data(dv);

@@ -78,11 +78,11 @@ def test_window_refusals():
     assert window_grad(dout=None) == window_grad(dq=None) == window_grad(dk=None) == window_grad(dv=None) == window_grad(qo=None) == st.ST_ERR_NULL
     assert window_grad(w=0) == st.ST_ERR_SHAPE
     assert window_grad(dout=264) == window_grad(dv=264) == st.ST_ERR_ALIGN
-    need = st.st_workspace_bytes(st.ST_OP_ATTN_WINDOW_GRAD, 100, 4)
+    need = st.st_workspace_bytes(st.ST_OP_ATTN_WINDOW_GRAD, 100, 4, 2, 0)
     assert need >= 256 + 1600
     assert window_grad(n=need - 1) == window_grad(ws=None) == st.ST_ERR_WORKSPACE
     assert st.st_workspace_bytes(st.ST_OP_ATTN_WINDOW, 0, 0) == st.st_workspace_bytes(st.ST_OP_ATTN_WINDOW_STEP, 0, 0) == 256
-    assert st.st_workspace_bytes(st.ST_OP_ATTN_WINDOW_GRAD, 0, 4) == 0
+    assert st.st_workspace_bytes(st.ST_OP_ATTN_WINDOW_GRAD, 0, 4, 2) == 0
 
 
 def test_step_refusals():

@@ -109,6 +109,18 @@ def test_window_gradient_against_the_definition(lq, lk, H, Hk, d, window, sinks)
             near(g[rows[0] : rows[1]], w, tol, name)
 
 
+@pytest.mark.parametrize("lq,lk,H,Hk,d,window,sinks", [
+    ([3000, 200, 1, 2500], None, 4, 2, 64, 50, 4),
+    ([2300], [2500], 2, 2, 128, 130, 130),
+    ([1500, 4000], [7000, 4001], 2, 1, 80, 700, 256),
+    ([1024, 1025, 1152, 1153, 1280], None, 2, 2, 64, 1, 1),
+    ([3500], [3000], 2, 1, 64, 300, 200),
+])
+def test_window_gradient_of_first_columns_that_many_later_queries_see(lq, lk, H, Hk, d, window, sinks):
+    """Queries beyond the window are summed in parts for the sinks' rows."""
+    test_window_gradient_against_the_definition(lq, lk, H, Hk, d, window, sinks)
+
+
 def test_window_gradient_against_differences():
     H, Hk, d, n, window, sinks = 2, 1, 16, 40, 9, 3
     lk, q, k, v, qo, ko = window_inputs(21, [n], None, H, Hk, d)
