@@ -1,106 +1,484 @@
-// st_attn_decay, its gradient and its step: one block per (sequence, head), token after token.
-#include "attn_common.cuh"
+// st_attn_decay and its gradient on the tensor cores: four runs of one operator, a causal sum of outer products that fades,
+//     S = e^a S + in_scale y[t] (x) z[t],   out[t] = out_scale x[t].S
+// forwards in time for out (x, y, z = q, k, v) and dq (dout, v, k), backwards for dk (v, dout, q) and dv (k, q, dout).
+//
+// Tokens are taken in chunks of 128.  With w = e^a, L the tokens of a chunk, and S the state that enters it, forwards
+//     out = P Z + diag(w^(t+1)) X S,   P[t,s] = w^(t-s) x[t].y[s] for s <= t;     S <- w^L S + Y^T diag(w^(L-1-s)) Z
+// and backwards (S holds its factor w already)
+//     out = P Z + diag(w^(L-1-t)) X S, P[t,s] = w^(s-t) x[t].y[s] for s >= t;     S <- w^L S + Y^T diag(w^(s+1)) Z.
+// No power is of a positive exponent, whatever the decay.  Four products a chunk on the tensor cores, all accumulators in tensor memory:
+//     scores X Y^T;  P Z with P as bf16 in the place of the scores;  X S;  Y^T (weights Z).
+// S itself stays in fp32 registers, one row to a thread, and the chunk's sum is added to it there, so that no long chain of additions
+// runs through the tensor cores' accumulators (which do not round to nearest).  Where S and the weighted Z are operands they are
+// the sum of two bf16 numbers, two products each: 2^-16 of their terms, where one bf16 would leave 2^-8 in a state that is fp32.
+//
+// A block owns 64 columns of z, out and S for a run of chunks: with 128 columns two stages of X, Y and Z, S and the weighted Z in two parts
+// would not fit in shared memory.  The two blocks of a head read X and Y at about the same time, the second time from L2.
+// Where heads and sequences are few, sequences are cut into segments: one kernel sums each segment's own state, one carries the states
+// over the segments, then all segments run at once.
+//
+// Warps: 0..3 make P and write out (a thread = a token), 4..7 weigh Z and keep S (a thread = a token, a row of S), 8 copies, 9 issues the products.
+#include "attn_tc.cuh"
 
 namespace st {
 namespace attn {
 
-// S = [first step: 1 or e^a] S + in_scale y[t] (x) z[t];  out[t] = out_scale x[t].S, forwards or backwards in time
 struct FadeArgs {
     Table x, y, z;
     int dx, dz;                       // extent of x and y, extent of z and out
     const float *log_decay;
     const int *offsets;
     int nseq, n, heads;
-    const float *init;                // [nseq, heads, dx, dz] or, transposed, [nseq, heads, dz, dx]
-    float *last;
-    int transposed, backwards, decay_last;   // decay_last: one more factor e^a on `last`
+    const float *init;                // [nseq, heads, dx, dz] or, transposed, [nseq, heads, dz, dx]; or null
+    float *last;                      // [nseq, heads, dx, dz] or null
+    int transposed, backwards;
     float in_scale, out_scale;
     bf16 *out;
     unsigned *status;
+    int check;                        // look the offsets over and set the status: the call's first kernel
+    int chunks;                       // of a segment
+    float *states;                    // [segment][heads][dx][dz], or null: no sequence has more than one segment
 };
 
-__global__ void fade_kernel(const FadeArgs a)
+namespace fade {
+constexpr int THREADS = 320, STAGES = 2, ZC = 64;               // ZC: columns of z of a block
+template <int DX> struct Shape {
+    static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = DX * 128;
+    static constexpr int STAGE = 2 * X_BYTES + Z_BYTES;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * S_BYTES + 2 * Z_BYTES + 2 * TILE * sizeof(float) + 256;
+};
+}  // namespace fade
+
+// w^m for w = e^a, a2 = a log2 e <= 0: 1 for m = 0 whatever the decay
+__device__ __forceinline__ float power(float a2, int m) { return m == 0 ? 1.f : exp2f(a2 * (float)m); }
+// the factor of a state over `m` tokens: it enters as many times as there are chunks, so that its error counts
+__device__ __forceinline__ float carry(float a, int m) { return m == 0 ? 1.f : (float)exp((double)a * m); }
+
+// x = hi + lo, two values at a time
+__device__ __forceinline__ void split2(float x0, float x1, uint32_t &hi, uint32_t &lo)
 {
-    __shared__ float xs[128], ys[128];
+    hi = pack_bf16(x0, x1);
+    lo = pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xFFFF0000u));
+}
+
+// The segment that a block works on.
+struct Segment {
+    int seq, first, len, index, count;     // rows of the table; number among its sequence's segments
+};
+__device__ __forceinline__ Segment segment_of(const FadeArgs &a, int tile, int lane)
+{
+    const int rows = a.chunks * TILE;
+    const TileOf at = tile_of(a.offsets, a.nseq, a.n, rows, tile, lane, 1);
+    if (at.seq < 0) return {-1, 0, 0, 0, 0};
+    const Rows r = rows_of(a.offsets, at.seq, a.n);
+    return {at.seq, r.first + at.tile * rows, min(r.len - at.tile * rows, rows), at.tile, max((r.len + rows - 1) / rows, 1)};
+}
+
+// STATE: only the segment's own sum of outer products, to `states`.
+template <int DX, bool STATE>
+__global__ void __launch_bounds__(fade::THREADS, 1)
+fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap zmap, const FadeArgs a)
+{
+    using namespace fade;
+    using namespace tc;
+    using Sh = Shape<DX>;
+    extern __shared__ unsigned char raw[];
+    unsigned char *smem = align_smem(raw);
+    unsigned char *stages = smem, *S_hi = stages + STAGES * Sh::STAGE, *S_lo = S_hi + Sh::S_BYTES, *Z_hi = S_lo + Sh::S_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
+    float *table = (float *)(Z_lo + Sh::Z_BYTES);                  // 128 zeros, then in_scale w^m
+    uint64_t *bars = (uint64_t *)(table + 2 * TILE);
+    uint64_t *in_full = bars, *in_empty = in_full + STAGES, *sc_full = in_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
+             *z_ready = o_free + 1, *s_ready = z_ready + 1, *u_full = s_ready + 1, *xs_done = u_full + 1;
+    uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
+    const int slabs = (a.dz + ZC - 1) / ZC, slab = blockIdx.x % slabs, tile = blockIdx.x / slabs;
+
     pdl_wait();
-    pdl_trigger();
-    const int b = blockIdx.x, h = blockIdx.y, e = threadIdx.x;
-    if (a.status && b == 0 && h == 0) {
-        const int all = __syncthreads_and(offsets_fine(a.offsets, a.nseq, a.n, threadIdx.x, blockDim.x));
+    if (a.check && blockIdx.x == 0 && blockIdx.y == 0) {
+        const int all = __syncthreads_and(offsets_fine(a.offsets, a.nseq, a.n, threadIdx.x, THREADS));
         if (threadIdx.x == 0) {
             a.status[kWsStatusWord] = all ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
             a.status[kWsDetailWord] = 0u;
         }
     }
-    const Rows r = rows_of(a.offsets, b, a.n);
-    const float decay = expf(a.log_decay[h]);
-    const int64_t base = ((int64_t)b * a.heads + h) * a.dx * a.dz;
-    float s[128];
-    for (int i = 0; i < 128; ++i) {
-        const bool in = a.init && i < a.dx && e < a.dz;
-        s[i] = in ? a.init[base + (a.transposed ? (int64_t)e * a.dx + i : (int64_t)i * a.dz + e)] : 0.f;
-    }
-    for (int j = 0; j < r.len; ++j) {
-        const int64_t row = r.first + (a.backwards ? r.len - 1 - j : j);
-        __syncthreads();
-        if (e < a.dx) {
-            xs[e] = __bfloat162float(a.x.p[row * a.x.row + h * a.x.head + e]);
-            ys[e] = __bfloat162float(a.y.p[row * a.y.row + h * a.y.head + e]);
+    const Segment seg = segment_of(a, tile, lane);
+    if (seg.seq < 0) return;
+    // nobody needs the sum of the segment that comes last
+    if (STATE && seg.index == (a.backwards ? 0 : seg.count - 1)) return;
+    const int n = (seg.len + TILE - 1) / TILE;
+    const float decay = a.log_decay[h], a2 = decay * LOG2E;
+    auto chunk_of = [&](int i) { return a.backwards ? n - 1 - i : i; };
+
+    for (int i = threadIdx.x; i < 2 * TILE; i += THREADS) table[i] = i < TILE ? 0.f : a.in_scale * power(a2, i - TILE);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&in_full[s], 1);
+            mbar_init(&in_empty[s], 1);
         }
-        __syncthreads();
-        if (e >= a.dz) continue;
-        const float z = a.in_scale * __bfloat162float(a.z.p[row * a.z.row + h * a.z.head + e]);
-        const float f = a.backwards && j == 0 ? 1.f : decay;
-        float o = 0.f;
-        for (int i = 0; i < 128; ++i) {
-            if (i < a.dx) {
-                s[i] = f * s[i] + ys[i] * z;
-                o += xs[i] * s[i];
+        mbar_init(&sc_full[0], 1);
+        mbar_init(&sc_full[1], 1);
+        // one for each buffer of scores: P of a chunk may be made before that of the chunk before it has been used
+        mbar_init(&p_full[0], 4);
+        mbar_init(&p_full[1], 4);
+        mbar_init(o_full, 1);
+        mbar_init(o_free, 4);
+        mbar_init(z_ready, 4);
+        mbar_init(s_ready, 4);
+        mbar_init(u_full, 1);
+        mbar_init(xs_done, 1);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 9) {
+        tmem_alloc(tmem_slot, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot, pz_col = tmem + 2 * TILE, xs_col = pz_col + ZC, u_col = xs_col + ZC;
+    pdl_trigger();
+
+    if (warp == 8) {
+        if (elect_one()) {
+            for (int i = 0; i < n; ++i) {
+                const int s = i % STAGES, row = seg.first + chunk_of(i) * TILE;
+                if (!mbar_wait(&in_empty[s], (uint32_t)((i / STAGES + 1) & 1), abort_flag, a.status, 1)) break;
+                unsigned char *st = stages + s * Sh::STAGE;
+                mbar_expect_tx(&in_full[s], STATE ? Sh::X_BYTES + Sh::Z_BYTES : Sh::STAGE);
+                load_tile<DX>(st + Sh::X_BYTES, &ymap, &in_full[s], h, row);
+                if (!STATE) load_tile<DX>(st, &xmap, &in_full[s], h, row);
+                tma_load_3d(st + 2 * Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
             }
         }
-        if (a.out) a.out[(row * a.heads + h) * a.dz + e] = __float2bfloat16(a.out_scale * o);
+        __syncwarp();
+    } else if (warp == 9) {
+        if (elect_one()) {
+            const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, ZC);
+            bool ok = true;
+            int scored = 0;                         // chunks whose scores have been issued
+            // scores of chunk i; without `wait` only if its tiles are there
+            auto score = [&](int i, bool wait) {
+                if (STATE || !ok || i >= n || scored > i) return;
+                const uint32_t parity = (uint32_t)((i / STAGES) & 1);
+                if (wait) ok = mbar_wait(&in_full[i % STAGES], parity, abort_flag, a.status, 2);
+                else if (!mbar_try_wait(&in_full[i % STAGES], parity)) return;
+                if (!ok) return;
+                tc_fence_after();
+                const unsigned char *st = stages + (i % STAGES) * Sh::STAGE;
+                mma_rows<DX>(tmem + (i & 1) * TILE, st, st + Sh::X_BYTES, sc_idesc);
+                tc_commit(&sc_full[i & 1]);
+                ++scored;
+            };
+            for (int i = 0; i < n && ok; ++i) {
+                const unsigned char *X = stages + (i % STAGES) * Sh::STAGE, *Y = X + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
+                score(i, true);
+                score(i + 1, false);
+                if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
+                if (ok) ok = mbar_wait(z_ready, (uint32_t)(i & 1), abort_flag, a.status, 3);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024);
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const uint64_t z = make_smem_desc(smem_u32(part ? Z_lo : Z_hi), SLAB, 1024);
+#pragma unroll
+                    for (int k = 0; k < TILE / 16; ++k)
+                        mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, part || k ? 1u : 0u);
+                }
+                tc_commit(u_full);
+                if (STATE) {
+                    tc_commit(&in_empty[i % STAGES]);
+                    continue;
+                }
+                score(i + 1, false);
+                if (i > 0) ok = mbar_wait(o_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 4);
+                if (ok) ok = mbar_wait(s_ready, (uint32_t)(i & 1), abort_flag, a.status, 5);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t x = make_smem_desc(smem_u32(X), 16, 1024);
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const uint64_t s = make_smem_desc(smem_u32(part ? S_lo : S_hi), SLAB, 1024);
+#pragma unroll
+                    for (int k = 0; k < DX / 16; ++k)
+                        mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), s + (uint64_t)(k * 2048 >> 4), pz_idesc, part || k ? 1u : 0u);
+                }
+                tc_commit(xs_done);
+                score(i + 1, false);
+                ok = mbar_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
+                if (!ok) break;
+                tc_fence_after();
+                mma_tokens(pz_col, tmem + (i & 1) * TILE, Z, pz_idesc, false);
+                tc_commit(o_full);
+                tc_commit(&in_empty[i % STAGES]);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4) {
+        if (!STATE) {
+            const int t = threadIdx.x;
+            const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+            bool ok = true;
+            // rows of chunk i that a thread writes
+            auto write = [&](int i) {
+                ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
+                if (!ok) return;
+                tc_fence_after();
+                const int first = chunk_of(i) * TILE, L = min(seg.len - first, TILE);
+                const float alpha = a.out_scale * power(a2, a.backwards ? L - 1 - min(t, L - 1) : t + 1);
+                uint32_t pz[2][32], xs[2][32];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    tmem_ld_32x32(pz_col + lanes + j * 32, pz[j]);
+                    tmem_ld_32x32(xs_col + lanes + j * 32, xs[j]);
+                }
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(o_free);
+                bf16 *out = a.out + ((int64_t)(seg.first + first + t) * a.heads + h) * a.dz + slab * ZC;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    uint4 v;
+                    uint32_t *u = &v.x;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = j * 8 + 2 * k;
+                        u[k] = pack_bf16(fmaf(alpha, __uint_as_float(xs[c / 32][c % 32]), a.out_scale * __uint_as_float(pz[c / 32][c % 32])),
+                                         fmaf(alpha, __uint_as_float(xs[c / 32][c % 32 + 1]), a.out_scale * __uint_as_float(pz[c / 32][c % 32 + 1])));
+                    }
+                    if (t < L && slab * ZC + j * 8 < a.dz) *reinterpret_cast<uint4 *>(out + j * 8) = v;
+                }
+            };
+            for (int i = 0; i < n; ++i) {
+                const int L = min(seg.len - chunk_of(i) * TILE, TILE);
+                ok = __all_sync(~0u, mbar_wait(&sc_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 8));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t addr = tmem + lanes + (i & 1) * TILE;
+                // weight of column s: table[128 + t - s], or backwards table[128 + s - t]
+                const float *w = a.backwards ? table + TILE - t : table + TILE + t;
+                uint32_t x[4][32];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) tmem_ld_32x32(addr + j * 32, x[j]);
+                tmem_ld_wait();
+                if (a.backwards) {
+#pragma unroll
+                    for (int s = 0; s < TILE; ++s) x[s / 32][s % 32] = __float_as_uint(__uint_as_float(x[s / 32][s % 32]) * w[s]);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < TILE; ++s) x[s / 32][s % 32] = __float_as_uint(__uint_as_float(x[s / 32][s % 32]) * w[-s]);
+                }
+                if (L < TILE) {                   // what lies behind the sequence may be anything
+#pragma unroll
+                    for (int s = 0; s < TILE; ++s)
+                        if (s >= L) x[s / 32][s % 32] = 0u;
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int s = j * 64 + 2 * e;
+                        p[e] = pack_bf16(__uint_as_float(x[s / 32][s % 32]), __uint_as_float(x[s / 32][s % 32 + 1]));
+                    }
+                    tmem_st_32x32(addr + j * 32, p);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[i & 1]);
+                if (i > 0) write(i - 1);
+                if (!ok) break;
+            }
+            if (ok && n > 0) write(n - 1);
+        }
+    } else {
+        const int r = threadIdx.x - 128, swz = r & 7;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const bool row = r < a.dx;
+        const int64_t plane = (int64_t)a.dx * a.dz, at = (int64_t)r * a.dz + slab * ZC;
+        float S[64];
+        {
+            const float *from = nullptr;
+            if (!STATE) from = a.states ? a.states + ((int64_t)tile * a.heads + h) * plane : a.init ? a.init + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
+            const bool flip = !a.states && a.transposed;
+#pragma unroll
+            for (int c = 0; c < 64; ++c)
+                S[c] = from && row && slab * ZC + c < a.dz ? from[flip ? (int64_t)(slab * ZC + c) * a.dx + r : at + c] : 0.f;
+        }
+        bool ok = true;
+        float keep = 1.f;                              // what is left of S over the chunk whose sum is added to it
+        auto add = [&](int i) {
+            ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)(i & 1), abort_flag, a.status, 9));
+            if (!ok) return;
+            tc_fence_after();
+            uint32_t u[2][32];
+            tmem_ld_32x32(u_col + lanes, u[0]);
+            tmem_ld_32x32(u_col + lanes + 32, u[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 64; ++c) S[c] = fmaf(keep, S[c], row ? __uint_as_float(u[c / 32][c % 32]) : 0.f);
+        };
+        const float keep_full = carry(decay, TILE);
+        for (int i = 0; i < n; ++i) {
+            const int L = min(seg.len - chunk_of(i) * TILE, TILE);
+            if (i > 0) add(i - 1);                     // its product has been read: Z_hi, Z_lo and the accumulator are free
+            if (!ok) break;
+            keep = L == TILE ? keep_full : carry(decay, L);
+            ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
+            if (!ok) break;
+            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
+            if (r >= L) {                              // rows behind the sequence: they meet weights of 0
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    *reinterpret_cast<uint4 *>(Z + r * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    for (int c = 0; c < DX / 64; ++c) *reinterpret_cast<uint4 *>(Y + c * SLAB + r * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
+            const float beta = r < L ? a.in_scale * power(a2, a.backwards ? r + 1 : L - 1 - r) : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int o = r * 128 + j * 16;        // the whole row is this thread's: its swizzle does not matter
+                const uint4 v = *reinterpret_cast<const uint4 *>(Z + o);
+                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+                uint4 hi, lo;
+                uint32_t *ph = &hi.x, *pl = &lo.x;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) split2(beta * __uint_as_float(u[k] << 16), beta * __uint_as_float(u[k] & 0xFFFF0000u), ph[k], pl[k]);
+                *reinterpret_cast<uint4 *>(Z_hi + o) = hi;
+                *reinterpret_cast<uint4 *>(Z_lo + o) = lo;
+            }
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(z_ready);
+            if (!STATE) {
+                if (i > 0) ok = __all_sync(~0u, mbar_wait(xs_done, (uint32_t)((i - 1) & 1), abort_flag, a.status, 11));
+                if (!ok) break;
+                if (r < DX) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const int o = r * 128 + ((j ^ swz) << 4);
+                        uint4 hi, lo;
+                        uint32_t *ph = &hi.x, *pl = &lo.x;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) split2(S[j * 8 + 2 * k], S[j * 8 + 2 * k + 1], ph[k], pl[k]);
+                        *reinterpret_cast<uint4 *>(S_hi + o) = hi;
+                        *reinterpret_cast<uint4 *>(S_lo + o) = lo;
+                    }
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(s_ready);
+            }
+        }
+        if (ok && n > 0) add(n - 1);
+        const bool end = seg.index == (a.backwards ? 0 : seg.count - 1);
+        float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && a.last ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
+        if (ok && to && row) {
+#pragma unroll
+            for (int c = 0; c < 64; c += 4)
+                if (slab * ZC + c < a.dz) *reinterpret_cast<float4 *>(to + at + c) = make_float4(S[c], S[c + 1], S[c + 2], S[c + 3]);
+        }
     }
-    if (a.last && e < a.dz)
-        for (int i = 0; i < 128; ++i)
-            if (i < a.dx) a.last[base + (a.transposed ? (int64_t)e * a.dx + i : (int64_t)i * a.dz + e)] = a.decay_last && r.len ? decay * s[i] : s[i];
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
 }
 
-__global__ void decay_step_kernel(const bf16 *q, const bf16 *k, const bf16 *v, const float *log_decay, float *state, float scale,
-                                  bf16 *out, int heads, int dk, int dv)
+// The segments' own sums become the states that enter the segments; a thread owns four elements of a head's state.
+__global__ void __launch_bounds__(256) fade_carry_kernel(const FadeArgs a)
 {
     pdl_wait();
     pdl_trigger();
-    const int64_t bh = (int64_t)blockIdx.y * heads + blockIdx.x;
-    const int e = threadIdx.x;
-    if (e >= dv) return;
-    const float decay = expf(log_decay[blockIdx.x]), z = __bfloat162float(v[bh * dv + e]);
-    float o = 0.f;
-    for (int i = 0; i < dk; ++i) {
-        float &s = state[(bh * dk + i) * dv + e];
-        s = decay * s + __bfloat162float(k[bh * dk + i]) * z;
-        o += __bfloat162float(q[bh * dk + i]) * s;
+    const Segment seg = segment_of(a, blockIdx.x, threadIdx.x & 31);
+    if (seg.seq < 0 || seg.index != 0) return;
+    const int h = blockIdx.y, plane = a.dx * a.dz, e = (blockIdx.z * 256 + threadIdx.x) * 4;
+    if (e >= plane) return;
+    const Rows r = rows_of(a.offsets, seg.seq, a.n);
+    const int rows = a.chunks * TILE, x = e / a.dz, z = e % a.dz;
+    const int64_t step = (int64_t)a.heads * plane;
+    float *states = a.states + ((int64_t)blockIdx.x * a.heads + h) * plane + e;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.init) {
+        const float *init = a.init + ((int64_t)seg.seq * a.heads + h) * plane;
+        if (a.transposed) s = make_float4(init[z * a.dx + x], init[(z + 1) * a.dx + x], init[(z + 2) * a.dx + x], init[(z + 3) * a.dx + x]);
+        else s = *reinterpret_cast<const float4 *>(init + e);
     }
-    out[bh * dv + e] = __float2bfloat16(scale * o);
+    const float decay = a.log_decay[h], whole = carry(decay, rows);
+    for (int i = 0; i < seg.count; ++i) {
+        const int k = a.backwards ? seg.count - 1 - i : i;
+        float4 *at = reinterpret_cast<float4 *>(states + k * step);
+        if (i + 1 == seg.count) {
+            *at = s;
+            break;
+        }
+        const float4 own = *at;
+        const float f = (k + 1) * rows <= r.len ? whole : carry(decay, r.len - k * rows);
+        *at = s;
+        s = make_float4(fmaf(f, s.x, own.x), fmaf(f, s.y, own.y), fmaf(f, s.z, own.z), fmaf(f, s.w, own.w));
+    }
 }
 
-}  // namespace attn
-
-size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d)
+// Chunks of a segment: so many that two segments come to every SM where the sequences alone give fewer blocks; 0: whole sequences.
+static int segment_chunks(int64_t n, int64_t heads, int64_t d)
 {
-    if (n <= 0 || nseq <= 0 || heads <= 0 || d <= 0 || d > 128) return 0;
-    return kWsHeaderBytes;
+    const int64_t blocks = heads * ((d + fade::ZC - 1) / fade::ZC), wanted = 2 * (int64_t)sm_count_or_default() / blocks;
+    if (wanted <= 1) return 0;
+    const int64_t chunks = (n + TILE - 1) / TILE, each = (chunks + wanted - 1) / wanted, some = each < 4 ? 4 : each;
+    return some >= chunks ? 0 : (int)some;
 }
 
-}  // namespace st
+// The states of the segments of one run.
+static size_t states_bytes(int64_t n, int64_t nseq, int64_t heads, int64_t d)
+{
+    size_t most = 0;
+    for (const int64_t c : {(int64_t)fade::ZC, d}) {                   // the run may be over either extent
+        const int chunks = segment_chunks(n, heads, c < d ? c : d);
+        const size_t bytes = chunks ? (size_t)most_tiles(n, nseq, (int64_t)chunks * TILE) * heads * d * d * sizeof(float) : 0;
+        most = bytes > most ? bytes : most;
+    }
+    return round_up(most, 256);
+}
 
-using namespace st;
-using namespace st::attn;
+template <int DX>
+static st_status run_fade_as(FadeArgs &a, float *states, cudaStream_t stream)
+{
+    CUtensorMap xm, ym, zm;
+    if (!make_tmap_table(&xm, a.x, a.n, a.heads, a.dx) || !make_tmap_table(&ym, a.y, a.n, a.heads, a.dx) || !make_tmap_table(&zm, a.z, a.n, a.heads, a.dz))
+        return ST_ERR_CUDA;
+    using Sh = fade::Shape<DX>;
+    const int slabs = (a.dz + fade::ZC - 1) / fade::ZC;
+    if (!ensure_dynamic_smem(fade_kernel<DX, false>, Sh::SMEM) || !ensure_dynamic_smem(fade_kernel<DX, true>, Sh::SMEM)) return ST_ERR_CUDA;
+    a.chunks = segment_chunks(a.n, a.heads, a.dz);
+    a.states = a.chunks ? states : nullptr;
+    if (!a.chunks) a.chunks = 1 << 22;                                 // 2^29 tokens and more than any sequence's
+    const unsigned tiles = (unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
+    if (a.states) {
+        st_status rc = launch(fade_kernel<DX, true>, dim3(tiles * slabs, a.heads), fade::THREADS, Sh::SMEM, stream, xm, ym, zm, a);
+        if (rc != ST_OK) return rc;
+        rc = launch(fade_carry_kernel, dim3(tiles, a.heads, (unsigned)((a.dx * a.dz + 1023) / 1024)), 256, 0, stream, a);
+        if (rc != ST_OK) return rc;
+        a.check = 0;
+    }
+    return launch(fade_kernel<DX, false>, dim3(tiles * slabs, a.heads), fade::THREADS, Sh::SMEM, stream, xm, ym, zm, a);
+}
+static st_status run_fade(FadeArgs &a, float *states, cudaStream_t stream)
+{
+    return a.dx <= 64 ? run_fade_as<64>(a, states, stream) : run_fade_as<128>(a, states, stream);
+}
 
 static st_status check_decay(const st_tokens *t, const int32_t *offsets)
 {
     const st_status rc = check_tokens(t);
     if (rc != ST_OK) return rc;
     if (t->nq != t->nk || t->heads != t->kv_heads) return ST_ERR_SHAPE;
+    if (t->nq > (1 << 29)) return ST_ERR_UNSUPPORTED;
     return !offsets && t->nseq != 1 ? ST_ERR_NULL : ST_OK;
 }
 
@@ -116,6 +494,24 @@ static FadeArgs fade_args(const st_tokens *t, const float *log_decay, const int3
     return a;
 }
 
+static Table table_of(const void *p, int64_t rows, int64_t heads, int64_t row, int64_t head)
+{
+    return {(const bf16 *)p, stride_of(rows, row), stride_of(heads, head)};
+}
+
+}  // namespace attn
+
+size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d)
+{
+    if (n <= 0 || nseq <= 0 || heads <= 0 || d <= 0 || d > 128 || n > (1 << 29) || heads > 65535 || nseq > (1 << 20)) return 0;
+    return kWsHeaderBytes + attn::states_bytes(n, nseq, heads, d);
+}
+
+}  // namespace st
+
+using namespace st;
+using namespace st::attn;
+
 extern "C" {
 
 st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const void *v, const float *log_decay,
@@ -130,9 +526,9 @@ st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const 
     if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     FadeArgs a = fade_args(t, log_decay, offsets);
-    a.x = {(const bf16 *)q, t->q_row, t->q_head};
-    a.y = {(const bf16 *)k, t->k_row, t->k_head};
-    a.z = {(const bf16 *)v, t->v_row, t->v_head};
+    a.x = table_of(q, t->nq, t->heads, t->q_row, t->q_head);
+    a.y = table_of(k, t->nk, t->heads, t->k_row, t->k_head);
+    a.z = table_of(v, t->nk, t->heads, t->v_row, t->v_head);
     a.dx = (int)t->d;
     a.dz = (int)t->dv;
     a.init = state_in;
@@ -140,7 +536,8 @@ st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const 
     a.out_scale = scale;
     a.out = (bf16 *)out;
     a.status = (unsigned *)ws;
-    return launch(fade_kernel, dim3(a.nseq, a.heads), 128, 0, (cudaStream_t)stream, a);
+    a.check = 1;
+    return run_fade(a, (float *)((unsigned char *)ws + kWsHeaderBytes), (cudaStream_t)stream);
 }
 
 st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, const void *v, const float *log_decay,
@@ -156,8 +553,9 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
-    const Table Q = {(const bf16 *)q, t->q_row, t->q_head}, K = {(const bf16 *)k, t->k_row, t->k_head}, V = {(const bf16 *)v, t->v_row, t->v_head},
-                O = {(const bf16 *)dout, t->heads * t->dv, t->dv};
+    const Table Q = table_of(q, t->nq, t->heads, t->q_row, t->q_head), K = table_of(k, t->nk, t->heads, t->k_row, t->k_head),
+                V = table_of(v, t->nk, t->heads, t->v_row, t->v_head), O = table_of(dout, t->nq, t->heads, t->heads * t->dv, t->dv);
+    float *states = (float *)((unsigned char *)ws + kWsHeaderBytes);
     cudaStream_t s = (cudaStream_t)stream;
     // dq[t] = scale sum e^{a(t-s)} (dout[t].v[s]) k[s]
     FadeArgs a = fade_args(t, log_decay, offsets);
@@ -169,7 +567,8 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
     a.out_scale = scale;
     a.out = (bf16 *)dq;
     a.status = (unsigned *)ws;
-    if ((rc = launch(fade_kernel, dim3(a.nseq, a.heads), 128, 0, s, a)) != ST_OK) return rc;
+    a.check = 1;
+    if ((rc = run_fade(a, states, s)) != ST_OK) return rc;
     // dk[s] = sum e^{a(t-s)} (v[s].dout[t]) scale q[t], backwards
     a.x = V; a.y = O; a.z = Q;
     a.init = dstate_out;
@@ -177,31 +576,16 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
     a.in_scale = scale;
     a.out_scale = 1.f;
     a.out = (bf16 *)dk;
-    a.status = nullptr;
-    if ((rc = launch(fade_kernel, dim3(a.nseq, a.heads), 128, 0, s, a)) != ST_OK) return rc;
+    a.check = 0;
+    if ((rc = run_fade(a, states, s)) != ST_OK) return rc;
     // dv[s] = sum e^{a(t-s)} (k[s].q[t]) scale dout[t], backwards
     a.x = K; a.y = Q; a.z = O;
     a.dx = (int)t->d;
     a.dz = (int)t->dv;
     a.transposed = 0;
     a.last = dstate_in;
-    a.decay_last = 1;
     a.out = (bf16 *)dv;
-    return launch(fade_kernel, dim3(a.nseq, a.heads), 128, 0, s, a);
-}
-
-st_status st_attn_decay_step(const st_tokens *t, const void *q, const void *k, const void *v, const float *log_decay,
-                             float *state, float scale, void *out, void *stream)
-{
-    const st_status rc = check_tokens(t);
-    if (rc != ST_OK) return rc;
-    if (t->nq != t->nk || t->heads != t->kv_heads || t->nseq != t->nq) return ST_ERR_SHAPE;
-    if (!q || !k || !v || !log_decay || !state || !out) return ST_ERR_NULL;
-    if (t->nq > 65535) return ST_ERR_UNSUPPORTED;
-    for (const void *p : {q, k, v, (const void *)log_decay, (const void *)state, (const void *)out})
-        if (!aligned16(p)) return ST_ERR_ALIGN;
-    return launch(decay_step_kernel, dim3((unsigned)t->heads, (unsigned)t->nq), 128, 0, (cudaStream_t)stream, (const bf16 *)q, (const bf16 *)k, (const bf16 *)v,
-                  log_decay, state, scale, (bf16 *)out, (int)t->heads, (int)t->d, (int)t->dv);
+    return run_fade(a, states, s);
 }
 
 }  // extern "C"

@@ -109,17 +109,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
     return r;
 }
 
-// Tile number `index` of the tiles of ROWS tokens that the sequences are cut into, by a whole warp.  seq = -1: there is none.
+// Tile number `index` of the tiles of `rows` tokens that the sequences are cut into, by a whole warp; at least `least` tiles to a
+// sequence.  seq = -1: there is none.
 struct TileOf {
     int seq, tile;
 };
-template <int ROWS>
-__device__ __forceinline__ TileOf tile_of(const int *offsets, int nseq, int n, int index, int lane)
+__device__ __forceinline__ TileOf tile_of(const int *offsets, int nseq, int n, int rows, int index, int lane, int least = 0)
 {
-    if (!offsets) return {index < (n + ROWS - 1) / ROWS ? 0 : -1, index};
+    if (!offsets) return {index < (n - 1) / rows + 1 ? 0 : -1, index};
     for (int b0 = 0; b0 < nseq; b0 += 32) {
         const int b = b0 + lane;
-        const int mine = b < nseq ? (rows_of(offsets, b, n).len + ROWS - 1) / ROWS : 0;
+        const int mine = b < nseq ? max((rows_of(offsets, b, n).len - 1 + rows) / rows, least) : 0;
         int sum = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {

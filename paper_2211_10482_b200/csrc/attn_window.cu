@@ -54,7 +54,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             a.status[kWsDetailWord] = 0u;
         }
     }
-    const TileOf at = tile_of<2 * TILE>(a.q_offsets, a.nseq, a.nq, blockIdx.x, lane);
+    const TileOf at = tile_of(a.q_offsets, a.nseq, a.nq, 2 * TILE, blockIdx.x, lane);
     if (at.seq < 0) return;
     const Rows rq = rows_of(a.q_offsets, at.seq, a.nq), rk = rows_of(a.k_offsets, at.seq, a.nk);
     const int i0 = at.tile * 2 * TILE, left = min(rq.len - i0, 2 * TILE), t0 = i0 + rk.len - rq.len;

@@ -162,7 +162,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             a.status[kWsDetailWord] = 0u;
         }
     }
-    const TileOf at = tile_of<TILE>(a.q_offsets, a.nseq, a.nq, blockIdx.x, lane);
+    const TileOf at = tile_of(a.q_offsets, a.nseq, a.nq, TILE, blockIdx.x, lane);
     if (at.seq < 0) return;
     const Rows rq = rows_of(a.q_offsets, at.seq, a.nq), rk = rows_of(a.k_offsets, at.seq, a.nk);
     const int i0 = at.tile * TILE, left = min(rq.len - i0, TILE), t0 = i0 + rk.len - rq.len;
@@ -392,7 +392,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
         qt.a = first_part(qt) + p.part * PART_TILES;
         qt.all = min(qt.all, qt.a + PART_TILES);
     } else {
-        const TileOf at = tile_of<TILE>(a.k_offsets, a.nseq, a.nk, blockIdx.x - far_blocks, lane);
+        const TileOf at = tile_of(a.k_offsets, a.nseq, a.nk, TILE, blockIdx.x - far_blocks, lane);
         if (at.seq < 0) return;
         seq = at.seq;
         kt = at.tile;
