@@ -361,8 +361,9 @@ typedef struct {
 /* st_attn_window for one new token of every sequence: lens[b] counts the tokens of sequence b with the new one, whose
  * key and value (k, v: [nseq, kv_heads, d]) are written to the cache at position lens[b]-1; out = attention of q
  * ([nseq, heads, d], position lens[b]-1) over the cache and the new token.  All contiguous but the cache.  lens[b] = 0: out = 0,
- * nothing written.  A length beyond the table's row, and a page number outside the cache, are reported (ST_ERR_DEV_BOUNDS); the
- * tokens concerned are left out.  Two sequences may share pages that neither writes. */
+ * nothing written.  Only table entries of visible tokens and of the new one are read.  A length beyond the table's row
+ * (cut to it), a negative one (0), and a page number outside the cache where a visible token lies (the token is left out)
+ * are reported: ST_ERR_DEV_BOUNDS.  Two sequences may share pages that neither writes. */
 st_status st_attn_window_step(const st_cache *cache, const void *q, const void *k, const void *v, void *k_pages,
                               void *v_pages, const int32_t *table, const int32_t *lens, int64_t window, int64_t sinks,
                               float scale, void *out, void *ws, size_t ws_bytes, void *stream);

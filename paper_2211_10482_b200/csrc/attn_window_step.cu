@@ -1,5 +1,16 @@
-// st_attn_window_step: one warp per (sequence, head), key after key.
+// st_attn_window_step: one new token of every sequence against a cache in pages.
+//
+// Bound by the cache's bytes: every visible row of K and V is read once for all query heads that share it.  A cluster of blocks owns
+// one key head of one sequence (and 16 of its query heads); its warps take tiles of 16 visible keys in turn.  Each warp copies its own
+// tiles to its own ring in shared memory (cp.async, two tiles ahead; page numbers one tile further), so that no barrier lies in the loop,
+// and multiplies with mma.sync: the 16 rows of the fragments are query heads, of which a group of 1 to 16 is filled.  The tensor
+// cores of tcgen05 would need 128 rows, and 2 to 32 flops a byte need no more than a tenth of mma.sync's rate.
+// Rows that are not visible are never read: their place in shared memory is zeroed by the copy.
+//
+// Warps, then blocks of the cluster, join their maxima, sums and outputs in shared memory, the blocks over distributed shared
+// memory: one launch and no workspace however the keys are split.
 #include "attn_common.cuh"
+#include "tc_common.cuh"
 
 namespace st {
 namespace attn {
@@ -15,51 +26,315 @@ struct StepArgs {
     unsigned *status;
 };
 
-__global__ void window_step_kernel(const StepArgs a)
+namespace wstep {
+constexpr int WARPS = 4, KEYS = 16, HEADS = 16, STAGES = 3;
+template <int DP> struct Shape {
+    static constexpr int TILE_BYTES = KEYS * DP * 2, STAGE = 2 * TILE_BYTES, RING = STAGES * STAGE;
+    static constexpr size_t SMEM = (size_t)WARPS * RING + 2 * (WARPS + 1) * HEADS * sizeof(float) + 16;
+    static_assert(HEADS * DP * 4 <= RING, "a warp's output takes the place of its ring");
+};
+}  // namespace wstep
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there)
 {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ld_cluster(uint32_t addr)
+{
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(addr) : "memory");
+    return x;
+}
+
+template <int DP>
+__global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const StepArgs a)
+{
+    using namespace wstep;
+    using S = Shape<DP>;
+    constexpr int CHUNKS = DP / 8;                        // 16-byte pieces of a row
+    extern __shared__ __align__(128) unsigned char smem[];
+    float *most_w = (float *)(smem + WARPS * S::RING), *sum_w = most_w + WARPS * HEADS, *most_b = sum_w + WARPS * HEADS, *sum_b = most_b + HEADS;
+    int *bad = (int *)(sum_b + HEADS);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int splits = gridDim.x, split = blockIdx.x, chunks = (a.group + HEADS - 1) / HEADS, b = blockIdx.z;
+    const int hk = blockIdx.y / chunks, g0 = blockIdx.y % chunks * HEADS, g = min(a.group - g0, HEADS), kv_heads = a.heads / a.group;
+
+    if (threadIdx.x == 0) *bad = 0;
     pdl_wait();
-    pdl_trigger();
-    const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x, hk = h / a.group, hkn = a.heads / a.group;
-    if (h == 0 && b == 0) {
-        bool fine = true;
-        for (int i = 0; i < a.nseq; ++i) {
-            const int n = a.lens[i];
-            fine = fine && n >= 0 && (int64_t)n <= (int64_t)a.cols * a.page;
-            for (int c = lane; c < min(a.cols, (n + a.page - 1) / a.page); c += 32) fine = fine && (unsigned)a.table[(int64_t)i * a.cols + c] < (unsigned)a.pages;
-        }
-        fine = __all_sync(~0u, fine);
-        if (lane == 0) {
-            a.status[kWsStatusWord] = fine ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
-            a.status[kWsDetailWord] = 0u;
-        }
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
+        // an error is reported 100 us after its block began, which was not before this one (see the end)
+        a.status[kWsStatusWord] = 0;
+        a.status[kWsDetailWord] = 0;
     }
-    const int len = (int)min((int64_t)max(a.lens[b], 0), (int64_t)a.cols * a.page), t = len - 1;
-    const bf16 *q = a.q + ((int64_t)b * a.heads + h) * a.d;
-    const bf16 *kn = a.k + ((int64_t)b * hkn + hk) * a.d, *vn = a.v + ((int64_t)b * hkn + hk) * a.d;
-    float most = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s <= t; ++s) {
-        if (!(s > t - a.window || s < a.sinks)) continue;
-        const int p = a.table[(int64_t)b * a.cols + s / a.page];
-        if ((unsigned)p >= (unsigned)a.pages) continue;
-        const int64_t at = p * a.page_stride + (s % a.page) * a.token_stride + hk * a.head_stride;
-        const bf16 *k = s == t ? kn : a.k_pages + at, *v = s == t ? vn : a.v_pages + at;
-        if (s == t && h % a.group == 0)
-            for (int c = lane; c < a.d; c += 32) {
-                a.k_pages[at + c] = kn[c];
-                a.v_pages[at + c] = vn[c];
+    __syncthreads();
+    const int told = a.lens[b], len = (int)min((int64_t)max(told, 0), (int64_t)a.cols * a.page), t = len - 1;
+    if (told != len && threadIdx.x == 0) *bad = 1;
+    // visible keys: [0, first) and [lo, t]; key number u of them
+    const int lo = max(0, t - a.window + 1), first = min(a.sinks, lo), seen = first + t + 1 - lo, tiles = (seen + KEYS - 1) / KEYS;
+    const bf16 *kn = a.k + ((int64_t)b * kv_heads + hk) * a.d, *vn = a.v + ((int64_t)b * kv_heads + hk) * a.d;
+    const bf16 *kc = a.k_pages + hk * a.head_stride, *vc = a.v_pages + hk * a.head_stride;
+    const uint32_t ring = tc::smem_u32(smem + warp * S::RING);
+    const int step = splits * WARPS, tile0 = split * WARPS + warp;
+
+    // the queries as fragments: row = head
+    uint32_t q[DP / 16][4];
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = lane / 4 + (i & 1) * 8, col = k * 16 + (lane & 3) * 2 + (i >> 1) * 8;
+            q[k][i] = row < g && col < a.d ? *reinterpret_cast<const uint32_t *>(a.q + ((int64_t)b * a.heads + hk * a.group + g0 + row) * a.d + col) : 0u;
+        }
+
+    // Lane r (of 16) knows where row r of a tile lies: the page's number (-1: none, -2: the new token), and the place in the page.
+    auto place = [&](int tile, int &page, int &slot) {
+        const int u = tile * KEYS + (lane & 15), s = u < first ? u : lo + u - first;
+        page = -1;
+        slot = 0;
+        if (u < seen) {
+            const int p = s / a.page;
+            slot = s - p * a.page;
+            page = a.table[(int64_t)b * a.cols + p];
+            if ((unsigned)page >= (unsigned)a.pages) {
+                page = -1;
+                *bad = 1;
+            } else if (s == t) {
+                page = -2;
             }
-        float x = 0.f;
-        for (int c = lane; c < a.d; c += 32) x += __bfloat162float(q[c]) * __bfloat162float(k[c]);
-        for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-        x *= a.scale;
-        const float m = fmaxf(most, x), old = expf(most - m), w = expf(x - m);
-        sum = sum * old + w;
-        most = m;
-        for (int c = 0; c < 4; ++c)
-            if (lane + 32 * c < a.d) acc[c] = acc[c] * old + w * __bfloat162float(v[lane + 32 * c]);
+        }
+    };
+    // bit r: row r of the tile is there
+    auto fetch = [&](int tile, int stage, int page, int slot) -> unsigned {
+        const int64_t at = (int64_t)max(page, 0) * a.page_stride + slot * a.token_stride;
+        const uint32_t dst = ring + stage * S::STAGE;
+        const unsigned there = __ballot_sync(~0u, page != -1) & 0xFFFFu, fresh = __ballot_sync(~0u, page == -2);
+        if (tile < tiles) {
+#pragma unroll
+            for (int i = 0; i < KEYS * CHUNKS / 32; ++i) {
+                const int row = (i * 32 + lane) / CHUNKS, c = (i * 32 + lane) % CHUNKS;
+                const int64_t from = __shfl_sync(~0u, at, row);
+                const bool in = (there >> row & 1) && c * 8 < a.d, is_new = fresh >> row & 1;
+                const uint32_t o = dst + row * (DP * 2) + ((c ^ (row & 7)) << 4);
+                copy16(o, in ? (is_new ? kn : kc + from) + c * 8 : a.q, in);
+                copy16(o + S::TILE_BYTES, in ? (is_new ? vn : vc + from) + c * 8 : a.q, in);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        return there;
+    };
+
+    const float c = a.scale * 1.4426950408889634f;
+    float o[DP / 8][4], most[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+    unsigned there[STAGES];
+    int page, slot;
+    place(tile0, page, slot);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        const int p = page, l = slot;
+        place(tile0 + (s + 1) * step, page, slot);
+        there[s] = fetch(tile0 + s * step, s, p, l);
     }
-    for (int c = 0; c < 4; ++c)
-        if (lane + 32 * c < a.d) a.out[((int64_t)b * a.heads + h) * a.d + lane + 32 * c] = __float2bfloat16(sum > 0.f ? acc[c] / sum : 0.f);
+    // the new token's row of the cache; nobody reads it there in this call
+    if (split == 0 && warp == 0 && g0 == 0 && len > 0) {
+        const int p = a.table[(int64_t)b * a.cols + t / a.page];
+        if ((unsigned)p < (unsigned)a.pages && lane * 8 < 2 * DP) {
+            const int col = lane * 8 % DP;
+            const int64_t at = (int64_t)p * a.page_stride + (t % a.page) * a.token_stride + hk * a.head_stride + col;
+            if (col < a.d) *reinterpret_cast<uint4 *>((lane * 8 < DP ? a.k_pages : a.v_pages) + at) = *reinterpret_cast<const uint4 *>((lane * 8 < DP ? kn : vn) + col);
+        }
+    }
+    int stage = 0;
+    for (int tile = tile0; tile < tiles; tile += step) {
+        {
+            const int p = page, l = slot, s = stage == 0 ? STAGES - 1 : stage - 1;
+            place(tile + STAGES * step, page, slot);
+            __syncwarp();                                  // every lane is done with the stage that is filled again
+            there[STAGES - 1] = fetch(tile + (STAGES - 1) * step, s, p, l);
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+        __syncwarp();
+        const uint32_t K = ring + stage * S::STAGE, V = K + S::TILE_BYTES;
+        float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int k = 0; k < DP / 32; ++k) {
+                uint32_t f[4];                             // 8 keys, 32 columns
+                const int row = n * 8 + (lane & 7), ch = k * 4 + lane / 8;
+                ldmatrix4(f, K + row * (DP * 2) + ((ch ^ (row & 7)) << 4));
+                mma16816(x[n], q[2 * k], f[0], f[1]);
+                mma16816(x[n], q[2 * k + 1], f[2], f[3]);
+            }
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!(there[0] >> (n * 8 + (lane & 3) * 2 + (i & 1)) & 1)) x[n][i] = -INFINITY;
+                top[i >> 1] = fmaxf(top[i >> 1], x[n][i]);
+            }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 1));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 2));
+        }
+        if (__any_sync(~0u, top[0] > most[0] || top[1] > most[1])) {
+            float f[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float now = fmaxf(most[i], top[i]);
+                f[i] = now == -INFINITY ? 1.f : exp2f(c * (most[i] - now));
+                most[i] = now;
+                sum[i] *= f[i];
+            }
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[n][i] *= f[i >> 1];
+        }
+        const float ref[2] = {most[0] == -INFINITY ? 0.f : c * most[0], most[1] == -INFINITY ? 0.f : c * most[1]};
+        uint32_t p[4];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float y0 = exp2f(fmaf(c, x[n][2 * i], -ref[i])), y1 = exp2f(fmaf(c, x[n][2 * i + 1], -ref[i]));
+                sum[i] += y0 + y1;
+                const __nv_bfloat162 w = __floats2bfloat162_rn(y0, y1);          // rounded once, for the product with V
+                p[n * 2 + i] = *reinterpret_cast<const uint32_t *>(&w);
+            }
+#pragma unroll
+        for (int n = 0; n < DP / 16; ++n) {
+            uint32_t f[4];                                 // 16 keys, 16 columns
+            const int row = lane & 15, ch = n * 2 + lane / 16;
+            ldmatrix4_trans(f, V + row * (DP * 2) + ((ch ^ (row & 7)) << 4));
+            mma16816(o[2 * n], p, f[0], f[1]);
+            mma16816(o[2 * n + 1], p, f[2], f[3]);
+        }
+#pragma unroll
+        for (int s = 0; s + 1 < STAGES; ++s) there[s] = there[s + 1];
+        if (++stage == STAGES) stage = 0;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    pdl_trigger();
+
+    // join the warps: each leaves its output where its ring was
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        sum[i] += __shfl_xor_sync(~0u, sum[i], 1);
+        sum[i] += __shfl_xor_sync(~0u, sum[i], 2);
+        if ((lane & 3) == 0) {
+            most_w[warp * HEADS + i * 8 + lane / 4] = most[i];
+            sum_w[warp * HEADS + i * 8 + lane / 4] = sum[i];
+        }
+    }
+    float *mine = (float *)(smem + warp * S::RING);
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<float2 *>(mine + (lane / 4 + i * 8) * DP + n * 8 + (lane & 3) * 2) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+    __syncthreads();
+    // weight of a part whose largest score is m, where the largest of all is `all`
+    auto weight = [&](float m, float all) { return m == -INFINITY ? 0.f : exp2f(c * (m - all)); };
+    if (threadIdx.x < HEADS) {
+        float all = -INFINITY, s = 0.f;
+        for (int w = 0; w < WARPS; ++w) all = fmaxf(all, most_w[w * HEADS + threadIdx.x]);
+        for (int w = 0; w < WARPS; ++w) s += sum_w[w * HEADS + threadIdx.x] * weight(most_w[w * HEADS + threadIdx.x], all);
+        most_b[threadIdx.x] = all;
+        sum_b[threadIdx.x] = s;
+    }
+    __syncthreads();
+    float *block = (float *)smem;                          // the first warp's place
+    for (int e = threadIdx.x; e < g * DP; e += WARPS * 32) {
+        const int row = e / DP;
+        float s = 0.f;
+        for (int w = 0; w < WARPS; ++w) s += ((const float *)(smem + w * S::RING))[e] * weight(most_w[w * HEADS + row], most_b[row]);
+        block[e] = s;
+    }
+    if (splits > 1) tc::cluster_sync_all();
+    else __syncthreads();
+    for (int e = 2 * (split * WARPS * 32 + threadIdx.x); e < g * DP; e += 2 * splits * WARPS * 32) {
+        const int row = e / DP, col = e % DP;
+        float all = -INFINITY, s = 0.f, y0 = 0.f, y1 = 0.f;
+        for (int r = 0; r < splits; ++r) all = fmaxf(all, splits > 1 ? ld_cluster(tc::map_to_cta(tc::smem_u32(most_b + row), r)) : most_b[row]);
+        for (int r = 0; r < splits; ++r) {
+            if (splits == 1) {
+                s = sum_b[row];
+                y0 = block[e];
+                y1 = block[e + 1];
+            } else {
+                const float w = weight(ld_cluster(tc::map_to_cta(tc::smem_u32(most_b + row), r)), all);
+                s += w * ld_cluster(tc::map_to_cta(tc::smem_u32(sum_b + row), r));
+                y0 += w * ld_cluster(tc::map_to_cta(tc::smem_u32(block + e), r));
+                y1 += w * ld_cluster(tc::map_to_cta(tc::smem_u32(block + e + 1), r));
+            }
+        }
+        const float inv = s > 0.f ? 1.f / s : 0.f;
+        if (col < a.d)
+            *reinterpret_cast<__nv_bfloat162 *>(a.out + ((int64_t)b * a.heads + hk * a.group + g0 + row) * a.d + col) = __floats2bfloat162_rn(y0 * inv, y1 * inv);
+    }
+    if (splits > 1) tc::cluster_sync_all();                // no block ends while another reads its shared memory
+    if (*bad && threadIdx.x == 0) {
+        // Block 0 begins no later than any other and sets the word at once; only a call with an error waits here.
+        for (int i = 0; i < 100; ++i) __nanosleep(1000);
+        atomicExch(a.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
+    }
+}
+
+// Blocks of a cluster: as many as it takes to give every SM two blocks, as long as a warp has two tiles; a power of two up to 16.
+static int step_splits(const StepArgs &a)
+{
+    const int64_t most = (int64_t)a.cols * a.page, visible = most < (int64_t)a.window + a.sinks ? most : (int64_t)a.window + a.sinks;
+    const int64_t blocks = (int64_t)a.nseq * (a.heads / a.group) * ((a.group + wstep::HEADS - 1) / wstep::HEADS);
+    int n = 1;
+    while (n < 16 && blocks * n < 2 * sm_count_or_default() && visible > (int64_t)2 * n * wstep::WARPS * wstep::KEYS * 2) n *= 2;
+    return n;
+}
+
+template <int DP>
+static st_status run_step(const StepArgs &a, cudaStream_t stream)
+{
+    const size_t smem = wstep::Shape<DP>::SMEM;
+    if (!ensure_dynamic_smem(window_step_kernel<DP>, smem) || !allow_large_clusters(window_step_kernel<DP>)) return ST_ERR_CUDA;
+    const int splits = step_splits(a), chunks = (a.group + wstep::HEADS - 1) / wstep::HEADS;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)splits, (unsigned)(a.heads / a.group * chunks), (unsigned)a.nseq);
+    cfg.blockDim = dim3(wstep::WARPS * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)splits;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = splits > 1 ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, window_step_kernel<DP>, a) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return ST_ERR_CUDA;
+    }
+    return ST_OK;
 }
 
 }  // namespace attn
@@ -112,5 +387,5 @@ extern "C" st_status st_attn_window_step(const st_cache *c, const void *q, const
     a.scale = scale;
     a.out = (bf16 *)out;
     a.status = (unsigned *)ws;
-    return launch(window_step_kernel, dim3(a.heads, a.nseq), 32, 0, (cudaStream_t)stream, a);
+    return a.d <= 64 ? run_step<64>(a, (cudaStream_t)stream) : run_step<128>(a, (cudaStream_t)stream);
 }
