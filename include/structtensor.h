@@ -372,8 +372,8 @@ st_status st_attn_window_step(const st_cache *cache, const void *q, const void *
  *     S[t] = exp(a) S[t-1] + k[t] (x) v[t];    out[t] = scale S[t]^T q[t],    S[-1] = state_in (or 0)
  * q, k: [n, heads, d]; v: [n, heads, dv]; one offsets array, nq = nk, kv_heads = heads.  state_in, state_out: fp32
  * [nseq, heads, d, dv], both may be NULL; out: bf16 [n, heads, dv].  An empty sequence hands its state on.
- * Sums and states are fp32; where they enter a product on the tensor cores they are the sum of two bf16 numbers, the
- * weighted scores of a chunk of tokens are rounded to bf16 once. */
+ * Sums and states are fp32.  For their products on the tensor cores the weighted scores of a chunk of 128 tokens and the state
+ * that enters the chunk are rounded to bf16, once each. */
 st_status st_attn_decay(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
                         const int32_t *offsets, const float *state_in, float scale, void *out, float *state_out,
                         void *ws, size_t ws_bytes, void *stream);

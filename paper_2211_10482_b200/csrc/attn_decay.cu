@@ -9,15 +9,18 @@
 // No power is of a positive exponent, whatever the decay.  Four products a chunk on the tensor cores, all accumulators in tensor memory:
 //     scores X Y^T;  P Z with P as bf16 in the place of the scores;  X S;  Y^T (weights Z).
 // S itself stays in fp32 registers, one row to a thread, and the chunk's sum is added to it there, so that no long chain of additions
-// runs through the tensor cores' accumulators (which do not round to nearest).  Where S and the weighted Z are operands they are
-// the sum of two bf16 numbers, two products each: 2^-16 of their terms, where one bf16 would leave 2^-8 in a state that is fp32.
+// runs through the tensor cores' accumulators (which do not round to nearest).  The weighted Z is the sum of two bf16 numbers, as one would
+// leave 2^-8 in a state that is fp32.  P, and S where it meets X, are rounded to bf16 once: out is bf16 itself.
 //
 // A block owns 64 columns of z, out and S for a run of chunks: with 128 columns two stages of X, Y and Z, S and the weighted Z in two parts
 // would not fit in shared memory.  The two blocks of a head read X and Y at about the same time, the second time from L2.
 // Where heads and sequences are few, sequences are cut into segments: one kernel sums each segment's own state, one carries the states
 // over the segments, then all segments run at once.
 //
-// Warps: 0..3 make P and write out (a thread = a token), 4..7 weigh Z and keep S (a thread = a token, a row of S), 8 copies, 9 issues the products.
+// Bound by shared memory: a chunk moves some 330 KB through it (80 of copies, 190 of operands, 64 of Z and S), 128 bytes a cycle.
+//
+// Warps: 0..3 make P and write out (a thread = a token), 4..7 weigh Z (a thread = a token), 8..11 keep S (a thread = a row of it), 12 copies,
+// 13 issues the products.
 #include "attn_tc.cuh"
 
 namespace st {
@@ -29,9 +32,9 @@ struct FadeArgs {
     const float *log_decay;
     const int *offsets;
     int nseq, n, heads;
-    const float *init;                // [nseq, heads, dx, dz] or, transposed, [nseq, heads, dz, dx]; or null
+    const float *init;                // the state before the first (after the last) token: [nseq, heads, dx, dz] or null
     float *last;                      // [nseq, heads, dx, dz] or null
-    int transposed, backwards;
+    int transposed, backwards;        // transposed: init and states are [.., dz, dx]
     float in_scale, out_scale;
     bf16 *out;
     unsigned *status;
@@ -41,11 +44,11 @@ struct FadeArgs {
 };
 
 namespace fade {
-constexpr int THREADS = 320, STAGES = 2, ZC = 64;               // ZC: columns of z of a block
+constexpr int THREADS = 448, STAGES = 2, ZC = 64;               // ZC: columns of z of a block
 template <int DX> struct Shape {
     static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = DX * 128;
     static constexpr int STAGE = 2 * X_BYTES + Z_BYTES;
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + 2 * S_BYTES + 2 * Z_BYTES + 2 * TILE * sizeof(float) + 256;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * Z_BYTES + 2 * TILE * sizeof(float) + 256;
 };
 }  // namespace fade
 
@@ -84,11 +87,11 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     using Sh = Shape<DX>;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
-    unsigned char *stages = smem, *S_hi = stages + STAGES * Sh::STAGE, *S_lo = S_hi + Sh::S_BYTES, *Z_hi = S_lo + Sh::S_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
+    unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_hi = S_op + Sh::S_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
     float *table = (float *)(Z_lo + Sh::Z_BYTES);                  // 128 zeros, then in_scale w^m
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
     uint64_t *in_full = bars, *in_empty = in_full + STAGES, *sc_full = in_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
-             *z_ready = o_free + 1, *s_ready = z_ready + 1, *u_full = s_ready + 1, *xs_done = u_full + 1;
+             *z_ready = o_free + 1, *s_ready = z_ready + 1, *u_full = s_ready + 1, *u_free = u_full + 1, *xs_done = u_free + 1;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
@@ -109,6 +112,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const int n = (seg.len + TILE - 1) / TILE;
     const float decay = a.log_decay[h], a2 = decay * LOG2E;
     auto chunk_of = [&](int i) { return a.backwards ? n - 1 - i : i; };
+    auto tokens_of = [&](int i) { return min(seg.len - chunk_of(i) * TILE, TILE); };
 
     for (int i = threadIdx.x; i < 2 * TILE; i += THREADS) table[i] = i < TILE ? 0.f : a.in_scale * power(a2, i - TILE);
     if (threadIdx.x == 0) {
@@ -126,11 +130,12 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         mbar_init(z_ready, 4);
         mbar_init(s_ready, 4);
         mbar_init(u_full, 1);
+        mbar_init(u_free, 4);
         mbar_init(xs_done, 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
-    if (warp == 9) {
+    if (warp == 13) {
         tmem_alloc(tmem_slot, 512);
         tmem_relinquish();
     }
@@ -140,22 +145,22 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const uint32_t tmem = *tmem_slot, pz_col = tmem + 2 * TILE, xs_col = pz_col + ZC, u_col = xs_col + ZC;
     pdl_trigger();
 
-    if (warp == 8) {
+    if (warp == 12) {
         if (elect_one()) {
             for (int i = 0; i < n; ++i) {
                 const int s = i % STAGES, row = seg.first + chunk_of(i) * TILE;
                 if (!mbar_wait(&in_empty[s], (uint32_t)((i / STAGES + 1) & 1), abort_flag, a.status, 1)) break;
                 unsigned char *st = stages + s * Sh::STAGE;
                 mbar_expect_tx(&in_full[s], STATE ? Sh::X_BYTES + Sh::Z_BYTES : Sh::STAGE);
+                tma_load_3d(st + 2 * Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
                 load_tile<DX>(st + Sh::X_BYTES, &ymap, &in_full[s], h, row);
                 if (!STATE) load_tile<DX>(st, &xmap, &in_full[s], h, row);
-                tma_load_3d(st + 2 * Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
             }
         }
         __syncwarp();
-    } else if (warp == 9) {
+    } else if (warp == 13) {
         if (elect_one()) {
-            const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, ZC);
+            const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, 2 * ZC);
             bool ok = true;
             int scored = 0;                         // chunks whose scores have been issued
             // scores of chunk i; without `wait` only if its tiles are there
@@ -177,16 +182,14 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 score(i + 1, false);
                 if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
                 if (ok) ok = mbar_wait(z_ready, (uint32_t)(i & 1), abort_flag, a.status, 3);
+                if (ok && i > 0) ok = mbar_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024);
+                // Y^T times both parts side by side: the tile of Y is read once
+                const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_hi), SLAB, 1024);
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const uint64_t z = make_smem_desc(smem_u32(part ? Z_lo : Z_hi), SLAB, 1024);
-#pragma unroll
-                    for (int k = 0; k < TILE / 16; ++k)
-                        mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, part || k ? 1u : 0u);
-                }
+                for (int k = 0; k < TILE / 16; ++k)
+                    mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k ? 1u : 0u);
                 tc_commit(u_full);
                 if (STATE) {
                     tc_commit(&in_empty[i % STAGES]);
@@ -197,14 +200,10 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 if (ok) ok = mbar_wait(s_ready, (uint32_t)(i & 1), abort_flag, a.status, 5);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t x = make_smem_desc(smem_u32(X), 16, 1024);
+                const uint64_t x = make_smem_desc(smem_u32(X), 16, 1024), st = make_smem_desc(smem_u32(S_op), SLAB, 1024);
 #pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const uint64_t s = make_smem_desc(smem_u32(part ? S_lo : S_hi), SLAB, 1024);
-#pragma unroll
-                    for (int k = 0; k < DX / 16; ++k)
-                        mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), s + (uint64_t)(k * 2048 >> 4), pz_idesc, part || k ? 1u : 0u);
-                }
+                for (int k = 0; k < DX / 16; ++k)
+                    mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), st + (uint64_t)(k * 2048 >> 4), pz_idesc, k ? 1u : 0u);
                 tc_commit(xs_done);
                 score(i + 1, false);
                 ok = mbar_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
@@ -217,17 +216,18 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         __syncwarp();
     } else if (warp < 4) {
+        // thread: token t of a chunk.  Scores to weights, and out.
         if (!STATE) {
             const int t = threadIdx.x;
             const uint32_t lanes = (uint32_t)(warp * 32) << 16;
             bool ok = true;
-            // rows of chunk i that a thread writes
             auto write = [&](int i) {
+                const int first = chunk_of(i) * TILE, L = tokens_of(i);
+                const float alpha = a.out_scale * power(a2, a.backwards ? L - 1 - min(t, L - 1) : t + 1);
+                bf16 *out = a.out + ((int64_t)(seg.first + first + t) * a.heads + h) * a.dz + slab * ZC;
                 ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
                 if (!ok) return;
                 tc_fence_after();
-                const int first = chunk_of(i) * TILE, L = min(seg.len - first, TILE);
-                const float alpha = a.out_scale * power(a2, a.backwards ? L - 1 - min(t, L - 1) : t + 1);
                 uint32_t pz[2][32], xs[2][32];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
@@ -238,7 +238,6 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(o_free);
-                bf16 *out = a.out + ((int64_t)(seg.first + first + t) * a.heads + h) * a.dz + slab * ZC;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     uint4 v;
@@ -252,39 +251,35 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     if (t < L && slab * ZC + j * 8 < a.dz) *reinterpret_cast<uint4 *>(out + j * 8) = v;
                 }
             };
+            // weight of column s: table[128 + t - s], or backwards table[128 + s - t]
+            const float *w = a.backwards ? table + TILE - t : table + TILE + t;
             for (int i = 0; i < n; ++i) {
-                const int L = min(seg.len - chunk_of(i) * TILE, TILE);
+                const int L = tokens_of(i);
                 ok = __all_sync(~0u, mbar_wait(&sc_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 8));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t addr = tmem + lanes + (i & 1) * TILE;
-                // weight of column s: table[128 + t - s], or backwards table[128 + s - t]
-                const float *w = a.backwards ? table + TILE - t : table + TILE + t;
-                uint32_t x[4][32];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) tmem_ld_32x32(addr + j * 32, x[j]);
+                uint32_t x[2][32];
+                tmem_ld_32x32(addr, x[0]);
                 tmem_ld_wait();
-                if (a.backwards) {
 #pragma unroll
-                    for (int s = 0; s < TILE; ++s) x[s / 32][s % 32] = __float_as_uint(__uint_as_float(x[s / 32][s % 32]) * w[s]);
-                } else {
+                for (int j = 0; j < 4; ++j) {
+                    if (j < 3) tmem_ld_32x32(addr + (j + 1) * 32, x[(j + 1) & 1]);
+                    uint32_t p[16];
 #pragma unroll
-                    for (int s = 0; s < TILE; ++s) x[s / 32][s % 32] = __float_as_uint(__uint_as_float(x[s / 32][s % 32]) * w[-s]);
-                }
-                if (L < TILE) {                   // what lies behind the sequence may be anything
+                    for (int e = 0; e < 16; ++e) {
+                        const int s = j * 32 + 2 * e;
+                        float y[2];
 #pragma unroll
-                    for (int s = 0; s < TILE; ++s)
-                        if (s >= L) x[s / 32][s % 32] = 0u;
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int s = j * 64 + 2 * e;
-                        p[e] = pack_bf16(__uint_as_float(x[s / 32][s % 32]), __uint_as_float(x[s / 32][s % 32 + 1]));
+                        for (int k = 0; k < 2; ++k) {
+                            y[k] = __uint_as_float(x[j & 1][2 * e + k]) * (a.backwards ? w[s + k] : w[-s - k]);
+                            if (L < TILE && s + k >= L) y[k] = 0.f;                 // what lies behind the sequence may be anything
+                        }
+                        p[e] = pack_bf16(y[0], y[1]);
                     }
-                    tmem_st_32x32(addr + j * 32, p);
+                    tmem_ld_wait();
+                    // over scores that have been read: 16 columns for 32
+                    tmem_st_32x16(addr + j * 16, p);
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -295,40 +290,15 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             }
             if (ok && n > 0) write(n - 1);
         }
-    } else {
+    } else if (warp < 8) {
+        // thread: token r of a chunk.  Z times its weights, in two parts.
         const int r = threadIdx.x - 128, swz = r & 7;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const bool row = r < a.dx;
-        const int64_t plane = (int64_t)a.dx * a.dz, at = (int64_t)r * a.dz + slab * ZC;
-        float S[64];
-        {
-            const float *from = nullptr;
-            if (!STATE) from = a.states ? a.states + ((int64_t)tile * a.heads + h) * plane : a.init ? a.init + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
-            const bool flip = !a.states && a.transposed;
-#pragma unroll
-            for (int c = 0; c < 64; ++c)
-                S[c] = from && row && slab * ZC + c < a.dz ? from[flip ? (int64_t)(slab * ZC + c) * a.dx + r : at + c] : 0.f;
-        }
         bool ok = true;
-        float keep = 1.f;                              // what is left of S over the chunk whose sum is added to it
-        auto add = [&](int i) {
-            ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)(i & 1), abort_flag, a.status, 9));
-            if (!ok) return;
-            tc_fence_after();
-            uint32_t u[2][32];
-            tmem_ld_32x32(u_col + lanes, u[0]);
-            tmem_ld_32x32(u_col + lanes + 32, u[1]);
-            tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < 64; ++c) S[c] = fmaf(keep, S[c], row ? __uint_as_float(u[c / 32][c % 32]) : 0.f);
-        };
-        const float keep_full = carry(decay, TILE);
         for (int i = 0; i < n; ++i) {
-            const int L = min(seg.len - chunk_of(i) * TILE, TILE);
-            if (i > 0) add(i - 1);                     // its product has been read: Z_hi, Z_lo and the accumulator are free
-            if (!ok) break;
-            keep = L == TILE ? keep_full : carry(decay, L);
+            const int L = tokens_of(i);
+            const float beta = r < L ? a.in_scale * power(a2, a.backwards ? r + 1 : L - 1 - r) : 0.f;
             ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
+            if (ok && i > 0) ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)((i - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
             unsigned char *Y = stages + (i % STAGES) * Sh::STAGE + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
             if (r >= L) {                              // rows behind the sequence: they meet weights of 0
@@ -338,10 +308,10 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     for (int c = 0; c < DX / 64; ++c) *reinterpret_cast<uint4 *>(Y + c * SLAB + r * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
             }
-            const float beta = r < L ? a.in_scale * power(a2, a.backwards ? r + 1 : L - 1 - r) : 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int o = r * 128 + j * 16;        // the whole row is this thread's: its swizzle does not matter
+                // a row is one thread's, in any order: this one meets every bank once in eight lanes
+                const int o = r * 128 + ((j ^ swz) << 4);
                 const uint4 v = *reinterpret_cast<const uint4 *>(Z + o);
                 const uint32_t u[4] = {v.x, v.y, v.z, v.w};
                 uint4 hi, lo;
@@ -354,27 +324,56 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(z_ready);
+        }
+    } else {
+        // thread: row r of S
+        const int r = threadIdx.x - 256, swz = r & 7;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const bool row = r < a.dx;
+        const int64_t plane = (int64_t)a.dx * a.dz, at = (int64_t)r * a.dz + slab * ZC;
+        float S[64];
+        {
+            const float *from = nullptr;
+            if (!STATE) from = a.states ? a.states + ((int64_t)tile * a.heads + h) * plane : a.init ? a.init + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
+#pragma unroll
+            for (int c = 0; c < 64; ++c)
+                S[c] = from && row && slab * ZC + c < a.dz ? from[a.transposed ? (int64_t)(slab * ZC + c) * a.dx + r : at + c] : 0.f;
+        }
+        bool ok = true;
+        const float keep_full = carry(decay, TILE);
+        for (int i = 0; i < n; ++i) {
+            const int L = tokens_of(i);
+            const float keep = L == TILE ? keep_full : carry(decay, L);
             if (!STATE) {
                 if (i > 0) ok = __all_sync(~0u, mbar_wait(xs_done, (uint32_t)((i - 1) & 1), abort_flag, a.status, 11));
                 if (!ok) break;
                 if (r < DX) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int o = r * 128 + ((j ^ swz) << 4);
-                        uint4 hi, lo;
-                        uint32_t *ph = &hi.x, *pl = &lo.x;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) split2(S[j * 8 + 2 * k], S[j * 8 + 2 * k + 1], ph[k], pl[k]);
-                        *reinterpret_cast<uint4 *>(S_hi + o) = hi;
-                        *reinterpret_cast<uint4 *>(S_lo + o) = lo;
-                    }
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<uint4 *>(S_op + r * 128 + ((j ^ swz) << 4)) =
+                            make_uint4(pack_bf16(S[j * 8], S[j * 8 + 1]), pack_bf16(S[j * 8 + 2], S[j * 8 + 3]), pack_bf16(S[j * 8 + 4], S[j * 8 + 5]),
+                                       pack_bf16(S[j * 8 + 6], S[j * 8 + 7]));
                 }
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(s_ready);
             }
+            ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)(i & 1), abort_flag, a.status, 14));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t hi[32], lo[32];
+                tmem_ld_32x32(u_col + lanes + j * 32, hi);
+                tmem_ld_32x32(u_col + lanes + ZC + j * 32, lo);
+                tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 32; ++c) S[j * 32 + c] = fmaf(keep, S[j * 32 + c], row ? __uint_as_float(hi[c]) + __uint_as_float(lo[c]) : 0.f);
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(u_free);
         }
-        if (ok && n > 0) add(n - 1);
         const bool end = seg.index == (a.backwards ? 0 : seg.count - 1);
         float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && a.last ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
         if (ok && to && row) {
@@ -385,7 +384,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 13) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -401,15 +400,11 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const FadeArgs a)
     const int h = blockIdx.y, plane = a.dx * a.dz, e = (blockIdx.z * 256 + threadIdx.x) * 4;
     if (e >= plane) return;
     const Rows r = rows_of(a.offsets, seg.seq, a.n);
-    const int rows = a.chunks * TILE, x = e / a.dz, z = e % a.dz;
+    const int rows = a.chunks * TILE;
     const int64_t step = (int64_t)a.heads * plane;
     float *states = a.states + ((int64_t)blockIdx.x * a.heads + h) * plane + e;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.init) {
-        const float *init = a.init + ((int64_t)seg.seq * a.heads + h) * plane;
-        if (a.transposed) s = make_float4(init[z * a.dx + x], init[(z + 1) * a.dx + x], init[(z + 2) * a.dx + x], init[(z + 3) * a.dx + x]);
-        else s = *reinterpret_cast<const float4 *>(init + e);
-    }
+    if (a.init) s = *reinterpret_cast<const float4 *>(a.init + ((int64_t)seg.seq * a.heads + h) * plane + e);
     const float decay = a.log_decay[h], whole = carry(decay, rows);
     for (int i = 0; i < seg.count; ++i) {
         const int k = a.backwards ? seg.count - 1 - i : i;
@@ -434,43 +429,29 @@ static int segment_chunks(int64_t n, int64_t heads, int64_t d)
     return some >= chunks ? 0 : (int)some;
 }
 
-// The states of the segments of one run.
-static size_t states_bytes(int64_t n, int64_t nseq, int64_t heads, int64_t d)
-{
-    size_t most = 0;
-    for (const int64_t c : {(int64_t)fade::ZC, d}) {                   // the run may be over either extent
-        const int chunks = segment_chunks(n, heads, c < d ? c : d);
-        const size_t bytes = chunks ? (size_t)most_tiles(n, nseq, (int64_t)chunks * TILE) * heads * d * d * sizeof(float) : 0;
-        most = bytes > most ? bytes : most;
-    }
-    return round_up(most, 256);
-}
-
-template <int DX>
-static st_status run_fade_as(FadeArgs &a, float *states, cudaStream_t stream)
+template <int DX, bool STATE>
+static st_status launch_fade(const FadeArgs &a, cudaStream_t stream)
 {
     CUtensorMap xm, ym, zm;
-    if (!make_tmap_table(&xm, a.x, a.n, a.heads, a.dx) || !make_tmap_table(&ym, a.y, a.n, a.heads, a.dx) || !make_tmap_table(&zm, a.z, a.n, a.heads, a.dz))
+    if (!make_tmap_table(&xm, STATE ? a.y : a.x, a.n, a.heads, a.dx) || !make_tmap_table(&ym, a.y, a.n, a.heads, a.dx) ||
+        !make_tmap_table(&zm, a.z, a.n, a.heads, a.dz))
         return ST_ERR_CUDA;
-    using Sh = fade::Shape<DX>;
-    const int slabs = (a.dz + fade::ZC - 1) / fade::ZC;
-    if (!ensure_dynamic_smem(fade_kernel<DX, false>, Sh::SMEM) || !ensure_dynamic_smem(fade_kernel<DX, true>, Sh::SMEM)) return ST_ERR_CUDA;
-    a.chunks = segment_chunks(a.n, a.heads, a.dz);
-    a.states = a.chunks ? states : nullptr;
-    if (!a.chunks) a.chunks = 1 << 22;                                 // 2^29 tokens and more than any sequence's
-    const unsigned tiles = (unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
-    if (a.states) {
-        st_status rc = launch(fade_kernel<DX, true>, dim3(tiles * slabs, a.heads), fade::THREADS, Sh::SMEM, stream, xm, ym, zm, a);
-        if (rc != ST_OK) return rc;
-        rc = launch(fade_carry_kernel, dim3(tiles, a.heads, (unsigned)((a.dx * a.dz + 1023) / 1024)), 256, 0, stream, a);
-        if (rc != ST_OK) return rc;
-        a.check = 0;
-    }
-    return launch(fade_kernel<DX, false>, dim3(tiles * slabs, a.heads), fade::THREADS, Sh::SMEM, stream, xm, ym, zm, a);
+    const size_t smem = fade::Shape<DX>::SMEM;
+    if (!ensure_dynamic_smem(fade_kernel<DX, STATE>, smem)) return ST_ERR_CUDA;
+    const int64_t tiles = most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE), slabs = (a.dz + fade::ZC - 1) / fade::ZC;
+    return launch(fade_kernel<DX, STATE>, dim3((unsigned)(tiles * slabs), a.heads), fade::THREADS, smem, stream, xm, ym, zm, a);
 }
-static st_status run_fade(FadeArgs &a, float *states, cudaStream_t stream)
+static st_status run_fade(const FadeArgs &a, cudaStream_t stream)
 {
-    return a.dx <= 64 ? run_fade_as<64>(a, states, stream) : run_fade_as<128>(a, states, stream);
+    return a.dx <= 64 ? launch_fade<64, false>(a, stream) : launch_fade<128, false>(a, stream);
+}
+// The states that enter the segments, of y (x) z as it is kept: not transposed.
+static st_status run_states(const FadeArgs &a, cudaStream_t stream)
+{
+    const st_status rc = a.dx <= 64 ? launch_fade<64, true>(a, stream) : launch_fade<128, true>(a, stream);
+    if (rc != ST_OK) return rc;
+    const unsigned tiles = (unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
+    return launch(fade_carry_kernel, dim3(tiles, a.heads, (unsigned)((a.dx * a.dz + 1023) / 1024)), 256, 0, stream, a);
 }
 
 static st_status check_decay(const st_tokens *t, const int32_t *offsets)
@@ -482,9 +463,16 @@ static st_status check_decay(const st_tokens *t, const int32_t *offsets)
     return !offsets && t->nseq != 1 ? ST_ERR_NULL : ST_OK;
 }
 
-static FadeArgs fade_args(const st_tokens *t, const float *log_decay, const int32_t *offsets)
+static FadeArgs fade_args(const st_tokens *t, const float *log_decay, const int32_t *offsets, void *ws)
 {
     FadeArgs a = {};
+    a.status = (unsigned *)ws;
+    a.check = 1;
+    a.chunks = segment_chunks(t->nq, t->heads, t->d > t->dv ? t->d : t->dv);
+    a.states = a.chunks ? (float *)((unsigned char *)ws + kWsHeaderBytes) : nullptr;
+    if (!a.chunks) a.chunks = 1 << 22;                                 // 2^29 tokens, as many as a sequence can have
+    a.dx = (int)t->d;
+    a.dz = (int)t->dv;
     a.log_decay = log_decay;
     a.offsets = offsets;
     a.nseq = (int)t->nseq;
@@ -504,7 +492,9 @@ static Table table_of(const void *p, int64_t rows, int64_t heads, int64_t row, i
 size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
     if (n <= 0 || nseq <= 0 || heads <= 0 || d <= 0 || d > 128 || n > (1 << 29) || heads > 65535 || nseq > (1 << 20)) return 0;
-    return kWsHeaderBytes + attn::states_bytes(n, nseq, heads, d);
+    const int chunks = attn::segment_chunks(n, heads, d);
+    const size_t states = chunks ? (size_t)attn::most_tiles(n, nseq, (int64_t)chunks * attn::TILE) * heads * d * d * sizeof(float) : 0;
+    return kWsHeaderBytes + round_up(states, 256);
 }
 
 }  // namespace st
@@ -518,26 +508,26 @@ st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const 
                         const int32_t *offsets, const float *state_in, float scale, void *out, float *state_out,
                         void *ws, size_t ws_bytes, void *stream)
 {
-    const st_status rc = check_decay(t, offsets);
+    st_status rc = check_decay(t, offsets);
     if (rc != ST_OK) return rc;
     if (!q || !k || !v || !log_decay || !out) return ST_ERR_NULL;
     for (const void *p : {q, k, v, (const void *)log_decay, (const void *)offsets, (const void *)state_in, (const void *)out, (const void *)state_out})
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
-    FadeArgs a = fade_args(t, log_decay, offsets);
+    FadeArgs a = fade_args(t, log_decay, offsets, ws);
     a.x = table_of(q, t->nq, t->heads, t->q_row, t->q_head);
     a.y = table_of(k, t->nk, t->heads, t->k_row, t->k_head);
     a.z = table_of(v, t->nk, t->heads, t->v_row, t->v_head);
-    a.dx = (int)t->d;
-    a.dz = (int)t->dv;
     a.init = state_in;
     a.last = state_out;
     a.out_scale = scale;
     a.out = (bf16 *)out;
-    a.status = (unsigned *)ws;
-    a.check = 1;
-    return run_fade(a, (float *)((unsigned char *)ws + kWsHeaderBytes), (cudaStream_t)stream);
+    if (a.states) {
+        if ((rc = run_states(a, (cudaStream_t)stream)) != ST_OK) return rc;
+        a.check = 0;
+    }
+    return run_fade(a, (cudaStream_t)stream);
 }
 
 st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, const void *v, const float *log_decay,
@@ -555,37 +545,51 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     const Table Q = table_of(q, t->nq, t->heads, t->q_row, t->q_head), K = table_of(k, t->nk, t->heads, t->k_row, t->k_head),
                 V = table_of(v, t->nk, t->heads, t->v_row, t->v_head), O = table_of(dout, t->nq, t->heads, t->heads * t->dv, t->dv);
-    float *states = (float *)((unsigned char *)ws + kWsHeaderBytes);
     cudaStream_t s = (cudaStream_t)stream;
-    // dq[t] = scale sum e^{a(t-s)} (dout[t].v[s]) k[s]
-    FadeArgs a = fade_args(t, log_decay, offsets);
-    a.x = O; a.y = V; a.z = K;
+    FadeArgs a = fade_args(t, log_decay, offsets, ws);
+    // dq[t] = scale sum e^{a(t-s)} (dout[t].v[s]) k[s], with the states of k (x) v
+    a.y = K;
+    a.z = V;
+    a.init = state_in;
+    if (a.states) {
+        if ((rc = run_states(a, s)) != ST_OK) return rc;
+        a.check = 0;
+    }
+    a.x = O;
+    a.y = V;
+    a.z = K;
     a.dx = (int)t->dv;
     a.dz = (int)t->d;
-    a.init = state_in;
     a.transposed = 1;
     a.out_scale = scale;
     a.out = (bf16 *)dq;
-    a.status = (unsigned *)ws;
-    a.check = 1;
-    if ((rc = run_fade(a, states, s)) != ST_OK) return rc;
-    // dk[s] = sum e^{a(t-s)} (v[s].dout[t]) scale q[t], backwards
-    a.x = V; a.y = O; a.z = Q;
-    a.init = dstate_out;
-    a.backwards = 1;
-    a.in_scale = scale;
-    a.out_scale = 1.f;
-    a.out = (bf16 *)dk;
+    if ((rc = run_fade(a, s)) != ST_OK) return rc;
     a.check = 0;
-    if ((rc = run_fade(a, states, s)) != ST_OK) return rc;
-    // dv[s] = sum e^{a(t-s)} (k[s].q[t]) scale dout[t], backwards
-    a.x = K; a.y = Q; a.z = O;
+    // dv[s] = sum e^{a(t-s)} (k[s].q[t]) scale dout[t], backwards, with the states of q (x) dout
+    a.x = K;
+    a.y = Q;
+    a.z = O;
     a.dx = (int)t->d;
     a.dz = (int)t->dv;
     a.transposed = 0;
-    a.last = dstate_in;
+    a.backwards = 1;
+    a.init = dstate_out;
+    a.in_scale = scale;
+    a.out_scale = 1.f;
     a.out = (bf16 *)dv;
-    return run_fade(a, states, s);
+    if (a.states && (rc = run_states(a, s)) != ST_OK) return rc;
+    a.last = dstate_in;
+    if ((rc = run_fade(a, s)) != ST_OK) return rc;
+    // dk[s] = sum e^{a(t-s)} (v[s].dout[t]) scale q[t], backwards, with the same states
+    a.x = V;
+    a.y = O;
+    a.z = Q;
+    a.dx = (int)t->dv;
+    a.dz = (int)t->d;
+    a.transposed = 1;
+    a.last = nullptr;
+    a.out = (bf16 *)dk;
+    return run_fade(a, s);
 }
 
 }  // extern "C"

@@ -4,7 +4,7 @@ the kernels' roundings may leave.
 Tolerances count roundings: to bf16 at most half a step, B = 2^-8 of the value.  The rest of the arithmetic is fp32; F = 2^-12 of the
 sum of absolute terms stands for it (sums of 128 products: 128 x 2^-24, once in a score, whose error is the relative error of its
 weight, and once in a product: 2^-16 of the absolute terms each; the operands' split into two bf16 numbers: 2^-16; scores reach
-about 16 times their typical size)."""
+about 16 times their typical size).  A state is rounded once where it meets a query: B of |query| |state|."""
 import math
 
 import torch
@@ -68,6 +68,23 @@ def powers(a, n):
     return torch.where(n == 0, 1.0, torch.exp(e))
 
 
+CHUNK = 128
+
+
+def held(y, z, w, s0, far, x):
+    """What the tokens of a chunk (rows of x) take from the state that enters it, in absolute terms, for a state that is rounded before the
+    product: sum_i |x_i| |S_ij| with S from the pairs of other chunks (weights w [H, t, s]) and the first state s0 (weights far)."""
+    n, out = x.shape[1], [x[:, :0] @ s0]
+    for c in range(0, n, CHUNK):
+        rows, before = slice(c, min(c + CHUNK, n)), torch.ones(n, dtype=torch.bool, device=x.device)
+        before[rows] = False
+        # all rows of a chunk take the same state with one factor each: the first row (or the last, backwards) has the largest
+        t = c if float(w[:, c, before].sum()) + float(far[:, c].sum()) >= float(w[:, rows.stop - 1, before].sum()) + float(far[:, rows.stop - 1].sum()) else rows.stop - 1
+        s = (y[:, before] * w[:, t, before][..., None]).transpose(1, 2) @ z[:, before] + far[:, t, :, None] * s0
+        out.append(x[:, rows].abs() @ s.abs())
+    return torch.cat(out, 1)
+
+
 def decay(q, k, v, a, state, scale=None):
     """out and the last state with their tolerances, for one sequence: q and k [n, H, d], v [n, H, dv], state [H, d, dv] or None."""
     n, H, d = q.shape
@@ -81,7 +98,7 @@ def decay(q, k, v, a, state, scale=None):
     first = powers(a, i + 1)[..., None]
     out = (x @ V + first * (Q @ S0)) * scale
     terms = ((Q.abs() @ K.abs().transpose(1, 2)) * w) @ V.abs() + first * (Q.abs() @ S0.abs())
-    tol = B * out.abs() + ((B * x.abs()) @ V.abs() + F * terms) * abs(scale)
+    tol = B * out.abs() + ((B * x.abs()) @ V.abs() + B * held(K, V, w, S0, first, Q) + F * terms) * abs(scale)
     wl = powers(a, n - 1 - i)[..., None]
     last = (K * wl).transpose(1, 2) @ V + powers(a, torch.tensor(n, device=q.device)).view(-1, 1, 1) * S0
     last_tol = 2.0 ** -14 * ((K * wl).abs().transpose(1, 2) @ V.abs() + powers(a, torch.tensor(n, device=q.device)).view(-1, 1, 1) * S0.abs())
@@ -101,12 +118,13 @@ def decay_grad(q, k, v, a, dout, state, dlast, scale=None):
     first, rest = powers(a, i + 1)[..., None], powers(a, n - 1 - i)[..., None]
     all_ = powers(a, torch.tensor(n, device=q.device)).view(-1, 1, 1)
 
-    def part(x, y, z, weight, far, held, held_scale):
+    def part(x, y, z, weight, far, first_state, held_scale):
         """sum over pairs of (x.y) weight z, and what the held state brings"""
         s = (x @ y.transpose(1, 2)) * weight
-        r = s @ z * scale + far * (x @ held) * held_scale
-        terms = ((x.abs() @ y.abs().transpose(1, 2)) * weight) @ z.abs() * scale + far * (x.abs() @ held.abs()) * held_scale
-        return r.transpose(0, 1), (B * r.abs() + (B * s.abs()) @ z.abs() * scale + F * terms).transpose(0, 1)
+        r = s @ z * scale + far * (x @ first_state) * held_scale
+        terms = ((x.abs() @ y.abs().transpose(1, 2)) * weight) @ z.abs() * scale + far * (x.abs() @ first_state.abs()) * held_scale
+        taken = held(y * scale, z, weight, first_state * held_scale, far, x)
+        return r.transpose(0, 1), (B * r.abs() + (B * s.abs()) @ z.abs() * scale + B * taken + F * terms).transpose(0, 1)
 
     wt = w.transpose(1, 2)
     dq = part(D, V, K, w, first, S0.transpose(1, 2), scale)
