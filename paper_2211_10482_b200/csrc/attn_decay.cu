@@ -19,7 +19,7 @@
 //
 // Bound by shared memory: a chunk moves some 330 KB through it (80 of copies, 190 of operands, 64 of Z and S), 128 bytes a cycle.
 //
-// Warps: 0..3 make P and write out (a thread = a token), 4..7 weigh Z (a thread = a token), 8..11 keep S (a thread = a row of it), 12 copies,
+// Warps: 0..3 make P (a thread = a token), 4..7 weigh Z and write out (a thread = a token), 8..11 keep S (a thread = a row of it), 12 copies,
 // 13 issues the products.
 #include "attn_tc.cuh"
 
@@ -48,7 +48,7 @@ constexpr int THREADS = 448, STAGES = 2, ZC = 64;               // ZC: columns o
 template <int DX> struct Shape {
     static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = DX * 128;
     static constexpr int STAGE = 2 * X_BYTES + Z_BYTES;
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * Z_BYTES + 2 * TILE * sizeof(float) + 256;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 3 * Z_BYTES + 2 * TILE * sizeof(float) + 256;
 };
 }  // namespace fade
 
@@ -57,11 +57,13 @@ __device__ __forceinline__ float power(float a2, int m) { return m == 0 ? 1.f : 
 // the factor of a state over `m` tokens: it enters as many times as there are chunks, so that its error counts
 __device__ __forceinline__ float carry(float a, int m) { return m == 0 ? 1.f : (float)exp((double)a * m); }
 
-// x = hi + lo, two values at a time
-__device__ __forceinline__ void split2(float x0, float x1, uint32_t &hi, uint32_t &lo)
+// b z = hi + lo for two values z at a time, b = b_hi + b_lo: hi the rounded product, its remainder exact (two significands of 8 bits have a product
+// of 16), lo the remainder and b_lo z rounded: 2^-17 of b z is lost.
+__device__ __forceinline__ void times(__nv_bfloat162 b_hi, __nv_bfloat162 b_lo, uint32_t z, uint32_t &hi, uint32_t &lo)
 {
-    hi = pack_bf16(x0, x1);
-    lo = pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xFFFF0000u));
+    const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&z), h = __hmul2(b_hi, x), l = __hfma2(b_lo, x, __hfma2(b_hi, x, __hneg2(h)));
+    hi = *reinterpret_cast<const uint32_t *>(&h);
+    lo = *reinterpret_cast<const uint32_t *>(&l);
 }
 
 // The segment that a block works on.
@@ -77,8 +79,8 @@ __device__ __forceinline__ Segment segment_of(const FadeArgs &a, int tile, int l
     return {at.seq, r.first + at.tile * rows, min(r.len - at.tile * rows, rows), at.tile, max((r.len + rows - 1) / rows, 1)};
 }
 
-// STATE: only the segment's own sum of outer products, to `states`.
-template <int DX, bool STATE>
+// STATE: only the segment's own sum of outer products, to `states`.  BACK: backwards in time.
+template <int DX, bool STATE, bool BACK>
 __global__ void __launch_bounds__(fade::THREADS, 1)
 fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap zmap, const FadeArgs a)
 {
@@ -88,9 +90,10 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
     unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_hi = S_op + Sh::S_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
-    float *table = (float *)(Z_lo + Sh::Z_BYTES);                  // 128 zeros, then in_scale w^m
+    unsigned char *out_rows = Z_lo + Sh::Z_BYTES;
+    float *table = (float *)(out_rows + Sh::Z_BYTES);              // 128 zeros, then in_scale w^m
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
-    uint64_t *in_full = bars, *in_empty = in_full + STAGES, *sc_full = in_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
+    uint64_t *in_full = bars, *xy_empty = in_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
              *z_ready = o_free + 1, *s_ready = z_ready + 1, *u_full = s_ready + 1, *u_free = u_full + 1, *xs_done = u_free + 1;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
@@ -108,17 +111,18 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const Segment seg = segment_of(a, tile, lane);
     if (seg.seq < 0) return;
     // nobody needs the sum of the segment that comes last
-    if (STATE && seg.index == (a.backwards ? 0 : seg.count - 1)) return;
+    if (STATE && seg.index == (BACK ? 0 : seg.count - 1)) return;
     const int n = (seg.len + TILE - 1) / TILE;
     const float decay = a.log_decay[h], a2 = decay * LOG2E;
-    auto chunk_of = [&](int i) { return a.backwards ? n - 1 - i : i; };
+    auto chunk_of = [&](int i) { return BACK ? n - 1 - i : i; };
     auto tokens_of = [&](int i) { return min(seg.len - chunk_of(i) * TILE, TILE); };
 
-    for (int i = threadIdx.x; i < 2 * TILE; i += THREADS) table[i] = i < TILE ? 0.f : a.in_scale * power(a2, i - TILE);
+    if (threadIdx.x < 2 * TILE) table[threadIdx.x] = threadIdx.x < TILE ? 0.f : a.in_scale * power(a2, threadIdx.x - TILE);
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&in_full[s], 1);
-            mbar_init(&in_empty[s], 1);
+            mbar_init(&xy_empty[s], 1);
+            mbar_init(&z_empty[s], 1);
         }
         mbar_init(&sc_full[0], 1);
         mbar_init(&sc_full[1], 1);
@@ -147,14 +151,17 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 
     if (warp == 12) {
         if (elect_one()) {
+            // a stage's tiles come back from the products one after another
             for (int i = 0; i < n; ++i) {
                 const int s = i % STAGES, row = seg.first + chunk_of(i) * TILE;
-                if (!mbar_wait(&in_empty[s], (uint32_t)((i / STAGES + 1) & 1), abort_flag, a.status, 1)) break;
+                const uint32_t parity = (uint32_t)((i / STAGES + 1) & 1);
                 unsigned char *st = stages + s * Sh::STAGE;
+                if (!mbar_wait(&xy_empty[s], parity, abort_flag, a.status, 1)) break;
                 mbar_expect_tx(&in_full[s], STATE ? Sh::X_BYTES + Sh::Z_BYTES : Sh::STAGE);
-                tma_load_3d(st + 2 * Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
                 load_tile<DX>(st + Sh::X_BYTES, &ymap, &in_full[s], h, row);
                 if (!STATE) load_tile<DX>(st, &xmap, &in_full[s], h, row);
+                if (!mbar_wait(&z_empty[s], parity, abort_flag, a.status, 15)) break;
+                tma_load_3d(st + 2 * Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
             }
         }
         __syncwarp();
@@ -163,9 +170,9 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, 2 * ZC);
             bool ok = true;
             int scored = 0;                         // chunks whose scores have been issued
-            // scores of chunk i; without `wait` only if its tiles are there
+            // scores of chunk i; without `wait` only if its tiles are there, and whole: else the rows behind the sequence are cleared first
             auto score = [&](int i, bool wait) {
-                if (STATE || !ok || i >= n || scored > i) return;
+                if (STATE || !ok || i >= n || scored > i || (!wait && tokens_of(i) < TILE)) return;
                 const uint32_t parity = (uint32_t)((i / STAGES) & 1);
                 if (wait) ok = mbar_wait(&in_full[i % STAGES], parity, abort_flag, a.status, 2);
                 else if (!mbar_try_wait(&in_full[i % STAGES], parity)) return;
@@ -178,10 +185,14 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             };
             for (int i = 0; i < n && ok; ++i) {
                 const unsigned char *X = stages + (i % STAGES) * Sh::STAGE, *Y = X + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
-                score(i, true);
-                score(i + 1, false);
+                const bool whole = tokens_of(i) == TILE;
+                if (whole) {
+                    score(i, true);
+                    score(i + 1, false);
+                }
                 if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
                 if (ok) ok = mbar_wait(z_ready, (uint32_t)(i & 1), abort_flag, a.status, 3);
+                if (!whole) score(i, true);
                 if (ok && i > 0) ok = mbar_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
                 if (!ok) break;
                 tc_fence_after();
@@ -192,7 +203,8 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k ? 1u : 0u);
                 tc_commit(u_full);
                 if (STATE) {
-                    tc_commit(&in_empty[i % STAGES]);
+                    tc_commit(&xy_empty[i % STAGES]);
+                    tc_commit(&z_empty[i % STAGES]);
                     continue;
                 }
                 score(i + 1, false);
@@ -205,139 +217,163 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 for (int k = 0; k < DX / 16; ++k)
                     mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), st + (uint64_t)(k * 2048 >> 4), pz_idesc, k ? 1u : 0u);
                 tc_commit(xs_done);
+                tc_commit(&xy_empty[i % STAGES]);
                 score(i + 1, false);
                 ok = mbar_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
                 if (!ok) break;
                 tc_fence_after();
                 mma_tokens(pz_col, tmem + (i & 1) * TILE, Z, pz_idesc, false);
                 tc_commit(o_full);
-                tc_commit(&in_empty[i % STAGES]);
+                tc_commit(&z_empty[i % STAGES]);
             }
         }
         __syncwarp();
     } else if (warp < 4) {
-        // thread: token t of a chunk.  Scores to weights, and out.
+        // thread: token t of a chunk.  Scores to weights.
         if (!STATE) {
-            const int t = threadIdx.x;
             const uint32_t lanes = (uint32_t)(warp * 32) << 16;
             bool ok = true;
-            auto write = [&](int i) {
-                const int first = chunk_of(i) * TILE, L = tokens_of(i);
-                const float alpha = a.out_scale * power(a2, a.backwards ? L - 1 - min(t, L - 1) : t + 1);
-                bf16 *out = a.out + ((int64_t)(seg.first + first + t) * a.heads + h) * a.dz + slab * ZC;
-                ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
-                if (!ok) return;
-                tc_fence_after();
-                uint32_t pz[2][32], xs[2][32];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    tmem_ld_32x32(pz_col + lanes + j * 32, pz[j]);
-                    tmem_ld_32x32(xs_col + lanes + j * 32, xs[j]);
-                }
-                tmem_ld_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(o_free);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint4 v;
-                    uint32_t *u = &v.x;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int c = j * 8 + 2 * k;
-                        u[k] = pack_bf16(fmaf(alpha, __uint_as_float(xs[c / 32][c % 32]), a.out_scale * __uint_as_float(pz[c / 32][c % 32])),
-                                         fmaf(alpha, __uint_as_float(xs[c / 32][c % 32 + 1]), a.out_scale * __uint_as_float(pz[c / 32][c % 32 + 1])));
-                    }
-                    if (t < L && slab * ZC + j * 8 < a.dz) *reinterpret_cast<uint4 *>(out + j * 8) = v;
-                }
-            };
-            // weight of column s: table[128 + t - s], or backwards table[128 + s - t]
-            const float *w = a.backwards ? table + TILE - t : table + TILE + t;
+            // weight of column s: table[128 + t - s], or backwards table[128 + s - t]; 32 columns that are all zeros are not read
+            const float *w = BACK ? table + TILE - threadIdx.x : table + TILE + threadIdx.x;
             for (int i = 0; i < n; ++i) {
-                const int L = tokens_of(i);
                 ok = __all_sync(~0u, mbar_wait(&sc_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 8));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t addr = tmem + lanes + (i & 1) * TILE;
-                uint32_t x[2][32];
-                tmem_ld_32x32(addr, x[0]);
-                tmem_ld_wait();
-#pragma unroll
+                // Weights go over scores that have been read: 16 columns for 32.  The loops of this kernel are no more unrolled than they have to
+                // be: one warp of each kind runs on every quarter of an SM, and with all loops unrolled the instruction cache missed
+                // in every chunk (65536 tokens of 16 heads 1070 us, 530 with loops like this one).
+#pragma unroll 1
                 for (int j = 0; j < 4; ++j) {
-                    if (j < 3) tmem_ld_32x32(addr + (j + 1) * 32, x[(j + 1) & 1]);
                     uint32_t p[16];
+                    if (BACK ? j < warp : j > warp) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int s = j * 32 + 2 * e;
-                        float y[2];
+                        for (int e = 0; e < 16; ++e) p[e] = 0u;
+                    } else {
+                        uint32_t x[32];
+                        tmem_ld_32x32(addr + j * 32, x);
+                        const float *wj = BACK ? w + j * 32 : w - j * 32;
+                        tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            y[k] = __uint_as_float(x[j & 1][2 * e + k]) * (a.backwards ? w[s + k] : w[-s - k]);
-                            if (L < TILE && s + k >= L) y[k] = 0.f;                 // what lies behind the sequence may be anything
+                        for (int e = 0; e < 16; ++e) {
+                            const int c = 2 * e;
+                            p[e] = pack_bf16(BACK ? wj[c] * __uint_as_float(x[c]) : wj[-c] * __uint_as_float(x[c]),
+                                             BACK ? wj[c + 1] * __uint_as_float(x[c + 1]) : wj[-c - 1] * __uint_as_float(x[c + 1]));
                         }
-                        p[e] = pack_bf16(y[0], y[1]);
                     }
-                    tmem_ld_wait();
-                    // over scores that have been read: 16 columns for 32
                     tmem_st_32x16(addr + j * 16, p);
                 }
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_full[i & 1]);
-                if (i > 0) write(i - 1);
-                if (!ok) break;
             }
-            if (ok && n > 0) write(n - 1);
         }
     } else if (warp < 8) {
-        // thread: token r of a chunk.  Z times its weights, in two parts.
-        const int r = threadIdx.x - 128, swz = r & 7;
+        // thread: token t of a chunk.  Z times its weights, in two parts; and out of the chunk before.
+        const int t = threadIdx.x - 128, swz = t & 7, w = warp & 3;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
         bool ok = true;
+            const float full_alpha = a.out_scale * power(a2, BACK ? TILE - 1 - t : t + 1);
+            auto write = [&](int i) {
+                const int first = chunk_of(i) * TILE, L = tokens_of(i);
+                const float alpha = !BACK || L == TILE ? full_alpha : a.out_scale * power(a2, max(L - 1 - t, 0));
+                ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
+                if (!ok) return;
+                tc_fence_after();
+                // rows go through shared memory, so that eight lanes write one row's 128 bytes
+#pragma unroll 1
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t pz[16], xs[16];
+                    tmem_ld_32x16(pz_col + lanes + b * 16, pz);
+                    tmem_ld_32x16(xs_col + lanes + b * 16, xs);
+                    tmem_ld_wait();
+                    if (b == 3) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(o_free);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int c = j * 8 + 2 * k;
+                            u[k] = pack_bf16(fma(pair(alpha, alpha), pair(xs[c], xs[c + 1]), mul(pair(a.out_scale, a.out_scale), pair(pz[c], pz[c + 1]))));
+                        }
+                        *reinterpret_cast<uint4 *>(out_rows + t * 128 + (((b * 2 + j) ^ swz) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                }
+                __syncwarp();
+                const int c = lane & 7;
+                bf16 *out = a.out + ((int64_t)(seg.first + first + w * 32) * a.heads + h) * a.dz + slab * ZC + c * 8;
+                if (slab * ZC + c * 8 < a.dz) {
+#pragma unroll 4
+                    for (int j = 0; j < 8; ++j) {
+                        const int r = j * 4 + lane / 8;
+                        if (w * 32 + r < L)
+                            *reinterpret_cast<uint4 *>(out + (int64_t)r * a.heads * a.dz) = *reinterpret_cast<const uint4 *>(out_rows + (w * 32 + r) * 128 + ((c ^ (r & 7)) << 4));
+                    }
+                }
+                __syncwarp();
+            };
         for (int i = 0; i < n; ++i) {
             const int L = tokens_of(i);
-            const float beta = r < L ? a.in_scale * power(a2, a.backwards ? r + 1 : L - 1 - r) : 0.f;
+            const float beta = t < L ? a.in_scale * power(a2, BACK ? t + 1 : L - 1 - t) : 0.f;
             ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
             if (ok && i > 0) ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)((i - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
             unsigned char *Y = stages + (i % STAGES) * Sh::STAGE + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
-            if (r >= L) {                              // rows behind the sequence: they meet weights of 0
-#pragma unroll
+            if (t >= L) {                              // rows behind the sequence: they meet weights of 0
+#pragma unroll 1
                 for (int j = 0; j < 8; ++j) {
-                    *reinterpret_cast<uint4 *>(Z + r * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    for (int c = 0; c < DX / 64; ++c) *reinterpret_cast<uint4 *>(Y + c * SLAB + r * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4 *>(Z + t * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    for (int c = 0; c < DX / 64; ++c) *reinterpret_cast<uint4 *>(Y + c * SLAB + t * 128 + j * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
             }
+            // a row is one thread's, in any order: this one meets every bank once in eight lanes
+            const __nv_bfloat162 b_hi = __float2bfloat162_rn(beta), b_lo = __float2bfloat162_rn(beta - __low2float(b_hi));
+#pragma unroll 1
+            for (int b = 0; b < 2; ++b) {
+                uint4 v[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                // a row is one thread's, in any order: this one meets every bank once in eight lanes
-                const int o = r * 128 + ((j ^ swz) << 4);
-                const uint4 v = *reinterpret_cast<const uint4 *>(Z + o);
-                const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-                uint4 hi, lo;
-                uint32_t *ph = &hi.x, *pl = &lo.x;
+                for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint4 *>(Z + t * 128 + (((b * 4 + j) ^ swz) << 4));
 #pragma unroll
-                for (int k = 0; k < 4; ++k) split2(beta * __uint_as_float(u[k] << 16), beta * __uint_as_float(u[k] & 0xFFFF0000u), ph[k], pl[k]);
-                *reinterpret_cast<uint4 *>(Z_hi + o) = hi;
-                *reinterpret_cast<uint4 *>(Z_lo + o) = lo;
+                for (int j = 0; j < 4; ++j) {
+                    const int o = t * 128 + (((b * 4 + j) ^ swz) << 4);
+                    uint4 hi, lo;
+                    times(b_hi, b_lo, v[j].x, hi.x, lo.x);
+                    times(b_hi, b_lo, v[j].y, hi.y, lo.y);
+                    times(b_hi, b_lo, v[j].z, hi.z, lo.z);
+                    times(b_hi, b_lo, v[j].w, hi.w, lo.w);
+                    *reinterpret_cast<uint4 *>(Z_hi + o) = hi;
+                    *reinterpret_cast<uint4 *>(Z_lo + o) = lo;
+                }
             }
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(z_ready);
+            if (!STATE && i > 0) write(i - 1);
+            if (!ok) break;
         }
+        if (!STATE && ok && n > 0) write(n - 1);
     } else {
         // thread: row r of S
         const int r = threadIdx.x - 256, swz = r & 7;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const bool row = r < a.dx;
         const int64_t plane = (int64_t)a.dx * a.dz, at = (int64_t)r * a.dz + slab * ZC;
-        float S[64];
+        Pair S[32];
         {
             const float *from = nullptr;
             if (!STATE) from = a.states ? a.states + ((int64_t)tile * a.heads + h) * plane : a.init ? a.init + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
+            const int64_t step = a.transposed ? a.dx : 1;
+            if (from) from += a.transposed ? (int64_t)slab * ZC * a.dx + r : at;
 #pragma unroll
-            for (int c = 0; c < 64; ++c)
-                S[c] = from && row && slab * ZC + c < a.dz ? from[a.transposed ? (int64_t)(slab * ZC + c) * a.dx + r : at + c] : 0.f;
+            for (int c = 0; c < 32; ++c) {
+                const bool in = from && row && slab * ZC + 2 * c < a.dz;
+                S[c] = pair(in ? from[2 * c * step] : 0.f, in ? from[(2 * c + 1) * step] : 0.f);
+            }
         }
         bool ok = true;
         const float keep_full = carry(decay, TILE);
@@ -351,8 +387,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
                         *reinterpret_cast<uint4 *>(S_op + r * 128 + ((j ^ swz) << 4)) =
-                            make_uint4(pack_bf16(S[j * 8], S[j * 8 + 1]), pack_bf16(S[j * 8 + 2], S[j * 8 + 3]), pack_bf16(S[j * 8 + 4], S[j * 8 + 5]),
-                                       pack_bf16(S[j * 8 + 6], S[j * 8 + 7]));
+                            make_uint4(pack_bf16(S[j * 4]), pack_bf16(S[j * 4 + 1]), pack_bf16(S[j * 4 + 2]), pack_bf16(S[j * 4 + 3]));
                 }
                 fence_proxy_async();
                 __syncwarp();
@@ -362,24 +397,28 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t hi[32], lo[32];
-                tmem_ld_32x32(u_col + lanes + j * 32, hi);
-                tmem_ld_32x32(u_col + lanes + ZC + j * 32, lo);
+            for (int j = 0; j < 4; ++j) {
+                uint32_t hi[16], lo[16];
+                tmem_ld_32x16(u_col + lanes + j * 16, hi);
+                tmem_ld_32x16(u_col + lanes + ZC + j * 16, lo);
                 tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 32; ++c) S[j * 32 + c] = fmaf(keep, S[j * 32 + c], row ? __uint_as_float(hi[c]) + __uint_as_float(lo[c]) : 0.f);
+                for (int c = 0; c < 8; ++c)
+                    S[j * 8 + c] = fma(pair(keep, keep), S[j * 8 + c], add(pair(hi[2 * c], hi[2 * c + 1]), pair(lo[2 * c], lo[2 * c + 1])));
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(u_free);
         }
-        const bool end = seg.index == (a.backwards ? 0 : seg.count - 1);
+        const bool end = seg.index == (BACK ? 0 : seg.count - 1);
         float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && a.last ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
         if (ok && to && row) {
 #pragma unroll
             for (int c = 0; c < 64; c += 4)
-                if (slab * ZC + c < a.dz) *reinterpret_cast<float4 *>(to + at + c) = make_float4(S[c], S[c + 1], S[c + 2], S[c + 3]);
+                if (slab * ZC + c < a.dz) {
+                    const float2 u = split(S[c / 2]), v = split(S[c / 2 + 1]);
+                    *reinterpret_cast<float4 *>(to + at + c) = make_float4(u.x, u.y, v.x, v.y);
+                }
         }
     }
     tc_fence_before();
@@ -429,7 +468,7 @@ static int segment_chunks(int64_t n, int64_t heads, int64_t d)
     return some >= chunks ? 0 : (int)some;
 }
 
-template <int DX, bool STATE>
+template <int DX, bool STATE, bool BACK>
 static st_status launch_fade(const FadeArgs &a, cudaStream_t stream)
 {
     CUtensorMap xm, ym, zm;
@@ -437,18 +476,20 @@ static st_status launch_fade(const FadeArgs &a, cudaStream_t stream)
         !make_tmap_table(&zm, a.z, a.n, a.heads, a.dz))
         return ST_ERR_CUDA;
     const size_t smem = fade::Shape<DX>::SMEM;
-    if (!ensure_dynamic_smem(fade_kernel<DX, STATE>, smem)) return ST_ERR_CUDA;
+    if (!ensure_dynamic_smem(fade_kernel<DX, STATE, BACK>, smem)) return ST_ERR_CUDA;
     const int64_t tiles = most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE), slabs = (a.dz + fade::ZC - 1) / fade::ZC;
-    return launch(fade_kernel<DX, STATE>, dim3((unsigned)(tiles * slabs), a.heads), fade::THREADS, smem, stream, xm, ym, zm, a);
+    return launch(fade_kernel<DX, STATE, BACK>, dim3((unsigned)(tiles * slabs), a.heads), fade::THREADS, smem, stream, xm, ym, zm, a);
 }
 static st_status run_fade(const FadeArgs &a, cudaStream_t stream)
 {
-    return a.dx <= 64 ? launch_fade<64, false>(a, stream) : launch_fade<128, false>(a, stream);
+    if (a.backwards) return a.dx <= 64 ? launch_fade<64, false, true>(a, stream) : launch_fade<128, false, true>(a, stream);
+    return a.dx <= 64 ? launch_fade<64, false, false>(a, stream) : launch_fade<128, false, false>(a, stream);
 }
 // The states that enter the segments, of y (x) z as it is kept: not transposed.
 static st_status run_states(const FadeArgs &a, cudaStream_t stream)
 {
-    const st_status rc = a.dx <= 64 ? launch_fade<64, true>(a, stream) : launch_fade<128, true>(a, stream);
+    const st_status rc = a.backwards ? (a.dx <= 64 ? launch_fade<64, true, true>(a, stream) : launch_fade<128, true, true>(a, stream))
+                                     : (a.dx <= 64 ? launch_fade<64, true, false>(a, stream) : launch_fade<128, true, false>(a, stream));
     if (rc != ST_OK) return rc;
     const unsigned tiles = (unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
     return launch(fade_carry_kernel, dim3(tiles, a.heads, (unsigned)((a.dx * a.dz + 1023) / 1024)), 256, 0, stream, a);
