@@ -19,8 +19,8 @@
 //
 // Bound by shared memory: a chunk moves some 330 KB through it (80 of copies, 190 of operands, 64 of Z and S), 128 bytes a cycle.
 //
-// Warps: 0..3 make P (a thread = a token), 4..7 weigh Z and write out (a thread = a token), 8..11 keep S (a thread = a row of it), 12 copies,
-// 13 issues the products.
+// Warps: 0..3 make P (a thread = a token), 4..7 weigh Z (a thread = a token), 8..11 keep S (a thread = a row of it) and write out (a thread = a
+// token), 12 copies, 13 issues the products.
 #include "attn_tc.cuh"
 
 namespace st {
@@ -44,11 +44,12 @@ struct FadeArgs {
 };
 
 namespace fade {
-constexpr int THREADS = 448, STAGES = 2, ZC = 64;               // ZC: columns of z of a block
-template <int DX> struct Shape {
-    static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = DX * 128;
-    static constexpr int STAGE = 2 * X_BYTES + Z_BYTES;
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 3 * Z_BYTES + 2 * TILE * sizeof(float) + 256;
+constexpr int THREADS = 448, ZC = 64;               // ZC: columns of z of a block
+template <int DX, bool STATE> struct Shape {
+    static constexpr int STAGES = STATE ? 4 : 2;
+    static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = STATE ? 0 : DX * 128, OUT_BYTES = STATE ? 0 : SLAB;
+    static constexpr int STAGE = (STATE ? 1 : 2) * X_BYTES + Z_BYTES;               // Y, Z, X
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * Z_BYTES + OUT_BYTES + 2 * TILE * sizeof(float) + 256;
 };
 }  // namespace fade
 
@@ -82,16 +83,18 @@ __device__ __forceinline__ Segment segment_of(const FadeArgs &a, int tile, int l
 // STATE: only the segment's own sum of outer products, to `states`.  BACK: backwards in time.
 template <int DX, bool STATE, bool BACK>
 __global__ void __launch_bounds__(fade::THREADS, 1)
-fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap zmap, const FadeArgs a)
+fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap zmap,
+            const __grid_constant__ CUtensorMap outmap, const FadeArgs a)
 {
     using namespace fade;
     using namespace tc;
-    using Sh = Shape<DX>;
+    using Sh = Shape<DX, STATE>;
+    constexpr int STAGES = Sh::STAGES;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
     unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_hi = S_op + Sh::S_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
     unsigned char *out_rows = Z_lo + Sh::Z_BYTES;
-    float *table = (float *)(out_rows + Sh::Z_BYTES);              // 128 zeros, then in_scale w^m
+    float *table = (float *)(out_rows + Sh::OUT_BYTES);              // 128 zeros, then in_scale w^m
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
     uint64_t *in_full = bars, *xy_empty = in_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
              *z_ready = o_free + 1, *s_ready = z_ready + 1, *u_full = s_ready + 1, *u_free = u_full + 1, *xs_done = u_free + 1;
@@ -151,17 +154,26 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 
     if (warp == 12) {
         if (elect_one()) {
-            // a stage's tiles come back from the products one after another
+            // a stage's tiles come back from the products one after another; what comes next is on its way to L2 before there is room for it
+            auto ahead = [&](int i) {
+                if (i >= n) return;
+                const int row = seg.first + chunk_of(i) * TILE;
+                prefetch_3d(&zmap, slab * ZC, h, row);
+                if (slab != 0) return;
+                prefetch_tile<DX>(&ymap, h, row);
+                if (!STATE) prefetch_tile<DX>(&xmap, h, row);
+            };
             for (int i = 0; i < n; ++i) {
                 const int s = i % STAGES, row = seg.first + chunk_of(i) * TILE;
                 const uint32_t parity = (uint32_t)((i / STAGES + 1) & 1);
                 unsigned char *st = stages + s * Sh::STAGE;
                 if (!mbar_wait(&xy_empty[s], parity, abort_flag, a.status, 1)) break;
-                mbar_expect_tx(&in_full[s], STATE ? Sh::X_BYTES + Sh::Z_BYTES : Sh::STAGE);
-                load_tile<DX>(st + Sh::X_BYTES, &ymap, &in_full[s], h, row);
-                if (!STATE) load_tile<DX>(st, &xmap, &in_full[s], h, row);
+                mbar_expect_tx(&in_full[s], Sh::STAGE);
+                load_tile<DX>(st, &ymap, &in_full[s], h, row);
+                if (!STATE) load_tile<DX>(st + Sh::X_BYTES + Sh::Z_BYTES, &xmap, &in_full[s], h, row);
                 if (!mbar_wait(&z_empty[s], parity, abort_flag, a.status, 15)) break;
-                tma_load_3d(st + 2 * Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
+                tma_load_3d(st + Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
+                ahead(i + STAGES);
             }
         }
         __syncwarp();
@@ -169,62 +181,56 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         if (elect_one()) {
             const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, 2 * ZC);
             bool ok = true;
-            int scored = 0;                         // chunks whose scores have been issued
-            // scores of chunk i; without `wait` only if its tiles are there, and whole: else the rows behind the sequence are cleared first
-            auto score = [&](int i, bool wait) {
-                if (STATE || !ok || i >= n || scored > i || (!wait && tokens_of(i) < TILE)) return;
-                const uint32_t parity = (uint32_t)((i / STAGES) & 1);
-                if (wait) ok = mbar_wait(&in_full[i % STAGES], parity, abort_flag, a.status, 2);
-                else if (!mbar_try_wait(&in_full[i % STAGES], parity)) return;
-                if (!ok) return;
-                tc_fence_after();
-                const unsigned char *st = stages + (i % STAGES) * Sh::STAGE;
-                mma_rows<DX>(tmem + (i & 1) * TILE, st, st + Sh::X_BYTES, sc_idesc);
-                tc_commit(&sc_full[i & 1]);
-                ++scored;
-            };
-            for (int i = 0; i < n && ok; ++i) {
-                const unsigned char *X = stages + (i % STAGES) * Sh::STAGE, *Y = X + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
-                const bool whole = tokens_of(i) == TILE;
-                if (whole) {
-                    score(i, true);
-                    score(i + 1, false);
-                }
-                if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
-                if (ok) ok = mbar_wait(z_ready, (uint32_t)(i & 1), abort_flag, a.status, 3);
-                if (!whole) score(i, true);
-                if (ok && i > 0) ok = mbar_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
-                if (!ok) break;
-                tc_fence_after();
-                // Y^T times both parts side by side: the tile of Y is read once
-                const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_hi), SLAB, 1024);
+            // U and XS of a chunk, scores of the next, PZ of the chunk: each product has one place in the code, for the instruction cache
+            for (int i = -1; i < n && ok; ++i) {
+                const unsigned char *Y = stages + (i & (STAGES - 1)) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *X = Z + Sh::Z_BYTES;
+                if (i >= 0) {
+                    if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
+                    if (ok) ok = mbar_wait(z_ready, (uint32_t)(i & 1), abort_flag, a.status, 3);
+                    if (ok && i > 0) ok = mbar_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
+                    if (!ok) break;
+                    tc_fence_after();
+                    // Y^T times both parts side by side: the tile of Y is read once
+                    const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_hi), SLAB, 1024);
 #pragma unroll
-                for (int k = 0; k < TILE / 16; ++k)
-                    mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k ? 1u : 0u);
-                tc_commit(u_full);
-                if (STATE) {
+                    for (int k = 0; k < TILE / 16; ++k)
+                        mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k ? 1u : 0u);
+                    tc_commit(u_full);
+                    if (STATE) {
+                        tc_commit(&xy_empty[i % STAGES]);
+                        tc_commit(&z_empty[i % STAGES]);
+                        continue;
+                    }
+                    if (i > 0) ok = mbar_wait(o_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 4);
+                    if (ok) ok = mbar_wait(s_ready, (uint32_t)(i & 1), abort_flag, a.status, 5);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t x = make_smem_desc(smem_u32(X), 16, 1024), st = make_smem_desc(smem_u32(S_op), SLAB, 1024);
+#pragma unroll
+                    for (int k = 0; k < DX / 16; ++k)
+                        mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), st + (uint64_t)(k * 2048 >> 4), pz_idesc, k ? 1u : 0u);
+                    tc_commit(xs_done);
                     tc_commit(&xy_empty[i % STAGES]);
-                    tc_commit(&z_empty[i % STAGES]);
-                    continue;
                 }
-                score(i + 1, false);
-                if (i > 0) ok = mbar_wait(o_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 4);
-                if (ok) ok = mbar_wait(s_ready, (uint32_t)(i & 1), abort_flag, a.status, 5);
-                if (!ok) break;
-                tc_fence_after();
-                const uint64_t x = make_smem_desc(smem_u32(X), 16, 1024), st = make_smem_desc(smem_u32(S_op), SLAB, 1024);
-#pragma unroll
-                for (int k = 0; k < DX / 16; ++k)
-                    mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), st + (uint64_t)(k * 2048 >> 4), pz_idesc, k ? 1u : 0u);
-                tc_commit(xs_done);
-                tc_commit(&xy_empty[i % STAGES]);
-                score(i + 1, false);
-                ok = mbar_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
-                if (!ok) break;
-                tc_fence_after();
-                mma_tokens(pz_col, tmem + (i & 1) * TILE, Z, pz_idesc, false);
-                tc_commit(o_full);
-                tc_commit(&z_empty[i % STAGES]);
+                if (!STATE && i + 1 < n) {
+                    const int e = i + 1;
+                    ok = mbar_wait(&in_full[e % STAGES], (uint32_t)((e / STAGES) & 1), abort_flag, a.status, 2);
+                    // rows behind the sequence are cleared first
+                    if (ok && tokens_of(e) < TILE) ok = mbar_wait(z_ready, (uint32_t)(e & 1), abort_flag, a.status, 16);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const unsigned char *st = stages + (e % STAGES) * Sh::STAGE;
+                    mma_rows<DX>(tmem + (e & 1) * TILE, st + Sh::X_BYTES + Sh::Z_BYTES, st, sc_idesc);
+                    tc_commit(&sc_full[e & 1]);
+                }
+                if (!STATE && i >= 0) {
+                    ok = mbar_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
+                    if (!ok) break;
+                    tc_fence_after();
+                    mma_tokens(pz_col, tmem + (i & 1) * TILE, Z, pz_idesc, false);
+                    tc_commit(o_full);
+                    tc_commit(&z_empty[i % STAGES]);
+                }
             }
         }
         __syncwarp();
@@ -270,60 +276,16 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             }
         }
     } else if (warp < 8) {
-        // thread: token t of a chunk.  Z times its weights, in two parts; and out of the chunk before.
-        const int t = threadIdx.x - 128, swz = t & 7, w = warp & 3;
-        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        // thread: token t of a chunk.  Z times its weights, in two parts.
+        const int t = threadIdx.x - 128, swz = t & 7;
         bool ok = true;
-            const float full_alpha = a.out_scale * power(a2, BACK ? TILE - 1 - t : t + 1);
-            auto write = [&](int i) {
-                const int first = chunk_of(i) * TILE, L = tokens_of(i);
-                const float alpha = !BACK || L == TILE ? full_alpha : a.out_scale * power(a2, max(L - 1 - t, 0));
-                ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
-                if (!ok) return;
-                tc_fence_after();
-                // rows go through shared memory, so that eight lanes write one row's 128 bytes
-#pragma unroll 1
-                for (int b = 0; b < 4; ++b) {
-                    uint32_t pz[16], xs[16];
-                    tmem_ld_32x16(pz_col + lanes + b * 16, pz);
-                    tmem_ld_32x16(xs_col + lanes + b * 16, xs);
-                    tmem_ld_wait();
-                    if (b == 3) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(o_free);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t u[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int c = j * 8 + 2 * k;
-                            u[k] = pack_bf16(fma(pair(alpha, alpha), pair(xs[c], xs[c + 1]), mul(pair(a.out_scale, a.out_scale), pair(pz[c], pz[c + 1]))));
-                        }
-                        *reinterpret_cast<uint4 *>(out_rows + t * 128 + (((b * 2 + j) ^ swz) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
-                    }
-                }
-                __syncwarp();
-                const int c = lane & 7;
-                bf16 *out = a.out + ((int64_t)(seg.first + first + w * 32) * a.heads + h) * a.dz + slab * ZC + c * 8;
-                if (slab * ZC + c * 8 < a.dz) {
-#pragma unroll 4
-                    for (int j = 0; j < 8; ++j) {
-                        const int r = j * 4 + lane / 8;
-                        if (w * 32 + r < L)
-                            *reinterpret_cast<uint4 *>(out + (int64_t)r * a.heads * a.dz) = *reinterpret_cast<const uint4 *>(out_rows + (w * 32 + r) * 128 + ((c ^ (r & 7)) << 4));
-                    }
-                }
-                __syncwarp();
-            };
         for (int i = 0; i < n; ++i) {
             const int L = tokens_of(i);
             const float beta = t < L ? a.in_scale * power(a2, BACK ? t + 1 : L - 1 - t) : 0.f;
             ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
             if (ok && i > 0) ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)((i - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
-            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE + Sh::X_BYTES, *Z = Y + Sh::X_BYTES;
+            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES;
             if (t >= L) {                              // rows behind the sequence: they meet weights of 0
 #pragma unroll 1
                 for (int j = 0; j < 8; ++j) {
@@ -353,14 +315,11 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(z_ready);
-            if (!STATE && i > 0) write(i - 1);
-            if (!ok) break;
         }
-        if (!STATE && ok && n > 0) write(n - 1);
     } else {
-        // thread: row r of S
-        const int r = threadIdx.x - 256, swz = r & 7;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        // thread: row r of S, and token r of a chunk's out
+        const int r = threadIdx.x - 256, swz = r & 7, w = warp & 3;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const bool row = r < a.dx;
         const int64_t plane = (int64_t)a.dx * a.dz, at = (int64_t)r * a.dz + slab * ZC;
         Pair S[32];
@@ -377,6 +336,52 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         bool ok = true;
         const float keep_full = carry(decay, TILE);
+        const float full_alpha = a.out_scale * power(a2, BACK ? TILE - 1 - r : r + 1);
+        auto write = [&](int i) {
+            const int first = chunk_of(i) * TILE, L = tokens_of(i);
+            const float alpha = !BACK || L == TILE ? full_alpha : a.out_scale * power(a2, max(L - 1 - r, 0));
+            ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
+            if (!ok) return;
+            tc_fence_after();
+            // a warp's 32 rows go through shared memory and out in one copy; rows at a sequence's end are written one by one
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+#pragma unroll 1
+            for (int b = 0; b < 4; ++b) {
+                uint32_t pz[16], xs[16];
+                tmem_ld_32x16(pz_col + lanes + b * 16, pz);
+                tmem_ld_32x16(xs_col + lanes + b * 16, xs);
+                tmem_ld_wait();
+                if (b == 3) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(o_free);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t u[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = j * 8 + 2 * k;
+                        u[k] = pack_bf16(fma(pair(alpha, alpha), pair(xs[c], xs[c + 1]), mul(pair(a.out_scale, a.out_scale), pair(pz[c], pz[c + 1]))));
+                    }
+                    *reinterpret_cast<uint4 *>(out_rows + r * 128 + (((b * 2 + j) ^ swz) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+            }
+            const int row = seg.first + first + w * 32;
+            if (w * 32 + 32 <= L) {
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) tma_store_3d(&outmap, out_rows + w * 4096, slab * ZC, h, row);
+            } else {
+                __syncwarp();
+                const int c = lane & 7;
+                for (int k = lane / 8; w * 32 + k < L; k += 4)
+                    if (slab * ZC + c * 8 < a.dz)
+                        *reinterpret_cast<uint4 *>(a.out + ((int64_t)(row + k) * a.heads + h) * a.dz + slab * ZC + c * 8) =
+                            *reinterpret_cast<const uint4 *>(out_rows + (w * 32 + k) * 128 + ((c ^ (k & 7)) << 4));
+            }
+        };
         for (int i = 0; i < n; ++i) {
             const int L = tokens_of(i);
             const float keep = L == TILE ? keep_full : carry(decay, L);
@@ -392,6 +397,8 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(s_ready);
+                if (i > 0) write(i - 1);
+                if (!ok) break;
             }
             ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)(i & 1), abort_flag, a.status, 14));
             if (!ok) break;
@@ -410,6 +417,8 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             __syncwarp();
             if (lane == 0) mbar_arrive(u_free);
         }
+        if (!STATE && ok && n > 0) write(n - 1);
+        if (!STATE && lane == 0) tma_store_wait();
         const bool end = seg.index == (BACK ? 0 : seg.count - 1);
         float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && a.last ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
         if (ok && to && row) {
@@ -445,17 +454,22 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const FadeArgs a)
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (a.init) s = *reinterpret_cast<const float4 *>(a.init + ((int64_t)seg.seq * a.heads + h) * plane + e);
     const float decay = a.log_decay[h], whole = carry(decay, rows);
-    for (int i = 0; i < seg.count; ++i) {
-        const int k = a.backwards ? seg.count - 1 - i : i;
-        float4 *at = reinterpret_cast<float4 *>(states + k * step);
-        if (i + 1 == seg.count) {
-            *at = s;
-            break;
+    constexpr int AT_ONCE = 8;
+    for (int i0 = 0; i0 < seg.count; i0 += AT_ONCE) {
+        float4 own[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int i = i0 + j, k = a.backwards ? seg.count - 1 - i : i;
+            own[j] = i + 1 < seg.count ? *reinterpret_cast<const float4 *>(states + k * step) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        const float4 own = *at;
-        const float f = (k + 1) * rows <= r.len ? whole : carry(decay, r.len - k * rows);
-        *at = s;
-        s = make_float4(fmaf(f, s.x, own.x), fmaf(f, s.y, own.y), fmaf(f, s.z, own.z), fmaf(f, s.w, own.w));
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            const int i = i0 + j, k = a.backwards ? seg.count - 1 - i : i;
+            if (i >= seg.count) break;
+            const float f = (k + 1) * rows <= r.len ? whole : carry(decay, r.len - k * rows);
+            *reinterpret_cast<float4 *>(states + k * step) = s;
+            s = make_float4(fmaf(f, s.x, own[j].x), fmaf(f, s.y, own[j].y), fmaf(f, s.z, own[j].z), fmaf(f, s.w, own[j].w));
+        }
     }
 }
 
@@ -471,14 +485,17 @@ static int segment_chunks(int64_t n, int64_t heads, int64_t d)
 template <int DX, bool STATE, bool BACK>
 static st_status launch_fade(const FadeArgs &a, cudaStream_t stream)
 {
-    CUtensorMap xm, ym, zm;
+    CUtensorMap xm, ym, zm, om;
+    const Table out{a.out, (int64_t)a.heads * a.dz, a.dz};
+    if (STATE) om = CUtensorMap{};
+    else if (!make_tmap_table(&om, out, a.n, a.heads, a.dz, 32)) return ST_ERR_CUDA;
     if (!make_tmap_table(&xm, STATE ? a.y : a.x, a.n, a.heads, a.dx) || !make_tmap_table(&ym, a.y, a.n, a.heads, a.dx) ||
         !make_tmap_table(&zm, a.z, a.n, a.heads, a.dz))
         return ST_ERR_CUDA;
-    const size_t smem = fade::Shape<DX>::SMEM;
+    const size_t smem = fade::Shape<DX, STATE>::SMEM;
     if (!ensure_dynamic_smem(fade_kernel<DX, STATE, BACK>, smem)) return ST_ERR_CUDA;
     const int64_t tiles = most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE), slabs = (a.dz + fade::ZC - 1) / fade::ZC;
-    return launch(fade_kernel<DX, STATE, BACK>, dim3((unsigned)(tiles * slabs), a.heads), fade::THREADS, smem, stream, xm, ym, zm, a);
+    return launch(fade_kernel<DX, STATE, BACK>, dim3((unsigned)(tiles * slabs), a.heads), fade::THREADS, smem, stream, xm, ym, zm, om, a);
 }
 static st_status run_fade(const FadeArgs &a, cudaStream_t stream)
 {

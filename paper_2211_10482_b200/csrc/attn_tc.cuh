@@ -41,6 +41,29 @@ __device__ __forceinline__ void load_tile(unsigned char *dst, const CUtensorMap 
     for (int c = 0; c < COLS / 64; ++c) tma_load_3d(dst + c * SLAB, m, bar, c * 64, head, row);
 }
 
+// The other way: what lies outside the table is not written.  Needs a proxy fence by the writers of the shared memory first.
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *m, const void *src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(src)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// The same copies as far as L2.
+__device__ __forceinline__ void prefetch_3d(const CUtensorMap *m, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global [%0, {%1, %2, %3}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+template <int COLS>
+__device__ __forceinline__ void prefetch_tile(const CUtensorMap *m, int head, int row)
+{
+#pragma unroll
+    for (int c = 0; c < COLS / 64; ++c) prefetch_3d(m, c * 64, head, row);
+}
+
 // The A operand from tensor memory: 128 lanes, two bf16 of consecutive k to a column.
 __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
