@@ -46,10 +46,11 @@ struct FadeArgs {
 namespace fade {
 constexpr int THREADS = 448, ZC = 64;               // ZC: columns of z of a block
 template <int DX, bool STATE> struct Shape {
-    static constexpr int STAGES = STATE ? 4 : 2;
+    static constexpr int STAGES = STATE ? 3 : 2;
+    static constexpr int BUFS = STATE ? 2 : 1;                                      // of the weighted Z
     static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = STATE ? 0 : DX * 128, OUT_BYTES = STATE ? 0 : SLAB;
     static constexpr int STAGE = (STATE ? 1 : 2) * X_BYTES + Z_BYTES;               // Y, Z, X
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * Z_BYTES + OUT_BYTES + 2 * TILE * sizeof(float) + 256;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * BUFS * Z_BYTES + OUT_BYTES + 2 * TILE * sizeof(float) + 256;
 };
 }  // namespace fade
 
@@ -89,15 +90,15 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     using namespace fade;
     using namespace tc;
     using Sh = Shape<DX, STATE>;
-    constexpr int STAGES = Sh::STAGES;
+    constexpr int STAGES = Sh::STAGES, BUFS = Sh::BUFS;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
-    unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_hi = S_op + Sh::S_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
-    unsigned char *out_rows = Z_lo + Sh::Z_BYTES;
+    unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_parts = S_op + Sh::S_BYTES,      // Z_parts: [buffer][2]
+                  *out_rows = Z_parts + 2 * BUFS * Sh::Z_BYTES;
     float *table = (float *)(out_rows + Sh::OUT_BYTES);              // 128 zeros, then in_scale w^m
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
     uint64_t *in_full = bars, *xy_empty = in_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
-             *z_ready = o_free + 1, *s_ready = z_ready + 1, *u_full = s_ready + 1, *u_free = u_full + 1, *xs_done = u_free + 1;
+             *z_ready = o_free + 1, *s_ready = z_ready + BUFS, *u_full = s_ready + 1, *u_free = u_full + BUFS, *xs_done = u_free + 1;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
@@ -134,9 +135,11 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         mbar_init(&p_full[1], 4);
         mbar_init(o_full, 1);
         mbar_init(o_free, 4);
-        mbar_init(z_ready, 4);
+        for (int b = 0; b < BUFS; ++b) {
+            mbar_init(&z_ready[b], 4);
+            mbar_init(&u_full[b], 1);
+        }
         mbar_init(s_ready, 4);
-        mbar_init(u_full, 1);
         mbar_init(u_free, 4);
         mbar_init(xs_done, 1);
         *abort_flag = 0;
@@ -183,19 +186,19 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             bool ok = true;
             // U and XS of a chunk, scores of the next, PZ of the chunk: each product has one place in the code, for the instruction cache
             for (int i = -1; i < n && ok; ++i) {
-                const unsigned char *Y = stages + (i & (STAGES - 1)) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *X = Z + Sh::Z_BYTES;
+                const unsigned char *Y = stages + ((i + STAGES) % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *X = Z + Sh::Z_BYTES;
                 if (i >= 0) {
                     if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
-                    if (ok) ok = mbar_wait(z_ready, (uint32_t)(i & 1), abort_flag, a.status, 3);
+                    if (ok) ok = mbar_wait(&z_ready[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 3);
                     if (ok && i > 0) ok = mbar_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
                     if (!ok) break;
                     tc_fence_after();
                     // Y^T times both parts side by side: the tile of Y is read once
-                    const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_hi), SLAB, 1024);
+                    const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_parts + (i % BUFS) * 2 * Sh::Z_BYTES), SLAB, 1024);
 #pragma unroll
                     for (int k = 0; k < TILE / 16; ++k)
                         mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k ? 1u : 0u);
-                    tc_commit(u_full);
+                    tc_commit(&u_full[i % BUFS]);
                     if (STATE) {
                         tc_commit(&xy_empty[i % STAGES]);
                         tc_commit(&z_empty[i % STAGES]);
@@ -216,7 +219,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                     const int e = i + 1;
                     ok = mbar_wait(&in_full[e % STAGES], (uint32_t)((e / STAGES) & 1), abort_flag, a.status, 2);
                     // rows behind the sequence are cleared first
-                    if (ok && tokens_of(e) < TILE) ok = mbar_wait(z_ready, (uint32_t)(e & 1), abort_flag, a.status, 16);
+                    if (ok && tokens_of(e) < TILE) ok = mbar_wait(&z_ready[e % BUFS], (uint32_t)((e / BUFS) & 1), abort_flag, a.status, 16);
                     if (!ok) break;
                     tc_fence_after();
                     const unsigned char *st = stages + (e % STAGES) * Sh::STAGE;
@@ -283,9 +286,9 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             const int L = tokens_of(i);
             const float beta = t < L ? a.in_scale * power(a2, BACK ? t + 1 : L - 1 - t) : 0.f;
             ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
-            if (ok && i > 0) ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)((i - 1) & 1), abort_flag, a.status, 9));
+            if (ok && i >= BUFS) ok = __all_sync(~0u, mbar_wait(&u_full[i % BUFS], (uint32_t)((i / BUFS - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
-            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES;
+            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *Z_hi = Z_parts + (i % BUFS) * 2 * Sh::Z_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
             if (t >= L) {                              // rows behind the sequence: they meet weights of 0
 #pragma unroll 1
                 for (int j = 0; j < 8; ++j) {
@@ -314,7 +317,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             }
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(z_ready);
+            if (lane == 0) mbar_arrive(&z_ready[i % BUFS]);
         }
     } else {
         // thread: row r of S, and token r of a chunk's out
@@ -400,7 +403,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 if (i > 0) write(i - 1);
                 if (!ok) break;
             }
-            ok = __all_sync(~0u, mbar_wait(u_full, (uint32_t)(i & 1), abort_flag, a.status, 14));
+            ok = __all_sync(~0u, mbar_wait(&u_full[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 14));
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
