@@ -20,6 +20,7 @@ struct StepArgs {
     bf16 *k_pages, *v_pages;
     const int *table, *lens;
     int nseq, heads, group, d, pages, page, cols, window, sinks;
+    unsigned page_magic;               // floor((2^32 - 1) / page): __umulhi with it is s / page or one less, s below 2^31
     int64_t page_stride, token_stride, head_stride;
     float scale;
     bf16 *out;
@@ -28,9 +29,10 @@ struct StepArgs {
 
 namespace wstep {
 constexpr int WARPS = 4, KEYS = 16, HEADS = 16, STAGES = 3;
+constexpr int BLOCKS = 2;                  // of an SM, wanted
 template <int DP> struct Shape {
     static constexpr int TILE_BYTES = KEYS * DP * 2, STAGE = 2 * TILE_BYTES, RING = STAGES * STAGE;
-    static constexpr size_t SMEM = (size_t)WARPS * RING + 2 * (WARPS + 1) * HEADS * sizeof(float) + 16;
+    static constexpr size_t SMEM = (size_t)WARPS * RING + 2 * (WARPS + 1) * HEADS * sizeof(float) + WARPS * KEYS * sizeof(int64_t) + 16;
     static_assert(HEADS * DP * 4 <= RING, "a warp's output takes the place of its ring");
 };
 }  // namespace wstep
@@ -60,6 +62,13 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr)
     return x;
 }
 
+__device__ __forceinline__ float fast_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 template <int DP>
 __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const StepArgs a)
 {
@@ -68,7 +77,8 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
     constexpr int CHUNKS = DP / 8;                        // 16-byte pieces of a row
     extern __shared__ __align__(128) unsigned char smem[];
     float *most_w = (float *)(smem + WARPS * S::RING), *sum_w = most_w + WARPS * HEADS, *most_b = sum_w + WARPS * HEADS, *sum_b = most_b + HEADS;
-    int *bad = (int *)(sum_b + HEADS);
+    int64_t *offsets = (int64_t *)(sum_b + HEADS);
+    int *bad = (int *)(offsets + WARPS * KEYS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = gridDim.x, split = blockIdx.x, chunks = (a.group + HEADS - 1) / HEADS, b = blockIdx.z;
     const int hk = blockIdx.y / chunks, g0 = blockIdx.y % chunks * HEADS, g = min(a.group - g0, HEADS), kv_heads = a.heads / a.group;
@@ -83,8 +93,8 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
     __syncthreads();
     const int told = a.lens[b], len = (int)min((int64_t)max(told, 0), (int64_t)a.cols * a.page), t = len - 1;
     if (told != len && threadIdx.x == 0) *bad = 1;
-    // visible keys: [0, first) and [lo, t]; key number u of them
-    const int lo = max(0, t - a.window + 1), first = min(a.sinks, lo), seen = first + t + 1 - lo, tiles = (seen + KEYS - 1) / KEYS;
+    // visible keys: [0, first) and [lo, t), which are cached, and t, the new one
+    const int lo = max(0, t - a.window + 1), first = min(a.sinks, lo), cached = first + max(t, 0) - lo, tiles = (cached + KEYS - 1) / KEYS;
     const bf16 *kn = a.k + ((int64_t)b * kv_heads + hk) * a.d, *vn = a.v + ((int64_t)b * kv_heads + hk) * a.d;
     const bf16 *kc = a.k_pages + hk * a.head_stride, *vc = a.v_pages + hk * a.head_stride;
     const uint32_t ring = tc::smem_u32(smem + warp * S::RING);
@@ -100,37 +110,48 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
             q[k][i] = row < g && col < a.d ? *reinterpret_cast<const uint32_t *>(a.q + ((int64_t)b * a.heads + hk * a.group + g0 + row) * a.d + col) : 0u;
         }
 
-    // Lane r (of 16) knows where row r of a tile lies: the page's number (-1: none, -2: the new token), and the place in the page.
-    auto place = [&](int tile, int &page, int &slot) {
+    // The new token's row of the cache; nobody reads it there in this call: it is taken from k and v, behind the cached keys.
+    if (split == 0 && warp == 0 && g0 == 0 && len > 0) {
+        const int p = a.table[(int64_t)b * a.cols + t / a.page], col = lane * 8 % DP;
+        if ((unsigned)p >= (unsigned)a.pages) *bad = 1;
+        else if (lane * 8 < 2 * DP && col < a.d)
+            *reinterpret_cast<uint4 *>((lane * 8 < DP ? a.k_pages : a.v_pages) + (int64_t)p * a.page_stride + (t % a.page) * a.token_stride + hk * a.head_stride + col) =
+                *reinterpret_cast<const uint4 *>((lane * 8 < DP ? kn : vn) + col);
+    }
+
+    // Lane r (of 16) finds row r of a tile: its page (-1: none, or outside the cache), then its offset in the pages, which goes where all lanes
+    // that copy a piece of the row see it.
+    auto page_of = [&](int tile, int &slot) -> int {
         const int u = tile * KEYS + (lane & 15), s = u < first ? u : lo + u - first;
-        page = -1;
         slot = 0;
-        if (u < seen) {
-            const int p = s / a.page;
-            slot = s - p * a.page;
-            page = a.table[(int64_t)b * a.cols + p];
-            if ((unsigned)page >= (unsigned)a.pages) {
-                page = -1;
-                *bad = 1;
-            } else if (s == t) {
-                page = -2;
-            }
-        }
+        if (u >= cached) return -1;
+        const int p = (int)__umulhi((unsigned)s, a.page_magic), q = s - p * a.page >= a.page ? p + 1 : p;
+        slot = s - q * a.page;
+        const int page = a.table[(int64_t)b * a.cols + q];
+        if ((unsigned)page < (unsigned)a.pages) return page;
+        *bad = 1;
+        return -1;
     };
-    // bit r: row r of the tile is there
+    int64_t *at = offsets + warp * KEYS;
+    const int piece = lane % CHUNKS, row0 = lane / CHUNKS;
+    const bool inside = piece * 8 < a.d;
+    constexpr int ROWS = 32 / CHUNKS;                      // rows that a warp copies at a time
+    // bit r: row r of the tile is there.  What is not there is zeros.
     auto fetch = [&](int tile, int stage, int page, int slot) -> unsigned {
-        const int64_t at = (int64_t)max(page, 0) * a.page_stride + slot * a.token_stride;
-        const uint32_t dst = ring + stage * S::STAGE;
-        const unsigned there = __ballot_sync(~0u, page != -1) & 0xFFFFu, fresh = __ballot_sync(~0u, page == -2);
+        const unsigned there = __ballot_sync(~0u, page >= 0) & 0xFFFFu;
         if (tile < tiles) {
+            __syncwarp();
+            if (lane < KEYS) at[lane] = page >= 0 ? (int64_t)page * a.page_stride + slot * a.token_stride : 0;
+            __syncwarp();
+            const uint32_t dst = ring + stage * S::STAGE;
 #pragma unroll
-            for (int i = 0; i < KEYS * CHUNKS / 32; ++i) {
-                const int row = (i * 32 + lane) / CHUNKS, c = (i * 32 + lane) % CHUNKS;
-                const int64_t from = __shfl_sync(~0u, at, row);
-                const bool in = (there >> row & 1) && c * 8 < a.d, is_new = fresh >> row & 1;
-                const uint32_t o = dst + row * (DP * 2) + ((c ^ (row & 7)) << 4);
-                copy16(o, in ? (is_new ? kn : kc + from) + c * 8 : a.q, in);
-                copy16(o + S::TILE_BYTES, in ? (is_new ? vn : vc + from) + c * 8 : a.q, in);
+            for (int i = 0; i < KEYS / ROWS; ++i) {
+                const int row = row0 + i * ROWS;
+                const int64_t from = at[row] + piece * 8;
+                const bool in = inside && (there >> row & 1);
+                const uint32_t o = dst + row * (DP * 2) + ((piece ^ (row & 7)) << 4);
+                copy16(o, kc + from, in);
+                copy16(o + S::TILE_BYTES, vc + from, in);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
@@ -143,60 +164,34 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
     for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
-    unsigned there[STAGES];
-    int page, slot;
-    place(tile0, page, slot);
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-        const int p = page, l = slot;
-        place(tile0 + (s + 1) * step, page, slot);
-        there[s] = fetch(tile0 + s * step, s, p, l);
-    }
-    // the new token's row of the cache; nobody reads it there in this call
-    if (split == 0 && warp == 0 && g0 == 0 && len > 0) {
-        const int p = a.table[(int64_t)b * a.cols + t / a.page];
-        if ((unsigned)p < (unsigned)a.pages && lane * 8 < 2 * DP) {
-            const int col = lane * 8 % DP;
-            const int64_t at = (int64_t)p * a.page_stride + (t % a.page) * a.token_stride + hk * a.head_stride + col;
-            if (col < a.d) *reinterpret_cast<uint4 *>((lane * 8 < DP ? a.k_pages : a.v_pages) + at) = *reinterpret_cast<const uint4 *>((lane * 8 < DP ? kn : vn) + col);
-        }
-    }
-    int stage = 0;
-    for (int tile = tile0; tile < tiles; tile += step) {
-        {
-            const int p = page, l = slot, s = stage == 0 ? STAGES - 1 : stage - 1;
-            place(tile + STAGES * step, page, slot);
-            __syncwarp();                                  // every lane is done with the stage that is filled again
-            there[STAGES - 1] = fetch(tile + (STAGES - 1) * step, s, p, l);
-        }
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-        __syncwarp();
+    // 16 keys in a stage
+    auto attend = [&](int stage, unsigned there) {
         const uint32_t K = ring + stage * S::STAGE, V = K + S::TILE_BYTES;
         float x[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int k = 0; k < DP / 32; ++k)
 #pragma unroll
-            for (int k = 0; k < DP / 32; ++k) {
+            for (int n = 0; n < 2; ++n) {
                 uint32_t f[4];                             // 8 keys, 32 columns
-                const int row = n * 8 + (lane & 7), ch = k * 4 + lane / 8;
-                ldmatrix4(f, K + row * (DP * 2) + ((ch ^ (row & 7)) << 4));
+                ldmatrix4(f, K + (n * 8 + (lane & 7)) * (DP * 2) + (((k * 4 + lane / 8) ^ (lane & 7)) << 4));
                 mma16816(x[n], q[2 * k], f[0], f[1]);
                 mma16816(x[n], q[2 * k + 1], f[2], f[3]);
             }
-        float top[2] = {-INFINITY, -INFINITY};
+        if (there != 0xFFFFu)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!(there[0] >> (n * 8 + (lane & 3) * 2 + (i & 1)) & 1)) x[n][i] = -INFINITY;
-                top[i >> 1] = fmaxf(top[i >> 1], x[n][i]);
-            }
+                for (int i = 0; i < 4; ++i)
+                    if (!(there >> (n * 8 + (lane & 3) * 2 + (i & 1)) & 1)) x[n][i] = -INFINITY;
+        float top[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            top[i] = fmaxf(fmaxf(x[0][2 * i], x[0][2 * i + 1]), fmaxf(x[1][2 * i], x[1][2 * i + 1]));
             top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 1));
             top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 2));
         }
-        if (__any_sync(~0u, top[0] > most[0] || top[1] > most[1])) {
+        // as long as no weight passes 2^8 the reference stays: any reference gives the same quotient
+        if (__any_sync(~0u, c * (top[0] - most[0]) > 8.f || c * (top[1] - most[1]) > 8.f)) {
             float f[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -216,7 +211,7 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float y0 = exp2f(fmaf(c, x[n][2 * i], -ref[i])), y1 = exp2f(fmaf(c, x[n][2 * i + 1], -ref[i]));
+                const float y0 = fast_exp2(fmaf(c, x[n][2 * i], -ref[i])), y1 = fast_exp2(fmaf(c, x[n][2 * i + 1], -ref[i]));
                 sum[i] += y0 + y1;
                 const __nv_bfloat162 w = __floats2bfloat162_rn(y0, y1);          // rounded once, for the product with V
                 p[n * 2 + i] = *reinterpret_cast<const uint32_t *>(&w);
@@ -224,17 +219,44 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
 #pragma unroll
         for (int n = 0; n < DP / 16; ++n) {
             uint32_t f[4];                                 // 16 keys, 16 columns
-            const int row = lane & 15, ch = n * 2 + lane / 16;
-            ldmatrix4_trans(f, V + row * (DP * 2) + ((ch ^ (row & 7)) << 4));
+            ldmatrix4_trans(f, V + (lane & 15) * (DP * 2) + (((n * 2 + lane / 16) ^ (lane & 7)) << 4));
             mma16816(o[2 * n], p, f[0], f[1]);
             mma16816(o[2 * n + 1], p, f[2], f[3]);
         }
+    };
+    unsigned there[STAGES];
+    int slot, page = page_of(tile0, slot);
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        const int p = page, l = slot;
+        page = page_of(tile0 + (s + 1) * step, slot);
+        there[s] = fetch(tile0 + s * step, s, p, l);
+    }
+    int stage = 0;
+    for (int tile = tile0; tile < tiles; tile += step) {
+        const int p = page, l = slot;
+        page = page_of(tile + STAGES * step, slot);
+        there[STAGES - 1] = fetch(tile + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1, p, l);      // the stage before was read by all lanes
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+        __syncwarp();
+        attend(stage, there[0]);
 #pragma unroll
         for (int s = 0; s + 1 < STAGES; ++s) there[s] = there[s + 1];
         if (++stage == STAGES) stage = 0;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncwarp();
+    if (split == 0 && warp == 0 && len > 0) {              // the new token, as a tile of one key
+        for (int i = lane; i < 2 * KEYS * CHUNKS; i += 32) {
+            const int v = i / (KEYS * CHUNKS), row = i / CHUNKS % KEYS, ch = i % CHUNKS;
+            const bool in = row == 0 && ch * 8 < a.d;
+            *reinterpret_cast<uint4 *>(smem + v * S::TILE_BYTES + row * (DP * 2) + ((ch ^ (row & 7)) << 4)) =
+                in ? *reinterpret_cast<const uint4 *>((v ? vn : kn) + ch * 8) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
+        attend(0, 1u);
+        __syncwarp();
+    }
     pdl_trigger();
 
     // join the warps: each leaves its output where its ring was
@@ -307,7 +329,7 @@ static int step_splits(const StepArgs &a)
     const int64_t most = (int64_t)a.cols * a.page, visible = most < (int64_t)a.window + a.sinks ? most : (int64_t)a.window + a.sinks;
     const int64_t blocks = (int64_t)a.nseq * (a.heads / a.group) * ((a.group + wstep::HEADS - 1) / wstep::HEADS);
     int n = 1;
-    while (n < 16 && blocks * n < 2 * sm_count_or_default() && visible > (int64_t)2 * n * wstep::WARPS * wstep::KEYS * 2) n *= 2;
+    while (n < 16 && blocks * n < wstep::BLOCKS * sm_count_or_default() && visible > (int64_t)2 * n * wstep::WARPS * wstep::KEYS * 2) n *= 2;
     return n;
 }
 
@@ -378,6 +400,7 @@ extern "C" st_status st_attn_window_step(const st_cache *c, const void *q, const
     a.d = (int)c->d;
     a.pages = (int)c->pages;
     a.page = (int)c->page;
+    a.page_magic = 0xFFFFFFFFu / (unsigned)c->page;
     a.cols = (int)c->table_cols;
     a.window = clamp_int(window);
     a.sinks = clamp_int(sinks);
