@@ -2,7 +2,7 @@
 //
 // Bound by the cache's bytes: every visible row of K and V is read once for all query heads that share it.  A cluster of blocks owns
 // one key head of one sequence (and 16 of its query heads); its warps take tiles of 16 visible keys in turn.  Each warp copies its own
-// tiles to its own ring in shared memory (cp.async, two tiles ahead; page numbers one tile further), so that no barrier lies in the loop,
+// tiles to its own ring in shared memory (cp.async, a tile ahead; page numbers one tile further), so that no barrier lies in the loop,
 // and multiplies with mma.sync: the 16 rows of the fragments are query heads, of which a group of 1 to 16 is filled.  The tensor
 // cores of tcgen05 would need 128 rows, and 2 to 32 flops a byte need no more than a tenth of mma.sync's rate.
 // Rows that are not visible are never read: their place in shared memory is zeroed by the copy.
@@ -28,11 +28,11 @@ struct StepArgs {
 };
 
 namespace wstep {
-constexpr int WARPS = 4, KEYS = 16, HEADS = 16, STAGES = 3;
-constexpr int BLOCKS = 2;                  // of an SM, wanted
-template <int DP> struct Shape {
+constexpr int KEYS = 16, HEADS = 16, MAX_SPLITS = 16;
+constexpr int FEWEST = 2;                  // tiles of a warp, where keys are split further
+template <int DP, int WARPS, int STAGES> struct Shape {
     static constexpr int TILE_BYTES = KEYS * DP * 2, STAGE = 2 * TILE_BYTES, RING = STAGES * STAGE;
-    static constexpr size_t SMEM = (size_t)WARPS * RING + 2 * (WARPS + 1) * HEADS * sizeof(float) + WARPS * KEYS * sizeof(int64_t) + 16;
+    static constexpr size_t SMEM = (size_t)WARPS * RING + (2 * WARPS + 2 + MAX_SPLITS) * HEADS * sizeof(float) + WARPS * KEYS * sizeof(int64_t) + 16;
     static_assert(HEADS * DP * 4 <= RING, "a warp's output takes the place of its ring");
 };
 }  // namespace wstep
@@ -69,15 +69,16 @@ __device__ __forceinline__ float fast_exp2(float x)
     return y;
 }
 
-template <int DP>
-__global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const StepArgs a)
+template <int DP, int WARPS, int STAGES>
+__global__ void __launch_bounds__(WARPS * 32) window_step_kernel(const StepArgs a)
 {
     using namespace wstep;
-    using S = Shape<DP>;
+    using S = Shape<DP, WARPS, STAGES>;
     constexpr int CHUNKS = DP / 8;                        // 16-byte pieces of a row
     extern __shared__ __align__(128) unsigned char smem[];
     float *most_w = (float *)(smem + WARPS * S::RING), *sum_w = most_w + WARPS * HEADS, *most_b = sum_w + WARPS * HEADS, *sum_b = most_b + HEADS;
-    int64_t *offsets = (int64_t *)(sum_b + HEADS);
+    float *share = sum_b + HEADS;                          // weight of every block's part, over the sum: [block][head]
+    int64_t *offsets = (int64_t *)(share + MAX_SPLITS * HEADS);
     int *bad = (int *)(offsets + WARPS * KEYS);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int splits = gridDim.x, split = blockIdx.x, chunks = (a.group + HEADS - 1) / HEADS, b = blockIdx.z;
@@ -85,6 +86,7 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
 
     if (threadIdx.x == 0) *bad = 0;
     pdl_wait();
+    pdl_trigger();
     if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
         // an error is reported 100 us after its block began, which was not before this one (see the end)
         a.status[kWsStatusWord] = 0;
@@ -257,7 +259,6 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
         attend(0, 1u);
         __syncwarp();
     }
-    pdl_trigger();
 
     // join the warps: each leaves its output where its ring was
 #pragma unroll
@@ -279,41 +280,73 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
     // weight of a part whose largest score is m, where the largest of all is `all`
     auto weight = [&](float m, float all) { return m == -INFINITY ? 0.f : exp2f(c * (m - all)); };
     if (threadIdx.x < HEADS) {
-        float all = -INFINITY, s = 0.f;
-        for (int w = 0; w < WARPS; ++w) all = fmaxf(all, most_w[w * HEADS + threadIdx.x]);
-        for (int w = 0; w < WARPS; ++w) s += sum_w[w * HEADS + threadIdx.x] * weight(most_w[w * HEADS + threadIdx.x], all);
+        float all = -INFINITY, s = 0.f, w[WARPS];
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) all = fmaxf(all, most_w[i * HEADS + threadIdx.x]);
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+            w[i] = weight(most_w[i * HEADS + threadIdx.x], all);
+            s += sum_w[i * HEADS + threadIdx.x] * w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) most_w[i * HEADS + threadIdx.x] = w[i];
         most_b[threadIdx.x] = all;
         sum_b[threadIdx.x] = s;
     }
     __syncthreads();
     float *block = (float *)smem;                          // the first warp's place
-    for (int e = threadIdx.x; e < g * DP; e += WARPS * 32) {
-        const int row = e / DP;
-        float s = 0.f;
-        for (int w = 0; w < WARPS; ++w) s += ((const float *)(smem + w * S::RING))[e] * weight(most_w[w * HEADS + row], most_b[row]);
-        block[e] = s;
+    for (int e = 4 * threadIdx.x; e < g * DP; e += 4 * WARPS * 32) {
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+            const float w = most_w[i * HEADS + e / DP];
+            const float4 x = *reinterpret_cast<const float4 *>(smem + i * S::RING + e * 4);
+            s = make_float4(fmaf(w, x.x, s.x), fmaf(w, x.y, s.y), fmaf(w, x.z, s.z), fmaf(w, x.w, s.w));
+        }
+        *reinterpret_cast<float4 *>(block + e) = s;
     }
     if (splits > 1) tc::cluster_sync_all();
     else __syncthreads();
-    for (int e = 2 * (split * WARPS * 32 + threadIdx.x); e < g * DP; e += 2 * splits * WARPS * 32) {
-        const int row = e / DP, col = e % DP;
-        float all = -INFINITY, s = 0.f, y0 = 0.f, y1 = 0.f;
-        for (int r = 0; r < splits; ++r) all = fmaxf(all, splits > 1 ? ld_cluster(tc::map_to_cta(tc::smem_u32(most_b + row), r)) : most_b[row]);
-        for (int r = 0; r < splits; ++r) {
-            if (splits == 1) {
-                s = sum_b[row];
-                y0 = block[e];
-                y1 = block[e + 1];
-            } else {
-                const float w = weight(ld_cluster(tc::map_to_cta(tc::smem_u32(most_b + row), r)), all);
-                s += w * ld_cluster(tc::map_to_cta(tc::smem_u32(sum_b + row), r));
-                y0 += w * ld_cluster(tc::map_to_cta(tc::smem_u32(block + e), r));
-                y1 += w * ld_cluster(tc::map_to_cta(tc::smem_u32(block + e + 1), r));
+    // then the blocks: their shares first, each read once, then every block its piece of the output
+    if (threadIdx.x < HEADS) {
+        float m[MAX_SPLITS], l[MAX_SPLITS], all = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int r = 0; r < MAX_SPLITS; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+            if (r < splits) {
+                m[r] = splits > 1 ? ld_cluster(tc::map_to_cta(tc::smem_u32(most_b + threadIdx.x), r)) : most_b[threadIdx.x];
+                l[r] = splits > 1 ? ld_cluster(tc::map_to_cta(tc::smem_u32(sum_b + threadIdx.x), r)) : sum_b[threadIdx.x];
             }
+            all = fmaxf(all, m[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < MAX_SPLITS; ++r) {
+            m[r] = weight(m[r], all);
+            s = fmaf(m[r], l[r], s);
         }
         const float inv = s > 0.f ? 1.f / s : 0.f;
-        if (col < a.d)
-            *reinterpret_cast<__nv_bfloat162 *>(a.out + ((int64_t)b * a.heads + hk * a.group + g0 + row) * a.d + col) = __floats2bfloat162_rn(y0 * inv, y1 * inv);
+#pragma unroll
+        for (int r = 0; r < MAX_SPLITS; ++r) share[r * HEADS + threadIdx.x] = m[r] * inv;
+    }
+    __syncthreads();
+    for (int e = 2 * (split * WARPS * 32 + threadIdx.x); e < g * DP; e += 2 * splits * WARPS * 32) {
+        const int row = e / DP, col = e % DP;
+        float y0 = 0.f, y1 = 0.f;
+        if (splits == 1) {
+            y0 = share[row] * block[e];
+            y1 = share[row] * block[e + 1];
+        } else {
+#pragma unroll 8
+            for (int r = 0; r < splits; ++r) {
+                const uint32_t at = tc::map_to_cta(tc::smem_u32(block + e), r);
+                float x0, x1;
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x0), "=f"(x1) : "r"(at) : "memory");
+                y0 = fmaf(share[r * HEADS + row], x0, y0);
+                y1 = fmaf(share[r * HEADS + row], x1, y1);
+            }
+        }
+        if (col < a.d) *reinterpret_cast<__nv_bfloat162 *>(a.out + ((int64_t)b * a.heads + hk * a.group + g0 + row) * a.d + col) = __floats2bfloat162_rn(y0, y1);
     }
     if (splits > 1) tc::cluster_sync_all();                // no block ends while another reads its shared memory
     if (*bad && threadIdx.x == 0) {
@@ -323,25 +356,16 @@ __global__ void __launch_bounds__(wstep::WARPS * 32) window_step_kernel(const St
     }
 }
 
-// Blocks of a cluster: as many as it takes to give every SM two blocks, as long as a warp has two tiles; a power of two up to 16.
-static int step_splits(const StepArgs &a)
+template <int DP, int WARPS, int STAGES>
+static st_status launch_step(const StepArgs &a, int splits, cudaStream_t stream)
 {
-    const int64_t most = (int64_t)a.cols * a.page, visible = most < (int64_t)a.window + a.sinks ? most : (int64_t)a.window + a.sinks;
-    const int64_t blocks = (int64_t)a.nseq * (a.heads / a.group) * ((a.group + wstep::HEADS - 1) / wstep::HEADS);
-    int n = 1;
-    while (n < 16 && blocks * n < wstep::BLOCKS * sm_count_or_default() && visible > (int64_t)2 * n * wstep::WARPS * wstep::KEYS * 2) n *= 2;
-    return n;
-}
-
-template <int DP>
-static st_status run_step(const StepArgs &a, cudaStream_t stream)
-{
-    const size_t smem = wstep::Shape<DP>::SMEM;
-    if (!ensure_dynamic_smem(window_step_kernel<DP>, smem) || !allow_large_clusters(window_step_kernel<DP>)) return ST_ERR_CUDA;
-    const int splits = step_splits(a), chunks = (a.group + wstep::HEADS - 1) / wstep::HEADS;
+    const auto kernel = window_step_kernel<DP, WARPS, STAGES>;
+    const size_t smem = wstep::Shape<DP, WARPS, STAGES>::SMEM;
+    if (!ensure_dynamic_smem(kernel, smem) || !allow_large_clusters(kernel)) return ST_ERR_CUDA;
+    const int chunks = (a.group + wstep::HEADS - 1) / wstep::HEADS;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)splits, (unsigned)(a.heads / a.group * chunks), (unsigned)a.nseq);
-    cfg.blockDim = dim3(wstep::WARPS * 32);
+    cfg.blockDim = dim3(WARPS * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -352,11 +376,27 @@ static st_status run_step(const StepArgs &a, cudaStream_t stream)
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = splits > 1 ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, window_step_kernel<DP>, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
         (void)cudaGetLastError();
         return ST_ERR_CUDA;
     }
     return ST_OK;
+}
+
+// Where heads and sequences are few the keys are split over a cluster of up to 16 blocks.  Blocks of four warps with one tile ahead leave room
+// for three on an SM; where even 16 blocks a head do not fill the SMs once, six warps, of which two blocks still fit: clusters of 16 need 16
+// blocks' room in one group of SMs, and with one block to an SM not all of them start (8 heads, 8192 keys: eight warps with two tiles ahead
+// 25 us, four warps 17.5, six 15.8; 64 sequences of 8 heads: four warps with one tile ahead 65 us, with two 85).
+template <int DP>
+static st_status run_step(const StepArgs &a, cudaStream_t stream)
+{
+    const int64_t most = (int64_t)a.cols * a.page, visible = most < (int64_t)a.window + a.sinks ? most : (int64_t)a.window + a.sinks;
+    const int64_t blocks = (int64_t)a.nseq * (a.heads / a.group) * ((a.group + wstep::HEADS - 1) / wstep::HEADS);
+    const int64_t sms = sm_count_or_default(), tiles = (visible + wstep::KEYS - 1) / wstep::KEYS;
+    int n = 1;
+    while (n < wstep::MAX_SPLITS && blocks * n < 3 * sms && tiles > (int64_t)2 * n * 4 * wstep::FEWEST) n *= 2;
+    if (blocks * n <= sms && tiles > (int64_t)n * 6) return launch_step<DP, 6, 2>(a, n, stream);
+    return launch_step<DP, 4, 2>(a, n, stream);
 }
 
 }  // namespace attn
