@@ -90,11 +90,11 @@ __device__ __forceinline__ void mma_rows(uint32_t d_tmem, const unsigned char *A
 // D[128, N] (+)= A B over the 128 tokens of a tile: A[128, 128 tokens] bf16 in tensor memory, its second 64 tokens HALF columns behind
 // the first, B a tile whose rows are the tokens.
 template <int HALF = 32>
-__device__ __forceinline__ void mma_tokens(uint32_t d_tmem, uint32_t a_tmem, const unsigned char *B, uint32_t idesc, bool add)
+__device__ __forceinline__ void mma_tokens(uint32_t d_tmem, uint32_t a_tmem, const unsigned char *B, uint32_t idesc, bool add, int k0 = 0, int k1 = TILE / 16)
 {
     const uint64_t b = tc::make_smem_desc(tc::smem_u32(B), SLAB, 1024);
 #pragma unroll
-    for (int k = 0; k < TILE / 16; ++k) mma_bf16_ts(d_tmem, a_tmem + (k >> 2) * HALF + (k & 3) * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0 ? 1u : 0u);
+    for (int k = k0; k < k1; ++k) mma_bf16_ts(d_tmem, a_tmem + (k >> 2) * HALF + (k & 3) * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0 ? 1u : 0u);
 }
 
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32])
@@ -123,6 +123,12 @@ __device__ __forceinline__ float ex2(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
     return y;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
@@ -227,6 +233,24 @@ __device__ __forceinline__ KeyTiles key_tiles(const Mask &m, int t0, int t1)
     k.first = min((min(m.sinks, 1 << 29) + TILE - 1) / TILE, k.lo);
     return k;
 }
+
+// Which of 32 columns, of which the first is `first` columns into a tile that begins at key s0, the query at position t sees: bit c, column c.
+struct RowMask {
+    int hi, lo, sinks;                         // columns of the tile: at most hi, and at least lo or below sinks
+    __device__ __forceinline__ RowMask(const Mask &m, int t, int s0) : hi(t - s0), lo(t - m.window + 1 - s0), sinks(m.sinks - s0) {}
+    static __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+    __device__ __forceinline__ unsigned of(int first) const { return below(hi + 1 - first) & (~below(lo - first) | below(sinks - first)); }
+};
+// The same for a key at position s and the 32 queries from position t0 + first: s <= t, and t < s + window or s < sinks.
+struct ColumnMask {
+    int lo, hi;
+    bool sink;
+    __device__ __forceinline__ ColumnMask(const Mask &m, int s, int t0) : lo(s - t0), hi(s + m.window - 1 - t0), sink(s < m.sinks) {}
+    __device__ __forceinline__ unsigned of(int first) const
+    {
+        return ~RowMask::below(lo - first) & (sink ? ~0u : RowMask::below(hi + 1 - first));
+    }
+};
 
 // Rows [valid, 128) of a tile in shared memory, whatever they are, become zero; by a whole warp, before the tensor cores read the tile.
 template <int COLS>

@@ -40,7 +40,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
     unsigned char *Q = smem, *K = Q + 2 * S::TILE_BYTES, *V = K + STAGES * S::TILE_BYTES;
     uint64_t *bars = (uint64_t *)(V + STAGES * S::TILE_BYTES);
     uint64_t *q_full = bars, *k_full = bars + 2, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES,
-             *v_copied = v_empty + STAGES, *s_full = v_copied + STAGES, *p_full = s_full + 2, *o_full = p_full + 2;
+             *v_copied = v_empty + STAGES, *s_full = v_copied + STAGES, *p_full = s_full + 2, *o_full = p_full + 4;
     uint32_t *tmem_slot = (uint32_t *)(o_full + 2);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
@@ -71,7 +71,8 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         for (int w = 0; w < 2; ++w) {
             mbar_init(&q_full[w], 1);
             mbar_init(&s_full[w], 1);
-            mbar_init(&p_full[w], 4);
+            mbar_init(&p_full[2 * w], 4);
+            mbar_init(&p_full[2 * w + 1], 4);
             mbar_init(&o_full[w], 1);
         }
         for (int s = 0; s < STAGES; ++s) {
@@ -166,11 +167,14 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                     ok = mbar_wait(&v_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 6);
                     v_seen = u + 1;
                 }
-                if (ok) ok = mbar_wait(&p_full[w], p_parity[w], abort_flag, a.status, 7);
-                if (!ok) return;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (ok) ok = mbar_wait(&p_full[2 * w + half], p_parity[w], abort_flag, a.status, 7);
+                    if (!ok) return;
+                    tc_fence_after();
+                    mma_tokens(tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, started[w], half * 4, half * 4 + 4);
+                }
                 p_parity[w] ^= 1u;
-                tc_fence_after();
-                mma_tokens(tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, started[w]);
                 started[w] = true;
             };
             for (int i = 0; i <= n && ok; ++i) {
@@ -222,13 +226,20 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             tmem_ld_wait();
             const int s0 = kt * TILE;
             if (!mask.all(t0 + w * TILE, t0 + w * TILE + TILE - 1, s0, s0 + TILE - 1)) {
+                const RowMask seen(mask, t, s0);
 #pragma unroll
-                for (int j = 0; j < 128; ++j)
-                    if (!mask.sees(t, s0 + j)) x[j / 32][j % 32] = __float_as_uint(-INFINITY);
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned bits = seen.of(j * 32);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(bits >> e & 1u)) x[j][e] = __float_as_uint(-INFINITY);
+                }
             }
             float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int j = 0; j < 128; ++j) most[j & 3] = fmaxf(most[j & 3], __uint_as_float(x[j / 32][j % 32]));
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) most[e / 2 & 3] = max3(most[e / 2 & 3], __uint_as_float(x[j][e]), __uint_as_float(x[j][e + 1]));
             const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
             // the reference moves: 8 is the factor 2^8 that P may exceed 1 by
             if (__any_sync(~0u, c * (top - m) > 8.f)) {
@@ -236,38 +247,41 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                 m = now;
                 l *= f;
                 if (started) {
-#pragma unroll
-                    for (int j = 0; j < DP / 32; ++j) {
-                        uint32_t o[32];
-                        tmem_ld_32x32(o_addr + j * 32, o);
+#pragma unroll 1
+                    for (int j = 0; j < DP / 16; ++j) {
+                        uint32_t o[16];
+                        tmem_ld_32x16(o_addr + j * 16, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                        tmem_st_32x32(o_addr + j * 32, o);
+                        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        tmem_st_32x16(o_addr + j * 16, o);
                     }
                 }
             }
             started = true;
-            const float mc = m == -INFINITY ? 0.f : m * c;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const float mc = m == -INFINITY ? 0.f : -m * c;
+            const Pair cc = pair(c, c), mm = pair(mc, mc);
+            Pair sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t p[32];
+            for (int j = 0; j < 4; ++j) {
+                uint32_t p[16];
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int k0 = j * 64 + 2 * e;
-                    const float y0 = ex2(fmaf(__uint_as_float(x[k0 / 32][k0 % 32]), c, -mc)), y1 = ex2(fmaf(__uint_as_float(x[k0 / 32][k0 % 32 + 1]), c, -mc));
-                    sum[(e & 1) * 2] += y0;
-                    sum[(e & 1) * 2 + 1] += y1;
-                    p[e] = pack_bf16(y0, y1);
+                for (int e = 0; e < 16; ++e) {
+                    const float2 z = split(fma(pair(x[j][2 * e], x[j][2 * e + 1]), cc, mm));
+                    const Pair y = pair(ex2(z.x), ex2(z.y));
+                    sum[e & 1] = add(sum[e & 1], y);
+                    p[e] = pack_bf16(y);
                 }
-                tmem_st_32x32(s_addr + j * 32, p);
+                tmem_st_32x16(s_addr + j * 16, p);
+                if (j & 1) {                              // the product with V begins when half of the keys' weights are there
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[2 * w + j / 2]);
+                }
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&p_full[w]);
+            const float2 part = split(add(sum[0], sum[1]));
+            l += part.x + part.y;
         }
         if (ok && n > 0) ok = __all_sync(~0u, mbar_wait(&o_full[w], 0, abort_flag, a.status, 9));
         if (ok) {
