@@ -30,7 +30,7 @@ template <int DP> struct Shape {
 template <int DP>
 __global__ void __launch_bounds__(wfwd::THREADS, 1)
 window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-              const WindowArgs a)
+              const __grid_constant__ CUtensorMap outmap, const WindowArgs a)
 {
     using namespace wfwd;
     using namespace tc;
@@ -45,6 +45,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
 
+    if (warp == 8 && lane < 4) prefetch_tmap(lane == 0 ? &qmap : lane == 1 ? &kmap : lane == 2 ? &vmap : &outmap);
     pdl_wait();
     if (blockIdx.x == 0 && blockIdx.y == 0) {
         const bool fine = offsets_fine(a.q_offsets, a.nseq, a.nq, threadIdx.x, THREADS) && offsets_fine(a.k_offsets, a.nseq, a.nk, threadIdx.x, THREADS);
@@ -145,7 +146,13 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             int next = 0, use = 0, k_seen = 0, v_seen = 0;       // next tile of keys for S; stages used by S
             bool q_seen[2] = {false, false}, started[2] = {false, false}, ok = true;
             uint32_t p_parity[2] = {0, 0};
-            int kt_prev = -1;
+            int kt_prev = -1, last[2] = {0, 0};                  // stages up to the last that each tile of queries uses
+            for (int i = 0, u = 0; i < n; ++i) {
+                const bool a0 = sees(0, tiles.at(i)), a1 = sees(1, tiles.at(i));
+                u += a0 || a1;
+                if (a0) last[0] = u;
+                if (a1) last[1] = u;
+            }
             auto score = [&](int w, int kt, int u) {
                 if (!ok || !sees(w, kt)) return;
                 if (!q_seen[w]) {
@@ -176,6 +183,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                 }
                 p_parity[w] ^= 1u;
                 started[w] = true;
+                if (u + 1 == last[w]) tc_commit(&o_full[w]);
             };
             for (int i = 0; i <= n && ok; ++i) {
                 int kt = -1;
@@ -200,10 +208,6 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             }
             for (int w = 0; w < 2; ++w)                          // a copy that no product waited for ends before the block does
                 if (!q_seen[w] && w * TILE < left) (void)mbar_wait(&q_full[w], 0, abort_flag, a.status, 10);
-            if (ok) {
-                tc_commit(&o_full[0]);
-                tc_commit(&o_full[1]);
-            }
         }
         __syncwarp();
     } else {
@@ -283,34 +287,49 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             const float2 part = split(add(sum[0], sum[1]));
             l += part.x + part.y;
         }
-        if (ok && n > 0) ok = __all_sync(~0u, mbar_wait(&o_full[w], 0, abort_flag, a.status, 9));
+        if (ok && started) ok = __all_sync(~0u, mbar_wait(&o_full[w], 0, abort_flag, a.status, 9));
         if (ok) {
             tc_fence_after();
-            const int row = rq.first + i0 + w * TILE + r;
-            const bool mine = w * TILE + r < left;
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            bf16 *out = a.out + ((int64_t)row * a.heads + h) * a.d;
-#pragma unroll
-            for (int j = 0; j < DP / 32; ++j) {
-                uint32_t o[32];
+            const int wr = (warp & 3) * 32, first = w * TILE + wr, row = rq.first + i0 + first;      // this warp's rows
+            const bool seen = l > 0.f, all = first + 32 <= left;
+            const Pair inv = pair(seen ? 1.f / l : 0.f, seen ? 1.f / l : 0.f);
+            if (first + lane < left) a.lse[(int64_t)(row + lane) * a.heads + h] = seen ? (m * c + log2f(l)) * LN2 : -INFINITY;
+            // Rows go out through the shared memory of the queries, which no product reads any more: a warp's 32 rows in one copy for each
+            // 64 columns, or at a sequence's end one by one.
+            unsigned char *rows = Q + w * S::TILE_BYTES;
+            const int r8 = r & 7;
+#pragma unroll 1
+            for (int j = 0; j < DP / 16; ++j) {
+                uint32_t o[16];
                 if (started) {
-                    tmem_ld_32x32(o_addr + j * 32, o);
+                    tmem_ld_32x16(o_addr + j * 16, o);
                     tmem_ld_wait();
                 }
+                uint4 v[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (mine && j * 32 + e * 8 < a.d) {
-                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                        if (l > 0.f) {
-                            uint32_t *u = &v.x;
+                for (int e = 0; e < 2; ++e) {
+                    uint32_t u[4];
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) u[k] = pack_bf16(__uint_as_float(o[e * 8 + 2 * k]) * inv, __uint_as_float(o[e * 8 + 2 * k + 1]) * inv);
-                        }
-                        *reinterpret_cast<uint4 *>(out + j * 32 + e * 8) = v;
-                    }
+                    for (int k = 0; k < 4; ++k) u[k] = seen ? pack_bf16(mul(pair(o[e * 8 + 2 * k], o[e * 8 + 2 * k + 1]), inv)) : 0u;
+                    v[e] = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+                unsigned char *at = rows + (j / 4) * SLAB + r * 128;
+                *reinterpret_cast<uint4 *>(at + (((j % 4) * 2) ^ r8) * 16) = v[0];
+                *reinterpret_cast<uint4 *>(at + (((j % 4) * 2 + 1) ^ r8) * 16) = v[1];
+                if (all && j % 4 == 3) {
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) tma_store_3d(&outmap, rows + (j / 4) * SLAB + wr * 128, j / 4 * 64, h, row);
                 }
             }
-            if (mine) a.lse[(int64_t)row * a.heads + h] = l > 0.f ? (m * c + log2f(l)) * LN2 : -INFINITY;
+            __syncwarp();
+            if (!all) {
+                for (int k = 0; k < 32 && first + k < left; ++k)
+                    if (lane * 8 < a.d && lane < DP / 8)
+                        *reinterpret_cast<uint4 *>(a.out + ((int64_t)(row + k) * a.heads + h) * a.d + lane * 8) =
+                            *reinterpret_cast<const uint4 *>(rows + (lane / 8) * SLAB + (wr + k) * 128 + (((lane & 7) ^ (k & 7)) << 4));
+            }
+            if (lane == 0) tma_store_wait();
         }
     }
     tc_fence_before();
@@ -324,13 +343,15 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
 template <int DP>
 static st_status run_window(const WindowArgs &a, const st_tokens *t, cudaStream_t stream)
 {
-    CUtensorMap qm, km, vm;
+    CUtensorMap qm, km, vm, om;
+    const Table out{a.out, (int64_t)t->heads * t->d, t->d};
+    if (!make_tmap_table(&om, out, t->nq, t->heads, t->d, 32)) return ST_ERR_CUDA;
     if (!make_tmap_table(&qm, a.q, t->nq, t->heads, t->d) || !make_tmap_table(&km, a.k, t->nk, t->kv_heads, t->d) ||
         !make_tmap_table(&vm, a.v, t->nk, t->kv_heads, t->d))
         return ST_ERR_CUDA;
     if (!ensure_dynamic_smem(window_kernel<DP>, wfwd::Shape<DP>::SMEM)) return ST_ERR_CUDA;
     const dim3 grid((unsigned)most_tiles(t->nq, t->nseq, 2 * TILE), (unsigned)t->heads);
-    return launch(window_kernel<DP>, grid, wfwd::THREADS, wfwd::Shape<DP>::SMEM, stream, qm, km, vm, a);
+    return launch(window_kernel<DP>, grid, wfwd::THREADS, wfwd::Shape<DP>::SMEM, stream, qm, km, vm, om, a);
 }
 
 }  // namespace attn
