@@ -101,7 +101,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
              *z_ready = o_free + 1, *s_ready = z_ready + BUFS, *u_full = s_ready + 1, *u_free = u_full + BUFS, *xs_done = u_free + 1;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
     const int slabs = (a.dz + ZC - 1) / ZC, slab = blockIdx.x % slabs, tile = blockIdx.x / slabs;
 
     pdl_wait();
@@ -152,7 +152,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot, pz_col = tmem + 2 * TILE, xs_col = pz_col + ZC, u_col = xs_col + ZC;
+    const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0), pz_col = tmem + 2 * TILE, xs_col = pz_col + ZC, u_col = xs_col + ZC;
     pdl_trigger();
 
     if (warp == 12) {
@@ -181,58 +181,59 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         __syncwarp();
     } else if (warp == 13) {
-        if (elect_one()) {
+        {
+            const bool lead = elect_one();
             const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, 2 * ZC);
             bool ok = true;
             // U and XS of a chunk, scores of the next, PZ of the chunk: each product has one place in the code, for the instruction cache
             for (int i = -1; i < n && ok; ++i) {
                 const unsigned char *Y = stages + ((i + STAGES) % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *X = Z + Sh::Z_BYTES;
                 if (i >= 0) {
-                    if (STATE) ok = mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
-                    if (ok) ok = mbar_wait(&z_ready[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 3);
-                    if (ok && i > 0) ok = mbar_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
+                    if (STATE) ok = warp_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
+                    if (ok) ok = warp_wait(&z_ready[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 3);
+                    if (ok && i > 0) ok = warp_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
                     if (!ok) break;
                     tc_fence_after();
                     // Y^T times both parts side by side: the tile of Y is read once
                     const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_parts + (i % BUFS) * 2 * Sh::Z_BYTES), SLAB, 1024);
 #pragma unroll
                     for (int k = 0; k < TILE / 16; ++k)
-                        mma_bf16(u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k ? 1u : 0u);
-                    tc_commit(&u_full[i % BUFS]);
+                        mma_ss(lead, u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k > 0);
+                    commit(lead, &u_full[i % BUFS]);
                     if (STATE) {
-                        tc_commit(&xy_empty[i % STAGES]);
-                        tc_commit(&z_empty[i % STAGES]);
+                        commit(lead, &xy_empty[i % STAGES]);
+                        commit(lead, &z_empty[i % STAGES]);
                         continue;
                     }
-                    if (i > 0) ok = mbar_wait(o_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 4);
-                    if (ok) ok = mbar_wait(s_ready, (uint32_t)(i & 1), abort_flag, a.status, 5);
+                    if (i > 0) ok = warp_wait(o_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 4);
+                    if (ok) ok = warp_wait(s_ready, (uint32_t)(i & 1), abort_flag, a.status, 5);
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t x = make_smem_desc(smem_u32(X), 16, 1024), st = make_smem_desc(smem_u32(S_op), SLAB, 1024);
 #pragma unroll
                     for (int k = 0; k < DX / 16; ++k)
-                        mma_bf16(xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), st + (uint64_t)(k * 2048 >> 4), pz_idesc, k ? 1u : 0u);
-                    tc_commit(xs_done);
-                    tc_commit(&xy_empty[i % STAGES]);
+                        mma_ss(lead, xs_col, x + (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4), st + (uint64_t)(k * 2048 >> 4), pz_idesc, k > 0);
+                    commit(lead, xs_done);
+                    commit(lead, &xy_empty[i % STAGES]);
                 }
                 if (!STATE && i + 1 < n) {
                     const int e = i + 1;
-                    ok = mbar_wait(&in_full[e % STAGES], (uint32_t)((e / STAGES) & 1), abort_flag, a.status, 2);
+                    ok = warp_wait(&in_full[e % STAGES], (uint32_t)((e / STAGES) & 1), abort_flag, a.status, 2);
                     // rows behind the sequence are cleared first
-                    if (ok && tokens_of(e) < TILE) ok = mbar_wait(&z_ready[e % BUFS], (uint32_t)((e / BUFS) & 1), abort_flag, a.status, 16);
+                    if (ok && tokens_of(e) < TILE) ok = warp_wait(&z_ready[e % BUFS], (uint32_t)((e / BUFS) & 1), abort_flag, a.status, 16);
                     if (!ok) break;
                     tc_fence_after();
                     const unsigned char *st = stages + (e % STAGES) * Sh::STAGE;
-                    mma_rows<DX>(tmem + (e & 1) * TILE, st + Sh::X_BYTES + Sh::Z_BYTES, st, sc_idesc);
-                    tc_commit(&sc_full[e & 1]);
+                    mma_rows<DX>(lead, tmem + (e & 1) * TILE, st + Sh::X_BYTES + Sh::Z_BYTES, st, sc_idesc);
+                    commit(lead, &sc_full[e & 1]);
                 }
                 if (!STATE && i >= 0) {
-                    ok = mbar_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
+                    ok = warp_wait(&p_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 6);
                     if (!ok) break;
                     tc_fence_after();
-                    mma_tokens(pz_col, tmem + (i & 1) * TILE, Z, pz_idesc, false);
-                    tc_commit(o_full);
-                    tc_commit(&z_empty[i % STAGES]);
+                    mma_tokens(lead, pz_col, tmem + (i & 1) * TILE, Z, pz_idesc, false);
+                    commit(lead, o_full);
+                    commit(lead, &z_empty[i % STAGES]);
                 }
             }
         }

@@ -64,37 +64,67 @@ __device__ __forceinline__ void prefetch_tile(const CUtensorMap *m, int head, in
     for (int c = 0; c < COLS / 64; ++c) prefetch_3d(m, c * 64, head, row);
 }
 
-// The A operand from tensor memory: 128 lanes, two bf16 of consecutive k to a column.
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+// Products are issued by one lane (`lead`) of a warp whose lanes all run the loop around them: what the instruction takes is the same
+// for the whole warp and stays in uniform registers.  Inside a branch that one lane took alone every operand was moved there first, at
+// some 90 cycles an instruction beside busy warps.
+__device__ __forceinline__ void mma_ss(bool lead, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)lead)
+        : "memory");
+}
+// The A operand from tensor memory: 128 lanes, two bf16 of consecutive k to a column.
+__device__ __forceinline__ void mma_ts(bool lead, uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"((uint32_t)add), "r"((uint32_t)lead)
+        : "memory");
+}
+__device__ __forceinline__ void commit(bool lead, uint64_t *bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+        ::"r"(tc::smem_u32(bar)), "r"((uint32_t)lead)
         : "memory");
 }
 
 // D[128, N] = A B^T over COLS columns of two K-major tiles (rows of A are lanes of D, rows of B are columns of D).
 template <int COLS>
-__device__ __forceinline__ void mma_rows(uint32_t d_tmem, const unsigned char *A, const unsigned char *B, uint32_t idesc, bool add = false)
+__device__ __forceinline__ void mma_rows(bool lead, uint32_t d_tmem, const unsigned char *A, const unsigned char *B, uint32_t idesc)
 {
     const uint64_t a = tc::make_smem_desc(tc::smem_u32(A), 16, 1024), b = tc::make_smem_desc(tc::smem_u32(B), 16, 1024);
 #pragma unroll
     for (int k = 0; k < COLS / 16; ++k) {
         const uint64_t off = (uint64_t)(((k >> 2) * SLAB + (k & 3) * 32) >> 4);
-        tc::mma_bf16(d_tmem, a + off, b + off, idesc, add || k > 0 ? 1u : 0u);
+        mma_ss(lead, d_tmem, a + off, b + off, idesc, k > 0);
     }
 }
 
-// D[128, N] (+)= A B over the 128 tokens of a tile: A[128, 128 tokens] bf16 in tensor memory, its second 64 tokens HALF columns behind
+// D[128, N] (+)= A B over tokens 16 K0 .. 16 K1 of a tile: A[128, 128 tokens] bf16 in tensor memory, its second 64 tokens HALF columns behind
 // the first, B a tile whose rows are the tokens.
-template <int HALF = 32>
-__device__ __forceinline__ void mma_tokens(uint32_t d_tmem, uint32_t a_tmem, const unsigned char *B, uint32_t idesc, bool add, int k0 = 0, int k1 = TILE / 16)
+template <int HALF = 32, int K0 = 0, int K1 = TILE / 16>
+__device__ __forceinline__ void mma_tokens(bool lead, uint32_t d_tmem, uint32_t a_tmem, const unsigned char *B, uint32_t idesc, bool add)
 {
     const uint64_t b = tc::make_smem_desc(tc::smem_u32(B), SLAB, 1024);
 #pragma unroll
-    for (int k = k0; k < k1; ++k) mma_bf16_ts(d_tmem, a_tmem + (k >> 2) * HALF + (k & 3) * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0 ? 1u : 0u);
+    for (int k = K0; k < K1; ++k) mma_ts(lead, d_tmem, a_tmem + (k >> 2) * HALF + (k & 3) * 8, b + (uint64_t)(k * 2048 >> 4), idesc, add || k > 0);
+}
+
+// A wait of a whole warp: all lanes see the phase over, or none goes on.
+template <typename... Args>
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Args... args)
+{
+    return __all_sync(~0u, tc::mbar_wait(bar, parity, args...));
 }
 
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32])

@@ -43,7 +43,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
              *v_copied = v_empty + STAGES, *s_full = v_copied + STAGES, *p_full = s_full + 2, *o_full = p_full + 4;
     uint32_t *tmem_slot = (uint32_t *)(o_full + 2);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
 
     if (warp == 8 && lane < 4) prefetch_tmap(lane == 0 ? &qmap : lane == 1 ? &kmap : lane == 2 ? &vmap : &outmap);
     pdl_wait();
@@ -93,24 +93,27 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
     pdl_trigger();
 
     if (warp == 8) {
         const int hk = h / a.group;
-        if (lane == 0) {
-            for (int w = 0; w < 2; ++w)
-                if (w * TILE < left) {
-                    mbar_expect_tx(&q_full[w], S::TILE_BYTES);
-                    load_tile<DP>(Q + w * S::TILE_BYTES, &qmap, &q_full[w], h, rq.first + i0 + w * TILE);
-                }
-        }
+        bool q_asked[2] = {false, false};       // queries that see nothing are not copied: their place is used for the output at once
         int use = 0;
         uint32_t copied = 0;                    // parity of v_copied, by stage
         bool ok = true;
         for (int i = 0; i < n && ok; ++i) {
             const int kt = tiles.at(i);
-            if (!sees(0, kt) && !sees(1, kt)) continue;
+            const bool a0 = sees(0, kt), a1 = sees(1, kt);
+            if (!a0 && !a1) continue;
+            for (int w = 0; w < 2; ++w)
+                if ((w ? a1 : a0) && !q_asked[w]) {
+                    q_asked[w] = true;
+                    if (lane == 0) {
+                        mbar_expect_tx(&q_full[w], S::TILE_BYTES);
+                        load_tile<DP>(Q + w * S::TILE_BYTES, &qmap, &q_full[w], h, rq.first + i0 + w * TILE);
+                    }
+                }
             const int s = use % STAGES, row = rk.first + kt * TILE;
             const uint32_t parity = (uint32_t)((use / STAGES + 1) & 1);
             const bool edge = kt * TILE + TILE > rk.len;
@@ -139,7 +142,8 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             ++use;
         }
     } else if (warp == 9) {
-        if (elect_one()) {
+        {
+            const bool lead = elect_one();
             const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
             // products are issued in the order S0 S1 | O0 S0' O1 S1' | O0' S0'' ..: one tile's rows are in the exponential while
             // the other's products run
@@ -156,34 +160,35 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             auto score = [&](int w, int kt, int u) {
                 if (!ok || !sees(w, kt)) return;
                 if (!q_seen[w]) {
-                    ok = mbar_wait(&q_full[w], 0, abort_flag, a.status, 4);
+                    ok = warp_wait(&q_full[w], 0, abort_flag, a.status, 4);
                     q_seen[w] = true;
                 }
                 if (ok && k_seen <= u) {
-                    ok = mbar_wait(&k_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 5);
+                    ok = warp_wait(&k_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 5);
                     k_seen = u + 1;
                 }
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(tmem + w * TILE, Q + w * S::TILE_BYTES, K + (u % STAGES) * S::TILE_BYTES, s_idesc);
-                tc_commit(&s_full[w]);
+                mma_rows<DP>(lead, tmem + w * TILE, Q + w * S::TILE_BYTES, K + (u % STAGES) * S::TILE_BYTES, s_idesc);
+                commit(lead, &s_full[w]);
             };
             auto weigh = [&](int w, int kt, int u) {
                 if (!ok || !sees(w, kt)) return;
                 if (v_seen <= u) {
-                    ok = mbar_wait(&v_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 6);
+                    ok = warp_wait(&v_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 6);
                     v_seen = u + 1;
                 }
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if (ok) ok = mbar_wait(&p_full[2 * w + half], p_parity[w], abort_flag, a.status, 7);
-                    if (!ok) return;
-                    tc_fence_after();
-                    mma_tokens(tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, started[w], half * 4, half * 4 + 4);
-                }
+                if (ok) ok = warp_wait(&p_full[2 * w], p_parity[w], abort_flag, a.status, 7);
+                if (!ok) return;
+                tc_fence_after();
+                mma_tokens<32, 0, 4>(lead, tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, started[w]);
+                ok = warp_wait(&p_full[2 * w + 1], p_parity[w], abort_flag, a.status, 7);
+                if (!ok) return;
+                tc_fence_after();
+                mma_tokens<32, 4, 8>(lead, tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, true);
                 p_parity[w] ^= 1u;
                 started[w] = true;
-                if (u + 1 == last[w]) tc_commit(&o_full[w]);
+                if (u + 1 == last[w]) commit(lead, &o_full[w]);
             };
             for (int i = 0; i <= n && ok; ++i) {
                 int kt = -1;
@@ -196,18 +201,16 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                 if (kt >= 0) score(0, kt, use);
                 if (kt_prev >= 0) {
                     weigh(1, kt_prev, use - 1);
-                    if (ok) tc_commit(&v_empty[(use - 1) % STAGES]);
+                    if (ok) commit(lead, &v_empty[(use - 1) % STAGES]);
                 }
                 if (kt >= 0) {
                     score(1, kt, use);
-                    if (ok) tc_commit(&k_empty[use % STAGES]);
+                    if (ok) commit(lead, &k_empty[use % STAGES]);
                 }
                 if (kt < 0) break;
                 kt_prev = kt;
                 ++use;
             }
-            for (int w = 0; w < 2; ++w)                          // a copy that no product waited for ends before the block does
-                if (!q_seen[w] && w * TILE < left) (void)mbar_wait(&q_full[w], 0, abort_flag, a.status, 10);
         }
         __syncwarp();
     } else {

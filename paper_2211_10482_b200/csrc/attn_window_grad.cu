@@ -151,7 +151,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
              *v_empty = v_full + VS, *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_full = dp_full + 1, *done = ds_full + 1;
     uint32_t *tmem_slot = (uint32_t *)(done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
 
     pdl_wait();
     if (blockIdx.x == 0 && blockIdx.y == 0) {
@@ -197,7 +197,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot, dp_col = tmem + 2 * TILE, dq_col = tmem + 3 * TILE;
+    const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0), dp_col = tmem + 2 * TILE, dq_col = tmem + 3 * TILE;
     pdl_trigger();
 
     if (warp == 8) {
@@ -237,42 +237,43 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             }
         }
     } else if (warp == 9) {
-        if (n > 0 && elect_one()) {
+        if (n > 0) {
+            const bool lead = elect_one();
             const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
             bool ok = true;
             auto score = [&](int j) {
                 if (!ok || j >= n) return;
-                ok = mbar_wait(&k_full[j % KS], (uint32_t)((j / KS) & 1), abort_flag, a.status, 4);
+                ok = warp_wait(&k_full[j % KS], (uint32_t)((j / KS) & 1), abort_flag, a.status, 4);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(tmem + (j & 1) * TILE, Q, K + (j % KS) * BYTES, s_idesc);
-                tc_commit(&s_full[j & 1]);
+                mma_rows<DP>(lead, tmem + (j & 1) * TILE, Q, K + (j % KS) * BYTES, s_idesc);
+                commit(lead, &s_full[j & 1]);
             };
             auto dprob = [&](int j) {
                 if (!ok || j >= n) return;
-                ok = mbar_wait(&v_full[j % VS], (uint32_t)((j / VS) & 1), abort_flag, a.status, 5);
+                ok = warp_wait(&v_full[j % VS], (uint32_t)((j / VS) & 1), abort_flag, a.status, 5);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(dp_col, DO, V + (j % VS) * BYTES, s_idesc);
-                tc_commit(dp_full);
-                tc_commit(&v_empty[j % VS]);
+                mma_rows<DP>(lead, dp_col, DO, V + (j % VS) * BYTES, s_idesc);
+                commit(lead, dp_full);
+                commit(lead, &v_empty[j % VS]);
             };
-            ok = mbar_wait(q_full, 0, abort_flag, a.status, 6);
+            ok = warp_wait(q_full, 0, abort_flag, a.status, 6);
             score(0);
-            if (ok) ok = mbar_wait(do_full, 0, abort_flag, a.status, 7);
+            if (ok) ok = warp_wait(do_full, 0, abort_flag, a.status, 7);
             dprob(0);
             score(1);
             for (int j = 0; j < n && ok; ++j) {
-                ok = mbar_wait(ds_full, (uint32_t)(j & 1), abort_flag, a.status, 8);
+                ok = warp_wait(ds_full, (uint32_t)(j & 1), abort_flag, a.status, 8);
                 if (!ok) break;
                 tc_fence_after();
                 dprob(j + 1);
                 if (!ok) break;
-                mma_tokens<64>(dq_col, tmem + (j & 1) * TILE, K + (j % KS) * BYTES, o_idesc, j > 0);
-                tc_commit(&k_empty[j % KS]);
+                mma_tokens<64>(lead, dq_col, tmem + (j & 1) * TILE, K + (j % KS) * BYTES, o_idesc, j > 0);
+                commit(lead, &k_empty[j % KS]);
                 score(j + 2);
             }
-            if (ok) tc_commit(done);
+            if (ok) commit(lead, done);
         }
         __syncwarp();
     } else {
@@ -371,7 +372,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
              *ds_full = p_full + 1, *done = ds_full + 1;
     uint32_t *tmem_slot = (uint32_t *)(done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, hk = blockIdx.y;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, hk = blockIdx.y;
 
     pdl_wait();
     const Mask mask{a.window, a.sinks};
@@ -437,7 +438,7 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot, dp_col = tmem + TILE, dv_col = tmem + 2 * TILE, dk_col = tmem + 2 * TILE + DP;
+    const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0), dp_col = tmem + TILE, dv_col = tmem + 2 * TILE, dk_col = tmem + 2 * TILE + DP;
     pdl_trigger();
 
     if (warp == 8) {
@@ -503,44 +504,45 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
             }
         }
     } else if (warp == 9) {
-        if (n > 0 && elect_one()) {
+        if (n > 0) {
+            const bool lead = elect_one();
             const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
             bool ok = true;
             auto score = [&](int i) {
                 if (!ok || i >= n) return;
-                ok = mbar_wait(&q_full[i % ST], (uint32_t)((i / ST) & 1), abort_flag, a.status, 5);
+                ok = warp_wait(&q_full[i % ST], (uint32_t)((i / ST) & 1), abort_flag, a.status, 5);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(tmem, K, Q + (i % ST) * BYTES, s_idesc);
-                tc_commit(s_full);
+                mma_rows<DP>(lead, tmem, K, Q + (i % ST) * BYTES, s_idesc);
+                commit(lead, s_full);
             };
             auto dprob = [&](int i) {
                 if (!ok || i >= n) return;
-                ok = mbar_wait(&do_full[i % ST], (uint32_t)((i / ST) & 1), abort_flag, a.status, 6);
+                ok = warp_wait(&do_full[i % ST], (uint32_t)((i / ST) & 1), abort_flag, a.status, 6);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(dp_col, V, DO + (i % ST) * BYTES, s_idesc);
-                tc_commit(dp_full);
+                mma_rows<DP>(lead, dp_col, V, DO + (i % ST) * BYTES, s_idesc);
+                commit(lead, dp_full);
             };
-            ok = mbar_wait(k_full, 0, abort_flag, a.status, 7);
+            ok = warp_wait(k_full, 0, abort_flag, a.status, 7);
             score(0);
-            if (ok) ok = mbar_wait(v_full, 0, abort_flag, a.status, 8);
+            if (ok) ok = warp_wait(v_full, 0, abort_flag, a.status, 8);
             dprob(0);
             for (int i = 0; i < n && ok; ++i) {
-                ok = mbar_wait(p_full, (uint32_t)(i & 1), abort_flag, a.status, 9);
+                ok = warp_wait(p_full, (uint32_t)(i & 1), abort_flag, a.status, 9);
                 if (!ok) break;
                 tc_fence_after();
-                mma_tokens<64>(dv_col, tmem, DO + (i % ST) * BYTES, o_idesc, i > 0);
-                tc_commit(&do_empty[i % ST]);
+                mma_tokens<64>(lead, dv_col, tmem, DO + (i % ST) * BYTES, o_idesc, i > 0);
+                commit(lead, &do_empty[i % ST]);
                 score(i + 1);
-                if (ok) ok = mbar_wait(ds_full, (uint32_t)(i & 1), abort_flag, a.status, 10);
+                if (ok) ok = warp_wait(ds_full, (uint32_t)(i & 1), abort_flag, a.status, 10);
                 if (!ok) break;
                 tc_fence_after();
-                mma_tokens<64>(dk_col, dp_col, Q + (i % ST) * BYTES, o_idesc, i > 0);
-                tc_commit(&q_empty[i % ST]);
+                mma_tokens<64>(lead, dk_col, dp_col, Q + (i % ST) * BYTES, o_idesc, i > 0);
+                commit(lead, &q_empty[i % ST]);
                 dprob(i + 1);
             }
-            if (ok) tc_commit(done);
+            if (ok) commit(lead, done);
         }
         __syncwarp();
     } else {
