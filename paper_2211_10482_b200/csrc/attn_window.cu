@@ -12,14 +12,19 @@
 // cuts are masked.  Values behind a sequence's last key may be anything: their weight is 0, and their rows of V are
 // cleared in shared memory, as 0 times NaN would be NaN.
 //
-// Warps: 0..3 and 4..7 one row per thread of the first and second tile of queries, 8 copies (TMA), 9 issues the products.
+// Bound by power where many tiles of keys are seen: 32768 tokens, 16 heads of 128, window 4096 run at 990 TFLOP/s whether the exponentials and the
+// products alternate (3100 cycles for both tiles, at 1.4 GHz) or not (3960, at 1.8), and slower with part of the exponentials as
+// polynomials on the FMA units (1050 us, so 1185 with an eighth of them).  Few tiles of keys: by a block's beginning and end.
+//
+// Warps: 0..3 and 4..7 one row per thread of the first and second tile of queries, 8 copies (TMA), 9 and 10 issue the products of one tile
+// each: by one warp for both the issue itself took longer than the products.
 #include "attn_window.cuh"
 
 namespace st {
 namespace attn {
 
 namespace wfwd {
-constexpr int THREADS = 320;
+constexpr int THREADS = 352;
 constexpr int STAGES = 2;
 template <int DP> struct Shape {
     static constexpr int TILE_BYTES = DP / 64 * SLAB;
@@ -78,9 +83,9 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         }
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&k_full[s], 1);
-            mbar_init(&k_empty[s], 1);
+            mbar_init(&k_empty[s], 2);
             mbar_init(&v_full[s], 1);
-            mbar_init(&v_empty[s], 1);
+            mbar_init(&v_empty[s], 2);
             mbar_init(&v_copied[s], 1);
         }
         *abort_flag = 0;
@@ -141,77 +146,64 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             }
             ++use;
         }
-    } else if (warp == 9) {
-        {
-            const bool lead = elect_one();
-            const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
-            // products are issued in the order S0 S1 | O0 S0' O1 S1' | O0' S0'' ..: one tile's rows are in the exponential while
-            // the other's products run
-            int next = 0, use = 0, k_seen = 0, v_seen = 0;       // next tile of keys for S; stages used by S
-            bool q_seen[2] = {false, false}, started[2] = {false, false}, ok = true;
-            uint32_t p_parity[2] = {0, 0};
-            int kt_prev = -1, last[2] = {0, 0};                  // stages up to the last that each tile of queries uses
-            for (int i = 0, u = 0; i < n; ++i) {
-                const bool a0 = sees(0, tiles.at(i)), a1 = sees(1, tiles.at(i));
-                u += a0 || a1;
-                if (a0) last[0] = u;
-                if (a1) last[1] = u;
+    } else if (warp >= 9) {
+        // One warp for each tile of queries: its scores S of a tile of keys follow its product with V of the tile before, whose weights they
+        // overwrite (products are carried out in the order of their issue), and the other tile's products fill the time between.
+        const int w = warp - 9;
+        const bool lead = elect_one();
+        const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
+        const uint32_t s_col = tmem + w * TILE, o_col = tmem + 2 * TILE + w * DP;
+        const unsigned char *mine = Q + w * S::TILE_BYTES;
+        bool ok = true, started = false;
+        int i = 0, use = 0, done = 0;                            // tiles looked at, copied, used by this tile of queries
+        int at_stage = -1;                                       // the stage whose scores are in the exponential
+        uint32_t at_parity = 0;
+        while (ok) {
+            // the next tile that was copied
+            bool a0 = false, a1 = false;
+            for (; i < n && !(a0 || a1); ++i) {
+                const int kt = tiles.at(i);
+                a0 = sees(0, kt);
+                a1 = sees(1, kt);
             }
-            auto score = [&](int w, int kt, int u) {
-                if (!ok || !sees(w, kt)) return;
-                if (!q_seen[w]) {
-                    ok = warp_wait(&q_full[w], 0, abort_flag, a.status, 4);
-                    q_seen[w] = true;
-                }
-                if (ok && k_seen <= u) {
-                    ok = warp_wait(&k_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 5);
-                    k_seen = u + 1;
-                }
-                if (!ok) return;
+            const bool more = a0 || a1, score = w ? a1 : a0;
+            const int s = use % STAGES;
+            const uint32_t parity = (uint32_t)((use / STAGES) & 1);
+            if (at_stage >= 0 && (score || !more)) {
+                ok = warp_wait(&v_full[at_stage], at_parity, abort_flag, a.status, 6);
+                if (ok) ok = warp_wait(&p_full[2 * w], (uint32_t)(done & 1), abort_flag, a.status, 7);
+                if (!ok) break;
                 tc_fence_after();
-                mma_rows<DP>(lead, tmem + w * TILE, Q + w * S::TILE_BYTES, K + (u % STAGES) * S::TILE_BYTES, s_idesc);
+                mma_tokens<32, 0, 4>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, started);
+                ok = warp_wait(&p_full[2 * w + 1], (uint32_t)(done & 1), abort_flag, a.status, 7);
+                if (!ok) break;
+                tc_fence_after();
+                mma_tokens<32, 4, 8>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, true);
+                commit(lead, &v_empty[at_stage]);
+                at_stage = -1;
+                started = true;
+                ++done;
+            }
+            if (!more) break;
+            ok = warp_wait(&k_full[s], parity, abort_flag, a.status, 5);
+            if (ok && score && !started && done == 0 && at_stage < 0) ok = warp_wait(&q_full[w], 0, abort_flag, a.status, 4);
+            if (!ok) break;
+            if (score) {
+                tc_fence_after();
+                mma_rows<DP>(lead, s_col, mine, K + s * S::TILE_BYTES, s_idesc);
                 commit(lead, &s_full[w]);
-            };
-            auto weigh = [&](int w, int kt, int u) {
-                if (!ok || !sees(w, kt)) return;
-                if (v_seen <= u) {
-                    ok = warp_wait(&v_full[u % STAGES], (uint32_t)((u / STAGES) & 1), abort_flag, a.status, 6);
-                    v_seen = u + 1;
-                }
-                if (ok) ok = warp_wait(&p_full[2 * w], p_parity[w], abort_flag, a.status, 7);
-                if (!ok) return;
-                tc_fence_after();
-                mma_tokens<32, 0, 4>(lead, tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, started[w]);
-                ok = warp_wait(&p_full[2 * w + 1], p_parity[w], abort_flag, a.status, 7);
-                if (!ok) return;
-                tc_fence_after();
-                mma_tokens<32, 4, 8>(lead, tmem + 2 * TILE + w * DP, tmem + w * TILE, V + (u % STAGES) * S::TILE_BYTES, o_idesc, true);
-                p_parity[w] ^= 1u;
-                started[w] = true;
-                if (u + 1 == last[w]) commit(lead, &o_full[w]);
-            };
-            for (int i = 0; i <= n && ok; ++i) {
-                int kt = -1;
-                while (next < n) {                               // the next tile that either sees
-                    kt = tiles.at(next++);
-                    if (sees(0, kt) || sees(1, kt)) break;
-                    kt = -1;
-                }
-                if (kt_prev >= 0) weigh(0, kt_prev, use - 1);
-                if (kt >= 0) score(0, kt, use);
-                if (kt_prev >= 0) {
-                    weigh(1, kt_prev, use - 1);
-                    if (ok) commit(lead, &v_empty[(use - 1) % STAGES]);
-                }
-                if (kt >= 0) {
-                    score(1, kt, use);
-                    if (ok) commit(lead, &k_empty[use % STAGES]);
-                }
-                if (kt < 0) break;
-                kt_prev = kt;
-                ++use;
+                at_stage = s;
+                at_parity = parity;
+            } else {
+                // a tile that the other queries alone see: given back once it is there, so that the stages' turns stay in order
+                ok = warp_wait(&v_full[s], parity, abort_flag, a.status, 8);
+                if (!ok) break;
+                if (lead) mbar_arrive(&v_empty[s]);
             }
+            commit(lead, &k_empty[s]);
+            ++use;
         }
+        if (ok && started) commit(lead, &o_full[w]);
         __syncwarp();
     } else {
         const int w = warp >> 2, r = (warp & 3) * 32 + lane, t = t0 + w * TILE + r;      // this thread's row and its position
@@ -227,12 +219,13 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             if (!ok) break;
             parity ^= 1u;
             tc_fence_after();
+            const int s0 = kt * TILE;
+            const bool cut = !mask.all(t0 + w * TILE, t0 + w * TILE + TILE - 1, s0, s0 + TILE - 1);
             uint32_t x[4][32];
 #pragma unroll
             for (int j = 0; j < 4; ++j) tmem_ld_32x32(s_addr + j * 32, x[j]);
             tmem_ld_wait();
-            const int s0 = kt * TILE;
-            if (!mask.all(t0 + w * TILE, t0 + w * TILE + TILE - 1, s0, s0 + TILE - 1)) {
+            if (cut) {
                 const RowMask seen(mask, t, s0);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
