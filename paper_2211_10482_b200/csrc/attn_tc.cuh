@@ -282,6 +282,54 @@ struct ColumnMask {
     }
 };
 
+// Values of the columns whose bit is not set become 0.
+template <int N>
+__device__ __forceinline__ void keep(Pair (&v)[N], unsigned bits)
+{
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float2 x = split(v[e]);
+        v[e] = pair(bits >> (2 * e) & 1u ? x.x : 0.f, bits >> (2 * e + 1) & 1u ? x.y : 0.f);
+    }
+}
+
+// A thread's row of an accumulator (128 lanes, COLS columns), scaled, as bf16 rows of a table from `row` on.  `rows`: shared memory of a tile that no
+// product reads any more.  A warp's 32 rows leave in one copy for each 64 columns, those at a sequence's end (`live` of the warp's are left) one
+// by one; rows up to `skip` not at all.  To be waited for with tma_store_wait by lane 0.
+template <int COLS>
+__device__ __forceinline__ void store_rows(uint32_t taddr, unsigned char *rows, const CUtensorMap *map, bf16 *table, int64_t stride, int cols, int row, int head,
+                                           int r, int live, int skip, float scale, bool zero)
+{
+    const int lane = r & 31, wr = r - lane, r8 = r & 7;
+    const bool all = live >= 32 && skip <= 0;
+    const Pair f = pair(scale, scale);
+#pragma unroll 1
+    for (int j = 0; j < COLS / 16; ++j) {
+        uint32_t o[16];
+        tc::tmem_ld_32x16(taddr + j * 16, o);
+        tc::tmem_ld_wait();
+        unsigned char *at = rows + (j / 4) * SLAB + r * 128;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            uint32_t u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = zero ? 0u : pack_bf16(mul(pair(o[e * 8 + 2 * k], o[e * 8 + 2 * k + 1]), f));
+            *reinterpret_cast<uint4 *>(at + (((j % 4) * 2 + e) ^ r8) * 16) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        if (all && j % 4 == 3) {
+            tc::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) tma_store_3d(map, rows + (j / 4) * SLAB + wr * 128, j / 4 * 64, head, row);
+        }
+    }
+    __syncwarp();
+    if (!all)
+        for (int k = max(skip, 0); k < min(live, 32); ++k)
+            if (lane * 8 < cols && lane < COLS / 8)
+                *reinterpret_cast<uint4 *>(table + (int64_t)(row + k) * stride + head * cols + lane * 8) =
+                    *reinterpret_cast<const uint4 *>(rows + (lane / 8) * SLAB + (wr + k) * 128 + (((lane & 7) ^ (k & 7)) << 4));
+}
+
 // Rows [valid, 128) of a tile in shared memory, whatever they are, become zero; by a whole warp, before the tensor cores read the tile.
 template <int COLS>
 __device__ __forceinline__ void clear_rows(unsigned char *tile, int valid, int lane)

@@ -109,34 +109,10 @@ __device__ __forceinline__ float dot8(uint4 x, uint4 y)
     return s;
 }
 
-// Columns [c0, c0 + N) of a thread's row of an accumulator, scaled, as bf16 where `dst` is not null (dst: the row's first column, d columns).
-template <int N>
-__device__ __forceinline__ void store_row(uint32_t taddr, int c0, bf16 *dst, int d, float scale, bool zero)
-{
-#pragma unroll
-    for (int j = 0; j < N / 32; ++j) {
-        uint32_t o[32];
-        tc::tmem_ld_32x32(taddr + c0 + j * 32, o);
-        tc::tmem_ld_wait();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = c0 + j * 32 + e * 8;
-            if (dst && c < d) {
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                uint32_t *u = &v.x;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (!zero) u[k] = pack_bf16(__uint_as_float(o[e * 8 + 2 * k]) * scale, __uint_as_float(o[e * 8 + 2 * k + 1]) * scale);
-                *reinterpret_cast<uint4 *>(dst + c) = v;
-            }
-        }
-    }
-}
-
 template <int DP>
 __global__ void __launch_bounds__(wgrad::THREADS, 1)
 window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-                 const __grid_constant__ CUtensorMap domap, const WindowGradArgs g)
+                 const __grid_constant__ CUtensorMap domap, const __grid_constant__ CUtensorMap dqmap, const WindowGradArgs g)
 {
     using namespace wgrad;
     using namespace tc;
@@ -303,15 +279,19 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             ok = __all_sync(~0u, mbar_wait(&s_full[j & 1], (uint32_t)((j >> 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
             tc_fence_after();
-            uint32_t x[2][32];
-            tmem_ld_32x32(s_addr, x[0]);
-            tmem_ld_32x32(s_addr + 32, x[1]);
-            tmem_ld_wait();
+            const RowMask seen(mask, t, s0);
+            Pair p[2][16];
 #pragma unroll
-            for (int e = 0; e < 64; ++e) {
-                float p = ex2(fmaf(__uint_as_float(x[e / 32][e % 32]), c, -lse2));
-                if (cut && !mask.sees(t, s0 + half * 64 + e)) p = 0.f;
-                x[e / 32][e % 32] = __float_as_uint(p);
+            for (int b = 0; b < 2; ++b) {
+                uint32_t x[32];
+                tmem_ld_32x32(s_addr + b * 32, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float2 z = split(fma(pair(x[2 * e], x[2 * e + 1]), pair(c, c), pair(-lse2, -lse2)));
+                    p[b][e] = pair(ex2(z.x), ex2(z.y));
+                }
+                if (cut) keep(p[b], seen.of(half * 64 + b * 32));
             }
             ok = __all_sync(~0u, mbar_wait(dp_full, (uint32_t)(j & 1), abort_flag, a.status, 10));
             if (!ok) break;
@@ -322,16 +302,10 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 tmem_ld_32x32(dp_addr + b * 32, dp);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float y[2];
+                for (int e = 0; e < 16; ++e) p[b][e] = mul(p[b][e], add(pair(dp[2 * e], dp[2 * e + 1]), pair(-delta, -delta)));
+                if (cut) keep(p[b], seen.of(half * 64 + b * 32));        // a masked weight is 0 whatever its dP is
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float p = __uint_as_float(x[b][2 * e + k]);
-                        // a masked weight is 0 whatever its dP is
-                        y[k] = cut && p == 0.f ? 0.f : p * (__uint_as_float(dp[2 * e + k]) - delta);
-                    }
-                    ds[e] = pack_bf16(y[0], y[1]);
-                }
+                for (int e = 0; e < 16; ++e) ds[e] = pack_bf16(p[b][e]);
                 tmem_st_32x16(s_addr + b * 16, ds);
             }
             tmem_st_wait();
@@ -342,7 +316,11 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         if (ok && n > 0) ok = __all_sync(~0u, mbar_wait(done, 0, abort_flag, a.status, 11));
         if (ok) {
             tc_fence_after();
-            store_row<DP / 2>(dq_col + lanes, half * (DP / 2), mine ? g.dq + (row * a.heads + h) * a.d : nullptr, a.d, a.scale, n == 0);
+            if (half == 0) {
+                store_rows<DP>(dq_col + lanes, Q, &dqmap, g.dq, (int64_t)a.heads * a.d, a.d, rq.first + i0 + (warp & 3) * 32, h, r, left - (warp & 3) * 32, 0, a.scale,
+                               n == 0);
+                if (lane == 0) tma_store_wait();
+            }
         }
     }
     tc_fence_before();
@@ -356,7 +334,8 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
 template <int DP>
 __global__ void __launch_bounds__(wgrad::THREADS, 1)
 window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-                  const __grid_constant__ CUtensorMap domap, const WindowGradArgs g)
+                  const __grid_constant__ CUtensorMap domap, const __grid_constant__ CUtensorMap dkmap, const __grid_constant__ CUtensorMap dvmap,
+                  const WindowGradArgs g)
 {
     using namespace wgrad;
     using namespace tc;
@@ -468,9 +447,9 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
             if (!ok) break;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                // a row that sees nothing, or is none, has weights exp2(x - inf) = 0
-                stats[s * 2 * TILE + k * 32 + lane] = lse[k] == -INFINITY ? INFINITY : lse[k] * LOG2E;
-                stats[s * 2 * TILE + TILE + k * 32 + lane] = delta[k];
+                // negative, as they are added; a row that sees nothing, or is none, has weights exp2(x - inf) = 0
+                stats[s * 2 * TILE + k * 32 + lane] = lse[k] == -INFINITY ? -INFINITY : -lse[k] * LOG2E;
+                stats[s * 2 * TILE + TILE + k * 32 + lane] = -delta[k];
             }
             __syncwarp();
             if (lane == 0) {
@@ -560,27 +539,24 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
             if (ok) ok = __all_sync(~0u, mbar_wait(s_full, (uint32_t)(i & 1), abort_flag, a.status, 12));
             if (!ok) break;
             tc_fence_after();
-            uint32_t x[2][32];
-            tmem_ld_32x32(s_addr, x[0]);
-            tmem_ld_32x32(s_addr + 32, x[1]);
-            tmem_ld_wait();
+            const ColumnMask seen(mask, s, t0);
+            Pair y[2][16];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                uint32_t p[16];
+                uint32_t x[32], p[16];
+                tmem_ld_32x32(s_addr + b * 32, x);
+                tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 l = *reinterpret_cast<const float4 *>(lse2 + b * 32 + e);
-                    const float ll[4] = {l.x, l.y, l.z, l.w};
-                    float y[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        y[k] = ex2(fmaf(__uint_as_float(x[b][e + k]), c, -ll[k]));
-                        if (cut && !mask.sees(t0 + half * 64 + b * 32 + e + k, s)) y[k] = 0.f;
-                        x[b][e + k] = __float_as_uint(y[k]);
-                    }
-                    p[e / 2] = pack_bf16(y[0], y[1]);
-                    p[e / 2 + 1] = pack_bf16(y[2], y[3]);
+                for (int e = 0; e < 16; e += 2) {
+                    const float4 l = *reinterpret_cast<const float4 *>(lse2 + b * 32 + 2 * e);
+                    const float2 z0 = split(fma(pair(x[2 * e], x[2 * e + 1]), pair(c, c), pair(l.x, l.y))),
+                                 z1 = split(fma(pair(x[2 * e + 2], x[2 * e + 3]), pair(c, c), pair(l.z, l.w)));
+                    y[b][e] = pair(ex2(z0.x), ex2(z0.y));
+                    y[b][e + 1] = pair(ex2(z1.x), ex2(z1.y));
                 }
+                if (cut) keep(y[b], seen.of(half * 64 + b * 32));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) p[e] = pack_bf16(y[b][e]);
                 tmem_st_32x16(s_addr + b * 16, p);
             }
             tmem_st_wait();
@@ -596,14 +572,10 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
                 tmem_ld_32x32(dp_addr + b * 32, dp);
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 d = *reinterpret_cast<const float4 *>(delta + b * 32 + e);
-                    const float dd[4] = {d.x, d.y, d.z, d.w};
-                    float y[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) y[k] = __uint_as_float(x[b][e + k]) * (__uint_as_float(dp[e + k]) - dd[k]);
-                    ds[e / 2] = pack_bf16(y[0], y[1]);
-                    ds[e / 2 + 1] = pack_bf16(y[2], y[3]);
+                for (int e = 0; e < 16; e += 2) {
+                    const float4 d = *reinterpret_cast<const float4 *>(delta + b * 32 + 2 * e);
+                    ds[e] = pack_bf16(mul(y[b][e], add(pair(dp[2 * e], dp[2 * e + 1]), pair(d.x, d.y))));
+                    ds[e + 1] = pack_bf16(mul(y[b][e + 1], add(pair(dp[2 * e + 2], dp[2 * e + 3]), pair(d.z, d.w))));
                 }
                 tmem_st_32x16(dp_addr + b * 16, ds);
             }
@@ -619,10 +591,14 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
             // the first half of the threads has dk, the second dv
             const uint32_t acc = (half ? dv_col : dk_col) + lanes;
             const float scale = half ? 1.f : a.scale;
-            const int kv_heads = a.heads / a.group;
+            const int kv_heads = a.heads / a.group, wr = (warp & 3) * 32;
             const bool inside = s < rk.len, partial = r < partial_rows;
-            bf16 *dst = inside && !partial && !far ? (half ? g.dv : g.dk) + ((int64_t)(rk.first + s) * kv_heads + hk) * a.d : nullptr;
-            store_row<DP>(acc, 0, dst, a.d, scale, n == 0);
+            if (!far) {
+                // K and V have been read for the last time
+                store_rows<DP>(acc, half ? V : K, half ? &dvmap : &dkmap, half ? g.dv : g.dk, (int64_t)kv_heads * a.d, a.d, rk.first + s0 + wr, hk, r, rk.len - s0 - wr,
+                               partial_rows - wr, scale, n == 0);
+                if (lane == 0) tma_store_wait();
+            }
             if (partial_rows > (warp & 3) * 32) {
                 float *part = part_of(g, far, kt, slot, hk) + ((int64_t)half * g.sink_rows + r) * a.d;
 #pragma unroll
@@ -689,7 +665,11 @@ template <int DP>
 static st_status run_grad(WindowGradArgs &g, const st_tokens *t, cudaStream_t stream)
 {
     const WindowArgs &a = g.w;
-    CUtensorMap qm, km, vm, dom;
+    CUtensorMap qm, km, vm, dom, dqm, dkm, dvm;
+    const Table dq{g.dq, (int64_t)t->heads * t->d, t->d}, dk{g.dk, (int64_t)t->kv_heads * t->d, t->d}, dv{g.dv, (int64_t)t->kv_heads * t->d, t->d};
+    if (!make_tmap_table(&dqm, dq, t->nq, t->heads, t->d, 32) || !make_tmap_table(&dkm, dk, t->nk, t->kv_heads, t->d, 32) ||
+        !make_tmap_table(&dvm, dv, t->nk, t->kv_heads, t->d, 32))
+        return ST_ERR_CUDA;
     const Table dout{g.dout, (int64_t)t->heads * t->d, t->d};
     if (!make_tmap_table(&qm, a.q, t->nq, t->heads, t->d) || !make_tmap_table(&km, a.k, t->nk, t->kv_heads, t->d) ||
         !make_tmap_table(&vm, a.v, t->nk, t->kv_heads, t->d) || !make_tmap_table(&dom, dout, t->nq, t->heads, t->d))
@@ -697,10 +677,10 @@ static st_status run_grad(WindowGradArgs &g, const st_tokens *t, cudaStream_t st
     using S = wgrad::Shape<DP>;
     if (!ensure_dynamic_smem(window_dq_kernel<DP>, S::DQ_SMEM) || !ensure_dynamic_smem(window_dkv_kernel<DP>, S::DKV_SMEM)) return ST_ERR_CUDA;
     st_status rc = launch(window_dq_kernel<DP>, dim3((unsigned)most_tiles(t->nq, t->nseq, TILE), (unsigned)t->heads), wgrad::THREADS, S::DQ_SMEM, stream,
-                          qm, km, vm, dom, g);
+                          qm, km, vm, dom, dqm, g);
     if (rc != ST_OK) return rc;
     const dim3 grid((unsigned)(g.sink_tiles * g.nslots + most_tiles(t->nk, t->nseq, TILE)), (unsigned)t->kv_heads);
-    rc = launch(window_dkv_kernel<DP>, grid, wgrad::THREADS, S::DKV_SMEM, stream, qm, km, vm, dom, g);
+    rc = launch(window_dkv_kernel<DP>, grid, wgrad::THREADS, S::DKV_SMEM, stream, qm, km, vm, dom, dkm, dvm, g);
     if (rc != ST_OK || g.sink_tiles == 0) return rc;
     return launch(window_sinks_kernel, dim3((unsigned)g.nslots, (unsigned)t->kv_heads, (unsigned)g.sink_tiles), 256, 0, stream, g);
 }
