@@ -477,12 +477,16 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const FadeArgs a)
     }
 }
 
-// Chunks of a segment: so many that two segments come to every SM where the sequences alone give fewer blocks; 0: whole sequences.
-static int segment_chunks(int64_t n, int64_t heads, int64_t d)
+// Chunks of a segment, 0: whole sequences.  Whole, a call takes the longest sequence's chunks one after another, here estimated as twice the mean
+// (the lengths are on the device); in segments 1.6 times its share of all chunks, as the states are summed first, and the time of some 12
+// chunks for two launches more.  Segments are so long that two come to every SM.
+// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 358 / SEG_TRAIN; 9 of up to 1333, 8 heads 26 / SEG_PROMPTS.
+static int segment_chunks(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
-    const int64_t blocks = heads * ((d + fade::ZC - 1) / fade::ZC), wanted = 2 * (int64_t)sm_count_or_default() / blocks;
-    if (wanted <= 1) return 0;
-    const int64_t chunks = (n + TILE - 1) / TILE, each = (chunks + wanted - 1) / wanted, some = each < 4 ? 4 : each;
+    const int64_t sms = sm_count_or_default(), blocks = heads * ((d + fade::ZC - 1) / fade::ZC), wanted = 2 * sms / blocks;
+    const int64_t chunks = (n + TILE - 1) / TILE, mean = (chunks + nseq - 1) / nseq, longest = 2 * mean < chunks ? 2 * mean : chunks;
+    if (wanted <= 1 || longest <= chunks * blocks * 8 / (5 * sms) + 12) return 0;
+    const int64_t each = (chunks + wanted - 1) / wanted, some = each < 4 ? 4 : each;
     return some >= chunks ? 0 : (int)some;
 }
 
@@ -530,7 +534,7 @@ static FadeArgs fade_args(const st_tokens *t, const float *log_decay, const int3
     FadeArgs a = {};
     a.status = (unsigned *)ws;
     a.check = 1;
-    a.chunks = segment_chunks(t->nq, t->heads, t->d > t->dv ? t->d : t->dv);
+    a.chunks = segment_chunks(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv);
     a.states = a.chunks ? (float *)((unsigned char *)ws + kWsHeaderBytes) : nullptr;
     if (!a.chunks) a.chunks = 1 << 22;                                 // 2^29 tokens, as many as a sequence can have
     a.dx = (int)t->d;
@@ -554,7 +558,7 @@ static Table table_of(const void *p, int64_t rows, int64_t heads, int64_t row, i
 size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
     if (n <= 0 || nseq <= 0 || heads <= 0 || d <= 0 || d > 128 || n > (1 << 29) || heads > 65535 || nseq > (1 << 20)) return 0;
-    const int chunks = attn::segment_chunks(n, heads, d);
+    const int chunks = attn::segment_chunks(n, nseq, heads, d);
     const size_t states = chunks ? (size_t)attn::most_tiles(n, nseq, (int64_t)chunks * attn::TILE) * heads * d * d * sizeof(float) : 0;
     return kWsHeaderBytes + round_up(states, 256);
 }

@@ -27,7 +27,7 @@ constexpr int PART_TILES = 8, PART = PART_TILES * TILE;      // queries of a par
 constexpr int MAX_SPLIT_SINKS = 2 * TILE;                    // with more first columns they are no small share of the work any more
 template <int DP> struct Shape {
     static constexpr int TILE_BYTES = DP / 64 * SLAB;
-    static constexpr size_t DQ_SMEM = 1024 + (size_t)TILE_BYTES * 7 + 2 * TILE * sizeof(float) + 256;
+    static constexpr size_t DQ_SMEM = 1024 + (size_t)TILE_BYTES * 7 + TILE * sizeof(float) + 256;
     static constexpr size_t DKV_SMEM = 1024 + (size_t)TILE_BYTES * 6 + 4 * TILE * sizeof(float) + 256;
 };
 }  // namespace wgrad
@@ -121,8 +121,8 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
     unsigned char *Q = smem, *DO = Q + BYTES, *K = DO + BYTES, *V = K + KS * BYTES;
-    float *halves = (float *)(V + VS * BYTES);
-    uint64_t *bars = (uint64_t *)(halves + 2 * TILE);
+    float *deltas = (float *)(V + VS * BYTES);
+    uint64_t *bars = (uint64_t *)(deltas + TILE);
     uint64_t *q_full = bars, *do_full = bars + 1, *k_full = bars + 2, *k_copied = k_full + KS, *k_empty = k_copied + KS, *v_full = k_empty + KS,
              *v_empty = v_full + VS, *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_full = dp_full + 1, *done = ds_full + 1;
     uint32_t *tmem_slot = (uint32_t *)(done + 1);
@@ -258,18 +258,38 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         const int64_t row = rq.first + i0 + r;
         const bool mine = r < left;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        float lse2 = 0.f, delta = 0.f;
+        float lse2 = 0.f;
         if (mine) {
             const float lse = g.lse[row * a.heads + h];
             lse2 = lse == -INFINITY ? 0.f : lse * LOG2E;
-            const int64_t base = (row * a.heads + h) * a.d;
-            for (int c = half * 8; c < a.d; c += 16)
-                delta += dot8(*reinterpret_cast<const uint4 *>(g.o + base + c), *reinterpret_cast<const uint4 *>(g.dout + base + c));
         }
-        halves[half * TILE + r] = delta;
+        // delta: a warp takes 16 rows, as many lanes to a row as it has pieces of 16 bytes, all loads at once
+        {
+            constexpr int LANES = DP / 8, AT_ONCE = 32 / LANES, N = 16 / AT_ONCE;
+            const int piece = lane % LANES, first = warp * 16 + lane / LANES;
+            uint4 x[N], y[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int i = first + k * AT_ONCE;
+                const bool in = i < left && piece * 8 < a.d;
+                const int64_t at = ((int64_t)(rq.first + i0 + i) * a.heads + h) * a.d + piece * 8;
+                x[k] = in ? *reinterpret_cast<const uint4 *>(g.o + at) : make_uint4(0u, 0u, 0u, 0u);
+                y[k] = in ? *reinterpret_cast<const uint4 *>(g.dout + at) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int i = first + k * AT_ONCE;
+                float sum = dot8(x[k], y[k]);
+#pragma unroll
+                for (int o = LANES / 2; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+                if (piece == 0) {
+                    deltas[i] = sum;
+                    if (i < left) g.delta[(int64_t)(rq.first + i0 + i) * a.heads + h] = sum;
+                }
+            }
+        }
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        delta = halves[r] + halves[TILE + r];
-        if (mine && half == 0) g.delta[row * a.heads + h] = delta;
+        const float delta = deltas[r];
         const float c = a.scale * LOG2E;
         bool ok = true;
         for (int j = 0; j < n; ++j) {
