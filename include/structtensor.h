@@ -381,7 +381,7 @@ st_status st_attn_decay(const st_tokens *tokens, const void *q, const void *k, c
 /* Gradient of st_attn_decay in q, k, v and state_in (the decay is a constant of the layer):
  *     dq[t] = scale S[t] dout[t];   R[t] = scale q[t] (x) dout[t] + exp(a) R[t+1], R[n] = exp(-a) dstate_out (or 0);
  *     dk[t] = R[t] v[t];   dv[t] = R[t]^T k[t];   dstate_in = exp(a) R[0]
- * state_in, dstate_out and dstate_in may be NULL. */
+ * state_in, dstate_out and dstate_in may be NULL; dstate_in is neither of the other two. */
 st_status st_attn_decay_grad(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
                              const void *dout, const int32_t *offsets, const float *state_in, const float *dstate_out,
                              float scale, void *dq, void *dk, void *dv, float *dstate_in, void *ws, size_t ws_bytes,

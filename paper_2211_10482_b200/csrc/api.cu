@@ -9,7 +9,7 @@ size_t ttm_tf32_tc_workspace(int64_t rows, int64_t K, int64_t R);
 size_t ttm_split_workspace(int64_t rows, int64_t K, int64_t R);
 size_t mttkrp_workspace(int64_t rows, int64_t I, int64_t K, int64_t R, unsigned flags);
 size_t attn_window_grad_workspace(int64_t nq, int64_t heads, int64_t kv_heads, int64_t sinks);
-size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d);
+size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d, bool gradient);
 }  // namespace st
 
 #ifdef ST_BOUNDS_CHECK
@@ -54,8 +54,8 @@ size_t st_workspace_bytes(st_op op, int64_t a, int64_t b, int64_t c, int64_t e, 
     case ST_OP_ATTN_WINDOW:
     case ST_OP_ATTN_WINDOW_STEP: return st::kWsHeaderBytes;
     case ST_OP_ATTN_WINDOW_GRAD: return st::attn_window_grad_workspace(a, b, c, e);
-    case ST_OP_ATTN_DECAY:
-    case ST_OP_ATTN_DECAY_GRAD: return st::attn_decay_workspace(a, b, c, e);
+    case ST_OP_ATTN_DECAY: return st::attn_decay_workspace(a, b, c, e, false);
+    case ST_OP_ATTN_DECAY_GRAD: return st::attn_decay_workspace(a, b, c, e, true);
     default: return 0;
     }
 }

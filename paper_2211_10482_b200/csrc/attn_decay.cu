@@ -22,11 +22,14 @@
 // Warps: 0..3 make P (a thread = a token), 4..7 weigh Z (a thread = a token), 8..11 keep S (a thread = a row of it) and write out (a thread = a
 // token), 12 copies, 13 issues the products.
 #include "attn_tc.cuh"
+#include <algorithm>
+#include <utility>
 
 namespace st {
 namespace attn {
 
 struct FadeArgs {
+    CUtensorMap xmap, ymap, zmap, outmap;
     Table x, y, z;
     int dx, dz;                       // extent of x and y, extent of z and out
     const float *log_decay;
@@ -81,12 +84,19 @@ __device__ __forceinline__ Segment segment_of(const FadeArgs &a, int tile, int l
     return {at.seq, r.first + at.tile * rows, min(r.len - at.tile * rows, rows), at.tile, max((r.len + rows - 1) / rows, 1)};
 }
 
-// STATE: only the segment's own sum of outer products, to `states`.  BACK: backwards in time.
-template <int DX, bool STATE, bool BACK>
+// The runs of one launch, one to a plane of the grid: those of the gradient are independent, and together fill the SMs where one alone has as
+// many blocks as heads and columns (6 sequences of up to 4096 tokens, 16 heads: one after another 274 us, together TOGETHER).
+constexpr int MAX_RUNS = 3;
+struct FadeRuns {
+    FadeArgs run[MAX_RUNS];
+};
+
+// STATE: only the segment's own sum of outer products, to `states`.
+template <int DX, bool STATE>
 __global__ void __launch_bounds__(fade::THREADS, 1)
-fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const __grid_constant__ CUtensorMap zmap,
-            const __grid_constant__ CUtensorMap outmap, const FadeArgs a)
+fade_kernel(const __grid_constant__ FadeRuns runs)
 {
+    const FadeArgs &a = runs.run[blockIdx.z];
     using namespace fade;
     using namespace tc;
     using Sh = Shape<DX, STATE>;
@@ -95,13 +105,14 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     unsigned char *smem = align_smem(raw);
     unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_parts = S_op + Sh::S_BYTES,      // Z_parts: [buffer][2]
                   *out_rows = Z_parts + 2 * BUFS * Sh::Z_BYTES;
-    float *table = (float *)(out_rows + Sh::OUT_BYTES);              // 128 zeros, then in_scale w^m
+    float *table = (float *)(out_rows + Sh::OUT_BYTES);              // in_scale w^m on one side of the middle, zeros on the other
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
     uint64_t *in_full = bars, *xy_empty = in_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
              *z_ready = o_free + 1, *s_ready = z_ready + BUFS, *u_full = s_ready + 1, *u_free = u_full + BUFS, *xs_done = u_free + 1;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
+    const bool back = a.backwards;
     const int slabs = (a.dz + ZC - 1) / ZC, slab = blockIdx.x % slabs, tile = blockIdx.x / slabs;
 
     pdl_wait();
@@ -115,13 +126,17 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
     const Segment seg = segment_of(a, tile, lane);
     if (seg.seq < 0) return;
     // nobody needs the sum of the segment that comes last
-    if (STATE && seg.index == (BACK ? 0 : seg.count - 1)) return;
+    if (STATE && seg.index == (back ? 0 : seg.count - 1)) return;
     const int n = (seg.len + TILE - 1) / TILE;
     const float decay = a.log_decay[h], a2 = decay * LOG2E;
-    auto chunk_of = [&](int i) { return BACK ? n - 1 - i : i; };
+    auto chunk_of = [&](int i) { return back ? n - 1 - i : i; };
     auto tokens_of = [&](int i) { return min(seg.len - chunk_of(i) * TILE, TILE); };
 
-    if (threadIdx.x < 2 * TILE) table[threadIdx.x] = threadIdx.x < TILE ? 0.f : a.in_scale * power(a2, threadIdx.x - TILE);
+    // the weight of column s for token t is table[128 + t - s], 0 on the side of the diagonal that is not summed
+    if (threadIdx.x < 2 * TILE) {
+        const int gap = back ? TILE - (int)threadIdx.x : (int)threadIdx.x - TILE;
+        table[threadIdx.x] = gap < 0 ? 0.f : a.in_scale * power(a2, gap);
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&in_full[s], 1);
@@ -161,10 +176,10 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             auto ahead = [&](int i) {
                 if (i >= n) return;
                 const int row = seg.first + chunk_of(i) * TILE;
-                prefetch_3d(&zmap, slab * ZC, h, row);
+                prefetch_3d(&a.zmap, slab * ZC, h, row);
                 if (slab != 0) return;
-                prefetch_tile<DX>(&ymap, h, row);
-                if (!STATE) prefetch_tile<DX>(&xmap, h, row);
+                prefetch_tile<DX>(&a.ymap, h, row);
+                if (!STATE) prefetch_tile<DX>(&a.xmap, h, row);
             };
             for (int i = 0; i < n; ++i) {
                 const int s = i % STAGES, row = seg.first + chunk_of(i) * TILE;
@@ -172,10 +187,10 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
                 unsigned char *st = stages + s * Sh::STAGE;
                 if (!mbar_wait(&xy_empty[s], parity, abort_flag, a.status, 1)) break;
                 mbar_expect_tx(&in_full[s], Sh::STAGE);
-                load_tile<DX>(st, &ymap, &in_full[s], h, row);
-                if (!STATE) load_tile<DX>(st + Sh::X_BYTES + Sh::Z_BYTES, &xmap, &in_full[s], h, row);
+                load_tile<DX>(st, &a.ymap, &in_full[s], h, row);
+                if (!STATE) load_tile<DX>(st + Sh::X_BYTES + Sh::Z_BYTES, &a.xmap, &in_full[s], h, row);
                 if (!mbar_wait(&z_empty[s], parity, abort_flag, a.status, 15)) break;
-                tma_load_3d(st + Sh::X_BYTES, &zmap, &in_full[s], slab * ZC, h, row);
+                tma_load_3d(st + Sh::X_BYTES, &a.zmap, &in_full[s], slab * ZC, h, row);
                 ahead(i + STAGES);
             }
         }
@@ -243,8 +258,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         if (!STATE) {
             const uint32_t lanes = (uint32_t)(warp * 32) << 16;
             bool ok = true;
-            // weight of column s: table[128 + t - s], or backwards table[128 + s - t]; 32 columns that are all zeros are not read
-            const float *w = BACK ? table + TILE - threadIdx.x : table + TILE + threadIdx.x;
+            const float *w = table + TILE + threadIdx.x;
             for (int i = 0; i < n; ++i) {
                 ok = __all_sync(~0u, mbar_wait(&sc_full[i & 1], (uint32_t)((i >> 1) & 1), abort_flag, a.status, 8));
                 if (!ok) break;
@@ -256,19 +270,18 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 #pragma unroll 1
                 for (int j = 0; j < 4; ++j) {
                     uint32_t p[16];
-                    if (BACK ? j < warp : j > warp) {
+                    if (back ? j < warp : j > warp) {                     // all zeros
 #pragma unroll
                         for (int e = 0; e < 16; ++e) p[e] = 0u;
                     } else {
                         uint32_t x[32];
                         tmem_ld_32x32(addr + j * 32, x);
-                        const float *wj = BACK ? w + j * 32 : w - j * 32;
+                        const float *wj = w - j * 32;
                         tmem_ld_wait();
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
                             const int c = 2 * e;
-                            p[e] = pack_bf16(BACK ? wj[c] * __uint_as_float(x[c]) : wj[-c] * __uint_as_float(x[c]),
-                                             BACK ? wj[c + 1] * __uint_as_float(x[c + 1]) : wj[-c - 1] * __uint_as_float(x[c + 1]));
+                            p[e] = pack_bf16(wj[-c] * __uint_as_float(x[c]), wj[-c - 1] * __uint_as_float(x[c + 1]));
                         }
                     }
                     tmem_st_32x16(addr + j * 16, p);
@@ -285,7 +298,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         bool ok = true;
         for (int i = 0; i < n; ++i) {
             const int L = tokens_of(i);
-            const float beta = t < L ? a.in_scale * power(a2, BACK ? t + 1 : L - 1 - t) : 0.f;
+            const float beta = t < L ? a.in_scale * power(a2, back ? t + 1 : L - 1 - t) : 0.f;
             ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
             if (ok && i >= BUFS) ok = __all_sync(~0u, mbar_wait(&u_full[i % BUFS], (uint32_t)((i / BUFS - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
@@ -340,10 +353,10 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         bool ok = true;
         const float keep_full = carry(decay, TILE);
-        const float full_alpha = a.out_scale * power(a2, BACK ? TILE - 1 - r : r + 1);
+        const float full_alpha = a.out_scale * power(a2, back ? TILE - 1 - r : r + 1);
         auto write = [&](int i) {
             const int first = chunk_of(i) * TILE, L = tokens_of(i);
-            const float alpha = !BACK || L == TILE ? full_alpha : a.out_scale * power(a2, max(L - 1 - r, 0));
+            const float alpha = !back || L == TILE ? full_alpha : a.out_scale * power(a2, max(L - 1 - r, 0));
             ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
             if (!ok) return;
             tc_fence_after();
@@ -376,7 +389,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
             if (w * 32 + 32 <= L) {
                 fence_proxy_async();
                 __syncwarp();
-                if (lane == 0) tma_store_3d(&outmap, out_rows + w * 4096, slab * ZC, h, row);
+                if (lane == 0) tma_store_3d(&a.outmap, out_rows + w * 4096, slab * ZC, h, row);
             } else {
                 __syncwarp();
                 const int c = lane & 7;
@@ -423,7 +436,7 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
         }
         if (!STATE && ok && n > 0) write(n - 1);
         if (!STATE && lane == 0) tma_store_wait();
-        const bool end = seg.index == (BACK ? 0 : seg.count - 1);
+        const bool end = seg.index == (back ? 0 : seg.count - 1);
         float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && a.last ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
         if (ok && to && row) {
 #pragma unroll
@@ -443,13 +456,14 @@ fade_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CU
 }
 
 // The segments' own sums become the states that enter the segments; a thread owns four elements of a head's state.
-__global__ void __launch_bounds__(256) fade_carry_kernel(const FadeArgs a)
+__global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__ FadeRuns runs, int parts)
 {
+    const FadeArgs &a = runs.run[blockIdx.z / parts];
     pdl_wait();
     pdl_trigger();
     const Segment seg = segment_of(a, blockIdx.x, threadIdx.x & 31);
     if (seg.seq < 0 || seg.index != 0) return;
-    const int h = blockIdx.y, plane = a.dx * a.dz, e = (blockIdx.z * 256 + threadIdx.x) * 4;
+    const int h = blockIdx.y, plane = a.dx * a.dz, e = (blockIdx.z % parts * 256 + threadIdx.x) * 4;
     if (e >= plane) return;
     const Rows r = rows_of(a.offsets, seg.seq, a.n);
     const int rows = a.chunks * TILE;
@@ -490,34 +504,42 @@ static int segment_chunks(int64_t n, int64_t nseq, int64_t heads, int64_t d)
     return some >= chunks ? 0 : (int)some;
 }
 
-template <int DX, bool STATE, bool BACK>
-static st_status launch_fade(const FadeArgs &a, cudaStream_t stream)
+template <int DX, bool STATE>
+static st_status launch_fade(const FadeRuns &r, int count, cudaStream_t stream)
 {
-    CUtensorMap xm, ym, zm, om;
-    const Table out{a.out, (int64_t)a.heads * a.dz, a.dz};
-    if (STATE) om = CUtensorMap{};
-    else if (!make_tmap_table(&om, out, a.n, a.heads, a.dz, 32)) return ST_ERR_CUDA;
-    if (!make_tmap_table(&xm, STATE ? a.y : a.x, a.n, a.heads, a.dx) || !make_tmap_table(&ym, a.y, a.n, a.heads, a.dx) ||
-        !make_tmap_table(&zm, a.z, a.n, a.heads, a.dz))
-        return ST_ERR_CUDA;
     const size_t smem = fade::Shape<DX, STATE>::SMEM;
-    if (!ensure_dynamic_smem(fade_kernel<DX, STATE, BACK>, smem)) return ST_ERR_CUDA;
-    const int64_t tiles = most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE), slabs = (a.dz + fade::ZC - 1) / fade::ZC;
-    return launch(fade_kernel<DX, STATE, BACK>, dim3((unsigned)(tiles * slabs), a.heads), fade::THREADS, smem, stream, xm, ym, zm, om, a);
+    if (!ensure_dynamic_smem(fade_kernel<DX, STATE>, smem)) return ST_ERR_CUDA;
+    const FadeArgs &a = r.run[0];
+    const int64_t tiles = most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
+    int slabs = 1;
+    for (int i = 0; i < count; ++i) slabs = std::max(slabs, (r.run[i].dz + fade::ZC - 1) / fade::ZC);
+    return launch(fade_kernel<DX, STATE>, dim3((unsigned)(tiles * slabs), (unsigned)a.heads, (unsigned)count), fade::THREADS, smem, stream, r);
 }
-static st_status run_fade(const FadeArgs &a, cudaStream_t stream)
+
+// `count` runs over the same tokens at once: their states that enter the segments (of y (x) z as it is kept: not transposed), or all of them.
+template <bool STATE>
+static st_status run_fades(FadeRuns &r, int count, cudaStream_t stream)
 {
-    if (a.backwards) return a.dx <= 64 ? launch_fade<64, false, true>(a, stream) : launch_fade<128, false, true>(a, stream);
-    return a.dx <= 64 ? launch_fade<64, false, false>(a, stream) : launch_fade<128, false, false>(a, stream);
+    bool wide = false;
+    for (int i = 0; i < count; ++i) {
+        FadeArgs &a = r.run[i];
+        const Table out{a.out, (int64_t)a.heads * a.dz, a.dz};
+        if (!make_tmap_table(&a.ymap, a.y, a.n, a.heads, a.dx) || !make_tmap_table(&a.zmap, a.z, a.n, a.heads, a.dz)) return ST_ERR_CUDA;
+        if (!STATE && (!make_tmap_table(&a.xmap, a.x, a.n, a.heads, a.dx) || !make_tmap_table(&a.outmap, out, a.n, a.heads, a.dz, 32))) return ST_ERR_CUDA;
+        wide = wide || a.dx > 64;
+    }
+    const st_status rc = wide ? launch_fade<128, STATE>(r, count, stream) : launch_fade<64, STATE>(r, count, stream);
+    if (!STATE || rc != ST_OK) return rc;
+    const FadeArgs &a = r.run[0];
+    const int parts = (a.dx * a.dz + 1023) / 1024;
+    return launch(fade_carry_kernel, dim3((unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE), (unsigned)a.heads, (unsigned)(parts * count)), 256, 0, stream, r, parts);
 }
-// The states that enter the segments, of y (x) z as it is kept: not transposed.
-static st_status run_states(const FadeArgs &a, cudaStream_t stream)
+
+// The states of the segments of one run.
+static size_t states_floats(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
-    const st_status rc = a.backwards ? (a.dx <= 64 ? launch_fade<64, true, true>(a, stream) : launch_fade<128, true, true>(a, stream))
-                                     : (a.dx <= 64 ? launch_fade<64, true, false>(a, stream) : launch_fade<128, true, false>(a, stream));
-    if (rc != ST_OK) return rc;
-    const unsigned tiles = (unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
-    return launch(fade_carry_kernel, dim3(tiles, a.heads, (unsigned)((a.dx * a.dz + 1023) / 1024)), 256, 0, stream, a);
+    const int chunks = segment_chunks(n, nseq, heads, d);
+    return chunks ? (size_t)most_tiles(n, nseq, (int64_t)chunks * TILE) * heads * d * d : 0;
 }
 
 static st_status check_decay(const st_tokens *t, const int32_t *offsets)
@@ -555,12 +577,10 @@ static Table table_of(const void *p, int64_t rows, int64_t heads, int64_t row, i
 
 }  // namespace attn
 
-size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d)
+size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d, bool gradient)
 {
     if (n <= 0 || nseq <= 0 || heads <= 0 || d <= 0 || d > 128 || n > (1 << 29) || heads > 65535 || nseq > (1 << 20)) return 0;
-    const int chunks = attn::segment_chunks(n, nseq, heads, d);
-    const size_t states = chunks ? (size_t)attn::most_tiles(n, nseq, (int64_t)chunks * attn::TILE) * heads * d * d * sizeof(float) : 0;
-    return kWsHeaderBytes + round_up(states, 256);
+    return kWsHeaderBytes + round_up((gradient ? 2 : 1) * attn::states_floats(n, nseq, heads, d) * sizeof(float), 256);
 }
 
 }  // namespace st
@@ -579,7 +599,7 @@ st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const 
     if (!q || !k || !v || !log_decay || !out) return ST_ERR_NULL;
     for (const void *p : {q, k, v, (const void *)log_decay, (const void *)offsets, (const void *)state_in, (const void *)out, (const void *)state_out})
         if (!aligned16(p)) return ST_ERR_ALIGN;
-    if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv)) return ST_ERR_WORKSPACE;
+    if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv, false)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     FadeArgs a = fade_args(t, log_decay, offsets, ws);
     a.x = table_of(q, t->nq, t->heads, t->q_row, t->q_head);
@@ -589,11 +609,13 @@ st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const 
     a.last = state_out;
     a.out_scale = scale;
     a.out = (bf16 *)out;
+    FadeRuns r = {};
+    r.run[0] = a;
     if (a.states) {
-        if ((rc = run_states(a, (cudaStream_t)stream)) != ST_OK) return rc;
-        a.check = 0;
+        if ((rc = run_fades<true>(r, 1, (cudaStream_t)stream)) != ST_OK) return rc;
+        r.run[0].check = 0;
     }
-    return run_fade(a, (cudaStream_t)stream);
+    return run_fades<false>(r, 1, (cudaStream_t)stream);
 }
 
 st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, const void *v, const float *log_decay,
@@ -604,58 +626,56 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
     st_status rc = check_decay(t, offsets);
     if (rc != ST_OK) return rc;
     if (!q || !k || !v || !log_decay || !dout || !dq || !dk || !dv) return ST_ERR_NULL;
+    // the runs go at once: one reads what another would write
+    if (dstate_in && (dstate_in == dstate_out || dstate_in == state_in)) return ST_ERR_UNSUPPORTED;
     for (const void *p : {q, k, v, (const void *)log_decay, dout, (const void *)offsets, (const void *)state_in, (const void *)dstate_out,
                           (const void *)dq, (const void *)dk, (const void *)dv, (const void *)dstate_in})
         if (!aligned16(p)) return ST_ERR_ALIGN;
-    if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv)) return ST_ERR_WORKSPACE;
+    if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv, true)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     const Table Q = table_of(q, t->nq, t->heads, t->q_row, t->q_head), K = table_of(k, t->nk, t->heads, t->k_row, t->k_head),
                 V = table_of(v, t->nk, t->heads, t->v_row, t->v_head), O = table_of(dout, t->nq, t->heads, t->heads * t->dv, t->dv);
     cudaStream_t s = (cudaStream_t)stream;
     FadeArgs a = fade_args(t, log_decay, offsets, ws);
+    FadeRuns r = {};
+    FadeArgs &dq_run = r.run[0], &dv_run = r.run[1], &dk_run = r.run[2];
     // dq[t] = scale sum e^{a(t-s)} (dout[t].v[s]) k[s], with the states of k (x) v
     a.y = K;
     a.z = V;
     a.init = state_in;
-    if (a.states) {
-        if ((rc = run_states(a, s)) != ST_OK) return rc;
-        a.check = 0;
-    }
-    a.x = O;
-    a.y = V;
-    a.z = K;
-    a.dx = (int)t->dv;
-    a.dz = (int)t->d;
-    a.transposed = 1;
-    a.out_scale = scale;
-    a.out = (bf16 *)dq;
-    if ((rc = run_fade(a, s)) != ST_OK) return rc;
-    a.check = 0;
+    dq_run = a;
     // dv[s] = sum e^{a(t-s)} (k[s].q[t]) scale dout[t], backwards, with the states of q (x) dout
     a.x = K;
     a.y = Q;
     a.z = O;
-    a.dx = (int)t->d;
-    a.dz = (int)t->dv;
-    a.transposed = 0;
     a.backwards = 1;
+    a.check = 0;
     a.init = dstate_out;
     a.in_scale = scale;
-    a.out_scale = 1.f;
     a.out = (bf16 *)dv;
-    if (a.states && (rc = run_states(a, s)) != ST_OK) return rc;
-    a.last = dstate_in;
-    if ((rc = run_fade(a, s)) != ST_OK) return rc;
+    if (a.states) a.states += states_floats(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv);
+    dv_run = a;
+    if (a.states) {
+        if ((rc = run_fades<true>(r, 2, s)) != ST_OK) return rc;
+        dq_run.check = 0;
+    }
+    dv_run.last = dstate_in;
+    dq_run.x = O;
+    dq_run.y = V;
+    dq_run.z = K;
+    std::swap(dq_run.dx, dq_run.dz);
+    dq_run.transposed = 1;
+    dq_run.out_scale = scale;
+    dq_run.out = (bf16 *)dq;
     // dk[s] = sum e^{a(t-s)} (v[s].dout[t]) scale q[t], backwards, with the same states
     a.x = V;
     a.y = O;
     a.z = Q;
-    a.dx = (int)t->dv;
-    a.dz = (int)t->d;
+    std::swap(a.dx, a.dz);
     a.transposed = 1;
-    a.last = nullptr;
     a.out = (bf16 *)dk;
-    return run_fade(a, s);
+    dk_run = a;
+    return run_fades<false>(r, 3, s);
 }
 
 }  // extern "C"
