@@ -319,7 +319,7 @@ typedef struct {
     int32_t dtype;            /* st_dtype of q, k, v, out, dout and the gradients: ST_BF16 */
     int32_t reserved;         /* must be 0 */
     int64_t nseq;             /* sequences */
-    int64_t nq, nk;           /* rows of q, out, dout, dq; rows of k, v, dk, dv */
+    int64_t nq, nk;           /* rows of q, out, dout, dq; rows of k, v, dk, dv: up to 2^29 */
     int64_t heads, kv_heads;  /* query head h reads key head h / (heads / kv_heads) */
     int64_t d, dv;            /* extent of a query and a key, extent of a value: multiples of 8 up to 128 */
     int64_t q_row, q_head;    /* strides */
@@ -354,7 +354,7 @@ typedef struct {
     int32_t reserved;         /* must be 0 */
     int64_t nseq, heads, kv_heads, d;
     int64_t pages, page;      /* pages of the cache, tokens of a page */
-    int64_t table_cols;       /* page numbers in a row of the table */
+    int64_t table_cols;       /* page numbers in a row of the table: page * table_cols up to 2^30 */
     int64_t page_stride, token_stride, head_stride;   /* of k_pages and v_pages, in elements, multiples of 8 */
 } st_cache;
 
@@ -362,8 +362,8 @@ typedef struct {
  * key and value (k, v: [nseq, kv_heads, d]) are written to the cache at position lens[b]-1; out = attention of q
  * ([nseq, heads, d], position lens[b]-1) over the cache and the new token.  All contiguous but the cache.  lens[b] = 0: out = 0,
  * nothing written.  Only table entries of visible tokens and of the new one are read.  A length beyond the table's row
- * (cut to it), a negative one (0), and a page number outside the cache where a visible token lies (the token is left out)
- * are reported: ST_ERR_DEV_BOUNDS.  Two sequences may share pages that neither writes. */
+ * (cut to it), a negative one (0), and a page number outside the cache where a visible token lies (a cached token is left
+ * out, the new one is not written) are reported: ST_ERR_DEV_BOUNDS.  Two sequences may share pages that neither writes. */
 st_status st_attn_window_step(const st_cache *cache, const void *q, const void *k, const void *v, void *k_pages,
                               void *v_pages, const int32_t *table, const int32_t *lens, int64_t window, int64_t sinks,
                               float scale, void *out, void *ws, size_t ws_bytes, void *stream);

@@ -26,8 +26,8 @@ inline st_status check_tokens(const st_tokens *t)
     if (t->reserved != 0 || t->nseq <= 0 || t->nq <= 0 || t->nk <= 0 || t->heads <= 0 || t->kv_heads <= 0 || t->d <= 0 || t->dv <= 0)
         return ST_ERR_SHAPE;
     if (t->heads % t->kv_heads != 0) return ST_ERR_SHAPE;
-    // rows and sequences are counted in 32 bits, heads are a grid's second extent
-    if (t->nq > (1 << 30) || t->nk > (1 << 30) || t->nseq > (1 << 20) || t->heads > 65535) return ST_ERR_UNSUPPORTED;
+    // rows and sequences are counted in 32 bits, with room for a position less a window less a position; heads are a grid's second extent
+    if (t->nq > (1 << 29) || t->nk > (1 << 29) || t->nseq > (1 << 20) || t->heads > 65535) return ST_ERR_UNSUPPORTED;
     if (t->d % 8 != 0 || t->dv % 8 != 0 || t->d > 128 || t->dv > 128) return ST_ERR_UNSUPPORTED;
     const bool fits = stride_ok(t->nq, t->q_row, t->d) && stride_ok(t->heads, t->q_head, t->d) && stride_ok(t->nk, t->k_row, t->d) &&
                       stride_ok(t->kv_heads, t->k_head, t->d) && stride_ok(t->nk, t->v_row, t->dv) && stride_ok(t->kv_heads, t->v_head, t->dv);
@@ -43,7 +43,8 @@ inline st_status check_tokens(const st_tokens *t)
 // The stride of an extent of one is never used; whatever was passed, it is a legal one.
 inline int64_t stride_of(int64_t extent, int64_t stride) { return extent == 1 ? 128 : stride; }
 
-inline int clamp_int(int64_t x) { return x > (1 << 30) ? 1 << 30 : (int)x; }
+// A window or a number of first columns: the whole of the longest sequence is as far as it goes.
+inline int clamp_int(int64_t x, int most = 1 << 29) { return x > most ? most : (int)x; }
 
 #if defined(__CUDACC__)
 

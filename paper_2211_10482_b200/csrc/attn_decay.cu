@@ -49,11 +49,11 @@ struct FadeArgs {
 namespace fade {
 constexpr int THREADS = 448, ZC = 64;               // ZC: columns of z of a block
 template <int DX, bool STATE> struct Shape {
-    static constexpr int STAGES = STATE ? 3 : 2;
+    static constexpr int STAGES = STATE || DX == 64 ? 3 : 2;
     static constexpr int BUFS = STATE ? 2 : 1;                                      // of the weighted Z
     static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = STATE ? 0 : DX * 128, OUT_BYTES = STATE ? 0 : SLAB;
     static constexpr int STAGE = (STATE ? 1 : 2) * X_BYTES + Z_BYTES;               // Y, Z, X
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * BUFS * Z_BYTES + OUT_BYTES + 2 * TILE * sizeof(float) + 256;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * BUFS * Z_BYTES + OUT_BYTES + 2 * TILE * sizeof(float) + 320;
 };
 }  // namespace fade
 
@@ -107,7 +107,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
                   *out_rows = Z_parts + 2 * BUFS * Sh::Z_BYTES;
     float *table = (float *)(out_rows + Sh::OUT_BYTES);              // in_scale w^m on one side of the middle, zeros on the other
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
-    uint64_t *in_full = bars, *xy_empty = in_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
+    uint64_t *xy_full = bars, *z_full = xy_full + STAGES, *xy_empty = z_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
              *z_ready = o_free + 1, *s_ready = z_ready + BUFS, *u_full = s_ready + 1, *u_free = u_full + BUFS, *xs_done = u_free + 1;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
@@ -139,7 +139,8 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
-            mbar_init(&in_full[s], 1);
+            mbar_init(&xy_full[s], 1);
+            mbar_init(&z_full[s], 1);
             mbar_init(&xy_empty[s], 1);
             mbar_init(&z_empty[s], 1);
         }
@@ -186,11 +187,12 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
                 const uint32_t parity = (uint32_t)((i / STAGES + 1) & 1);
                 unsigned char *st = stages + s * Sh::STAGE;
                 if (!mbar_wait(&xy_empty[s], parity, abort_flag, a.status, 1)) break;
-                mbar_expect_tx(&in_full[s], Sh::STAGE);
-                load_tile<DX>(st, &a.ymap, &in_full[s], h, row);
-                if (!STATE) load_tile<DX>(st + Sh::X_BYTES + Sh::Z_BYTES, &a.xmap, &in_full[s], h, row);
+                mbar_expect_tx(&xy_full[s], Sh::STAGE - Sh::Z_BYTES);
+                load_tile<DX>(st, &a.ymap, &xy_full[s], h, row);
+                if (!STATE) load_tile<DX>(st + Sh::X_BYTES + Sh::Z_BYTES, &a.xmap, &xy_full[s], h, row);
                 if (!mbar_wait(&z_empty[s], parity, abort_flag, a.status, 15)) break;
-                tma_load_3d(st + Sh::X_BYTES, &a.zmap, &in_full[s], slab * ZC, h, row);
+                mbar_expect_tx(&z_full[s], Sh::Z_BYTES);
+                tma_load_3d(st + Sh::X_BYTES, &a.zmap, &z_full[s], slab * ZC, h, row);
                 ahead(i + STAGES);
             }
         }
@@ -204,7 +206,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             for (int i = -1; i < n && ok; ++i) {
                 const unsigned char *Y = stages + ((i + STAGES) % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *X = Z + Sh::Z_BYTES;
                 if (i >= 0) {
-                    if (STATE) ok = warp_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
+                    if (STATE) ok = warp_wait(&xy_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
                     if (ok) ok = warp_wait(&z_ready[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 3);
                     if (ok && i > 0) ok = warp_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
                     if (!ok) break;
@@ -233,7 +235,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
                 }
                 if (!STATE && i + 1 < n) {
                     const int e = i + 1;
-                    ok = warp_wait(&in_full[e % STAGES], (uint32_t)((e / STAGES) & 1), abort_flag, a.status, 2);
+                    ok = warp_wait(&xy_full[e % STAGES], (uint32_t)((e / STAGES) & 1), abort_flag, a.status, 2);
                     // rows behind the sequence are cleared first
                     if (ok && tokens_of(e) < TILE) ok = warp_wait(&z_ready[e % BUFS], (uint32_t)((e / BUFS) & 1), abort_flag, a.status, 16);
                     if (!ok) break;
@@ -299,7 +301,8 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
         for (int i = 0; i < n; ++i) {
             const int L = tokens_of(i);
             const float beta = t < L ? a.in_scale * power(a2, back ? t + 1 : L - 1 - t) : 0.f;
-            ok = __all_sync(~0u, mbar_wait(&in_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
+            ok = __all_sync(~0u, mbar_wait(&z_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
+            if (ok && L < TILE) ok = __all_sync(~0u, mbar_wait(&xy_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 17));
             if (ok && i >= BUFS) ok = __all_sync(~0u, mbar_wait(&u_full[i % BUFS], (uint32_t)((i / BUFS - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
             unsigned char *Y = stages + (i % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *Z_hi = Z_parts + (i % BUFS) * 2 * Sh::Z_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
@@ -462,7 +465,8 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__
     pdl_wait();
     pdl_trigger();
     const Segment seg = segment_of(a, blockIdx.x, threadIdx.x & 31);
-    if (seg.seq < 0 || seg.index != 0) return;
+    // offsets that decrease can make more segments than there is room for: those have no states
+    if (seg.seq < 0 || seg.index != 0 || blockIdx.x + seg.count > gridDim.x) return;
     const int h = blockIdx.y, plane = a.dx * a.dz, e = (blockIdx.z % parts * 256 + threadIdx.x) * 4;
     if (e >= plane) return;
     const Rows r = rows_of(a.offsets, seg.seq, a.n);
@@ -547,7 +551,6 @@ static st_status check_decay(const st_tokens *t, const int32_t *offsets)
     const st_status rc = check_tokens(t);
     if (rc != ST_OK) return rc;
     if (t->nq != t->nk || t->heads != t->kv_heads) return ST_ERR_SHAPE;
-    if (t->nq > (1 << 29)) return ST_ERR_UNSUPPORTED;
     return !offsets && t->nseq != 1 ? ST_ERR_NULL : ST_OK;
 }
 

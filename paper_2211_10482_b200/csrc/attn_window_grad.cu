@@ -709,7 +709,7 @@ static st_status run_grad(WindowGradArgs &g, const st_tokens *t, cudaStream_t st
 
 size_t attn_window_grad_workspace(int64_t nq, int64_t heads, int64_t kv_heads, int64_t sinks)
 {
-    if (nq <= 0 || heads <= 0 || kv_heads <= 0 || kv_heads > heads || sinks < 0 || nq > (1 << 30) || heads > 65535) return 0;
+    if (nq <= 0 || heads <= 0 || kv_heads <= 0 || kv_heads > heads || sinks < 0 || nq > (1 << 29) || heads > 65535) return 0;
     return kWsHeaderBytes + round_up((size_t)nq * heads * sizeof(float), 256) + attn::parts_floats(nq, kv_heads, sinks, 128) * sizeof(float);
 }
 

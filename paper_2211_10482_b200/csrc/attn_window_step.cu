@@ -414,7 +414,8 @@ extern "C" st_status st_attn_window_step(const st_cache *c, const void *q, const
     if (c->reserved != 0 || c->nseq <= 0 || c->heads <= 0 || c->kv_heads <= 0 || c->d <= 0 || c->pages <= 0 || c->page <= 0 || c->table_cols <= 0 ||
         c->heads % c->kv_heads != 0 || window < 1 || sinks < 0)
         return ST_ERR_SHAPE;
-    if (c->nseq > 65535 || c->heads > 65535 || c->d % 8 != 0 || c->d > 128 || c->pages > (1 << 30) || c->page > (1 << 30) || c->table_cols > (1 << 30))
+    if (c->nseq > 65535 || c->heads > 65535 || c->d % 8 != 0 || c->d > 128 || c->pages > (1 << 30) || c->page > (1 << 30) || c->table_cols > (1 << 30) ||
+        c->page * c->table_cols > (1 << 30))               // tokens of a sequence
         return ST_ERR_UNSUPPORTED;
     if (!stride_ok(c->pages, c->page_stride, c->d) || !stride_ok(c->page, c->token_stride, c->d) || !stride_ok(c->kv_heads, c->head_stride, c->d))
         return ST_ERR_SHAPE;
@@ -442,8 +443,8 @@ extern "C" st_status st_attn_window_step(const st_cache *c, const void *q, const
     a.page = (int)c->page;
     a.page_magic = 0xFFFFFFFFu / (unsigned)c->page;
     a.cols = (int)c->table_cols;
-    a.window = clamp_int(window);
-    a.sinks = clamp_int(sinks);
+    a.window = clamp_int(window, 1 << 30);
+    a.sinks = clamp_int(sinks, 1 << 30);
     a.page_stride = stride_of(c->pages, c->page_stride);
     a.token_stride = stride_of(c->page, c->token_stride);
     a.head_stride = stride_of(c->kv_heads, c->head_stride);

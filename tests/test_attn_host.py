@@ -55,7 +55,7 @@ def decay_step(t=None, q=P[0], state=P[4]):
 BAD_TOKENS = [
     (dict(dtype=st.ST_F32), st.ST_ERR_DTYPE), (dict(reserved=1), st.ST_ERR_SHAPE), (dict(nseq=0), st.ST_ERR_SHAPE), (dict(d=0), st.ST_ERR_SHAPE),
     (dict(heads=0), st.ST_ERR_SHAPE), (dict(dv=-8), st.ST_ERR_SHAPE), (dict(nq=0, nk=0), st.ST_ERR_SHAPE),
-    (dict(d=12, dv=12), st.ST_ERR_UNSUPPORTED), (dict(d=136, dv=136), st.ST_ERR_UNSUPPORTED), (dict(nq=1 << 31, nk=1 << 31), st.ST_ERR_UNSUPPORTED),
+    (dict(d=12, dv=12), st.ST_ERR_UNSUPPORTED), (dict(d=136, dv=136), st.ST_ERR_UNSUPPORTED), (dict(nq=(1 << 29) + 1, nk=(1 << 29) + 1), st.ST_ERR_UNSUPPORTED),
     (dict(q_row=60), st.ST_ERR_SHAPE), (dict(k_head=-64), st.ST_ERR_SHAPE), (dict(v_row=0), st.ST_ERR_SHAPE), (dict(q_row=260), st.ST_ERR_ALIGN),
     (dict(k_head=68), st.ST_ERR_ALIGN), (dict(v_row=1 << 50), st.ST_ERR_UNSUPPORTED)]
 
@@ -89,7 +89,7 @@ def test_step_refusals():
     assert step(q=None) == step(kp=None) == step(table=None) == step(lens=None) == st.ST_ERR_NULL
     for change in (dict(nseq=0), dict(pages=0), dict(page=0), dict(table_cols=0), dict(heads=3), dict(reserved=2), dict(token_stride=8), dict(page_stride=-8)):
         assert step(cache(**change)) == st.ST_ERR_SHAPE, change
-    for change in (dict(d=20), dict(d=256, token_stride=512, head_stride=256), dict(nseq=1 << 20)):
+    for change in (dict(d=20), dict(d=256, token_stride=512, head_stride=256), dict(nseq=1 << 20), dict(page=1 << 20, table_cols=1 << 11)):
         assert step(cache(**change)) == st.ST_ERR_UNSUPPORTED, change
     assert step(cache(dtype=st.ST_F64)) == st.ST_ERR_DTYPE
     assert step(w=0) == step(sinks=-1) == st.ST_ERR_SHAPE
@@ -107,6 +107,8 @@ def test_decay_refusals():
     need = st.st_workspace_bytes(st.ST_OP_ATTN_DECAY_GRAD, 100, 2, 4, 64)
     assert need >= 256 and decay_grad(n=need - 1) == st.ST_ERR_WORKSPACE
     assert st.st_workspace_bytes(st.ST_OP_ATTN_DECAY, 100, 2, 4, 136) == 0
+    assert st.lib().st_attn_decay_grad(tokens(**EVEN), *P[:5], P[5], P[9], P[10], 1.0, *P[6:9], P[10], P[11], 1 << 40, None) == st.ST_ERR_UNSUPPORTED
+    assert st.lib().st_attn_decay_grad(tokens(**EVEN), *P[:5], P[5], P[9], P[10], 1.0, *P[6:9], P[9], P[11], 1 << 40, None) == st.ST_ERR_UNSUPPORTED
     assert decay_step(q=None) == decay_step(state=None) == st.ST_ERR_NULL
     assert decay_step(tokens(nseq=99, **EVEN)) == decay_step(tokens(nseq=100)) == st.ST_ERR_SHAPE
     assert decay_step(state=264) == st.ST_ERR_ALIGN

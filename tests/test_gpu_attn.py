@@ -243,6 +243,23 @@ def test_bad_offsets_are_reported_and_touch_nothing_outside(bad):
     ok()
 
 
+def test_offsets_that_name_the_same_rows_again_stay_within_the_workspace():
+    """More segments than the lengths can have: reported, and no state outside of its place (the guard bands see to that)."""
+    n = 128 * 300
+    q, k, v = (normal(75 + i, n, 1, 64) for i in range(3))
+    at = torch.tensor([0, n, 0, n, 0, n, 0, n], dtype=torch.int32, device="cuda")
+    a = -torch.ones(1, device="cuda")
+    assert st.st_workspace_bytes(st.ST_OP_ATTN_DECAY, n, 1, 1, 64) > 256                 # one sequence of that length is cut
+    st.st_attn_decay(q, k, v, a, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_decay_grad(q, k, v, a, q, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    out, lse = st.st_attn_window(q, k, v, 20, 2, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_window_grad(q, k, v, out, lse, q, 20, 2, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+
+
 # --------------------------------------------------------------------------------- window: step
 
 STEPS = [
@@ -493,6 +510,30 @@ def test_decay_step_against_the_definition(n, H, d, dv):
 
 
 # --------------------------------------------------------------------------- used together, and otherwise
+
+def test_tables_whose_offsets_pass_32_bits():
+    st.set_allocator(None)
+    H, d, last = 64, 128, 300
+    n = (1 << 31) // (H * d) + 500
+    q = torch.zeros(n, H, d, dtype=BF16, device="cuda")
+    k, v, do = (torch.zeros_like(q) for _ in range(3))
+    for i, x in enumerate((q, k, v, do)):
+        x[-last:] = normal(190 + i, last, H, d)
+    at = torch.tensor([0, n - last, n], dtype=torch.int32, device="cuda")
+    a = -torch.linspace(0.01, 1.0, H, device="cuda")
+    tail = [x[-last:].clone() for x in (q, k, v, do)]
+    out, lse = st.st_attn_window(q, k, v, 70, 3, at)
+    want = st.st_attn_window(*tail[:3], 70, 3)
+    assert torch.equal(out[-last:], want[0]) and torch.equal(lse[-last:], want[1])
+    for g, w in zip(st.st_attn_window_grad(q, k, v, out, lse, do, 70, 3, at), st.st_attn_window_grad(*tail[:3], *want, tail[3], 70, 3)):
+        assert torch.equal(g[-last:], w)
+    out, s = st.st_attn_decay(q, k, v, a, at)
+    want = st.st_attn_decay(*tail[:3], a)
+    assert torch.equal(out[-last:], want[0]) and torch.equal(s[1:], want[1])
+    for g, w in zip(st.st_attn_decay_grad(q, k, v, a, do, at)[:3], st.st_attn_decay_grad(*tail[:3], a, tail[3])[:3]):
+        assert torch.equal(g[-last:], w)
+    ok()
+
 
 def test_a_prompt_and_its_steps_are_the_whole_sequence():
     """Two layers, one of each kind: a prompt of 150 tokens, then 20 single steps, against one pass over all 170."""
