@@ -85,7 +85,7 @@ __device__ __forceinline__ Segment segment_of(const FadeArgs &a, int tile, int l
 }
 
 // The runs of one launch, one to a plane of the grid: those of the gradient are independent, and together fill the SMs where one alone has as
-// many blocks as heads and columns (6 sequences of up to 4096 tokens, 16 heads: one after another 274 us, together TOGETHER).
+// many blocks as heads and columns (6 sequences of up to 4096 tokens, 16 heads: one after another 274 us, together 231).
 constexpr int MAX_RUNS = 3;
 struct FadeRuns {
     FadeArgs run[MAX_RUNS];
@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__
 // Chunks of a segment, 0: whole sequences.  Whole, a call takes the longest sequence's chunks one after another, here estimated as twice the mean
 // (the lengths are on the device); in segments 1.6 times its share of all chunks, as the states are summed first, and the time of some 12
 // chunks for two launches more.  Segments are so long that two come to every SM.
-// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 358 / SEG_TRAIN; 9 of up to 1333, 8 heads 26 / SEG_PROMPTS.
+// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 358 / 274; 9 of up to 1333, 8 heads 26 / 22.
 static int segment_chunks(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
     const int64_t sms = sm_count_or_default(), blocks = heads * ((d + fade::ZC - 1) / fade::ZC), wanted = 2 * sms / blocks;

@@ -127,18 +127,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Args..
     return __all_sync(~0u, tc::mbar_wait(bar, parity, args...));
 }
 
-__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
-          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
-          "r"(r[30]), "r"(r[31])
-        : "memory");
-}
 __device__ __forceinline__ void tmem_st_32x16(uint32_t taddr, const uint32_t (&r)[16])
 {
     asm volatile(
@@ -249,28 +237,46 @@ struct Mask {
     __device__ __forceinline__ bool all(int t0, int t1, int s0, int s1) const { return s1 <= t0 && (s0 > t1 - window || s1 < sinks); }
 };
 
-// The tiles of keys that the queries at positions t0..t1 see: [0, first) with the sinks and [lo, hi).
-struct KeyTiles {
-    int first, lo, hi;
-    __device__ __forceinline__ int count() const { return first + max(0, hi - lo); }
-    __device__ __forceinline__ int at(int i) const { return i < first ? i : lo + i - first; }
-};
-__device__ __forceinline__ KeyTiles key_tiles(const Mask &m, int t0, int t1)
-{
-    KeyTiles k;
-    k.hi = t1 < 0 ? 0 : t1 / TILE + 1;
-    k.lo = min(max(0, t0 - m.window + 1) / TILE, k.hi);
-    k.first = min((min(m.sinks, 1 << 29) + TILE - 1) / TILE, k.lo);
-    return k;
-}
-
 // Which of 32 columns, of which the first is `first` columns into a tile that begins at key s0, the query at position t sees: bit c, column c.
 struct RowMask {
     int hi, lo, sinks;                         // columns of the tile: at most hi, and at least lo or below sinks
     __device__ __forceinline__ RowMask(const Mask &m, int t, int s0) : hi(t - s0), lo(t - m.window + 1 - s0), sinks(m.sinks - s0) {}
+    __device__ __forceinline__ explicit RowMask(int last) : hi(last), lo(0), sinks(0) {}            // columns up to `last`
     static __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
     __device__ __forceinline__ unsigned of(int first) const { return below(hi + 1 - first) & (~below(lo - first) | below(sinks - first)); }
 };
+// The tiles of keys that the queries at positions t0..t1 see: `first` with the first columns in front of the band, cut at `sinks`, and `band` from
+// key `origin` on.  The band's tiles begin where it does, not at multiples of 128: 128 queries with a window of 512 meet five of them wherever
+// they stand, and not six (prompts of up to 2111 tokens behind 40, 16 heads: with the piece of the first columns 145 -> 132 us).
+struct KeyTiles {
+    static constexpr int PIECE = 32;
+    int first, band, origin, sinks;
+    __device__ __forceinline__ int count() const { return first + band; }
+    __device__ __forceinline__ int key(int i) const { return i < first ? i * TILE : origin + (i - first) * TILE; }
+    // a few first columns alone in the first tile: only so many columns of it are multiplied
+    __device__ __forceinline__ bool piece(int i) const { return i == 0 && first == 1 && sinks <= PIECE; }
+    // whether each of the queries t0..t1 sees all of tile i, and which columns of it the one at t sees
+    __device__ __forceinline__ bool all(const Mask &m, int t0, int t1, int i) const
+    {
+        return i < first ? (i + 1) * TILE <= sinks : m.all(t0, t1, key(i), key(i) + TILE - 1);
+    }
+    __device__ __forceinline__ RowMask row_mask(const Mask &m, int t, int i) const
+    {
+        RowMask r(m, t, key(i));
+        if (i < first) r = RowMask(sinks - 1 - i * TILE);
+        return r;
+    }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const Mask &m, int t0, int t1)
+{
+    KeyTiles k;
+    k.origin = max(0, t0 - m.window + 1);
+    k.band = t1 < k.origin ? 0 : (t1 - k.origin) / TILE + 1;
+    k.sinks = k.band ? min(m.sinks, k.origin) : 0;
+    k.first = (k.sinks + TILE - 1) / TILE;
+    return k;
+}
+
 // The same for a key at position s and the 32 queries from position t0 + first: s <= t, and t < s + window or s < sinks.
 struct ColumnMask {
     int lo, hi;

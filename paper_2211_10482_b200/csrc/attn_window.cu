@@ -68,9 +68,9 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
     const KeyTiles tiles = key_tiles(mask, t0, t0 + left - 1);
     const int n = tiles.count();
     // positions of the rows of a tile of queries (none: t1 < t0), and whether it sees a tile of keys
-    auto sees = [&](int w, int kt) {
-        const int first = t0 + w * TILE;
-        return mask.any(first, min(first + TILE, t0 + left) - 1, kt * TILE, kt * TILE + TILE - 1);
+    auto sees = [&](int w, int i) {
+        const int first = t0 + w * TILE, s0 = tiles.key(i);
+        return mask.any(first, min(first + TILE, t0 + left) - 1, s0, s0 + TILE - 1);
     };
 
     if (threadIdx.x == 0) {
@@ -108,8 +108,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         uint32_t copied = 0;                    // parity of v_copied, by stage
         bool ok = true;
         for (int i = 0; i < n && ok; ++i) {
-            const int kt = tiles.at(i);
-            const bool a0 = sees(0, kt), a1 = sees(1, kt);
+            const bool a0 = sees(0, i), a1 = sees(1, i);
             if (!a0 && !a1) continue;
             for (int w = 0; w < 2; ++w)
                 if ((w ? a1 : a0) && !q_asked[w]) {
@@ -119,9 +118,9 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                         load_tile<DP>(Q + w * S::TILE_BYTES, &qmap, &q_full[w], h, rq.first + i0 + w * TILE);
                     }
                 }
-            const int s = use % STAGES, row = rk.first + kt * TILE;
+            const int s = use % STAGES, s0 = tiles.key(i), row = rk.first + s0;
             const uint32_t parity = (uint32_t)((use / STAGES + 1) & 1);
-            const bool edge = kt * TILE + TILE > rk.len;
+            const bool edge = s0 + TILE > rk.len;
             if (lane == 0) {
                 ok = mbar_wait(&k_empty[s], parity, abort_flag, a.status, 1);
                 if (ok) {
@@ -140,7 +139,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                 ok = __all_sync(~0u, mbar_wait(&v_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
                 copied ^= 1u << s;
                 if (ok) {
-                    clear_rows<DP>(V + s * S::TILE_BYTES, rk.len - kt * TILE, lane);
+                    clear_rows<DP>(V + s * S::TILE_BYTES, rk.len - s0, lane);
                     if (lane == 0) mbar_arrive(&v_full[s]);
                 }
             }
@@ -151,22 +150,22 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         // overwrite (products are carried out in the order of their issue), and the other tile's products fill the time between.
         const int w = warp - 9;
         const bool lead = elect_one();
-        const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
+        const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP), piece_idesc = make_idesc(1, 0, 0, TILE, KeyTiles::PIECE);
         const uint32_t s_col = tmem + w * TILE, o_col = tmem + 2 * TILE + w * DP;
         const unsigned char *mine = Q + w * S::TILE_BYTES;
         bool ok = true, started = false;
         int i = 0, use = 0, done = 0;                            // tiles looked at, copied, used by this tile of queries
         int at_stage = -1;                                       // the stage whose scores are in the exponential
         uint32_t at_parity = 0;
+        bool at_piece = false;
         while (ok) {
             // the next tile that was copied
             bool a0 = false, a1 = false;
             for (; i < n && !(a0 || a1); ++i) {
-                const int kt = tiles.at(i);
-                a0 = sees(0, kt);
-                a1 = sees(1, kt);
+                a0 = sees(0, i);
+                a1 = sees(1, i);
             }
-            const bool more = a0 || a1, score = w ? a1 : a0;
+            const bool more = a0 || a1, score = w ? a1 : a0, piece = more && tiles.piece(i - 1);
             const int s = use % STAGES;
             const uint32_t parity = (uint32_t)((use / STAGES) & 1);
             if (at_stage >= 0 && (score || !more)) {
@@ -174,11 +173,12 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                 if (ok) ok = warp_wait(&p_full[2 * w], (uint32_t)(done & 1), abort_flag, a.status, 7);
                 if (!ok) break;
                 tc_fence_after();
-                mma_tokens<32, 0, 4>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, started);
+                if (at_piece) mma_tokens<32, 0, KeyTiles::PIECE / 16>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, started);
+                else mma_tokens<32, 0, 4>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, started);
                 ok = warp_wait(&p_full[2 * w + 1], (uint32_t)(done & 1), abort_flag, a.status, 7);
                 if (!ok) break;
                 tc_fence_after();
-                mma_tokens<32, 4, 8>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, true);
+                if (!at_piece) mma_tokens<32, 4, 8>(lead, o_col, s_col, V + at_stage * S::TILE_BYTES, o_idesc, true);
                 commit(lead, &v_empty[at_stage]);
                 at_stage = -1;
                 started = true;
@@ -190,9 +190,10 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             if (!ok) break;
             if (score) {
                 tc_fence_after();
-                mma_rows<DP>(lead, s_col, mine, K + s * S::TILE_BYTES, s_idesc);
+                mma_rows<DP>(lead, s_col, mine, K + s * S::TILE_BYTES, piece ? piece_idesc : s_idesc);
                 commit(lead, &s_full[w]);
                 at_stage = s;
+                at_piece = piece;
                 at_parity = parity;
             } else {
                 // a tile that the other queries alone see: given back once it is there, so that the stages' turns stay in order
@@ -213,20 +214,42 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         uint32_t parity = 0;
         bool ok = true, started = false;
         for (int i = 0; i < n; ++i) {
-            const int kt = tiles.at(i);
-            if (!sees(w, kt)) continue;
+            if (!sees(w, i)) continue;
             ok = __all_sync(~0u, mbar_wait(&s_full[w], parity, abort_flag, a.status, 8));
             if (!ok) break;
             parity ^= 1u;
             tc_fence_after();
-            const int s0 = kt * TILE;
-            const bool cut = !mask.all(t0 + w * TILE, t0 + w * TILE + TILE - 1, s0, s0 + TILE - 1);
+            if (tiles.piece(i)) {                         // comes first, and every query sees the same columns
+                uint32_t x[32], p[16];
+                tmem_ld_32x32(s_addr, x);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    if (e >= tiles.sinks) x[e] = __float_as_uint(-INFINITY);
+                    m = fmaxf(m, __uint_as_float(x[e]));
+                }
+                const float mc = m == -INFINITY ? 0.f : -m * c;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float2 y = {ex2(fmaf(__uint_as_float(x[2 * e]), c, mc)), ex2(fmaf(__uint_as_float(x[2 * e + 1]), c, mc))};
+                    l += y.x + y.y;
+                    p[e] = pack_bf16(y.x, y.y);
+                }
+                tmem_st_32x16(s_addr, p);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane < 2) mbar_arrive(&p_full[2 * w + lane]);
+                started = true;
+                continue;
+            }
+            const bool cut = !tiles.all(mask, t0 + w * TILE, t0 + w * TILE + TILE - 1, i);
             uint32_t x[4][32];
 #pragma unroll
             for (int j = 0; j < 4; ++j) tmem_ld_32x32(s_addr + j * 32, x[j]);
             tmem_ld_wait();
             if (cut) {
-                const RowMask seen(mask, t, s0);
+                const RowMask seen = tiles.row_mask(mask, t, i);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const unsigned bits = seen.of(j * 32);

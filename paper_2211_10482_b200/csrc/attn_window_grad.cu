@@ -187,8 +187,8 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         bool ok = true;
         uint32_t copied = 0;
         for (int i = 0; i < n && ok; ++i) {
-            const int kt = tiles.at(i), row = rk.first + kt * TILE, s = i % KS, sv = i % VS;
-            const bool edge = kt * TILE + TILE > rk.len;
+            const int s0 = tiles.key(i), row = rk.first + s0, s = i % KS, sv = i % VS;
+            const bool edge = s0 + TILE > rk.len;
             if (lane == 0) {
                 ok = mbar_wait(&k_empty[s], (uint32_t)((i / KS + 1) & 1), abort_flag, a.status, 1);
                 if (ok) {
@@ -207,7 +207,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 ok = __all_sync(~0u, mbar_wait(&k_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
                 copied ^= 1u << s;
                 if (ok) {
-                    clear_rows<DP>(K + s * BYTES, rk.len - kt * TILE, lane);
+                    clear_rows<DP>(K + s * BYTES, rk.len - s0, lane);
                     if (lane == 0) mbar_arrive(&k_full[s]);
                 }
             }
@@ -215,14 +215,14 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     } else if (warp == 9) {
         if (n > 0) {
             const bool lead = elect_one();
-            const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP);
+            const uint32_t s_idesc = make_idesc(1, 0, 0, TILE, TILE), o_idesc = make_idesc(1, 0, 1, TILE, DP), piece_idesc = make_idesc(1, 0, 0, TILE, KeyTiles::PIECE);
             bool ok = true;
             auto score = [&](int j) {
                 if (!ok || j >= n) return;
                 ok = warp_wait(&k_full[j % KS], (uint32_t)((j / KS) & 1), abort_flag, a.status, 4);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(lead, tmem + (j & 1) * TILE, Q, K + (j % KS) * BYTES, s_idesc);
+                mma_rows<DP>(lead, tmem + (j & 1) * TILE, Q, K + (j % KS) * BYTES, tiles.piece(j) ? piece_idesc : s_idesc);
                 commit(lead, &s_full[j & 1]);
             };
             auto dprob = [&](int j) {
@@ -230,7 +230,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 ok = warp_wait(&v_full[j % VS], (uint32_t)((j / VS) & 1), abort_flag, a.status, 5);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<DP>(lead, dp_col, DO, V + (j % VS) * BYTES, s_idesc);
+                mma_rows<DP>(lead, dp_col, DO, V + (j % VS) * BYTES, tiles.piece(j) ? piece_idesc : s_idesc);
                 commit(lead, dp_full);
                 commit(lead, &v_empty[j % VS]);
             };
@@ -245,7 +245,8 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 tc_fence_after();
                 dprob(j + 1);
                 if (!ok) break;
-                mma_tokens<64>(lead, dq_col, tmem + (j & 1) * TILE, K + (j % KS) * BYTES, o_idesc, j > 0);
+                if (tiles.piece(j)) mma_tokens<64, 0, KeyTiles::PIECE / 16>(lead, dq_col, tmem + (j & 1) * TILE, K + (j % KS) * BYTES, o_idesc, false);
+                else mma_tokens<64>(lead, dq_col, tmem + (j & 1) * TILE, K + (j % KS) * BYTES, o_idesc, j > 0);
                 commit(lead, &k_empty[j % KS]);
                 score(j + 2);
             }
@@ -294,15 +295,15 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         bool ok = true;
         for (int j = 0; j < n; ++j) {
             const uint32_t s_addr = tmem + lanes + (j & 1) * TILE + half * 64, dp_addr = dp_col + lanes + half * 64;
-            const int s0 = tiles.at(j) * TILE;
-            const bool cut = !mask.all(t0, t0 + TILE - 1, s0, s0 + TILE - 1);
+            const bool cut = !tiles.all(mask, t0, t0 + TILE - 1, j), piece = tiles.piece(j);
             ok = __all_sync(~0u, mbar_wait(&s_full[j & 1], (uint32_t)((j >> 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
             tc_fence_after();
-            const RowMask seen(mask, t, s0);
+            const RowMask seen = tiles.row_mask(mask, t, j);
             Pair p[2][16];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
+                if (piece && half + b > 0) continue;
                 uint32_t x[32];
                 tmem_ld_32x32(s_addr + b * 32, x);
                 tmem_ld_wait();
@@ -318,6 +319,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
             tc_fence_after();
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
+                if (piece && half + b > 0) continue;
                 uint32_t dp[32], ds[16];
                 tmem_ld_32x32(dp_addr + b * 32, dp);
                 tmem_ld_wait();
