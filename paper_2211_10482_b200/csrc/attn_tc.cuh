@@ -7,7 +7,7 @@
 namespace st {
 namespace attn {
 
-constexpr int TILE = 128;                     // tokens of a tile
+constexpr int TILE_LOG = 7, TILE = 1 << TILE_LOG;                     // tokens of a tile
 constexpr int SLAB = TILE * 128;              // bytes of 64 columns of a tile: rows of 128 bytes, 128-byte swizzle
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 

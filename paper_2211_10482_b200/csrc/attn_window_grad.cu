@@ -12,7 +12,7 @@
 // Products and exponentials overlap: while a tile's dS is made the tensor cores work on the next tile's S.
 //
 // The first columns (sinks) are seen by every later query, so that their tiles of keys would take as long as the whole sequence:
-// queries beyond the window are cut into parts of 1024 for blocks of their own, which leave fp32 sums of the sinks' rows in the
+// queries beyond the window are cut into parts of 256 or 1024 for blocks of their own, which leave fp32 sums of the sinks' rows in the
 // workspace; window_sinks_kernel adds them in the order of the parts.
 //
 // Rows behind a sequence may hold anything: where they would be multiplied by weights of 0 they are cleared in shared memory.
@@ -23,7 +23,10 @@ namespace attn {
 
 namespace wgrad {
 constexpr int THREADS = 320;
-constexpr int PART_TILES = 8, PART = PART_TILES * TILE;      // queries of a part beyond the window
+// Tiles of queries of a part beyond the window: short ones where their sums are few, so that these blocks take no longer than the others (4
+// sequences of up to 4096 tokens, window 1024, forward and backward: 511 us with parts of 1024, 493 of 256).
+constexpr int part_log(int64_t sinks) { return sinks <= 32 ? 1 : 3; }
+constexpr int part_rows(int64_t sinks) { return TILE << part_log(sinks); }
 constexpr int MAX_SPLIT_SINKS = 2 * TILE;                    // with more first columns they are no small share of the work any more
 template <int DP> struct Shape {
     static constexpr int TILE_BYTES = DP / 64 * SLAB;
@@ -40,6 +43,7 @@ struct WindowGradArgs {
     float *delta;                  // [nq, heads]
     float *parts;                  // sums of the sinks' rows: [2: near, far][tile of keys][slot][key head][2: dk, dv][rows][d]
     int nslots, sink_tiles, sink_rows;   // 0 sink_tiles: nothing is split
+    int part_log;                        // a part has 2^part_log tiles of queries
 };
 
 __device__ __forceinline__ float *part_of(const WindowGradArgs &g, int far, int kt, int slot, int hk)
@@ -66,15 +70,17 @@ __device__ __forceinline__ QueryTiles query_tiles(const Mask &m, const Rows &rq,
     return q;
 }
 // First query tile that is left to the parts, where a tile of keys is split.
-__device__ __forceinline__ int first_part(const QueryTiles &q) { return q.near + wgrad::PART_TILES; }
+__device__ __forceinline__ int first_part(const WindowGradArgs &g, const QueryTiles &q) { return q.near + (1 << g.part_log); }
 
-// The sequence one of whose parts begins in rows [slot * PART, slot * PART + PART), and that part; by a whole warp.  Parts begin PART rows
-// apart and the first of a sequence more than PART rows behind its beginning, so that there is one at most.
+// The sequence one of whose parts begins in rows [slot P, slot P + P) for P rows a part, and that part; by a whole warp.  Parts begin P rows
+// apart and the first of a sequence more than P rows behind its beginning, so that there is one at most.
 struct PartOf {
     int seq, part;
 };
-__device__ __forceinline__ PartOf part_at(const WindowArgs &a, const Mask &m, int kt, int slot, int lane)
+__device__ __forceinline__ PartOf part_at(const WindowGradArgs &g, const Mask &m, int kt, int slot, int lane)
 {
+    const WindowArgs &a = g.w;
+    const int shift = TILE_LOG + g.part_log, rows = 1 << shift;
     for (int b0 = 0; b0 < a.nseq; b0 += 32) {
         const int b = b0 + lane;
         int part = -1;
@@ -82,9 +88,9 @@ __device__ __forceinline__ PartOf part_at(const WindowArgs &a, const Mask &m, in
             const Rows rq = rows_of(a.q_offsets, b, a.nq), rk = rows_of(a.k_offsets, b, a.nk);
             if (kt * TILE < rk.len) {
                 const QueryTiles q = query_tiles(m, rq, rk, kt * TILE);
-                const int begin = rq.first + first_part(q) * TILE, p = max(0, (slot * wgrad::PART - begin + wgrad::PART - 1) / wgrad::PART);
-                const int row = begin + p * wgrad::PART;
-                if (first_part(q) + p * wgrad::PART_TILES < q.all && row / wgrad::PART == slot) part = p;
+                const int begin = rq.first + first_part(g, q) * TILE, p = max(0, (slot * rows - begin + rows - 1) >> shift);
+                const int row = begin + p * rows;
+                if (first_part(g, q) + (p << g.part_log) < q.all && row >> shift == slot) part = p;
             }
         }
         const unsigned found = __ballot_sync(~0u, part >= 0);
@@ -385,14 +391,14 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
     if (far) {
         kt = blockIdx.x / g.nslots;
         slot = blockIdx.x % g.nslots;
-        const PartOf p = part_at(a, mask, kt, slot, lane);
+        const PartOf p = part_at(g, mask, kt, slot, lane);
         if (p.seq < 0) return;
         seq = p.seq;
         rq = rows_of(a.q_offsets, seq, a.nq);
         rk = rows_of(a.k_offsets, seq, a.nk);
         qt = query_tiles(mask, rq, rk, kt * TILE);
-        qt.a = first_part(qt) + p.part * PART_TILES;
-        qt.all = min(qt.all, qt.a + PART_TILES);
+        qt.a = first_part(g, qt) + (p.part << g.part_log);
+        qt.all = min(qt.all, qt.a + (1 << g.part_log));
     } else {
         const TileOf at = tile_of(a.k_offsets, a.nseq, a.nk, TILE, blockIdx.x - far_blocks, lane);
         if (at.seq < 0) return;
@@ -406,10 +412,10 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
     int partial_rows = 0;
     if (far) {
         partial_rows = min(a.sinks - kt * TILE, TILE);
-    } else if (kt < g.sink_tiles && first_part(qt) < qt.all) {
+    } else if (kt < g.sink_tiles && first_part(g, qt) < qt.all) {
         partial_rows = min(a.sinks - kt * TILE, TILE);
-        slot = (rq.first + first_part(qt) * TILE) / PART;
-        qt.all = first_part(qt);
+        slot = (rq.first + first_part(g, qt) * TILE) >> (TILE_LOG + g.part_log);
+        qt.all = first_part(g, qt);
     }
     const int s0 = kt * TILE, per_head = max(0, qt.all - qt.a), n = per_head * a.group, off = rk.len - rq.len;
 
@@ -655,32 +661,39 @@ __global__ void __launch_bounds__(256) window_sinks_kernel(const WindowGradArgs 
     pdl_trigger();
     const int kt = blockIdx.z, hk = blockIdx.y, kv_heads = a.heads / a.group;
     const Mask mask{a.window, a.sinks};
-    const PartOf p = part_at(a, mask, kt, blockIdx.x, threadIdx.x & 31);
+    const PartOf p = part_at(g, mask, kt, blockIdx.x, threadIdx.x & 31);
     if (p.seq < 0 || p.part != 0) return;
     const Rows rq = rows_of(a.q_offsets, p.seq, a.nq), rk = rows_of(a.k_offsets, p.seq, a.nk);
     const QueryTiles qt = query_tiles(mask, rq, rk, kt * TILE);
-    const int first = first_part(qt), parts = (qt.all - first + wgrad::PART_TILES - 1) / wgrad::PART_TILES;
+    const int first = first_part(g, qt), parts = (qt.all - first + (1 << g.part_log) - 1) >> g.part_log;
     const int rows = min(min(a.sinks - kt * TILE, TILE), rk.len - kt * TILE), quads = a.d / 4;
     for (int i = threadIdx.x; i < 2 * rows * quads; i += blockDim.x) {
         const int which = i / (rows * quads), r = i / quads % rows, c = i % quads * 4;
         const int64_t at = ((int64_t)which * g.sink_rows + r) * a.d + c;
         float4 sum = *reinterpret_cast<const float4 *>(part_of(g, 0, kt, blockIdx.x, hk) + at);
-        for (int k = 0; k < parts; ++k) {
-            const int slot = (rq.first + (first + k * wgrad::PART_TILES) * TILE) / wgrad::PART;
-            const float4 x = *reinterpret_cast<const float4 *>(part_of(g, 1, kt, slot, hk) + at);
-            sum = make_float4(sum.x + x.x, sum.y + x.y, sum.z + x.z, sum.w + x.w);
+        constexpr int AT_ONCE = 8;
+        for (int k0 = 0; k0 < parts; k0 += AT_ONCE) {
+            float4 x[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int tile = rq.first / TILE + first + (min(k0 + k, parts - 1) << g.part_log);
+                x[k] = *reinterpret_cast<const float4 *>(part_of(g, 1, kt, tile >> g.part_log, hk) + at);
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                if (k0 + k < parts) sum = make_float4(sum.x + x[k].x, sum.y + x[k].y, sum.z + x[k].z, sum.w + x[k].w);
         }
         bf16 *dst = (which ? g.dv : g.dk) + ((int64_t)(rk.first + kt * TILE + r) * kv_heads + hk) * a.d + c;
         *reinterpret_cast<uint2 *>(dst) = make_uint2(pack_bf16(sum.x, sum.y), pack_bf16(sum.z, sum.w));
     }
 }
 
-// Sums of parts: for up to two tiles of first columns, one slot per PART queries.
+// Sums of parts: for up to two tiles of first columns, one slot per part's queries.
 static size_t parts_floats(int64_t nq, int64_t kv_heads, int64_t sinks, int64_t d)
 {
     if (sinks <= 0 || sinks > wgrad::MAX_SPLIT_SINKS) return 0;
     const int64_t tiles = (sinks + TILE - 1) / TILE, rows = sinks < TILE ? sinks : TILE;
-    return (size_t)(2 * tiles * (nq / wgrad::PART + 1) * kv_heads * 2 * rows * d);
+    return (size_t)(2 * tiles * (nq / wgrad::part_rows(sinks) + 1) * kv_heads * 2 * rows * d);
 }
 
 template <int DP>
@@ -743,10 +756,11 @@ extern "C" st_status st_attn_window_grad(const st_tokens *tokens, const void *q,
     g.delta = (float *)((unsigned char *)ws + kWsHeaderBytes);
     g.parts = (float *)((unsigned char *)ws + kWsHeaderBytes + round_up((size_t)tokens->nq * tokens->heads * sizeof(float), 256));
     // queries beyond the window and a part: only a sequence that is longer has them
-    if (sinks > 0 && sinks <= wgrad::MAX_SPLIT_SINKS && tokens->nq - wgrad::PART > window) {
+    if (sinks > 0 && sinks <= wgrad::MAX_SPLIT_SINKS && tokens->nq - wgrad::part_rows(sinks) > window) {
         g.sink_tiles = (int)((sinks + TILE - 1) / TILE);
         g.sink_rows = (int)(sinks < TILE ? sinks : TILE);
-        g.nslots = (int)(tokens->nq / wgrad::PART + 1);
+        g.part_log = wgrad::part_log(sinks);
+        g.nslots = (int)(tokens->nq / wgrad::part_rows(sinks) + 1);
     }
     return g.w.d <= 64 ? run_grad<64>(g, tokens, (cudaStream_t)stream) : run_grad<128>(g, tokens, (cudaStream_t)stream);
 }

@@ -77,6 +77,12 @@ WINDOWS = [
     ([50, 300, 8, 260], [20, 150, 0, 260], 2, 2, 64, 40, 3),       # fewer keys than queries: the first rows see nothing
     ([1500], [1500], 2, 2, 64, 600, 10),
     ([17] * 40, None, 2, 2, 64, 8, 1),
+    # first columns that end just before, at and behind the band, and at the width that is multiplied alone
+    ([300], None, 2, 1, 64, 200, 32),
+    ([300], None, 2, 1, 64, 200, 33),
+    ([259, 258], [290, 600], 2, 2, 128, 257, 31),
+    ([130, 129, 200], [640, 257, 513], 2, 1, 64, 100, 128),
+    ([40], [200], 1, 1, 64, 129, 64),
 ]
 
 
@@ -115,6 +121,8 @@ def test_window_gradient_against_the_definition(lq, lk, H, Hk, d, window, sinks)
     ([1500, 4000], [7000, 4001], 2, 1, 80, 700, 256),
     ([1024, 1025, 1152, 1153, 1280], None, 2, 2, 64, 1, 1),
     ([3500], [3000], 2, 1, 64, 300, 200),
+    ([257, 513, 769, 255, 900], [300, 513, 770, 400, 900], 2, 1, 64, 1, 32),
+    ([2100, 700], None, 2, 2, 80, 129, 33),
 ])
 def test_window_gradient_of_first_columns_that_many_later_queries_see(lq, lk, H, Hk, d, window, sinks):
     """Queries beyond the window are summed in parts for the sinks' rows."""
