@@ -9,15 +9,18 @@
 // No power is of a positive exponent, whatever the decay.  Four products a chunk on the tensor cores, all accumulators in tensor memory:
 //     scores X Y^T;  P Z with P as bf16 in the place of the scores;  X S;  Y^T (weights Z).
 // S itself stays in fp32 registers, one row to a thread, and the chunk's sum is added to it there, so that no long chain of additions
-// runs through the tensor cores' accumulators (which do not round to nearest).  The weighted Z is the sum of two bf16 numbers, as one would
-// leave 2^-8 in a state that is fp32.  P, and S where it meets X, are rounded to bf16 once: out is bf16 itself.
+// runs through the tensor cores' accumulators (which do not round to nearest).  For a state that the caller gets, which is fp32, the weighted Z is
+// the sum of three bf16 numbers (2e-7 off in the root mean square); for one that only meets bf16 tables of two (5e-6), in 15 % less time.
+// P, and S where it meets X, are rounded to bf16 once: out is bf16 itself.
 //
-// A block owns 64 columns of z, out and S for a run of chunks: with 128 columns two stages of X, Y and Z, S and the weighted Z in two parts
+// A block owns 64 columns of z, out and S for a run of chunks: with 128 columns two stages of X, Y and Z, S and the weighted Z
 // would not fit in shared memory.  The two blocks of a head read X and Y at about the same time, the second time from L2.
 // Where heads and sequences are few, sequences are cut into segments: one kernel sums each segment's own state, one carries the states
-// over the segments, then all segments run at once.
+// over the segments and behind the last, then all segments run at once.
 //
-// Bound by shared memory: a chunk moves some 330 KB through it (80 of copies, 190 of operands, 64 of Z and S), 128 bytes a cycle.
+// Bound by shared memory: a chunk moves some 370 KB through it (80 of copies, 190 of operands, 100 of Z, S and out), 128 bytes a cycle, in 2850
+// cycles; with a third part 64 KB more.  And by power: 65536 tokens of 16 heads run at 1000 W and 1.5 GHz.  Two warps that issue products, or four
+// more that write out, changed nothing or lost 5 %.
 //
 // Warps: 0..3 make P (a thread = a token), 4..7 weigh Z (a thread = a token), 8..11 keep S (a thread = a row of it) and write out (a thread = a
 // token), 12 copies, 13 issues the products.
@@ -49,11 +52,11 @@ struct FadeArgs {
 namespace fade {
 constexpr int THREADS = 448, ZC = 64;               // ZC: columns of z of a block
 template <int DX, bool STATE> struct Shape {
-    static constexpr int STAGES = STATE || DX == 64 ? 3 : 2;
-    static constexpr int BUFS = STATE ? 2 : 1;                                      // of the weighted Z
-    static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = STATE ? 0 : DX * 128, OUT_BYTES = STATE ? 0 : SLAB;
+    static constexpr int STAGES = DX == 64 ? 3 : 2;
+    static constexpr int BUFS = STATE ? 2 : 1;                                      // of the weighted Z and of U
+    static constexpr int X_BYTES = DX / 64 * SLAB, Z_BYTES = SLAB, S_BYTES = STATE ? 0 : DX * 128;
     static constexpr int STAGE = (STATE ? 1 : 2) * X_BYTES + Z_BYTES;               // Y, Z, X
-    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 2 * BUFS * Z_BYTES + OUT_BYTES + 2 * TILE * sizeof(float) + 320;
+    static constexpr size_t SMEM = 1024 + (size_t)STAGES * STAGE + S_BYTES + 3 * BUFS * Z_BYTES + 2 * TILE * sizeof(float) + 320;
 };
 }  // namespace fade
 
@@ -62,13 +65,23 @@ __device__ __forceinline__ float power(float a2, int m) { return m == 0 ? 1.f : 
 // the factor of a state over `m` tokens: it enters as many times as there are chunks, so that its error counts
 __device__ __forceinline__ float carry(float a, int m) { return m == 0 ? 1.f : (float)exp((double)a * m); }
 
-// b z = hi + lo for two values z at a time, b = b_hi + b_lo: hi the rounded product, its remainder exact (two significands of 8 bits have a product
-// of 16), lo the remainder and b_lo z rounded: 2^-17 of b z is lost.
+// b z for two values z at a time as a sum of bf16 numbers.  Two, b = b_hi + b_lo: hi the rounded product, its remainder exact (two
+// significands of 8 bits have a product of 16), lo the remainder and b_lo z rounded: 2^-17 of b z is lost.
 __device__ __forceinline__ void times(__nv_bfloat162 b_hi, __nv_bfloat162 b_lo, uint32_t z, uint32_t &hi, uint32_t &lo)
 {
     const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&z), h = __hmul2(b_hi, x), l = __hfma2(b_lo, x, __hfma2(b_hi, x, __hneg2(h)));
     hi = *reinterpret_cast<const uint32_t *>(&h);
     lo = *reinterpret_cast<const uint32_t *>(&l);
+}
+// Three: each the rounded remainder of the fp32 product, which fp32 holds exactly.
+__device__ __forceinline__ void times(float b, uint32_t z, uint32_t &hi, uint32_t &mid, uint32_t &lo)
+{
+    auto wide = [](uint32_t x) { return pair(x << 16, x & 0xffff0000u); };
+    const Pair minus = pair(-1.f, -1.f), x = mul(pair(b, b), wide(z));
+    hi = pack_bf16(x);
+    const Pair y = fma(minus, wide(hi), x);
+    mid = pack_bf16(y);
+    lo = pack_bf16(fma(minus, wide(mid), y));
 }
 
 // The segment that a block works on.
@@ -85,7 +98,7 @@ __device__ __forceinline__ Segment segment_of(const FadeArgs &a, int tile, int l
 }
 
 // The runs of one launch, one to a plane of the grid: those of the gradient are independent, and together fill the SMs where one alone has as
-// many blocks as heads and columns (6 sequences of up to 4096 tokens, 16 heads: one after another 274 us, together 231).
+// many blocks as heads and columns (6 sequences of up to 4096 tokens, 16 heads: one after another 274 us, together 231; with two parts of Z everywhere).
 constexpr int MAX_RUNS = 3;
 struct FadeRuns {
     FadeArgs run[MAX_RUNS];
@@ -100,19 +113,20 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     using namespace fade;
     using namespace tc;
     using Sh = Shape<DX, STATE>;
-    constexpr int STAGES = Sh::STAGES, BUFS = Sh::BUFS;
+    constexpr int STAGES = Sh::STAGES, BUFS = Sh::BUFS, U_COLS = 256;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
-    unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_parts = S_op + Sh::S_BYTES,      // Z_parts: [buffer][2]
-                  *out_rows = Z_parts + 2 * BUFS * Sh::Z_BYTES;
-    float *table = (float *)(out_rows + Sh::OUT_BYTES);              // in_scale w^m on one side of the middle, zeros on the other
+    unsigned char *stages = smem, *S_op = stages + STAGES * Sh::STAGE, *Z_parts = S_op + Sh::S_BYTES,      // Z_parts: [buffer][3]
+                  *out_rows = Z_parts + (3 * BUFS - 1) * Sh::Z_BYTES;                   // in the place of the third part
+    float *table = (float *)(out_rows + Sh::Z_BYTES);              // in_scale w^m on one side of the middle, zeros on the other
     uint64_t *bars = (uint64_t *)(table + 2 * TILE);
     uint64_t *xy_full = bars, *z_full = xy_full + STAGES, *xy_empty = z_full + STAGES, *z_empty = xy_empty + STAGES, *sc_full = z_empty + STAGES, *p_full = sc_full + 2, *o_full = p_full + 2, *o_free = o_full + 1,
-             *z_ready = o_free + 1, *s_ready = z_ready + BUFS, *u_full = s_ready + 1, *u_free = u_full + BUFS, *xs_done = u_free + 1;
+             *z_ready = o_free + 1, *s_ready = z_ready + BUFS, *u_full = s_ready + 1, *u_free = u_full + BUFS, *xs_done = u_free + BUFS;
     uint32_t *tmem_slot = (uint32_t *)(xs_done + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
-    const bool back = a.backwards;
+    // the state that the caller gets takes every weighted value as three bf16 numbers, one that only meets bf16 tables as two
+    const bool back = a.backwards, third = STATE ? a.last != nullptr : a.last && !a.states;
     const int slabs = (a.dz + ZC - 1) / ZC, slab = blockIdx.x % slabs, tile = blockIdx.x / slabs;
 
     pdl_wait();
@@ -125,8 +139,8 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     }
     const Segment seg = segment_of(a, tile, lane);
     if (seg.seq < 0) return;
-    // nobody needs the sum of the segment that comes last
-    if (STATE && seg.index == (back ? 0 : seg.count - 1)) return;
+    // the sum of the segment that comes last only goes to the caller
+    if (STATE && !a.last && seg.index == (back ? 0 : seg.count - 1)) return;
     const int n = (seg.len + TILE - 1) / TILE;
     const float decay = a.log_decay[h], a2 = decay * LOG2E;
     auto chunk_of = [&](int i) { return back ? n - 1 - i : i; };
@@ -142,7 +156,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             mbar_init(&xy_full[s], 1);
             mbar_init(&z_full[s], 1);
             mbar_init(&xy_empty[s], 1);
-            mbar_init(&z_empty[s], 1);
+            mbar_init(&z_empty[s], STATE ? 4 : 1);
         }
         mbar_init(&sc_full[0], 1);
         mbar_init(&sc_full[1], 1);
@@ -154,9 +168,9 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
         for (int b = 0; b < BUFS; ++b) {
             mbar_init(&z_ready[b], 4);
             mbar_init(&u_full[b], 1);
+            mbar_init(&u_free[b], 4);
         }
         mbar_init(s_ready, 4);
-        mbar_init(u_free, 4);
         mbar_init(xs_done, 1);
         *abort_flag = 0;
         fence_barrier_init();
@@ -168,7 +182,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0), pz_col = tmem + 2 * TILE, xs_col = pz_col + ZC, u_col = xs_col + ZC;
+    const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0), pz_col = tmem + 2 * TILE, xs_col = pz_col + ZC, u_col = STATE ? tmem : xs_col + ZC;
     pdl_trigger();
 
     if (warp == 12) {
@@ -186,13 +200,19 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
                 const int s = i % STAGES, row = seg.first + chunk_of(i) * TILE;
                 const uint32_t parity = (uint32_t)((i / STAGES + 1) & 1);
                 unsigned char *st = stages + s * Sh::STAGE;
+                auto load_z = [&] {
+                    if (!mbar_wait(&z_empty[s], parity, abort_flag, a.status, 15)) return false;
+                    mbar_expect_tx(&z_full[s], Sh::Z_BYTES);
+                    tma_load_3d(st + Sh::X_BYTES, &a.zmap, &z_full[s], slab * ZC, h, row);
+                    return true;
+                };
+                // without scores Z is given back as soon as it is weighted, before Y
+                if (STATE && !load_z()) break;
                 if (!mbar_wait(&xy_empty[s], parity, abort_flag, a.status, 1)) break;
                 mbar_expect_tx(&xy_full[s], Sh::STAGE - Sh::Z_BYTES);
                 load_tile<DX>(st, &a.ymap, &xy_full[s], h, row);
                 if (!STATE) load_tile<DX>(st + Sh::X_BYTES + Sh::Z_BYTES, &a.xmap, &xy_full[s], h, row);
-                if (!mbar_wait(&z_empty[s], parity, abort_flag, a.status, 15)) break;
-                mbar_expect_tx(&z_full[s], Sh::Z_BYTES);
-                tma_load_3d(st + Sh::X_BYTES, &a.zmap, &z_full[s], slab * ZC, h, row);
+                if (!STATE && !load_z()) break;
                 ahead(i + STAGES);
             }
         }
@@ -200,7 +220,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     } else if (warp == 13) {
         {
             const bool lead = elect_one();
-            const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), u_idesc = make_idesc(1, 1, 1, TILE, 2 * ZC);
+            const uint32_t sc_idesc = make_idesc(1, 0, 0, TILE, TILE), pz_idesc = make_idesc(1, 0, 1, TILE, ZC), third_idesc = make_idesc(1, 1, 1, TILE, ZC);
             bool ok = true;
             // U and XS of a chunk, scores of the next, PZ of the chunk: each product has one place in the code, for the instruction cache
             for (int i = -1; i < n && ok; ++i) {
@@ -208,18 +228,24 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
                 if (i >= 0) {
                     if (STATE) ok = warp_wait(&xy_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 12);
                     if (ok) ok = warp_wait(&z_ready[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 3);
-                    if (ok && i > 0) ok = warp_wait(u_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 13);
+                    if (ok && i >= BUFS) ok = warp_wait(&u_free[i % BUFS], (uint32_t)((i / BUFS - 1) & 1), abort_flag, a.status, 13);
                     if (!ok) break;
                     tc_fence_after();
-                    // Y^T times both parts side by side: the tile of Y is read once
-                    const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_parts + (i % BUFS) * 2 * Sh::Z_BYTES), SLAB, 1024);
+                    // Y^T times all parts side by side: the tile of Y is read once.  Beside scores there is tensor memory for two, and the third is added
+                    // to the second.
+                    const uint32_t u_idesc = make_idesc(1, 1, 1, TILE, STATE && third ? 3 * ZC : 2 * ZC);
+                    const uint64_t y = make_smem_desc(smem_u32(Y), SLAB, 1024), z = make_smem_desc(smem_u32(Z_parts + (i % BUFS) * 3 * Sh::Z_BYTES), SLAB, 1024);
 #pragma unroll
                     for (int k = 0; k < TILE / 16; ++k)
-                        mma_ss(lead, u_col, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k > 0);
+                        mma_ss(lead, u_col + (i % BUFS) * U_COLS, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)(k * 2048 >> 4), u_idesc, k > 0);
+                    if (!STATE && third) {
+#pragma unroll
+                        for (int k = 0; k < TILE / 16; ++k)
+                            mma_ss(lead, u_col + ZC, y + (uint64_t)(k * 2048 >> 4), z + (uint64_t)((2 * SLAB + k * 2048) >> 4), third_idesc, true);
+                    }
                     commit(lead, &u_full[i % BUFS]);
                     if (STATE) {
                         commit(lead, &xy_empty[i % STAGES]);
-                        commit(lead, &z_empty[i % STAGES]);
                         continue;
                     }
                     if (i > 0) ok = warp_wait(o_free, (uint32_t)((i - 1) & 1), abort_flag, a.status, 4);
@@ -255,9 +281,9 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             }
         }
         __syncwarp();
-    } else if (warp < 4) {
+    } else if (warp < 4 && !STATE) {
         // thread: token t of a chunk.  Scores to weights.
-        if (!STATE) {
+        {
             const uint32_t lanes = (uint32_t)(warp * 32) << 16;
             bool ok = true;
             const float *w = table + TILE + threadIdx.x;
@@ -295,17 +321,17 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             }
         }
     } else if (warp < 8) {
-        // thread: token t of a chunk.  Z times its weights, in two parts.
-        const int t = threadIdx.x - 128, swz = t & 7;
+        // thread: token t of a chunk.  Z times its weights, in three parts; where there are no scores warps 0..3 take every other chunk.
+        const int t = threadIdx.x & 127, swz = t & 7;
         bool ok = true;
-        for (int i = 0; i < n; ++i) {
+        for (int i = STATE ? warp >> 2 : 0; i < n; i += STATE ? 2 : 1) {
             const int L = tokens_of(i);
             const float beta = t < L ? a.in_scale * power(a2, back ? t + 1 : L - 1 - t) : 0.f;
             ok = __all_sync(~0u, mbar_wait(&z_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 10));
             if (ok && L < TILE) ok = __all_sync(~0u, mbar_wait(&xy_full[i % STAGES], (uint32_t)((i / STAGES) & 1), abort_flag, a.status, 17));
             if (ok && i >= BUFS) ok = __all_sync(~0u, mbar_wait(&u_full[i % BUFS], (uint32_t)((i / BUFS - 1) & 1), abort_flag, a.status, 9));
             if (!ok) break;
-            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *Z_hi = Z_parts + (i % BUFS) * 2 * Sh::Z_BYTES, *Z_lo = Z_hi + Sh::Z_BYTES;
+            unsigned char *Y = stages + (i % STAGES) * Sh::STAGE, *Z = Y + Sh::X_BYTES, *Z_hi = Z_parts + (i % BUFS) * 3 * Sh::Z_BYTES;
             if (t >= L) {                              // rows behind the sequence: they meet weights of 0
 #pragma unroll 1
                 for (int j = 0; j < 8; ++j) {
@@ -320,21 +346,39 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
                 uint4 v[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const uint4 *>(Z + t * 128 + (((b * 4 + j) ^ swz) << 4));
+                if (third) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int o = t * 128 + (((b * 4 + j) ^ swz) << 4);
-                    uint4 hi, lo;
-                    times(b_hi, b_lo, v[j].x, hi.x, lo.x);
-                    times(b_hi, b_lo, v[j].y, hi.y, lo.y);
-                    times(b_hi, b_lo, v[j].z, hi.z, lo.z);
-                    times(b_hi, b_lo, v[j].w, hi.w, lo.w);
-                    *reinterpret_cast<uint4 *>(Z_hi + o) = hi;
-                    *reinterpret_cast<uint4 *>(Z_lo + o) = lo;
+                    for (int j = 0; j < 4; ++j) {
+                        const int o = t * 128 + (((b * 4 + j) ^ swz) << 4);
+                        uint4 hi, mid, lo;
+                        times(beta, v[j].x, hi.x, mid.x, lo.x);
+                        times(beta, v[j].y, hi.y, mid.y, lo.y);
+                        times(beta, v[j].z, hi.z, mid.z, lo.z);
+                        times(beta, v[j].w, hi.w, mid.w, lo.w);
+                        *reinterpret_cast<uint4 *>(Z_hi + o) = hi;
+                        *reinterpret_cast<uint4 *>(Z_hi + Sh::Z_BYTES + o) = mid;
+                        *reinterpret_cast<uint4 *>(Z_hi + 2 * Sh::Z_BYTES + o) = lo;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int o = t * 128 + (((b * 4 + j) ^ swz) << 4);
+                        uint4 hi, lo;
+                        times(b_hi, b_lo, v[j].x, hi.x, lo.x);
+                        times(b_hi, b_lo, v[j].y, hi.y, lo.y);
+                        times(b_hi, b_lo, v[j].z, hi.z, lo.z);
+                        times(b_hi, b_lo, v[j].w, hi.w, lo.w);
+                        *reinterpret_cast<uint4 *>(Z_hi + o) = hi;
+                        *reinterpret_cast<uint4 *>(Z_hi + Sh::Z_BYTES + o) = lo;
+                    }
                 }
             }
             fence_proxy_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&z_ready[i % BUFS]);
+            if (lane == 0) {
+                mbar_arrive(&z_ready[i % BUFS]);
+                if (STATE) mbar_arrive(&z_empty[i % STAGES]);
+            }
         }
     } else {
         // thread: row r of S, and token r of a chunk's out
@@ -363,43 +407,86 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             ok = __all_sync(~0u, mbar_wait(o_full, (uint32_t)(i & 1), abort_flag, a.status, 7));
             if (!ok) return;
             tc_fence_after();
-            // a warp's 32 rows go through shared memory and out in one copy; rows at a sequence's end are written one by one
-            if (lane == 0) tma_store_wait_read();
-            __syncwarp();
+            if (!third) {
+                // a warp's 32 rows go through shared memory and out in one copy; rows at a sequence's end are written one by one
+                if (lane == 0) tma_store_wait_read();
+                __syncwarp();
 #pragma unroll 1
-            for (int b = 0; b < 4; ++b) {
-                uint32_t pz[16], xs[16];
-                tmem_ld_32x16(pz_col + lanes + b * 16, pz);
-                tmem_ld_32x16(xs_col + lanes + b * 16, xs);
-                tmem_ld_wait();
-                if (b == 3) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(o_free);
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint32_t u[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int c = j * 8 + 2 * k;
-                        u[k] = pack_bf16(fma(pair(alpha, alpha), pair(xs[c], xs[c + 1]), mul(pair(a.out_scale, a.out_scale), pair(pz[c], pz[c + 1]))));
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t pz[16], xs[16];
+                    tmem_ld_32x16(pz_col + lanes + b * 16, pz);
+                    tmem_ld_32x16(xs_col + lanes + b * 16, xs);
+                    tmem_ld_wait();
+                    if (b == 3) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(o_free);
                     }
-                    *reinterpret_cast<uint4 *>(out_rows + r * 128 + (((b * 2 + j) ^ swz) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int c = j * 8 + 2 * k;
+                            u[k] = pack_bf16(fma(pair(alpha, alpha), pair(xs[c], xs[c + 1]), mul(pair(a.out_scale, a.out_scale), pair(pz[c], pz[c + 1]))));
+                        }
+                        *reinterpret_cast<uint4 *>(out_rows + r * 128 + (((b * 2 + j) ^ swz) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
                 }
-            }
-            const int row = seg.first + first + w * 32;
-            if (w * 32 + 32 <= L) {
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) tma_store_3d(&a.outmap, out_rows + w * 4096, slab * ZC, h, row);
+                const int row = seg.first + first + w * 32;
+                if (w * 32 + 32 <= L) {
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) tma_store_3d(&a.outmap, out_rows + w * 4096, slab * ZC, h, row);
+                } else {
+                    __syncwarp();
+                    const int c = lane & 7;
+                    for (int k = lane / 8; w * 32 + k < L; k += 4)
+                        if (slab * ZC + c * 8 < a.dz)
+                            *reinterpret_cast<uint4 *>(a.out + ((int64_t)(row + k) * a.heads + h) * a.dz + slab * ZC + c * 8) =
+                                *reinterpret_cast<const uint4 *>(out_rows + (w * 32 + k) * 128 + ((c ^ (k & 7)) << 4));
+                }
             } else {
-                __syncwarp();
-                const int c = lane & 7;
-                for (int k = lane / 8; w * 32 + k < L; k += 4)
-                    if (slab * ZC + c * 8 < a.dz)
-                        *reinterpret_cast<uint4 *>(a.out + ((int64_t)(row + k) * a.heads + h) * a.dz + slab * ZC + c * 8) =
-                            *reinterpret_cast<const uint4 *>(out_rows + (w * 32 + k) * 128 + ((c ^ (k & 7)) << 4));
+                // Four lanes exchange their rows' pieces, so that they write 64 bytes of a row side by side; one by one every piece of 16 bytes
+                // took a cycle of the store (65536 tokens of 16 heads 300 us in this kernel, so 271).
+                bf16 *to = a.out + ((int64_t)(seg.first + first + w * 32 + (lane & ~3)) * a.heads + h) * a.dz + slab * ZC + (lane & 3) * 8;
+                const int64_t stride = (int64_t)a.heads * a.dz;
+                const int rows = L - (w * 32 + (lane & ~3)), cols = a.dz - slab * ZC - (lane & 3) * 8;
+#pragma unroll 1
+                for (int b = 0; b < 2; ++b) {
+                    uint32_t v[4][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t pz[16], xs[16];
+                        tmem_ld_32x16(pz_col + lanes + b * 32 + j * 16, pz);
+                        tmem_ld_32x16(xs_col + lanes + b * 32 + j * 16, xs);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            v[j * 2 + k / 4][k % 4] = pack_bf16(fma(pair(alpha, alpha), pair(xs[2 * k], xs[2 * k + 1]),
+                                                                    mul(pair(a.out_scale, a.out_scale), pair(pz[2 * k], pz[2 * k + 1]))));
+                    }
+                    if (b == 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(o_free);
+                    }
+#pragma unroll
+                    for (int s = 1; s < 4; s *= 2)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (!(k & s))
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const bool odd = lane & s;
+                                    const uint32_t got = __shfl_xor_sync(~0u, odd ? v[k][e] : v[k | s][e], s);
+                                    if (odd) v[k][e] = got;
+                                    else v[k | s][e] = got;
+                                }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (k < rows && b * 32 < cols) *reinterpret_cast<uint4 *>(to + k * stride + b * 32) = make_uint4(v[k][0], v[k][1], v[k][2], v[k][3]);
+                }
             }
         };
         for (int i = 0; i < n; ++i) {
@@ -423,24 +510,32 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             ok = __all_sync(~0u, mbar_wait(&u_full[i % BUFS], (uint32_t)((i / BUFS) & 1), abort_flag, a.status, 14));
             if (!ok) break;
             tc_fence_after();
+            const uint32_t u_addr = u_col + lanes + (i % BUFS) * U_COLS;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t hi[16], lo[16];
-                tmem_ld_32x16(u_col + lanes + j * 16, hi);
-                tmem_ld_32x16(u_col + lanes + ZC + j * 16, lo);
+                tmem_ld_32x16(u_addr + j * 16, hi);
+                tmem_ld_32x16(u_addr + ZC + j * 16, lo);
                 tmem_ld_wait();
+                if (STATE && third) {
+                    uint32_t more[16];
+                    tmem_ld_32x16(u_addr + 2 * ZC + j * 16, more);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) lo[c] = __float_as_uint(__uint_as_float(lo[c]) + __uint_as_float(more[c]));
+                }
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
                     S[j * 8 + c] = fma(pair(keep, keep), S[j * 8 + c], add(pair(hi[2 * c], hi[2 * c + 1]), pair(lo[2 * c], lo[2 * c + 1])));
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(u_free);
+            if (lane == 0) mbar_arrive(&u_free[i % BUFS]);
         }
         if (!STATE && ok && n > 0) write(n - 1);
         if (!STATE && lane == 0) tma_store_wait();
         const bool end = seg.index == (back ? 0 : seg.count - 1);
-        float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && a.last ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
+        float *to = STATE ? a.states + ((int64_t)tile * a.heads + h) * plane : end && third ? a.last + ((int64_t)seg.seq * a.heads + h) * plane : nullptr;
         if (ok && to && row) {
 #pragma unroll
             for (int c = 0; c < 64; c += 4)
@@ -458,7 +553,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     }
 }
 
-// The segments' own sums become the states that enter the segments; a thread owns four elements of a head's state.
+// The segments' own sums become the states that enter the segments and the one behind the last; a thread owns four elements of a head's state.
 __global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__ FadeRuns runs, int parts)
 {
     const FadeArgs &a = runs.run[blockIdx.z / parts];
@@ -482,7 +577,7 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
             const int i = i0 + j, k = a.backwards ? seg.count - 1 - i : i;
-            own[j] = i + 1 < seg.count ? *reinterpret_cast<const float4 *>(states + k * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+            own[j] = i < seg.count && (a.last || i + 1 < seg.count) ? *reinterpret_cast<const float4 *>(states + k * step) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
@@ -493,12 +588,13 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__
             s = make_float4(fmaf(f, s.x, own[j].x), fmaf(f, s.y, own[j].y), fmaf(f, s.z, own[j].z), fmaf(f, s.w, own[j].w));
         }
     }
+    if (a.last) *reinterpret_cast<float4 *>(a.last + ((int64_t)seg.seq * a.heads + h) * plane + e) = s;
 }
 
 // Chunks of a segment, 0: whole sequences.  Whole, a call takes the longest sequence's chunks one after another, here estimated as twice the mean
 // (the lengths are on the device); in segments 1.6 times its share of all chunks, as the states are summed first, and the time of some 12
 // chunks for two launches more.  Segments are so long that two come to every SM.
-// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 358 / 274; 9 of up to 1333, 8 heads 26 / 22.
+// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 358 / 274; 9 of up to 1333, 8 heads 26 / 22 (two parts of Z everywhere).
 static int segment_chunks(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
     const int64_t sms = sm_count_or_default(), blocks = heads * ((d + fade::ZC - 1) / fade::ZC), wanted = 2 * sms / blocks;
@@ -658,11 +754,11 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
     a.out = (bf16 *)dv;
     if (a.states) a.states += states_floats(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv);
     dv_run = a;
+    dv_run.last = dstate_in;
     if (a.states) {
         if ((rc = run_fades<true>(r, 2, s)) != ST_OK) return rc;
         dq_run.check = 0;
     }
-    dv_run.last = dstate_in;
     dq_run.x = O;
     dq_run.y = V;
     dq_run.z = K;
