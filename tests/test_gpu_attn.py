@@ -396,6 +396,7 @@ DECAYS = [
     ([1100], 1, 128, 40, [-0.003], False),
     ([16] * 30, 2, 64, 64, [-0.05, -0.7], True),
     ([6000], 1, 128, 128, [-0.0005], True),
+    ([5000, 0, 1, 900], 1, 64, 72, [-0.01], True),                 # in segments, one sequence without any token
 ]
 
 
@@ -434,6 +435,36 @@ def test_decay_gradient_against_the_definition(lens, H, d, dv, a, state):
             near(g[x:y], w, tol, name)
         if state:
             near(got[3][b], *want[3], "dstate")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_decay_states_have_the_precision_of_fp32(d):
+    """Sequences of two tokens: a state is the sum of two products, nothing cancels in the sum of their absolute values.  Off by at most
+    2^-22 of a term (exp2f: two units) and 2^-23 (its rounded argument, |a2| < 1, and the product), 2^-25 (what three parts leave) and
+    2^-23 for each of up to six summands on the tensor cores: below 2^-19."""
+    H, n = 2, 40
+    q, k, v, do = (normal(170 + i, 2 * n, H, d) for i in range(4))
+    a = torch.tensor([-0.3, -0.6], device="cuda")
+    at = offsets([2] * n)
+    w = torch.exp(a.double())[None, :, None, None]
+    zero = torch.zeros(n, H, d, d, device="cuda")
+    _, last = st.st_attn_decay(q, k, v, a, at)
+    dstate = st.st_attn_decay_grad(q, k, v, a, do, at, zero, None, scale=1.0)[3]
+    ok()
+    for got, x, y, first, second in ((last, k, v, w, 1.0), (dstate, q, do, w, w * w)):
+        t = torch.einsum("nthd,nthe->nthde", x.double().view(n, 2, H, d), y.double().view(n, 2, H, d))
+        want, size = first * t[:, 0] + second * t[:, 1], first * t[:, 0].abs() + second * t[:, 1].abs()
+        assert bool(((got.double() - want).abs() <= size * 2.0 ** -19).all())
+
+
+@pytest.mark.parametrize("lens,H", [([300, 0, 77], 2), ([5000, 0, 900], 1)])
+def test_decay_state_in_place(lens, H):
+    q, k, v, a, s, at = decay_inputs(180, lens, H, 64, 64, [-0.02] * H, True)
+    want = st.st_attn_decay(q, k, v, a, at, s)
+    same = s.clone()
+    got = st.st_attn_decay(q, k, v, a, at, same, state_out=same)
+    ok()
+    assert got[1] is same and torch.equal(got[0], want[0]) and torch.equal(same, want[1])
 
 
 def test_decay_gradient_against_differences():
