@@ -594,7 +594,7 @@ __global__ void __launch_bounds__(256) fade_carry_kernel(const __grid_constant__
 // Chunks of a segment, 0: whole sequences.  Whole, a call takes the longest sequence's chunks one after another, here estimated as twice the mean
 // (the lengths are on the device); in segments 1.6 times its share of all chunks, as the states are summed first, and the time of some 12
 // chunks for two launches more.  Segments are so long that two come to every SM.
-// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 358 / 274; 9 of up to 1333, 8 heads 26 / 22 (two parts of Z everywhere).
+// us, in segments / whole: 6 sequences of up to 4096 tokens, 16 heads, with gradient 355 / 256; 9 of up to 1333, 8 heads of 64 28 / 27; 2 of up to 4000 28 / 64.
 static int segment_chunks(int64_t n, int64_t nseq, int64_t heads, int64_t d)
 {
     const int64_t sms = sm_count_or_default(), blocks = heads * ((d + fade::ZC - 1) / fade::ZC), wanted = 2 * sms / blocks;
