@@ -46,6 +46,7 @@ struct FadeArgs {
     unsigned *status;
     int check;                        // look the offsets over and set the status: the call's first kernel
     int chunks;                       // of a segment
+    int tiles;                        // segments that the grid and the states have room for
     float *states;                    // [segment][heads][dx][dz], or null: no sequence has more than one segment
 };
 
@@ -127,7 +128,8 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
     // the state that the caller gets takes every weighted value as three bf16 numbers, one that only meets bf16 tables as two
     const bool back = a.backwards, third = STATE ? a.last != nullptr : a.last && !a.states;
-    const int slabs = (a.dz + ZC - 1) / ZC, slab = blockIdx.x % slabs, tile = blockIdx.x / slabs;
+    const SlabOf place = slab_of(blockIdx.x, (a.dz + ZC - 1) / ZC, a.tiles);
+    const int slab = place.slab, tile = place.tile;
 
     pdl_wait();
     if (a.check && blockIdx.x == 0 && blockIdx.y == 0) {
@@ -137,6 +139,7 @@ fade_kernel(const __grid_constant__ FadeRuns runs)
             a.status[kWsDetailWord] = 0u;
         }
     }
+    if (tile < 0) return;
     const Segment seg = segment_of(a, tile, lane);
     if (seg.seq < 0) return;
     // the sum of the segment that comes last only goes to the caller
@@ -610,10 +613,9 @@ static st_status launch_fade(const FadeRuns &r, int count, cudaStream_t stream)
     const size_t smem = fade::Shape<DX, STATE>::SMEM;
     if (!ensure_dynamic_smem(fade_kernel<DX, STATE>, smem)) return ST_ERR_CUDA;
     const FadeArgs &a = r.run[0];
-    const int64_t tiles = most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
     int slabs = 1;
     for (int i = 0; i < count; ++i) slabs = std::max(slabs, (r.run[i].dz + fade::ZC - 1) / fade::ZC);
-    return launch(fade_kernel<DX, STATE>, dim3((unsigned)(tiles * slabs), (unsigned)a.heads, (unsigned)count), fade::THREADS, smem, stream, r);
+    return launch(fade_kernel<DX, STATE>, dim3((unsigned)((int64_t)a.tiles * slabs), (unsigned)a.heads, (unsigned)count), fade::THREADS, smem, stream, r);
 }
 
 // `count` runs over the same tokens at once: their states that enter the segments (of y (x) z as it is kept: not transposed), or all of them.
@@ -632,7 +634,7 @@ static st_status run_fades(FadeRuns &r, int count, cudaStream_t stream)
     if (!STATE || rc != ST_OK) return rc;
     const FadeArgs &a = r.run[0];
     const int parts = (a.dx * a.dz + 1023) / 1024;
-    return launch(fade_carry_kernel, dim3((unsigned)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE), (unsigned)a.heads, (unsigned)(parts * count)), 256, 0, stream, r, parts);
+    return launch(fade_carry_kernel, dim3((unsigned)a.tiles, (unsigned)a.heads, (unsigned)(parts * count)), 256, 0, stream, r, parts);
 }
 
 // The states of the segments of one run.
@@ -664,6 +666,7 @@ static FadeArgs fade_args(const st_tokens *t, const float *log_decay, const int3
     a.offsets = offsets;
     a.nseq = (int)t->nseq;
     a.n = (int)t->nq;
+    a.tiles = (int)most_tiles(a.n, a.nseq, (int64_t)a.chunks * TILE);
     a.heads = (int)t->heads;
     a.in_scale = a.out_scale = 1.f;
     return a;

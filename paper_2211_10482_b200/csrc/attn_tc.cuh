@@ -2,6 +2,7 @@
 // tiles of keys a tile of queries sees.
 #pragma once
 #include "attn_common.cuh"
+#include "attn_index.cuh"
 #include "tc_common.cuh"
 
 namespace st {
@@ -223,10 +224,6 @@ __device__ __forceinline__ TileOf tile_of(const int *offsets, int nseq, int n, i
     }
     return {-1, 0};
 }
-// A table of n rows in nseq sequences has at most this many tiles.
-#endif
-inline int64_t most_tiles(int64_t n, int64_t nseq, int64_t rows) { return n / rows + nseq; }
-#if defined(__CUDACC__)
 
 // Which pairs of positions the window and the first columns leave.
 struct Mask {

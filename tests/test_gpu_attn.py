@@ -268,6 +268,26 @@ def test_offsets_that_name_the_same_rows_again_stay_within_the_workspace():
     assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
 
 
+@pytest.mark.parametrize("d,dv", [(64, 96), (96, 64), (72, 64), (64, 72)])
+def test_offsets_that_name_the_same_rows_again_with_states_of_two_widths(d, dv):
+    """Rows of queries and of values in different numbers of 64 columns: the runs of the gradient have grids of different widths.  (What each
+    block may reach is tested on the CPU.)"""
+    n = 128 * 300
+    q, k, v, do = normal(76, n, 1, d), normal(77, n, 1, d), normal(78, n, 1, dv), normal(79, n, 1, dv)
+    at = torch.tensor([0, n, 0, n, 0, n, 0, n], dtype=torch.int32, device="cuda")
+    a = -torch.ones(1, device="cuda")
+    assert st.st_workspace_bytes(st.ST_OP_ATTN_DECAY_GRAD, n, 4, 1, max(d, dv)) > 256
+    st.st_attn_decay(q, k, v, a, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    st.st_attn_decay_grad(q, k, v, a, do, at)
+    assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+    # the same rows as one sequence, in segments as well
+    one_at = offsets([n])
+    got, want = st.st_attn_decay_grad(q, k, v, a, do, one_at), st.st_attn_decay_grad(q, k, v, a, do)
+    ok()
+    assert all(torch.equal(x, y) for x, y in zip(got[:3], want[:3]))
+
+
 # --------------------------------------------------------------------------------- window: step
 
 STEPS = [
