@@ -388,6 +388,42 @@ def test_step_leaves_out_bad_pages_and_reports_them():
     ok()
 
 
+def test_step_reports_are_ordered_by_the_stream_and_not_by_time():
+    """The status is cleared ahead of all blocks that may report, so that a report is neither lost nor has to wait: 3000 sequences with
+    bad pages, seven turns of blocks, take no longer than with good ones, and one bad sequence is seen wherever it stands."""
+    n, d, page = 3000, 64, 16
+    q, k, v = normal(105, n, 1, d), normal(106, n, 1, d), normal(107, n, 1, d)
+    kp, vp = normal(108, 3 * n, page, 1, d), normal(109, 3 * n, page, 1, d)
+    lens = torch.full((n,), 40, dtype=torch.int32, device="cuda")
+    good = torch.arange(3 * n, dtype=torch.int32, device="cuda").view(n, 3)
+    bad = torch.full_like(good, -1)
+    out, ws = torch.empty_like(q), torch.empty(256, dtype=torch.uint8, device="cuda")
+
+    def timed(table):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        for _ in range(5):
+            st.st_attn_window_step(q, k, v, kp, vp, table, lens, 100, 4, out=out, ws=ws)
+        end.record()
+        end.synchronize()
+        return begin.elapsed_time(end)
+
+    for _ in range(3):
+        fine = timed(good)
+        assert st.st_check_status(ws) == st.ST_OK
+        wrong = timed(bad)
+        assert st.st_check_status(ws) == st.ST_ERR_DEV_BOUNDS
+    assert wrong < 5 * fine, (wrong, fine)
+    for b in (0, 1, n // 2, n - 1):
+        table = good.clone()
+        table[b, 1] = -1
+        for _ in range(5):
+            st.st_attn_window_step(q, k, v, kp, vp, table, lens, 100, 4, out=out, ws=ws)
+            assert st.st_check_status(ws) == st.ST_ERR_DEV_BOUNDS
+        st.st_attn_window_step(q, k, v, kp, vp, good, lens, 100, 4, out=out, ws=ws)
+        assert st.st_check_status(ws) == st.ST_OK
+
+
 def test_step_on_a_cache_whose_offsets_pass_32_bits():
     page, Hk, d = 64, 8, 128
     pages = (1 << 31) // (page * Hk * d) + 40                          # elements: beyond 2^31
