@@ -332,6 +332,7 @@ typedef struct {
  *     x[t,s] = scale q[t].k[s];  lse[t] = log sum_s exp x[t,s];  out[t] = sum_s exp(x[t,s] - lse[t]) v[s]
  * Positions count within a sequence; where it has more keys (Lk, k_offsets) than queries (Lq, q_offsets), the
  * queries are its last tokens: query i stands at t = Lk - Lq + i.  A query that sees nothing (t < 0) gets out = 0 and
+ * lse = -inf.  A visible score that is NaN or +inf makes out and lse of its query NaN, and one whose visible scores are all -inf has out = NaN and
  * lse = -inf.  q: [nq, heads, d]; k, v: [nk, kv_heads, d]; dv must equal d.  window >= 1 (as large as you like: the whole
  * triangle), sinks >= 0, scale > 0.  out: bf16 [nq, heads, d]; lse: fp32 [nq, heads].  Scores, maxima and sums are fp32; the weights are
  * rounded to bf16 (relative to the row's largest) for the product with v. */

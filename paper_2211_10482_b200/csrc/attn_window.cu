@@ -310,7 +310,8 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         if (ok) {
             tc_fence_after();
             const int wr = (warp & 3) * 32, first = w * TILE + wr, row = rq.first + i0 + first;      // this warp's rows
-            const bool seen = l > 0.f, all = first + 32 <= left;
+            // a query from position 0 on sees itself at least: where its sum is NaN (a score is, or is +inf) or 0 (all scores are -inf), so is the row NaN
+            const bool seen = t >= 0, all = first + 32 <= left;
             const Pair inv = pair(seen ? 1.f / l : 0.f, seen ? 1.f / l : 0.f);
             if (first + lane < left) a.lse[(int64_t)(row + lane) * a.heads + h] = seen ? (m * c + log2f(l)) * LN2 : -INFINITY;
             // Rows go out through the shared memory of the queries, which no product reads any more: a warp's 32 rows in one copy for each

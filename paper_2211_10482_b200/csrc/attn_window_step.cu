@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(WARPS * 32) window_step_kernel(const StepArgs 
             m[r] = weight(m[r], all);
             s = fmaf(m[r], l[r], s);
         }
-        const float inv = s > 0.f ? 1.f / s : 0.f;
+        const float inv = len > 0 ? 1.f / s : 0.f;         // a sum of 0 (all scores are -inf) or NaN gives NaN
 #pragma unroll
         for (int r = 0; r < MAX_SPLITS; ++r) share[r * HEADS + threadIdx.x] = m[r] * inv;
     }

@@ -202,6 +202,50 @@ def test_large_scores_do_not_overflow():
     near(out, o, ot + 1.1e-2 * (p @ V.abs()).transpose(0, 1), "out")
 
 
+@pytest.mark.parametrize("what", ["q nan", "k nan", "k inf", "all -inf", "overflow"])
+@pytest.mark.parametrize("window,sinks", [(50, 3), (300, 0), (20, 140)])
+def test_scores_that_are_not_finite_are_not_taken_for_none(what, window, sinks):
+    """A query whose visible scores hold NaN or +inf, or are all -inf, gets NaN as by the definition, and every other one its row;
+    the gradient of such a query is NaN.  The same for a single token.  (The other rows are held against the definition and not bit for bit
+    against a call without: the reference that weights are relative to moves for the 32 rows of a warp together, and a weight is
+    rounded relative to it, by half a step at most wherever it lies.)"""
+    n, H, d, bad = 300, 2, 64, 140
+    q, k, v, do = (normal(170 + i, n, H, d) for i in range(4))
+    t = torch.arange(n, device="cuda")
+    sees_bad = ref.visible(n, n, window, sinks, "cuda")[:, bad]
+    if what == "q nan":
+        put, at, value, rows = q, (bad, 0, 5), math.nan, t == bad
+    elif what == "k nan":
+        put, at, value, rows = k, (bad, 0, 7), math.nan, sees_bad
+    elif what == "k inf":
+        q[:, 0, 9] = q[:, 0, 9].abs() + 1
+        put, at, value, rows = k, (bad, 0, 9), math.inf, sees_bad
+    elif what == "all -inf":
+        q[bad, 0], k[:, 0, 0] = 0.0, k[:, 0, 0].abs() + 1
+        put, at, value, rows = q, (bad, 0, 0), -math.inf, t == bad
+    else:                                                  # finite values whose products leave fp32
+        q[:, 0, 9], k[:, 0, 9] = 2.0 ** 100, 0.0
+        put, at, value, rows = k, (bad, 0, 9), 2.0 ** 100, sees_bad
+    want, wl, tol, lt = ref.window(q, k, v, window, sinks)
+    put[at] = value
+    out, lse = st.st_attn_window(q, k, v, window, sinks)
+    ok()
+    assert bool(out[rows, 0].isnan().all())
+    assert bool((lse[rows, 0] == -math.inf).all() if what == "all -inf" else lse[rows, 0].isnan().all())
+    for h, others in ((0, ~rows), (1, torch.ones_like(rows))):
+        near(out[others, h], want[others, h], tol[others, h], "out")
+        near(lse[others, h], wl[others, h], lt[others, h], "lse")
+    dq = st.st_attn_window_grad(q, k, v, out, lse, do, window, sinks)[0]
+    assert bool(dq[rows, 0].isnan().all()) and bool(torch.isfinite(dq[:, 1].float()).all())
+    for i in (bad, bad + 1, bad + 30, n - 1):
+        kp, vp = torch.zeros(1, 320, H, d, dtype=BF16, device="cuda"), torch.zeros(1, 320, H, d, dtype=BF16, device="cuda")
+        kp[0, :i], vp[0, :i] = k[:i], v[:i]
+        o = st.st_attn_window_step(q[i : i + 1], k[i : i + 1], v[i : i + 1], kp, vp, torch.zeros(1, 1, dtype=torch.int32, device="cuda"),
+                                   torch.tensor([i + 1], dtype=torch.int32, device="cuda"), window, sinks)
+        assert bool(o[0, 0].isnan().all()) == bool(rows[i]) and bool(torch.isfinite(o[0, 1].float()).all())
+    ok()
+
+
 def test_rows_of_no_sequence_are_neither_read_nor_written():
     """Rows before, between and behind the sequences hold NaN; so do the other sequences, one at a time."""
     lq, H, Hk, d = [70, 130, 200], 4, 2, 64
