@@ -388,7 +388,7 @@ st_status st_attn_decay_grad(const st_tokens *tokens, const void *q, const void 
                              float scale, void *dq, void *dk, void *dv, float *dstate_in, void *ws, size_t ws_bytes,
                              void *stream);
 
-/* st_attn_decay for one new token of every sequence (nq = nk = nseq), all arrays contiguous: state
+/* st_attn_decay for one new token of every sequence (nq = nk = nseq), all arrays contiguous (other strides: ST_ERR_SHAPE): state
  * ([nseq, heads, d, dv] fp32) is updated in place. */
 st_status st_attn_decay_step(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
                              float *state, float scale, void *out, void *stream);

@@ -69,6 +69,9 @@ extern "C" st_status st_attn_decay_step(const st_tokens *t, const void *q, const
     const st_status rc = check_tokens(t);
     if (rc != ST_OK) return rc;
     if (t->nq != t->nk || t->heads != t->kv_heads || t->nseq != t->nq) return ST_ERR_SHAPE;
+    // the kernel takes the tables as contiguous ones
+    auto contiguous = [t](int64_t cols, int64_t row, int64_t head) { return (t->heads == 1 || head == cols) && (t->nq == 1 || row == t->heads * cols); };
+    if (!contiguous(t->d, t->q_row, t->q_head) || !contiguous(t->d, t->k_row, t->k_head) || !contiguous(t->dv, t->v_row, t->v_head)) return ST_ERR_SHAPE;
     if (!q || !k || !v || !log_decay || !state || !out) return ST_ERR_NULL;
     if (t->nq > 65535) return ST_ERR_UNSUPPORTED;
     for (const void *p : {q, k, v, (const void *)log_decay, (const void *)state, (const void *)out})

@@ -114,6 +114,16 @@ def test_decay_refusals():
     assert decay_step(state=264) == st.ST_ERR_ALIGN
 
 
+@pytest.mark.parametrize("change", [dict(q_row=512), dict(k_row=264), dict(v_row=320), dict(q_head=128, q_row=512), dict(k_head=72, k_row=288), dict(v_head=6400, v_row=64),
+                                    dict(q_head=6400, q_row=64)])
+def test_a_step_of_the_decay_takes_contiguous_tables_only(change):
+    """Its kernel reads them as such: strided ones would be read in the wrong places."""
+    assert decay_step(tokens(nseq=100, **{**EVEN, **change})) == st.ST_ERR_SHAPE
+    # the stride of an extent of one is never used: these pass, as far as the next refusal
+    assert decay_step(tokens(nseq=1, nq=1, nk=1, **{**EVEN, "q_row": 7, "k_row": 9, "v_row": 11}), state=264) == st.ST_ERR_ALIGN
+    assert decay_step(tokens(nseq=100, heads=1, kv_heads=1, q_row=64, k_row=64, v_row=64, q_head=0, k_head=3, v_head=5), state=264) == st.ST_ERR_ALIGN
+
+
 def test_tensors_on_the_host_are_refused_by_name():
     x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     for f in (lambda: st.st_attn_window(x, x, x, 4), lambda: st.st_attn_window_grad(x, x, x, x, x, x, 4),
