@@ -1,6 +1,7 @@
 // What the attention calls share: checks of their arguments, and where the tokens of a sequence lie.
 #pragma once
 #include <cuda_bf16.h>
+#include "attn_index.cuh"
 #include "st_common.cuh"
 
 namespace st {
@@ -42,6 +43,27 @@ inline st_status check_tokens(const st_tokens *t)
 
 // The stride of an extent of one is never used; whatever was passed, it is a legal one.
 inline int64_t stride_of(int64_t extent, int64_t stride) { return extent == 1 ? 128 : stride; }
+
+// The tables of a call, for the check of its results: a result may not lie over an operand that is still read when it is written.
+struct Operand {
+    const void *p;
+    int64_t rows, heads, cols, row, head;
+    // whether `bytes` bytes of results at `to` lie over it; in_place: they may take its place as a whole, if it is contiguous
+    bool under(const void *to, int64_t bytes, bool in_place = false) const
+    {
+        const bool whole = to == p && bytes == rows * heads * cols * 2 && (heads == 1 || head == cols) && (rows == 1 || row == heads * cols);
+        return !(in_place && whole) && overlap((uint64_t)p, rows, heads, cols * 2, row * 2, head * 2, (uint64_t)to, bytes);
+    }
+};
+inline Operand q_of(const st_tokens *t, const void *q) { return {q, t->nq, t->heads, t->d, stride_of(t->nq, t->q_row), stride_of(t->heads, t->q_head)}; }
+inline Operand k_of(const st_tokens *t, const void *k) { return {k, t->nk, t->kv_heads, t->d, stride_of(t->nk, t->k_row), stride_of(t->kv_heads, t->k_head)}; }
+inline Operand v_of(const st_tokens *t, const void *v) { return {v, t->nk, t->kv_heads, t->dv, stride_of(t->nk, t->v_row), stride_of(t->kv_heads, t->v_head)}; }
+inline Operand dense_of(const void *p, int64_t rows, int64_t heads, int64_t cols) { return {p, rows, heads, cols, heads * cols, cols}; }
+// Two arrays without gaps; none where one is missing.
+inline bool arrays_meet(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
+{
+    return a && b && (uint64_t)a < (uint64_t)b + b_bytes && (uint64_t)b < (uint64_t)a + a_bytes;
+}
 
 // A window or a number of first columns: the whole of the longest sequence is as far as it goes.
 inline int clamp_int(int64_t x, int most = 1 << 29) { return x > most ? most : (int)x; }

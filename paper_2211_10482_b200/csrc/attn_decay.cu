@@ -703,6 +703,16 @@ st_status st_attn_decay(const st_tokens *t, const void *q, const void *k, const 
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv, false)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
+    // the blocks of a head share its x and y; what one reads of z and of the first state it alone writes
+    const int64_t out_bytes = t->nq * t->heads * t->dv * 2, state_bytes = t->nseq * t->heads * t->d * t->dv * 4;
+    const Operand Q = q_of(t, q), K = k_of(t, k), V = v_of(t, v);
+    const bool alone = t->dv <= fade::ZC;
+    if (Q.under(out, out_bytes, alone) || K.under(out, out_bytes, alone) || V.under(out, out_bytes, true) || arrays_meet(out, out_bytes, state_in, state_bytes) ||
+        arrays_meet(out, out_bytes, state_out, state_bytes))
+        return ST_ERR_UNSUPPORTED;
+    if (state_out && (Q.under(state_out, state_bytes) || K.under(state_out, state_bytes) || V.under(state_out, state_bytes) ||
+                      (state_out != state_in && arrays_meet(state_out, state_bytes, state_in, state_bytes))))
+        return ST_ERR_UNSUPPORTED;
     FadeArgs a = fade_args(t, log_decay, offsets, ws);
     a.x = table_of(q, t->nq, t->heads, t->q_row, t->q_head);
     a.y = table_of(k, t->nk, t->heads, t->k_row, t->k_head);
@@ -735,6 +745,24 @@ st_status st_attn_decay_grad(const st_tokens *t, const void *q, const void *k, c
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < attn_decay_workspace(t->nq, t->nseq, t->heads, t->d > t->dv ? t->d : t->dv, true)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
+    {
+        // nor may any other result take the place of an operand or of a result
+        struct Result {
+            const void *p;
+            int64_t bytes;
+        };
+        const int64_t rows = t->nq * t->heads, state_bytes = t->nseq * t->heads * t->d * t->dv * 4;
+        const Operand tables[] = {q_of(t, q), k_of(t, k), v_of(t, v), dense_of(dout, t->nq, t->heads, t->dv)};
+        const Result results[] = {{dq, rows * t->d * 2}, {dk, rows * t->d * 2}, {dv, rows * t->dv * 2}, {dstate_in, dstate_in ? state_bytes : 0}};
+        for (int i = 0; i < 4; ++i) {
+            const Result &r = results[i];
+            if (!r.p) continue;
+            bool wrong = arrays_meet(r.p, r.bytes, state_in, state_bytes) || arrays_meet(r.p, r.bytes, dstate_out, state_bytes);
+            for (const Operand &o : tables) wrong = wrong || o.under(r.p, r.bytes);
+            for (int j = 0; j < i; ++j) wrong = wrong || arrays_meet(r.p, r.bytes, results[j].p, results[j].bytes);
+            if (wrong) return ST_ERR_UNSUPPORTED;
+        }
+    }
     const Table Q = table_of(q, t->nq, t->heads, t->q_row, t->q_head), K = table_of(k, t->nk, t->heads, t->k_row, t->k_head),
                 V = table_of(v, t->nk, t->heads, t->v_row, t->v_head), O = table_of(dout, t->nq, t->heads, t->heads * t->dv, t->dv);
     cudaStream_t s = (cudaStream_t)stream;

@@ -76,6 +76,13 @@ extern "C" st_status st_attn_decay_step(const st_tokens *t, const void *q, const
     if (t->nq > 65535) return ST_ERR_UNSUPPORTED;
     for (const void *p : {q, k, v, (const void *)log_decay, (const void *)state, (const void *)out})
         if (!aligned16(p)) return ST_ERR_ALIGN;
+    // a block reads all of its head's q and k, and of v the columns that it writes
+    const int64_t rows = t->nq * t->heads, out_bytes = rows * t->dv * 2, state_bytes = rows * t->d * t->dv * 4;
+    const Operand Q = q_of(t, q), K = k_of(t, k), V = v_of(t, v);
+    const bool alone = t->dv <= dstep::COLS;
+    if (Q.under(out, out_bytes, alone) || K.under(out, out_bytes, alone) || V.under(out, out_bytes, true) || Q.under(state, state_bytes) ||
+        K.under(state, state_bytes) || V.under(state, state_bytes) || arrays_meet(out, out_bytes, state, state_bytes))
+        return ST_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)(t->heads * ((t->dv + dstep::COLS - 1) / dstep::COLS)), (unsigned)t->nq);
     return launch(t->d <= 64 ? decay_step_kernel<4> : decay_step_kernel<8>, grid, dstep::THREADS, 0, (cudaStream_t)stream, (const bf16 *)q, (const bf16 *)k,
                   (const bf16 *)v, log_decay, state, scale, (bf16 *)out, (int)t->heads, (int)t->d, (int)t->dv);

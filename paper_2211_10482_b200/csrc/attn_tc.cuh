@@ -2,7 +2,6 @@
 // tiles of keys a tile of queries sees.
 #pragma once
 #include "attn_common.cuh"
-#include "attn_index.cuh"
 #include "tc_common.cuh"
 
 namespace st {

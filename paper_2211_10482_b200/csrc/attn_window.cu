@@ -391,6 +391,12 @@ extern "C" st_status st_attn_window(const st_tokens *tokens, const void *q, cons
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < kWsHeaderBytes) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
+    // a block reads its own queries alone, and every key and value of its band
+    const Operand Q = q_of(tokens, q), K = k_of(tokens, k), V = v_of(tokens, v);
+    const int64_t rows = tokens->nq * tokens->heads, out_bytes = rows * tokens->d * 2, lse_bytes = rows * 4;
+    if (Q.under(out, out_bytes, true) || K.under(out, out_bytes) || V.under(out, out_bytes) || Q.under(lse, lse_bytes) || K.under(lse, lse_bytes) ||
+        V.under(lse, lse_bytes) || arrays_meet(out, out_bytes, lse, lse_bytes))
+        return ST_ERR_UNSUPPORTED;
     WindowArgs a = window_args(tokens, q, k, v, q_offsets, k_offsets, window, sinks, scale, ws);
     a.out = (bf16 *)out;
     a.lse = lse;

@@ -745,6 +745,19 @@ extern "C" st_status st_attn_window_grad(const st_tokens *tokens, const void *q,
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < attn_window_grad_workspace(tokens->nq, tokens->heads, tokens->kv_heads, sinks)) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
+    // the second kernel reads q, dout and lse again; a block of it reads its own keys and values alone
+    {
+        const int64_t rows = tokens->nq * tokens->heads, q_bytes = rows * tokens->d * 2, k_bytes = tokens->nk * tokens->kv_heads * tokens->d * 2;
+        const Operand Q = q_of(tokens, q), K = k_of(tokens, k), V = v_of(tokens, v), O = dense_of(out, tokens->nq, tokens->heads, tokens->d),
+                      D = dense_of(dout, tokens->nq, tokens->heads, tokens->d);
+        bool wrong = Q.under(dq, q_bytes) || K.under(dq, q_bytes) || V.under(dq, q_bytes) || D.under(dq, q_bytes) || O.under(dq, q_bytes, true) ||
+                     arrays_meet(dq, q_bytes, lse, rows * 4) || arrays_meet(dq, q_bytes, dk, k_bytes) || arrays_meet(dq, q_bytes, dv, k_bytes) ||
+                     arrays_meet(dk, k_bytes, dv, k_bytes);
+        for (const void *to : {dk, dv})
+            wrong = wrong || Q.under(to, k_bytes) || D.under(to, k_bytes) || arrays_meet(to, k_bytes, lse, rows * 4) || K.under(to, k_bytes, true) ||
+                    V.under(to, k_bytes, true);
+        if (wrong) return ST_ERR_UNSUPPORTED;
+    }
     WindowGradArgs g = {};
     g.w = window_args(tokens, q, k, v, q_offsets, k_offsets, window, sinks, scale, ws);
     g.o = (const bf16 *)out;

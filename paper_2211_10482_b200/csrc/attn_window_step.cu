@@ -430,6 +430,9 @@ extern "C" st_status st_attn_window_step(const st_cache *c, const void *q, const
         if (!aligned16(p)) return ST_ERR_ALIGN;
     if (!ws || ws_bytes < kWsHeaderBytes) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
+    const int64_t out_bytes = c->nseq * c->heads * c->d * 2, new_bytes = c->nseq * c->kv_heads * c->d * 2;
+    if (dense_of(q, c->nseq, c->heads, c->d).under(out, out_bytes, true) || arrays_meet(out, out_bytes, k, new_bytes) || arrays_meet(out, out_bytes, v, new_bytes))
+        return ST_ERR_UNSUPPORTED;
     StepArgs a = {};
     a.q = (const bf16 *)q;
     a.k = (const bf16 *)k;

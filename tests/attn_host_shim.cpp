@@ -8,4 +8,8 @@ void shim_slab_of(int x, int slabs, int tiles, int *tile, int *slab)
     *tile = s.tile;
     *slab = s.slab;
 }
+int shim_overlap(long long table, long long rows, long long heads, long long piece, long long row, long long head, long long p, long long bytes)
+{
+    return st::attn::overlap(table, rows, heads, piece, row, head, p, bytes);
+}
 }

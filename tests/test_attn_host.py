@@ -124,6 +124,69 @@ def test_a_step_of_the_decay_takes_contiguous_tables_only(change):
     assert decay_step(tokens(nseq=100, heads=1, kv_heads=1, q_row=64, k_row=64, v_row=64, q_head=0, k_head=3, v_head=5), state=264) == st.ST_ERR_ALIGN
 
 
+FAR = [(i + 1) << 30 for i in range(14)]         # addresses whose tables do not meet
+
+
+def test_results_over_operands_are_refused():
+    """Calls that would be wrong: another block reads, or another kernel of the call reads again, what a result has replaced.  All tables
+    of 100 rows and four heads of 64 bf16 are contiguous; a result lies over an operand from its beginning, its middle or its last byte on."""
+    L, t, size, bad = st.lib(), tokens(**EVEN), 100 * 256 * 2, st.ST_ERR_UNSUPPORTED
+    q, k, v, out, lse, dout, dq, dk, dv, at, a, s0, s1, ws = FAR
+    big = 1 << 40
+    shifts = (16, size // 2, size - 16, 16 - size)
+
+    def window(q=q, k=k, v=v, out=out, lse=lse):
+        return L.st_attn_window(t, q, k, v, at, at, 10, 0, 1.0, out, lse, ws, big, None)
+
+    def window_grad(q=q, k=k, v=v, out=out, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv):
+        return L.st_attn_window_grad(t, q, k, v, out, lse, dout, at, at, 10, 0, 1.0, dq, dk, dv, ws, big, None)
+
+    def decay(q=q, k=k, v=v, out=out, s0=s0, s1=s1):
+        return L.st_attn_decay(t, q, k, v, a, at, s0, 1.0, out, s1, ws, big, None)
+
+    def decay_grad(q=q, k=k, v=v, dout=dout, s0=s0, s1=s1, dq=dq, dk=dk, dv=dv, ds=lse):
+        return L.st_attn_decay_grad(t, q, k, v, a, dout, at, s0, s1, 1.0, dq, dk, dv, ds, ws, big, None)
+
+    def decay_step(t=tokens(nseq=100, **EVEN), q=q, k=k, v=v, state=s0, out=out):
+        return L.st_attn_decay_step(t, q, k, v, a, state, 1.0, out, None)
+
+    def step(q=q, k=k, v=v, out=out):
+        return L.st_attn_window_step(cache(), q, k, v, dq, dk, at, a, 10, 0, 1.0, out, ws, big, None)
+
+    for x in (k, v):
+        assert window(out=x) == window(lse=x) == bad
+    assert window(lse=q) == window(lse=out) == window(lse=out + size - 16) == bad
+    for d in shifts:
+        assert window(out=q + d) == window(out=k + d) == window(out=v + d) == bad
+    for x in (q, k, v, dout, lse, dk, dv):
+        assert window_grad(dq=x) == bad
+    for d in shifts:
+        assert window_grad(dq=q + d) == window_grad(dq=out + d) == window_grad(dk=k + d) == window_grad(dv=k + d) == window_grad(dk=v + d) == bad
+    for x in (q, dout, lse):
+        assert window_grad(dk=x) == window_grad(dv=x) == bad
+    assert window_grad(dv=dk) == window_grad(dv=dk + 32) == bad
+    for d in shifts:
+        assert decay(out=q + d) == decay(out=k + d) == decay(out=v + d) == bad
+    for x in (q, k, v, out):
+        assert decay(s1=x) == bad
+    assert decay(out=s0) == decay(s1=s0 + 16) == decay(s1=s0 - 16) == bad
+    for x in (q, k, v, dout, s0, s1):
+        assert decay_grad(dq=x) == decay_grad(dk=x) == decay_grad(dv=x) == decay_grad(ds=x) == bad
+    assert decay_grad(dq=dk) == decay_grad(dk=dv) == decay_grad(dv=dq + 16) == decay_grad(ds=dq) == decay_grad(ds=s1 + 64) == bad
+    for x in (q, k, v, out):
+        assert decay_step(state=x) == bad
+    assert decay_step(out=v + 16) == decay_step(out=q + 16) == decay_step(out=s0) == bad
+    # the two halves of 128 columns are two blocks', which both read q and k
+    wide = tokens(nseq=100, nq=100, nk=100, **{**EVEN, "d": 128, "dv": 128, "q_row": 512, "k_row": 512, "v_row": 512, "q_head": 128, "k_head": 128, "v_head": 128})
+    assert decay_step(wide, out=q) == decay_step(wide, out=k) == bad
+    t = tokens(**{**EVEN, "d": 128, "dv": 128, "q_row": 512, "k_row": 512, "v_row": 512, "q_head": 128, "k_head": 128, "v_head": 128})
+    assert decay(out=q) == decay(out=k) == bad
+    assert step(out=k) == step(out=v) == step(out=q + 16) == step(out=v + 3 * 128 * 2 - 16) == bad
+    # slices of one projection: out lies over its q, k and v
+    t = tokens(kv_heads=4, q_row=768, k_row=768, v_row=768)
+    assert window(k=q + 512, v=q + 1024, out=q) == bad
+
+
 def test_tensors_on_the_host_are_refused_by_name():
     x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     for f in (lambda: st.st_attn_window(x, x, x, 4), lambda: st.st_attn_window_grad(x, x, x, x, x, x, 4),

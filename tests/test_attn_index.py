@@ -24,6 +24,7 @@ def shim():
     ll, ip = ctypes.c_longlong, ctypes.POINTER(ctypes.c_int)
     L.shim_most_tiles.argtypes, L.shim_most_tiles.restype = [ll] * 3, ll
     L.shim_slab_of.argtypes, L.shim_slab_of.restype = [ctypes.c_int] * 3 + [ip, ip], None
+    L.shim_overlap.argtypes, L.shim_overlap.restype = [ll] * 8, ctypes.c_int
     return L
 
 
@@ -59,3 +60,12 @@ def test_runs_of_a_gradient_stay_within_their_states(shim, d, dv):
 def test_every_sequence_has_its_tiles(shim):
     for n, lens, rows in ((1000, [1000], 128), (1000, [0, 1, 999], 256), (257, [128, 129], 128), (40, [1] * 40, 128), (5000, [4999, 1], 1 << 29)):
         assert sum(max(1, -(-x // rows)) for x in lens) <= shim.shim_most_tiles(n, len(lens), rows)
+
+
+@pytest.mark.parametrize("rows,heads,piece,row,head", [(1, 1, 4, 4, 4), (3, 2, 4, 8, 4), (3, 2, 4, 4, 12), (4, 3, 2, 16, 4), (5, 2, 3, 3, 40), (1, 3, 2, 128, 5), (4, 1, 2, 7, 128)])
+def test_overlap_is_that_of_the_bytes(shim, rows, heads, piece, row, head):
+    table = 200
+    bytes_of = {table + r * row + h * head + i for r in range(rows) for h in range(heads) for i in range(piece)}
+    for p in range(table - 12, max(bytes_of) + 12):
+        for n in (1, 2, 5, 30):
+            assert bool(shim.shim_overlap(table, rows, heads, piece, row, head, p, n)) == bool(bytes_of & set(range(p, p + n)))

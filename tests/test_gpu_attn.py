@@ -704,6 +704,45 @@ def test_a_prompt_and_its_steps_are_the_whole_sequence():
     ok()
 
 
+@pytest.mark.parametrize("d,sinks", [(64, 3), (128, 40)])
+def test_results_in_the_place_of_operands_that_are_not_read_again(d, sinks):
+    """out over q or v, dq over out, dk and dv over k and v: the same bits as with results of their own."""
+    st.set_allocator(None)
+    lens, H = [700, 33, 0, 1300], 2
+    q, k, v, do = (normal(300 + i, sum(lens), H, d) for i in range(4))
+    at, a = offsets(lens), torch.tensor([-0.1, -0.01], device="cuda")
+    out, lse = st.st_attn_window(q, k, v, 60, sinks, at)
+    x = q.clone()
+    assert st.st_attn_window(x, k, v, 60, sinks, at, out=x)[0] is x and torch.equal(x, out)
+    want = st.st_attn_window_grad(q, k, v, out, lse, do, 60, sinks, at)
+    for swap in (False, True):
+        o, x, y = out.clone(), k.clone(), v.clone()
+        dk, dv = (y, x) if swap else (x, y)
+        got = st.st_attn_window_grad(q, x, y, o, lse, do, 60, sinks, at, dq=o, dk=dk, dv=dv)
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    s = floats(305, len(lens), H, d, d)
+    out, last = st.st_attn_decay(q, k, v, a, at, s)
+    x, y = v.clone(), s.clone()
+    st.st_attn_decay(q, k, x, a, at, y, out=x, state_out=y)
+    assert torch.equal(x, out) and torch.equal(y, last)
+    n = 4
+    q1, k1, v1, s1 = q[:n].clone(), k[:n].clone(), v[:n].clone(), s.clone()
+    out = st.st_attn_decay_step(q1, k1, v1, a, s1)
+    x = v1.clone()
+    assert torch.equal(st.st_attn_decay_step(q1, k1, x, a, s.clone(), out=x), out)
+    kp, vp, table = cache_of(306, [200] * n, H, d, 16)
+    ns = torch.tensor([200, 17, 1, 0], dtype=torch.int32, device="cuda")
+    out = st.st_attn_window_step(q1, k1, v1, kp, vp, table, ns, 100, sinks)
+    assert torch.equal(st.st_attn_window_step(q1, k1, v1, kp, vp, table, ns, 100, sinks, out=q1), out)
+    with pytest.raises(st.StError) as e:
+        st.st_attn_window(q, k, v, 60, sinks, at, out=k)
+    assert e.value.status == st.ST_ERR_UNSUPPORTED
+    with pytest.raises(st.StError) as e:
+        st.st_attn_decay_grad(q, k, v, a, do, at, dv=v)
+    assert e.value.status == st.ST_ERR_UNSUPPORTED
+    ok()
+
+
 def everything(seed, H=2, d=64, lens=(150, 40, 300)):
     """One call of each kind, as a list of (inputs to overwrite, function)."""
     lens = list(lens)
