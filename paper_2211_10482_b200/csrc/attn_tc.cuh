@@ -227,7 +227,6 @@ __device__ __forceinline__ TileOf tile_of(const int *offsets, int nseq, int n, i
 // Which pairs of positions the window and the first columns leave.
 struct Mask {
     int window, sinks;
-    __device__ __forceinline__ bool sees(int t, int s) const { return s <= t && (s > t - window || s < sinks); }
     // whether any of the queries t0..t1 sees any of the keys s0..s1, or each of them every one
     __device__ __forceinline__ bool any(int t0, int t1, int s0, int s1) const { return s0 <= t1 && (s1 > t0 - window || s0 < sinks) && t1 >= t0; }
     __device__ __forceinline__ bool all(int t0, int t1, int s0, int s1) const { return s1 <= t0 && (s0 > t1 - window || s1 < sinks); }
