@@ -313,9 +313,10 @@ st_status st_packed_mul(int64_t n, const float *a, const float *b, float *out, v
  * neither read nor written.  Offsets that decrease or leave the table are cut to it and reported: st_check_status returns
  * ST_ERR_DEV_BOUNDS.  The values of one head are contiguous; rows and heads have strides (in elements, a multiple
  * of 8, at least the head's extent), so that slices of one projection's output need no copy.  out, lse, dout and the
- * gradients are contiguous.  In the calls on whole sequences an infinity or NaN in a row of a table may reach results of
- * the same sequence whose mask excludes it (its weight 0 times it): a key's or value's out of queries near it that do not see it, a query's or
- * dout's dk and dv of such keys.  Nothing of another sequence or of rows of no sequence does.  st_attn_window_step reads visible rows only.
+ * gradients are contiguous.  Rows that no pair of the mask meets (keys between the first columns and the window of the first query,
+ * queries before the first key) may hold anything.  In the calls on whole sequences an infinity or NaN in a row that some pair meets may reach
+ * results of rows of the same sequence near it whose mask excludes it (its weight 0 times it); nothing of another sequence does.
+ * st_attn_window_step reads visible rows only.
  * A result may not lie over an operand or another result (ST_ERR_UNSUPPORTED where it would be wrong), with these exceptions, each in the place of
  * the whole of a contiguous operand: out over q (st_attn_window, st_attn_window_step), out over v (st_attn_decay, st_attn_decay_step), dq
  * over out, dk and dv over k and v, either way (st_attn_window_grad), state_out over state_in (st_attn_decay). */

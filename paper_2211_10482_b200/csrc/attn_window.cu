@@ -45,8 +45,8 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
     unsigned char *Q = smem, *K = Q + 2 * S::TILE_BYTES, *V = K + STAGES * S::TILE_BYTES;
     uint64_t *bars = (uint64_t *)(V + STAGES * S::TILE_BYTES);
     uint64_t *q_full = bars, *k_full = bars + 2, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES,
-             *v_copied = v_empty + STAGES, *s_full = v_copied + STAGES, *p_full = s_full + 2, *o_full = p_full + 4;
-    uint32_t *tmem_slot = (uint32_t *)(o_full + 2);
+             *v_copied = v_empty + STAGES, *s_full = v_copied + STAGES, *p_full = s_full + 2, *o_full = p_full + 4, *v_first = o_full + 2;
+    uint32_t *tmem_slot = (uint32_t *)(v_first + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
 
@@ -88,6 +88,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
             mbar_init(&v_empty[s], 2);
             mbar_init(&v_copied[s], 1);
         }
+        mbar_init(v_first, 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -107,6 +108,17 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
         int use = 0;
         uint32_t copied = 0;                    // parity of v_copied, by stage
         bool ok = true;
+        // the last tile of first columns, where its values are cleared behind them: when they have come, and the next tile has been asked for
+        const int cleared = tiles.cleared();
+        bool clear = false;
+        auto clear_first = [&] {
+            clear = false;
+            const int s = cleared % STAGES;
+            ok = warp_wait(v_first, 0, abort_flag, a.status, 10);
+            if (!ok) return;
+            clear_rows<DP>(V + s * S::TILE_BYTES, tiles.unseen(), tiles.used(), lane);
+            if (lane == 0) mbar_arrive(&v_full[s]);
+        };
         for (int i = 0; i < n && ok; ++i) {
             const bool a0 = sees(0, i), a1 = sees(1, i);
             if (!a0 && !a1) continue;
@@ -120,7 +132,7 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                 }
             const int s = use % STAGES, s0 = tiles.key(i), row = rk.first + s0;
             const uint32_t parity = (uint32_t)((use / STAGES + 1) & 1);
-            const bool edge = s0 + TILE > rk.len;
+            const bool edge = s0 + TILE > rk.len && i != cleared;
             if (lane == 0) {
                 ok = mbar_wait(&k_empty[s], parity, abort_flag, a.status, 1);
                 if (ok) {
@@ -129,22 +141,25 @@ window_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ 
                     ok = mbar_wait(&v_empty[s], parity, abort_flag, a.status, 2);
                 }
                 if (ok) {
-                    uint64_t *bar = edge ? &v_copied[s] : &v_full[s];
+                    uint64_t *bar = i == cleared ? v_first : edge ? &v_copied[s] : &v_full[s];
                     mbar_expect_tx(bar, S::TILE_BYTES);
                     load_tile<DP>(V + s * S::TILE_BYTES, &vmap, bar, hk, row);
                 }
             }
             ok = __shfl_sync(~0u, ok, 0);
+            if (clear && ok) clear_first();
+            clear = i == cleared;
             if (edge && ok) {
                 ok = __all_sync(~0u, mbar_wait(&v_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
                 copied ^= 1u << s;
                 if (ok) {
-                    clear_rows<DP>(V + s * S::TILE_BYTES, rk.len - s0, lane);
+                    clear_rows<DP>(V + s * S::TILE_BYTES, rk.len - s0, TILE, lane);
                     if (lane == 0) mbar_arrive(&v_full[s]);
                 }
             }
             ++use;
         }
+        if (clear && ok) clear_first();
     } else if (warp >= 9) {
         // One warp for each tile of queries: its scores S of a tile of keys follow its product with V of the tile before, whose weights they
         // overwrite (products are carried out in the order of their issue), and the other tile's products fill the time between.

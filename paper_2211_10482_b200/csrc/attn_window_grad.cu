@@ -130,8 +130,9 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
     float *deltas = (float *)(V + VS * BYTES);
     uint64_t *bars = (uint64_t *)(deltas + TILE);
     uint64_t *q_full = bars, *do_full = bars + 1, *k_full = bars + 2, *k_copied = k_full + KS, *k_empty = k_copied + KS, *v_full = k_empty + KS,
-             *v_empty = v_full + VS, *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_full = dp_full + 1, *done = ds_full + 1;
-    uint32_t *tmem_slot = (uint32_t *)(done + 1);
+             *v_empty = v_full + VS, *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_full = dp_full + 1, *done = ds_full + 1,
+             *k_first = done + 1;
+    uint32_t *tmem_slot = (uint32_t *)(k_first + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, h = blockIdx.y;
 
@@ -169,6 +170,7 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         mbar_init(dp_full, 1);
         mbar_init(ds_full, 8);
         mbar_init(done, 1);
+        mbar_init(k_first, 1);
         *abort_flag = 0;
         fence_barrier_init();
     }
@@ -192,13 +194,24 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
         }
         bool ok = true;
         uint32_t copied = 0;
+        // the last tile of first columns, where its keys are cleared behind them: when they have come, and the next tile has been asked for
+        const int cleared = tiles.cleared();
+        bool clear = false;
+        auto clear_first = [&] {
+            clear = false;
+            const int s = cleared % KS;
+            ok = warp_wait(k_first, 0, abort_flag, a.status, 12);
+            if (!ok) return;
+            clear_rows<DP>(K + s * BYTES, tiles.unseen(), tiles.used(), lane);
+            if (lane == 0) mbar_arrive(&k_full[s]);
+        };
         for (int i = 0; i < n && ok; ++i) {
             const int s0 = tiles.key(i), row = rk.first + s0, s = i % KS, sv = i % VS;
-            const bool edge = s0 + TILE > rk.len;
+            const bool edge = s0 + TILE > rk.len && i != cleared;
             if (lane == 0) {
                 ok = mbar_wait(&k_empty[s], (uint32_t)((i / KS + 1) & 1), abort_flag, a.status, 1);
                 if (ok) {
-                    uint64_t *bar = edge ? &k_copied[s] : &k_full[s];
+                    uint64_t *bar = i == cleared ? k_first : edge ? &k_copied[s] : &k_full[s];
                     mbar_expect_tx(bar, BYTES);
                     load_tile<DP>(K + s * BYTES, &kmap, bar, hk, row);
                     ok = mbar_wait(&v_empty[sv], (uint32_t)((i / VS + 1) & 1), abort_flag, a.status, 2);
@@ -209,15 +222,18 @@ window_dq_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant
                 }
             }
             ok = __shfl_sync(~0u, ok, 0);
+            if (clear && ok) clear_first();
+            clear = i == cleared;
             if (edge && ok) {
                 ok = __all_sync(~0u, mbar_wait(&k_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
                 copied ^= 1u << s;
                 if (ok) {
-                    clear_rows<DP>(K + s * BYTES, rk.len - s0, lane);
+                    clear_rows<DP>(K + s * BYTES, rk.len - s0, TILE, lane);
                     if (lane == 0) mbar_arrive(&k_full[s]);
                 }
             }
         }
+        if (clear && ok) clear_first();
     } else if (warp == 9) {
         if (n > 0) {
             const bool lead = elect_one();
@@ -461,12 +477,13 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
         for (int i = 0; i < n && ok; ++i) {
             const int s = i % ST, i0 = tile * TILE;
             const uint32_t parity = (uint32_t)((i / ST + 1) & 1);
-            const bool edge = i0 + TILE > rq.len;
+            const int unseen = -off - i0;              // rows before the first key, which may hold anything
+            const bool edge = i0 + TILE > rq.len || unseen > 0;
             float lse[4], delta[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int j = i0 + k * 32 + lane;
-                const bool in = j < rq.len;
+                const bool in = j < rq.len && k * 32 + lane >= unseen;
                 const int64_t at = (int64_t)(rq.first + j) * a.heads + h;
                 lse[k] = in ? g.lse[at] : -INFINITY;
                 delta[k] = in ? g.delta[at] : 0.f;
@@ -495,12 +512,14 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
             if (edge && ok) {
                 ok = __all_sync(~0u, mbar_wait(&q_copied[s], (copied >> s) & 1u, abort_flag, a.status, 3));
                 if (ok) {
-                    clear_rows<DP>(Q + s * BYTES, rq.len - i0, lane);
+                    clear_rows<DP>(Q + s * BYTES, rq.len - i0, TILE, lane);
+                    clear_rows<DP>(Q + s * BYTES, 0, unseen, lane);
                     if (lane == 0) mbar_arrive(&q_full[s]);
                     ok = __all_sync(~0u, mbar_wait(&do_copied[s], (copied >> s) & 1u, abort_flag, a.status, 4));
                 }
                 if (ok) {
-                    clear_rows<DP>(DO + s * BYTES, rq.len - i0, lane);
+                    clear_rows<DP>(DO + s * BYTES, rq.len - i0, TILE, lane);
+                    clear_rows<DP>(DO + s * BYTES, 0, unseen, lane);
                     if (lane == 0) mbar_arrive(&do_full[s]);
                 }
                 copied ^= 1u << s;
@@ -623,8 +642,10 @@ window_dkv_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constan
             const bool inside = s < rk.len, partial = r < partial_rows;
             if (!far) {
                 // K and V have been read for the last time
+                // a key that no query sees, the first one at `off` neither: its value may hold anything, and 0 times dP - delta be NaN
+                const bool unseen = s >= a.sinks && s <= off - a.window;
                 store_rows<DP>(acc, half ? V : K, half ? &dvmap : &dkmap, half ? g.dv : g.dk, (int64_t)kv_heads * a.d, a.d, rk.first + s0 + wr, hk, r, rk.len - s0 - wr,
-                               partial_rows - wr, scale, n == 0);
+                               partial_rows - wr, scale, n == 0 || unseen);
                 if (lane == 0) tma_store_wait();
             }
             if (partial_rows > (warp & 3) * 32) {

@@ -275,6 +275,43 @@ def test_rows_of_no_sequence_are_neither_read_nor_written():
     ok()
 
 
+@pytest.mark.parametrize("lq,lk,window,sinks", [
+    ([300, 40], [900, 1000], 100, 4), ([300], [900], 100, 40), ([513, 3], [900, 700], 100, 130), ([300], [900], 128, 128), ([300, 200], [1400, 700], 33, 32),
+    ([300, 1], [900, 500], 100, 0), ([2100], [2600], 70, 7), ([2100], [2600], 70, 200),
+    ([300, 260, 140], [100, 0, 20], 50, 3), ([400, 300], [130, 171], 1000, 0)])
+@pytest.mark.parametrize("d", [64, 128, 80])
+def test_rows_of_a_sequence_that_no_pair_meets_may_hold_anything(lq, lk, window, sinks, d):
+    """Keys and values between the first columns and the window of the first query, as a cache leaves them that keeps no more, and queries that
+    stand before the first key: NaN there changes no bit, and their own gradients are 0."""
+    H, Hk = 4, 2
+    lk, q, k, v, qo, ko = window_inputs(63, lq, lk, H, Hk, d)
+    do = normal(66, *q.shape)
+    seen_k, seen_q = [], []
+    for x, y in zip(lq, lk):
+        see = ref.visible(x, y, window, sinks, "cuda")
+        seen_k.append(see.any(0))
+        seen_q.append(see.any(1))
+    none_k, none_q = ~torch.cat(seen_k), ~torch.cat(seen_q)
+    assert bool(none_k.any() | none_q.any())
+
+    def run(q, k, v, do):
+        out, lse = st.st_attn_window(q, k, v, window, sinks, qo, ko)
+        grads = st.st_attn_window_grad(q, k, v, out, lse, do, window, sinks, qo, ko)
+        ok()
+        return out, lse, *grads
+
+    want = run(q, k, v, do)
+    for value in (math.nan, math.inf, -math.inf):
+        for which in ((0,), (1,), (2,), (3,), (0, 1, 2, 3)):
+            tables = [x.clone() for x in (q, k, v, do)]
+            for i in which:
+                tables[i][none_k if i in (1, 2) else none_q] = value
+            got = run(*tables)
+            assert all(torch.equal(x, y) for x, y in zip(got, want)), (value, which)
+    for g, rows in ((want[0], none_q), (want[2], none_q), (want[3], none_k), (want[4], none_k)):
+        assert bool((g[rows] == 0).all())
+
+
 @pytest.mark.parametrize("bad", [[0, 50, 40, 100], [0, 50, 60, 101], [-1, 50, 60, 100], [0, 1 << 30, 5, 100]])
 def test_bad_offsets_are_reported_and_touch_nothing_outside(bad):
     q, k, v = (normal(70 + i, 100, 2, 64) for i in range(3))
