@@ -21,7 +21,7 @@
 // Bound by what a chunk does in turn: P Z and X S have one place each in tensor memory and are issued in a fixed order, so that X S of a chunk and the
 // scores behind it wait until P of the chunk before has been made, multiplied and read.  One head of 128 alone takes 1.4 us a chunk (1.8 with the third
 // part), 148 blocks at once 1.9 (2.4).  Some 370 KB go through shared memory for it (80 of copies, 190 of operands, 100 of Z, S and out; 64 more with
-// a third part), and more than a third of its wavefronts are bank conflicts.  65536 tokens of 16 heads run at 1000 W and 1.4 to 1.5 GHz.
+// a third part), and about a third of its wavefronts are bank conflicts.  65536 tokens of 16 heads run at 1000 W and 1.4 to 1.5 GHz.
 // Two warps that issue products, or four more that write out, changed nothing or lost 5 %: they leave the wait where it is.
 //
 // Warps: 0..3 make P (a thread = a token), 4..7 weigh Z (a thread = a token), 8..11 keep S (a thread = a row of it) and write out (a thread = a

@@ -12,7 +12,7 @@
 // cuts are masked.  Values behind a sequence's last key may be anything: their weight is 0, and their rows of V are
 // cleared in shared memory, as 0 times NaN would be NaN.
 //
-// Bound by power where many tiles of keys are seen: 32768 tokens, 16 heads of 128, window 4096 run at 990 TFLOP/s whether the exponentials and the
+// Bound by power where many tiles of keys are seen: 32768 tokens, 16 heads of 128, window 4096 run at 960 to 990 TFLOP/s whether the exponentials and the
 // products alternate (3100 cycles for both tiles, at 1.4 GHz) or not (3960, at 1.8), and slower with part of the exponentials as
 // polynomials on the FMA units (1050 us, so 1185 with an eighth of them).  Few tiles of keys: by a block's beginning and end.
 //
