@@ -9,7 +9,8 @@
  *
  * Conventions for every call
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The library
- *     never allocates, frees or keeps them.  Base pointers must be 16-byte aligned.
+ *     never allocates, frees or keeps them.  Base pointers must be 16-byte aligned (whole
+ *     numbers that st_attn_rotate and the calls on st_cells take: 4-byte aligned).
  *   - Everything is row-major; extents are int64_t.
  *   - `stream` is a cudaStream_t passed as void* (NULL = the default stream).
  *     Calls are asynchronous on that stream and do not synchronise, except
@@ -66,13 +67,14 @@ typedef enum {
                                   built-in ST_STATIC_SCRATCH_BYTES */
 } st_status;
 
-typedef enum { ST_F32 = 0, ST_BF16 = 1, ST_F64 = 2 } st_dtype;
+typedef enum { ST_F32 = 0, ST_BF16 = 1, ST_F64 = 2, ST_I8 = 3, ST_I4 = 4 } st_dtype;   /* ST_I8, ST_I4: cells of a cache (st_cells) */
 typedef enum { ST_TRI_UPPER = 0, ST_TET = 1, ST_BAND = 2, ST_BLOCKDIAG = 3, ST_FIXED_ROW = 4, ST_FIXED_COL = 5,
                ST_SIMPLEX4 = 6 } st_kind;
 typedef enum { ST_FILL_ZERO = 0, ST_FILL_SYMMETRIC = 1 } st_fill;
 typedef enum { ST_OP_SYM_MOMENT2 = 0, ST_OP_SYM_MOMENT3 = 1, ST_OP_MTTKRP_TRI = 2,
                ST_OP_TTM_BLOCKDIAG = 3, ST_OP_SYM_MOMENT4 = 4, ST_OP_MTTKRP_SLICE = 5, ST_OP_ATTN_WINDOW = 6,
-               ST_OP_ATTN_WINDOW_GRAD = 7, ST_OP_ATTN_WINDOW_STEP = 8, ST_OP_ATTN_DECAY = 9, ST_OP_ATTN_DECAY_GRAD = 10 } st_op;
+               ST_OP_ATTN_WINDOW_GRAD = 7, ST_OP_ATTN_WINDOW_STEP = 8, ST_OP_ATTN_DECAY = 9, ST_OP_ATTN_DECAY_GRAD = 10,
+               ST_OP_ATTN_ROTATE_GRAD = 11, ST_OP_ATTN_CACHE = 12, ST_OP_ATTN_SHARED_STEP = 13 } st_op;
 
 /* flags (bit mask) */
 #define ST_FLAG_DENSE_CONTROL 1u /* run the same kernel over the dense, unstructured iteration
@@ -132,6 +134,9 @@ st_status st_unpack(const st_layout *layout, st_dtype dtype, const void *packed,
  *   ST_OP_ATTN_WINDOW   unused: the header alone;  ST_OP_ATTN_WINDOW_STEP likewise
  *   ST_OP_ATTN_WINDOW_GRAD a=nq, b=heads, c=kv_heads, e=sinks
  *   ST_OP_ATTN_DECAY, ST_OP_ATTN_DECAY_GRAD  a=nq, b=nseq, c=heads, e=max(d, dv)
+ *   ST_OP_ATTN_ROTATE_GRAD  a=d (0 where no weights have a gradient: the header alone)
+ *   ST_OP_ATTN_CACHE    unused: the header alone, for st_attn_cache_write, st_attn_cache_read and st_attn_cache_step
+ *   ST_OP_ATTN_SHARED_STEP  a=nseq, b=heads, c=kv_heads, e=groups
  * Returns 0 for an invalid request (the call itself reports the error).  The current
  * device is queried for its SM count. */
 size_t st_workspace_bytes(st_op op, int64_t a, int64_t b, int64_t c, int64_t e, unsigned flags);
@@ -397,6 +402,92 @@ st_status st_attn_decay_grad(const st_tokens *tokens, const void *q, const void 
  * ([nseq, heads, d, dv] fp32) is updated in place. */
 st_status st_attn_decay_step(const st_tokens *tokens, const void *q, const void *k, const void *v, const float *log_decay,
                              float *state, float scale, void *out, void *stream);
+
+/* ---- norms and rotations of queries and keys --------------------------------------------------
+ * What comes between a projection and the attention: an RMS norm of every head and a rotation by the token's position, a block-diagonal
+ * matrix of 2 x 2 blocks in the first `rot` columns, in one pass over the table.  The paper has no counterpart.
+ *     r = 1 / sqrt(mean_i x[i]^2 + eps);   y[i] = x[i] r w[i]      (norm = 0: y = x)
+ *     columns (a, b) of pair i:  y'[a] = factor (y[a] cos t - y[b] sin t),  y'[b] = factor (y[b] cos t + y[a] sin t),  t = position freq[i]
+ * Pairs: (2i, 2i+1) where interleaved, else (i, i + rot/2); columns from rot on have no pair and no factor.  The angle is the exact product of
+ * the position and the fp32 frequency, reduced in 64 bits: far positions lose nothing.  Sums, norms and rotations are fp32, a result is rounded once. */
+typedef struct {
+    int32_t dtype;            /* of the tables: ST_BF16 */
+    int32_t weight_dtype;     /* of q_weight and k_weight: ST_BF16 or ST_F32 */
+    int32_t norm;             /* 1: RMS norms */
+    int32_t interleaved;      /* 1: pairs are neighbours */
+    int64_t n;                /* tokens: up to 2^29 */
+    int64_t heads, kv_heads;  /* heads of q and of k; kv_heads = 0: no k */
+    int64_t d, rot;           /* extent of a head, a multiple of 8 up to 128; columns that turn, even, 0 to d */
+    int64_t q_row, q_head;    /* strides as in st_tokens */
+    int64_t k_row, k_head;
+    float eps;                /* of the norms, at least 0 */
+    float factor;             /* of what is rotated (1 but for scaled contexts), finite */
+} st_rotation;
+
+/* positions: int32 [n], any sign; freq: fp32 [rot/2]; q_weight, k_weight: [d] or NULL (ones).  q_out: bf16 [n, heads, d], k_out: [n, kv_heads, d],
+ * contiguous; each may take the place of the whole of its own operand, where that is contiguous. */
+st_status st_attn_rotate(const st_rotation *rotation, const void *q, const void *k, const int32_t *positions, const float *freq,
+                         const void *q_weight, const void *k_weight, void *q_out, void *k_out, void *stream);
+
+/* Gradient of st_attn_rotate.  With g = the rotation's transpose of dy, times factor where it turned, and n = x r:
+ *     dw = sum over tokens and heads of g n;   dx = r (g w - n mean(g w n))      (norm = 0: dx = g)
+ * q and k are what st_attn_rotate was given (norm = 0: not read, may be NULL); dq_out and dk_out the gradients of its results, contiguous.  dq, dk
+ * contiguous: each may take the place of dq_out, dk_out.  dq_weight, dk_weight: fp32 [d], or NULL where none is wanted; fixed order of sums. */
+st_status st_attn_rotate_grad(const st_rotation *rotation, const void *q, const void *k, const void *dq_out, const void *dk_out,
+                              const int32_t *positions, const float *freq, const void *q_weight, const void *k_weight, void *dq,
+                              void *dk, float *dq_weight, float *dk_weight, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- a cache in cells -------------------------------------------------------------------------
+ * Keys and values in pages as in st_cache, as they are or quantised when they are written.  A row is one token's key or value of one head:
+ *   ST_BF16  d values.
+ *   ST_I8    d int8 cells c and one fp32 scale: the row stands for scale c.  With a = max |x|: scale = a / 127, c = round(x (127 / a)).
+ *   ST_I4    d cells c of 4 bits (column 2i in the low half of byte i) and, for each 32 columns, two bf16 numbers (step, lo): lo + step c.
+ *            lo = min x, step = bf16((max x - lo) / 15), c = round((x - lo) (1 / step)), at most 15.
+ * Each operation in fp32, rounded to nearest even.  A scale or step whose a or step is below 2^-100 is 0 (the row stands for 0, or the columns for
+ * lo); one of a row (32 columns) with an infinity or NaN is NaN, and so is what the row (the columns) stands for. */
+typedef struct {
+    int32_t dtype;            /* ST_BF16, ST_I8, ST_I4 */
+    int32_t reserved;         /* must be 0 */
+    int64_t nseq, heads, kv_heads;   /* heads: of the queries of st_attn_cache_step and st_attn_shared_step */
+    int64_t d;                /* a multiple of 8 (ST_I4: of 16) up to 128 */
+    int64_t pages, page;      /* pages of the cache, tokens of a page */
+    int64_t table_cols;       /* page numbers in a row of the table: page * table_cols up to 2^30 */
+    int64_t page_stride, token_stride, head_stride;      /* of k_pages and v_pages, in bytes: multiples of 16 (ST_I8, ST_I4: of 8) */
+    int64_t scale_page, scale_token, scale_head;         /* of k_scales and v_scales, in units of 4 bytes (a scale; step and lo) */
+} st_cells;
+
+/* Writes the last tokens of every sequence to its pages: rows offsets[b] .. offsets[b+1]-1 of k and v are the tokens lens[b] - L .. lens[b] - 1 of sequence b,
+ * L of them (tokens: nk rows, kv_heads, d = dv, k_* and v_* strides; its other members are not looked at).  offsets NULL: a row for every sequence (nk = nseq), or one sequence of all rows.
+ * k_scales, v_scales: NULL for ST_BF16.  A token whose position is negative or behind the table's row, or whose page is outside the cache, is not
+ * written and reported: ST_ERR_DEV_BOUNDS.  Rows of no sequence are not looked at.  No two tokens of one call may have one place. */
+st_status st_attn_cache_write(const st_cells *cells, const st_tokens *tokens, const void *k, const void *v, const int32_t *table,
+                              const int32_t *lens, const int32_t *offsets, void *k_pages, void *v_pages, void *k_scales,
+                              void *v_scales, void *ws, size_t ws_bytes, void *stream);
+
+/* The other way: the last tokens of every sequence as bf16 rows of k and v [n, kv_heads, d] (contiguous), what their cells stand for, rounded once.  Rows of
+ * no sequence are left as they are; a token without a place is a row of zeros and reported. */
+st_status st_attn_cache_read(const st_cells *cells, int64_t n, const void *k_pages, const void *v_pages, const void *k_scales,
+                             const void *v_scales, const int32_t *table, const int32_t *lens, const int32_t *offsets, void *k, void *v,
+                             void *ws, size_t ws_bytes, void *stream);
+
+/* st_attn_window for the last token of every sequence over such a cache, which holds it already (st_attn_cache_write): q [nseq, heads, d] with strides
+ * q_row, q_head (multiples of 8), position lens[b] - 1; out bf16 [nseq, heads, d], contiguous, which may take the place of the whole of a contiguous q.  lens[b] = 0: out = 0.
+ * Only table entries of visible tokens are read.  Lengths beyond the table's row (cut), negative ones (0) and page numbers outside the cache where
+ * a visible token lies (left out; where no token is left, out = 0) are reported: ST_ERR_DEV_BOUNDS.  Scores, maxima and sums are fp32; cells meet the queries as whole numbers and their
+ * scales the scores; a weight times its value's scale is rounded to bf16 for the product with the values' cells. */
+st_status st_attn_cache_step(const st_cells *cells, const void *q, int64_t q_row, int64_t q_head, const void *k_pages, const void *v_pages,
+                             const void *k_scales, const void *v_scales, const int32_t *table, const int32_t *lens, int64_t window,
+                             int64_t sinks, float scale, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* Attention of one token of every sequence over all of a prefix that its group shares, then all of its own tokens: sequences group_offsets[g] ..
+ * group_offsets[g+1]-1 (int32, groups+1 of them; NULL = one group of all) share the prefix_lens[g] tokens behind row g of prefix_table [groups,
+ * prefix_cols]; lens[b] tokens behind row b of table are sequence b's own and may be none.  The prefix's scores are computed once for all queries of a group, on the tensor
+ * cores.  A sequence of no group, or of an empty prefix, sees its own tokens alone; one without any token has out = 0.  ST_BF16 only.  Reports as
+ * st_attn_cache_step; prefix lengths likewise; group_offsets that decrease or leave 0 .. nseq are cut and reported. */
+st_status st_attn_shared_step(const st_cells *cells, const void *q, int64_t q_row, int64_t q_head, const void *k_pages, const void *v_pages,
+                              const int32_t *prefix_table, int64_t prefix_cols, const int32_t *prefix_lens, int64_t groups,
+                              const int32_t *group_offsets, const int32_t *table, const int32_t *lens, float scale, void *out,
+                              void *ws, size_t ws_bytes, void *stream);
 
 /* Synchronises `stream`, then reads the status word a kernel may have written into the
  * workspace (a bounded wait that ran out, a failed consistency check).  ws may be NULL. */

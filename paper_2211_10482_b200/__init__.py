@@ -27,7 +27,7 @@ ST_OK, ST_ERR_NULL, ST_ERR_SHAPE, ST_ERR_ALIGN, ST_ERR_DTYPE, ST_ERR_WORKSPACE, 
     ST_ERR_CUDA, ST_ERR_DEV_TIMEOUT, ST_ERR_DEV_BOUNDS, ST_ERR_STATIC_SCRATCH = range(11)
 ST_STATIC_SCRATCH_BYTES = 16 << 20
 # st_dtype
-ST_F32, ST_BF16, ST_F64 = 0, 1, 2
+ST_F32, ST_BF16, ST_F64, ST_I8, ST_I4 = 0, 1, 2, 3, 4
 # st_kind
 ST_TRI_UPPER, ST_TET, ST_BAND, ST_BLOCKDIAG, ST_FIXED_ROW, ST_FIXED_COL, ST_SIMPLEX4 = 0, 1, 2, 3, 4, 5, 6
 # st_fill
@@ -35,7 +35,7 @@ ST_FILL_ZERO, ST_FILL_SYMMETRIC = 0, 1
 # st_op
 ST_OP_SYM_MOMENT2, ST_OP_SYM_MOMENT3, ST_OP_MTTKRP_TRI, ST_OP_TTM_BLOCKDIAG, ST_OP_SYM_MOMENT4, \
     ST_OP_MTTKRP_SLICE, ST_OP_ATTN_WINDOW, ST_OP_ATTN_WINDOW_GRAD, ST_OP_ATTN_WINDOW_STEP, ST_OP_ATTN_DECAY, \
-    ST_OP_ATTN_DECAY_GRAD = range(11)
+    ST_OP_ATTN_DECAY_GRAD, ST_OP_ATTN_ROTATE_GRAD, ST_OP_ATTN_CACHE, ST_OP_ATTN_SHARED_STEP = range(14)
 # flags
 ST_FLAG_DENSE_CONTROL = 1
 ST_FLAG_TC_TF32 = 2
@@ -46,7 +46,8 @@ EXPORTS = [
     "st_packed_elems", "st_dense_elems", "st_pack", "st_unpack", "st_workspace_bytes", "st_sym_moment2",
     "st_sym_moment3", "st_sym_moment3_static", "st_sym_moment4", "st_mttkrp_tri", "st_mttkrp_slice", "st_ttm_blockdiag", "st_ttm_packed",
     "st_thp", "st_packed_axpby", "st_packed_mul", "st_attn_window", "st_attn_window_grad", "st_attn_window_step",
-    "st_attn_decay", "st_attn_decay_grad", "st_attn_decay_step", "st_check_status", "st_status_string",
+    "st_attn_decay", "st_attn_decay_grad", "st_attn_decay_step", "st_attn_rotate", "st_attn_rotate_grad", "st_attn_cache_write",
+    "st_attn_cache_read", "st_attn_cache_step", "st_attn_shared_step", "st_check_status", "st_status_string",
     "st_abi_version", "st_bounds_checked_build", "st_bounds_self_test",
 ]
 
@@ -65,6 +66,17 @@ class StTokens(ctypes.Structure):
 class StCache(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in (
         "nseq", "heads", "kv_heads", "d", "pages", "page", "table_cols", "page_stride", "token_stride", "head_stride")]
+
+
+class StRotation(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "weight_dtype", "norm", "interleaved")] + [(n, ctypes.c_int64) for n in (
+        "n", "heads", "kv_heads", "d", "rot", "q_row", "q_head", "k_row", "k_head")] + [("eps", ctypes.c_float), ("factor", ctypes.c_float)]
+
+
+class StCells(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in (
+        "nseq", "heads", "kv_heads", "d", "pages", "page", "table_cols", "page_stride", "token_stride", "head_stride", "scale_page",
+        "scale_token", "scale_head")]
 
 
 @dataclass(frozen=True)
@@ -128,13 +140,22 @@ def lib() -> ctypes.CDLL:
         L.st_attn_decay.argtypes = [TP, vp, vp, vp, vp, vp, vp, cf, vp, vp, vp, sz, vp]
         L.st_attn_decay_grad.argtypes = [TP, vp, vp, vp, vp, vp, vp, vp, vp, cf, vp, vp, vp, vp, vp, sz, vp]
         L.st_attn_decay_step.argtypes = [TP, vp, vp, vp, vp, vp, cf, vp, vp]
+        RP, EP = ctypes.POINTER(StRotation), ctypes.POINTER(StCells)
+        L.st_attn_rotate.argtypes = [RP, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.st_attn_rotate_grad.argtypes = [RP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.st_attn_cache_write.argtypes = [EP, TP, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.st_attn_cache_read.argtypes = [EP, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.st_attn_cache_step.argtypes = [EP, vp, i64, i64, vp, vp, vp, vp, vp, vp, i64, i64, cf, vp, vp, sz, vp]
+        L.st_attn_shared_step.argtypes = [EP, vp, i64, i64, vp, vp, vp, i64, vp, i64, vp, vp, vp, cf, vp, vp, sz, vp]
         L.st_check_status.argtypes = [vp, vp]
         L.st_status_string.argtypes = [ci]
         L.st_status_string.restype = ctypes.c_char_p
         L.st_abi_version.restype = ci
         for name in ("st_pack", "st_unpack", "st_sym_moment2", "st_sym_moment3", "st_sym_moment3_static", "st_sym_moment4", "st_mttkrp_tri",
                      "st_mttkrp_slice", "st_ttm_blockdiag", "st_ttm_packed", "st_thp", "st_packed_axpby", "st_packed_mul", "st_attn_window",
-                     "st_attn_window_grad", "st_attn_window_step", "st_attn_decay", "st_attn_decay_grad", "st_attn_decay_step", "st_check_status"):
+                     "st_attn_window_grad", "st_attn_window_step", "st_attn_decay", "st_attn_decay_grad", "st_attn_decay_step",
+                     "st_attn_rotate", "st_attn_rotate_grad", "st_attn_cache_write", "st_attn_cache_read", "st_attn_cache_step",
+                     "st_attn_shared_step", "st_check_status"):
             getattr(L, name).restype = ci
         _lib = L
     return _lib
@@ -156,7 +177,7 @@ def _bind():
     except ModuleNotFoundError:
         raise RuntimeError("_binding.so is missing: build it with `python -m paper_2211_10482_b200._build`") from None
     b.bind({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS}, StError,
-           torch.float32, torch.uint8, _last_ws)
+           torch.float32, torch.uint8, torch.bfloat16, _last_ws)
     b.set_allocator(_allocator)
     _native = b
     return b
@@ -354,6 +375,88 @@ def st_attn_decay_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_de
     """st_attn_decay for one new token of every sequence: q and k [n, heads, d], v [n, heads, dv]; state [n, heads, d, dv]
     is updated in place."""
     return (_native or _bind()).attn_decay_step(q, k, v, log_decay, state, scale, out)
+
+
+def st_rotary_frequencies(rot: int, base: float = 10000.0, kind: str = "none", stretch: float = 1.0, trained: int = 0,
+                          turns: tuple[float, float] = (1.0, 32.0)) -> torch.Tensor:
+    """Frequencies base^(-2i/rot) of ``rot`` columns (float32 [rot/2], on the CPU), for contexts ``stretch`` times as long:
+    "linear" divides all of them by stretch; "base" takes base stretch^(rot/(rot-2)), which leaves the highest one and divides the lowest by
+    stretch; "turns" divides those that make at most turns[0] turns within ``trained`` tokens, leaves those that make turns[1] or more, and
+    goes from one to the other in proportion to the turns."""
+    if rot <= 0 or rot % 2 or not base > 0 or not stretch > 0:
+        raise ValueError("rot must be even and positive, base and stretch positive")
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    if kind == "base":
+        if rot == 2:
+            raise ValueError("one frequency has no base to be stretched")
+        base = base * stretch ** (rot / (rot - 2))
+    f = base ** (-2.0 * i / rot)
+    if kind == "linear":
+        f = f / stretch
+    elif kind == "turns":
+        if trained <= 0 or not 0 <= turns[0] < turns[1]:
+            raise ValueError("trained must be positive and turns[0] below turns[1]")
+        whole = ((trained * f / (2 * math.pi) - turns[0]) / (turns[1] - turns[0])).clamp(0, 1)
+        f = f * whole + f / stretch * (1 - whole)
+    elif kind not in ("none", "base"):
+        raise ValueError("kind must be none, linear, base or turns")
+    return f.float()
+
+
+def st_attn_rotate(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, freq: torch.Tensor | None, interleaved: bool = False,
+                   q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float | None = None,
+                   factor: float = 1.0, q_out: torch.Tensor | None = None,
+                   k_out: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor | None]:
+    """RMS norms of the heads of q [n, heads, d] and k [n, kv_heads, d] (bfloat16; with eps, and weights [d] float32 or bfloat16), then the
+    rotation of their first 2 len(freq) columns by positions (int32 [n]) times freq (float32), halves or neighbours paired, what turns times
+    factor; either part may be left out (eps None, freq None).  q_out may be q, k_out k.  Returns (q, k)."""
+    return (_native or _bind()).attn_rotate(q, k, positions, freq, interleaved, q_weight, k_weight, eps, factor, q_out, k_out)
+
+
+def st_attn_rotate_grad(q: torch.Tensor, k: torch.Tensor | None, dq_out: torch.Tensor, dk_out: torch.Tensor | None, positions: torch.Tensor,
+                        freq: torch.Tensor | None, interleaved: bool = False, q_weight: torch.Tensor | None = None,
+                        k_weight: torch.Tensor | None = None, eps: float | None = None, factor: float = 1.0,
+                        dq: torch.Tensor | None = None, dk: torch.Tensor | None = None, dq_weight: torch.Tensor | None = None,
+                        dk_weight: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """(dq, dk, dq_weight, dk_weight) of st_attn_rotate, from its operands and the gradients of its results; the weights' are float32, None
+    where there is no weight.  dq may be dq_out, dk dk_out."""
+    return (_native or _bind()).attn_rotate_grad(q, k, dq_out, dk_out, positions, freq, interleaved, q_weight, k_weight, eps, factor, dq, dk,
+                                                 dq_weight, dk_weight, ws)
+
+
+def st_attn_cache_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor,
+                        lens: torch.Tensor, offsets: torch.Tensor | None = None, k_scales: torch.Tensor | None = None,
+                        v_scales: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> None:
+    """Writes k and v [n, kv_heads, d] (bfloat16) to the pages of a cache as the last tokens of every sequence.  Pages
+    [pages, page, kv_heads, d] are bfloat16, or int8 with one float32 scale a row ([pages, page, kv_heads]), or uint8 with two cells of 4 bits
+    in each ([.., d/2]) and scales bfloat16 [pages, page, kv_heads, ceil(d/32), 2] (step, lowest value).  table and lens as in
+    st_attn_window_step, lens with the new tokens; offsets int32 say where each sequence's rows begin (None: a row for every sequence, or one sequence)."""
+    return (_native or _bind()).attn_cache_write(k, v, k_pages, v_pages, table, lens, offsets, k_scales, v_scales, ws)
+
+
+def st_attn_cache_read(k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, offsets: torch.Tensor | None,
+                       rows: int, k_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None, k: torch.Tensor | None = None,
+                       v: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> tuple[torch.Tensor, torch.Tensor]:
+    """The last tokens of every sequence, as many as ``offsets`` has rows for it, as k and v bfloat16 [rows, kv_heads, d]: what st_attn_window
+    takes for a prompt behind a cache.  Rows of no sequence are not written."""
+    return (_native or _bind()).attn_cache_read(k_pages, v_pages, table, lens, offsets, rows, k_scales, v_scales, k, v, ws)
+
+
+def st_attn_cache_step(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, window: int,
+                       sinks: int = 0, k_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None,
+                       scale: float | None = None, out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """st_attn_window for the last token of every sequence (q [n, heads, d]) over a cache as st_attn_cache_write fills it, which
+    holds that token's key and value already; nothing is written to the cache."""
+    return (_native or _bind()).attn_cache_step(q, k_pages, v_pages, table, lens, window, sinks, k_scales, v_scales, scale, out, ws)
+
+
+def st_attn_shared_step(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, prefix_table: torch.Tensor, prefix_lens: torch.Tensor,
+                        table: torch.Tensor, lens: torch.Tensor, group_offsets: torch.Tensor | None = None, scale: float | None = None,
+                        out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """st_attn_cache_step for a batch whose sequences share prefixes: sequences group_offsets[g] .. group_offsets[g+1]-1 (int32; None: one
+    group) see the prefix_lens[g] tokens behind prefix_table[g], then their own lens behind table; bfloat16 pages, no window.  A prefix is
+    read once for all queries of its group."""
+    return (_native or _bind()).attn_shared_step(q, k_pages, v_pages, prefix_table, prefix_lens, table, lens, group_offsets, scale, out, ws)
 
 
 def st_check_status(ws: torch.Tensor | None = None) -> int:

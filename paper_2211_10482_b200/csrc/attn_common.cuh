@@ -70,6 +70,27 @@ inline int clamp_int(int64_t x, int most = 1 << 29) { return x > most ? most : (
 
 #if defined(__CUDACC__)
 
+// Eight bf16 as floats and back, rounded once.
+__device__ __forceinline__ void unpack8(const uint4 &u, float (&x)[8])
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float (&x)[8])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Rows [first, first + len) of sequence b, cut to the table.
 struct Rows {
     int first, len;

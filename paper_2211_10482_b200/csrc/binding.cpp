@@ -45,10 +45,16 @@ struct Api {
     decltype(&st_attn_decay) attn_decay;
     decltype(&st_attn_decay_grad) attn_decay_grad;
     decltype(&st_attn_decay_step) attn_decay_step;
+    decltype(&st_attn_rotate) attn_rotate;
+    decltype(&st_attn_rotate_grad) attn_rotate_grad;
+    decltype(&st_attn_cache_write) attn_cache_write;
+    decltype(&st_attn_cache_read) attn_cache_read;
+    decltype(&st_attn_cache_step) attn_cache_step;
+    decltype(&st_attn_shared_step) attn_shared_step;
 } api;
 
 PyObject *error_class, *allocator;             // StError; callable or null
-PyObject *dtype_f32, *dtype_u8;                // torch.float32, torch.uint8
+PyObject *dtype_f32, *dtype_u8, *dtype_bf16;   // torch.float32, torch.uint8, torch.bfloat16
 PyObject *s_kind, *s_d, *s_inner, *s_kl, *s_ku, *s_nblocks, *s_bs, *s_dtype, *s_device, *s_view;
 PyObject *last_ws;                             // dict: device index -> workspace of the most recent compute call
 
@@ -818,6 +824,316 @@ PyObject *py_attn_decay_step(PyObject *const *v)         // q, k, v, log_decay, 
     return out.release();
 }
 
+// ---- rotations ------------------------------------------------------------------------
+
+struct Rotation {
+    st_rotation r;
+    const at::Tensor &q;
+    const at::Tensor *k;                       // or null
+    const int32_t *positions;
+    const float *freq;
+    const void *q_weight, *k_weight;
+};
+
+const void *weight_of(const Rotation &x, PyObject *o, const char *name, at::ScalarType *type)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &w = cuda_tensor(o, name);
+    if (w.scalar_type() != at::kFloat && w.scalar_type() != at::kBFloat16) {
+        PyErr_Format(PyExc_TypeError, "%s must be float32 or bfloat16", name);
+        throw Failed();
+    }
+    if (*type != at::kByte && w.scalar_type() != *type) fail(PyExc_TypeError, "q_weight and k_weight must have the same type");
+    *type = w.scalar_type();
+    contiguous(x.q, o, *type, name);
+    want_shape(w, {x.r.d}, name);
+    return w.data_ptr();
+}
+
+// q, k, positions, freq, interleaved, q_weight, k_weight, eps, factor
+Rotation rotation(PyObject *pq, PyObject *pk, PyObject *const *v)
+{
+    const at::Tensor &q = cuda_tensor(pq, "q");
+    table(q, pq, "q", 3);
+    const at::Tensor *k = pk == Py_None ? nullptr : &table(q, pk, "k", 3);
+    if (k && (k->size(0) != q.size(0) || k->size(2) != q.size(2))) fail(PyExc_ValueError, "shape mismatch");
+    Rotation x = {{}, q, k, nullptr, nullptr, nullptr, nullptr};
+    st_rotation &r = x.r;
+    r.dtype = ST_BF16;
+    r.n = q.size(0);
+    r.heads = q.size(1);
+    r.d = q.size(2);
+    r.q_row = q.stride(0);
+    r.q_head = q.stride(1);
+    if (k) {
+        r.kv_heads = k->size(1);
+        r.k_row = k->stride(0);
+        r.k_head = k->stride(1);
+        if (r.kv_heads == 0) fail(PyExc_ValueError, "k has no heads");
+    }
+    const at::Tensor &positions = contiguous(q, v[0], at::kInt, "positions");
+    want_shape(positions, {r.n}, "positions");
+    x.positions = (const int32_t *)positions.data_ptr();
+    if (v[1] != Py_None) {
+        const at::Tensor &freq = contiguous(q, v[1], at::kFloat, "freq");
+        if (freq.dim() != 1) fail(PyExc_ValueError, "freq must have one dimension");
+        r.rot = 2 * freq.size(0);
+        x.freq = (const float *)freq.data_ptr();
+    }
+    const int interleaved = PyObject_IsTrue(v[2]);
+    if (interleaved < 0) throw Failed();
+    r.interleaved = interleaved;
+    r.norm = v[5] != Py_None;
+    r.eps = r.norm ? real(v[5]) : 0.f;
+    r.factor = real(v[6]);
+    if (!r.norm && (v[3] != Py_None || v[4] != Py_None)) fail(PyExc_ValueError, "weights belong to norms: eps is missing");
+    if (!k && v[4] != Py_None) fail(PyExc_ValueError, "k_weight without k");
+    at::ScalarType type = at::kByte;
+    x.q_weight = weight_of(x, v[3], "q_weight", &type);
+    x.k_weight = weight_of(x, v[4], "k_weight", &type);
+    r.weight_dtype = type == at::kFloat ? ST_F32 : ST_BF16;
+    return x;
+}
+
+Ref none() { return Ref((Py_INCREF(Py_None), Py_None)); }
+
+// q, k, positions, freq, interleaved, q_weight, k_weight, eps, factor, q_out, k_out
+PyObject *py_attn_rotate(PyObject *const *v)
+{
+    const Guard guard(cuda_tensor(v[0], "q").device());
+    const Rotation x = rotation(v[0], v[1], v + 2);
+    const st_rotation &r = x.r;
+    Ref q_out(result(v[9], v[0], x.q, {r.n, r.heads, r.d}, at::kBFloat16, "q_out"));
+    Ref k_out = x.k ? Ref(result(v[10], v[0], x.q, {r.n, r.kv_heads, r.d}, at::kBFloat16, "k_out")) : none();
+    const void *q = x.q.data_ptr(), *k = x.k ? x.k->data_ptr() : nullptr;
+    void *po = data(q_out), *ko = x.k ? data(k_out) : nullptr;
+    call("st_attn_rotate", [&](void *s) { return api.attn_rotate(&r, q, k, x.positions, x.freq, x.q_weight, x.k_weight, po, ko, s); });
+    return pair(std::move(q_out), std::move(k_out));
+}
+
+// q, k, dq_out, dk_out, positions, freq, interleaved, q_weight, k_weight, eps, factor, dq, dk, dq_weight, dk_weight, ws
+PyObject *py_attn_rotate_grad(PyObject *const *v)
+{
+    const Guard guard(cuda_tensor(v[0], "q").device());
+    const Rotation x = rotation(v[0], v[1], v + 4);
+    const st_rotation &r = x.r;
+    const at::Tensor &dqo = contiguous(x.q, v[2], at::kBFloat16, "dq_out");
+    want_shape(dqo, {r.n, r.heads, r.d}, "dq_out");
+    if (!x.k != (v[3] == Py_None)) fail(PyExc_ValueError, "k and dk_out belong together");
+    const void *q = x.q.data_ptr(), *k = x.k ? x.k->data_ptr() : nullptr, *pdq = dqo.data_ptr(), *pdk = nullptr;
+    if (x.k) {
+        const at::Tensor &dko = contiguous(x.q, v[3], at::kBFloat16, "dk_out");
+        want_shape(dko, {r.n, r.kv_heads, r.d}, "dk_out");
+        pdk = dko.data_ptr();
+    }
+    Ref dq(result(v[11], v[0], x.q, {r.n, r.heads, r.d}, at::kBFloat16, "dq"));
+    Ref dk = x.k ? Ref(result(v[12], v[0], x.q, {r.n, r.kv_heads, r.d}, at::kBFloat16, "dk")) : none();
+    Ref dqw = x.q_weight ? Ref(result(v[13], v[0], x.q, {r.d}, at::kFloat, "dq_weight")) : none();
+    Ref dkw = x.k_weight ? Ref(result(v[14], v[0], x.q, {r.d}, at::kFloat, "dk_weight")) : none();
+    const Workspace w = workspace(v[15], v[0], x.q, ST_OP_ATTN_ROTATE_GRAD, x.q_weight || x.k_weight ? r.d : 0, 0, 0, 0, 0);
+    void *po = data(dq), *ko = x.k ? data(dk) : nullptr;
+    float *pqw = x.q_weight ? (float *)data(dqw) : nullptr, *pkw = x.k_weight ? (float *)data(dkw) : nullptr;
+    call("st_attn_rotate_grad", [&](void *s) {
+        return api.attn_rotate_grad(&r, q, k, pdq, pdk, x.positions, x.freq, x.q_weight, x.k_weight, po, ko, pqw, pkw, w.ptr, w.bytes, s);
+    });
+    return PyTuple_Pack(4, dq.o, dk.o, dqw.o, dkw.o);
+}
+
+// ---- caches in cells ------------------------------------------------------------------
+
+struct CellTensors {
+    st_cells c;
+    void *k, *v, *k_scales, *v_scales;
+    const int32_t *table, *lens;
+};
+
+// A tensor of `dims` dimensions, of which the last `whole` ones lie without gaps.
+const at::Tensor &dense_tail(const at::Tensor &x, PyObject *o, at::ScalarType type, int64_t dims, int64_t whole, const char *name)
+{
+    const at::Tensor &t = cuda_tensor(o, name);
+    want_device_of(x, t, name);
+    if (t.scalar_type() != type) {
+        PyErr_Format(PyExc_TypeError, "%s has the wrong type", name);
+        throw Failed();
+    }
+    if (t.dim() != dims) {
+        PyErr_Format(PyExc_ValueError, "%s must have %lld dimensions", name, (long long)dims);
+        throw Failed();
+    }
+    int64_t want = 1;
+    for (int64_t i = dims - 1; i >= dims - whole; --i) {
+        if (t.size(i) != 1 && t.stride(i) != want) {
+            PyErr_Format(PyExc_ValueError, "the last dimension of %s must be contiguous", name);
+            throw Failed();
+        }
+        want *= t.size(i);
+    }
+    return t;
+}
+
+// k_pages, v_pages, table, lens, k_scales, v_scales; heads and d of what meets them
+CellTensors cell_tensors(const at::Tensor &x, PyObject *pk, PyObject *pv, PyObject *ptable, PyObject *plens, PyObject *pks, PyObject *pvs, int64_t heads, int64_t d)
+{
+    const at::Tensor &k = cuda_tensor(pk, "k_pages");
+    const at::ScalarType type = k.scalar_type();
+    if (type != at::kBFloat16 && type != at::kChar && type != at::kByte) fail(PyExc_TypeError, "k_pages must be bfloat16, int8 or uint8 (two cells of 4 bits)");
+    dense_tail(x, pk, type, 4, 1, "k_pages");
+    const at::Tensor &v = dense_tail(x, pv, type, 4, 1, "v_pages");
+    if (v.sizes() != k.sizes()) fail(PyExc_ValueError, "v_pages has the wrong shape");
+    if (v.strides() != k.strides()) fail(PyExc_ValueError, "k_pages and v_pages must have the same strides");
+    CellTensors r = {};
+    st_cells &c = r.c;
+    c.dtype = type == at::kBFloat16 ? ST_BF16 : type == at::kChar ? ST_I8 : ST_I4;
+    const int64_t cols = c.dtype == ST_I4 ? 2 * k.size(3) : k.size(3), bytes = k.element_size();
+    if (d >= 0 && cols != d) fail(PyExc_ValueError, "k_pages has the wrong shape");
+    const at::Tensor &table = contiguous(x, ptable, at::kInt, "table"), &lens = contiguous(x, plens, at::kInt, "lens");
+    if (lens.dim() != 1 || table.dim() != 2 || table.size(0) != lens.size(0)) fail(PyExc_ValueError, "table must have one row for every sequence");
+    c.nseq = lens.size(0);
+    c.kv_heads = k.size(2);
+    c.heads = heads >= 0 ? heads : c.kv_heads;
+    c.d = cols;
+    c.pages = k.size(0);
+    c.page = k.size(1);
+    c.table_cols = table.size(1);
+    c.page_stride = k.stride(0) * bytes;
+    c.token_stride = k.stride(1) * bytes;
+    c.head_stride = k.stride(2) * bytes;
+    r.k = k.data_ptr();
+    r.v = v.data_ptr();
+    r.table = (const int32_t *)table.data_ptr();
+    r.lens = (const int32_t *)lens.data_ptr();
+    if (c.dtype == ST_BF16) {
+        if (pks != Py_None || pvs != Py_None) fail(PyExc_ValueError, "bfloat16 pages have no scales");
+        return r;
+    }
+    // float32 [pages, page, heads], or bfloat16 [pages, page, heads, groups, 2] in units of two
+    const bool four = c.dtype == ST_I4;
+    const at::ScalarType scale_type = four ? at::kBFloat16 : at::kFloat;
+    const at::Tensor &ks = dense_tail(x, pks, scale_type, four ? 5 : 3, four ? 2 : 0, "k_scales"), &vs = dense_tail(x, pvs, scale_type, four ? 5 : 3, four ? 2 : 0, "v_scales");
+    if (four) want_shape(ks, {c.pages, c.page, c.kv_heads, (c.d + 31) / 32, 2}, "k_scales");
+    else want_shape(ks, {c.pages, c.page, c.kv_heads}, "k_scales");
+    want_shape(vs, ks.sizes(), "v_scales");
+    if (ks.strides() != vs.strides()) fail(PyExc_ValueError, "k_scales and v_scales must have the same strides");
+    int64_t *const to[3] = {&c.scale_page, &c.scale_token, &c.scale_head};
+    for (int i = 0; i < 3; ++i) {
+        if (four && ks.size(i) != 1 && ks.stride(i) % 2 != 0) fail(PyExc_ValueError, "strides of k_scales and v_scales must be even");
+        *to[i] = four ? ks.stride(i) / 2 : ks.stride(i);
+    }
+    r.k_scales = ks.data_ptr();
+    r.v_scales = vs.data_ptr();
+    return r;
+}
+
+// Offsets of rows, one more than there are sequences, or None: a row for every sequence, or one sequence of all rows.
+const int32_t *row_offsets(const at::Tensor &x, PyObject *o, const st_cells &c, int64_t n)
+{
+    int64_t nseq = 0;
+    if (o == Py_None) {
+        if (c.nseq != 1 && c.nseq != n) fail(PyExc_ValueError, "offsets are needed where there is not one row for every sequence");
+        return nullptr;
+    }
+    const int32_t *p = offsets_of(x, o, "offsets", &nseq);
+    if (nseq != c.nseq) fail(PyExc_ValueError, "offsets must have one entry more than there are sequences");
+    return p;
+}
+
+// k, v, k_pages, v_pages, table, lens, offsets, k_scales, v_scales, ws
+PyObject *py_attn_cache_write(PyObject *const *v)
+{
+    const at::Tensor &k = cuda_tensor(v[0], "k");
+    const Guard guard(k.device());
+    table(k, v[0], "k", 3);
+    const at::Tensor &vv = table(k, v[1], "v", 3);
+    want_shape(vv, k.sizes(), "v");
+    const CellTensors x = cell_tensors(k, v[2], v[3], v[4], v[5], v[7], v[8], -1, k.size(2));
+    if (x.c.kv_heads != k.size(1)) fail(PyExc_ValueError, "k_pages has the wrong shape");
+    st_tokens t = {};
+    t.dtype = ST_BF16;
+    t.nseq = x.c.nseq;
+    t.nk = k.size(0);
+    t.kv_heads = k.size(1);
+    t.d = t.dv = k.size(2);
+    t.k_row = k.stride(0);
+    t.k_head = k.stride(1);
+    t.v_row = vv.stride(0);
+    t.v_head = vv.stride(1);
+    const int32_t *at = row_offsets(k, v[6], x.c, t.nk);
+    const Workspace w = workspace(v[9], v[0], k, ST_OP_ATTN_CACHE, 0, 0, 0, 0, 0);
+    const void *pk = k.data_ptr(), *pv = vv.data_ptr();
+    call("st_attn_cache_write", [&](void *s) { return api.attn_cache_write(&x.c, &t, pk, pv, x.table, x.lens, at, x.k, x.v, x.k_scales, x.v_scales, w.ptr, w.bytes, s); });
+    Py_RETURN_NONE;
+}
+
+// k_pages, v_pages, table, lens, offsets, rows, k_scales, v_scales, k, v, ws
+PyObject *py_attn_cache_read(PyObject *const *v)
+{
+    const at::Tensor &kp = cuda_tensor(v[0], "k_pages");
+    const Guard guard(kp.device());
+    const CellTensors x = cell_tensors(kp, v[0], v[1], v[2], v[3], v[6], v[7], -1, -1);
+    const int64_t n = integer(v[5]);
+    if (n <= 0) fail(PyExc_ValueError, "rows must be positive");
+    const int32_t *at = row_offsets(kp, v[4], x.c, n);
+    // new tensors are bfloat16, whatever the pages are
+    auto rows = [&](PyObject *given, const char *name) -> PyObject * {
+        if (given != Py_None) return result(given, v[0], kp, {n, x.c.kv_heads, x.c.d}, at::kBFloat16, name);
+        return allocate(v[0], kp, {n, x.c.kv_heads, x.c.d}, at::kBFloat16, dtype_bf16);
+    };
+    Ref k(rows(v[8], "k")), vv(rows(v[9], "v"));
+    const Workspace w = workspace(v[10], v[0], kp, ST_OP_ATTN_CACHE, 0, 0, 0, 0, 0);
+    void *pk = data(k), *pv = data(vv);
+    call("st_attn_cache_read", [&](void *s) { return api.attn_cache_read(&x.c, n, x.k, x.v, x.k_scales, x.v_scales, x.table, x.lens, at, pk, pv, w.ptr, w.bytes, s); });
+    return pair(std::move(k), std::move(vv));
+}
+
+// q, k_pages, v_pages, table, lens, window, sinks, k_scales, v_scales, scale, out, ws
+PyObject *py_attn_cache_step(PyObject *const *v)
+{
+    const at::Tensor &q = cuda_tensor(v[0], "q");
+    const Guard guard(q.device());
+    table(q, v[0], "q", 3);
+    const CellTensors x = cell_tensors(q, v[1], v[2], v[3], v[4], v[7], v[8], q.size(1), q.size(2));
+    if (x.c.nseq != q.size(0)) fail(PyExc_ValueError, "table must have one row for every sequence");
+    const int64_t window = count_of(v[5]), sinks = count_of(v[6]);
+    const float scale = scale_of(v[9], x.c.d);
+    Ref out(result(v[10], v[0], q, q.sizes(), at::kBFloat16, "out"));
+    const Workspace w = workspace(v[11], v[0], q, ST_OP_ATTN_CACHE, 0, 0, 0, 0, 0);
+    const void *pq = q.data_ptr();
+    const int64_t row = q.stride(0), head = q.stride(1);
+    void *po = data(out);
+    call("st_attn_cache_step", [&](void *s) {
+        return api.attn_cache_step(&x.c, pq, row, head, x.k, x.v, x.k_scales, x.v_scales, x.table, x.lens, window, sinks, scale, po, w.ptr, w.bytes, s);
+    });
+    return out.release();
+}
+
+// q, k_pages, v_pages, prefix_table, prefix_lens, table, lens, group_offsets, scale, out, ws
+PyObject *py_attn_shared_step(PyObject *const *v)
+{
+    const at::Tensor &q = cuda_tensor(v[0], "q");
+    const Guard guard(q.device());
+    table(q, v[0], "q", 3);
+    want_bf16(cuda_tensor(v[1], "k_pages"), "k_pages");
+    const CellTensors x = cell_tensors(q, v[1], v[2], v[5], v[6], Py_None, Py_None, q.size(1), q.size(2));
+    if (x.c.nseq != q.size(0)) fail(PyExc_ValueError, "table must have one row for every sequence");
+    const at::Tensor &ptable = contiguous(q, v[3], at::kInt, "prefix_table"), &plens = contiguous(q, v[4], at::kInt, "prefix_lens");
+    if (plens.dim() != 1 || ptable.dim() != 2 || ptable.size(0) != plens.size(0)) fail(PyExc_ValueError, "prefix_table must have one row for every group");
+    const int64_t groups = plens.size(0), cols = ptable.size(1);
+    int64_t told = 1;
+    const int32_t *at = offsets_of(q, v[7], "group_offsets", &told);
+    if (told != groups) fail(PyExc_ValueError, "group_offsets must have one entry more than there are groups");
+    const float scale = scale_of(v[8], x.c.d);
+    Ref out(result(v[9], v[0], q, q.sizes(), at::kBFloat16, "out"));
+    const Workspace w = workspace(v[10], v[0], q, ST_OP_ATTN_SHARED_STEP, x.c.nseq, x.c.heads, x.c.kv_heads, groups, 0);
+    const void *pq = q.data_ptr();
+    const int64_t row = q.stride(0), head = q.stride(1);
+    const int32_t *pt = (const int32_t *)ptable.data_ptr(), *pl = (const int32_t *)plens.data_ptr();
+    void *po = data(out);
+    call("st_attn_shared_step", [&](void *s) {
+        return api.attn_shared_step(&x.c, pq, row, head, x.k, x.v, pt, cols, pl, groups, at, x.table, x.lens, scale, po, w.ptr, w.bytes, s);
+    });
+    return out.release();
+}
+
 // Argument count, and C++ errors as Python ones.
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
@@ -839,11 +1155,11 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
     return nullptr;
 }
 
-// bind(addresses: dict name -> int, StError, torch.float32, torch.uint8, last_ws: dict)
+// bind(addresses: dict name -> int, StError, torch.float32, torch.uint8, torch.bfloat16, last_ws: dict)
 PyObject *py_bind(PyObject *, PyObject *args)
 {
-    PyObject *table, *err, *f32, *u8, *last;
-    if (!PyArg_ParseTuple(args, "O!OOOO!", &PyDict_Type, &table, &err, &f32, &u8, &PyDict_Type, &last)) return nullptr;
+    PyObject *table, *err, *f32, *u8, *b16, *last;
+    if (!PyArg_ParseTuple(args, "O!OOOOO!", &PyDict_Type, &table, &err, &f32, &u8, &b16, &PyDict_Type, &last)) return nullptr;
     Api a;
     const struct { const char *name; void *slot; } want[] = {
         {"st_packed_elems", &a.packed_elems}, {"st_dense_elems", &a.dense_elems}, {"st_workspace_bytes", &a.workspace_bytes},
@@ -852,7 +1168,9 @@ PyObject *py_bind(PyObject *, PyObject *args)
         {"st_sym_moment4", &a.sym_moment4}, {"st_mttkrp_tri", &a.mttkrp_tri}, {"st_mttkrp_slice", &a.mttkrp_slice},
         {"st_ttm_blockdiag", &a.ttm_blockdiag}, {"st_ttm_packed", &a.ttm_packed}, {"st_attn_window", &a.attn_window},
         {"st_attn_window_grad", &a.attn_window_grad}, {"st_attn_window_step", &a.attn_window_step}, {"st_attn_decay", &a.attn_decay},
-        {"st_attn_decay_grad", &a.attn_decay_grad}, {"st_attn_decay_step", &a.attn_decay_step}};
+        {"st_attn_decay_grad", &a.attn_decay_grad}, {"st_attn_decay_step", &a.attn_decay_step}, {"st_attn_rotate", &a.attn_rotate},
+        {"st_attn_rotate_grad", &a.attn_rotate_grad}, {"st_attn_cache_write", &a.attn_cache_write}, {"st_attn_cache_read", &a.attn_cache_read},
+        {"st_attn_cache_step", &a.attn_cache_step}, {"st_attn_shared_step", &a.attn_shared_step}};
     for (const auto &w : want) {
         PyObject *v = PyDict_GetItemString(table, w.name);
         void *p = v ? PyLong_AsVoidPtr(v) : nullptr;
@@ -862,10 +1180,11 @@ PyObject *py_bind(PyObject *, PyObject *args)
         }
         std::memcpy(w.slot, &p, sizeof(p));
     }
-    for (PyObject *o : {err, f32, u8, last}) Py_INCREF(o);
+    for (PyObject *o : {err, f32, u8, b16, last}) Py_INCREF(o);
     error_class = err;
     dtype_f32 = f32;
     dtype_u8 = u8;
+    dtype_bf16 = b16;
     last_ws = last;
     api = a;
     Py_RETURN_NONE;
@@ -886,7 +1205,8 @@ PyMethodDef methods[] = {
     ENTRY(pack, 3), ENTRY(unpack, 4), ENTRY(thp, 4), ENTRY(axpby, 5), ENTRY(mul, 3), ENTRY(moment2, 4), ENTRY(moment3, 4),
     ENTRY(moment4, 4), ENTRY(mttkrp_tri, 6), ENTRY(mttkrp_slice, 9), ENTRY(ttm_blockdiag, 7), ENTRY(ttm_packed, 6),
     ENTRY(attn_window, 11), ENTRY(attn_window_grad, 15), ENTRY(attn_window_step, 12), ENTRY(attn_decay, 10), ENTRY(attn_decay_grad, 14),
-    ENTRY(attn_decay_step, 7),
+    ENTRY(attn_decay_step, 7), ENTRY(attn_rotate, 11), ENTRY(attn_rotate_grad, 16), ENTRY(attn_cache_write, 10), ENTRY(attn_cache_read, 11),
+    ENTRY(attn_cache_step, 12), ENTRY(attn_shared_step, 11),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

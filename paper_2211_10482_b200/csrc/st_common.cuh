@@ -37,6 +37,7 @@ __device__ __forceinline__ bool st_bounds_ok(long long idx, long long n, unsigne
 // sites: 1 pack/unpack copy, 2 second-moment reductions, 3 third-moment partial sums, 4 tensor-core third moment,
 // 5 MTTKRP partial slots, 6 MTTKRP row sums, 7 fourth-moment gather, 8 TTM rows
 
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool aligned256(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
