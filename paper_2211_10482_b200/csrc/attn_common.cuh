@@ -70,6 +70,42 @@ inline int clamp_int(int64_t x, int most = 1 << 29) { return x > most ? most : (
 
 #if defined(__CUDACC__)
 
+// Two fp32 at a time.
+struct Pair {
+    uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float lo, float hi)
+{
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ Pair pair(uint32_t lo, uint32_t hi) { return pair(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ float2 split(Pair a)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ Pair mul(Pair a, Pair b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair add(Pair a, Pair b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
 // Eight bf16 as floats and back, rounded once.
 __device__ __forceinline__ void unpack8(const uint4 &u, float (&x)[8])
 {
@@ -86,6 +122,25 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8])
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ void unpack8(const uint4 &u, Pair (&x)[4])
+{
+    x[0] = pair(u.x << 16, u.x & 0xFFFF0000u);
+    x[1] = pair(u.y << 16, u.y & 0xFFFF0000u);
+    x[2] = pair(u.z << 16, u.z & 0xFFFF0000u);
+    x[3] = pair(u.w << 16, u.w & 0xFFFF0000u);
+}
+__device__ __forceinline__ uint4 pack8(const Pair (&x)[4])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = split(x[i]);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
         w[i] = *reinterpret_cast<const uint32_t *>(&b);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);

@@ -1,13 +1,15 @@
 // st_attn_rotate and its gradient: an RMS norm of every head and a rotation of pairs of its columns, in one pass.
 //
-// Bound by memory: a result is 8 multiplications and additions for each 4 bytes (8 for each 8 in the gradient).  16 lanes own a row (one head of
-// one token), each 8 of its columns: 16 bytes.  A block has T tokens and C of their heads of q and k; the angles of its T tokens, which all heads
-// share, are turned into sines and cosines once, while the block's first rows are on their way: in fp64 up to the fraction of a turn
-// (position freq / 2 pi reaches 2^17 turns and more, where fp32 has no digits left for the fraction), then in fp32.
+// Bound by memory as long as a row (one head of one token) takes few instructions.  8 lanes (4 up to 64 columns) own a row, each 16 of its columns as two
+// pieces of 16 bytes which hold both columns of eight pairs, whichever way they are paired: a lane turns its pairs by itself, two at a time in packed fp32.  A
+// warp takes a token, or some of its heads.  Its lanes make the sines and cosines of two of its angles each, all others take them by shuffles, once for all
+// heads.  An angle is position freq / 2 pi turns, of which only the fraction counts: with freq / 2 pi as a fraction of 2^64, the product's low 64 bits are
+// that fraction of a turn, exactly, for any position; the nearest quarter of a turn is its top two bits, and the rest, at most pi / 4, goes into the Taylor
+// series of sine and cosine (their next terms are below 2^-25).  Rows come by asynchronous copies to a ring of the warp's own, over the ends of tokens and of q.
 //
-// The gradient's blocks take several tiles in turn and keep the weights' sums in registers; a second kernel adds the blocks' sums in a
-// fixed order.
+// The gradient's warps keep the weights' sums in registers; a second kernel adds the blocks' sums in a fixed order.
 #include "attn_common.cuh"
+#include "tc_common.cuh"
 
 namespace st {
 namespace attn {
@@ -23,174 +25,376 @@ struct RotateArgs {
     bool weight_f32;
     int n, heads, width, d, rot;           // width: heads of q and k
     float eps, factor;
-    int tokens, cols, col_tiles;           // of a tile
-    int64_t tiles;
+    int cols, chunks, items;               // heads of an item, items of a token, items
     float *part;                           // [block][q, k][128] sums of the weights' gradient, or NULL
 };
 
 namespace rot {
-constexpr int THREADS = 256, LANES = 16, ROWS = THREADS / LANES;      // rows that a block has in hand at a time
-enum Pairs { HALF = 0, INTERLEAVED = 1, HALF_ODD = 2 };               // HALF_ODD: a half that is no whole number of lanes
-constexpr int MAX_D = 128;
+constexpr int MAX_D = 128, WEIGHTS = 2 * 4 * 16;      // pieces of the weights in shared memory
+ST_HD constexpr int warps(bool grad) { return grad ? 6 : 8; }                            // of a block
+ST_HD constexpr int min_blocks(bool odd, bool grad) { return odd || grad ? 2 : 3; }       // on an SM
+ST_HD constexpr int ahead(bool grad) { return grad ? 4 : 4; }                            // rows of a lane on their way
 }  // namespace rot
 
-// Sum over the 16 lanes of a row, the same in all of them.
+// Sum over the lanes of a row, the same in all of them.
+template <int LANES>
 __device__ __forceinline__ float row_sum(float x)
 {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+    for (int o = LANES / 2; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
     return x;
 }
+__device__ __forceinline__ void copy_piece(uint32_t dst, const void *src, bool there)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst), "l"(src), "r"((int)there) : "memory");
+}
+// Cosines and sines of two angles, given as fractions of 2^32 turns.
+__device__ __forceinline__ void cos_sin(uint32_t t0, uint32_t t1, float (&c)[2], float (&s)[2])
+{
+    const uint32_t q0 = t0 + 0x20000000u, q1 = t1 + 0x20000000u;          // top two bits: the nearest quarter
+    constexpr float unit = 1.4629180792671596e-9f;                         // 2 pi / 2^32
+    const Pair x = pair((float)(int)(t0 - (q0 & 0xC0000000u)) * unit, (float)(int)(t1 - (q1 & 0xC0000000u)) * unit), y = mul(x, x);
+    auto all = [](float v) { return pair(v, v); };
+    const Pair si = fma(mul(x, y), fma(y, fma(y, fma(y, all(1.f / 362880), all(-1.f / 5040)), all(1.f / 120)), all(-1.f / 6)), x);
+    const Pair co = fma(y, fma(y, fma(y, fma(y, all(1.f / 40320), all(-1.f / 720)), all(1.f / 24)), all(-0.5f)), all(1.f));
+    const float2 ss = split(si), cc = split(co);
+    const uint32_t q[2] = {q0, q1};
+    const float sv[2] = {ss.x, ss.y}, cv[2] = {cc.x, cc.y};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        // quarters 0..3: (c, s), (-s, c), (-c, -s), (s, -c)
+        const bool odd = q[i] & 0x40000000u;
+        const float a = odd ? sv[i] : cv[i], b = odd ? cv[i] : sv[i];
+        c[i] = __uint_as_float(__float_as_uint(a) ^ ((q[i] ^ (q[i] << 1)) & 0x80000000u));
+        s[i] = __uint_as_float(__float_as_uint(b) ^ (q[i] & 0x80000000u));
+    }
+}
+// Eight pairs from two pieces of a row: first columns in a, second ones in b.
+template <bool INTER>
+__device__ __forceinline__ void pairs_of(const uint4 &p, const uint4 &q, Pair (&a)[4], Pair (&b)[4])
+{
+    if (!INTER) {
+        unpack8(p, a);
+        unpack8(q, b);
+    } else {
+        const uint32_t w[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = pair(w[2 * i] << 16, w[2 * i + 1] << 16);
+            b[i] = pair(w[2 * i] & 0xFFFF0000u, w[2 * i + 1] & 0xFFFF0000u);
+        }
+    }
+}
+template <bool INTER>
+__device__ __forceinline__ void pieces_of(const Pair (&a)[4], const Pair (&b)[4], uint4 &p, uint4 &q)
+{
+    if (!INTER) {
+        p = pack8(a);
+        q = pack8(b);
+    } else {
+        Pair x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = split(a[i]), g = split(b[i]);
+            (i < 2 ? x[2 * i] : y[2 * i - 4]) = pair(f.x, g.x);
+            (i < 2 ? x[2 * i + 1] : y[2 * i - 3]) = pair(f.y, g.y);
+        }
+        p = pack8(x);
+        q = pack8(y);
+    }
+}
 
-// R rows of each group of 16 lanes: rows g R .. g R + R - 1 of the tile, so that a group's rows share their token's angles.
-template <int R, bool NORM, int PAIRS, bool GRAD>
-__global__ void __launch_bounds__(rot::THREADS) rotate_kernel(const RotateArgs a)
+// LANES to a row; ODD: `rot` is no multiple of 16, so that pieces and pairs do not fit together and columns are taken one by one.
+template <int LANES, bool NORM, bool INTER, bool ODD, bool GRAD>
+__global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GRAD)) rotate_kernel(const RotateArgs a)
 {
     using namespace rot;
-    extern __shared__ __align__(16) float smem[];
-    float *weights = smem;                                 // [q, k][128]
-    float *turns = smem + (NORM ? 2 * MAX_D : 0);          // [token][cosines, sines][rot / 2]
-    const int lane = threadIdx.x & 31, group = threadIdx.x / LANES, e0 = (threadIdx.x % LANES) * 8, half = a.rot / 2;
-    const bool inside = e0 < a.d;
-    // the other half's columns are in another lane; a lane without any meets itself
-    const int there = PAIRS == HALF && e0 < a.rot ? (e0 < half ? lane + half / 8 : lane - half / 8) : lane;
-    const int p0 = PAIRS == INTERLEAVED ? e0 / 2 : e0 < half ? e0 : e0 - half;       // first pair of this lane
-    const int stride = (half + 3) / 4 * 4;                 // of a token's cosines: whole 16-byte pieces
-    float dw[2][8];
-    if (GRAD && NORM)
+    constexpr int ROWS = 32 / LANES, AHEAD = rot::ahead(GRAD), WARPS = rot::warps(GRAD);
+    constexpr bool TWO = GRAD && NORM;                     // tables that are read: x and dy, or one of them
+    constexpr int TABLE = ODD ? 32 : 64, STAGE = TABLE * (TWO ? 2 : 1);       // pieces of a step
+    extern __shared__ __align__(16) uint4 smem[];
+    float4(*weights)[4][LANES] = reinterpret_cast<float4(*)[4][LANES]>(smem);      // [q, k][a's pairs 0..3, 4..7, b's][lane of a row]
+    uint4 *ring = smem + (NORM ? WEIGHTS : 0);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES, half = a.rot / 2;
+    uint4 *mine = ring + warp * AHEAD * STAGE;
+    // A lane's pieces begin at columns a0 and b0, both of which are next to its neighbours': pairs in halves 8 l .. 8 l + 7, then the lanes whose columns do
+    // not turn; neighbours 8 columns each of the row's halves.  p0 and p1: the first pairs of a0..7 and b0..7.
+    const int turning = (half + 7) / 8, resting = (a.d - a.rot + 15) / 16;
+    const bool turns = l < turning;                        // halves
+    const int a0 = INTER || turns ? 8 * l : a.rot + 8 * (l - turning) + (ODD ? 8 * (l - turning) : 0);
+    const int b0 = INTER ? 8 * (l + LANES) : turns ? half + 8 * l : a0 + (ODD ? 8 : l - turning < resting ? 8 * resting : MAX_D);
+    const bool turn_a = ODD || (INTER ? a0 < a.rot : turns), turn_b = ODD || (INTER ? b0 < a.rot : turns);
+    const bool in_a = a0 < a.d && (INTER || turns || l - turning < resting), in_b = b0 < a.d;
+    // columns of pair e
+    auto col_a = [&](int e) { return INTER ? (ODD ? 16 * l + 2 * e : (e < 4 ? a0 : b0 - 8) + 2 * e) : a0 + e; };
+    auto col_b = [&](int e) { return INTER ? col_a(e) + 1 : b0 + e; };
+    auto has_a = [&](int e) { return ODD ? col_a(e) < (!INTER && turns ? half : a.d) : INTER && e >= 4 ? in_b : in_a; };
+    auto has_b = [&](int e) { return ODD ? col_b(e) < (!INTER && turns ? a.rot : a.d) : INTER && e < 4 ? in_a : in_b; };
+    // this lane's angles, of pairs 2 lane and 2 lane + 1, as fractions of 2^64 turns a position
+    uint64_t turn[2] = {0, 0};
+    const float inv_d = 1.f / a.d;
+    Pair dwa[2][4], dwb[2][4];
+    if (TWO)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dw[0][e] = dw[1][e] = 0.f;
+        for (int e = 0; e < 4; ++e) dwa[0][e] = dwa[1][e] = dwb[0][e] = dwb[1][e] = pair(0.f, 0.f);
 
+#pragma unroll
+    for (int i = 0; i < AHEAD * STAGE / 32; ++i) mine[i * 32 + lane] = make_uint4(0u, 0u, 0u, 0u);      // what no copy reaches
     pdl_wait();
     pdl_trigger();
-    if (NORM)
-        for (int i = threadIdx.x; i < 2 * MAX_D; i += THREADS) {
-            const void *w = i < MAX_D ? a.q_weight : a.k_weight;
-            const int e = i % MAX_D;
-            weights[i] = e >= a.d ? 0.f : !w ? 1.f : a.weight_f32 ? ((const float *)w)[e] : __bfloat162float(((const bf16 *)w)[e]);
-        }
-    for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-        const int t0 = (int)(tile / a.col_tiles) * a.tokens, c0 = (int)(tile % a.col_tiles) * a.cols;
-        const int nt = min(a.tokens, a.n - t0), nc = min(a.cols, a.width - c0);
-        // the rows on their way
-        uint4 x[R], y[R];
-        float other[PAIRS == HALF_ODD ? R : 1][8];
-        int token[R], col[R];
+    float freq[2];
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int row = group * R + j;
-            token[j] = row / a.cols;
-            col[j] = row - token[j] * a.cols;
-            const bool in = token[j] < nt && col[j] < nc;
-            if (!in) token[j] = -1;
-            const int h = c0 + col[j], t = t0 + token[j];
-            const bool is_q = h < a.heads;
-            const bf16 *src = is_q ? a.q + t * a.q_row + h * a.q_head : a.k + t * a.k_row + (h - a.heads) * a.k_head;
-            const bf16 *dy = is_q ? a.dq_out + ((int64_t)t * a.heads + h) * a.d : a.dk_out + ((int64_t)t * (a.width - a.heads) + h - a.heads) * a.d;
-            x[j] = (NORM || !GRAD) && in && inside ? *reinterpret_cast<const uint4 *>(src + e0) : make_uint4(0u, 0u, 0u, 0u);
-            if (GRAD) y[j] = in && inside ? *reinterpret_cast<const uint4 *>(dy + e0) : make_uint4(0u, 0u, 0u, 0u);
-            if (PAIRS == HALF_ODD)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i = e0 + e;
-                    other[j][e] = in && i < a.rot ? __bfloat162float((GRAD ? dy : src)[i < half ? i + half : i - half]) : 0.f;
+    for (int i = 0; i < 2; ++i) freq[i] = 2 * lane + i < half ? a.freq[2 * lane + i] : 0.f;
+    const int kv_heads = a.width - a.heads;
+    // Heads q0.. of nq of q and k0.. of nk of k of a token: an item.
+    struct Item {
+        int t, q0, nq, k0, nk;
+    };
+    auto item_of = [&](int i) {
+        if (a.chunks == 1) return Item{i, 0, a.heads, 0, kv_heads};
+        const int t = i / a.chunks, c0 = (i - t * a.chunks) * a.cols, c1 = min(c0 + a.cols, a.width);
+        const int q0 = min(c0, a.heads), k0 = max(c0, a.heads);
+        return Item{t, q0, min(c1, a.heads) - q0, k0 - a.heads, max(c1 - k0, 0)};
+    };
+    const int hop = gridDim.x * WARPS, begin = blockIdx.x * WARPS + warp;
+    // What is fetched next: rows `f_left` and on of a table's heads (q's, then k's) of item f_item.
+    int f_item = begin, f_left = 0, f_stage = 0;
+    bool f_k = true;                                       // k's heads are what is fetched
+    const bf16 *f_x = nullptr, *f_dy = nullptr;
+    int64_t f_hop = 0;
+    auto fetch = [&] {
+        if (f_left <= 0) {                                 // the next table with rows, if there is one
+            if (f_x) {
+                if (f_k) f_item += hop;
+                f_k = !f_k;
+            } else {
+                f_k = false;
+            }
+            while (f_item < a.items) {
+                const Item f = item_of(f_item);
+                f_left = f_k ? f.nk : f.nq;
+                if (f_left > 0) {
+                    const int h = (f_k ? f.k0 : f.q0) + sub;
+                    const int64_t head = f_k ? a.k_head : a.q_head;
+                    f_x = (f_k ? a.k + f.t * a.k_row : a.q + f.t * a.q_row) + h * head;
+                    f_hop = ROWS * head;
+                    if (GRAD) f_dy = (f_k ? a.dk_out + (int64_t)f.t * kv_heads * a.d : a.dq_out + (int64_t)f.t * a.heads * a.d) + h * a.d;
+                    break;
                 }
+                if (f_k) f_item += hop;
+                f_k = !f_k;
+            }
         }
-        for (int i = threadIdx.x; i < nt * half; i += THREADS) {
-            const int t = i / half, p = i - t * half;
-            // the fraction of a turn, -1/2 to 1/2
-            const double turn = (double)a.positions[t0 + t] * ((double)a.freq[p] * 0.15915494309189533577);
-            float s, c;
-            sincospif(2.f * (float)(turn - rint(turn)), &s, &c);
-            turns[(2 * t) * stride + p] = a.factor * c;
-            turns[(2 * t + 1) * stride + p] = a.factor * (GRAD ? -s : s);
+        if (f_item < a.items) {
+            // a row that is not there leaves an older one in its place, of which nothing is kept
+            const bool in = sub < f_left, there = in && (ODD ? 8 * l < a.d : in_a), more = in && in_b;
+            const uint32_t to = tc::smem_u32(mine + f_stage * STAGE + lane);
+            if (!GRAD || TWO) {
+                copy_piece(to, f_x + (ODD ? 8 * l : a0), there);
+                if (!ODD) copy_piece(to + 512, f_x + b0, more);
+            }
+            if (GRAD) {
+                copy_piece(to + (TWO ? TABLE * 16 : 0), f_dy + (ODD ? 8 * l : a0), there);
+                if (!ODD) copy_piece(to + (TWO ? TABLE * 16 : 0) + 512, f_dy + b0, more);
+            }
+            f_left -= ROWS;
+            f_x += f_hop;
+            if (GRAD) f_dy += ROWS * a.d;
         }
-        __syncthreads();
-        float c[8], s[8];
-        int held = -1;
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int h = c0 + col[j];
-            const bool is_q = h < a.heads;
-            // cosine and sine of every column, the sine with the sign that its product has: y'[i] = c[i] y[i] + s[i] y[other column of the pair]
-            if (token[j] != held && token[j] >= 0) {
-                held = token[j];
-                const float *at = turns + 2 * held * stride;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool turned = e0 + e < a.rot;
-                    const int p = PAIRS == INTERLEAVED ? p0 + e / 2 : PAIRS == HALF ? p0 + e : e0 + e < half ? e0 + e : e0 + e - half;
-                    const bool first = PAIRS == INTERLEAVED ? e % 2 == 0 : e0 + e < half;
-                    c[e] = turned ? at[p] : 1.f;
-                    s[e] = turned ? (first ? -at[stride + p] : at[stride + p]) : 0.f;
-                }
-            }
-            const float *w = weights + (is_q ? 0 : MAX_D);
-            float v[8], o[8], r = 1.f, z[8];
-            unpack8(x[j], v);
-            if (NORM) {
-                float sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(v[e], v[e], sum);
-                r = rsqrtf(row_sum(sum) / a.d + a.eps);
-            }
-            // what is turned, and the other columns of its pairs
-            const uint4 mine = GRAD ? y[j] : x[j];
-            float u[8];
-            unpack8(mine, u);
-            if (PAIRS == HALF) {
-                const uint4 theirs = make_uint4(__shfl_sync(~0u, mine.x, there), __shfl_sync(~0u, mine.y, there), __shfl_sync(~0u, mine.z, there),
-                                                __shfl_sync(~0u, mine.w, there));
-                unpack8(theirs, o);
-            }
+        if (++f_stage == AHEAD) f_stage = 0;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll 1
+    for (int i = 0; i < AHEAD; ++i) fetch();
+    if (NORM) {
+        // a warp each for the weights of q and k; ones where there are none
+        if (warp < 2 && sub == 0)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int i = e0 + e, pair = PAIRS == INTERLEAVED ? (i ^ 1) : i < half ? i + half : i - half;
-                if (PAIRS == INTERLEAVED) o[e] = u[e ^ 1];
-                if (PAIRS == HALF_ODD) o[e] = other[j][e];
-                if (NORM && !GRAD) {
-                    z[e] = r * fmaf(c[e], u[e] * w[i], s[e] * (i < a.rot ? o[e] * w[pair] : 0.f));
-                } else {
-                    z[e] = i < a.rot ? fmaf(c[e], u[e], s[e] * o[e]) : u[e];
-                }
+                const void *w = warp ? a.k_weight : a.q_weight;
+                auto weight = [&](int col, bool has) { return !w || !has ? 1.f : a.weight_f32 ? ((const float *)w)[col] : __bfloat162float(((const bf16 *)w)[col]); };
+                reinterpret_cast<float *>(&weights[warp][e / 4][l])[e % 4] = weight(col_a(e), has_a(e));
+                reinterpret_cast<float *>(&weights[warp][2 + e / 4][l])[e % 4] = weight(col_b(e), has_b(e));
             }
-            if (GRAD && NORM) {
-                float sum = 0.f;
+        __syncthreads();
+    }
+    int stage = 0, next_position = begin < a.items ? a.positions[item_of(begin).t] : 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] *= r;
-                    if (token[j] >= 0) {
-                        // one of the two is added 0 of what is finite: which head a row is, lanes of a warp may differ in
-                        dw[0][e] += is_q ? z[e] * v[e] : 0.f;
-                        dw[1][e] += is_q ? 0.f : z[e] * v[e];
-                    }
-                    z[e] *= w[e0 + e];
-                    sum = fmaf(z[e], v[e], sum);
-                }
-                sum = row_sum(sum) / a.d;
+    for (int i = 0; i < 2; ++i) {
+        const double t = (double)freq[i] * 0.15915494309189533577;
+        turn[i] = (uint64_t)((t - floor(t)) * 18446744073709551616.0);
+    }
+    for (int i = begin; i < a.items; i += hop) {
+        const Item it = item_of(i);
+        // cosine and sine of every pair: y'[a] = c y[a] - s y[b], y'[b] = c y[b] + s y[a]
+        Pair c[4], s[4], minus_s[4];
+        {
+            const int64_t position = next_position;
+            if (i + hop < a.items) next_position = a.positions[item_of(i + hop).t];
+            float mine_c[2], mine_s[2];
+            cos_sin((uint32_t)((uint64_t)position * turn[0] >> 32), (uint32_t)((uint64_t)position * turn[1] >> 32), mine_c, mine_s);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = r * fmaf(-sum, v[e], z[e]);
+            for (int i = 0; i < 2; ++i) {
+                mine_c[i] *= a.factor;
+                mine_s[i] *= GRAD ? -a.factor : a.factor;
             }
-            if (token[j] >= 0 && inside) {
-                const int64_t t = t0 + token[j];
-                bf16 *dst = is_q ? a.q_out + (t * a.heads + h) * a.d : a.k_out + (t * (a.width - a.heads) + h - a.heads) * a.d;
-                *reinterpret_cast<uint4 *>(dst + e0) = pack8(z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // pairs 8 l + 2 e and the next; neighbours, where the row is in two halves: 4 l + 2 e, and from e = 2 on the second half's
+                const int from = (INTER && !ODD ? 2 * (e < 2 ? l : l + LANES) + (e & 1) : 4 * l + e) & 31;
+                float x[2], y[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    x[i] = __shfl_sync(~0u, mine_c[i], from);
+                    y[i] = __shfl_sync(~0u, mine_s[i], from);
+                }
+                c[e] = pair(x[0], x[1]);
+                s[e] = pair(y[0], y[1]);
+                minus_s[e] = pair(-y[0], -y[1]);
             }
         }
-        if (GRAD) __syncthreads();                         // the next tile's angles take this one's place
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {                      // heads of q, then of k
+            const int first = m ? it.k0 : it.q0, n = m ? it.nk : it.nq;
+            if (n == 0) continue;
+            Pair wa[4], wb[4];
+            if (NORM)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float4 x = weights[m][e][l], y = weights[m][2 + e][l];
+                    wa[2 * e] = pair(x.x, x.y);
+                    wa[2 * e + 1] = pair(x.z, x.w);
+                    wb[2 * e] = pair(y.x, y.y);
+                    wb[2 * e + 1] = pair(y.z, y.w);
+                }
+            bf16 *dst = (m ? a.k_out : a.q_out) + ((int64_t)it.t * (m ? kv_heads : a.heads) + first + sub) * a.d;
+            for (int h = 0; h < n; h += ROWS, dst += ROWS * a.d) {
+                const bool in = h + sub < n;
+                asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+                __syncwarp();
+                const uint4 *x_at = mine + stage * STAGE, *u_at = x_at + (TWO ? TABLE : 0);       // u: what is turned, x or dy
+                Pair xa[4], xb[4], ua[4], ub[4];
+                if (ODD) {
+                    auto column = [&](const uint4 *at, int col, bool has) { return has ? __bfloat162float(reinterpret_cast<const bf16 *>(at + sub * LANES)[col]) : 0.f; };
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        ua[e] = pair(column(u_at, col_a(2 * e), has_a(2 * e)), column(u_at, col_a(2 * e + 1), has_a(2 * e + 1)));
+                        ub[e] = pair(column(u_at, col_b(2 * e), has_b(2 * e)), column(u_at, col_b(2 * e + 1), has_b(2 * e + 1)));
+                        if (TWO) {
+                            xa[e] = pair(column(x_at, col_a(2 * e), has_a(2 * e)), column(x_at, col_a(2 * e + 1), has_a(2 * e + 1)));
+                            xb[e] = pair(column(x_at, col_b(2 * e), has_b(2 * e)), column(x_at, col_b(2 * e + 1), has_b(2 * e + 1)));
+                        }
+                    }
+                    __syncwarp();                          // rows of several lanes: read by all of them before the next copy
+                } else {
+                    pairs_of<INTER>(u_at[lane], u_at[lane + 32], ua, ub);
+                    if (TWO) pairs_of<INTER>(x_at[lane], x_at[lane + 32], xa, xb);
+                }
+                fetch();                                   // into the place that has been read
+                if (++stage == AHEAD) stage = 0;
+                float r = 1.f;
+                if (NORM) {
+                    const Pair *y = TWO ? xa : ua, *z = TWO ? xb : ub;
+                    Pair sum = mul(y[0], y[0]), sum1 = mul(z[0], z[0]);
+#pragma unroll
+                    for (int e = 1; e < 4; ++e) {
+                        sum = fma(y[e], y[e], sum);
+                        sum1 = fma(z[e], z[e], sum1);
+                    }
+                    const float2 two = split(add(sum, sum1));
+                    r = rsqrtf(fmaf(row_sum<LANES>(two.x + two.y), inv_d, a.eps));
+                }
+                if (TWO && !in) {                          // a row that is not there adds nothing to the weights' sums
+                    r = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) xa[e] = xb[e] = ua[e] = ub[e] = pair(0.f, 0.f);
+                }
+                const Pair rr = pair(r, r);
+                if (NORM && !GRAD)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        ua[e] = mul(mul(ua[e], wa[e]), rr);
+                        ub[e] = mul(mul(ub[e], wb[e]), rr);
+                    }
+                // columns that do not turn stay as they are, whatever lies beside them
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    if (!(g ? turn_b : turn_a)) continue;
+#pragma unroll
+                    for (int e = 2 * g; e < 2 * g + 2; ++e) {
+                        const Pair x = fma(minus_s[e], ub[e], mul(c[e], ua[e])), y = fma(s[e], ua[e], mul(c[e], ub[e]));
+                        if (ODD) {
+                            const bool t0 = 8 * l + 2 * e < half, t1 = 8 * l + 2 * e + 1 < half;
+                            const float2 x2 = split(x), y2 = split(y), a2 = split(ua[e]), b2 = split(ub[e]);
+                            ua[e] = pair(t0 ? x2.x : a2.x, t1 ? x2.y : a2.y);
+                            ub[e] = pair(t0 ? y2.x : b2.x, t1 ? y2.y : b2.y);
+                        } else {
+                            ua[e] = x;
+                            ub[e] = y;
+                        }
+                    }
+                }
+                if (TWO) {
+                    Pair sum = pair(0.f, 0.f), sum1 = pair(0.f, 0.f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        xa[e] = mul(xa[e], rr);
+                        xb[e] = mul(xb[e], rr);
+                        dwa[m][e] = fma(ua[e], xa[e], dwa[m][e]);
+                        dwb[m][e] = fma(ub[e], xb[e], dwb[m][e]);
+                        ua[e] = mul(ua[e], wa[e]);
+                        ub[e] = mul(ub[e], wb[e]);
+                        sum = fma(ua[e], xa[e], sum);
+                        sum1 = fma(ub[e], xb[e], sum1);
+                    }
+                    const float2 two = split(add(sum, sum1));
+                    const float mean = -row_sum<LANES>(two.x + two.y) * inv_d;
+                    const Pair mm = pair(mean, mean);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        ua[e] = mul(rr, fma(mm, xa[e], ua[e]));
+                        ub[e] = mul(rr, fma(mm, xb[e], ub[e]));
+                    }
+                }
+                if (ODD) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 x = split(ua[e / 2]), y = split(ub[e / 2]);
+                        if (in && has_a(e)) dst[col_a(e)] = __float2bfloat16(e % 2 ? x.y : x.x);
+                        if (in && has_b(e)) dst[col_b(e)] = __float2bfloat16(e % 2 ? y.y : y.x);
+                    }
+                } else {
+                    uint4 p, q;
+                    pieces_of<INTER>(ua, ub, p, q);
+                    if (in && in_a) *reinterpret_cast<uint4 *>(dst + a0) = p;
+                    if (in && in_b) *reinterpret_cast<uint4 *>(dst + b0) = q;
+                }
+            }
+        }
     }
-    if (GRAD && NORM && a.part) {
-        __shared__ float sums[ROWS][MAX_D];
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (TWO && a.part) {
+        float *sums = reinterpret_cast<float *>(ring);     // [warp][column]
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             __syncthreads();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sums[group][e0 + e] = dw[m][e];
+            for (int e = 0; e < 8; ++e) {
+                const float2 x = split(dwa[m][e / 2]), y = split(dwb[m][e / 2]);
+                float va = e % 2 ? x.y : x.x, vb = e % 2 ? y.y : y.x;
+#pragma unroll
+                for (int o = 16; o >= LANES; o >>= 1) {
+                    va += __shfl_xor_sync(~0u, va, o);
+                    vb += __shfl_xor_sync(~0u, vb, o);
+                }
+                if (sub == 0 && has_a(e)) sums[warp * MAX_D + col_a(e)] = va;
+                if (sub == 0 && has_b(e)) sums[warp * MAX_D + col_b(e)] = vb;
+            }
             __syncthreads();
-            if (threadIdx.x < MAX_D) {
+            if (threadIdx.x < a.d) {
                 float sum = 0.f;
 #pragma unroll
-                for (int g = 0; g < ROWS; ++g) sum += sums[g][threadIdx.x];
+                for (int g = 0; g < WARPS; ++g) sum += sums[g * MAX_D + threadIdx.x];
                 a.part[((int64_t)blockIdx.x * 2 + m) * MAX_D + threadIdx.x] = sum;
             }
         }
@@ -207,7 +411,10 @@ __global__ void __launch_bounds__(1024) rotate_weight_kernel(const float *part, 
     float *out = blockIdx.y ? dk_weight : dq_weight;
     if (!out) return;
     float sum = 0.f;
-    for (int b = first; b < blocks; b += 32) sum += part[((int64_t)b * 2 + blockIdx.y) * rot::MAX_D + col];
+    if (col < d) {
+#pragma unroll 8
+        for (int b = first; b < blocks; b += 32) sum += part[((int64_t)b * 2 + blockIdx.y) * rot::MAX_D + col];
+    }
     sums[first][threadIdx.x & 31] = sum;
     __syncthreads();
     if (threadIdx.x < 32) {
@@ -218,30 +425,37 @@ __global__ void __launch_bounds__(1024) rotate_weight_kernel(const float *part, 
     }
 }
 
-namespace rot {
-constexpr int GRAD_BLOCKS = 4;             // blocks of the gradient to an SM
-}
+size_t rotate_partials(bool wanted) { return wanted ? (size_t)sm_count_or_default() * rot::min_blocks(false, true) * 2 * rot::MAX_D * sizeof(float) : 0; }
 
-size_t rotate_partials(bool wanted) { return wanted ? (size_t)sm_count_or_default() * rot::GRAD_BLOCKS * 2 * rot::MAX_D * sizeof(float) : 0; }
-
-template <int R, bool GRAD>
-static st_status run_rotate(RotateArgs a, bool norm, int pairs, cudaStream_t stream, int *blocks)
+template <int LANES, bool ODD, bool GRAD>
+static st_status launch_rotate(const RotateArgs &a, bool norm, bool inter, int grid, cudaStream_t stream)
 {
     using namespace rot;
-    a.cols = a.width < ROWS * R ? a.width : ROWS * R;
-    a.tokens = ROWS * R / a.cols;
-    a.col_tiles = (a.width + a.cols - 1) / a.cols;
-    a.tiles = ((int64_t)a.n + a.tokens - 1) / a.tokens * a.col_tiles;
-    const size_t smem = ((norm ? 2 * MAX_D : 0) + (size_t)a.tokens * 2 * ((a.rot / 2 + 3) / 4 * 4)) * sizeof(float);
-    int64_t grid = a.tiles;
-    if (GRAD && grid > (int64_t)sm_count_or_default() * GRAD_BLOCKS) grid = (int64_t)sm_count_or_default() * GRAD_BLOCKS;
-    if (grid > INT32_MAX) return ST_ERR_UNSUPPORTED;
-    *blocks = (int)grid;
-    void (*kernel)(RotateArgs) = nullptr;
-    if (norm) kernel = pairs == HALF ? rotate_kernel<R, true, HALF, GRAD> : pairs == INTERLEAVED ? rotate_kernel<R, true, INTERLEAVED, GRAD> : rotate_kernel<R, true, HALF_ODD, GRAD>;
-    else kernel = pairs == HALF ? rotate_kernel<R, false, HALF, GRAD> : pairs == INTERLEAVED ? rotate_kernel<R, false, INTERLEAVED, GRAD> : rotate_kernel<R, false, HALF_ODD, GRAD>;
+    void (*kernel)(RotateArgs) = norm ? (inter ? rotate_kernel<LANES, true, true, ODD, GRAD> : rotate_kernel<LANES, true, false, ODD, GRAD>)
+                                      : (inter ? rotate_kernel<LANES, false, true, ODD, GRAD> : rotate_kernel<LANES, false, false, ODD, GRAD>);
+    const size_t smem = (size_t)warps(GRAD) * 32 * ahead(GRAD) * 16 * (ODD ? 1 : 2) * (GRAD && norm ? 2 : 1) + (norm ? WEIGHTS * 16 : 0);
     if (!ensure_dynamic_smem(kernel, smem)) return ST_ERR_CUDA;
-    return launch(kernel, dim3((unsigned)grid), THREADS, smem, stream, a);
+    return launch(kernel, dim3((unsigned)grid), warps(GRAD) * 32, smem, stream, a);
+}
+
+// An item is a token where half of the warps have one; where not, its heads are divided, down to one row of each group of lanes.
+template <bool GRAD>
+static st_status run_rotate(RotateArgs &a, bool norm, bool inter, cudaStream_t stream, int *blocks)
+{
+    using namespace rot;
+    constexpr int WARPS = warps(GRAD);
+    const bool odd = a.rot % 16 != 0;
+    const int rows = odd ? 2 : a.d <= 64 ? 8 : 4;          // of a warp at a time
+    const int64_t sms = sm_count_or_default(), most = sms * min_blocks(odd, GRAD);
+    a.cols = a.width;
+    while ((int64_t)a.n * ((a.width + a.cols - 1) / a.cols) < most * WARPS / 2 && a.cols > rows) a.cols = ((a.cols + 1) / 2 + rows - 1) / rows * rows;
+    a.chunks = (a.width + a.cols - 1) / a.cols;
+    a.items = a.n * a.chunks;
+    int64_t grid = ((int64_t)a.items + WARPS - 1) / WARPS;
+    if (grid > most) grid = most;
+    *blocks = (int)grid;
+    if (odd) return launch_rotate<16, true, GRAD>(a, norm, inter, (int)grid, stream);
+    return a.d <= 64 ? launch_rotate<4, false, GRAD>(a, norm, inter, (int)grid, stream) : launch_rotate<8, false, GRAD>(a, norm, inter, (int)grid, stream);
 }
 
 static st_status check_rotation(const st_rotation *r, const void *positions, const void *freq)
@@ -291,8 +505,6 @@ static RotateArgs rotate_args(const st_rotation *r, const void *q, const void *k
     return a;
 }
 
-static int pairs_of(const st_rotation *r) { return r->interleaved ? rot::INTERLEAVED : r->rot % 16 == 0 ? rot::HALF : rot::HALF_ODD; }
-
 }  // namespace attn
 }  // namespace st
 
@@ -323,9 +535,7 @@ extern "C" st_status st_attn_rotate(const st_rotation *r, const void *q, const v
             arrays_meet(o.first, o.second, q_weight, w_bytes) || arrays_meet(o.first, o.second, k_weight, w_bytes))
             return ST_ERR_UNSUPPORTED;
     int blocks;
-    // rows for four blocks on every SM: four rows to a group of lanes, so that a token's angles serve more of its heads
-    if ((int64_t)a.n * a.width >= (int64_t)sm_count_or_default() * 4 * rot::ROWS * 4) return run_rotate<4, false>(a, r->norm, pairs_of(r), (cudaStream_t)stream, &blocks);
-    return run_rotate<1, false>(a, r->norm, pairs_of(r), (cudaStream_t)stream, &blocks);
+    return run_rotate<false>(a, r->norm, r->interleaved, (cudaStream_t)stream, &blocks);
 }
 
 extern "C" st_status st_attn_rotate_grad(const st_rotation *r, const void *q, const void *k, const void *dq_out, const void *dk_out, const int32_t *positions,
@@ -364,8 +574,7 @@ extern "C" st_status st_attn_rotate_grad(const st_rotation *r, const void *q, co
             if (arrays_meet(p, bytes, outs[j].first, outs[j].second)) return ST_ERR_UNSUPPORTED;
     }
     int blocks = 0;
-    if ((int64_t)a.n * a.width >= (int64_t)sm_count_or_default() * rot::GRAD_BLOCKS * rot::ROWS * 2) rc = run_rotate<2, true>(a, r->norm, pairs_of(r), (cudaStream_t)stream, &blocks);
-    else rc = run_rotate<1, true>(a, r->norm, pairs_of(r), (cudaStream_t)stream, &blocks);
+    rc = run_rotate<true>(a, r->norm, r->interleaved, (cudaStream_t)stream, &blocks);
     if (rc != ST_OK || !weights) return rc;
     return launch(rotate_weight_kernel, dim3((unsigned)((r->d + 31) / 32), 2), 1024, 0, (cudaStream_t)stream, (const float *)a.part, blocks, (int)r->d, dq_weight, dk_weight);
 }
