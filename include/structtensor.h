@@ -74,7 +74,7 @@ typedef enum { ST_FILL_ZERO = 0, ST_FILL_SYMMETRIC = 1 } st_fill;
 typedef enum { ST_OP_SYM_MOMENT2 = 0, ST_OP_SYM_MOMENT3 = 1, ST_OP_MTTKRP_TRI = 2,
                ST_OP_TTM_BLOCKDIAG = 3, ST_OP_SYM_MOMENT4 = 4, ST_OP_MTTKRP_SLICE = 5, ST_OP_ATTN_WINDOW = 6,
                ST_OP_ATTN_WINDOW_GRAD = 7, ST_OP_ATTN_WINDOW_STEP = 8, ST_OP_ATTN_DECAY = 9, ST_OP_ATTN_DECAY_GRAD = 10,
-               ST_OP_ATTN_ROTATE_GRAD = 11, ST_OP_ATTN_CACHE = 12, ST_OP_ATTN_SHARED_STEP = 13 } st_op;
+               ST_OP_ATTN_ROTATE_GRAD = 11, ST_OP_ATTN_CACHE = 12, ST_OP_ATTN_CACHE_STEP = 13, ST_OP_ATTN_SHARED_STEP = 14 } st_op;
 
 /* flags (bit mask) */
 #define ST_FLAG_DENSE_CONTROL 1u /* run the same kernel over the dense, unstructured iteration
@@ -135,7 +135,8 @@ st_status st_unpack(const st_layout *layout, st_dtype dtype, const void *packed,
  *   ST_OP_ATTN_WINDOW_GRAD a=nq, b=heads, c=kv_heads, e=sinks
  *   ST_OP_ATTN_DECAY, ST_OP_ATTN_DECAY_GRAD  a=nq, b=nseq, c=heads, e=max(d, dv)
  *   ST_OP_ATTN_ROTATE_GRAD  a=d (0 where no weights have a gradient: the header alone)
- *   ST_OP_ATTN_CACHE    unused: the header alone, for st_attn_cache_write, st_attn_cache_read and st_attn_cache_step
+ *   ST_OP_ATTN_CACHE    unused: the header alone, for st_attn_cache_write and st_attn_cache_read
+ *   ST_OP_ATTN_CACHE_STEP  a=nseq
  *   ST_OP_ATTN_SHARED_STEP  a=nseq, b=heads, c=kv_heads, e=groups
  * Returns 0 for an invalid request (the call itself reports the error).  The current
  * device is queried for its SM count. */

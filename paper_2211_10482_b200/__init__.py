@@ -35,7 +35,8 @@ ST_FILL_ZERO, ST_FILL_SYMMETRIC = 0, 1
 # st_op
 ST_OP_SYM_MOMENT2, ST_OP_SYM_MOMENT3, ST_OP_MTTKRP_TRI, ST_OP_TTM_BLOCKDIAG, ST_OP_SYM_MOMENT4, \
     ST_OP_MTTKRP_SLICE, ST_OP_ATTN_WINDOW, ST_OP_ATTN_WINDOW_GRAD, ST_OP_ATTN_WINDOW_STEP, ST_OP_ATTN_DECAY, \
-    ST_OP_ATTN_DECAY_GRAD, ST_OP_ATTN_ROTATE_GRAD, ST_OP_ATTN_CACHE, ST_OP_ATTN_SHARED_STEP = range(14)
+    ST_OP_ATTN_DECAY_GRAD, ST_OP_ATTN_ROTATE_GRAD, ST_OP_ATTN_CACHE, ST_OP_ATTN_CACHE_STEP, \
+    ST_OP_ATTN_SHARED_STEP = range(15)
 # flags
 ST_FLAG_DENSE_CONTROL = 1
 ST_FLAG_TC_TF32 = 2

@@ -12,6 +12,7 @@ size_t attn_window_grad_workspace(int64_t nq, int64_t heads, int64_t kv_heads, i
 size_t attn_decay_workspace(int64_t n, int64_t nseq, int64_t heads, int64_t d, bool gradient);
 namespace attn {
 size_t rotate_partials(bool wanted);
+size_t attn_step_workspace(int64_t nseq);
 size_t attn_shared_workspace(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t groups);
 }
 }  // namespace st
@@ -62,6 +63,7 @@ size_t st_workspace_bytes(st_op op, int64_t a, int64_t b, int64_t c, int64_t e, 
     case ST_OP_ATTN_DECAY_GRAD: return st::attn_decay_workspace(a, b, c, e, true);
     case ST_OP_ATTN_ROTATE_GRAD: return st::kWsHeaderBytes + st::attn::rotate_partials(a > 0);
     case ST_OP_ATTN_CACHE: return st::kWsHeaderBytes;
+    case ST_OP_ATTN_CACHE_STEP: return st::attn::attn_step_workspace(a);
     case ST_OP_ATTN_SHARED_STEP: return st::attn::attn_shared_workspace(a, b, c, e);
     default: return 0;
     }

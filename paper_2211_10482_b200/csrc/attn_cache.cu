@@ -69,6 +69,15 @@ __device__ __forceinline__ Spot spot_of(const CacheArgs &a, int row, bool there)
     return {page * c.page_stride + p.slot * c.token_stride, page * c.scale_page + p.slot * c.scale_token};
 }
 
+__global__ void clear_status_kernel(unsigned *status)
+{
+    pdl_trigger();
+    pdl_wait();
+    status[kWsStatusWord] = 0u;
+    status[kWsDetailWord] = 0u;
+}
+st_status clear_status(unsigned *status, cudaStream_t stream) { return launch(clear_status_kernel, dim3(1), 1, 0, stream, status); }
+
 __device__ __forceinline__ void report_offsets(const CacheArgs &a)
 {
     if (blockIdx.x == 0 && !offsets_fine(a.offsets, a.c.nseq, a.n, threadIdx.x, cells::THREADS)) a.status[kWsStatusWord] = (unsigned)ST_ERR_DEV_BOUNDS;
@@ -233,7 +242,7 @@ static st_status run_cache(CacheArgs &a, int dtype, bool write, cudaStream_t str
     a.col_tiles = (width + a.cols - 1) / a.cols;
     const int64_t grid = ((int64_t)a.n + a.tokens - 1) / a.tokens * a.col_tiles;
     if (grid > INT32_MAX) return ST_ERR_UNSUPPORTED;
-    const st_status rc = clear_status(a.status, nullptr, 0, stream);
+    const st_status rc = clear_status(a.status, stream);
     if (rc != ST_OK) return rc;
     void (*kernel)(CacheArgs) = nullptr;
     if (write) kernel = dtype == ST_BF16 ? cache_write_kernel<ST_BF16> : dtype == ST_I8 ? cache_write_kernel<ST_I8> : cache_write_kernel<ST_I4>;

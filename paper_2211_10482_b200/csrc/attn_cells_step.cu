@@ -1,11 +1,16 @@
 // st_attn_cache_step: one token of every sequence against a cache in cells, which holds it already; and the own tokens of st_attn_shared_step.
 //
-// Bound by the cells' bytes: every visible row of K and V is read once for all query heads that share it.  The division of work is that of
-// st_attn_window_step: a cluster of blocks owns one key head of one sequence and 16 of its query heads, its warps take tiles of 16 or 32 visible keys in
-// turn through rings of their own (cp.async, page numbers one tile further ahead), and multiply with mma.sync, of whose 16 rows a group of heads fills some.
+// Bound by the cells' bytes: every visible row of K and V is read once for all query heads that share it.  The work is a line of units (one key head of one
+// sequence with 8 or 16 of its query heads), each as long as its tiles of 16 or 32 visible keys and what a unit costs beside them, and every warp takes an equal
+// piece of that line, however long the sequences are: a small kernel ahead sums up their tiles, and one behind joins the units that warps share.  (Clusters of
+// blocks that split each unit alike waited for the longest sequences, and blocks whose warps shared units waited for each other at every end of a short
+// one: 64 sequences of up to 6000 tokens 125 and 134 us.)  A warp's page numbers are two tiles ahead and its rows one, in a ring of its own (cp.async), over
+// the ends of units; no barrier of a block lies anywhere.  It multiplies with mma.sync, keys and the values' columns as the 16 rows of a product and
+// heads as its 8 columns:  S^T = K Q^T,  O^T = V^T P^T.  (Heads as rows would leave half of a product, of the scores in registers and of the sums empty
+// up to 8 heads.)  Weights go from the first product's layout to the second's by transposing 8 x 8 matrices of bf16 within the warp.
 //
-// Cells meet the tensor cores as whole numbers in bf16, which holds all of them exactly: 8 bits by their bits (128 + low seven bits, less 128 or 256),
-// 4 bits likewise (128 + c, less 128).  Scales come in afterwards, where they are one number for a key (ST_I8: a score times its key's scale, a weight
+// Cells meet the tensor cores as whole numbers in bf16, which holds all of them exactly, made from their bits (0x43 beside a byte or nibble c below 128 is
+// 128 + c).  Scales come in afterwards, where they are one number for a key (ST_I8: a score times its key's scale, a weight
 // times its value's) or for 32 columns (ST_I4: partial scores of 32 columns, x += step acc + lo sum(q); a set of weights for each 32 columns, and what lo
 // brings beside it, sum(w lo)).  The order of a fragment's columns is free as long as both operands agree, so that no byte has to change its lane:
 // a lane's four bytes of K are four or eight consecutive columns, of which the queries' fragments take the same ones.
@@ -16,16 +21,20 @@ namespace st {
 namespace attn {
 
 namespace cstep {
-constexpr int HEADS = 16, MAX_SPLITS = 16;
-constexpr int FEWEST = 2;                  // tiles of a warp, where keys are split further
-template <int DTYPE, int DP, int WARPS, int STAGES> struct Shape {
+constexpr int WARPS = 4, STAGES = 2, MOST_BLOCKS = 4;      // warps of a block, tiles in a ring, blocks on an SM
+// What a unit costs a warp beside its tiles, in tiles: its queries, its results.
+constexpr int UNIT_COST = 3;
+// The shortest piece of the line that is worth a warp, in tiles.
+constexpr int LEAST = 3;
+template <int DTYPE, int DP, int HN> struct Shape {
+    static constexpr int HEADS = 8 * HN;                                           // of a unit
+    static constexpr int BLOCKS = HN == 2 ? 2 : DTYPE == ST_I4 ? MOST_BLOCKS : 3;  // on an SM, as registers and shared memory leave room for
     static constexpr int KEYS = DTYPE == ST_BF16 ? 16 : 32;                        // of a tile
     static constexpr int ROW = DTYPE == ST_BF16 ? 2 * DP : DTYPE == ST_I8 ? DP : DP / 2;       // bytes
     static constexpr int SCALES = DTYPE == ST_BF16 ? 0 : DTYPE == ST_I8 ? 1 : DP / GROUP;      // of a row, 4 bytes each
     static constexpr int PIECES = ROW / 16;
     static constexpr int TILE = KEYS * ROW, STAGE = 2 * (TILE + KEYS * SCALES * 4), RING = STAGES * STAGE;
-    static constexpr size_t SMEM = (size_t)WARPS * RING + (2 * WARPS + 2 + MAX_SPLITS + MAX_PARTS) * HEADS * sizeof(float) + WARPS * KEYS * sizeof(int64_t) + 32;
-    static_assert(HEADS * DP * 4 <= RING, "a warp's output takes the place of its ring");
+    static constexpr size_t SMEM = (size_t)WARPS * (RING + KEYS * sizeof(int64_t));
     // 16-byte pieces of a tile lie so that eight rows of one piece fall on different banks
     static __device__ __forceinline__ int swizzle(int row) { return ROW >= 128 ? row & 7 : ROW == 64 ? row >> 1 & 3 : row >> 2 & 1; }
 };
@@ -41,10 +50,6 @@ __device__ __forceinline__ void load4x8x8(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ void load2x8x8(uint32_t (&r)[4], uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(addr) : "memory");
-}
 __device__ __forceinline__ void load4x8x8_trans(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -55,11 +60,12 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float load_cluster(uint32_t addr)
+// An 8 x 8 matrix of bf16, two to a lane, transposed.
+__device__ __forceinline__ uint32_t transposed(uint32_t x)
 {
-    float x;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(addr) : "memory");
-    return x;
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ float exp2_fast(float x)
 {
@@ -77,516 +83,731 @@ __device__ __forceinline__ uint32_t minus_bf16(uint32_t a, uint32_t b)
     const __nv_bfloat162 w = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&w);
 }
-// Two signed bytes of w as bf16, those that `which` picks: 0x43 beside a byte b is 128 + b up to 127, so its low seven bits are taken as that, less
-// 128, or less 256 (0x4380) where its sign bit is set.
+// Two bytes of w as bf16, those that `which` picks; w holds them with 128 added (sign bits flipped).  0x43 beside a byte u is x = 128 + u up to 127 and
+// x = 2 u from 128 on, so that u - 128 = (x - 256) - max(0, x / 2 - 128), all of it exact.  On the pipe of the multipliers, where masks (the low seven
+// bits less 128 or 256 by the sign bit) kept the other one at its limit.
 __device__ __forceinline__ uint32_t bytes_bf16(uint32_t w, uint32_t which)
 {
     const uint32_t x = __byte_perm(w, 0x43434343u, which);
-    return minus_bf16(x & 0xFF7FFF7Fu, x & 0xFF80FF80u);
+    uint32_t r;
+    asm("{\n\t.reg .b32 t, h;\n\t"
+        "fma.rn.relu.bf16x2 h, %1, %2, %3;\n\t"
+        "fma.rn.bf16x2 t, %1, %4, %5;\n\t"
+        "fma.rn.bf16x2 %0, h, %6, t;\n\t}"
+        : "=r"(r)
+        : "r"(x), "r"(0x3F003F00u), "r"(0xC300C300u), "r"(0x3F803F80u), "r"(0xC380C380u), "r"(0xBF80BF80u));
+    return r;
 }
 // Nibbles i and i + 4 of w.
 __device__ __forceinline__ uint32_t nibbles_bf16(uint32_t w, int i) { return minus_bf16((w >> (4 * i) & 0x000F000Fu) | 0x43004300u, 0x43004300u); }
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// Weight of a part whose largest score is m, where the largest of all is `all`.
+__device__ __forceinline__ float weight_of(float m, float all, float c) { return m == -INFINITY ? 0.f : exp2f(c * (m - all)); }
+
+// A sequence's visible keys: [0, first) and [lo, len).
+struct Visible {
+    int lo, first, keys;
+    __device__ __forceinline__ Visible(const CellsStepArgs &a, int told)
+    {
+        const int len = length_of(told, a.c.cols, a.c.page);
+        lo = max(0, len - a.window);
+        first = min(a.sinks, lo);
+        keys = first + len - lo;
+    }
+};
+__host__ __device__ __forceinline__ int length_on_line(int tiles) { return tiles ? tiles + cstep::UNIT_COST : 0; }
+// Warps that take pieces of a line of that length, the beginning of one's piece, and the one whose piece a place is in.
+__device__ __forceinline__ int workers_of(int64_t total, int most) { return (int)min((int64_t)most, (total + cstep::LEAST - 1) / cstep::LEAST); }
+__device__ __forceinline__ int64_t piece_of(int64_t total, int workers, int i) { return total * i / workers; }
+__device__ __forceinline__ int worker_at(int64_t total, int workers, int64_t at) { return (int)(((at + 1) * workers - 1) / total); }
+
+// The sequence that place `at` of the line is in: the last one that begins at or before it.  By a whole warp.
+__device__ __forceinline__ int sequence_at(const int64_t *starts, int nseq, int64_t at)
+{
+    const int lane = threadIdx.x & 31;
+    int lo = 0;
+    for (int span = nseq, step; span > 1; span = step) {
+        step = (span + 31) / 32;
+        const int i = lo + (lane + 1) * step;
+        const bool before = lane < 31 && i < min(lo + span, nseq) && starts[i] <= at;
+        lo += __popc(__ballot_sync(~0u, before)) * step;
+    }
+    return lo;
+}
+
+// A team's way along its piece of the line, unit by unit (of each of the team's heads).
+template <int KEYS>
+struct Walk {
+    int64_t left;                          // of the piece, behind the unit
+    int b, unit, within;                   // the unit; places of its part of the line that are other warps'
+    int told_next;                         // length of the sequence behind it, read ahead
+    Visible see;
+    int tiles, tile, last;                 // of the unit; the piece of it that is this warp's
+    __device__ __forceinline__ Walk(const CellsStepArgs &a, int b_, int64_t within_b, int64_t left_) : left(left_), b(b_), see(a, a.c.lens[b_])
+    {
+        told_next = b + 1 < a.c.nseq ? a.c.lens[b + 1] : 0;
+        tiles = (see.keys + KEYS - 1) / KEYS;
+        const int length = max(length_on_line(tiles), 1);
+        unit = (int)(within_b / length) - 1;
+        within = (int)(within_b - (int64_t)(unit + 1) * length);
+    }
+    // On to the next unit with tiles for this warp; false: there is none.
+    __device__ __forceinline__ bool next(const CellsStepArgs &a)
+    {
+        while (left > 0) {
+            ++unit;
+            while (unit == a.units / a.team || tiles == 0) {
+                unit = 0;
+                if (++b >= a.c.nseq) return false;
+                see = Visible(a, told_next);
+                told_next = b + 1 < a.c.nseq ? a.c.lens[b + 1] : 0;
+                tiles = (see.keys + KEYS - 1) / KEYS;
+            }
+            const int take = (int)min(left, (int64_t)(length_on_line(tiles) - within));
+            tile = max(0, within - cstep::UNIT_COST);
+            last = within + take - cstep::UNIT_COST;
+            within = 0;
+            left -= take;
+            if (last > tile) return true;
+        }
+        return false;
+    }
+};
+
 // WIDE: rows and scales may be copied in 16-byte pieces
-template <int DTYPE, int DP, int WARPS, int STAGES, bool WIDE>
-__global__ void __launch_bounds__(WARPS * 32) cells_step_kernel(const CellsStepArgs a)
+template <int DTYPE, int DP, int HN, bool WIDE>
+__global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN>::BLOCKS)) cells_step_kernel(const CellsStepArgs a)
 {
     using namespace cstep;
-    using S = Shape<DTYPE, DP, WARPS, STAGES>;
-    constexpr int KEYS = S::KEYS, ROW = S::ROW, PIECES = S::PIECES, NB = KEYS / 8, GROUPS = DP / GROUP;
+    using S = Shape<DTYPE, DP, HN>;
+    constexpr int KEYS = S::KEYS, ROW = S::ROW, PIECES = S::PIECES, NK = KEYS / 16, GROUPS = DP / GROUP, HEADS = S::HEADS;
     extern __shared__ __align__(128) unsigned char smem[];
-    float *most_w = (float *)(smem + WARPS * S::RING), *sum_w = most_w + WARPS * HEADS, *most_b = sum_w + WARPS * HEADS, *sum_b = most_b + HEADS;
-    float *share = sum_b + HEADS;                          // weight of every block's part, over the sum: [block][head]
-    float *part_share = share + MAX_SPLITS * HEADS;        // likewise of every part of the prefix
-    int64_t *offsets = (int64_t *)(part_share + MAX_PARTS * HEADS);
-    int *flags = (int *)(offsets + WARPS * KEYS);          // [0]: something to report, [1]: this block has a visible key
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3;
-    const int splits = gridDim.x, split = blockIdx.x, chunks = (a.group + HEADS - 1) / HEADS, b = blockIdx.z;
-    const int hk = blockIdx.y / chunks, g0 = blockIdx.y % chunks * HEADS, g = min(a.group - g0, HEADS);
+    const int chunks = (a.group + HEADS - 1) / HEADS;
     const Cells &cs = a.c;
+    const float c = a.scale * 1.4426950408889634f;
+    unsigned char *mine = smem + warp * S::RING;
+    const uint32_t ring = tc::smem_u32(mine);
+    int64_t *at = (int64_t *)(smem + WARPS * S::RING) + warp * KEYS;
 
-    if (threadIdx.x < 2) flags[threadIdx.x] = 0;
-    // Parts of a prefix come from the kernel before this one, which lets this one begin only when all before itself is there: they alone are waited for.
+    // Behind a prefix's kernel: that one lets this one begin only when all before itself is there, and this one reads nothing of it.
     if (!a.part_count) pdl_wait();
     pdl_trigger();
-    __syncthreads();
-    const int told = cs.lens[b], len = length_of(told, cs.cols, cs.page);
-    if (told != len && threadIdx.x == 0) flags[0] = 1;
-    // visible keys: [0, first) and [lo, len)
-    const int lo = max(0, len - a.window), first = min(a.sinks, lo), keys = first + len - lo, tiles = (keys + KEYS - 1) / KEYS;
-    const unsigned char *kc = cs.k + hk * cs.head_stride, *vc = cs.v + hk * cs.head_stride;
-    const uint32_t *ks = cs.k_scales + hk * cs.scale_head, *vs = cs.v_scales + hk * cs.scale_head;
-    const uint32_t ring = tc::smem_u32(smem + warp * S::RING);
-    const int step = splits * WARPS, tile0 = split * WARPS + warp;
-    const int64_t head0 = hk * a.group + g0;
+    const int64_t total = a.starts[cs.nseq];
+    // few pieces go to as many SMs as there are
+    const int teams = workers_of(total, a.slots / a.team), team = warp / a.team * gridDim.x + blockIdx.x, head_of_team = warp % a.team, worker = team * a.team + head_of_team;
+    if (team < teams) {
+        const int64_t begin = piece_of(total, teams, team), left = piece_of(total, teams, team + 1) - begin;
+        const int b0 = sequence_at(a.starts, cs.nseq, begin);
+        Walk<KEYS> ahead(a, b0, begin - a.starts[b0], left), here = ahead;
+        bool more = ahead.next(a), bad = false;
 
-    // The queries as fragments: row = head; which columns a lane has is what its bytes of K are.
-    uint32_t q[DP / 16][4];
-#pragma unroll
-    for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = lane / 4 + (i & 1) * 8, j = i >> 1;
-            const int c0 = DTYPE == ST_BF16 ? k * 16 + quad * 2 + j * 8 : DTYPE == ST_I8 ? k * 16 + quad * 4 + j * 2 : (k / 2) * 32 + quad * 8 + (k & 1) * 2 + j;
-            const int c1 = DTYPE == ST_I4 ? c0 + 4 : c0 + 1;
-            const unsigned short *at = reinterpret_cast<const unsigned short *>(a.q + b * a.q_row + (head0 + row) * a.q_head);
-            q[k][i] = row < g ? (c0 < cs.d ? (uint32_t)at[c0] : 0u) | (c1 < cs.d ? (uint32_t)at[c1] << 16 : 0u) : 0u;
-        }
-    // ST_I4: sums of 32 columns of the queries, for the two heads of this lane
-    float qsum[2][GROUPS];
-    if (DTYPE == ST_I4)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int p = 0; p < GROUPS; ++p) {
-                float s = 0.f;
-#pragma unroll
-                for (int k = 2 * p; k < 2 * p + 2; ++k) s += low_bf16(q[k][i]) + high_bf16(q[k][i]) + low_bf16(q[k][i + 2]) + high_bf16(q[k][i + 2]);
-                s += __shfl_xor_sync(~0u, s, 1);
-                qsum[i][p] = s + __shfl_xor_sync(~0u, s, 2);
-            }
-
-    // Lane r finds row r of a tile: its page (-1: none, or outside the cache), then its place in the pages, which goes where all lanes that copy a
-    // piece of the row see it.
-    auto page_of = [&](int tile, int &slot) -> int {
-        const int u = tile * KEYS + (lane & (KEYS - 1)), s = u < first ? u : lo + u - first;
-        slot = 0;
-        if (u >= keys) return -1;
-        const Place p = place_of(s, cs.page, cs.page_magic);
-        slot = p.slot;
-        const int page = cs.table[(int64_t)b * cs.cols + p.col];
-        if ((unsigned)page < (unsigned)cs.pages) return page;
-        flags[0] = 1;
-        return -1;
-    };
-    int64_t *at = offsets + warp * KEYS;
-    const int piece = lane % PIECES, row0 = lane / PIECES;
-    const int left = DTYPE == ST_BF16 ? 2 * cs.d - piece * 16 : DTYPE == ST_I8 ? cs.d - piece * 16 : cs.d / 2 - piece * 16;     // bytes of the row from this piece on
-    constexpr int ROWS = 32 / PIECES;                      // rows that a warp copies at a time
-    // bit r: row r of the tile is there.  What is not there is zeros.
-    auto fetch = [&](int tile, int stage, int page, int slot) -> unsigned {
-        const unsigned there = __ballot_sync(~0u, page >= 0 && lane < KEYS);
-        if (tile < tiles) {
-            const uint32_t dst = ring + stage * S::STAGE;
-            __syncwarp();
-            if (lane < KEYS) at[lane] = page >= 0 ? page * cs.page_stride + slot * cs.token_stride : 0;
-            if (DTYPE != ST_BF16) {
-                const int64_t from = page >= 0 ? page * cs.scale_page + slot * cs.scale_token : 0;
-                const uint32_t o = dst + 2 * S::TILE + lane * S::SCALES * 4;
-                const int n = (cs.d + GROUP - 1) / GROUP;
-                if (DTYPE == ST_I8) {
-                    copy_async<4>(o, ks + from, page >= 0);
-                    copy_async<4>(o + KEYS * 4, vs + from, page >= 0);
-                } else if (WIDE && DP == 128) {
-                    copy_async<16>(o, ks + from, page >= 0);
-                    copy_async<16>(o + KEYS * S::SCALES * 4, vs + from, page >= 0);
+        // Lane r finds row r of the tile after: where it lies in the pages of keys (those of values lie alike), and its scales; -1: nowhere.
+        int64_t cell = -1, scale = 0;
+        bool coming = false;                               // there is a tile whose places these are
+        auto look = [&] {
+            cell = -1;
+            coming = more;
+            if (!more) return;
+            const int u = ahead.tile * KEYS + (lane & (KEYS - 1)), s = u < ahead.see.first ? u : ahead.see.lo + u - ahead.see.first;
+            if (u < ahead.see.keys) {
+                const Place p = place_of(s, cs.page, cs.page_magic);
+                const int page = cs.table[(int64_t)ahead.b * cs.cols + p.col], hk = (ahead.unit * a.team + head_of_team) / chunks;
+                if ((unsigned)page < (unsigned)cs.pages) {
+                    cell = page * cs.page_stride + p.slot * cs.token_stride + hk * cs.head_stride;
+                    scale = page * cs.scale_page + p.slot * cs.scale_token + hk * cs.scale_head;
                 } else {
+                    bad = true;
+                }
+            }
+            if (++ahead.tile == ahead.last) more = ahead.next(a);
+        };
+        const int piece = lane % PIECES, row0 = lane / PIECES;
+        const int bytes = DTYPE == ST_BF16 ? 2 * cs.d - piece * 16 : DTYPE == ST_I8 ? cs.d - piece * 16 : cs.d / 2 - piece * 16;   // of the row from this piece on
+        constexpr int ROWS = 32 / PIECES;                  // rows that a warp copies at a time
+        // Copies the tile whose places were found.  Bit r: row r is there; what is not there is zeros.
+        auto fetch = [&](int stage) -> unsigned {
+            const unsigned there = __ballot_sync(~0u, cell >= 0 && lane < KEYS);
+            if (coming) {
+                const uint32_t dst = ring + stage * S::STAGE;
+                __syncwarp();
+                if (lane < KEYS) at[lane] = max(cell, (int64_t)0);
+                if (DTYPE != ST_BF16) {
+                    const bool in = cell >= 0;
+                    const uint32_t *ks = cs.k_scales + (in ? scale : 0), *vs = cs.v_scales + (in ? scale : 0);
+                    const uint32_t o = dst + 2 * S::TILE + lane * S::SCALES * 4;
+                    const int n = (cs.d + GROUP - 1) / GROUP;
+                    if (DTYPE == ST_I8) {
+                        copy_async<4>(o, ks, in);
+                        copy_async<4>(o + KEYS * 4, vs, in);
+                    } else if (WIDE && DP == 128) {
+                        copy_async<16>(o, ks, in);
+                        copy_async<16>(o + KEYS * S::SCALES * 4, vs, in);
+                    } else {
 #pragma unroll
-                    for (int p = 0; p < S::SCALES; ++p) {
-                        const int at_p = p < n ? p : 0;
-                        copy_async<4>(o + p * 4, ks + from + at_p, page >= 0 && p < n);
-                        copy_async<4>(o + KEYS * S::SCALES * 4 + p * 4, vs + from + at_p, page >= 0 && p < n);
+                        for (int p = 0; p < S::SCALES; ++p) {
+                            const int at_p = p < n ? p : 0;
+                            copy_async<4>(o + p * 4, ks + at_p, in && p < n);
+                            copy_async<4>(o + KEYS * S::SCALES * 4 + p * 4, vs + at_p, in && p < n);
+                        }
+                    }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < KEYS / ROWS; ++i) {
+                    const int row = row0 + i * ROWS;
+                    const bool in = (there >> row & 1) && bytes > 0;
+                    const int64_t from = at[row] + (bytes > 0 ? piece * 16 : 0);
+                    const uint32_t o = dst + row * ROW + ((piece ^ S::swizzle(row)) << 4);
+                    if (WIDE) {
+                        copy_async<16>(o, cs.k + from, in);
+                        copy_async<16>(o + S::TILE, cs.v + from, in);
+                    } else {
+                        const int next = bytes > 8 ? 8 : 0;
+                        copy_async<8>(o, cs.k + from, in);
+                        copy_async<8>(o + 8, cs.k + from + next, in && bytes > 8);
+                        copy_async<8>(o + S::TILE, cs.v + from, in);
+                        copy_async<8>(o + S::TILE + 8, cs.v + from + next, in && bytes > 8);
                     }
                 }
             }
-            __syncwarp();
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            return there;
+        };
+        unsigned there[STAGES];
+        look();
 #pragma unroll
-            for (int i = 0; i < KEYS / ROWS; ++i) {
-                const int row = row0 + i * ROWS;
-                const bool in = there >> row & 1;
-                const int64_t from = at[row] + (left > 0 ? piece * 16 : 0);
-                const uint32_t o = dst + row * ROW + ((piece ^ S::swizzle(row)) << 4);
-                if (WIDE) {
-                    copy_async<16>(o, kc + from, in && left > 0);
-                    copy_async<16>(o + S::TILE, vc + from, in && left > 0);
-                } else {
-                    const int next = left > 8 ? 8 : 0;
-                    copy_async<8>(o, kc + from, in && left > 0);
-                    copy_async<8>(o + 8, kc + from + next, in && left > 8);
-                    copy_async<8>(o + S::TILE, vc + from, in && left > 0);
-                    copy_async<8>(o + S::TILE + 8, vc + from + next, in && left > 8);
+        for (int s = 0; s < STAGES - 1; ++s) {
+            there[s] = fetch(s);
+            look();
+        }
+        int stage = 0;
+        while (here.next(a)) {
+            const int unit = here.unit * a.team + head_of_team, hk = unit / chunks, g0 = unit % chunks * HEADS, g = min(a.group - g0, HEADS);
+            const int64_t head0 = hk * a.group + g0;
+            // The queries as fragments: column = head lane / 4; which rows (columns of q) a lane has is what its bytes of K are.
+            uint32_t q[DP / 16][HN][2];
+#pragma unroll
+            for (int n = 0; n < HN; ++n) {
+                const int head = n * 8 + lane / 4;
+                const unsigned short *from = reinterpret_cast<const unsigned short *>(a.q + here.b * a.q_row + (head0 + head) * a.q_head);
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int col = DTYPE == ST_BF16 ? k * 16 + quad * 2 + j * 8 : DTYPE == ST_I8 ? k * 16 + quad * 4 + j * 2 : (k / 2) * 32 + quad * 8 + (k & 1) * 2 + j;
+                        q[k][n][j] = 0u;
+                        if (head < g && col < cs.d)        // rows are whole eights of columns
+                            q[k][n][j] = DTYPE == ST_I4 ? (uint32_t)from[col] | (uint32_t)from[col + 4] << 16 : *reinterpret_cast<const uint32_t *>(from + col);
+                    }
+            }
+            // ST_I4: sums of 32 columns of the queries, for the two heads of this lane's scores
+            float qsum[HN][2][GROUPS];
+            if (DTYPE == ST_I4)
+#pragma unroll
+                for (int n = 0; n < HN; ++n)
+#pragma unroll
+                    for (int p = 0; p < GROUPS; ++p) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int k = 2 * p; k < 2 * p + 2; ++k) s += low_bf16(q[k][n][0]) + high_bf16(q[k][n][0]) + low_bf16(q[k][n][1]) + high_bf16(q[k][n][1]);
+                        s += __shfl_xor_sync(~0u, s, 1);
+                        s += __shfl_xor_sync(~0u, s, 2);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) qsum[n][i][p] = __shfl_sync(~0u, s, (2 * quad + i) * 4);
+                    }
+            // o: rows are columns of the values, columns heads 2 quad and 2 quad + 1
+            float o[DP / 16][HN][4], most[HN][2], sum[HN][2];
+            float low[HN][2][GROUPS];                      // ST_I4: what the values' lowest numbers bring to 32 columns
+            unsigned any = 0;                              // whether a key of this piece is there
+#pragma unroll
+            for (int n = 0; n < HN; ++n) {
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[k][n][i] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    most[n][i] = -INFINITY;
+                    sum[n][i] = 0.f;
+#pragma unroll
+                    for (int p = 0; p < GROUPS; ++p) low[n][i][p] = 0.f;
                 }
             }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        return there;
-    };
-
-    const float c = a.scale * 1.4426950408889634f;
-    float o[DP / 8][4], most[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-    float low[2][GROUPS];                                  // ST_I4: what the values' lowest numbers bring to 32 columns
+            auto attend = [&](int stage, unsigned there) {
+                const uint32_t K = ring + stage * S::STAGE, V = K + S::TILE;
+                const uint32_t *kscale = reinterpret_cast<const uint32_t *>(mine + stage * S::STAGE + 2 * S::TILE) + lane / 4 * S::SCALES, *vscale = kscale + KEYS * S::SCALES;
+                float x[NK][HN][4];                                // keys lane / 4 (and 8 more) of 16, heads 2 quad and 2 quad + 1
 #pragma unroll
-    for (int n = 0; n < DP / 8; ++n)
+                for (int h = 0; h < NK; ++h) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+                    for (int n = 0; n < HN; ++n)
 #pragma unroll
-    for (int p = 0; p < GROUPS; ++p) low[0][p] = low[1][p] = 0.f;
-
-    auto attend = [&](int stage, unsigned there) {
-        const uint32_t K = ring + stage * S::STAGE, V = K + S::TILE;
-        const uint32_t *kscale = reinterpret_cast<const uint32_t *>(smem + warp * S::RING + stage * S::STAGE + 2 * S::TILE), *vscale = kscale + KEYS * S::SCALES;
-        float x[NB][4];
+                        for (int i = 0; i < 4; ++i) x[h][n][i] = 0.f;
+                    const int row = h * 16 + (lane & 15);
+                    const uint32_t at_row = K + row * ROW;
+                    if (DTYPE == ST_BF16) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
+                        for (int k = 0; k < DP / 16; ++k) {
+                            uint32_t f[4];                         // 16 keys, 16 columns
+                            load4x8x8(f, at_row + (((k * 2 + lane / 16) ^ S::swizzle(row)) << 4));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[n][i] = 0.f;
-            const int row = n * 8 + (lane & 7);
-            if (DTYPE == ST_BF16) {
+                            for (int n = 0; n < HN; ++n) mma(x[h][n], f, q[k][n][0], q[k][n][1]);
+                        }
+                    } else if (DTYPE == ST_I8) {
 #pragma unroll
-                for (int k = 0; k < DP / 32; ++k) {
-                    uint32_t f[4];                         // 8 keys, 32 columns
-                    load4x8x8(f, K + row * ROW + (((k * 4 + lane / 8) ^ S::swizzle(row)) << 4));
-                    mma(x[n], q[2 * k], f[0], f[1]);
-                    mma(x[n], q[2 * k + 1], f[2], f[3]);
+                        for (int k = 0; k < DP / 32; ++k) {
+                            uint32_t f[4];                         // 16 keys, 32 columns
+                            load4x8x8(f, at_row + (((k * 2 + lane / 16) ^ S::swizzle(row)) << 4));
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) f[m] ^= 0x80808080u;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const uint32_t c[4] = {bytes_bf16(f[2 * m], 0x4140u), bytes_bf16(f[2 * m + 1], 0x4140u), bytes_bf16(f[2 * m], 0x4342u), bytes_bf16(f[2 * m + 1], 0x4342u)};
+#pragma unroll
+                                for (int n = 0; n < HN; ++n) mma(x[h][n], c, q[2 * k + m][n][0], q[2 * k + m][n][1]);
+                            }
+                        }
+                        const float s0 = __uint_as_float(kscale[h * 16]), s1 = __uint_as_float(kscale[h * 16 + 8]);
+#pragma unroll
+                        for (int n = 0; n < HN; ++n) {
+                            x[h][n][0] *= s0;
+                            x[h][n][1] *= s0;
+                            x[h][n][2] *= s1;
+                            x[h][n][3] *= s1;
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < DP / 64; ++k) {
+                            uint32_t f[4];                         // 16 keys, 64 columns
+                            load4x8x8(f, at_row + (((k * 2 + lane / 16) ^ S::swizzle(row)) << 4));
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const int p = 2 * k + m;
+                                float y[HN][4];
+#pragma unroll
+                                for (int n = 0; n < HN; ++n)
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) y[n][i] = 0.f;
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const uint32_t c[4] = {nibbles_bf16(f[2 * m], 2 * j), nibbles_bf16(f[2 * m + 1], 2 * j), nibbles_bf16(f[2 * m], 2 * j + 1), nibbles_bf16(f[2 * m + 1], 2 * j + 1)};
+#pragma unroll
+                                    for (int n = 0; n < HN; ++n) mma(y[n], c, q[2 * p + j][n][0], q[2 * p + j][n][1]);
+                                }
+                                const uint32_t s0 = kscale[h * 16 * S::SCALES + p], s1 = kscale[(h * 16 + 8) * S::SCALES + p];
+#pragma unroll
+                                for (int n = 0; n < HN; ++n)
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        x[h][n][i] = fmaf(low_bf16(s0), y[n][i], fmaf(high_bf16(s0), qsum[n][i][p], x[h][n][i]));
+                                        x[h][n][2 + i] = fmaf(low_bf16(s1), y[n][2 + i], fmaf(high_bf16(s1), qsum[n][i][p], x[h][n][2 + i]));
+                                    }
+                            }
+                        }
+                    }
                 }
-            } else if (DTYPE == ST_I8) {
+                if (there != (KEYS == 32 ? ~0u : 0xFFFFu)) {
+                    const unsigned mine = there >> (lane / 4);
 #pragma unroll
-                for (int k = 0; k < DP / 64; ++k) {
-                    uint32_t f[4];                         // 8 keys, 64 columns
-                    load4x8x8(f, K + row * ROW + (((k * 4 + lane / 8) ^ S::swizzle(row)) << 4));
+                    for (int h = 0; h < NK; ++h)
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) mma(x[n], q[4 * k + m], bytes_bf16(f[m], 0x4140u), bytes_bf16(f[m], 0x4342u));
+                        for (int n = 0; n < HN; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (!(mine >> (h * 16 + i / 2 * 8) & 1u)) x[h][n][i] = -INFINITY;
                 }
-                const float2 s = *reinterpret_cast<const float2 *>(kscale + n * 8 + quad * 2);
-                x[n][0] *= s.x;
-                x[n][1] *= s.y;
-                x[n][2] *= s.x;
-                x[n][3] *= s.y;
-            } else {
-                uint32_t f[4];                             // 8 keys, all columns
-                const uint32_t from = K + row * ROW + (((lane / 8 % PIECES) ^ S::swizzle(row)) << 4);
-                if (DP == 128) load4x8x8(f, from);
-                else load2x8x8(f, from);
+                float top[HN][2];
+                bool moves = false;
 #pragma unroll
-                for (int p = 0; p < GROUPS; ++p) {
-                    float y[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma(y, q[2 * p], nibbles_bf16(f[p], 0), nibbles_bf16(f[p], 1));
-                    mma(y, q[2 * p + 1], nibbles_bf16(f[p], 2), nibbles_bf16(f[p], 3));
-                    const uint32_t s0 = kscale[(n * 8 + quad * 2) * S::SCALES + p], s1 = kscale[(n * 8 + quad * 2 + 1) * S::SCALES + p];
+                for (int n = 0; n < HN; ++n)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        x[n][2 * i] = fmaf(low_bf16(s0), y[2 * i], fmaf(high_bf16(s0), qsum[i][p], x[n][2 * i]));
-                        x[n][2 * i + 1] = fmaf(low_bf16(s1), y[2 * i + 1], fmaf(high_bf16(s1), qsum[i][p], x[n][2 * i + 1]));
+                        float m = fmaxf(x[0][n][i], x[0][n][2 + i]);
+#pragma unroll
+                        for (int h = 1; h < NK; ++h) m = fmaxf(m, fmaxf(x[h][n][i], x[h][n][2 + i]));
+#pragma unroll
+                        for (int e = 4; e < 32; e <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, e));
+                        top[n][i] = m;
+                        moves = moves || c * (m - most[n][i]) > 8.f;
                     }
-                }
-            }
-        }
-        if (there != (KEYS == 32 ? ~0u : 0xFFFFu))
+                // as long as no weight passes 2^8 the reference stays: any reference gives the same quotient
+                if (__any_sync(~0u, moves)) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+                    for (int n = 0; n < HN; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (!(there >> (n * 8 + quad * 2 + (i & 1)) & 1)) x[n][i] = -INFINITY;
-        float top[2];
+                        for (int i = 0; i < 2; ++i) {
+                            const float now = fmaxf(most[n][i], top[n][i]), f = now == -INFINITY ? 1.f : exp2f(c * (most[n][i] - now));
+                            most[n][i] = now;
+                            sum[n][i] *= f;
+                            if (DTYPE == ST_I4)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            top[i] = fmaxf(x[0][2 * i], x[0][2 * i + 1]);
+                                for (int p = 0; p < GROUPS; ++p) low[n][i][p] *= f;
 #pragma unroll
-            for (int n = 1; n < NB; ++n) top[i] = fmaxf(top[i], fmaxf(x[n][2 * i], x[n][2 * i + 1]));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 1));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(~0u, top[i], 2));
-        }
-        // as long as no weight passes 2^8 the reference stays: any reference gives the same quotient
-        if (__any_sync(~0u, c * (top[0] - most[0]) > 8.f || c * (top[1] - most[1]) > 8.f)) {
-            float f[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float now = fmaxf(most[i], top[i]);
-                f[i] = now == -INFINITY ? 1.f : exp2f(c * (most[i] - now));
-                most[i] = now;
-                sum[i] *= f[i];
-                if (DTYPE == ST_I4)
-#pragma unroll
-                    for (int p = 0; p < GROUPS; ++p) low[i][p] *= f[i];
-            }
-#pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[n][i] *= f[i >> 1];
-        }
-        const float ref[2] = {most[0] == -INFINITY ? 0.f : c * most[0], most[1] == -INFINITY ? 0.f : c * most[1]};
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[n][i] = exp2_fast(fmaf(c, x[n][i], -ref[i >> 1]));
-                sum[i >> 1] += x[n][i];
-            }
-        // weights, times their values' scales, rounded once for the product with V
-#pragma unroll
-        for (int h = 0; h < KEYS / 16; ++h) {
-            const int row = h * 16 + (lane & 15);
-            if (DTYPE == ST_BF16) {
-                const uint32_t p[4] = {pair_bf16(x[2 * h][0], x[2 * h][1]), pair_bf16(x[2 * h][2], x[2 * h][3]), pair_bf16(x[2 * h + 1][0], x[2 * h + 1][1]),
-                                       pair_bf16(x[2 * h + 1][2], x[2 * h + 1][3])};
-#pragma unroll
-                for (int n = 0; n < DP / 16; ++n) {
-                    uint32_t f[4];                         // 16 keys, 16 columns
-                    load4x8x8_trans(f, V + row * ROW + (((n * 2 + lane / 16) ^ S::swizzle(row)) << 4));
-                    mma(o[2 * n], p, f[0], f[1]);
-                    mma(o[2 * n + 1], p, f[2], f[3]);
-                }
-            } else if (DTYPE == ST_I8) {
-                uint32_t p[4];
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const float2 s = *reinterpret_cast<const float2 *>(vscale + (2 * h + n) * 8 + quad * 2);
-                    const float *y = x[2 * h + n];
-                    p[2 * n] = pair_bf16(y[0] * s.x, y[1] * s.y);
-                    p[2 * n + 1] = pair_bf16(y[2] * s.x, y[3] * s.y);
-                }
-#pragma unroll
-                for (int n = 0; n < DP / 32; ++n) {
-                    uint32_t f[4];                         // 16 keys, 32 columns: even columns in one product, odd ones in another
-                    load4x8x8_trans(f, V + row * ROW + (((n * 2 + lane / 16) ^ S::swizzle(row)) << 4));
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        mma(o[4 * n + 2 * m], p, bytes_bf16(f[2 * m], 0x4240u), bytes_bf16(f[2 * m + 1], 0x4240u));
-                        mma(o[4 * n + 2 * m + 1], p, bytes_bf16(f[2 * m], 0x4341u), bytes_bf16(f[2 * m + 1], 0x4341u));
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int n = 0; n < DP / 64; ++n) {
-                    uint32_t f[4];                         // 16 keys, 64 columns
-                    load4x8x8_trans(f, V + row * ROW + (((n * 2 + lane / 16) ^ S::swizzle(row)) << 4));
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const int group = 2 * n + m;
-                        uint32_t p[4];
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int key = (2 * h + e) * 8 + quad * 2;
-                            const uint32_t s0 = vscale[key * S::SCALES + group], s1 = vscale[(key + 1) * S::SCALES + group];
-                            const float *y = x[2 * h + e];
-                            p[2 * e] = pair_bf16(y[0] * low_bf16(s0), y[1] * low_bf16(s1));
-                            p[2 * e + 1] = pair_bf16(y[2] * low_bf16(s0), y[3] * low_bf16(s1));
-                            low[0][group] = fmaf(y[0], high_bf16(s0), fmaf(y[1], high_bf16(s1), low[0][group]));
-                            low[1][group] = fmaf(y[2], high_bf16(s0), fmaf(y[3], high_bf16(s1), low[1][group]));
+                            for (int k = 0; k < DP / 16; ++k) {
+                                o[k][n][i] *= f;
+                                o[k][n][2 + i] *= f;
+                            }
                         }
+                }
+                uint32_t p[NK][HN][2];                             // weights as fragments: heads lane / 4, keys 2 quad and 2 quad + 1 (and 8 more); not ST_I4
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) mma(o[4 * group + i], p, nibbles_bf16(f[2 * m], i), nibbles_bf16(f[2 * m + 1], i));
+                for (int h = 0; h < NK; ++h) {
+                    const float s0 = DTYPE == ST_I8 ? __uint_as_float(vscale[h * 16]) : 1.f, s1 = DTYPE == ST_I8 ? __uint_as_float(vscale[h * 16 + 8]) : 1.f;
+#pragma unroll
+                    for (int n = 0; n < HN; ++n) {
+                        float *y = x[h][n];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            y[i] = exp2_fast(fmaf(c, y[i], most[n][i & 1] == -INFINITY ? 0.f : -c * most[n][i & 1]));
+                            sum[n][i & 1] += y[i];
+                        }
+                        // times their values' scales, rounded once for the product with V
+                        if (DTYPE == ST_BF16) {
+                            p[h][n][0] = transposed(pair_bf16(y[0], y[1]));
+                            p[h][n][1] = transposed(pair_bf16(y[2], y[3]));
+                        } else if (DTYPE == ST_I8) {
+                            p[h][n][0] = transposed(pair_bf16(y[0] * s0, y[1] * s0));
+                            p[h][n][1] = transposed(pair_bf16(y[2] * s1, y[3] * s1));
+                        }
                     }
                 }
+#pragma unroll
+                for (int h = 0; h < NK; ++h) {
+                    const int row = h * 16 + (lane & 15);
+                    const uint32_t at_row = V + row * ROW;
+                    if (DTYPE == ST_BF16) {
+#pragma unroll
+                        for (int k = 0; k < DP / 16; ++k) {
+                            uint32_t f[4];                         // 16 keys, 16 columns: columns 0..7 of keys 0..7 and 8..15, then 8..15
+                            load4x8x8_trans(f, at_row + (((k * 2 + lane / 16) ^ S::swizzle(row)) << 4));
+                            const uint32_t c[4] = {f[0], f[2], f[1], f[3]};
+#pragma unroll
+                            for (int n = 0; n < HN; ++n) mma(o[k][n], c, p[h][n][0], p[h][n][1]);
+                        }
+                    } else if (DTYPE == ST_I8) {
+#pragma unroll
+                        for (int k = 0; k < DP / 32; ++k) {
+                            uint32_t f[4];                         // 16 keys, 32 columns: of 16, even ones are rows 0..7 of a product and odd ones rows 8..15
+                            load4x8x8_trans(f, at_row + (((k * 2 + lane / 16) ^ S::swizzle(row)) << 4));
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) f[m] ^= 0x80808080u;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const uint32_t c[4] = {bytes_bf16(f[2 * m], 0x4240u), bytes_bf16(f[2 * m], 0x4341u), bytes_bf16(f[2 * m + 1], 0x4240u), bytes_bf16(f[2 * m + 1], 0x4341u)};
+#pragma unroll
+                                for (int n = 0; n < HN; ++n) mma(o[2 * k + m][n], c, p[h][n][0], p[h][n][1]);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < DP / 64; ++k) {
+                            uint32_t f[4];                         // 16 keys, 64 columns: of four neighbours, two are rows 0..7 and 8..15 of one product, two of the next
+                            load4x8x8_trans(f, at_row + (((k * 2 + lane / 16) ^ S::swizzle(row)) << 4));
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const int group = 2 * k + m;
+                                const uint32_t s0 = vscale[h * 16 * S::SCALES + group], s1 = vscale[(h * 16 + 8) * S::SCALES + group];
+                                uint32_t w[HN][2];
+#pragma unroll
+                                for (int n = 0; n < HN; ++n) {
+                                    const float *y = x[h][n];
+                                    w[n][0] = transposed(pair_bf16(y[0] * low_bf16(s0), y[1] * low_bf16(s0)));
+                                    w[n][1] = transposed(pair_bf16(y[2] * low_bf16(s1), y[3] * low_bf16(s1)));
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) low[n][i][group] = fmaf(y[i], high_bf16(s0), fmaf(y[2 + i], high_bf16(s1), low[n][i][group]));
+                                }
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const uint32_t c[4] = {nibbles_bf16(f[2 * m], 2 * j), nibbles_bf16(f[2 * m], 2 * j + 1), nibbles_bf16(f[2 * m + 1], 2 * j), nibbles_bf16(f[2 * m + 1], 2 * j + 1)};
+#pragma unroll
+                                    for (int n = 0; n < HN; ++n) mma(o[2 * group + j][n], c, w[n][0], w[n][1]);
+                                }
+                            }
+                        }
+                    }
+                }
+            };
+            for (int tile = here.tile; tile < here.last; ++tile) {
+                there[STAGES - 1] = fetch(stage == 0 ? STAGES - 1 : stage - 1);              // the stage before was read by all lanes
+                look();
+                asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+                __syncwarp();
+                any |= there[0];
+                attend(stage, there[0]);
+                __syncwarp();
+#pragma unroll
+                for (int s = 0; s + 1 < STAGES; ++s) there[s] = there[s + 1];
+                if (++stage == STAGES) stage = 0;
             }
-        }
-    };
-    unsigned there[STAGES], any = 0;
-    int slot, page = page_of(tile0, slot);
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-        const int p = page, l = slot;
-        page = page_of(tile0 + (s + 1) * step, slot);
-        there[s] = fetch(tile0 + s * step, s, p, l);
-    }
-    int stage = 0;
-    for (int tile = tile0; tile < tiles; tile += step) {
-        const int p = page, l = slot;
-        page = page_of(tile + STAGES * step, slot);
-        there[STAGES - 1] = fetch(tile + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1, p, l);      // the stage before was read by all lanes
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-        __syncwarp();
-        any |= there[0];
-        attend(stage, there[0]);
-        __syncwarp();
-#pragma unroll
-        for (int s = 0; s + 1 < STAGES; ++s) there[s] = there[s + 1];
-        if (++stage == STAGES) stage = 0;
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncwarp();
-    if (any && lane == 0) flags[1] = 1;
 
-    // join the warps: each leaves its output where its ring was
+            // A whole unit's output is done; with a prefix it goes to where the prefix's parts lie, a piece to where pieces are joined.
+            const bool whole = here.tile == 0 && here.last == here.tiles, done = whole && !a.part_count;
+            const int64_t slot = ((int64_t)worker * 2 + (here.tile > 0 ? 0 : 1)) * HEADS;
+            const int64_t rows = (int64_t)cs.nseq * a.group, part = (int64_t)a.own_part * (a.heads / a.group) + hk, id = (int64_t)here.b * a.group + g0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        sum[i] += __shfl_xor_sync(~0u, sum[i], 1);
-        sum[i] += __shfl_xor_sync(~0u, sum[i], 2);
-        if (DTYPE == ST_I4)
+            for (int n = 0; n < HN; ++n)
 #pragma unroll
-            for (int p = 0; p < GROUPS; ++p) {
-                low[i][p] += __shfl_xor_sync(~0u, low[i][p], 1);
-                low[i][p] += __shfl_xor_sync(~0u, low[i][p], 2);
-            }
-        if (quad == 0) {
-            most_w[warp * HEADS + i * 8 + lane / 4] = most[i];
-            sum_w[warp * HEADS + i * 8 + lane / 4] = sum[i];
+                for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                    for (int e = 4; e < 32; e <<= 1) {
+                        sum[n][i] += __shfl_xor_sync(~0u, sum[n][i], e);
+                        if (DTYPE == ST_I4)
+#pragma unroll
+                            for (int p = 0; p < GROUPS; ++p) low[n][i][p] += __shfl_xor_sync(~0u, low[n][i][p], e);
+                    }
+                    const int head = n * 8 + 2 * quad + i, r = lane / 4;
+                    if (head >= g) continue;
+                    // a sum of 0 says that there is no key; where there are, of scores -inf all, it is 1, of weight 0
+                    const bool least = most[n][i] == -INFINITY && any != 0u && sum[n][i] == 0.f;
+                    if (!done && r == 0) {
+                        (whole ? a.part_most + part * rows + id : a.slot_most + slot)[head] = most[n][i];
+                        (whole ? a.part_sum + part * rows + id : a.slot_sum + slot)[head] = least ? 1.f : sum[n][i];
+                    }
+                    const float f = !done ? 1.f : any ? (least ? NAN : 1.f / sum[n][i]) : 0.f;
+                    bf16 *out = a.out + ((int64_t)here.b * a.heads + head0 + head) * cs.d;
+                    float *values = a.slot + (slot + head) * DP;
+                    // four columns from `col` on of the output, or of where it goes to be joined
+                    auto put4 = [&](int col, float x, float y, float z, float w) {
+                        if (!done) *reinterpret_cast<float4 *>(whole ? a.part + ((part * (DP / 4) + col / 4) * rows + id + head) * 4 : values + col) = make_float4(x, y, z, w);
+                        else if (col < cs.d) *reinterpret_cast<uint2 *>(out + col) = make_uint2(pair_bf16(x * f, y * f), pair_bf16(z * f, w * f));
+                    };
+                    auto put2 = [&](int col, float x, float y) {
+                        if (!done) *reinterpret_cast<float2 *>(whole ? a.part + ((part * (DP / 4) + col / 4) * rows + id + head) * 4 + col % 4 : values + col) = make_float2(x, y);
+                        else if (col < cs.d) *reinterpret_cast<uint32_t *>(out + col) = pair_bf16(x * f, y * f);
+                    };
+                    auto put1 = [&](int col, float x) {
+                        if (!done) (whole ? a.part + ((part * (DP / 4) + col / 4) * rows + id + head) * 4 + col % 4 : values + col)[0] = x;
+                        else if (col < cs.d) out[col] = __float2bfloat16(x * f);
+                    };
+                    // the rows of a product's results, as the values' cells lay
+                    if (DTYPE == ST_BF16)
+#pragma unroll
+                        for (int k = 0; k < DP / 16; ++k) {
+                            put1(k * 16 + r, o[k][n][i]);
+                            put1(k * 16 + r + 8, o[k][n][2 + i]);
+                        }
+                    if (DTYPE == ST_I8)
+#pragma unroll
+                        for (int k = 0; k < DP / 16; ++k) put2(k * 16 + r * 2, o[k][n][i], o[k][n][2 + i]);
+                    if (DTYPE == ST_I4)
+#pragma unroll
+                        for (int k = 0; k < GROUPS; ++k)
+                            put4(k * 32 + r * 4, o[2 * k][n][i] + low[n][i][k], o[2 * k][n][2 + i] + low[n][i][k], o[2 * k + 1][n][i] + low[n][i][k],
+                                 o[2 * k + 1][n][2 + i] + low[n][i][k]);
+                }
         }
-        // the columns of a product's results, as the values' cells lay
-        float *mine = (float *)(smem + warp * S::RING) + (lane / 4 + i * 8) * DP;
-        if (DTYPE == ST_BF16)
-#pragma unroll
-            for (int n = 0; n < DP / 8; ++n) *reinterpret_cast<float2 *>(mine + n * 8 + quad * 2) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
-        if (DTYPE == ST_I8)
-#pragma unroll
-            for (int n = 0; n < DP / 16; ++n)
-                *reinterpret_cast<float4 *>(mine + n * 16 + quad * 4) = make_float4(o[2 * n][2 * i], o[2 * n + 1][2 * i], o[2 * n][2 * i + 1], o[2 * n + 1][2 * i + 1]);
-        if (DTYPE == ST_I4)
-#pragma unroll
-            for (int n = 0; n < DP / 32; ++n)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    *reinterpret_cast<float4 *>(mine + n * 32 + quad * 8 + e * 4) =
-                        make_float4(o[4 * n][2 * i + e] + low[i][n], o[4 * n + 1][2 * i + e] + low[i][n], o[4 * n + 2][2 * i + e] + low[i][n],
-                                    o[4 * n + 3][2 * i + e] + low[i][n]);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (__any_sync(~0u, bad) && lane == 0) atomicExch(a.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
     }
-    __syncthreads();
-    // weight of a part whose largest score is m, where the largest of all is `all`
-    auto weight = [&](float m, float all) { return m == -INFINITY ? 0.f : exp2f(c * (m - all)); };
-    if (threadIdx.x < HEADS) {
-        float all = -INFINITY, s = 0.f, w[WARPS];
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) all = fmaxf(all, most_w[i * HEADS + threadIdx.x]);
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) {
-            w[i] = weight(most_w[i * HEADS + threadIdx.x], all);
-            s += sum_w[i * HEADS + threadIdx.x] * w[i];
-        }
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) most_w[i * HEADS + threadIdx.x] = w[i];
-        most_b[threadIdx.x] = all;
-        // a sum of 0 says that there is no key; where there are, of scores -inf all, it is 1, of weight 0
-        sum_b[threadIdx.x] = all == -INFINITY && flags[1] && s == 0.f ? 1.f : s;
+    if (a.part_count) pdl_wait();                          // whoever waits for this kernel waits for the prefix's too
+}
+
+// Units that several warps had pieces of, and all of them where prefixes have parts; what has no visible key is 0.  A block to a unit: first the largest score
+// and the sum of its pieces and parts, then their weights and the values, four columns to a thread, and several threads for the same columns where there are
+// pieces enough.
+namespace cstep {
+constexpr int JOIN = 512, BATCH = 128;     // threads at most; pieces and parts whose weights are made at a time
+}
+template <int DP>
+__global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStepArgs a, int unit_heads, int keys_of_tile)
+{
+    using namespace cstep;
+    __shared__ float4 joined[JOIN];
+    __shared__ float weights[BATCH][16], all_of[16], inv_of[16];
+    const Cells &cs = a.c;
+    const int chunks = (a.group + unit_heads - 1) / unit_heads, unit = blockIdx.x, b = blockIdx.y;
+    const int hk = unit / chunks, g0 = unit % chunks * unit_heads, g = min(a.group - g0, unit_heads);
+    const float c = a.scale * 1.4426950408889634f;
+    pdl_wait();
+    pdl_trigger();
+    const int64_t total = a.starts[cs.nseq], start = a.starts[b];
+    const int prefix = a.part_count ? min(a.part_count[b], MAX_PARTS) : 0, tiles = (Visible(a, cs.lens[b]).keys + keys_of_tile - 1) / keys_of_tile;
+    int t0 = 0, pieces = 0;                                // the teams whose pieces its first tile and its last are in
+    if (tiles) {
+        const int teams = workers_of(total, a.slots / a.team);
+        const int64_t from = start + (int64_t)(unit / a.team) * length_on_line(tiles) + UNIT_COST;
+        t0 = worker_at(total, teams, from);
+        pieces = worker_at(total, teams, from + tiles - 1) - t0 + 1;
     }
-    __syncthreads();
-    float *block = (float *)smem;                          // the first warp's place
-    for (int e = 4 * threadIdx.x; e < g * DP; e += 4 * WARPS * 32) {
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) {
-            const float w = most_w[i * HEADS + e / DP];
-            const float4 x = *reinterpret_cast<const float4 *>(smem + i * S::RING + e * 4);
-            s = make_float4(fmaf(w, x.x, s.x), fmaf(w, x.y, s.y), fmaf(w, x.z, s.z), fmaf(w, x.w, s.w));
-        }
-        *reinterpret_cast<float4 *>(block + e) = s;
-    }
-    if (splits > 1) tc::cluster_sync_all();
-    else __syncthreads();
-    // then the blocks, and the prefix's parts: their shares first, each read once, then every block its piece of the output
-    int parts = 0;
-    const int rows = cs.nseq * a.group;
-    const int64_t part_row = (int64_t)hk * rows + b * a.group + g0, part_rows = (int64_t)(a.heads / a.group) * rows;
-    if (a.part_count) {
-        pdl_wait();
-        parts = min(a.part_count[b], MAX_PARTS);
-    }
-    if (threadIdx.x < HEADS) {
-        float m[MAX_SPLITS], l[MAX_SPLITS], all = -INFINITY, s = 0.f;
+    if (pieces == 1 && !a.part_count) return;
+    // a unit that one warp had the whole of is among the parts
+    const int n = pieces == 1 ? 0 : pieces, parts = prefix + (pieces == 1), threads = blockDim.x;
+    const int64_t rows = (int64_t)cs.nseq * a.group, id = (int64_t)b * a.group + g0;
+    auto slot_of = [&](int i) { return ((int64_t)((t0 + i) * a.team + unit % a.team) * 2 + (i == 0 ? 1 : 0)) * unit_heads; };
+    auto part_of = [&](int i) { return (int64_t)(i < prefix ? i : a.own_part) * (a.heads / a.group) + hk; };
+    auto most_of = [&](int i, int h) { return i < n ? a.slot_most[slot_of(i) + h] : a.part_most[part_of(i - n) * rows + id + h]; };
+    auto sum_of = [&](int i, int h) { return i < n ? a.slot_sum[slot_of(i) + h] : a.part_sum[part_of(i - n) * rows + id + h]; };
+    for (int h = threadIdx.x / 32; h < g; h += threads / 32) {
+        const int lane = threadIdx.x & 31;
+        float all = -INFINITY, s = 0.f;
         bool seen = false;
-#pragma unroll
-        for (int r = 0; r < MAX_SPLITS; ++r) {
-            m[r] = -INFINITY;
-            l[r] = 0.f;
-            if (r < splits) {
-                m[r] = splits > 1 ? load_cluster(tc::map_to_cta(tc::smem_u32(most_b + threadIdx.x), r)) : most_b[threadIdx.x];
-                l[r] = splits > 1 ? load_cluster(tc::map_to_cta(tc::smem_u32(sum_b + threadIdx.x), r)) : sum_b[threadIdx.x];
-            }
-            all = fmaxf(all, m[r]);
-            seen = seen || l[r] != 0.f;
-        }
-        const int n = threadIdx.x < g ? parts : 0;
-        for (int r = 0; r < n; ++r) all = fmaxf(all, a.part_most[r * part_rows + part_row + threadIdx.x]);
-#pragma unroll
-        for (int r = 0; r < MAX_SPLITS; ++r) {
-            m[r] = weight(m[r], all);
-            s = fmaf(m[r], l[r], s);
-        }
-        for (int r = 0; r < n; ++r) {
-            const float w = weight(a.part_most[r * part_rows + part_row + threadIdx.x], all), x = a.part_sum[r * part_rows + part_row + threadIdx.x];
-            part_share[r * HEADS + threadIdx.x] = w;
-            s = fmaf(w, x, s);
+        for (int i = lane; i < n + parts; i += 32) {
+            // what has come so far relative to the largest so far
+            const float m = most_of(i, h), x = sum_of(i, h), now = fmaxf(all, m);
+            s = s * weight_of(all, now, c) + x * weight_of(m, now, c);
+            all = now;
             seen = seen || x != 0.f;
         }
-        const float inv = seen ? 1.f / s : 0.f;            // a sum of 0 (all scores are -inf) or NaN gives NaN
+        float most = all;
 #pragma unroll
-        for (int r = 0; r < MAX_SPLITS; ++r) share[r * HEADS + threadIdx.x] = m[r] * inv;
-        for (int r = 0; r < n; ++r) part_share[r * HEADS + threadIdx.x] *= inv;
+        for (int e = 16; e > 0; e >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, e));
+        s *= weight_of(all, most, c);
+#pragma unroll
+        for (int e = 16; e > 0; e >>= 1) s += __shfl_xor_sync(~0u, s, e);
+        // no visible key: 0; otherwise a sum of 0 (all scores are -inf) or NaN gives NaN
+        seen = __any_sync(~0u, seen);
+        if (lane == 0) {
+            all_of[h] = most;
+            inv_of[h] = seen ? (s == 0.f ? NAN : 1.f / s) : 0.f;
+        }
     }
     __syncthreads();
-    // four columns to a thread, heads next to one another as they lie in the parts
-    for (int e = split * WARPS * 32 + threadIdx.x; e < g * (DP / 4); e += splits * WARPS * 32) {
-        const int row = e % g, quad4 = e / g, col = quad4 * 4;
+    // heads next to one another, as they lie in the parts
+    const int items = g * (DP / 4), slices = max(1, threads / items), slice = slices > 1 ? threadIdx.x / items : 0;
+    for (int e0 = 0; e0 < items; e0 += threads) {
+        const int e = slices > 1 ? threadIdx.x % items : e0 + threadIdx.x, row = e % g, quad4 = e / g;
+        const bool busy = slice < slices && e < items;
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto more = [&](float w, const float4 &x) { y = make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w)); };
-        if (splits == 1) {
-            more(share[row], *reinterpret_cast<const float4 *>(block + row * DP + col));
-        } else {
+        for (int i0 = 0; i0 < n + parts; i0 += BATCH) {
+            const int end = min(n + parts, i0 + BATCH);
+            __syncthreads();
+            for (int i = threadIdx.x; i < (end - i0) * g; i += threads) weights[i / g][i % g] = weight_of(most_of(i0 + i / g, i % g), all_of[i % g], c);
+            __syncthreads();
+            if (!busy) continue;
+            const int m = min(n, end);                     // pieces, then parts, each from the same slice on
+            int i = i0 + slice;
+            auto more = [&](float w, const float4 &x) { y = make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w)); };
 #pragma unroll 8
-            for (int r = 0; r < splits; ++r) {
-                const uint32_t at = tc::map_to_cta(tc::smem_u32(block + row * DP + col), r);
-                float4 x;
-                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(at) : "memory");
-                more(share[r * HEADS + row], x);
-            }
+            for (; i < m; i += slices) more(weights[i - i0][row], *reinterpret_cast<const float4 *>(a.slot + (slot_of(i) + row) * DP + quad4 * 4));
+#pragma unroll 8
+            for (; i < end; i += slices) more(weights[i - i0][row], *reinterpret_cast<const float4 *>(a.part + ((part_of(i - n) * (DP / 4) + quad4) * rows + id + row) * 4));
         }
-#pragma unroll 4
-        for (int r = 0; r < parts; ++r) {
-            const int64_t unit = (int64_t)r * (a.heads / a.group) + hk;
-            const float w = part_share[r * HEADS + row];
-            // a part without a finite score was not written, and one whose sum is NaN says so by its share
-            if (w != 0.f) more(w, *reinterpret_cast<const float4 *>(a.part + ((unit * (DP / 4) + quad4) * rows + b * a.group + g0 + row) * 4));
+        if (slices > 1) {
+            joined[threadIdx.x] = y;
+            __syncthreads();
+            if (busy && slice == 0)
+                for (int i = 1; i < slices; ++i) {
+                    const float4 x = joined[i * items + e];
+                    y = make_float4(y.x + x.x, y.y + x.y, y.z + x.z, y.w + x.w);
+                }
         }
-        if (col < cs.d)
-            *reinterpret_cast<uint2 *>(a.out + ((int64_t)b * a.heads + head0 + row) * cs.d + col) = make_uint2(pair_bf16(y.x, y.y), pair_bf16(y.z, y.w));
+        if (busy && slice == 0 && quad4 * 4 < cs.d) {
+            const float f = inv_of[row];
+            *reinterpret_cast<uint2 *>(a.out + ((int64_t)b * a.heads + hk * a.group + g0 + row) * cs.d + quad4 * 4) =
+                make_uint2(pair_bf16(y.x * f, y.y * f), pair_bf16(y.z * f, y.w * f));
+        }
     }
-    if (splits > 1) tc::cluster_sync_all();                // no block ends while another reads its shared memory
-    if (flags[0] && threadIdx.x == 0) atomicExch(a.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
 }
 
-__global__ void clear_status_kernel(unsigned *status, int *counts, int n)
+// Sums up the tiles of all sequences; one block, so that it may clear the status and then report lengths that the tables do not hold.
+__global__ void __launch_bounds__(1024) cells_plan_kernel(const CellsStepArgs a, int keys_of_tile)
 {
+    __shared__ int64_t sums[32];
+    __shared__ int64_t before;
     pdl_trigger();
     pdl_wait();
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < 2) status[i == 0 ? kWsStatusWord : kWsDetailWord] = 0u;
-    if (i < n) counts[i] = 0;
-}
-
-st_status clear_status(unsigned *status, int *counts, int n, cudaStream_t stream)
-{
-    return launch(clear_status_kernel, dim3((unsigned)(n / 256 + 1)), n > 32 ? 256 : 32, 0, stream, status, counts, n);
-}
-
-template <int DTYPE, int DP, int WARPS, int STAGES, bool WIDE>
-static st_status launch_cells(const CellsStepArgs &a, int splits, cudaStream_t stream)
-{
-    const auto kernel = cells_step_kernel<DTYPE, DP, WARPS, STAGES, WIDE>;
-    const size_t smem = cstep::Shape<DTYPE, DP, WARPS, STAGES>::SMEM;
-    if (!ensure_dynamic_smem(kernel, smem) || !allow_large_clusters(kernel)) return ST_ERR_CUDA;
-    const int chunks = (a.group + cstep::HEADS - 1) / cstep::HEADS;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)splits, (unsigned)(a.heads / a.group * chunks), (unsigned)a.c.nseq);
-    cfg.blockDim = dim3(WARPS * 32);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)splits;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = splits > 1 ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return ST_ERR_CUDA;
+    const Cells &cs = a.c;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    bool fine = true;
+    if (threadIdx.x == 0) before = 0;
+    for (int b0 = 0; b0 < cs.nseq; b0 += blockDim.x) {
+        const int b = b0 + threadIdx.x;
+        int64_t mine = 0;
+        if (b < cs.nseq) {
+            const int told = cs.lens[b];
+            fine = fine && told == length_of(told, cs.cols, cs.page);
+            mine = (int64_t)length_on_line((Visible(a, told).keys + keys_of_tile - 1) / keys_of_tile) * (a.units / a.team);
+            if (a.part_count) a.part_count[b] = 0;
+        }
+        int64_t sum = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(~0u, sum, o);
+            if (lane >= o) sum += x;
+        }
+        if (lane == 31) sums[warp] = sum;
+        __syncthreads();
+        if (warp == 0) {
+            int64_t s = lane < warps ? sums[lane] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t x = __shfl_up_sync(~0u, s, o);
+                if (lane >= o) s += x;
+            }
+            sums[lane] = s;
+        }
+        __syncthreads();
+        const int64_t at = before + (warp ? sums[warp - 1] : 0) + sum;
+        if (b < cs.nseq) a.starts[b + 1] = at;
+        __syncthreads();
+        if (threadIdx.x == blockDim.x - 1) before = at;
+        __syncthreads();
     }
-    return ST_OK;
+    fine = __syncthreads_and(fine);
+    if (threadIdx.x == 0) {
+        a.starts[0] = 0;
+        a.status[kWsStatusWord] = fine ? 0u : (unsigned)ST_ERR_DEV_BOUNDS;
+        a.status[kWsDetailWord] = 0u;
+    }
 }
 
-// Where heads and sequences are few the keys are split over a cluster of up to 16 blocks.
+StepPlan step_plan(int64_t nseq, size_t from)
+{
+    StepPlan p;
+    // slots of 16 heads and two blocks an SM, or of 8 and up to four
+    const size_t rows = (size_t)sm_count_or_default() * cstep::MOST_BLOCKS * cstep::WARPS * 2 * 8;
+    p.starts = round_up(from, 256);
+    p.most = round_up(p.starts + (nseq + 1) * sizeof(int64_t), 256);
+    p.sum = p.most + rows * sizeof(float);
+    p.values = p.sum + rows * sizeof(float);
+    p.bytes = p.values + rows * 128 * sizeof(float);
+    return p;
+}
+
+void place_step(CellsStepArgs &a, const StepPlan &p, void *ws)
+{
+    char *at = (char *)ws;
+    a.starts = (int64_t *)(at + p.starts);
+    a.slot_most = (float *)(at + p.most);
+    a.slot_sum = (float *)(at + p.sum);
+    a.slot = (float *)(at + p.values);
+}
+
+size_t attn_step_workspace(int64_t nseq) { return nseq > 0 && nseq <= 65535 ? step_plan(nseq, kWsHeaderBytes).bytes : 0; }
+
+// Query heads of a unit: up to 8 of them take half of the products of 16.
+static int unit_heads(const CellsStepArgs &a) { return a.group <= 8 ? 8 : 16; }
+static int tile_keys(int dtype) { return dtype == ST_BF16 ? 16 : 32; }
+
+st_status plan_step(CellsStepArgs &a, int dtype, cudaStream_t stream)
+{
+    a.units = a.heads / a.group * ((a.group + unit_heads(a) - 1) / unit_heads(a));
+    a.team = a.units % 4 == 0 ? 4 : a.units % 2 == 0 ? 2 : 1;
+    return launch(cells_plan_kernel, dim3(1), a.c.nseq > 256 ? 1024 : 256, 0, stream, a, tile_keys(dtype));
+}
+
+template <int DTYPE, int DP, int HN, bool WIDE>
+static st_status run_heads(CellsStepArgs a, cudaStream_t stream)
+{
+    using S = cstep::Shape<DTYPE, DP, HN>;
+    static_assert(S::BLOCKS * S::HEADS <= cstep::MOST_BLOCKS * 8 && S::KEYS == (DTYPE == ST_BF16 ? 16 : 32), "as the workspace and the plan have it");
+    if (!ensure_dynamic_smem(cells_step_kernel<DTYPE, DP, HN, WIDE>, S::SMEM)) return ST_ERR_CUDA;
+    const int blocks = sm_count_or_default() * S::BLOCKS;
+    a.slots = blocks * cstep::WARPS;
+    const st_status rc = launch(cells_step_kernel<DTYPE, DP, HN, WIDE>, dim3((unsigned)blocks), cstep::WARPS * 32, S::SMEM, stream, a);
+    if (rc != ST_OK) return rc;
+    // few units may have many pieces each
+    const int threads = (int64_t)a.units * a.c.nseq >= 2 * sm_count_or_default() ? 128 : 512;
+    return launch(cells_join_kernel<DP>, dim3((unsigned)a.units, (unsigned)a.c.nseq), threads, 0, stream, a, S::HEADS, S::KEYS);
+}
+
 template <int DTYPE, int DP, bool WIDE>
 static st_status run_cells(const CellsStepArgs &a, cudaStream_t stream)
 {
-    using S = cstep::Shape<DTYPE, DP, 4, 2>;
-    const int64_t most = (int64_t)a.c.cols * a.c.page, visible = most < (int64_t)a.window + a.sinks ? most : (int64_t)a.window + a.sinks;
-    const int64_t blocks = (int64_t)a.c.nseq * (a.heads / a.group) * ((a.group + cstep::HEADS - 1) / cstep::HEADS);
-    const int64_t sms = sm_count_or_default(), tiles = (visible + S::KEYS - 1) / S::KEYS;
-    int n = 1;
-    while (n < cstep::MAX_SPLITS && blocks * n < 3 * sms && tiles > (int64_t)2 * n * 4 * cstep::FEWEST) n *= 2;
-    return launch_cells<DTYPE, DP, 4, 2, WIDE>(a, n, stream);
+    return unit_heads(a) == 8 ? run_heads<DTYPE, DP, 1, WIDE>(a, stream) : run_heads<DTYPE, DP, 2, WIDE>(a, stream);
 }
 
 st_status run_cells_step(const CellsStepArgs &a, int dtype, cudaStream_t stream)
@@ -645,17 +866,19 @@ extern "C" st_status st_attn_cache_step(const st_cells *c, const void *q, int64_
     if (rc != ST_OK) return rc;
     if (window < 1 || sinks < 0) return ST_ERR_SHAPE;
     if ((rc = check_step(c, q, q_row, q_head, scale, out)) != ST_OK) return rc;
-    if (!ws || ws_bytes < kWsHeaderBytes) return ST_ERR_WORKSPACE;
+    const StepPlan plan = step_plan(c->nseq, kWsHeaderBytes);
+    if (!ws || ws_bytes < plan.bytes) return ST_ERR_WORKSPACE;
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     CellsStepArgs a = step_args(c, q, q_row, q_head, k_pages, v_pages, k_scales, v_scales, table, lens, scale, out, ws);
     a.window = clamp_int(window, 1 << 30);
     a.sinks = clamp_int(sinks, 1 << 30);
     const int64_t bytes = c->nseq * c->heads * c->d * 2;
-    // blocks that share 16 heads or fewer read their queries before any of them writes
+    // a unit's output is written when all that reads its queries is done
     const Operand Q = {q, c->nseq, c->heads, c->d, a.q_row, a.q_head};
     if (Q.under(out, bytes, true) || meets_cells(c, k_pages, k_scales, out, bytes) || meets_cells(c, v_pages, v_scales, out, bytes) ||
         arrays_meet(out, bytes, table, c->nseq * c->table_cols * 4) || arrays_meet(out, bytes, lens, c->nseq * 4))
         return ST_ERR_UNSUPPORTED;
-    if ((rc = clear_status(a.status, nullptr, 0, (cudaStream_t)stream)) != ST_OK) return rc;
+    place_step(a, plan, ws);
+    if ((rc = plan_step(a, c->dtype, (cudaStream_t)stream)) != ST_OK) return rc;
     return run_cells_step(a, c->dtype, (cudaStream_t)stream);
 }

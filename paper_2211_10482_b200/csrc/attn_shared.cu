@@ -1,9 +1,9 @@
 // st_attn_shared_step: one token of every sequence over a prefix that its group of sequences shares, then over its own tokens.
 //
-// Two kernels.  The first takes all queries of a group that read one key head as the rows of a matrix, up to 256 of them, and makes
+// Two kernels, between one that lays out the work and one that joins.  The first takes all queries of a group that read one key head as the rows of a matrix, up to 256 of them, and makes
 //     S = Q K^T  (tcgen05, fp32 in tensor memory);   P = exp2(c S - c m)  (one thread per row);   O += P V
 // over a range of the prefix's keys, as st_attn_window does for a tile of a prompt; it leaves (m, l, O) as a part.  The second is the single-token kernel over
-// each sequence's own keys, which joins the parts with what it has itself.  A row of the prefix is so read once for 256 queries, not once for
+// each sequence's own keys, whose pieces are joined with the parts.  A row of the prefix is so read once for 256 queries, not once for
 // every sequence.
 //
 // The prefix lies in pages of any size, so its rows are gathered by cp.async into the swizzled tiles that the tensor cores read; one or two warps for each stage,
@@ -24,7 +24,6 @@ struct SharedArgs {
     int groups, prefix_cols;
     int seqs;                              // of a tile of rows
     int slots, most_parts;                 // blocks, parts of a prefix
-    int *part_count;
     float *part_most, *part_sum, *part;
 };
 
@@ -176,7 +175,7 @@ __global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_p
         tmem_relinquish();
     }
     if (hk == 0 && at.part == 0)
-        for (int i = threadIdx.x; i < seqs; i += S::THREADS) a.part_count[b0 + i] = at.parts;
+        for (int i = threadIdx.x; i < seqs; i += S::THREADS) a.step.part_count[b0 + i] = at.parts;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -413,6 +412,7 @@ __global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_p
 struct SharedPlan {
     int tiles_of, seqs, slots, most_parts;
     size_t counts, most, sum, part, bytes;                 // where they begin
+    StepPlan step;
 };
 static bool shared_plan(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t groups, SharedPlan *p)
 {
@@ -426,12 +426,13 @@ static bool shared_plan(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t g
     // room for as many parts of one prefix as the SMs can take at a time, beside the other tiles of rows that there are at least
     const int64_t parts = (sms + least - 1) / least;
     p->most_parts = (int)(parts < 1 ? 1 : parts > MAX_PARTS ? MAX_PARTS : parts);
-    const size_t rows = (size_t)nseq * heads * p->most_parts;
+    const size_t rows = (size_t)nseq * heads * (p->most_parts + 1);        // and one for the own tokens
     p->counts = kWsHeaderBytes;
     p->most = round_up(p->counts + nseq * sizeof(int), 256);
     p->sum = round_up(p->most + rows * sizeof(float), 256);
     p->part = round_up(p->sum + rows * sizeof(float), 256);
-    p->bytes = p->part + rows * 128 * sizeof(float);
+    p->step = step_plan(nseq, p->part + rows * 128 * sizeof(float));
+    p->bytes = p->step.bytes;
     return true;
 }
 
@@ -475,7 +476,7 @@ extern "C" st_status st_attn_shared_step(const st_cells *c, const void *q, int64
     if (!aligned256(ws)) return ST_ERR_ALIGN;
     SharedArgs a = {};
     a.step = step_args(c, q, q_row, q_head, k_pages, v_pages, nullptr, nullptr, table, lens, scale, out, ws);
-    // the second kernel writes out, and blocks of it read their own queries alone; the first has read all of them by then
+    // out is written when all queries have been read
     const int64_t bytes = c->nseq * c->heads * c->d * 2;
     const Operand Q = {q, c->nseq, c->heads, c->d, a.step.q_row, a.step.q_head};
     if (Q.under(out, bytes, true) || meets_cells(c, k_pages, nullptr, out, bytes) || meets_cells(c, v_pages, nullptr, out, bytes) ||
@@ -491,17 +492,18 @@ extern "C" st_status st_attn_shared_step(const st_cells *c, const void *q, int64
     a.seqs = p.seqs;
     a.slots = p.slots;
     a.most_parts = p.most_parts;
-    a.part_count = (int *)((char *)ws + p.counts);
     a.part_most = (float *)((char *)ws + p.most);
     a.part_sum = (float *)((char *)ws + p.sum);
     a.part = (float *)((char *)ws + p.part);
-    if ((rc = clear_status(a.step.status, a.part_count, (int)c->nseq, (cudaStream_t)stream)) != ST_OK) return rc;
-    if (c->d <= 64) rc = p.tiles_of == 1 ? run_prefix<64, 1>(a, (cudaStream_t)stream) : run_prefix<64, 2>(a, (cudaStream_t)stream);
-    else rc = p.tiles_of == 1 ? run_prefix<128, 1>(a, (cudaStream_t)stream) : run_prefix<128, 2>(a, (cudaStream_t)stream);
-    if (rc != ST_OK) return rc;
-    a.step.part_count = a.part_count;
+    place_step(a.step, p.step, ws);
+    a.step.part_count = (int *)((char *)ws + p.counts);
+    a.step.own_part = p.most_parts;
     a.step.part_most = a.part_most;
     a.step.part_sum = a.part_sum;
     a.step.part = a.part;
+    if ((rc = plan_step(a.step, ST_BF16, (cudaStream_t)stream)) != ST_OK) return rc;
+    if (c->d <= 64) rc = p.tiles_of == 1 ? run_prefix<64, 1>(a, (cudaStream_t)stream) : run_prefix<64, 2>(a, (cudaStream_t)stream);
+    else rc = p.tiles_of == 1 ? run_prefix<128, 1>(a, (cudaStream_t)stream) : run_prefix<128, 2>(a, (cudaStream_t)stream);
+    if (rc != ST_OK) return rc;
     return run_cells_step(a.step, ST_BF16, (cudaStream_t)stream);
 }

@@ -1096,7 +1096,7 @@ PyObject *py_attn_cache_step(PyObject *const *v)
     const int64_t window = count_of(v[5]), sinks = count_of(v[6]);
     const float scale = scale_of(v[9], x.c.d);
     Ref out(result(v[10], v[0], q, q.sizes(), at::kBFloat16, "out"));
-    const Workspace w = workspace(v[11], v[0], q, ST_OP_ATTN_CACHE, 0, 0, 0, 0, 0);
+    const Workspace w = workspace(v[11], v[0], q, ST_OP_ATTN_CACHE_STEP, x.c.nseq, 0, 0, 0, 0);
     const void *pq = q.data_ptr();
     const int64_t row = q.stride(0), head = q.stride(1);
     void *po = data(out);
