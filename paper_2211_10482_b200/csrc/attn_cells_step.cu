@@ -9,13 +9,15 @@
 // heads as its 8 columns:  S^T = K Q^T,  O^T = V^T P^T.  (Heads as rows would leave half of a product, of the scores in registers and of the sums empty
 // up to 8 heads.)  Weights go from the first product's layout to the second's by transposing 8 x 8 matrices of bf16 within the warp.
 //
-// Cells meet the tensor cores as whole numbers in bf16, which holds all of them exactly, made from their bits (0x43 beside a byte or nibble c below 128 is
-// 128 + c).  Scales come in afterwards, where they are one number for a key (ST_I8: a score times its key's scale, a weight
+// Cells meet the tensor cores as whole numbers in fp16 or bf16, which hold all of them exactly, made from their bits (0x64 beside a byte u is 1024 + u in
+// fp16, 0x43 beside a byte or nibble below 128 is 128 + it in bf16).  fp16 takes less, where the other operand fits: the queries, each head's times the power
+// of two that brings its largest number to 2^8, which leaves all of bf16's digits down to 2^-22 of that; weights times their values' scales do not.  Scales come in afterwards, where they are one number for a key (ST_I8: a score times its key's scale, a weight
 // times its value's) or for 32 columns (ST_I4: partial scores of 32 columns, x += step acc + lo sum(q); a set of weights for each 32 columns, and what lo
 // brings beside it, sum(w lo)).  The order of a fragment's columns is free as long as both operands agree, so that no byte has to change its lane:
 // a lane's four bytes of K are four or eight consecutive columns, of which the queries' fragments take the same ones.
 #include "attn_cells_step.cuh"
 #include "tc_common.cuh"
+#include <cuda_fp16.h>
 
 namespace st {
 namespace attn {
@@ -60,6 +62,12 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_half(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 // An 8 x 8 matrix of bf16, two to a lane, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x)
 {
@@ -96,6 +104,13 @@ __device__ __forceinline__ uint32_t bytes_bf16(uint32_t w, uint32_t which)
         "fma.rn.bf16x2 %0, h, %6, t;\n\t}"
         : "=r"(r)
         : "r"(x), "r"(0x3F003F00u), "r"(0xC300C300u), "r"(0x3F803F80u), "r"(0xC380C380u), "r"(0xBF80BF80u));
+    return r;
+}
+// The same in fp16: 0x64 beside u is 1024 + u.
+__device__ __forceinline__ uint32_t bytes_half(uint32_t w, uint32_t which)
+{
+    uint32_t r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(__byte_perm(w, 0x64646464u, which)), "r"(0xE480E480u));
     return r;
 }
 // Nibbles i and i + 4 of w.
@@ -227,6 +242,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
         const int piece = lane % PIECES, row0 = lane / PIECES;
         const int bytes = DTYPE == ST_BF16 ? 2 * cs.d - piece * 16 : DTYPE == ST_I8 ? cs.d - piece * 16 : cs.d / 2 - piece * 16;   // of the row from this piece on
         constexpr int ROWS = 32 / PIECES;                  // rows that a warp copies at a time
+        constexpr unsigned ALL = KEYS == 32 ? ~0u : 0xFFFFu;
         // Copies the tile whose places were found.  Bit r: row r is there; what is not there is zeros.
         auto fetch = [&](int stage) -> unsigned {
             const unsigned there = __ballot_sync(~0u, cell >= 0 && lane < KEYS);
@@ -255,6 +271,17 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                     }
                 }
                 __syncwarp();
+                if (WIDE && there == ALL && bytes > 0) {
+                    const unsigned char *k = cs.k + piece * 16, *v = cs.v + piece * 16;
+#pragma unroll
+                    for (int i = 0; i < KEYS / ROWS; ++i) {
+                        const int row = row0 + i * ROWS;
+                        const int64_t from = at[row];
+                        const uint32_t o = dst + row * ROW + ((piece ^ S::swizzle(row)) << 4);
+                        copy_async<16>(o, k + from, true);
+                        copy_async<16>(o + S::TILE, v + from, true);
+                    }
+                } else
 #pragma unroll
                 for (int i = 0; i < KEYS / ROWS; ++i) {
                     const int row = row0 + i * ROWS;
@@ -302,6 +329,36 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                         if (head < g && col < cs.d)        // rows are whole eights of columns
                             q[k][n][j] = DTYPE == ST_I4 ? (uint32_t)from[col] | (uint32_t)from[col + 4] << 16 : *reinterpret_cast<const uint32_t *>(from + col);
                     }
+            }
+            // ST_I8: as fp16, times a power of two; unit[n][i] is what scores are in, for the two heads of this lane's scores
+            float unit_c[HN][2], unit_of[HN][2];
+#pragma unroll
+            for (int n = 0; n < HN; ++n) {
+                float in = 1.f;
+                if (DTYPE == ST_I8) {
+                    unsigned top = 0;
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) top = max(top, max(q[k][n][j] & 0x7FFFu, q[k][n][j] >> 16 & 0x7FFFu));
+                    top = max(top, __shfl_xor_sync(~0u, top, 1));
+                    top = max(top, __shfl_xor_sync(~0u, top, 2));
+                    const int exponent = top >> 7;         // of the largest, with 127 added
+                    const float f = __uint_as_float((unsigned)min(262 - exponent, 254) << 23);
+                    in = exp2f((float)(127 - min(262 - exponent, 254)));
+#pragma unroll
+                    for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const __half2 two = __floats2half2_rn(low_bf16(q[k][n][j]) * f, high_bf16(q[k][n][j]) * f);
+                            q[k][n][j] = *reinterpret_cast<const uint32_t *>(&two);
+                        }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    unit_of[n][i] = DTYPE == ST_I8 ? __shfl_sync(~0u, in, (2 * quad + i) * 4) : 1.f;
+                    unit_c[n][i] = DTYPE == ST_I8 ? c * unit_of[n][i] : c;
+                }
             }
             // ST_I4: sums of 32 columns of the queries, for the two heads of this lane's scores
             float qsum[HN][2][GROUPS];
@@ -365,9 +422,9 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             for (int m = 0; m < 4; ++m) f[m] ^= 0x80808080u;
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
-                                const uint32_t c[4] = {bytes_bf16(f[2 * m], 0x4140u), bytes_bf16(f[2 * m + 1], 0x4140u), bytes_bf16(f[2 * m], 0x4342u), bytes_bf16(f[2 * m + 1], 0x4342u)};
+                                const uint32_t c[4] = {bytes_half(f[2 * m], 0x4140u), bytes_half(f[2 * m + 1], 0x4140u), bytes_half(f[2 * m], 0x4342u), bytes_half(f[2 * m + 1], 0x4342u)};
 #pragma unroll
-                                for (int n = 0; n < HN; ++n) mma(x[h][n], c, q[2 * k + m][n][0], q[2 * k + m][n][1]);
+                                for (int n = 0; n < HN; ++n) mma_half(x[h][n], c, q[2 * k + m][n][0], q[2 * k + m][n][1]);
                             }
                         }
                         const float s0 = __uint_as_float(kscale[h * 16]), s1 = __uint_as_float(kscale[h * 16 + 8]);
@@ -409,7 +466,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                         }
                     }
                 }
-                if (there != (KEYS == 32 ? ~0u : 0xFFFFu)) {
+                if (there != ALL) {
                     const unsigned mine = there >> (lane / 4);
 #pragma unroll
                     for (int h = 0; h < NK; ++h)
@@ -431,7 +488,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
 #pragma unroll
                         for (int e = 4; e < 32; e <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, e));
                         top[n][i] = m;
-                        moves = moves || c * (m - most[n][i]) > 8.f;
+                        moves = moves || unit_c[n][i] * (m - most[n][i]) > 8.f;
                     }
                 // as long as no weight passes 2^8 the reference stays: any reference gives the same quotient
                 if (__any_sync(~0u, moves)) {
@@ -439,7 +496,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                     for (int n = 0; n < HN; ++n)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const float now = fmaxf(most[n][i], top[n][i]), f = now == -INFINITY ? 1.f : exp2f(c * (most[n][i] - now));
+                            const float now = fmaxf(most[n][i], top[n][i]), f = now == -INFINITY ? 1.f : exp2f(unit_c[n][i] * (most[n][i] - now));
                             most[n][i] = now;
                             sum[n][i] *= f;
                             if (DTYPE == ST_I4)
@@ -461,7 +518,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                         float *y = x[h][n];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            y[i] = exp2_fast(fmaf(c, y[i], most[n][i & 1] == -INFINITY ? 0.f : -c * most[n][i & 1]));
+                            y[i] = exp2_fast(fmaf(unit_c[n][i & 1], y[i], most[n][i & 1] == -INFINITY ? 0.f : -unit_c[n][i & 1] * most[n][i & 1]));
                             sum[n][i & 1] += y[i];
                         }
                         // times their values' scales, rounded once for the product with V
@@ -563,7 +620,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                     // a sum of 0 says that there is no key; where there are, of scores -inf all, it is 1, of weight 0
                     const bool least = most[n][i] == -INFINITY && any != 0u && sum[n][i] == 0.f;
                     if (!done && r == 0) {
-                        (whole ? a.part_most + part * rows + id : a.slot_most + slot)[head] = most[n][i];
+                        (whole ? a.part_most + part * rows + id : a.slot_most + slot)[head] = most[n][i] * unit_of[n][i];
                         (whole ? a.part_sum + part * rows + id : a.slot_sum + slot)[head] = least ? 1.f : sum[n][i];
                     }
                     const float f = !done ? 1.f : any ? (least ? NAN : 1.f / sum[n][i]) : 0.f;
@@ -605,18 +662,18 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
     if (a.part_count) pdl_wait();                          // whoever waits for this kernel waits for the prefix's too
 }
 
-// Units that several warps had pieces of, and all of them where prefixes have parts; what has no visible key is 0.  A block to a unit: first the largest score
-// and the sum of its pieces and parts, then their weights and the values, four columns to a thread, and several threads for the same columns where there are
-// pieces enough.
+// Units that several warps had pieces of, and all of them where prefixes have parts; what has no visible key is 0.  A block to a unit, four columns of a head to
+// a thread, and several threads for the same columns where there are pieces enough: each goes through its pieces and parts once, with the largest score and
+// the sum of those so far, a few on their way at a time.
 namespace cstep {
-constexpr int JOIN = 512, BATCH = 128;     // threads at most; pieces and parts whose weights are made at a time
+constexpr int JOIN = 512, BATCH = 4;       // threads at most; pieces on their way
 }
 template <int DP>
 __global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStepArgs a, int unit_heads, int keys_of_tile)
 {
     using namespace cstep;
     __shared__ float4 joined[JOIN];
-    __shared__ float weights[BATCH][16], all_of[16], inv_of[16];
+    __shared__ float most_j[JOIN], sum_j[JOIN];
     const Cells &cs = a.c;
     const int chunks = (a.group + unit_heads - 1) / unit_heads, unit = blockIdx.x, b = blockIdx.y;
     const int hk = unit / chunks, g0 = unit % chunks * unit_heads, g = min(a.group - g0, unit_heads);
@@ -638,64 +695,58 @@ __global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStep
     const int64_t rows = (int64_t)cs.nseq * a.group, id = (int64_t)b * a.group + g0;
     auto slot_of = [&](int i) { return ((int64_t)((t0 + i) * a.team + unit % a.team) * 2 + (i == 0 ? 1 : 0)) * unit_heads; };
     auto part_of = [&](int i) { return (int64_t)(i < prefix ? i : a.own_part) * (a.heads / a.group) + hk; };
-    auto most_of = [&](int i, int h) { return i < n ? a.slot_most[slot_of(i) + h] : a.part_most[part_of(i - n) * rows + id + h]; };
-    auto sum_of = [&](int i, int h) { return i < n ? a.slot_sum[slot_of(i) + h] : a.part_sum[part_of(i - n) * rows + id + h]; };
-    for (int h = threadIdx.x / 32; h < g; h += threads / 32) {
-        const int lane = threadIdx.x & 31;
-        float all = -INFINITY, s = 0.f;
-        bool seen = false;
-        for (int i = lane; i < n + parts; i += 32) {
-            // what has come so far relative to the largest so far
-            const float m = most_of(i, h), x = sum_of(i, h), now = fmaxf(all, m);
-            s = s * weight_of(all, now, c) + x * weight_of(m, now, c);
-            all = now;
-            seen = seen || x != 0.f;
-        }
-        float most = all;
-#pragma unroll
-        for (int e = 16; e > 0; e >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, e));
-        s *= weight_of(all, most, c);
-#pragma unroll
-        for (int e = 16; e > 0; e >>= 1) s += __shfl_xor_sync(~0u, s, e);
-        // no visible key: 0; otherwise a sum of 0 (all scores are -inf) or NaN gives NaN
-        seen = __any_sync(~0u, seen);
-        if (lane == 0) {
-            all_of[h] = most;
-            inv_of[h] = seen ? (s == 0.f ? NAN : 1.f / s) : 0.f;
-        }
-    }
-    __syncthreads();
     // heads next to one another, as they lie in the parts
     const int items = g * (DP / 4), slices = max(1, threads / items), slice = slices > 1 ? threadIdx.x / items : 0;
     for (int e0 = 0; e0 < items; e0 += threads) {
         const int e = slices > 1 ? threadIdx.x % items : e0 + threadIdx.x, row = e % g, quad4 = e / g;
         const bool busy = slice < slices && e < items;
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i0 = 0; i0 < n + parts; i0 += BATCH) {
-            const int end = min(n + parts, i0 + BATCH);
-            __syncthreads();
-            for (int i = threadIdx.x; i < (end - i0) * g; i += threads) weights[i / g][i % g] = weight_of(most_of(i0 + i / g, i % g), all_of[i % g], c);
-            __syncthreads();
-            if (!busy) continue;
-            const int m = min(n, end);                     // pieces, then parts, each from the same slice on
-            int i = i0 + slice;
-            auto more = [&](float w, const float4 &x) { y = make_float4(fmaf(w, x.x, y.x), fmaf(w, x.y, y.y), fmaf(w, x.z, y.z), fmaf(w, x.w, y.w)); };
-#pragma unroll 8
-            for (; i < m; i += slices) more(weights[i - i0][row], *reinterpret_cast<const float4 *>(a.slot + (slot_of(i) + row) * DP + quad4 * 4));
-#pragma unroll 8
-            for (; i < end; i += slices) more(weights[i - i0][row], *reinterpret_cast<const float4 *>(a.part + ((part_of(i - n) * (DP / 4) + quad4) * rows + id + row) * 4));
+        float all = -INFINITY, s = 0.f;
+        bool seen = false;
+        auto more = [&](float m, float l, const float4 &x) {
+            const float now = fmaxf(all, m), f = weight_of(all, now, c), w = weight_of(m, now, c);
+            y = make_float4(fmaf(w, x.x, y.x * f), fmaf(w, x.y, y.y * f), fmaf(w, x.z, y.z * f), fmaf(w, x.w, y.w * f));
+            s = fmaf(w, l, s * f);
+            all = now;
+            seen = seen || l != 0.f;
+        };
+        // the pieces from this slice on, then the parts; what there is no more of is what has no key
+        auto go = [&](int count, auto most, auto sum, auto values) {
+            for (int i0 = slice; i0 < count; i0 += BATCH * slices) {
+                float m[BATCH], l[BATCH];
+                float4 x[BATCH];
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) {
+                    const int i = i0 + u * slices;
+                    m[u] = -INFINITY;
+                    l[u] = 0.f;
+                    x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (i >= count) continue;
+                    m[u] = *most(i);
+                    l[u] = *sum(i);
+                    x[u] = *reinterpret_cast<const float4 *>(values(i));
+                }
+#pragma unroll
+                for (int u = 0; u < BATCH; ++u) more(m[u], l[u], x[u]);
+            }
+        };
+        if (busy) {
+            go(n, [&](int i) { return a.slot_most + slot_of(i) + row; }, [&](int i) { return a.slot_sum + slot_of(i) + row; },
+               [&](int i) { return a.slot + (slot_of(i) + row) * DP + quad4 * 4; });
+            go(parts, [&](int i) { return a.part_most + part_of(i) * rows + id + row; }, [&](int i) { return a.part_sum + part_of(i) * rows + id + row; },
+               [&](int i) { return a.part + ((part_of(i) * (DP / 4) + quad4) * rows + id + row) * 4; });
         }
         if (slices > 1) {
             joined[threadIdx.x] = y;
+            most_j[threadIdx.x] = all;
+            sum_j[threadIdx.x] = seen && s == 0.f ? (all == -INFINITY ? 1.f : 0.f) : s;
             __syncthreads();
             if (busy && slice == 0)
-                for (int i = 1; i < slices; ++i) {
-                    const float4 x = joined[i * items + e];
-                    y = make_float4(y.x + x.x, y.y + x.y, y.z + x.z, y.w + x.w);
-                }
+                for (int i = 1; i < slices; ++i) more(most_j[i * items + e], sum_j[i * items + e], joined[i * items + e]);
         }
         if (busy && slice == 0 && quad4 * 4 < cs.d) {
-            const float f = inv_of[row];
+            // no visible key: 0; otherwise a sum of 0 (all scores are -inf) or NaN gives NaN
+            const float f = seen ? (s == 0.f ? NAN : 1.f / s) : 0.f;
             *reinterpret_cast<uint2 *>(a.out + ((int64_t)b * a.heads + hk * a.group + g0 + row) * cs.d + quad4 * 4) =
                 make_uint2(pair_bf16(y.x * f, y.y * f), pair_bf16(y.z * f, y.w * f));
         }

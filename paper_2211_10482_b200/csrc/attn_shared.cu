@@ -6,9 +6,11 @@
 // each sequence's own keys, whose pieces are joined with the parts.  A row of the prefix is so read once for 256 queries, not once for
 // every sequence.
 //
-// The prefix lies in pages of any size, so its rows are gathered by cp.async into the swizzled tiles that the tensor cores read; one or two warps for each stage,
-// which copy, see the copies done, make them visible to the tensor cores' proxy and hand the tile over.  Keys without a place and the places behind the
-// last key are zeros, and a bit of a mask each.
+// Pages whose length divides a tile of 128 keys, or is a multiple of it, come by TMA, a box to a page: one warp looks the pages up and asks for them.  A page
+// that is not there is a box outside the tensor and so zeros; values behind the last key are cleared.  Pages of other lengths are gathered by cp.async
+// into the swizzled tiles that the tensor cores read, by one or two warps for each stage, which copy, see the copies done, make them visible to the tensor
+// cores' proxy and hand the tile over.  (With pages of 64 and all rows gathered by cp.async 84 us for 128 sequences behind two prefixes of 16384 and less.)
+// Either way a bit of a mask says which keys have a place.
 //
 // Which part of which prefix a block takes is decided on the device, where the lengths are: key tiles of a part are as many as give no more parts than there
 // are blocks in one turn on the SMs.
@@ -30,62 +32,96 @@ struct SharedArgs {
 namespace shared {
 // TILES of 128 rows; with one there is room for a third stage of keys and values, whose bytes bound few rows, and for a second warp to copy each: twelve warps
 // have 168 registers a thread, which a row of scores needs
-template <int DP, int TILES> struct Shape {
+template <int DP, int TILES, bool BOXES> struct Shape {
     static constexpr int STAGES = TILES == 1 ? 3 : 2;
     static constexpr int TILE_BYTES = DP / 64 * SLAB;
-    static constexpr int SOFTMAX = 4 * TILES, ISSUE = SOFTMAX, COPY = ISSUE + TILES, COPIERS = 2 / TILES, WARPS = COPY + COPIERS * STAGES, THREADS = WARPS * 32;
+    static constexpr int SOFTMAX = 4 * TILES, ISSUE = SOFTMAX, COPY = ISSUE + TILES, COPIERS = BOXES ? 1 : 2 / TILES, WARPS = COPY + (BOXES ? 1 : COPIERS * STAGES), THREADS = WARPS * 32;
     static constexpr int TMEM = TILES == 1 ? 256 : 512;            // columns: S of every tile, O of every tile
     static constexpr size_t SMEM = 1024 + (size_t)TILE_BYTES * (TILES + 2 * STAGES) + 512;
 };
 constexpr int MOST_ROWS = 256;
 }  // namespace shared
 
+// A cache's pages as a tensor map {column, head, token, page}, boxes of 64 columns of one head's `rows` tokens of one page.
+static bool make_tmap_pages(CUtensorMap *m, const unsigned char *p, const Cells &c, uint32_t rows)
+{
+    const tc::EncodeTiledFn fn = tc::encode_tiled_fn();
+    if (!fn) return false;
+    // the stride of an extent of one is never used: whatever was passed, it is a legal one
+    auto stride = [](int64_t s) { return (cuuint64_t)(s ? s : 256); };
+    cuuint64_t dims[4] = {(cuuint64_t)c.d, (cuuint64_t)c.kv_heads, (cuuint64_t)c.page, (cuuint64_t)c.pages};
+    cuuint64_t strides[3] = {stride(c.head_stride), stride(c.token_stride), stride(c.page_stride)};
+    cuuint32_t box[4] = {64, 1, rows, 1}, estr[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<unsigned char *>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+__device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *m, uint64_t *bar, int x, int y, int z, int w)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(tc::smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(tc::smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+        : "memory");
+}
+
+__device__ __forceinline__ void prefetch_4d(const CUtensorMap *m, int x, int y, int z, int w)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
 __device__ __forceinline__ void copy_row(uint32_t dst, const void *src, bool there)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// Key tiles of a group's prefix, and tiles of its rows.
+// Key tiles of a group's prefix, tiles of its rows, and what a key tile costs with one of these: 2.7 us where the 256 rows are two products, else 1.7.
 struct GroupOf {
     Rows seqs;
-    int tiles, keys;
+    int tiles, keys, cost;
+    __device__ __forceinline__ int parts(int work) const { return (keys * cost + work - 1) / work; }
 };
 __device__ __forceinline__ GroupOf group_of(const SharedArgs &a, int i)
 {
+    if (i >= a.groups) return {{0, 0}, 0, 0, 2};
     const Rows r = rows_of(a.group_offsets, i, a.step.c.nseq);
     const int len = length_of(a.prefix_lens[i], a.prefix_cols, a.step.c.page);
-    return {r, (r.len + a.seqs - 1) / a.seqs, (len + TILE - 1) / TILE};
+    return {r, (r.len + a.seqs - 1) / a.seqs, (len + TILE - 1) / TILE, (int64_t)r.len * a.step.group > TILE ? 3 : 2};
 }
 
 // Part `part` of `parts` of a tile of rows; none: group -1.
 struct PartOf {
     int group, tile, part, parts;
 };
-// By a whole warp: the fewest key tiles to a part that need no more parts than there are blocks, and no more of one prefix than there is room for; then what
+// By a whole warp: the least work in a part that needs no more parts than there are blocks, and no more of one prefix than there is room for; then what
 // block `index` of one key head does.
 __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv_heads, int lane)
 {
-    int most = 0;
+    const GroupOf mine = group_of(a, lane);                // all there is, up to 32 groups
+    auto nth = [&](int i) { return i == lane ? mine : group_of(a, i); };
+    int most = 0, least = 1;
     int64_t work = 0;
     for (int i = lane; i < a.groups; i += 32) {
-        const GroupOf g = group_of(a, i);
-        if (g.tiles) most = max(most, g.keys);
-        work += (int64_t)g.tiles * g.keys;
+        const GroupOf g = nth(i);
+        if (g.tiles) {
+            most = max(most, g.keys * g.cost);
+            least = max(least, (g.keys + a.most_parts - 1) / a.most_parts * g.cost);
+        }
+        work += (int64_t)g.tiles * g.keys * g.cost;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         most = max(most, __shfl_xor_sync(~0u, most, o));
+        least = max(least, __shfl_xor_sync(~0u, least, o));
         work += __shfl_xor_sync(~0u, work, o);
     }
     if (most == 0) return {-1, 0, 0, 0};
     const int room = max(a.slots / kv_heads, 1);
-    int lo = max((most + a.most_parts - 1) / a.most_parts, (int)min((work + room - 1) / room, (int64_t)most)), hi = most;
+    int lo = max(least, (int)min((work + room - 1) / room, (int64_t)most)), hi = most;
     while (lo < hi) {
         const int mid = (lo + hi) / 2;
         int64_t parts = 0;
         for (int i = lane; i < a.groups; i += 32) {
-            const GroupOf g = group_of(a, i);
-            parts += (int64_t)g.tiles * ((g.keys + mid - 1) / mid);
+            const GroupOf g = nth(i);
+            parts += (int64_t)g.tiles * g.parts(mid);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) parts += __shfl_xor_sync(~0u, parts, o);
@@ -93,13 +129,9 @@ __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv
         else lo = mid + 1;
     }
     for (int i0 = 0; i0 < a.groups; i0 += 32) {
-        int mine = 0, parts = 0;
-        if (i0 + lane < a.groups) {
-            const GroupOf g = group_of(a, i0 + lane);
-            parts = (g.keys + lo - 1) / lo;
-            mine = g.tiles * parts;
-        }
-        int sum = mine;
+        const GroupOf g = nth(i0 + lane);
+        const int parts = g.parts(lo), here = g.tiles * parts;
+        int sum = here;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int x = __shfl_up_sync(~0u, sum, o);
@@ -107,7 +139,7 @@ __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv
         }
         const unsigned behind = __ballot_sync(~0u, index < sum);
         if (behind) {
-            const int l = __ffs(behind) - 1, rest = index - __shfl_sync(~0u, sum - mine, l), n = __shfl_sync(~0u, parts, l);
+            const int l = __ffs(behind) - 1, rest = index - __shfl_sync(~0u, sum - here, l), n = __shfl_sync(~0u, parts, l);
             return {i0 + l, rest / n, rest % n, n};
         }
         index -= __shfl_sync(~0u, sum, 31);
@@ -115,11 +147,12 @@ __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv
     return {-1, 0, 0, 0};
 }
 
-template <int DP, int TILES>
-__global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_prefix_kernel(const SharedArgs a)
+template <int DP, int TILES, bool BOXES>
+__global__ void __launch_bounds__((shared::Shape<DP, TILES, BOXES>::THREADS), 1)
+shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const SharedArgs a)
 {
     using namespace tc;
-    using S = shared::Shape<DP, TILES>;
+    using S = shared::Shape<DP, TILES, BOXES>;
     constexpr int STAGES = S::STAGES, SLOTS = 2 * STAGES, PIECES = DP / 8, COPIERS = S::COPIERS;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = align_smem(raw);
@@ -129,13 +162,14 @@ __global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_p
     uint32_t *valid = (uint32_t *)(V + STAGES * S::TILE_BYTES);        // [SLOTS][4]
     uint64_t *bars = (uint64_t *)(valid + SLOTS * 4);
     uint64_t *k_full = bars, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES, *q_full = v_empty + STAGES,
-             *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES;
-    uint32_t *tmem_slot = (uint32_t *)(valid_full + SLOTS);
+             *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES, *copied = valid_full + SLOTS;
+    uint32_t *tmem_slot = (uint32_t *)(copied + 1);
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
     const Cells &cs = a.step.c;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int group = a.step.group, kv_heads = cs.kv_heads, hk = blockIdx.x % kv_heads;
 
+    if (BOXES && warp == S::COPY && lane < 2) prefetch_tmap(lane ? &vmap : &kmap);
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0) {
@@ -160,6 +194,7 @@ __global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_p
             mbar_init(&v_empty[s], active);
         }
         for (int s = 0; s < SLOTS; ++s) mbar_init(&valid_full[s], COPIERS);
+        mbar_init(copied, 1);
         for (int w = 0; w < TILES; ++w) {
             mbar_init(&q_full[w], 4);
             mbar_init(&s_full[w], 1);
@@ -181,7 +216,80 @@ __global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_p
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
 
-    if (warp >= S::COPY) {
+    if (BOXES && warp == S::COPY) {
+        // a lane to a box: `box` keys of one page; a page that is not there is one behind the last
+        const int *table = a.prefix_table + (int64_t)at.group * a.prefix_cols;
+        const int box = min(cs.page, TILE), boxes = TILE / box;
+        bool ok = true, bad = false;
+        int next_page = 0, next_slot = 0;
+        auto look = [&](int i) {
+            const int key = (first + i) * TILE + lane * box;
+            next_page = cs.pages;
+            next_slot = 0;
+            if (i >= n || lane >= boxes || key >= len) return;
+            const Place p = place_of(key, cs.page, cs.page_magic);
+            const int page = table[p.col];
+            next_slot = p.slot;
+            if ((unsigned)page < (unsigned)cs.pages) next_page = page;
+            else bad = true;
+        };
+        // places are looked up two tiles ahead, and their rows asked for as far as L2
+        look(0);
+        int soon_page = next_page, soon_slot = next_slot;
+        look(1);
+        for (int i = 0; i < n && ok; ++i) {
+            const int page = soon_page, in_page = soon_slot;
+            soon_page = next_page;
+            soon_slot = next_slot;
+            look(i + 2);
+            if (lane < boxes && soon_page < cs.pages)
+#pragma unroll
+                for (int c = 0; c < DP / 64; ++c) {
+                    prefetch_4d(&kmap, c * 64, hk, soon_slot, soon_page);
+                    prefetch_4d(&vmap, c * 64, hk, soon_slot, soon_page);
+                }
+            const int s = i % STAGES, use = i / STAGES, slot = (use & 1) * STAGES + s;
+            const uint32_t parity = (uint32_t)((use + 1) & 1);
+            // bits of this lane's word: 32 keys, which may be several boxes or a part of one
+            unsigned word = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const bool there = __shfl_sync(~0u, page, (w * 32 + lane) / box) < cs.pages && (first + i) * TILE + w * 32 + lane < len;
+                const unsigned bits = __ballot_sync(~0u, there);
+                if (lane == w) word = bits;
+            }
+            const int left = len - (first + i) * TILE;     // keys from here on
+            const bool edge = left < TILE;
+            ok = warp_wait(&k_empty[s], parity, abort_flag, a.step.status, 1);
+            if (!ok) break;
+            if (lane < 4) valid[slot * 4 + lane] = word;
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&valid_full[slot]);
+                mbar_expect_tx(&k_full[s], S::TILE_BYTES);
+            }
+            __syncwarp();
+            auto ask = [&](unsigned char *tile, const CUtensorMap *map, uint64_t *bar) {
+                if (lane < boxes)
+#pragma unroll
+                    for (int c = 0; c < DP / 64; ++c) tma_load_4d(tile + c * SLAB + lane * box * 128, map, bar, c * 64, hk, in_page, page);
+            };
+            ask(K + s * S::TILE_BYTES, &kmap, &k_full[s]);
+            ok = warp_wait(&v_empty[s], parity, abort_flag, a.step.status, 2);
+            if (!ok) break;
+            uint64_t *bar = edge ? copied : &v_full[s];
+            if (lane == 0) mbar_expect_tx(bar, S::TILE_BYTES);
+            __syncwarp();
+            ask(V + s * S::TILE_BYTES, &vmap, bar);
+            if (edge) {                                    // the last tile: what lies behind the last key may be anything
+                ok = warp_wait(copied, 0, abort_flag, a.step.status, 11);
+                if (!ok) break;
+                clear_rows<DP>(V + s * S::TILE_BYTES, left, TILE, lane);
+                if (lane == 0) mbar_arrive(&v_full[s]);
+            }
+        }
+        if (__any_sync(~0u, bad) && lane == 0) atomicExch(a.step.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
+    } else if (!BOXES && warp >= S::COPY) {
         // each copies 128 / COPIERS keys of a stage; 16 (8) lanes to a row
         constexpr int KEYS = TILE / COPIERS, WORDS = KEYS / 32;
         const int s = (warp - S::COPY) / COPIERS, half = (warp - S::COPY) % COPIERS;
@@ -249,7 +357,7 @@ __global__ void __launch_bounds__(shared::Shape<DP, TILES>::THREADS, 1) shared_p
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (__any_sync(~0u, bad) && lane == 0) atomicExch(a.step.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
-    } else if (warp >= S::ISSUE) {
+    } else if (warp >= S::ISSUE && warp < S::COPY) {
         // A tile of rows has a warp that issues its products: the scores of a tile of keys follow the product with the values of the one before, whose weights
         // they overwrite (products are carried out in the order of their issue).
         const int w = warp - S::ISSUE;
@@ -442,12 +550,25 @@ size_t attn_shared_workspace(int64_t nseq, int64_t heads, int64_t kv_heads, int6
     return shared_plan(nseq, heads, kv_heads, groups, &p) ? p.bytes : 0;
 }
 
+template <int DP, int TILES, bool BOXES>
+static st_status launch_prefix(const SharedArgs &a, const CUtensorMap &km, const CUtensorMap &vm, cudaStream_t stream)
+{
+    using S = shared::Shape<DP, TILES, BOXES>;
+    if (!ensure_dynamic_smem(shared_prefix_kernel<DP, TILES, BOXES>, S::SMEM)) return ST_ERR_CUDA;
+    return launch(shared_prefix_kernel<DP, TILES, BOXES>, dim3((unsigned)a.slots), S::THREADS, S::SMEM, stream, km, vm, a);
+}
+
+// Pages that a tile is a whole number of, or that are a whole number of tiles, come as boxes: of 8 rows and more, as the swizzle of a tile repeats every 8.
 template <int DP, int TILES>
 static st_status run_prefix(const SharedArgs &a, cudaStream_t stream)
 {
-    using S = shared::Shape<DP, TILES>;
-    if (!ensure_dynamic_smem(shared_prefix_kernel<DP, TILES>, S::SMEM)) return ST_ERR_CUDA;
-    return launch(shared_prefix_kernel<DP, TILES>, dim3((unsigned)a.slots), S::THREADS, S::SMEM, stream, a);
+    const Cells &c = a.step.c;
+    CUtensorMap km = {}, vm = {};
+    const bool boxes = c.page >= 8 && (TILE % c.page == 0 || c.page % TILE == 0);
+    if (!boxes) return launch_prefix<DP, TILES, false>(a, km, vm, stream);
+    const uint32_t rows = c.page < TILE ? c.page : TILE;
+    if (!make_tmap_pages(&km, c.k, c, rows) || !make_tmap_pages(&vm, c.v, c, rows)) return ST_ERR_CUDA;
+    return launch_prefix<DP, TILES, true>(a, km, vm, stream);
 }
 
 }  // namespace attn
