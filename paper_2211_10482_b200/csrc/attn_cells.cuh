@@ -79,9 +79,6 @@ inline bool meets_cells(const st_cells *c, const void *pages, const void *scales
     return arrays_meet(pages, n, p, bytes) || (scales && arrays_meet(scales, m, p, bytes));
 }
 
-// Clears the status of a workspace ahead of a kernel whose blocks may report: within one kernel no block is known to run before another.
-st_status clear_status(unsigned *status, cudaStream_t stream);
-
 #if defined(__CUDACC__)
 
 // Tokens of a sequence, as far as its row of a table goes.
