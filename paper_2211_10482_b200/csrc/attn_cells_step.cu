@@ -662,26 +662,26 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
     if (a.part_count) pdl_wait();                          // whoever waits for this kernel waits for the prefix's too
 }
 
-// Units that several warps had pieces of, and all of them where prefixes have parts; what has no visible key is 0.  A block to a unit, four columns of a head to
-// a thread, and several threads for the same columns where there are pieces enough: each goes through its pieces and parts once, with the largest score and
+// Units that several warps had pieces of, and all of them where prefixes have parts; what has no visible key is 0.  A block to a unit, or to a quarter of its
+// columns where units are few, four columns of a head to a thread, and several threads for the same columns where there are pieces enough: each goes through its pieces and parts once, with the largest score and
 // the sum of those so far, a few on their way at a time.
 namespace cstep {
 constexpr int JOIN = 512, BATCH = 4;       // threads at most; pieces on their way
 }
 template <int DP>
-__global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStepArgs a, int unit_heads, int keys_of_tile)
+__global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStepArgs a, int unit_heads, int keys_of_tile, int quarters)
 {
     using namespace cstep;
     __shared__ float4 joined[JOIN];
     __shared__ float most_j[JOIN], sum_j[JOIN];
     const Cells &cs = a.c;
-    const int chunks = (a.group + unit_heads - 1) / unit_heads, unit = blockIdx.x, b = blockIdx.y;
+    const int chunks = (a.group + unit_heads - 1) / unit_heads, unit = blockIdx.x / quarters, b = blockIdx.y;
     const int hk = unit / chunks, g0 = unit % chunks * unit_heads, g = min(a.group - g0, unit_heads);
     const float c = a.scale * 1.4426950408889634f;
     pdl_wait();
     pdl_trigger();
     const int64_t total = a.starts[cs.nseq], start = a.starts[b];
-    const int prefix = a.part_count ? min(a.part_count[b], MAX_PARTS) : 0, tiles = (Visible(a, cs.lens[b]).keys + keys_of_tile - 1) / keys_of_tile;
+    const int prefix = a.part_count ? min(a.part_count[b], a.own_part) : 0, tiles = (Visible(a, cs.lens[b]).keys + keys_of_tile - 1) / keys_of_tile;
     int t0 = 0, pieces = 0;                                // the teams whose pieces its first tile and its last are in
     if (tiles) {
         const int teams = workers_of(total, a.slots / a.team);
@@ -696,9 +696,9 @@ __global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStep
     auto slot_of = [&](int i) { return ((int64_t)((t0 + i) * a.team + unit % a.team) * 2 + (i == 0 ? 1 : 0)) * unit_heads; };
     auto part_of = [&](int i) { return (int64_t)(i < prefix ? i : a.own_part) * (a.heads / a.group) + hk; };
     // heads next to one another, as they lie in the parts
-    const int items = g * (DP / 4), slices = max(1, threads / items), slice = slices > 1 ? threadIdx.x / items : 0;
+    const int quads = DP / 4 / quarters, quad0 = blockIdx.x % quarters * quads, items = g * quads, slices = max(1, threads / items), slice = slices > 1 ? threadIdx.x / items : 0;
     for (int e0 = 0; e0 < items; e0 += threads) {
-        const int e = slices > 1 ? threadIdx.x % items : e0 + threadIdx.x, row = e % g, quad4 = e / g;
+        const int e = slices > 1 ? threadIdx.x % items : e0 + threadIdx.x, row = e % g, quad4 = quad0 + e / g;
         const bool busy = slice < slices && e < items;
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
         float all = -INFINITY, s = 0.f;
@@ -851,8 +851,9 @@ static st_status run_heads(CellsStepArgs a, cudaStream_t stream)
     const st_status rc = launch(cells_step_kernel<DTYPE, DP, HN, WIDE>, dim3((unsigned)blocks), cstep::WARPS * 32, S::SMEM, stream, a);
     if (rc != ST_OK) return rc;
     // few units may have many pieces each
-    const int threads = (int64_t)a.units * a.c.nseq >= 2 * sm_count_or_default() ? 128 : 512;
-    return launch(cells_join_kernel<DP>, dim3((unsigned)a.units, (unsigned)a.c.nseq), threads, 0, stream, a, S::HEADS, S::KEYS);
+    const bool few = (int64_t)a.units * a.c.nseq < 2 * sm_count_or_default();
+    const int quarters = few ? 4 : 1;
+    return launch(cells_join_kernel<DP>, dim3((unsigned)(a.units * quarters), (unsigned)a.c.nseq), few ? 512 : 128, 0, stream, a, S::HEADS, S::KEYS, quarters);
 }
 
 template <int DTYPE, int DP, bool WIDE>
