@@ -63,11 +63,6 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *m, uin
         : "memory");
 }
 
-__device__ __forceinline__ void prefetch_4d(const CUtensorMap *m, int x, int y, int z, int w)
-{
-    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-
 __device__ __forceinline__ void copy_row(uint32_t dst, const void *src, bool there)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -91,45 +86,48 @@ __device__ __forceinline__ GroupOf group_of(const SharedArgs &a, int i)
 struct PartOf {
     int group, tile, part, parts;
 };
-// By a whole warp: the least work in a part that needs no more parts than there are blocks, and no more of one prefix than there is room for; then what
-// block `index` of one key head does.
+// By a whole warp: the least work in a part that needs no more parts than there are blocks, and no more of one prefix than there is room for, 32 candidates at
+// a time (one after the other took 3 to 5 us); then what block `index` of one key head does.
 __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv_heads, int lane)
 {
     const GroupOf mine = group_of(a, lane);                // all there is, up to 32 groups
-    auto nth = [&](int i) { return i == lane ? mine : group_of(a, i); };
+    const int chunks = (a.groups + 31) / 32;
+    auto chunk = [&](int i) { return i == 0 ? mine : group_of(a, i * 32 + lane); };
     int most = 0, least = 1;
-    int64_t work = 0;
-    for (int i = lane; i < a.groups; i += 32) {
-        const GroupOf g = nth(i);
+    for (int i = 0; i < chunks; ++i) {
+        const GroupOf g = chunk(i);
         if (g.tiles) {
             most = max(most, g.keys * g.cost);
             least = max(least, (g.keys + a.most_parts - 1) / a.most_parts * g.cost);
         }
-        work += (int64_t)g.tiles * g.keys * g.cost;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         most = max(most, __shfl_xor_sync(~0u, most, o));
         least = max(least, __shfl_xor_sync(~0u, least, o));
-        work += __shfl_xor_sync(~0u, work, o);
     }
     if (most == 0) return {-1, 0, 0, 0};
     const int room = max(a.slots / kv_heads, 1);
-    int lo = max(least, (int)min((work + room - 1) / room, (int64_t)most)), hi = most;
+    int lo = min(least, most), hi = most;                  // at `most` every tile of rows is one part, for which there is room
     while (lo < hi) {
-        const int mid = (lo + hi) / 2;
+        const int step = (hi - lo + 31) / 32, mid = min(lo + lane * step, hi);
         int64_t parts = 0;
-        for (int i = lane; i < a.groups; i += 32) {
-            const GroupOf g = nth(i);
-            parts += (int64_t)g.tiles * g.parts(mid);
+        for (int i = 0; i < chunks; ++i) {
+            const GroupOf g = chunk(i);
+            const int work = g.keys * g.cost, n = min(32, a.groups - i * 32);
+            for (int l = 0; l < n; ++l) parts += (int64_t)__shfl_sync(~0u, g.tiles, l) * ((__shfl_sync(~0u, work, l) + mid - 1) / mid);
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) parts += __shfl_xor_sync(~0u, parts, o);
-        if (parts <= room) hi = mid;
-        else lo = mid + 1;
+        const unsigned fits = __ballot_sync(~0u, parts <= room || mid == hi);
+        if (!fits) {                                       // the last candidate is short of hi
+            lo = lo + 31 * step + 1;
+        } else {
+            const int l = __ffs(fits) - 1;
+            hi = min(lo + l * step, hi);
+            if (l > 0) lo = lo + (l - 1) * step + 1;
+        }
     }
-    for (int i0 = 0; i0 < a.groups; i0 += 32) {
-        const GroupOf g = nth(i0 + lane);
+    for (int i = 0; i < chunks; ++i) {
+        const GroupOf g = chunk(i);
         const int parts = g.parts(lo), here = g.tiles * parts;
         int sum = here;
 #pragma unroll
@@ -140,7 +138,7 @@ __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv
         const unsigned behind = __ballot_sync(~0u, index < sum);
         if (behind) {
             const int l = __ffs(behind) - 1, rest = index - __shfl_sync(~0u, sum - here, l), n = __shfl_sync(~0u, parts, l);
-            return {i0 + l, rest / n, rest % n, n};
+            return {i * 32 + l, rest / n, rest % n, n};
         }
         index -= __shfl_sync(~0u, sum, 31);
     }
@@ -164,7 +162,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     uint64_t *k_full = bars, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES, *q_full = v_empty + STAGES,
              *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES, *copied = valid_full + SLOTS;
     uint32_t *tmem_slot = (uint32_t *)(copied + 1);
-    volatile int *abort_flag = (volatile int *)(tmem_slot + 1);
+    volatile int *abort_flag = (volatile int *)(tmem_slot + 1), *met = abort_flag + 1;         // met: a page outside the cache
     const Cells &cs = a.step.c;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int group = a.step.group, kv_heads = cs.kv_heads, hk = blockIdx.x % kv_heads;
@@ -186,6 +184,17 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     const int first = (int)((int64_t)mine.keys * at.part / at.parts), n = (int)((int64_t)mine.keys * (at.part + 1) / at.parts) - first;      // key tiles
     const int active = TILES == 2 && rows > TILE ? 2 : 1;  // tiles of rows that there are
 
+    // The queries' rows, 16 (8) lanes to a row, on their way while the rest is set up; what is no row is zeros.
+    constexpr int LOADS = PIECES;                          // of a lane: 32 rows of PIECES pieces to a warp
+    uint4 queries[LOADS];
+    if (warp < S::SOFTMAX && warp / 4 < active)
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int piece = lane % PIECES, id = warp * 32 + lane / PIECES + j * (32 / PIECES), b = id / group;
+            const bf16 *from = a.step.q + (b0 + b) * a.step.q_row + (hk * group + id - b * group) * a.step.q_head + piece * 8;
+            queries[j] = id < rows && piece * 8 < cs.d ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0u, 0u, 0u, 0u);
+        }
+
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&k_full[s], COPIERS);
@@ -203,6 +212,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             mbar_init(&o_full[w], 1);
         }
         *abort_flag = 0;
+        *met = 0;
         fence_barrier_init();
     }
     if (warp == S::ISSUE) {
@@ -220,7 +230,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         // a lane to a box: `box` keys of one page; a page that is not there is one behind the last
         const int *table = a.prefix_table + (int64_t)at.group * a.prefix_cols;
         const int box = min(cs.page, TILE), boxes = TILE / box;
-        bool ok = true, bad = false;
+        bool ok = true;
         int next_page = 0, next_slot = 0;
         auto look = [&](int i) {
             const int key = (first + i) * TILE + lane * box;
@@ -231,23 +241,11 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             const int page = table[p.col];
             next_slot = p.slot;
             if ((unsigned)page < (unsigned)cs.pages) next_page = page;
-            else bad = true;
+            else *met = 1;
         };
-        // places are looked up two tiles ahead, and their rows asked for as far as L2
         look(0);
-        int soon_page = next_page, soon_slot = next_slot;
-        look(1);
         for (int i = 0; i < n && ok; ++i) {
-            const int page = soon_page, in_page = soon_slot;
-            soon_page = next_page;
-            soon_slot = next_slot;
-            look(i + 2);
-            if (lane < boxes && soon_page < cs.pages)
-#pragma unroll
-                for (int c = 0; c < DP / 64; ++c) {
-                    prefetch_4d(&kmap, c * 64, hk, soon_slot, soon_page);
-                    prefetch_4d(&vmap, c * 64, hk, soon_slot, soon_page);
-                }
+            const int page = next_page, in_page = next_slot;
             const int s = i % STAGES, use = i / STAGES, slot = (use & 1) * STAGES + s;
             const uint32_t parity = (uint32_t)((use + 1) & 1);
             // bits of this lane's word: 32 keys, which may be several boxes or a part of one
@@ -275,6 +273,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                     for (int c = 0; c < DP / 64; ++c) tma_load_4d(tile + c * SLAB + lane * box * 128, map, bar, c * 64, hk, in_page, page);
             };
             ask(K + s * S::TILE_BYTES, &kmap, &k_full[s]);
+            look(i + 1);
             ok = warp_wait(&v_empty[s], parity, abort_flag, a.step.status, 2);
             if (!ok) break;
             uint64_t *bar = edge ? copied : &v_full[s];
@@ -288,7 +287,6 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                 if (lane == 0) mbar_arrive(&v_full[s]);
             }
         }
-        if (__any_sync(~0u, bad) && lane == 0) atomicExch(a.step.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
     } else if (!BOXES && warp >= S::COPY) {
         // each copies 128 / COPIERS keys of a stage; 16 (8) lanes to a row
         constexpr int KEYS = TILE / COPIERS, WORDS = KEYS / 32;
@@ -299,7 +297,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         constexpr int ROWS = 32 / PIECES;                  // rows that a warp copies at a time
         const bool inside = piece * 8 < cs.d;
         const uint32_t to = (uint32_t)(piece / 8 * SLAB + half * KEYS * 128);
-        bool ok = true, bad = false;
+        bool ok = true;
         int64_t next[WORDS];                               // places of this lane's keys of the tile after
         auto place = [&](int i) {
 #pragma unroll
@@ -310,7 +308,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                 const Place p = place_of(key, cs.page, cs.page_magic);
                 const int page = table[p.col];
                 if ((unsigned)page < (unsigned)cs.pages) next[e] = page * cs.page_stride + p.slot * cs.token_stride;
-                else bad = true;
+                else *met = 1;
             }
         };
         place(s);
@@ -356,7 +354,6 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             if (lane == 0) mbar_arrive(&v_full[s]);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (__any_sync(~0u, bad) && lane == 0) atomicExch(a.step.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
     } else if (warp >= S::ISSUE && warp < S::COPY) {
         // A tile of rows has a warp that issues its products: the scores of a tile of keys follow the product with the values of the one before, whose weights
         // they overwrite (products are carried out in the order of their issue).
@@ -397,17 +394,13 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     } else if (warp / 4 < active) {
         const int w = warp >> 2, r = (warp & 3) * 32 + lane;                 // this thread's row of the tile
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + w * TILE, o_addr = tmem + lanes + TILES * TILE + w * DP;
-        // the queries' rows, 16 (8) lanes to a row; what is no row is zeros
         {
             unsigned char *to = Q + w * S::TILE_BYTES;
             const int piece = lane % PIECES;
-#pragma unroll 4
-            for (int i = lane / PIECES; i < 32; i += 32 / PIECES) {
-                const int row = (warp & 3) * 32 + i, id = w * TILE + row, b = id / group;
-                const bool in = id < rows && piece * 8 < cs.d;
-                const bf16 *from = a.step.q + (b0 + b) * a.step.q_row + (hk * group + id - b * group) * a.step.q_head + piece * 8;
-                *reinterpret_cast<uint4 *>(to + piece / 8 * SLAB + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) =
-                    in ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int row = (warp & 3) * 32 + lane / PIECES + j * (32 / PIECES);
+                *reinterpret_cast<uint4 *>(to + piece / 8 * SLAB + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = queries[j];
             }
             fence_proxy_async();
             __syncwarp();
@@ -418,11 +411,14 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         bool ok = true, seen = false;
         for (int i = 0; i < n; ++i) {
             ok = warp_wait(&s_full[w], (uint32_t)(i & 1), abort_flag, a.step.status, 8);
+            // the bits are looked at behind the last key, and once a page was met that is not there (which is said before its rows are asked for)
             const int slot = (i / STAGES & 1) * STAGES + i % STAGES;
-            if (ok) ok = warp_wait(&valid_full[slot], (uint32_t)(i / SLOTS & 1), abort_flag, a.step.status, 9);
+            const bool holes = (first + i + 1) * TILE > len || *met;
+            if (ok && holes) ok = warp_wait(&valid_full[slot], (uint32_t)(i / SLOTS & 1), abort_flag, a.step.status, 9);
             if (!ok) break;
             tc_fence_after();
-            const uint4 bits = *reinterpret_cast<const uint4 *>(valid + slot * 4);
+            uint4 bits = make_uint4(~0u, ~0u, ~0u, ~0u);
+            if (holes) bits = *reinterpret_cast<const uint4 *>(valid + slot * 4);
             const bool cut = (bits.x & bits.y & bits.z & bits.w) != ~0u;
             seen = seen || (bits.x | bits.y | bits.z | bits.w) != 0u;
             uint32_t x[4][32];
@@ -510,6 +506,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     }
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0 && *met) atomicExch(a.step.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
     if (warp == S::ISSUE) {
         tc_fence_after();
         tmem_dealloc(tmem, S::TMEM);
