@@ -410,7 +410,7 @@ st_status st_attn_decay_step(const st_tokens *tokens, const void *q, const void 
  *     r = 1 / sqrt(mean_i x[i]^2 + eps);   y[i] = x[i] r w[i]      (norm = 0: y = x)
  *     columns (a, b) of pair i:  y'[a] = factor (y[a] cos t - y[b] sin t),  y'[b] = factor (y[b] cos t + y[a] sin t),  t = position freq[i]
  * Pairs: (2i, 2i+1) where interleaved, else (i, i + rot/2); columns from rot on have no pair and no factor.  The angle is the exact product of
- * the position and the fp32 frequency, reduced in 64 bits: far positions lose nothing.  Sums, norms and rotations are fp32, a result is rounded once. */
+ * the position and the fp32 frequency (|freq| below 2^24), reduced in 64 bits: far positions lose nothing.  Sums, norms and rotations are fp32, a result is rounded once. */
 typedef struct {
     int32_t dtype;            /* of the tables: ST_BF16 */
     int32_t weight_dtype;     /* of q_weight and k_weight: ST_BF16 or ST_F32 */
@@ -425,7 +425,7 @@ typedef struct {
     float factor;             /* of what is rotated (1 but for scaled contexts), finite */
 } st_rotation;
 
-/* positions: int32 [n], any sign; freq: fp32 [rot/2]; q_weight, k_weight: [d] or NULL (ones).  q_out: bf16 [n, heads, d], k_out: [n, kv_heads, d],
+/* positions: int32 [n], any sign; freq: fp32 [rot/2], finite; q_weight, k_weight: [d] or NULL (ones).  q_out: bf16 [n, heads, d], k_out: [n, kv_heads, d],
  * contiguous; each may take the place of the whole of its own operand, where that is contiguous. */
 st_status st_attn_rotate(const st_rotation *rotation, const void *q, const void *k, const int32_t *positions, const float *freq,
                          const void *q_weight, const void *k_weight, void *q_out, void *k_out, void *stream);
@@ -445,7 +445,8 @@ st_status st_attn_rotate_grad(const st_rotation *rotation, const void *q, const 
  *   ST_I4    d cells c of 4 bits (column 2i in the low half of byte i) and, for each 32 columns, two bf16 numbers (step, lo): lo + step c.
  *            lo = min x, step = bf16((max x - lo) / 15), c = round((x - lo) (1 / step)), at most 15.
  * Each operation in fp32, rounded to nearest even.  A scale or step whose a or step is below 2^-100 is 0 (the row stands for 0, or the columns for
- * lo); one of a row (32 columns) with an infinity or NaN is NaN, and so is what the row (the columns) stands for. */
+ * lo); one of a row (32 columns) with an infinity or NaN, or whose
+ * step is beyond bf16, is NaN, and so is what the row (the columns) stands for. */
 typedef struct {
     int32_t dtype;            /* ST_BF16, ST_I8, ST_I4 */
     int32_t reserved;         /* must be 0 */
@@ -453,7 +454,7 @@ typedef struct {
     int64_t d;                /* a multiple of 8 (ST_I4: of 16) up to 128 */
     int64_t pages, page;      /* pages of the cache, tokens of a page */
     int64_t table_cols;       /* page numbers in a row of the table: page * table_cols up to 2^30 */
-    int64_t page_stride, token_stride, head_stride;      /* of k_pages and v_pages, in bytes: multiples of 16 (ST_I8, ST_I4: of 8) */
+    int64_t page_stride, token_stride, head_stride;      /* of k_pages and v_pages, in bytes: multiples of 16 (ST_I8, ST_I4: of 8), up to 2^38 */
     int64_t scale_page, scale_token, scale_head;         /* of k_scales and v_scales, in units of 4 bytes (a scale; step and lo) */
 } st_cells;
 

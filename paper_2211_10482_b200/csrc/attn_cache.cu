@@ -410,7 +410,9 @@ extern "C" st_status st_attn_cache_read(const st_cells *c, int64_t n, const void
     const int64_t bytes = n * c->kv_heads * c->d * 2;
     if (arrays_meet(k, bytes, v, bytes)) return ST_ERR_UNSUPPORTED;
     for (const void *p : {(const void *)k, (const void *)v})
-        if (meets_cells(c, k_pages, k_scales, p, bytes) || meets_cells(c, v_pages, v_scales, p, bytes)) return ST_ERR_UNSUPPORTED;
+        if (meets_cells(c, k_pages, k_scales, p, bytes) || meets_cells(c, v_pages, v_scales, p, bytes) || arrays_meet(p, bytes, table, c->nseq * c->table_cols * 4) ||
+            arrays_meet(p, bytes, lens, c->nseq * 4) || arrays_meet(p, bytes, offsets, (c->nseq + 1) * 4))
+            return ST_ERR_UNSUPPORTED;
     CacheArgs a = {};
     a.c = cells_of(c, k_pages, v_pages, k_scales, v_scales, table, lens);
     a.k_out = (bf16 *)k;

@@ -20,6 +20,13 @@ struct Cells {
 inline int64_t row_bytes(int dtype, int64_t d) { return dtype == ST_BF16 ? 2 * d : dtype == ST_I8 ? d : d / 2; }
 inline int64_t row_scales(int dtype, int64_t d) { return dtype == ST_BF16 ? 0 : dtype == ST_I8 ? 1 : (d + GROUP - 1) / GROUP; }
 
+// How far behind the first row the last one begins, each in the units of the strides.
+constexpr __int128 MOST_BYTES = (__int128)1 << 61;
+inline __int128 cells_extent(int64_t pages, int64_t page_stride, int64_t page, int64_t token_stride, int64_t heads, int64_t head_stride)
+{
+    return (__int128)(pages - 1) * page_stride + (__int128)(page - 1) * token_stride + (__int128)(heads - 1) * head_stride;
+}
+
 inline st_status check_cells(const st_cells *c, const void *k_pages, const void *v_pages, const void *k_scales, const void *v_scales, const void *table,
                              const void *lens)
 {
@@ -33,9 +40,11 @@ inline st_status check_cells(const st_cells *c, const void *k_pages, const void 
     const int64_t bytes = row_bytes(c->dtype, c->d), scales = row_scales(c->dtype, c->d), unit = c->dtype == ST_BF16 ? 16 : 8;
     if (!stride_ok(c->pages, c->page_stride, bytes) || !stride_ok(c->page, c->token_stride, bytes) || !stride_ok(c->kv_heads, c->head_stride, bytes)) return ST_ERR_SHAPE;
     if (scales && (!stride_ok(c->pages, c->scale_page, scales) || !stride_ok(c->page, c->scale_token, scales) || !stride_ok(c->kv_heads, c->scale_head, scales))) return ST_ERR_SHAPE;
-    // a page's place is a product of two numbers, one below 2^30
     for (const int64_t s : {c->page_stride, c->token_stride, c->head_stride, c->scale_page, c->scale_token, c->scale_head})
-        if (s > ((int64_t)1 << 31)) return ST_ERR_UNSUPPORTED;
+        if (s > ((int64_t)1 << 38)) return ST_ERR_UNSUPPORTED;         // half of what a tensor map's stride may be
+    if (cells_extent(c->pages, c->page_stride, c->page, c->token_stride, c->kv_heads, c->head_stride) > MOST_BYTES ||
+        (scales && 4 * cells_extent(c->pages, c->scale_page, c->page, c->scale_token, c->kv_heads, c->scale_head) > MOST_BYTES))
+        return ST_ERR_UNSUPPORTED;
     if ((c->pages > 1 && c->page_stride % unit != 0) || (c->page > 1 && c->token_stride % unit != 0) || (c->kv_heads > 1 && c->head_stride % unit != 0)) return ST_ERR_ALIGN;
     if (!k_pages || !v_pages || !table || !lens || (scales && (!k_scales || !v_scales))) return ST_ERR_NULL;
     if (!scales && (k_scales || v_scales)) return ST_ERR_SHAPE;

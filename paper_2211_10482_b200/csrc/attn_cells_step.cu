@@ -884,6 +884,8 @@ st_status check_step(const st_cells *c, const void *q, int64_t q_row, int64_t q_
     if (!stride_ok(c->nseq, q_row, c->d) || !stride_ok(c->heads, q_head, c->d)) return ST_ERR_SHAPE;
     if (q_row > ((int64_t)1 << 38) || q_head > ((int64_t)1 << 38) || !(scale > 0.f && scale < INFINITY)) return ST_ERR_UNSUPPORTED;
     if ((c->nseq > 1 && q_row % 8 != 0) || (c->heads > 1 && q_head % 8 != 0) || !aligned16(q) || !aligned16(out)) return ST_ERR_ALIGN;
+    // a place on the line of work times the number of warps stays below 2^63
+    if (c->nseq * c->heads * (c->page * c->table_cols / 16 + cstep::UNIT_COST + 1) > ((int64_t)1 << 50)) return ST_ERR_UNSUPPORTED;
     return ST_OK;
 }
 

@@ -36,6 +36,18 @@ ST_HD constexpr int min_blocks(bool odd, bool grad) { return odd || grad ? 2 : 3
 ST_HD constexpr int ahead(bool grad) { return grad ? 4 : 4; }                            // rows of a lane on their way
 }  // namespace rot
 
+// The fraction of freq / 2 pi, in units of 2^-64: the frequency's 24 bits times the first 128 bits of 1 / 2 pi, in whole numbers.  |freq| below 2^24.  (One
+// product in 64-bit floating point takes as long, within 0.4 us of a call, and keeps too few bits of the fraction where a frequency is many turns.)
+__device__ __forceinline__ uint64_t turns_of(float freq)
+{
+    const uint32_t bits = __float_as_uint(freq), exponent = bits >> 23 & 255;
+    const uint64_t m = (bits & 0x7FFFFF) | (exponent ? 0x800000 : 0);
+    const int shift = 150 - (int)max(exponent, 1u);        // m 2^-shift
+    const uint64_t low = m * 0x28be60db9391054aull, p = low + __umul64hi(m, 0x7f09d5f47d4d3770ull), q = __umul64hi(m, 0x28be60db9391054aull) + (p < low);
+    const uint64_t t = shift <= 0 ? p : shift < 64 ? p >> shift | q << (64 - shift) : shift < 128 ? q >> (shift - 64) : 0;
+    return bits >> 31 ? 0 - t : t;
+}
+
 // Sum over the lanes of a row, the same in all of them.
 template <int LANES>
 __device__ __forceinline__ float row_sum(float x)
@@ -220,10 +232,7 @@ __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GR
     }
     int stage = 0, next_position = begin < a.items ? a.positions[item_of(begin).t] : 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const double t = (double)freq[i] * 0.15915494309189533577;
-        turn[i] = (uint64_t)((t - floor(t)) * 18446744073709551616.0);
-    }
+    for (int i = 0; i < 2; ++i) turn[i] = turns_of(freq[i]);
     for (int i = begin; i < a.items; i += hop) {
         const Item it = item_of(i);
         // cosine and sine of every pair: y'[a] = c y[a] - s y[b], y'[b] = c y[b] + s y[a]

@@ -527,6 +527,7 @@ static bool shared_plan(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t g
     p->tiles_of = nseq * group <= TILE ? 1 : 2;
     p->seqs = (int)(p->tiles_of * TILE / group);
     const int64_t least = (nseq + p->seqs - 1) / p->seqs * kv_heads, most = most_tiles(nseq, groups, p->seqs) * kv_heads;
+    if (most > INT32_MAX) return false;
     p->slots = (int)(most > sms ? most : sms);
     // room for as many parts of one prefix as the SMs can take at a time, beside the other tiles of rows that there are at least
     const int64_t parts = (sms + least - 1) / least;

@@ -887,3 +887,157 @@ def test_wrong_tensors_are_refused():
         (lambda: shared(x, *plain.cells, plain.table[:1], plain.lens[:1], plain.table, plain.lens, ws=torch.empty(512, dtype=torch.uint8, device="cuda")), st.StError)):
         with pytest.raises(error):
             bad()
+
+
+# ------------------------------------------------------------------------- extents and layouts
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_caches_whose_heads_lie_apart(bits):
+    """Heads before pages, and tokens before pages: the other strides are the largest."""
+    lens, Hk, d, page = [40, 0, 133], 3, 64, 16
+    c = Cache(251, lens, Hk, d, page, bits)
+    q = normal(252, 3, 6, d)
+    k, v = normal(253, 6, Hk, d), normal(254, 6, Hk, d)
+    at = offsets([3, 0, 3])
+    plain = [c.copies() for _ in range(2)]
+    n = len(plain[0]) // 2
+    for order in ((2, 0, 1), (1, 0, 2), (0, 2, 1)):
+        def moved(x):
+            if x is None:
+                return None
+            rest = tuple(range(3, x.dim()))
+            y = torch.empty([x.shape[i] for i in order] + list(x.shape[3:]), dtype=x.dtype, device="cuda")
+            view = y.permute(*[order.index(i) for i in range(3)], *rest)
+            view.copy_(x)
+            return view
+        cells, scales = [moved(x) for x in c.cells], [moved(x) for x in c.scales]
+        if bits == 4 and scales[0].stride(-2) != 2:
+            continue
+        how = dict(k_scales=scales[0], v_scales=scales[1])
+        got = st.st_attn_cache_step(q, *cells, c.table, c.lens, 100, 3, **how)
+        want = st.st_attn_cache_step(q, *c.pages(), 100, 3, **c.how())
+        ok()
+        assert torch.equal(got, want)
+        for a, b in zip(st.st_attn_cache_read(*cells, c.table, c.lens, at, 6, **how), st.st_attn_cache_read(*c.pages(), at, 6, **c.how())):
+            assert same(a, b)
+        kept = Cache(251, lens, Hk, d, page, bits)
+        st.st_attn_cache_write(k, v, *kept.pages(), at, **kept.how())
+        st.st_attn_cache_write(k, v, *cells, c.table, c.lens, at, **how)
+        ok()
+        for a, b in zip((*cells, *scales), (*kept.cells, *kept.scales)):
+            assert a is None or same(a.contiguous(), b)
+        if bits == 16:
+            args = c.table[2:].contiguous(), c.lens[2:].contiguous(), c.table, c.lens
+            cells = [moved(x) for x in c.cells]
+            assert torch.equal(st.st_attn_shared_step(q, *cells, *args), st.st_attn_shared_step(q, *c.cells, *args))
+            ok()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("H,Hk,d", [(1, 1, 64), (16, 1, 128), (9, 3, 80)])
+def test_one_long_sequence_is_every_warps(H, Hk, d, bits):
+    n, page = 40003, 64
+    c = Cache(261, [n], Hk, d, page, bits)
+    q = normal(262, 1, H, d)
+    got = st.st_attn_cache_step(q, *c.pages(), 1 << 62, 0, **c.how())
+    ok()
+    check_step(got, c, q, 1 << 62, 0)
+
+
+@pytest.mark.parametrize("bits,H,Hk", [(16, 4, 4), (8, 4, 2), (4, 6, 6), (8, 10, 1)])
+def test_more_sequences_than_a_block_has_threads(bits, H, Hk):
+    lens = [(i * 7) % 45 if i % 11 else 0 for i in range(2100)] + [3000]
+    c = Cache(271, lens, Hk, 32, 16, bits, fill=False)
+    for i in range(2):                                   # one random fill of all pages instead of a sequence's each
+        x = normal(272 + i, *c.cells[i].shape[:3], 32)
+        if bits == 16:
+            c.cells[i] = x
+        else:
+            c.cells[i], c.scales[i] = ref.quantise(x, bits)
+    q = normal(274, len(lens), H, 32)
+    got = st.st_attn_cache_step(q, *c.pages(), 30, 2, **c.how())
+    ok()
+    some = [0, 1, 2, 10, 11, 12, 255, 256, 257, 1022, 1023, 1024, 1025, 2047, 2048, 2098, 2099, 2100]
+    for b in some:
+        n = lens[b]
+        lo = max(0, n - 30)
+        s = torch.cat([torch.arange(min(2, lo), device="cuda"), torch.arange(lo, n, device="cuda")])
+        at = (c.table[b].long()[s // 16], s % 16)
+        near(got[b], *ref.attend(q[b], c.parts(0, b, at), c.parts(1, b, at)), "out of sequence %d" % b)
+    # each alone gives the same up to the order of its sums, and what is empty is zeros
+    empty = torch.tensor([n == 0 for n in lens], device="cuda")
+    assert bool((got[empty] == 0).all()) and not bool(torch.isnan(got).any())
+
+
+def test_more_groups_than_a_warp_has_lanes():
+    groups = [(i * 5) % 4 for i in range(75)]
+    prefix = [(i * 37) % 300 if i % 6 else 0 for i in range(75)]
+    c, q, args, lens = shared_inputs(281, groups, prefix, [0, 3, 17], 4, 2, 64, 16)
+    got = st.st_attn_shared_step(q, *c.cells, *args)
+    ok()
+    check_shared(got, c, q, groups, prefix, lens)
+
+
+def test_a_batch_of_more_than_a_thousand_with_prefixes():
+    groups = [700, 0, 500]
+    prefix, own = [390, 5, 200], [2, 0, 33, 1]
+    c, q, args, lens = shared_inputs(291, groups, prefix, own, 16, 1, 64, 32)      # 16 heads to a key head
+    got = st.st_attn_shared_step(q, *c.cells, *args)
+    ok()
+    keep = [0, 1, 7, 8, 9, 15, 16, 17, 255, 256, 698, 699, 700, 701, 702, 703, 1023, 1024, 1198, 1199]
+    for n in keep:
+        g = 0 if n < 700 else 2
+        (k0, k1), (v0, v1) = (tuple(torch.cat(x) for x in zip(c.parts(i, g), c.parts(i, 3 + n))) for i in range(2))
+        near(got[n], *ref.attend(q[n], (k0, k1), (v0, v1)), "out of sequence %d" % n)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_sequences_may_share_pages(bits):
+    """The same row of the table for all, the same page more than once in a row."""
+    c = Cache(301, [64], 2, 64, 16, bits)
+    table = c.table[:, [0, 1, 0, 3, 3]].expand(5, 5).contiguous()
+    lens = ints(80, 80, 33, 16, 71)
+    q = normal(302, 1, 4, 64).expand(5, 4, 64).contiguous()
+    got = st.st_attn_cache_step(q, c.cells[0], c.cells[1], table, lens, 1 << 30, 0, **c.how())
+    ok()
+    for b, n in enumerate(lens.tolist()):
+        s = torch.arange(n, device="cuda")
+        at = (table[b].long()[s // 16], s % 16)
+        near(got[b], *ref.attend(q[b], c.parts(0, 0, at), c.parts(1, 0, at)), "out of sequence %d" % b)
+    if bits == 16:
+        got = st.st_attn_shared_step(q, *c.cells, table[:1].contiguous(), ints(80), table, lens)
+        ok()
+        for b, n in enumerate(lens.tolist()):
+            s = torch.cat([torch.arange(80, device="cuda"), torch.arange(n, device="cuda")])
+            at = (table[b].long()[s // 16], s % 16)
+            near(got[b], *ref.attend(q[b], c.parts(0, 0, at), c.parts(1, 0, at)), "out of sequence %d" % b)
+
+
+def test_the_ends_of_the_positions():
+    q = normal(311, 4, 2, 64)
+    positions = ints(2**31 - 1, -(2**31), 0, -1)
+    freq = st.st_rotary_frequencies(64).cuda()
+    freq[3], freq[4], freq[5] = 3.0e4, -0.75, 0.0
+    for inter in (False, True):
+        got, _ = st.st_attn_rotate(q, None, positions, freq, inter)
+        near(got, *ref.rotate(q, None, positions, freq, inter, None, 1.0), "rotated")
+
+
+def test_one_workspace_for_calls_one_after_the_other():
+    """A workspace holds nothing from one call for the next: not after a larger call, a failed one or another kind."""
+    big, small = Cache(321, [900, 44, 0, 7], 2, 64, 16, 16), Cache(322, [3, 50], 1, 128, 16, 8)
+    n = max(st.st_workspace_bytes(st.ST_OP_ATTN_CACHE_STEP, 4, 0), st.st_workspace_bytes(st.ST_OP_ATTN_SHARED_STEP, 4, 8, 2, 1))
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    q, r = normal(323, 4, 8, 64), normal(324, 2, 3, 128)
+    args = big.table[:1].contiguous(), big.lens[:1].contiguous(), big.table, big.lens
+    want = st.st_attn_cache_step(q, *big.pages(), 500, 1), st.st_attn_cache_step(r, *small.pages(), 40, **small.how()), st.st_attn_shared_step(q, *big.cells, *args)
+    for _ in range(2):
+        assert torch.equal(st.st_attn_cache_step(q, *big.pages(), 500, 1, ws=ws), want[0])
+        assert torch.equal(st.st_attn_shared_step(q, *big.cells, *args, ws=ws), want[2])
+        assert torch.equal(st.st_attn_cache_step(r, *small.pages(), 40, **small.how(), ws=ws), want[1])
+        ok()
+        bad = small.table.clone()
+        bad[1, 0] = 1 << 20
+        st.st_attn_cache_step(r, small.cells[0], small.cells[1], bad, small.lens, 100, **small.how(), ws=ws)
+        assert st.st_check_status(ws) == st.ST_ERR_DEV_BOUNDS
