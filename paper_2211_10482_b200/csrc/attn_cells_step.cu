@@ -58,21 +58,34 @@ __device__ __forceinline__ void load4x8x8_trans(uint32_t (&r)[4], uint32_t addr)
 }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_half(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same without a sum before it.
+__device__ __forceinline__ void mma_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_half_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 // An 8 x 8 matrix of bf16, two to a lane, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t x)
 {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 __device__ __forceinline__ float exp2_fast(float x)
@@ -115,8 +128,29 @@ __device__ __forceinline__ uint32_t bytes_half(uint32_t w, uint32_t which)
 }
 // Nibbles i and i + 4 of w.
 __device__ __forceinline__ uint32_t nibbles_bf16(uint32_t w, int i) { return minus_bf16((w >> (4 * i) & 0x000F000Fu) | 0x43004300u, 0x43004300u); }
+// The same in fp16, where 0x64 above 16 u is 1024 + 16 u: odd ones need no shift.
+__device__ __forceinline__ uint32_t nibbles_half(uint32_t w, int i)
+{
+    const uint32_t v = i >= 2 ? w >> 8 : w;
+    uint32_t r;
+    if (i & 1) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"((v & 0x00F000F0u) | 0x64006400u), "r"(0x2C002C00u), "r"(0xD400D400u));
+    else asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((v & 0x000F000Fu) | 0x64006400u), "r"(0xE400E400u));
+    return r;
+}
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// ST_I4's scales of a row
+__device__ __forceinline__ void scales_of(uint32_t (&s)[4], const uint32_t *from)
+{
+    const uint4 x = *reinterpret_cast<const uint4 *>(from);
+    s[0] = x.x, s[1] = x.y, s[2] = x.z, s[3] = x.w;
+}
+__device__ __forceinline__ void scales_of(uint32_t (&s)[2], const uint32_t *from)
+{
+    const uint2 x = *reinterpret_cast<const uint2 *>(from);
+    s[0] = x.x, s[1] = x.y;
+}
 
 // Weight of a part whose largest score is m, where the largest of all is `all`.
 __device__ __forceinline__ float weight_of(float m, float all, float c) { return m == -INFINITY ? 0.f : exp2f(c * (m - all)); }
@@ -330,12 +364,12 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             q[k][n][j] = DTYPE == ST_I4 ? (uint32_t)from[col] | (uint32_t)from[col + 4] << 16 : *reinterpret_cast<const uint32_t *>(from + col);
                     }
             }
-            // ST_I8: as fp16, times a power of two; unit[n][i] is what scores are in, for the two heads of this lane's scores
+            // ST_I8, ST_I4: as fp16, times a power of two; unit[n][i] is what scores are in, for the two heads of this lane's scores
             float unit_c[HN][2], unit_of[HN][2];
 #pragma unroll
             for (int n = 0; n < HN; ++n) {
                 float in = 1.f;
-                if (DTYPE == ST_I8) {
+                if (DTYPE != ST_BF16) {
                     unsigned top = 0;
 #pragma unroll
                     for (int k = 0; k < DP / 16; ++k)
@@ -356,25 +390,42 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    unit_of[n][i] = DTYPE == ST_I8 ? __shfl_sync(~0u, in, (2 * quad + i) * 4) : 1.f;
-                    unit_c[n][i] = DTYPE == ST_I8 ? c * unit_of[n][i] : c;
+                    unit_of[n][i] = DTYPE != ST_BF16 ? __shfl_sync(~0u, in, (2 * quad + i) * 4) : 1.f;
+                    unit_c[n][i] = DTYPE != ST_BF16 ? c * unit_of[n][i] : c;
                 }
             }
-            // ST_I4: sums of 32 columns of the queries, for the two heads of this lane's scores
-            float qsum[HN][2][GROUPS];
+            // ST_I4: sums of 32 columns of the queries, which meet a key's lowest numbers in a product of their own: rows 0 to 3 of it (32 columns each) are the
+            // sums' first 8 bits, 4 to 7 the next 8 and 8 to 11 the last 8.
+            uint32_t qsum[HN][2];
             if (DTYPE == ST_I4)
 #pragma unroll
-                for (int n = 0; n < HN; ++n)
+                for (int n = 0; n < HN; ++n) {
+                    float s[4], part[4];
 #pragma unroll
-                    for (int p = 0; p < GROUPS; ++p) {
-                        float s = 0.f;
+                    for (int p = 0; p < 4; ++p) {
+                        s[p] = 0.f;
+                        if (p < GROUPS)
 #pragma unroll
-                        for (int k = 2 * p; k < 2 * p + 2; ++k) s += low_bf16(q[k][n][0]) + high_bf16(q[k][n][0]) + low_bf16(q[k][n][1]) + high_bf16(q[k][n][1]);
-                        s += __shfl_xor_sync(~0u, s, 1);
-                        s += __shfl_xor_sync(~0u, s, 2);
+                            for (int k = 2 * p; k < 2 * p + 2; ++k)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) qsum[n][i][p] = __shfl_sync(~0u, s, (2 * quad + i) * 4);
+                                for (int j = 0; j < 2; ++j) {
+                                    const float2 two = __half22float2(*reinterpret_cast<const __half2 *>(&q[k][n][j]));
+                                    s[p] += two.x + two.y;
+                                }
+                        s[p] += __shfl_xor_sync(~0u, s[p], 1);
+                        s[p] += __shfl_xor_sync(~0u, s[p], 2);
                     }
+                    qsum[n][0] = qsum[n][1] = 0u;
+#pragma unroll
+                    for (int i = 0; i < 3; ++i) {
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
+                            part[p] = __bfloat162float(__float2bfloat16(s[p]));
+                            s[p] -= part[p];
+                        }
+                        if (quad / 2 == (i & 1)) qsum[n][i / 2] = quad & 1 ? pair_bf16(part[2], part[3]) : pair_bf16(part[0], part[1]);
+                    }
+                }
             // o: rows are columns of the values, columns heads 2 quad and 2 quad + 1
             float o[DP / 16][HN][4], most[HN][2], sum[HN][2];
             float low[HN][2][GROUPS];                      // ST_I4: what the values' lowest numbers bring to 32 columns
@@ -436,6 +487,16 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             x[h][n][3] *= s1;
                         }
                     } else {
+                        // scales of 32 columns each, of keys lane / 4 and 8 more
+                        uint32_t s0[GROUPS], s1[GROUPS];
+                        scales_of(s0, kscale + h * 16 * S::SCALES);
+                        scales_of(s1, kscale + (h * 16 + 8) * S::SCALES);
+                        const bool second = GROUPS == 4 && quad & 1;
+                        const uint32_t lo0 = __byte_perm(second ? s0[GROUPS - 2] : s0[0], second ? s0[GROUPS - 1] : s0[1], 0x7632);
+                        const uint32_t lo1 = __byte_perm(second ? s1[GROUPS - 2] : s1[0], second ? s1[GROUPS - 1] : s1[1], 0x7632);
+                        const uint32_t lows[4] = {lo0, lo1, lo0, lo1};
+#pragma unroll
+                        for (int n = 0; n < HN; ++n) mma_first(x[h][n], lows, qsum[n][0], qsum[n][1]);
 #pragma unroll
                         for (int k = 0; k < DP / 64; ++k) {
                             uint32_t f[4];                         // 16 keys, 64 columns
@@ -445,22 +506,20 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                                 const int p = 2 * k + m;
                                 float y[HN][4];
 #pragma unroll
-                                for (int n = 0; n < HN; ++n)
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) y[n][i] = 0.f;
-#pragma unroll
                                 for (int j = 0; j < 2; ++j) {
-                                    const uint32_t c[4] = {nibbles_bf16(f[2 * m], 2 * j), nibbles_bf16(f[2 * m + 1], 2 * j), nibbles_bf16(f[2 * m], 2 * j + 1), nibbles_bf16(f[2 * m + 1], 2 * j + 1)};
+                                    const uint32_t c[4] = {nibbles_half(f[2 * m], 2 * j), nibbles_half(f[2 * m + 1], 2 * j), nibbles_half(f[2 * m], 2 * j + 1), nibbles_half(f[2 * m + 1], 2 * j + 1)};
 #pragma unroll
-                                    for (int n = 0; n < HN; ++n) mma(y[n], c, q[2 * p + j][n][0], q[2 * p + j][n][1]);
+                                    for (int n = 0; n < HN; ++n) {
+                                        if (j == 0) mma_half_first(y[n], c, q[2 * p][n][0], q[2 * p][n][1]);
+                                        else mma_half(y[n], c, q[2 * p + 1][n][0], q[2 * p + 1][n][1]);
+                                    }
                                 }
-                                const uint32_t s0 = kscale[h * 16 * S::SCALES + p], s1 = kscale[(h * 16 + 8) * S::SCALES + p];
 #pragma unroll
                                 for (int n = 0; n < HN; ++n)
 #pragma unroll
                                     for (int i = 0; i < 2; ++i) {
-                                        x[h][n][i] = fmaf(low_bf16(s0), y[n][i], fmaf(high_bf16(s0), qsum[n][i][p], x[h][n][i]));
-                                        x[h][n][2 + i] = fmaf(low_bf16(s1), y[n][2 + i], fmaf(high_bf16(s1), qsum[n][i][p], x[h][n][2 + i]));
+                                        x[h][n][i] = fmaf(low_bf16(s0[p]), y[n][i], x[h][n][i]);
+                                        x[h][n][2 + i] = fmaf(low_bf16(s1[p]), y[n][2 + i], x[h][n][2 + i]);
                                     }
                             }
                         }
@@ -559,6 +618,9 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             }
                         }
                     } else {
+                        uint32_t v0[GROUPS], v1[GROUPS];
+                        scales_of(v0, vscale + h * 16 * S::SCALES);
+                        scales_of(v1, vscale + (h * 16 + 8) * S::SCALES);
 #pragma unroll
                         for (int k = 0; k < DP / 64; ++k) {
                             uint32_t f[4];                         // 16 keys, 64 columns: of four neighbours, two are rows 0..7 and 8..15 of one product, two of the next
@@ -566,7 +628,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
                                 const int group = 2 * k + m;
-                                const uint32_t s0 = vscale[h * 16 * S::SCALES + group], s1 = vscale[(h * 16 + 8) * S::SCALES + group];
+                                const uint32_t s0 = v0[group], s1 = v1[group];
                                 uint32_t w[HN][2];
 #pragma unroll
                                 for (int n = 0; n < HN; ++n) {
