@@ -35,9 +35,9 @@ namespace shared {
 template <int DP, int TILES, bool BOXES> struct Shape {
     static constexpr int STAGES = TILES == 1 ? 3 : 2;
     static constexpr int TILE_BYTES = DP / 64 * SLAB;
-    static constexpr int SOFTMAX = 4 * TILES, ISSUE = SOFTMAX, COPY = ISSUE + TILES, COPIERS = BOXES ? 1 : 2 / TILES, WARPS = COPY + (BOXES ? 1 : COPIERS * STAGES), THREADS = WARPS * 32;
+    static constexpr int SOFTMAX = 8 * TILES, ISSUE = SOFTMAX, COPY = ISSUE + TILES, COPIERS = BOXES ? 1 : 2 / TILES, WARPS = COPY + (BOXES ? 1 : COPIERS * STAGES), THREADS = WARPS * 32;
     static constexpr int TMEM = TILES == 1 ? 256 : 512;            // columns: S of every tile, O of every tile
-    static constexpr size_t SMEM = 1024 + (size_t)TILE_BYTES * (TILES + 2 * STAGES) + 512;
+    static constexpr size_t SMEM = 1024 + (size_t)TILE_BYTES * (TILES + 2 * STAGES) + 512 + TILES * 2 * TILE * sizeof(float);
 };
 constexpr int MOST_ROWS = 256;
 }  // namespace shared
@@ -160,8 +160,9 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     uint32_t *valid = (uint32_t *)(V + STAGES * S::TILE_BYTES);        // [SLOTS][4]
     uint64_t *bars = (uint64_t *)(valid + SLOTS * 4);
     uint64_t *k_full = bars, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES, *q_full = v_empty + STAGES,
-             *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES, *copied = valid_full + SLOTS;
-    uint32_t *tmem_slot = (uint32_t *)(copied + 1);
+             *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES, *copied = valid_full + SLOTS, *told = copied + 1;
+    uint32_t *tmem_slot = (uint32_t *)(told + 4 * TILES);
+    float *halves = (float *)(valid + 512 / 4);            // [TILES][2][128]: what the halves of the rows have to tell one another
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1), *met = abort_flag + 1;         // met: a page outside the cache
     const Cells &cs = a.step.c;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -185,12 +186,12 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     const int active = TILES == 2 && rows > TILE ? 2 : 1;  // tiles of rows that there are
 
     // The queries' rows, 16 (8) lanes to a row, on their way while the rest is set up; what is no row is zeros.
-    constexpr int LOADS = PIECES;                          // of a lane: 32 rows of PIECES pieces to a warp
+    constexpr int LOADS = PIECES / 2;                      // of a lane: 16 rows of PIECES pieces to a warp
     uint4 queries[LOADS];
-    if (warp < S::SOFTMAX && warp / 4 < active)
+    if (warp < S::SOFTMAX && warp / 8 < active)
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int piece = lane % PIECES, id = warp * 32 + lane / PIECES + j * (32 / PIECES), b = id / group;
+            const int piece = lane % PIECES, id = warp * 16 + lane / PIECES + j * (32 / PIECES), b = id / group;
             const bf16 *from = a.step.q + (b0 + b) * a.step.q_row + (hk * group + id - b * group) * a.step.q_head + piece * 8;
             queries[j] = id < rows && piece * 8 < cs.d ? *reinterpret_cast<const uint4 *>(from) : make_uint4(0u, 0u, 0u, 0u);
         }
@@ -205,11 +206,12 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         for (int s = 0; s < SLOTS; ++s) mbar_init(&valid_full[s], COPIERS);
         mbar_init(copied, 1);
         for (int w = 0; w < TILES; ++w) {
-            mbar_init(&q_full[w], 4);
+            mbar_init(&q_full[w], 8);
             mbar_init(&s_full[w], 1);
             mbar_init(&p_full[2 * w], 4);
             mbar_init(&p_full[2 * w + 1], 4);
             mbar_init(&o_full[w], 1);
+            for (int i = 0; i < 4; ++i) mbar_init(&told[4 * w + i], 2);
         }
         *abort_flag = 0;
         *met = 0;
@@ -391,15 +393,30 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             if (ok) commit(lead, &o_full[w]);
             __syncwarp();
         }
-    } else if (warp / 4 < active) {
-        const int w = warp >> 2, r = (warp & 3) * 32 + lane;                 // this thread's row of the tile
+    } else if (warp / 8 < active) {
+        // Two threads to a row of scores, half of a tile's keys each, in warps on one scheduler.
+        const int w = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;                 // this thread's row of the tile
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + w * TILE, o_addr = tmem + lanes + TILES * TILE + w * DP;
+        float *mine_told = halves + (w * 2 + half) * TILE + r;
+        const float *other_told = halves + (w * 2 + (half ^ 1)) * TILE + r;
+        uint64_t *both = &told[4 * w + (warp & 3)];
+        // What the other thread of the row tells, the i-th time.  It is read before that thread's weights are handed over, and written again after their product.
+        auto exchange = [&](float x, int i, float *y) {
+            *mine_told = x;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(both);
+            const bool there = warp_wait(both, (uint32_t)(i & 1), abort_flag, a.step.status, 12);
+            tc_fence_after();
+            *y = *other_told;
+            return there;
+        };
         {
             unsigned char *to = Q + w * S::TILE_BYTES;
             const int piece = lane % PIECES;
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
-                const int row = (warp & 3) * 32 + lane / PIECES + j * (32 / PIECES);
+                const int row = (warp & 7) * 16 + lane / PIECES + j * (32 / PIECES);
                 *reinterpret_cast<uint4 *>(to + piece / 8 * SLAB + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = queries[j];
             }
             fence_proxy_async();
@@ -421,30 +438,33 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             if (holes) bits = *reinterpret_cast<const uint4 *>(valid + slot * 4);
             const bool cut = (bits.x & bits.y & bits.z & bits.w) != ~0u;
             seen = seen || (bits.x | bits.y | bits.z | bits.w) != 0u;
-            uint32_t x[4][32];
+            uint32_t x[2][32];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tmem_ld_32x32(s_addr + j * 32, x[j]);
+            for (int j = 0; j < 2; ++j) tmem_ld_32x32(s_addr + half * 64 + j * 32, x[j]);
             tmem_ld_wait();
             if (cut) {
-                const uint32_t word[4] = {bits.x, bits.y, bits.z, bits.w};
+                const uint32_t word[2] = {half ? bits.z : bits.x, half ? bits.w : bits.y};
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         if (!(word[j] >> e & 1u)) x[j][e] = __float_as_uint(-INFINITY);
             }
             float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) most[e / 2 & 3] = max3(most[e / 2 & 3], __uint_as_float(x[j][e]), __uint_as_float(x[j][e + 1]));
-            const float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), other;
+            ok = exchange(top, i, &other);                 // both have their scores: weights may overwrite them
+            if (!ok) break;
+            top = fmaxf(top, other);
             // the reference moves: 8 is the factor 2^8 that P may exceed 1 by
             if (__any_sync(~0u, c * (top - m) > 8.f)) {
                 const float now = fmaxf(top, m), f = now == -INFINITY ? 1.f : ex2(c * (m - now));
                 m = now;
                 l *= f;
-                if (i > 0) {
+                if (i > 0 && half == 0) {                  // whose weights are waited for first
 #pragma unroll 1
                     for (int j = 0; j < DP / 16; ++j) {
                         uint32_t o[16];
@@ -460,7 +480,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             const Pair cc = pair(c, c), mm = pair(mc, mc);
             Pair sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 2; ++j) {
                 uint32_t p[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -469,30 +489,31 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                     sum[e & 1] = add(sum[e & 1], y);
                     p[e] = pack_bf16(y);                   // rounded once, for the product with V
                 }
-                tmem_st_32x16(s_addr + j * 16, p);
-                if (j & 1) {                               // the product with V begins when half of the keys' weights are there
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[2 * w + j / 2]);
-                }
+                tmem_st_32x16(s_addr + half * 32 + j * 16, p);
             }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_full[2 * w + half]);
             const float2 part = split(add(sum[0], sum[1]));
             l += part.x + part.y;
         }
         if (ok) ok = warp_wait(&o_full[w], 0, abort_flag, a.step.status, 10);
+        float other = 0.f;
+        if (ok) ok = exchange(l, n, &other);
+        l = half ? other + l : l + other;
         const int id = w * TILE + r;
         if (ok) {
             tc_fence_after();
             const int64_t all = (int64_t)cs.nseq * group, unit = (int64_t)at.part * kv_heads + hk, row = (int64_t)b0 * group + id;
-            if (id < rows) {
+            if (id < rows && half == 0) {
                 a.part_most[unit * all + row] = m;
                 a.part_sum[unit * all + row] = m == -INFINITY && l == 0.f ? (seen ? 1.f : 0.f) : l;
             }
             // quads of columns, rows next to one another: a warp writes 512 bytes at a time
             float4 *out = reinterpret_cast<float4 *>(a.part) + unit * (DP / 4) * all + row;
 #pragma unroll 1
-            for (int j = 0; j < DP / 16; ++j) {
+            for (int j = half * (DP / 32); j < (half + 1) * (DP / 32); ++j) {
                 uint32_t o[16];
                 tmem_ld_32x16(o_addr + j * 16, o);
                 tmem_ld_wait();
