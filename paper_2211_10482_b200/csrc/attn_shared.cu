@@ -160,8 +160,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     uint32_t *valid = (uint32_t *)(V + STAGES * S::TILE_BYTES);        // [SLOTS][4]
     uint64_t *bars = (uint64_t *)(valid + SLOTS * 4);
     uint64_t *k_full = bars, *k_empty = k_full + STAGES, *v_full = k_empty + STAGES, *v_empty = v_full + STAGES, *q_full = v_empty + STAGES,
-             *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES, *copied = valid_full + SLOTS, *told = copied + 1;
-    uint32_t *tmem_slot = (uint32_t *)(told + 4 * TILES);
+             *s_full = q_full + TILES, *p_full = s_full + TILES, *o_full = p_full + 2 * TILES, *valid_full = o_full + TILES, *copied = valid_full + SLOTS, *turn = copied + 1;
+    uint32_t *tmem_slot = (uint32_t *)(turn + 4 * TILES);
     float *halves = (float *)(valid + 512 / 4);            // [TILES][2][128]: what the halves of the rows have to tell one another
     volatile int *abort_flag = (volatile int *)(tmem_slot + 1), *met = abort_flag + 1;         // met: a page outside the cache
     const Cells &cs = a.step.c;
@@ -208,10 +208,10 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         for (int w = 0; w < TILES; ++w) {
             mbar_init(&q_full[w], 8);
             mbar_init(&s_full[w], 1);
+            mbar_init(&o_full[w], 1);
             mbar_init(&p_full[2 * w], 4);
             mbar_init(&p_full[2 * w + 1], 4);
-            mbar_init(&o_full[w], 1);
-            for (int i = 0; i < 4; ++i) mbar_init(&told[4 * w + i], 2);
+            for (int i = 0; i < 4; ++i) mbar_init(&turn[4 * w + i], 2);
         }
         *abort_flag = 0;
         *met = 0;
@@ -399,17 +399,14 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + w * TILE, o_addr = tmem + lanes + TILES * TILE + w * DP;
         float *mine_told = halves + (w * 2 + half) * TILE + r;
         const float *other_told = halves + (w * 2 + (half ^ 1)) * TILE + r;
-        uint64_t *both = &told[4 * w + (warp & 3)];
-        // What the other thread of the row tells, the i-th time.  It is read before that thread's weights are handed over, and written again after their product.
-        auto exchange = [&](float x, int i, float *y) {
+        // What the other thread of the row tells.  It is read before that thread's weights are handed over, and written again after their product.  Both come here
+        // as often whatever fails: the barrier of the two warps has no limit of its own.
+        auto exchange = [&](float x) {
             *mine_told = x;
             tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(both);
-            const bool there = warp_wait(both, (uint32_t)(i & 1), abort_flag, a.step.status, 12);
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + 4 * w + (warp & 3)) : "memory");
             tc_fence_after();
-            *y = *other_told;
-            return there;
+            return *(volatile const float *)other_told;
         };
         {
             unsigned char *to = Q + w * S::TILE_BYTES;
@@ -427,12 +424,15 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         float m = -INFINITY, l = 0.f;
         bool ok = true, seen = false;
         for (int i = 0; i < n; ++i) {
-            ok = warp_wait(&s_full[w], (uint32_t)(i & 1), abort_flag, a.step.status, 8);
+            if (ok) ok = warp_wait(&s_full[w], (uint32_t)(i & 1), abort_flag, a.step.status, 8);
             // the bits are looked at behind the last key, and once a page was met that is not there (which is said before its rows are asked for)
             const int slot = (i / STAGES & 1) * STAGES + i % STAGES;
             const bool holes = (first + i + 1) * TILE > len || *met;
             if (ok && holes) ok = warp_wait(&valid_full[slot], (uint32_t)(i / SLOTS & 1), abort_flag, a.step.status, 9);
-            if (!ok) break;
+            if (!ok) {
+                exchange(0.f);
+                continue;
+            }
             tc_fence_after();
             uint4 bits = make_uint4(~0u, ~0u, ~0u, ~0u);
             if (holes) bits = *reinterpret_cast<const uint4 *>(valid + slot * 4);
@@ -455,10 +455,8 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) most[e / 2 & 3] = max3(most[e / 2 & 3], __uint_as_float(x[j][e]), __uint_as_float(x[j][e + 1]));
-            float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])), other;
-            ok = exchange(top, i, &other);                 // both have their scores: weights may overwrite them
-            if (!ok) break;
-            top = fmaxf(top, other);
+            float top = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            top = fmaxf(top, exchange(top));               // both have their scores: weights may overwrite them
             // the reference moves: 8 is the factor 2^8 that P may exceed 1 by
             if (__any_sync(~0u, c * (top - m) > 8.f)) {
                 const float now = fmaxf(top, m), f = now == -INFINITY ? 1.f : ex2(c * (m - now));
@@ -479,6 +477,10 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             const float mc = m == -INFINITY ? 0.f : -m * c;
             const Pair cc = pair(c, c), mm = pair(mc, mc);
             Pair sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+            if (active == 2) {                             // one tile of rows after the other: the products of one go on under the weights of the other
+                ok = warp_wait(&turn[4 * w + (warp & 3)], (uint32_t)((i + 1 - w) & 1), abort_flag, a.step.status, 13);
+                if (!ok) continue;
+            }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 uint32_t p[16];
@@ -491,6 +493,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                 }
                 tmem_st_32x16(s_addr + half * 32 + j * 16, p);
             }
+            if (active == 2 && lane == 0) mbar_arrive(&turn[4 * (w ^ 1) + (warp & 3)]);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -499,8 +502,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             l += part.x + part.y;
         }
         if (ok) ok = warp_wait(&o_full[w], 0, abort_flag, a.step.status, 10);
-        float other = 0.f;
-        if (ok) ok = exchange(l, n, &other);
+        const float other = exchange(l);
         l = half ? other + l : l + other;
         const int id = w * TILE + r;
         if (ok) {
