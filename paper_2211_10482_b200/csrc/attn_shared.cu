@@ -68,7 +68,7 @@ __device__ __forceinline__ void copy_row(uint32_t dst, const void *src, bool the
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// Key tiles of a group's prefix, tiles of its rows, and what a key tile costs with one of these: 2.7 us where the 256 rows are two products, else 1.7.
+// Key tiles of a group's prefix, tiles of its rows, and what a key tile costs with one of these: 4250 cycles where the 256 rows are two products, else 3700.
 struct GroupOf {
     Rows seqs;
     int tiles, keys, cost;
@@ -76,10 +76,10 @@ struct GroupOf {
 };
 __device__ __forceinline__ GroupOf group_of(const SharedArgs &a, int i)
 {
-    if (i >= a.groups) return {{0, 0}, 0, 0, 2};
+    if (i >= a.groups) return {{0, 0}, 0, 0, 7};
     const Rows r = rows_of(a.group_offsets, i, a.step.c.nseq);
     const int len = length_of(a.prefix_lens[i], a.prefix_cols, a.step.c.page);
-    return {r, (r.len + a.seqs - 1) / a.seqs, (len + TILE - 1) / TILE, (int64_t)r.len * a.step.group > TILE ? 3 : 2};
+    return {r, (r.len + a.seqs - 1) / a.seqs, (len + TILE - 1) / TILE, (int64_t)r.len * a.step.group > TILE ? 8 : 7};
 }
 
 // Part `part` of `parts` of a tile of rows; none: group -1.
@@ -223,31 +223,33 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     }
     if (hk == 0 && at.part == 0)
         for (int i = threadIdx.x; i < seqs; i += S::THREADS) a.step.part_count[b0 + i] = at.parts;
+    // BOXES: a lane to a box, `box` keys of one page; a page that is not there is one behind the last.  The first tile's are looked up during the set-up.
+    const int *table = a.prefix_table + (int64_t)at.group * a.prefix_cols;
+    const int box = min(cs.page, TILE), boxes = TILE / box;
+    int next_page = 0, next_slot = 0;
+    bool missing = false;
+    auto look = [&](int i) {
+        const int key = (first + i) * TILE + lane * box;
+        next_page = cs.pages;
+        next_slot = 0;
+        if (i >= n || lane >= boxes || key >= len) return;
+        const Place p = place_of(key, cs.page, cs.page_magic);
+        const int page = table[p.col];
+        next_slot = p.slot;
+        missing = (unsigned)page >= (unsigned)cs.pages;
+        if (!missing) next_page = page;
+    };
+    if (BOXES && warp == S::COPY) look(0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(~0u, *tmem_slot, 0);
 
     if (BOXES && warp == S::COPY) {
-        // a lane to a box: `box` keys of one page; a page that is not there is one behind the last
-        const int *table = a.prefix_table + (int64_t)at.group * a.prefix_cols;
-        const int box = min(cs.page, TILE), boxes = TILE / box;
         bool ok = true;
-        int next_page = 0, next_slot = 0;
-        auto look = [&](int i) {
-            const int key = (first + i) * TILE + lane * box;
-            next_page = cs.pages;
-            next_slot = 0;
-            if (i >= n || lane >= boxes || key >= len) return;
-            const Place p = place_of(key, cs.page, cs.page_magic);
-            const int page = table[p.col];
-            next_slot = p.slot;
-            if ((unsigned)page < (unsigned)cs.pages) next_page = page;
-            else *met = 1;
-        };
-        look(0);
         for (int i = 0; i < n && ok; ++i) {
             const int page = next_page, in_page = next_slot;
+            if (missing) *met = 1;                         // said before the tile's rows are asked for
             const int s = i % STAGES, use = i / STAGES, slot = (use & 1) * STAGES + s;
             const uint32_t parity = (uint32_t)((use + 1) & 1);
             // bits of this lane's word: 32 keys, which may be several boxes or a part of one
@@ -293,7 +295,6 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         // each copies 128 / COPIERS keys of a stage; 16 (8) lanes to a row
         constexpr int KEYS = TILE / COPIERS, WORDS = KEYS / 32;
         const int s = (warp - S::COPY) / COPIERS, half = (warp - S::COPY) % COPIERS;
-        const int *table = a.prefix_table + (int64_t)at.group * a.prefix_cols;
         const unsigned char *kc = cs.k + hk * cs.head_stride, *vc = cs.v + hk * cs.head_stride;
         const int piece = lane % PIECES, row0 = lane / PIECES;
         constexpr int ROWS = 32 / PIECES;                  // rows that a warp copies at a time
