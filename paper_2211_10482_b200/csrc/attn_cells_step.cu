@@ -728,9 +728,11 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
 // columns where units are few, four columns of a head to a thread, and several threads for the same columns where there are pieces enough: each goes through its pieces and parts once, with the largest score and
 // the sum of those so far, a few on their way at a time.
 namespace cstep {
-constexpr int JOIN = 512, BATCH = 4;       // threads at most; pieces on their way
+constexpr int JOIN = 512;                  // threads at most
 }
-template <int DP>
+// BATCH pieces on their way at a time: 8 of them where there are pieces alone (one sequence of 8192 keys 19.2 us, with 4 20.6), 4 beside a prefix's parts, where
+// the registers of 8 leave an SM one block (8 sequences behind one prefix 21.6 and 24.9 us).
+template <int DP, int BATCH>
 __global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStepArgs a, int unit_heads, int keys_of_tile, int quarters)
 {
     using namespace cstep;
@@ -789,7 +791,8 @@ __global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStep
                     x[u] = *reinterpret_cast<const float4 *>(values(i));
                 }
 #pragma unroll
-                for (int u = 0; u < BATCH; ++u) more(m[u], l[u], x[u]);
+                for (int u = 0; u < BATCH; ++u)
+                    if (i0 + u * slices < count) more(m[u], l[u], x[u]);
             }
         };
         if (busy) {
@@ -915,7 +918,8 @@ static st_status run_heads(CellsStepArgs a, cudaStream_t stream)
     // few units may have many pieces each
     const bool few = (int64_t)a.units * a.c.nseq < 2 * sm_count_or_default();
     const int quarters = few ? 4 : 1;
-    return launch(cells_join_kernel<DP>, dim3((unsigned)(a.units * quarters), (unsigned)a.c.nseq), few ? 512 : 128, 0, stream, a, S::HEADS, S::KEYS, quarters);
+    return launch(a.part_count ? cells_join_kernel<DP, 4> : cells_join_kernel<DP, 8>, dim3((unsigned)(a.units * quarters), (unsigned)a.c.nseq), few ? 512 : 128, 0, stream, a,
+                  S::HEADS, S::KEYS, quarters);
 }
 
 template <int DTYPE, int DP, bool WIDE>
