@@ -23,14 +23,17 @@ namespace st {
 namespace attn {
 
 namespace cstep {
-constexpr int WARPS = 4, STAGES = 2, MOST_BLOCKS = 4;      // warps of a block, tiles in a ring, blocks on an SM
+constexpr int WARPS = 4, MOST_HEADS = 32;                  // warps of a block; blocks on an SM times heads of a unit
 // What a unit costs a warp beside its tiles, in tiles: its queries, its results.
 constexpr int UNIT_COST = 3;
 // The shortest piece of the line that is worth a warp, in tiles.
 constexpr int LEAST = 3;
 template <int DTYPE, int DP, int HN> struct Shape {
     static constexpr int HEADS = 8 * HN;                                           // of a unit
-    static constexpr int BLOCKS = HN == 2 ? 2 : DTYPE == ST_I4 ? MOST_BLOCKS : 3;  // on an SM, as registers and shared memory leave room for
+    static constexpr int BLOCKS = HN == 2 ? 2 : 3;                                 // on an SM, as registers and shared memory leave room for
+    // Tiles in a ring.  Of 4 bits, whose tiles are half as large, three (64 sequences of up to 6000 tokens 74.4 us; two 89; two and a fourth block on the SM,
+    // for which registers are few, 79.7); of 8 bits three leave room for two blocks only (117 us, not 85.9).
+    static constexpr int STAGES = DTYPE == ST_I4 ? 3 : 2;
     static constexpr int KEYS = DTYPE == ST_BF16 ? 16 : 32;                        // of a tile
     static constexpr int ROW = DTYPE == ST_BF16 ? 2 * DP : DTYPE == ST_I8 ? DP : DP / 2;       // bytes
     static constexpr int SCALES = DTYPE == ST_BF16 ? 0 : DTYPE == ST_I8 ? 1 : DP / GROUP;      // of a row, 4 bytes each
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
 {
     using namespace cstep;
     using S = Shape<DTYPE, DP, HN>;
-    constexpr int KEYS = S::KEYS, ROW = S::ROW, PIECES = S::PIECES, NK = KEYS / 16, GROUPS = DP / GROUP, HEADS = S::HEADS;
+    constexpr int STAGES = S::STAGES, KEYS = S::KEYS, ROW = S::ROW, PIECES = S::PIECES, NK = KEYS / 16, GROUPS = DP / GROUP, HEADS = S::HEADS;
     extern __shared__ __align__(128) unsigned char smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3;
     const int chunks = (a.group + HEADS - 1) / HEADS;
@@ -873,8 +876,7 @@ __global__ void __launch_bounds__(1024) cells_plan_kernel(const CellsStepArgs a,
 StepPlan step_plan(int64_t nseq, size_t from)
 {
     StepPlan p;
-    // slots of 16 heads and two blocks an SM, or of 8 and up to four
-    const size_t rows = (size_t)sm_count_or_default() * cstep::MOST_BLOCKS * cstep::WARPS * 2 * 8;
+    const size_t rows = (size_t)sm_count_or_default() * cstep::MOST_HEADS * cstep::WARPS * 2;
     p.starts = round_up(from, 256);
     p.most = round_up(p.starts + (nseq + 1) * sizeof(int64_t), 256);
     p.sum = p.most + rows * sizeof(float);
@@ -909,7 +911,7 @@ template <int DTYPE, int DP, int HN, bool WIDE>
 static st_status run_heads(CellsStepArgs a, cudaStream_t stream)
 {
     using S = cstep::Shape<DTYPE, DP, HN>;
-    static_assert(S::BLOCKS * S::HEADS <= cstep::MOST_BLOCKS * 8 && S::KEYS == (DTYPE == ST_BF16 ? 16 : 32), "as the workspace and the plan have it");
+    static_assert(S::BLOCKS * S::HEADS <= cstep::MOST_HEADS && S::KEYS == (DTYPE == ST_BF16 ? 16 : 32), "as the workspace and the plan have it");
     if (!ensure_dynamic_smem(cells_step_kernel<DTYPE, DP, HN, WIDE>, S::SMEM)) return ST_ERR_CUDA;
     const int blocks = sm_count_or_default() * S::BLOCKS;
     a.slots = blocks * cstep::WARPS;
