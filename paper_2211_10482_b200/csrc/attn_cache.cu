@@ -337,7 +337,7 @@ static st_status run_cache(CacheArgs &a, int dtype, bool write, cudaStream_t str
     const int64_t runs = (int64_t)a.n * 2 * a.chunks / (sm_count_or_default() * 64);
     a.run = (int)(runs < 1 ? 1 : runs > 16 ? 16 : runs);
     const int64_t items = ((int64_t)a.n + a.run - 1) / a.run * 2 * a.chunks, grid = (items + WARPS - 1) / WARPS;
-    if (items > INT32_MAX) return ST_ERR_UNSUPPORTED;
+    if (items > INT32_MAX - WARPS) return ST_ERR_UNSUPPORTED;
     const st_status rc = clear_status(a.status, stream);
     if (rc != ST_OK) return rc;
     void (*kernel)(CacheArgs) = nullptr;

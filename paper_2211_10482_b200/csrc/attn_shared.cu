@@ -1,7 +1,8 @@
 // st_attn_shared_step: one token of every sequence over a prefix that its group of sequences shares, then over its own tokens.
 //
-// Two kernels, between one that lays out the work and one that joins.  The first takes all queries of a group that read one key head as the rows of a matrix, up to 256 of them, and makes
-//     S = Q K^T  (tcgen05, fp32 in tensor memory);   P = exp2(c S - c m)  (one thread per row);   O += P V
+// Two kernels, between one that lays out the work and one that joins.  The first takes all queries of a group that read one key head as the rows of a
+// matrix, up to 256 of them, and makes
+//     S = Q K^T  (tcgen05, fp32 in tensor memory);   P = exp2(c S - c m)  (two threads per row);   O += P V
 // over a range of the prefix's keys, as st_attn_window does for a tile of a prompt; it leaves (m, l, O) as a part.  The second is the single-token kernel over
 // each sequence's own keys, whose pieces are joined with the parts.  A row of the prefix is so read once for 256 queries, not once for
 // every sequence.
@@ -9,8 +10,13 @@
 // Pages whose length divides a tile of 128 keys, or is a multiple of it, come by TMA, a box to a page: one warp looks the pages up and asks for them.  A page
 // that is not there is a box outside the tensor and so zeros; values behind the last key are cleared.  Pages of other lengths are gathered by cp.async
 // into the swizzled tiles that the tensor cores read, by one or two warps for each stage, which copy, see the copies done, make them visible to the tensor
-// cores' proxy and hand the tile over.  (With pages of 64 and all rows gathered by cp.async 84 us for 128 sequences behind two prefixes of 16384 and less.)
+// cores' proxy and hand the tile over.  (With pages of 64 and all rows gathered by cp.async this kernel took 84 us for 128 sequences behind two prefixes, by boxes 70.)
 // Either way a bit of a mask says which keys have a place.
+//
+// A tile of keys takes 4250 cycles where it meets two tiles of rows, whose four products of 128 x 128 x 128 take half of that: one tile's weights (scores from
+// tensor memory, maxima, an exchange with the other half's thread, 64 exponentials) are made while the other one's products run, and in turns, as without them both tiles
+// wanted the exponentials at once and the tensor cores then (128 sequences behind two prefixes: 114.9 us, with turns 107.4).  With one thread to a row and no
+// turns 112; with weights handed over in quarters 113.
 //
 // Which part of which prefix a block takes is decided on the device, where the lengths are: key tiles of a part are as many as give no more parts than there
 // are blocks in one turn on the SMs.
@@ -30,8 +36,7 @@ struct SharedArgs {
 };
 
 namespace shared {
-// TILES of 128 rows; with one there is room for a third stage of keys and values, whose bytes bound few rows, and for a second warp to copy each: twelve warps
-// have 168 registers a thread, which a row of scores needs
+// TILES of 128 rows; with one there is room for a third stage of keys and values, whose bytes bound few rows, and for a second warp to copy each
 template <int DP, int TILES, bool BOXES> struct Shape {
     static constexpr int STAGES = TILES == 1 ? 3 : 2;
     static constexpr int TILE_BYTES = DP / 64 * SLAB;
@@ -87,7 +92,7 @@ struct PartOf {
     int group, tile, part, parts;
 };
 // By a whole warp: the least work in a part that needs no more parts than there are blocks, and no more of one prefix than there is room for, 32 candidates at
-// a time (one after the other took 3 to 5 us); then what block `index` of one key head does.
+// a time (6000 cycles with the loads ahead of it; one after the other 5500 to 10000); then what block `index` of one key head does.
 __device__ __forceinline__ PartOf part_of(const SharedArgs &a, int index, int kv_heads, int lane)
 {
     const GroupOf mine = group_of(a, lane);                // all there is, up to 32 groups

@@ -1041,3 +1041,5 @@ def test_one_workspace_for_calls_one_after_the_other():
         bad[1, 0] = 1 << 20
         st.st_attn_cache_step(r, small.cells[0], small.cells[1], bad, small.lens, 100, **small.how(), ws=ws)
         assert st.st_check_status(ws) == st.ST_ERR_DEV_BOUNDS
+    assert torch.equal(st.st_attn_cache_step(r, *small.pages(), 40, **small.how(), ws=ws), want[1])
+    ok()
