@@ -116,8 +116,9 @@ __device__ __forceinline__ void pieces_of(const Pair (&a)[4], const Pair (&b)[4]
     }
 }
 
+// MIXED: all rows of a token, of q and of k, fit a warp's groups of lanes and are taken at once; a group's row is of one table for good.
 // LANES to a row; ODD: `rot` is no multiple of 16, so that pieces and pairs do not fit together and columns are taken one by one.
-template <int LANES, bool NORM, bool INTER, bool ODD, bool GRAD>
+template <int LANES, bool NORM, bool INTER, bool ODD, bool GRAD, bool MIXED>
 __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GRAD)) rotate_kernel(const RotateArgs a)
 {
     using namespace rot;
@@ -171,26 +172,26 @@ __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GR
     const int hop = gridDim.x * WARPS, begin = blockIdx.x * WARPS + warp;
     // What is fetched next: rows `f_left` and on of a table's heads (q's, then k's) of item f_item.
     int f_item = begin, f_left = 0, f_stage = 0;
-    bool f_k = true;                                       // k's heads are what is fetched
+    bool f_k = false, f_begun = false;                     // k's heads are what is fetched; there was a fetch before
     const bf16 *f_x = nullptr, *f_dy = nullptr;
     int64_t f_hop = 0;
     auto fetch = [&] {
         if (f_left <= 0) {                                 // the next table with rows, if there is one
-            if (f_x) {
-                if (f_k) f_item += hop;
-                f_k = !f_k;
-            } else {
-                f_k = false;
+            if (f_begun) {                                 // (f_x may be NULL where the gradient needs no x)
+                if (MIXED || f_k) f_item += hop;
+                f_k = !MIXED && !f_k;
             }
+            f_begun = true;
             while (f_item < a.items) {
                 const Item f = item_of(f_item);
-                f_left = f_k ? f.nk : f.nq;
+                f_left = MIXED ? a.width : f_k ? f.nk : f.nq;
                 if (f_left > 0) {
-                    const int h = (f_k ? f.k0 : f.q0) + sub;
-                    const int64_t head = f_k ? a.k_head : a.q_head;
-                    f_x = (f_k ? a.k + f.t * a.k_row : a.q + f.t * a.q_row) + h * head;
+                    const bool of_k = MIXED ? sub >= a.heads : f_k;
+                    const int h = MIXED ? sub - (of_k ? a.heads : 0) : (of_k ? f.k0 : f.q0) + sub;
+                    const int64_t head = of_k ? a.k_head : a.q_head;
+                    f_x = (of_k ? a.k + f.t * a.k_row : a.q + f.t * a.q_row) + h * head;
                     f_hop = ROWS * head;
-                    if (GRAD) f_dy = (f_k ? a.dk_out + (int64_t)f.t * kv_heads * a.d : a.dq_out + (int64_t)f.t * a.heads * a.d) + h * a.d;
+                    if (GRAD) f_dy = (of_k ? a.dk_out + (int64_t)f.t * kv_heads * a.d : a.dq_out + (int64_t)f.t * a.heads * a.d) + h * a.d;
                     break;
                 }
                 if (f_k) f_item += hop;
@@ -263,20 +264,21 @@ __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GR
             }
         }
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {                      // heads of q, then of k
-            const int first = m ? it.k0 : it.q0, n = m ? it.nk : it.nq;
+        for (int m = 0; m < (MIXED ? 1 : 2); ++m) {        // heads of q, then of k
+            const bool of_k = MIXED ? sub >= a.heads : m;
+            const int first = MIXED ? (of_k ? -a.heads : 0) : m ? it.k0 : it.q0, n = MIXED ? a.width : m ? it.nk : it.nq;
             if (n == 0) continue;
             Pair wa[4], wb[4];
             if (NORM)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float4 x = weights[m][e][l], y = weights[m][2 + e][l];
+                    const float4 x = weights[of_k][e][l], y = weights[of_k][2 + e][l];
                     wa[2 * e] = pair(x.x, x.y);
                     wa[2 * e + 1] = pair(x.z, x.w);
                     wb[2 * e] = pair(y.x, y.y);
                     wb[2 * e + 1] = pair(y.z, y.w);
                 }
-            bf16 *dst = (m ? a.k_out : a.q_out) + ((int64_t)it.t * (m ? kv_heads : a.heads) + first + sub) * a.d;
+            bf16 *dst = (of_k ? a.k_out : a.q_out) + ((int64_t)it.t * (of_k ? kv_heads : a.heads) + first + sub) * a.d;
             for (int h = 0; h < n; h += ROWS, dst += ROWS * a.d) {
                 const bool in = h + sub < n;
                 asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
@@ -389,8 +391,9 @@ __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GR
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float2 x = split(dwa[m][e / 2]), y = split(dwb[m][e / 2]);
+                const float2 x = split(dwa[MIXED ? 0 : m][e / 2]), y = split(dwb[MIXED ? 0 : m][e / 2]);
                 float va = e % 2 ? x.y : x.x, vb = e % 2 ? y.y : y.x;
+                if (MIXED && (sub >= a.heads) != (m == 1)) va = vb = 0.f;
 #pragma unroll
                 for (int o = 16; o >= LANES; o >>= 1) {
                     va += __shfl_xor_sync(~0u, va, o);
@@ -436,12 +439,12 @@ __global__ void __launch_bounds__(1024) rotate_weight_kernel(const float *part, 
 
 size_t rotate_partials(bool wanted) { return wanted ? (size_t)sm_count_or_default() * rot::min_blocks(false, true) * 2 * rot::MAX_D * sizeof(float) : 0; }
 
-template <int LANES, bool ODD, bool GRAD>
+template <int LANES, bool ODD, bool GRAD, bool MIXED>
 static st_status launch_rotate(const RotateArgs &a, bool norm, bool inter, int grid, cudaStream_t stream)
 {
     using namespace rot;
-    void (*kernel)(RotateArgs) = norm ? (inter ? rotate_kernel<LANES, true, true, ODD, GRAD> : rotate_kernel<LANES, true, false, ODD, GRAD>)
-                                      : (inter ? rotate_kernel<LANES, false, true, ODD, GRAD> : rotate_kernel<LANES, false, false, ODD, GRAD>);
+    void (*kernel)(RotateArgs) = norm ? (inter ? rotate_kernel<LANES, true, true, ODD, GRAD, MIXED> : rotate_kernel<LANES, true, false, ODD, GRAD, MIXED>)
+                                      : (inter ? rotate_kernel<LANES, false, true, ODD, GRAD, MIXED> : rotate_kernel<LANES, false, false, ODD, GRAD, MIXED>);
     const size_t smem = (size_t)warps(GRAD) * 32 * ahead(GRAD) * 16 * (ODD ? 1 : 2) * (GRAD && norm ? 2 : 1) + (norm ? WEIGHTS * 16 : 0);
     if (!ensure_dynamic_smem(kernel, smem)) return ST_ERR_CUDA;
     return launch(kernel, dim3((unsigned)grid), warps(GRAD) * 32, smem, stream, a);
@@ -463,8 +466,10 @@ static st_status run_rotate(RotateArgs &a, bool norm, bool inter, cudaStream_t s
     int64_t grid = ((int64_t)a.items + WARPS - 1) / WARPS;
     if (grid > most) grid = most;
     *blocks = (int)grid;
-    if (odd) return launch_rotate<16, true, GRAD>(a, norm, inter, (int)grid, stream);
-    return a.d <= 64 ? launch_rotate<4, false, GRAD>(a, norm, inter, (int)grid, stream) : launch_rotate<8, false, GRAD>(a, norm, inter, (int)grid, stream);
+    if (odd) return launch_rotate<16, true, GRAD, false>(a, norm, inter, (int)grid, stream);
+    if (a.chunks == 1 && a.width > a.heads && a.width <= rows)
+        return a.d <= 64 ? launch_rotate<4, false, GRAD, true>(a, norm, inter, (int)grid, stream) : launch_rotate<8, false, GRAD, true>(a, norm, inter, (int)grid, stream);
+    return a.d <= 64 ? launch_rotate<4, false, GRAD, false>(a, norm, inter, (int)grid, stream) : launch_rotate<8, false, GRAD, false>(a, norm, inter, (int)grid, stream);
 }
 
 static st_status check_rotation(const st_rotation *r, const void *positions, const void *freq)

@@ -1,5 +1,7 @@
 """Norms with rotation, a cache in cells and the steps over it on the GPU: every call against its definition in 64 bits
 (attn_more_reference.py, which derives the tolerances), at the sizes, types and masks where tiles, pages and groups end."""
+import ctypes
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -1043,3 +1045,57 @@ def test_one_workspace_for_calls_one_after_the_other():
         assert st.st_check_status(ws) == st.ST_ERR_DEV_BOUNDS
     assert torch.equal(st.st_attn_cache_step(r, *small.pages(), 40, **small.how(), ws=ws), want[1])
     ok()
+
+
+@pytest.mark.parametrize("n,H,Hk,d", [(7, 1, 1, 64), (5000, 1, 1, 128), (5000, 1, 0, 64), (9, 4, 2, 128), (3001, 6, 3, 64)])
+def test_a_gradient_without_norms_needs_no_operands(n, H, Hk, d):
+    """q and k may be NULL: they are not read."""
+    dq, dk = normal(331, n, H, d), normal(332, n, Hk, d) if Hk else None
+    at, freq = torch.arange(n, dtype=torch.int32, device="cuda"), st.st_rotary_frequencies(d).cuda()
+    out = [torch.full_like(x, NAN) if x is not None else None for x in (dq, dk)]
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    p = lambda x: None if x is None else x.data_ptr()
+    r = st.StRotation(st.ST_BF16, st.ST_BF16, 0, 0, n, H, Hk, d, d, 0, 0, 0, 0, 0.0, 1.0)
+    rc = st.lib().st_attn_rotate_grad(ctypes.byref(r), None, None, p(dq), p(dk), p(at), p(freq), None, None, p(out[0]), p(out[1]), None, None, p(ws), 256,
+                                      torch.cuda.current_stream().cuda_stream)
+    assert rc == st.ST_OK
+    for x, g in ((dq, out[0]), (dk, out[1])):
+        if x is not None:
+            near(g, *ref.rotate_grad(x, None, x, at, freq, False, None, 1.0)[0], "gradient")
+
+
+@pytest.mark.parametrize("n,H,Hk,d", [(1, 1, 1, 32), (20000, 2, 2, 32), (20000, 1, 1, 128), (9001, 2, 1, 96), (15000, 5, 3, 64), (15000, 4, 4, 48), (12000, 5, 4, 64)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotations_of_tokens_of_few_heads(n, H, Hk, d, inter):
+    """All heads of a token, or all but one, fit a warp at once."""
+    both = normal(341, n, H + Hk + 1, d)
+    q, k = both[:, :H], both[:, H : H + Hk]
+    qw, kw = 1 + 0.3 * floats(342, d), 1 - 0.3 * floats(343, d)
+    at = torch.arange(n, dtype=torch.int32, device="cuda") - n // 2
+    rot = d - d % 16
+    freq = st.st_rotary_frequencies(rot).cuda()
+    out = st.st_attn_rotate(q, k, at, freq, inter, qw, kw, 1e-5)
+    for got, x, w in zip(out, (q, k), (qw, kw)):
+        near(got, *ref.rotate(x, w, at, freq, inter, 1e-5, 1.0), "rotated")
+    dq, dk = normal(344, n, H, d), normal(345, n, Hk, d)
+    gq, gk, gqw, gkw = st.st_attn_rotate_grad(q, k, dq, dk, at, freq, inter, qw, kw, 1e-5)
+    for got, gotw, x, w, dy in ((gq, gqw, q, qw, dq), (gk, gkw, k, kw, dk)):
+        (dx, tol), (dw, wtol) = ref.rotate_grad(x, w, dy, at, freq, inter, 1e-5, 1.0)
+        near(got, dx, tol, "gradient")
+        near(gotw, dw, wtol, "gradient of the weights")
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_steps_where_nothing_is_to_be_seen(bits):
+    c = Cache(351, [0, 0, 0], 2, 64, 16, bits)
+    q = normal(352, 3, 4, 64)
+    out = torch.full_like(q, NAN)
+    st.st_attn_cache_step(q, *c.pages(), 7, 2, **c.how(), out=out)
+    ok()
+    assert bool((out == 0).all())
+    if bits == 16:
+        for at in (offsets([1, 2]), offsets([0, 0]), offsets([3, 0])):
+            out.fill_(NAN)
+            st.st_attn_shared_step(q, *c.cells, c.table[:2].contiguous(), c.lens[:2].contiguous(), c.table, c.lens, at, out=out)
+            ok()
+            assert bool((out == 0).all())
