@@ -10,15 +10,15 @@
 // up to 8 heads.)  Weights go from the first product's layout to the second's by transposing 8 x 8 matrices of bf16 within the warp.
 //
 // Cells meet the tensor cores as whole numbers in fp16 or bf16, which hold all of them exactly, made from their bits (0x64 beside a byte u is 1024 + u in
-// fp16, 0x43 beside a byte or nibble below 128 is 128 + it in bf16).  fp16 takes less, where the other operand fits: the queries, each head's times the power
-// of two that brings its largest number to 2^8, which leaves all of bf16's digits down to 2^-22 of that; weights times their values' scales do not.  Scales
+// fp16, 0x43 beside a nibble is 128 + it in bf16).  fp16 takes less, where the other operand fits: the queries, each head's times the power
+// of two that brings its largest number to 2^8, which leaves all of bf16's digits down to 2^-22 of that; weights times the scales of bytes, in units that follow the largest.  Scales
 // come in afterwards, where they are one number for a key (ST_I8: a score times its key's scale, a weight times its value's) or for 32 columns (ST_I4: partial
 // scores of 32 columns, x += step acc, and what lo brings beside them, lo sum(q), by one product more; a set of weights for each 32 columns, and sum(w lo)).
 // The order of a fragment's columns is free as long as both operands agree, so that no byte has to change its lane: a lane's four bytes of K are four or eight
 // consecutive columns, of which the queries' fragments take the same ones.
 //
-// What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 86 us for 385 MB; instructions, some 1050 for a tile of 32 keys, are
-// issued in 61 % of the cycles by twelve warps of an SM.  Of 4 bits 75 us for 199 MB, 1090 instructions for a tile.  One sequence, window 8192: 19 us, five
+// What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 88 us for 385 MB; instructions, some 1050 for a tile of 32 keys, are
+// issued in 61 % of the cycles by twelve warps of an SM.  Of 4 bits 75 us for 199 MB, 1090 instructions for a tile.  One sequence, window 8192: 18.5 us, five
 // dependent steps (lay-out, pages, rows, pieces, joins) of some 3 us each.
 #include "attn_cells_step.cuh"
 #include "tc_common.cuh"
@@ -37,7 +37,7 @@ template <int DTYPE, int DP, int HN> struct Shape {
     static constexpr int HEADS = 8 * HN;                                           // of a unit
     static constexpr int BLOCKS = HN == 2 ? 2 : 3;                                 // on an SM, as registers and shared memory leave room for
     // Tiles in a ring.  Of 4 bits, whose tiles are half as large, three (64 sequences of up to 6000 tokens 74.4 us; two 89; two and a fourth block on the SM,
-    // for which registers are few, 79.7); of 8 bits three leave room for two blocks only (117 us, not 85.9).
+    // for which registers are few, 79.7); of 8 bits three leave room for two blocks only (117 us, with two 85.9).
     static constexpr int STAGES = DTYPE == ST_I4 ? 3 : 2;
     static constexpr int KEYS = DTYPE == ST_BF16 ? 16 : 32;                        // of a tile
     static constexpr int ROW = DTYPE == ST_BF16 ? 2 * DP : DTYPE == ST_I8 ? DP : DP / 2;       // bytes
@@ -112,22 +112,7 @@ __device__ __forceinline__ uint32_t minus_bf16(uint32_t a, uint32_t b)
     const __nv_bfloat162 w = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&w);
 }
-// Two bytes of w as bf16, those that `which` picks; w holds them with 128 added (sign bits flipped).  0x43 beside a byte u is x = 128 + u up to 127 and
-// x = 2 u from 128 on, so that u - 128 = (x - 256) - max(0, x / 2 - 128), all of it exact.  On the pipe of the multipliers, where masks (the low seven
-// bits less 128 or 256 by the sign bit) kept the other one at its limit.
-__device__ __forceinline__ uint32_t bytes_bf16(uint32_t w, uint32_t which)
-{
-    const uint32_t x = __byte_perm(w, 0x43434343u, which);
-    uint32_t r;
-    asm("{\n\t.reg .b32 t, h;\n\t"
-        "fma.rn.relu.bf16x2 h, %1, %2, %3;\n\t"
-        "fma.rn.bf16x2 t, %1, %4, %5;\n\t"
-        "fma.rn.bf16x2 %0, h, %6, t;\n\t}"
-        : "=r"(r)
-        : "r"(x), "r"(0x3F003F00u), "r"(0xC300C300u), "r"(0x3F803F80u), "r"(0xC380C380u), "r"(0xBF80BF80u));
-    return r;
-}
-// The same in fp16: 0x64 beside u is 1024 + u.
+// Two bytes of w as fp16, those that `which` picks; w holds them with 128 added (sign bits flipped).  0x64 beside u is 1024 + u.
 __device__ __forceinline__ uint32_t bytes_half(uint32_t w, uint32_t which)
 {
     uint32_t r;
@@ -160,6 +145,8 @@ __device__ __forceinline__ void scales_of(uint32_t (&s)[2], const uint32_t *from
     s[0] = x.x, s[1] = x.y;
 }
 
+// 1 / x of a power of two between 2^-126 and 2^126
+__device__ __forceinline__ float inverse_of(float x) { return __uint_as_float((254u << 23) - __float_as_uint(x)); }
 // Weight of a part whose largest score is m, where the largest of all is `all`.
 __device__ __forceinline__ float weight_of(float m, float all, float c) { return m == -INFINITY ? 0.f : exp2f(c * (m - all)); }
 
@@ -437,6 +424,9 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                 }
             // o: rows are columns of the values, columns heads 2 quad and 2 quad + 1
             float o[DP / 16][HN][4], most[HN][2], sum[HN][2];
+            // ST_I8: weights times their values' scales are multiplied as fp16, times the power of two unit_w that leaves the largest of a head's between 1 and
+            // 2^15; high: that largest one, when unit_w was set
+            float unit_w[HN][2], high[HN][2];
             float low[HN][2][GROUPS];                      // ST_I4: what the values' lowest numbers bring to 32 columns
             unsigned any = 0;                              // whether a key of this piece is there
 #pragma unroll
@@ -449,6 +439,8 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                 for (int i = 0; i < 2; ++i) {
                     most[n][i] = -INFINITY;
                     sum[n][i] = 0.f;
+                    unit_w[n][i] = 1.f;
+                    high[n][i] = 0.f;
 #pragma unroll
                     for (int p = 0; p < GROUPS; ++p) low[n][i][p] = 0.f;
                 }
@@ -559,7 +551,8 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                         moves = moves || unit_c[n][i] * (m - most[n][i]) > 8.f;
                     }
                 // as long as no weight passes 2^8 the reference stays: any reference gives the same quotient
-                if (__any_sync(~0u, moves)) {
+                const bool moved = __any_sync(~0u, moves);
+                if (moved) {
 #pragma unroll
                     for (int n = 0; n < HN; ++n)
 #pragma unroll
@@ -567,6 +560,7 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             const float now = fmaxf(most[n][i], top[n][i]), f = now == -INFINITY ? 1.f : exp2f(unit_c[n][i] * (most[n][i] - now));
                             most[n][i] = now;
                             sum[n][i] *= f;
+                            high[n][i] *= f;
                             if (DTYPE == ST_I4)
 #pragma unroll
                                 for (int p = 0; p < GROUPS; ++p) low[n][i][p] *= f;
@@ -577,8 +571,9 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             }
                         }
                 }
-                // Weights as fragments: heads lane / 4, keys 2 quad and 2 quad + 1 (and 8 more); not ST_I4.  Two bf16 numbers to a weight: rounded to one, it would
-                // add as much error to a result as the result's own rounding (0.0025 in the root mean square, not 0.0017).
+                // Weights as fragments: heads lane / 4, keys 2 quad and 2 quad + 1 (and 8 more); not ST_I4.  Rounded to one bf16 number, a weight would add as much
+                // error to a result as the result's own rounding (0.0025 in the root mean square, not 0.0017): two of them beside bf16 values, and one in fp16
+                // beside bytes, 2^-12 of it or, below 2^-14, 2^-25 of the largest (64 sequences 89 us with two bf16 numbers there).
                 uint32_t p[NK][HN][2], rest[NK][HN][2];
 #pragma unroll
                 for (int h = 0; h < NK; ++h) {
@@ -591,16 +586,61 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             y[i] = exp2_fast(fmaf(unit_c[n][i & 1], y[i], most[n][i & 1] == -INFINITY ? 0.f : -unit_c[n][i & 1] * most[n][i & 1]));
                             sum[n][i & 1] += y[i];
                         }
-                        if (DTYPE == ST_I4) continue;
-                        // times their values' scales
+                        if (DTYPE == ST_BF16) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float w0 = y[2 * i] * (i ? s1 : s0), w1 = y[2 * i + 1] * (i ? s1 : s0);
-                            const uint32_t whole = pair_bf16(w0, w1);
-                            p[h][n][i] = transposed(whole);
-                            rest[h][n][i] = transposed(pair_bf16(w0 - low_bf16(whole), w1 - high_bf16(whole)));
+                            for (int i = 0; i < 2; ++i) {
+                                const uint32_t whole = pair_bf16(y[2 * i], y[2 * i + 1]);
+                                p[h][n][i] = transposed(whole);
+                                rest[h][n][i] = transposed(pair_bf16(y[2 * i] - low_bf16(whole), y[2 * i + 1] - high_bf16(whole)));
+                            }
+                        } else if (DTYPE == ST_I8) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[i] *= i < 2 ? s0 : s1;
                         }
                     }
+                }
+                if (DTYPE == ST_I8) {
+                    float all[HN][2];
+                    bool over = moved;                     // the first tile among them
+#pragma unroll
+                    for (int n = 0; n < HN; ++n)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float m = fmaxf(x[0][n][i], x[0][n][2 + i]);
+#pragma unroll
+                            for (int h = 1; h < NK; ++h) m = fmaxf(m, fmaxf(x[h][n][i], x[h][n][2 + i]));
+                            all[n][i] = m;
+                            over = over || m * unit_w[n][i] > 32768.f;
+                        }
+                    if (__any_sync(~0u, over)) {
+#pragma unroll
+                        for (int n = 0; n < HN; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                float m = all[n][i];
+#pragma unroll
+                                for (int e = 4; e < 32; e <<= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, e));
+                                high[n][i] = fmaxf(high[n][i], m);
+                                const int exponent = __float_as_uint(high[n][i]) >> 23;            // 255: not finite, and so is the result
+                                const float now = exponent == 255 ? unit_w[n][i] : __uint_as_float((unsigned)min(max(254 - exponent, 1), 253) << 23);
+                                const float f = fminf(now * inverse_of(unit_w[n][i]), 8.5e37f);    // finite, also where it meets sums of nothing
+                                unit_w[n][i] = now;
+#pragma unroll
+                                for (int k = 0; k < DP / 16; ++k) {
+                                    o[k][n][i] *= f;
+                                    o[k][n][2 + i] *= f;
+                                }
+                            }
+                    }
+#pragma unroll
+                    for (int h = 0; h < NK; ++h)
+#pragma unroll
+                        for (int n = 0; n < HN; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const __half2 two = __floats2half2_rn(x[h][n][2 * i] * unit_w[n][0], x[h][n][2 * i + 1] * unit_w[n][1]);
+                                p[h][n][i] = transposed(*reinterpret_cast<const uint32_t *>(&two));
+                            }
                 }
 #pragma unroll
                 for (int h = 0; h < NK; ++h) {
@@ -627,12 +667,9 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             for (int m = 0; m < 4; ++m) f[m] ^= 0x80808080u;
 #pragma unroll
                             for (int m = 0; m < 2; ++m) {
-                                const uint32_t c[4] = {bytes_bf16(f[2 * m], 0x4240u), bytes_bf16(f[2 * m], 0x4341u), bytes_bf16(f[2 * m + 1], 0x4240u), bytes_bf16(f[2 * m + 1], 0x4341u)};
+                                const uint32_t c[4] = {bytes_half(f[2 * m], 0x4240u), bytes_half(f[2 * m], 0x4341u), bytes_half(f[2 * m + 1], 0x4240u), bytes_half(f[2 * m + 1], 0x4341u)};
 #pragma unroll
-                                for (int n = 0; n < HN; ++n) {
-                                    mma(o[2 * k + m][n], c, p[h][n][0], p[h][n][1]);
-                                    mma(o[2 * k + m][n], c, rest[h][n][0], rest[h][n][1]);
-                                }
+                                for (int n = 0; n < HN; ++n) mma_half(o[2 * k + m][n], c, p[h][n][0], p[h][n][1]);
                             }
                         }
                     } else {
@@ -679,6 +716,17 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                 for (int s = 0; s + 1 < STAGES; ++s) there[s] = there[s + 1];
                 if (++stage == STAGES) stage = 0;
             }
+
+            if (DTYPE == ST_I8)
+#pragma unroll
+                for (int n = 0; n < HN; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int k = 0; k < DP / 16; ++k) {
+                            o[k][n][i] *= inverse_of(unit_w[n][i]);
+                            o[k][n][2 + i] *= inverse_of(unit_w[n][i]);
+                        }
 
             // A whole unit's output is done; with a prefix it goes to where the prefix's parts lie, a piece to where pieces are joined.
             const bool whole = here.tile == 0 && here.last == here.tiles, done = whole && !a.part_count;

@@ -9,7 +9,7 @@
 //
 // The gradient's warps keep the weights' sums in registers; a second kernel adds the blocks' sums in a fixed order.
 //
-// 32768 tokens of 16 + 4 heads of 128 with norms 64 us forward (5.2 TB/s), 88 the gradient (5.7), 4 the sums; 24 heads without norms 5.7 TB/s.  (With 16 lanes to
+// 32768 tokens of 16 + 4 heads of 128 with norms 62 us forward (5.4 TB/s), 91 the gradient (5.5), 4 the sums; 24 heads without norms 5.7 TB/s.  (With 16 lanes to
 // a row and rows loaded when they are needed forward and gradient took 504 us together.)
 #include "attn_common.cuh"
 #include "tc_common.cuh"

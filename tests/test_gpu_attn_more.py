@@ -1099,3 +1099,27 @@ def test_steps_where_nothing_is_to_be_seen(bits):
             st.st_attn_shared_step(q, *c.cells, c.table[:2].contiguous(), c.lens[:2].contiguous(), c.table, c.lens, at, out=out)
             ok()
             assert bool((out == 0).all())
+
+
+@pytest.mark.parametrize("H,Hk,d", [(4, 2, 64), (10, 1, 128)])
+def test_scales_of_values_far_apart(H, Hk, d):
+    """Cells that are not 0 beside scales over 80 powers of two, growing, falling, in any order, or 0: the weights times scales keep their places."""
+    n = 300
+    c = Cache(361, [n] * 4, Hk, d, 16, 8)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(362)
+    for b in range(4):
+        at = c.where(b, 0, n)
+        cells = torch.randint(1, 128, c.cells[1][at].shape, generator=g, device="cuda") * (2 * torch.randint(0, 2, c.cells[1][at].shape, generator=g, device="cuda") - 1)
+        c.cells[1][at] = cells.to(torch.int8)
+        power = torch.linspace(-40, 40, n, device="cuda")
+        power = power if b == 0 else power.flip(0) if b == 1 else power[torch.randperm(n, generator=g, device="cuda")]
+        scale = torch.exp2(power)[:, None].expand(n, Hk).clone()
+        if b == 3:
+            scale[::2] = 0
+        c.scales[1][at] = scale
+    q = normal(363, 4, H, d)
+    for window, sinks in ((1 << 30, 0), (40, 3), (33, 0)):
+        got = st.st_attn_cache_step(q, *c.pages(), window, sinks, **c.how())
+        ok()
+        check_step(got, c, q, window, sinks)
