@@ -476,8 +476,8 @@ st_status st_attn_cache_read(const st_cells *cells, int64_t n, const void *k_pag
  * q_row, q_head (multiples of 8), position lens[b] - 1; out bf16 [nseq, heads, d], contiguous, which may take the place of the whole of a contiguous q.  lens[b] = 0: out = 0.
  * Only table entries of visible tokens are read.  Lengths beyond the table's row (cut), negative ones (0) and page numbers outside the cache where
  * a visible token lies (left out; where no token is left, out = 0) are reported: ST_ERR_DEV_BOUNDS.  Scores, maxima and sums are fp32; cells meet the queries as whole numbers and their
- * scales the scores.  Weights meet the values as two bf16 numbers each (ST_BF16); times the value's scale, as one fp16 number (ST_I8; what is below 2^-14 of
- * the largest so far, to 2^-25 of that); times the steps of 32 columns, as one bf16 number (ST_I4). */
+ * scales the scores.  Weights meet the values as two bf16 numbers each (ST_BF16, and ST_I4 times the steps of 32 columns); times the value's scale, as
+ * one fp16 number (ST_I8; what is below 2^-14 of the largest so far, to 2^-25 of that). */
 st_status st_attn_cache_step(const st_cells *cells, const void *q, int64_t q_row, int64_t q_head, const void *k_pages, const void *v_pages,
                              const void *k_scales, const void *v_scales, const int32_t *table, const int32_t *lens, int64_t window,
                              int64_t sinks, float scale, void *out, void *ws, size_t ws_bytes, void *stream);

@@ -18,7 +18,7 @@
 // consecutive columns, of which the queries' fragments take the same ones.
 //
 // What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 88 us for 385 MB; instructions, some 1050 for a tile of 32 keys, are
-// issued in 61 % of the cycles by twelve warps of an SM.  Of 4 bits 75 us for 199 MB, 1090 instructions for a tile.  One sequence, window 8192: 18.5 us, five
+// issued in 61 % of the cycles by twelve warps of an SM.  Of 4 bits 83 us for 199 MB, some 1200 instructions for a tile.  One sequence, window 8192: 18.5 us, five
 // dependent steps (lay-out, pages, rows, pieces, joins) of some 3 us each.
 #include "attn_cells_step.cuh"
 #include "tc_common.cuh"
@@ -36,8 +36,8 @@ constexpr int LEAST = 3;
 template <int DTYPE, int DP, int HN> struct Shape {
     static constexpr int HEADS = 8 * HN;                                           // of a unit
     static constexpr int BLOCKS = HN == 2 ? 2 : 3;                                 // on an SM, as registers and shared memory leave room for
-    // Tiles in a ring.  Of 4 bits, whose tiles are half as large, three (64 sequences of up to 6000 tokens 74.4 us; two 89; two and a fourth block on the SM,
-    // for which registers are few, 79.7); of 8 bits three leave room for two blocks only (117 us, with two 85.9).
+    // Tiles in a ring.  Of 4 bits, whose tiles are half as large, three (64 sequences of up to 6000 tokens 74.4 us, weights one bf16 number; two 89; two and
+    // a fourth block on the SM, for which registers are few, 79.7); of 8 bits three leave room for two blocks only (117 us, with two 85.9).
     static constexpr int STAGES = DTYPE == ST_I4 ? 3 : 2;
     static constexpr int KEYS = DTYPE == ST_BF16 ? 16 : 32;                        // of a tile
     static constexpr int ROW = DTYPE == ST_BF16 ? 2 * DP : DTYPE == ST_I8 ? DP : DP / 2;       // bytes
@@ -571,9 +571,11 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             }
                         }
                 }
-                // Weights as fragments: heads lane / 4, keys 2 quad and 2 quad + 1 (and 8 more); not ST_I4.  Rounded to one bf16 number, a weight would add as much
-                // error to a result as the result's own rounding (0.0025 in the root mean square, not 0.0017): two of them beside bf16 values, and one in fp16
-                // beside bytes, 2^-12 of it or, below 2^-14, 2^-25 of the largest (64 sequences 89 us with two bf16 numbers there).
+                // Weights as fragments: heads lane / 4, keys 2 quad and 2 quad + 1 (and 8 more); those of ST_I4 are made for each 32 columns below.  Rounded to one bf16
+                // number, a weight would add as much error to a result as the result's own rounding (0.0025 in the root mean square, not 0.0017; of 4 bits, where step
+                // sum(w c) and sum(w lo) cancel, up to 0.0042): two of them beside bf16 values and nibbles, and one in fp16 beside bytes, 2^-12 of it or,
+                // below 2^-14, 2^-25 of the largest (64 sequences of 8 bits 89 us with two bf16 numbers there, 88 so; of 4 bits 75 with one, 83 with two, where one
+                // in fp16 would want a unit for each 32 columns).
                 uint32_t p[NK][HN][2], rest[NK][HN][2];
 #pragma unroll
                 for (int h = 0; h < NK; ++h) {
@@ -684,12 +686,17 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                             for (int m = 0; m < 2; ++m) {
                                 const int group = 2 * k + m;
                                 const uint32_t s0 = v0[group], s1 = v1[group];
-                                uint32_t w[HN][2];
+                                uint32_t w[HN][2], more[HN][2];
 #pragma unroll
                                 for (int n = 0; n < HN; ++n) {
                                     const float *y = x[h][n];
-                                    w[n][0] = transposed(pair_bf16(y[0] * low_bf16(s0), y[1] * low_bf16(s0)));
-                                    w[n][1] = transposed(pair_bf16(y[2] * low_bf16(s1), y[3] * low_bf16(s1)));
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i) {
+                                        const float step = low_bf16(i ? s1 : s0), w0 = y[2 * i] * step, w1 = y[2 * i + 1] * step;
+                                        const uint32_t whole = pair_bf16(w0, w1);
+                                        w[n][i] = transposed(whole);
+                                        more[n][i] = transposed(pair_bf16(w0 - low_bf16(whole), w1 - high_bf16(whole)));
+                                    }
 #pragma unroll
                                     for (int i = 0; i < 2; ++i) low[n][i][group] = fmaf(y[i], high_bf16(s0), fmaf(y[2 + i], high_bf16(s1), low[n][i][group]));
                                 }
@@ -697,7 +704,10 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
                                 for (int j = 0; j < 2; ++j) {
                                     const uint32_t c[4] = {nibbles_bf16(f[2 * m], 2 * j), nibbles_bf16(f[2 * m], 2 * j + 1), nibbles_bf16(f[2 * m + 1], 2 * j), nibbles_bf16(f[2 * m + 1], 2 * j + 1)};
 #pragma unroll
-                                    for (int n = 0; n < HN; ++n) mma(o[2 * group + j][n], c, w[n][0], w[n][1]);
+                                    for (int n = 0; n < HN; ++n) {
+                                        mma(o[2 * group + j][n], c, w[n][0], w[n][1]);
+                                        mma(o[2 * group + j][n], c, more[n][0], more[n][1]);
+                                    }
                                 }
                             }
                         }
