@@ -17,8 +17,8 @@
 // The order of a fragment's columns is free as long as both operands agree, so that no byte has to change its lane: a lane's four bytes of K are four or eight
 // consecutive columns, of which the queries' fragments take the same ones.
 //
-// What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 88 us for 385 MB; instructions, some 1050 for a tile of 32 keys, are
-// issued in 61 % of the cycles by twelve warps of an SM.  Of 4 bits 83 us for 199 MB, some 1200 instructions for a tile.  One sequence, window 8192: 18.5 us, five
+// What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 88 us for 385 MB; instructions, some 890 for a tile of 32 keys, are
+// issued in 59 % of the cycles by twelve warps of an SM.  Of 4 bits 83 us for 199 MB, some 1160 instructions for a tile.  One sequence, window 8192: 18.5 us, five
 // dependent steps (lay-out, pages, rows, pieces, joins) of some 3 us each.
 #include "attn_cells_step.cuh"
 #include "tc_common.cuh"
