@@ -236,8 +236,8 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
     const uint32_t ring = tc::smem_u32(mine);
     int64_t *at = (int64_t *)(smem + WARPS * S::RING) + warp * KEYS;
 
-    // Behind a prefix's kernel: that one lets this one begin only when all before itself is there, and this one reads nothing of it.
-    if (!a.part_count) pdl_wait();
+    // Behind a prefix's kernel too: that one's wait makes what was written before it visible to its own blocks, and says nothing of this one's.
+    pdl_wait();
     pdl_trigger();
     const int64_t total = a.starts[cs.nseq];
     // few pieces go to as many SMs as there are
@@ -797,7 +797,6 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (__any_sync(~0u, bad) && lane == 0) atomicExch(a.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
     }
-    if (a.part_count) pdl_wait();                          // whoever waits for this kernel waits for the prefix's too
 }
 
 // Units that several warps had pieces of, and all of them where prefixes have parts; what has no visible key is 0.  A block to a unit, or to a quarter of its
