@@ -980,15 +980,18 @@ st_status plan_step(CellsStepArgs &a, int dtype, cudaStream_t stream)
 }
 
 template <int DTYPE, int DP, int HN, bool WIDE>
-static st_status run_heads(CellsStepArgs a, cudaStream_t stream)
+static st_status run_heads(CellsStepArgs a, unsigned what, cudaStream_t stream)
 {
     using S = cstep::Shape<DTYPE, DP, HN>;
     static_assert(S::BLOCKS * S::HEADS <= cstep::MOST_HEADS && S::KEYS == (DTYPE == ST_BF16 ? 16 : 32), "as the workspace and the plan have it");
     if (!ensure_dynamic_smem(cells_step_kernel<DTYPE, DP, HN, WIDE>, S::SMEM)) return ST_ERR_CUDA;
     const int blocks = sm_count_or_default() * S::BLOCKS;
     a.slots = blocks * cstep::WARPS;
-    const st_status rc = launch(cells_step_kernel<DTYPE, DP, HN, WIDE>, dim3((unsigned)blocks), cstep::WARPS * 32, S::SMEM, stream, a);
-    if (rc != ST_OK) return rc;
+    if (what & STEP_UNITS) {
+        const st_status rc = launch(cells_step_kernel<DTYPE, DP, HN, WIDE>, dim3((unsigned)blocks), cstep::WARPS * 32, S::SMEM, stream, a);
+        if (rc != ST_OK) return rc;
+    }
+    if (!(what & STEP_JOIN)) return ST_OK;
     // few units may have many pieces each
     const bool few = (int64_t)a.units * a.c.nseq < 2 * sm_count_or_default();
     const int quarters = few ? 4 : 1;
@@ -997,24 +1000,24 @@ static st_status run_heads(CellsStepArgs a, cudaStream_t stream)
 }
 
 template <int DTYPE, int DP, bool WIDE>
-static st_status run_cells(const CellsStepArgs &a, cudaStream_t stream)
+static st_status run_cells(const CellsStepArgs &a, unsigned what, cudaStream_t stream)
 {
-    return unit_heads(a) == 8 ? run_heads<DTYPE, DP, 1, WIDE>(a, stream) : run_heads<DTYPE, DP, 2, WIDE>(a, stream);
+    return unit_heads(a) == 8 ? run_heads<DTYPE, DP, 1, WIDE>(a, what, stream) : run_heads<DTYPE, DP, 2, WIDE>(a, what, stream);
 }
 
-st_status run_cells_step(const CellsStepArgs &a, int dtype, cudaStream_t stream)
+st_status run_cells_step(const CellsStepArgs &a, int dtype, unsigned what, cudaStream_t stream)
 {
     const bool small = a.c.d <= 64;
     const int64_t row = row_bytes(dtype, a.c.d);
     bool wide = row % 16 == 0 && a.c.page_stride % 16 == 0 && a.c.token_stride % 16 == 0 && a.c.head_stride % 16 == 0;
-    if (dtype == ST_BF16) return small ? run_cells<ST_BF16, 64, true>(a, stream) : run_cells<ST_BF16, 128, true>(a, stream);
+    if (dtype == ST_BF16) return small ? run_cells<ST_BF16, 64, true>(a, what, stream) : run_cells<ST_BF16, 128, true>(a, what, stream);
     if (dtype == ST_I8) {
-        if (small) return wide ? run_cells<ST_I8, 64, true>(a, stream) : run_cells<ST_I8, 64, false>(a, stream);
-        return wide ? run_cells<ST_I8, 128, true>(a, stream) : run_cells<ST_I8, 128, false>(a, stream);
+        if (small) return wide ? run_cells<ST_I8, 64, true>(a, what, stream) : run_cells<ST_I8, 64, false>(a, what, stream);
+        return wide ? run_cells<ST_I8, 128, true>(a, what, stream) : run_cells<ST_I8, 128, false>(a, what, stream);
     }
     if (!small) wide = wide && a.c.d > 96 && a.c.scale_page % 4 == 0 && a.c.scale_token % 4 == 0 && a.c.scale_head % 4 == 0;
-    if (small) return wide ? run_cells<ST_I4, 64, true>(a, stream) : run_cells<ST_I4, 64, false>(a, stream);
-    return wide ? run_cells<ST_I4, 128, true>(a, stream) : run_cells<ST_I4, 128, false>(a, stream);
+    if (small) return wide ? run_cells<ST_I4, 64, true>(a, what, stream) : run_cells<ST_I4, 64, false>(a, what, stream);
+    return wide ? run_cells<ST_I4, 128, true>(a, what, stream) : run_cells<ST_I4, 128, false>(a, what, stream);
 }
 
 st_status check_step(const st_cells *c, const void *q, int64_t q_row, int64_t q_head, float scale, const void *out)
@@ -1074,5 +1077,5 @@ extern "C" st_status st_attn_cache_step(const st_cells *c, const void *q, int64_
         return ST_ERR_UNSUPPORTED;
     place_step(a, plan, ws);
     if ((rc = plan_step(a, c->dtype, (cudaStream_t)stream)) != ST_OK) return rc;
-    return run_cells_step(a, c->dtype, (cudaStream_t)stream);
+    return run_cells_step(a, c->dtype, STEP_UNITS | STEP_JOIN, (cudaStream_t)stream);
 }

@@ -39,7 +39,9 @@ StepPlan step_plan(int64_t nseq, size_t from);
 void place_step(CellsStepArgs &a, const StepPlan &p, void *ws);
 // Clears the status and part_count, and lays out the work.
 st_status plan_step(CellsStepArgs &a, int dtype, cudaStream_t stream);
-st_status run_cells_step(const CellsStepArgs &a, int dtype, cudaStream_t stream);
+// The units' kernel, the joins' or both.
+constexpr unsigned STEP_UNITS = 1, STEP_JOIN = 2;
+st_status run_cells_step(const CellsStepArgs &a, int dtype, unsigned what, cudaStream_t stream);
 st_status check_step(const st_cells *c, const void *q, int64_t q_row, int64_t q_head, float scale, const void *out);
 CellsStepArgs step_args(const st_cells *c, const void *q, int64_t q_row, int64_t q_head, const void *k_pages, const void *v_pages, const void *k_scales,
                         const void *v_scales, const int32_t *table, const int32_t *lens, float scale, void *out, void *ws);

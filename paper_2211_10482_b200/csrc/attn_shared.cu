@@ -1,11 +1,11 @@
 // st_attn_shared_step: one token of every sequence over a prefix that its group of sequences shares, then over its own tokens.
 //
-// Two kernels, between one that lays out the work and one that joins.  The first takes all queries of a group that read one key head as the rows of a
-// matrix, up to 256 of them, and makes
+// Two kernels, between one that lays out the work and one that joins.  The first is the single-token kernel over each sequence's own keys.  The second
+// takes all queries of a group that read one key head as the rows of a matrix, up to 256 of them, and makes
 //     S = Q K^T  (tcgen05, fp32 in tensor memory);   P = exp2(c S - c m)  (two threads per row);   O += P V
-// over a range of the prefix's keys, as st_attn_window does for a tile of a prompt; it leaves (m, l, O) as a part.  The second is the single-token kernel over
-// each sequence's own keys, whose pieces are joined with the parts.  A row of the prefix is so read once for 256 queries, not once for
-// every sequence.
+// over a range of the prefix's keys, as st_attn_window does for a tile of a prompt; it leaves (m, l, O) as a part, and the pieces of the own keys are joined
+// with the parts.  A row of the prefix is so read once for 256 queries, not once for every sequence.  (The prefix's blocks, which fill their SMs, are set up
+// while the own tokens' last ones run; the other way round nothing of the second kernel is under way when the first ends: 116 and 112.6 us for 128 sequences.)
 //
 // Pages whose length divides a tile of 128 keys, or is a multiple of it, come by TMA, a box to a page: one warp looks the pages up and asks for them.  A page
 // that is not there is a box outside the tensor and so zeros; values behind the last key are cleared.  Pages of other lengths are gathered by cp.async
@@ -650,8 +650,9 @@ extern "C" st_status st_attn_shared_step(const st_cells *c, const void *q, int64
     a.step.part_sum = a.part_sum;
     a.step.part = a.part;
     if ((rc = plan_step(a.step, ST_BF16, (cudaStream_t)stream)) != ST_OK) return rc;
+    if ((rc = run_cells_step(a.step, ST_BF16, STEP_UNITS, (cudaStream_t)stream)) != ST_OK) return rc;
     if (c->d <= 64) rc = p.tiles_of == 1 ? run_prefix<64, 1>(a, (cudaStream_t)stream) : run_prefix<64, 2>(a, (cudaStream_t)stream);
     else rc = p.tiles_of == 1 ? run_prefix<128, 1>(a, (cudaStream_t)stream) : run_prefix<128, 2>(a, (cudaStream_t)stream);
     if (rc != ST_OK) return rc;
-    return run_cells_step(a.step, ST_BF16, (cudaStream_t)stream);
+    return run_cells_step(a.step, ST_BF16, STEP_JOIN, (cudaStream_t)stream);
 }
