@@ -387,7 +387,8 @@ __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     unit_of[n][i] = DTYPE != ST_BF16 ? __shfl_sync(~0u, in, (2 * quad + i) * 4) : 1.f;
-                    unit_c[n][i] = DTYPE != ST_BF16 ? c * unit_of[n][i] : c;
+                    // above 0 whatever the scale: 0 times a score of -inf would be no number (2^-149 times any score moves a weight by 2^-21 of it at most)
+                    unit_c[n][i] = DTYPE != ST_BF16 ? fmaxf(c * unit_of[n][i], 1.4e-45f) : c;
                 }
             }
             // ST_I4: sums of 32 columns of the queries, which meet a key's lowest numbers in a product of their own: rows 0 to 3 of it (32 columns each) are the
