@@ -894,48 +894,61 @@ __global__ void __launch_bounds__(cstep::JOIN) cells_join_kernel(const CellsStep
     }
 }
 
-// Sums up the tiles of all sequences; one block, so that it may clear the status and then report lengths that the tables do not hold.
+// Sums up the tiles of all sequences; one block, so that it may clear the status and then report lengths that the tables do not hold.  With groups of sequences it
+// takes the largest offset so far for each group's beginning: groups of offsets that decrease would have sequences in common, whose parts two blocks write.
 __global__ void __launch_bounds__(1024) cells_plan_kernel(const CellsStepArgs a, int keys_of_tile)
 {
     __shared__ int64_t sums[32];
     __shared__ int64_t before;
+    __shared__ int mosts[32], most_before;
     pdl_trigger();
     pdl_wait();
     const Cells &cs = a.c;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     bool fine = true;
-    if (threadIdx.x == 0) before = 0;
-    for (int b0 = 0; b0 < cs.nseq; b0 += blockDim.x) {
-        const int b = b0 + threadIdx.x;
+    if (threadIdx.x == 0) before = 0, most_before = 0;
+    const int ends = a.group_offsets ? a.groups + 1 : 0;
+    for (int i0 = 0; i0 < max(cs.nseq, ends); i0 += blockDim.x) {
+        const int i = i0 + threadIdx.x, told_group = i < ends ? a.group_offsets[i] : 0;
         int64_t mine = 0;
-        if (b < cs.nseq) {
-            const int told = cs.lens[b];
+        if (i < cs.nseq) {
+            const int told = cs.lens[i];
             fine = fine && told == length_of(told, cs.cols, cs.page);
             mine = (int64_t)length_on_line((Visible(a, told).keys + keys_of_tile - 1) / keys_of_tile) * (a.units / a.team);
-            if (a.part_count) a.part_count[b] = 0;
+            if (a.part_count) a.part_count[i] = 0;
         }
         int64_t sum = mine;
+        int most = min(max(told_group, 0), cs.nseq);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int64_t x = __shfl_up_sync(~0u, sum, o);
             if (lane >= o) sum += x;
+            if (ends) most = max(most, __shfl_up_sync(~0u, most, o));          // of lanes without one before them, their own
         }
-        if (lane == 31) sums[warp] = sum;
+        if (lane == 31) sums[warp] = sum, mosts[warp] = most;
         __syncthreads();
         if (warp == 0) {
             int64_t s = lane < warps ? sums[lane] : 0;
+            int m = lane < warps ? mosts[lane] : 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int64_t x = __shfl_up_sync(~0u, s, o);
                 if (lane >= o) s += x;
+                m = max(m, __shfl_up_sync(~0u, m, o));
             }
             sums[lane] = s;
+            mosts[lane] = m;
         }
         __syncthreads();
         const int64_t at = before + (warp ? sums[warp - 1] : 0) + sum;
-        if (b < cs.nseq) a.starts[b + 1] = at;
+        if (i < cs.nseq) a.starts[i + 1] = at;
+        most = max(most, max(most_before, warp ? mosts[warp - 1] : 0));
+        if (i < ends) {
+            a.group_cuts[i] = most;
+            fine = fine && told_group == most;
+        }
         __syncthreads();
-        if (threadIdx.x == blockDim.x - 1) before = at;
+        if (threadIdx.x == blockDim.x - 1) before = at, most_before = most;
         __syncthreads();
     }
     fine = __syncthreads_and(fine);

@@ -26,6 +26,10 @@ struct CellsStepArgs {
     // part_count [sequence]: how many there are of each; NULL: none.  Part own_part holds the own tokens of units that one warp has the whole of.
     int *part_count;
     int own_part;
+    // Where the groups of sequences that share a prefix begin, as they were told and, `group_cuts`, as no sequence is in two of them; NULL: one group of all.
+    const int *group_offsets;
+    int *group_cuts;
+    int groups;
     float *part_most, *part_sum, *part;
 };
 
@@ -37,7 +41,7 @@ struct StepPlan {
 };
 StepPlan step_plan(int64_t nseq, size_t from);
 void place_step(CellsStepArgs &a, const StepPlan &p, void *ws);
-// Clears the status and part_count, and lays out the work.
+// Clears the status and part_count, lays out the work and cuts the groups.
 st_status plan_step(CellsStepArgs &a, int dtype, cudaStream_t stream);
 // The units' kernel, the joins' or both.
 constexpr unsigned STEP_UNITS = 1, STEP_JOIN = 2;

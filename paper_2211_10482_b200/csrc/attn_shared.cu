@@ -28,7 +28,7 @@ namespace attn {
 
 struct SharedArgs {
     CellsStepArgs step;
-    const int *prefix_table, *prefix_lens, *group_offsets;
+    const int *prefix_table, *prefix_lens;
     int groups, prefix_cols;
     int seqs;                              // of a tile of rows
     int slots, most_parts;                 // blocks, parts of a prefix
@@ -82,7 +82,7 @@ struct GroupOf {
 __device__ __forceinline__ GroupOf group_of(const SharedArgs &a, int i)
 {
     if (i >= a.groups) return {{0, 0}, 0, 0, 7};
-    const Rows r = rows_of(a.group_offsets, i, a.step.c.nseq);
+    const Rows r = rows_of(a.step.group_cuts, i, a.step.c.nseq);
     const int len = length_of(a.prefix_lens[i], a.prefix_cols, a.step.c.page);
     return {r, (r.len + a.seqs - 1) / a.seqs, (len + TILE - 1) / TILE, (int64_t)r.len * a.step.group > TILE ? 8 : 7};
 }
@@ -177,7 +177,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x == 0) {
-        bool fine = offsets_fine(a.group_offsets, a.groups, cs.nseq, threadIdx.x, S::THREADS);
+        bool fine = true;
         for (int i = threadIdx.x; i < a.groups; i += S::THREADS)
             fine = fine && a.prefix_lens[i] == length_of(a.prefix_lens[i], a.prefix_cols, cs.page);
         if (!fine) atomicExch(a.step.status + kWsStatusWord, (unsigned)ST_ERR_DEV_BOUNDS);
@@ -545,7 +545,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
 // What a call's workspace holds behind its header.
 struct SharedPlan {
     int tiles_of, seqs, slots, most_parts;
-    size_t counts, most, sum, part, bytes;                 // where they begin
+    size_t counts, cuts, most, sum, part, bytes;           // where they begin
     StepPlan step;
 };
 static bool shared_plan(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t groups, SharedPlan *p)
@@ -563,7 +563,8 @@ static bool shared_plan(int64_t nseq, int64_t heads, int64_t kv_heads, int64_t g
     p->most_parts = (int)(parts < 1 ? 1 : parts > MAX_PARTS ? MAX_PARTS : parts);
     const size_t rows = (size_t)nseq * heads * (p->most_parts + 1);        // and one for the own tokens
     p->counts = kWsHeaderBytes;
-    p->most = round_up(p->counts + nseq * sizeof(int), 256);
+    p->cuts = round_up(p->counts + nseq * sizeof(int), 256);
+    p->most = round_up(p->cuts + (groups + 1) * sizeof(int), 256);
     p->sum = round_up(p->most + rows * sizeof(float), 256);
     p->part = round_up(p->sum + rows * sizeof(float), 256);
     p->step = step_plan(nseq, p->part + rows * 128 * sizeof(float));
@@ -634,8 +635,10 @@ extern "C" st_status st_attn_shared_step(const st_cells *c, const void *q, int64
         return ST_ERR_UNSUPPORTED;
     a.prefix_table = prefix_table;
     a.prefix_lens = prefix_lens;
-    a.group_offsets = group_offsets;
     a.groups = (int)groups;
+    a.step.groups = (int)groups;
+    a.step.group_offsets = group_offsets;
+    a.step.group_cuts = group_offsets ? (int *)((char *)ws + p.cuts) : nullptr;
     a.prefix_cols = (int)prefix_cols;
     a.seqs = p.seqs;
     a.slots = p.slots;

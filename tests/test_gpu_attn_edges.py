@@ -7,7 +7,7 @@ pytestmark = pytest.mark.gpu
 import attn_more_reference as ref
 import paper_2211_10482_b200 as st
 from test_gpu_attn import near, normal, ok, spans
-from test_gpu_attn_more import Cache, check_step, shared_inputs
+from test_gpu_attn_more import Cache, check_shared, check_step, ints, shared_inputs
 from test_gpu_parity import GuardAllocator
 
 
@@ -53,3 +53,51 @@ def test_queries_of_nothing_behind_a_prefix(scale):
         for n in range(a, b):
             (k0, k1), (v0, v1) = (tuple(torch.cat(x) for x in zip(c.parts(i, g), c.parts(i, G + n))) for i in range(2))
             near(got[n], *ref.attend(q[n], (k0, k1), (v0, v1), scale), "out of sequence %d" % n)
+
+
+# --------------------------------------------------------------------------------------- groups
+
+
+@pytest.mark.parametrize("told,cut", [
+    ([0, 4, 2, 6], [0, 4, 4, 6]),
+    ([0, 6, 0, 6], [0, 6, 6, 6]),                        # two groups of the same sequences
+    ([3, 0, 5, 8], [3, 3, 5, 8]),
+    ([-3, 2, 100, 5, 8], [0, 2, 8, 8, 8]),
+    ([8, 0, 8, 0, 8], [8, 8, 8, 8, 8]),                  # nobody is left
+    ([0, 2, 2, -1, 1, 7], [0, 2, 2, 2, 2, 7]),
+    ([-(2**31), 2**31 - 1], [0, 8]),
+])
+@pytest.mark.parametrize("H,Hk", [(4, 2), (40, 1)])       # with 40 heads to a key head a tile of rows holds six sequences
+def test_a_sequence_is_in_one_group_whatever_the_offsets(told, cut, H, Hk):
+    G = len(told) - 1
+    groups = [b - a for a, b in zip(cut, cut[1:])]
+    c, q, args, lens = shared_inputs(501, [8] + [0] * (G - 1), [500, 130, 64, 900, 33][:G], [20, 0, 3], H, Hk, 64, 16)
+    want = st.st_attn_shared_step(q, *c.cells, *args[:4], ints(*cut))
+    ok()
+    for _ in range(3):
+        got = st.st_attn_shared_step(q, *c.cells, *args[:4], ints(*told))
+        assert st.st_check_status() == st.ST_ERR_DEV_BOUNDS
+        assert torch.equal(got, want)
+    alone = st.st_attn_cache_step(q, *c.cells, args[2], args[3], 1 << 30)
+    assert torch.equal(got[: cut[0]], alone[: cut[0]]) and torch.equal(got[cut[-1] :], alone[cut[-1] :])
+    prefix = [500, 130, 64, 900, 33]
+    for g, (a, b) in enumerate(zip(cut, cut[1:])):
+        for n in range(a, b):
+            (k0, k1), (v0, v1) = (tuple(torch.cat(x) for x in zip(c.parts(i, g), c.parts(i, G + n))) for i in range(2))
+            near(got[n], *ref.attend(q[n], (k0, k1), (v0, v1)), "out of sequence %d" % n)
+
+
+def test_offsets_of_thousands_of_groups():
+    """More groups than the block that cuts them has threads; some of them fall back, at the ends of warps and blocks too."""
+    n, G = 300, 2500
+    told = torch.tensor([i * n // G for i in range(G + 1)], dtype=torch.int32)
+    for fine in (True, False):
+        if not fine:
+            told[[31, 32, 255, 256, 257, 1023, 1024, 1025, 2047, 2048, 2400]] = torch.tensor([0, 0, -1, 0, 3, 5, 0, 1, 0, 9, n], dtype=torch.int32)
+        cut = told.clamp(0, n).cummax(0).values
+        sizes = (cut[1:] - cut[:-1]).tolist()
+        prefix = [17 if s else 0 for s in sizes]
+        c, q, args, lens = shared_inputs(511, sizes, prefix, [2, 0], 2, 1, 32, 16)
+        got = st.st_attn_shared_step(q, *c.cells, *args[:4], told.cuda())
+        assert st.st_check_status() == (st.ST_OK if fine else st.ST_ERR_DEV_BOUNDS)
+        check_shared(got, c, q, sizes, prefix, lens)
