@@ -485,7 +485,7 @@ st_status st_attn_cache_step(const st_cells *cells, const void *q, int64_t q_row
 /* Attention of one token of every sequence over all of a prefix that its group shares, then all of its own tokens: sequences group_offsets[g] ..
  * group_offsets[g+1]-1 (int32, groups+1 of them; NULL = one group of all) share the prefix_lens[g] tokens behind row g of prefix_table [groups,
  * prefix_cols]; lens[b] tokens behind row b of table are sequence b's own and may be none.  The prefix's scores are computed once for all queries of a group, on the tensor
- * cores.  A sequence of no group, or of an empty prefix, sees its own tokens alone; one without any token has out = 0.  ST_BF16 only.  Reports as
+ * cores; weights meet the values as two bf16 numbers each.  A sequence of no group, or of an empty prefix, sees its own tokens alone; one without any token has out = 0.  ST_BF16 only.  Reports as
  * st_attn_cache_step; prefix lengths likewise.  No sequence is in two groups: one of group_offsets below 0, beyond nseq or below one before it is reported and taken as
  * 0, as nseq, as the largest before it. */
 st_status st_attn_shared_step(const st_cells *cells, const void *q, int64_t q_row, int64_t q_head, const void *k_pages, const void *v_pages,

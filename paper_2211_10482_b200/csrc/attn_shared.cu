@@ -13,10 +13,14 @@
 // cores' proxy and hand the tile over.  (With pages of 64 and all rows gathered by cp.async this kernel took 84 us for 128 sequences behind two prefixes, by boxes 70.)
 // Either way a bit of a mask says which keys have a place.
 //
-// A tile of keys takes 4250 cycles where it meets two tiles of rows, whose four products of 128 x 128 x 128 take half of that: one tile's weights (scores from
+// Weights meet the values as two bf16 numbers each, P and behind it in tensor memory what is left of P, in place of the scores: two products where one would do, and
+// none of the error that one would add (0.0022 to 0.0025 in the root mean square where a result's own rounding is 0.0017).  128 sequences behind two prefixes
+// 113.3 to 122.2 us, 8 samples of one prompt 30.8 to 31.6.  (Splitting weights by cutting bits off instead of rounding takes as long: 122.8.)
+//
+// A tile of keys takes some 4900 cycles where it meets two tiles of rows, whose six products of 128 x 128 x 128 take 3072 of them: one tile's weights (scores from
 // tensor memory, maxima, an exchange with the other half's thread, 64 exponentials) are made while the other one's products run, and in turns, as without them both tiles
-// wanted the exponentials at once and the tensor cores then (128 sequences behind two prefixes: 114.9 us, with turns 107.4).  With one thread to a row and no
-// turns 112; with weights handed over in quarters 113.
+// wanted the exponentials at once and the tensor cores then (with one number to a weight 107.4 us for 114.9; with one thread to a row and no turns 112;
+// with weights handed over in quarters 113.5).
 //
 // Which part of which prefix a block takes is decided on the device, where the lengths are: key tiles of a part are as many as give no more parts than there
 // are blocks in one turn on the SMs.
@@ -73,7 +77,8 @@ __device__ __forceinline__ void copy_row(uint32_t dst, const void *src, bool the
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// Key tiles of a group's prefix, tiles of its rows, and what a key tile costs with one of these: 4250 cycles where the 256 rows are two products, else 3700.
+// Key tiles of a group's prefix, tiles of its rows, and what a key tile costs with one of these: 8 where the 256 rows are two products, else 7.  Nothing hangs on the
+// exact ratio (128 sequences 122 us with 4 to 3 and 9 to 8 too; with none 131), nor at 64 columns, where none is as good (95.8 and 95.3 us).
 struct GroupOf {
     Rows seqs;
     int tiles, keys, cost;
@@ -381,10 +386,12 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                     if (!ok) break;
                     tc_fence_after();
                     mma_tokens<32, 0, 4>(lead, o_col, s_col, V + s * S::TILE_BYTES, o_idesc, i > 1);
+                    mma_tokens<32, 0, 4>(lead, o_col, s_col + 64, V + s * S::TILE_BYTES, o_idesc, true);
                     ok = warp_wait(&p_full[2 * w + 1], done, abort_flag, a.step.status, 6);
                     if (!ok) break;
                     tc_fence_after();
                     mma_tokens<32, 4, 8>(lead, o_col, s_col, V + s * S::TILE_BYTES, o_idesc, true);
+                    mma_tokens<32, 4, 8>(lead, o_col, s_col + 64, V + s * S::TILE_BYTES, o_idesc, true);
                     commit(lead, &v_empty[s]);
                 }
                 if (i == n) break;
@@ -481,7 +488,7 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
                 }
             }
             const float mc = m == -INFINITY ? 0.f : -m * c;
-            const Pair cc = pair(c, c), mm = pair(mc, mc);
+            const Pair cc = pair(c, c), mm = pair(mc, mc), minus = pair(-1.f, -1.f);
             Pair sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
             if (active == 2) {                             // one tile of rows after the other: the products of one go on under the weights of the other
                 ok = warp_wait(&turn[4 * w + (warp & 3)], (uint32_t)((i + 1 - w) & 1), abort_flag, a.step.status, 13);
@@ -489,15 +496,17 @@ shared_prefix_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                uint32_t p[16];
+                uint32_t p[16], rest[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float2 z = split(fma(pair(x[j][2 * e], x[j][2 * e + 1]), cc, mm));
                     const Pair y = pair(ex2(z.x), ex2(z.y));
                     sum[e & 1] = add(sum[e & 1], y);
-                    p[e] = pack_bf16(y);                   // rounded once, for the product with V
+                    p[e] = pack_bf16(y);
+                    rest[e] = pack_bf16(fma(pair(p[e] << 16, p[e] & 0xFFFF0000u), minus, y));
                 }
                 tmem_st_32x16(s_addr + half * 32 + j * 16, p);
+                tmem_st_32x16(s_addr + 64 + half * 32 + j * 16, rest);
             }
             if (active == 2 && lane == 0) mbar_arrive(&turn[4 * (w ^ 1) + (warp & 3)]);
             tmem_st_wait();
