@@ -410,7 +410,7 @@ st_status st_attn_decay_step(const st_tokens *tokens, const void *q, const void 
  *     r = 1 / sqrt(mean_i x[i]^2 + eps);   y[i] = x[i] r w[i]      (norm = 0: y = x)
  *     columns (a, b) of pair i:  y'[a] = factor (y[a] cos t - y[b] sin t),  y'[b] = factor (y[b] cos t + y[a] sin t),  t = position freq[i]
  * Pairs: (2i, 2i+1) where interleaved, else (i, i + rot/2); columns from rot on have no pair and no factor.  The angle is the exact product of
- * the position and the fp32 frequency (|freq| below 2^24), reduced in 64 bits: far positions lose nothing.  Sums, norms and rotations are fp32, a result is rounded once. */
+ * the position and the fp32 frequency (|freq| below 2^24; others, infinities and NaN make their pairs NaN), reduced in 64 bits: far positions lose nothing.  Sums, norms and rotations are fp32, a result is rounded once. */
 typedef struct {
     int32_t dtype;            /* of the tables: ST_BF16 */
     int32_t weight_dtype;     /* of q_weight and k_weight: ST_BF16 or ST_F32 */
@@ -425,7 +425,7 @@ typedef struct {
     float factor;             /* of what is rotated (1 but for scaled contexts), finite */
 } st_rotation;
 
-/* positions: int32 [n], any sign; freq: fp32 [rot/2], finite; q_weight, k_weight: [d] or NULL (ones).  q_out: bf16 [n, heads, d], k_out: [n, kv_heads, d],
+/* positions: int32 [n], any sign; freq: fp32 [rot/2]; q_weight, k_weight: [d] or NULL (ones).  q_out: bf16 [n, heads, d], k_out: [n, kv_heads, d],
  * contiguous; each may take the place of the whole of its own operand, where that is contiguous. */
 st_status st_attn_rotate(const st_rotation *rotation, const void *q, const void *k, const int32_t *positions, const float *freq,
                          const void *q_weight, const void *k_weight, void *q_out, void *k_out, void *stream);

@@ -161,6 +161,9 @@ __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GR
     float freq[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) freq[i] = 2 * lane + i < half ? a.freq[2 * lane + i] : 0.f;
+    // whether one of the row's is no number, or more than the product is exact for
+    auto no_turn = [](float f) { return !(fabsf(f) < 16777216.f); };
+    const bool some_none = __any_sync(~0u, no_turn(freq[0]) || no_turn(freq[1]));
     const int kv_heads = a.width - a.heads;
     // Heads q0.. of nq of q and k0.. of nk of k of a token: an item.
     struct Item {
@@ -251,6 +254,10 @@ __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GR
                 mine_c[i] *= a.factor;
                 mine_s[i] *= GRAD ? -a.factor : a.factor;
             }
+            if (some_none)                                 // read again: kept, a factor for each would take registers in every call (training 152 us, so 150)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (2 * lane + i < half && no_turn(a.freq[2 * lane + i])) mine_c[i] = mine_s[i] = NAN;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 // pairs 8 l + 2 e and the next; neighbours, where the row is in two halves: 4 l + 2 e, and from e = 2 on the second half's

@@ -101,3 +101,34 @@ def test_offsets_of_thousands_of_groups():
         got = st.st_attn_shared_step(q, *c.cells, *args[:4], told.cuda())
         assert st.st_check_status() == (st.ST_OK if fine else st.ST_ERR_DEV_BOUNDS)
         check_shared(got, c, q, sizes, prefix, lens)
+
+
+# ---------------------------------------------------------------------------------- frequencies
+
+
+@pytest.mark.parametrize("rot,inter", [(64, False), (64, True), (20, False), (20, True)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_frequencies_that_are_no_numbers_or_too_large_give_none(rot, inter, norm):
+    """Their pairs are NaN, and the others what they are without them."""
+    n, H, Hk, d = 70, 3, 2, 64
+    q, k = normal(521, n, H, d), normal(522, n, Hk, d)
+    positions = torch.arange(-3, n - 3, dtype=torch.int32, device="cuda")
+    freq = st.st_rotary_frequencies(rot).cuda()
+    bad = {0: float("inf"), 3: float("nan"), 5: 2.0 ** 24, 6: -(2.0 ** 40), rot // 2 - 1: -float("inf")}
+    wrong, clean = freq.clone(), freq.clone()
+    for i, f in bad.items():
+        wrong[i], clean[i] = f, 0.0
+    clean[1], wrong[1] = 16777215.0, 16777215.0          # the largest that there is an exact product for
+    a, b = ref.pairs_of(rot, inter, q.device)
+    hit = torch.zeros(d, dtype=torch.bool, device="cuda")
+    hit[a[list(bad)]] = hit[b[list(bad)]] = True
+    eps = 1e-6 if norm else None
+    for got, want in zip(st.st_attn_rotate(q, k, positions, wrong, inter, eps=eps), st.st_attn_rotate(q, k, positions, clean, inter, eps=eps)):
+        assert bool(got[..., hit].isnan().all()) and torch.equal(got[..., ~hit], want[..., ~hit])
+    near(st.st_attn_rotate(q, k, positions, clean, inter, eps=eps)[0], *ref.rotate(q, None, positions, clean, inter, eps, 1.0), "clean")
+    dq, dk = normal(523, n, H, d), normal(524, n, Hk, d)
+    for got, want in zip(st.st_attn_rotate_grad(q, k, dq, dk, positions, wrong, inter, eps=eps)[:2], st.st_attn_rotate_grad(q, k, dq, dk, positions, clean, inter, eps=eps)[:2]):
+        if norm:
+            assert bool(got.isnan().all())                 # a row's mean is over all of its columns
+        else:
+            assert bool(got[..., hit].isnan().all()) and torch.equal(got[..., ~hit], want[..., ~hit])
