@@ -409,8 +409,8 @@ st_status st_attn_decay_step(const st_tokens *tokens, const void *q, const void 
  * matrix of 2 x 2 blocks in the first `rot` columns, in one pass over the table.  The paper has no counterpart.
  *     r = 1 / sqrt(mean_i x[i]^2 + eps);   y[i] = x[i] r w[i]      (norm = 0: y = x)
  *     columns (a, b) of pair i:  y'[a] = factor (y[a] cos t - y[b] sin t),  y'[b] = factor (y[b] cos t + y[a] sin t),  t = position freq[i]
- * Pairs: (2i, 2i+1) where interleaved, else (i, i + rot/2); columns from rot on have no pair and no factor.  The angle is the exact product of
- * the position and the fp32 frequency (|freq| below 2^24; others, infinities and NaN make their pairs NaN), reduced in 64 bits: far positions lose nothing.  Sums, norms and rotations are fp32, a result is rounded once. */
+ * Pairs: (2i, 2i+1) where interleaved, else (i, i + rot/2); columns from rot on have no pair and no factor.  The angle is the product of
+ * the position and the fp32 frequency (|freq| below 2^24; others, infinities and NaN make their pairs NaN) in whole numbers, to 2^-31 of a turn at any position.  Sums, norms and rotations are fp32, a result is rounded once. */
 typedef struct {
     int32_t dtype;            /* of the tables: ST_BF16 */
     int32_t weight_dtype;     /* of q_weight and k_weight: ST_BF16 or ST_F32 */
@@ -472,7 +472,8 @@ st_status st_attn_cache_read(const st_cells *cells, int64_t n, const void *k_pag
                              const void *v_scales, const int32_t *table, const int32_t *lens, const int32_t *offsets, void *k, void *v,
                              void *ws, size_t ws_bytes, void *stream);
 
-/* st_attn_window for the last token of every sequence over such a cache, which holds it already (st_attn_cache_write): q [nseq, heads, d] with strides
+/* st_attn_window for the last token of every sequence over such a cache, which holds it already (st_attn_cache_write; over ST_BF16 pages alone
+ * st_attn_window_step writes the token itself, in one call and less time): q [nseq, heads, d] with strides
  * q_row, q_head (multiples of 8), position lens[b] - 1; out bf16 [nseq, heads, d], contiguous, which may take the place of the whole of a contiguous q.  lens[b] = 0: out = 0.
  * Only table entries of visible tokens are read.  Lengths beyond the table's row (cut), negative ones (0) and page numbers outside the cache where
  * a visible token lies (left out; where no token is left, out = 0) are reported: ST_ERR_DEV_BOUNDS.  Scores, maxima and sums are fp32; cells meet the queries as whole numbers and their

@@ -447,7 +447,8 @@ def st_attn_cache_step(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Te
                        sinks: int = 0, k_scales: torch.Tensor | None = None, v_scales: torch.Tensor | None = None,
                        scale: float | None = None, out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
     """st_attn_window for the last token of every sequence (q [n, heads, d]) over a cache as st_attn_cache_write fills it, which
-    holds that token's key and value already; nothing is written to the cache."""
+    holds that token's key and value already; nothing is written to the cache.  (With bfloat16 pages and one new token st_attn_window_step writes
+    it and attends in one call, in less time.)"""
     return (_native or _bind()).attn_cache_step(q, k_pages, v_pages, table, lens, window, sinks, k_scales, v_scales, scale, out, ws)
 
 
@@ -456,7 +457,7 @@ def st_attn_shared_step(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.T
                         out: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
     """st_attn_cache_step for a batch whose sequences share prefixes: sequences group_offsets[g] .. group_offsets[g+1]-1 (int32; None: one
     group) see the prefix_lens[g] tokens behind prefix_table[g], then their own lens behind table; bfloat16 pages, no window.  A prefix is
-    read once for all queries of its group."""
+    read once for all queries of its group.  No sequence is in two groups: an offset below one before it is taken as that one, and reported."""
     return (_native or _bind()).attn_shared_step(q, k_pages, v_pages, prefix_table, prefix_lens, table, lens, group_offsets, scale, out, ws)
 
 

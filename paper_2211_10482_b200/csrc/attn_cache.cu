@@ -3,8 +3,9 @@
 // Bound by memory: a row is read once and written once.  16 lanes (8 up to 64 columns) own a row, 8 of its columns each.  A warp takes a run of tokens, of each
 // the keys or the values of some heads (to read, with those of the token after on their way): the sequence that a token belongs to, its length and its page are
 // looked up where the run begins, a sequence ends or a page does, and the next page's number while the one before is in use.
-// 12 prompts at 8 bits, written 22 us and read back 19 (with a look-up and divisions of its own for each row 62 together), some 4 TB/s: issue slots
-// 69 %, conversions and places; 62000 tokens of 4 bits read back 58 us, 5 TB/s.
+// 8 key heads of 128, pages of 64: 12 prompts at 8 bits, 17000 tokens, written in 23 us and read back in 20.5 (with a look-up and divisions of its own for each row 62
+// together), 4.6 and 5.1 TB/s: issue slots 70 %, conversions and places.  25000 tokens of 4 bits 36.6 us (3.6 TB/s, divisions and two extremes for 32 columns) and
+// 27.5 (4.9); 27000 of 16 bits 37.9 (5.8 TB/s) and 38.7.
 #include "attn_cells.cuh"
 
 namespace st {

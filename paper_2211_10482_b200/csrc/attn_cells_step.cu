@@ -17,8 +17,8 @@
 // The order of a fragment's columns is free as long as both operands agree, so that no byte has to change its lane: a lane's four bytes of K are four or eight
 // consecutive columns, of which the queries' fragments take the same ones.
 //
-// What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 88 us for 385 MB; instructions, some 890 for a tile of 32 keys, are
-// issued in 59 % of the cycles by twelve warps of an SM.  Of 4 bits 83 us for 199 MB, some 1160 instructions for a tile.  One sequence, window 8192: 18.5 us, five
+// What bounds it now (64 sequences of up to 6000 tokens, 32 heads on 8 key heads of 128): of 8 bits 84 us for 377 MB; instructions, some 890 for a tile of 32 keys, are
+// issued in 59 % of the cycles by twelve warps of an SM.  Of 4 bits 83 us for 189 MB, some 1160 instructions for a tile.  One sequence, window 8192: 18.3 us, five
 // dependent steps (lay-out, pages, rows, pieces, joins) of some 3 us each.
 #include "attn_cells_step.cuh"
 #include "tc_common.cuh"
@@ -29,15 +29,17 @@ namespace attn {
 
 namespace cstep {
 constexpr int WARPS = 4, MOST_HEADS = 32;                  // warps of a block; blocks on an SM times heads of a unit
-// What a unit costs a warp beside its tiles, in tiles: its queries, its results.
+// What a unit costs a warp beside its tiles, in tiles: its queries, its results.  64 sequences of up to 6000 tokens with a cost of 1, 3 and 6: of 8 bits 88, 86 and 83 us,
+// of 4 bits 83, 83 and 85.5, of 16 bits 153, 151.5 and 148; 96 sequences of up to 100 tokens 19.8, 18.9 and 19.0.
 constexpr int UNIT_COST = 3;
-// The shortest piece of the line that is worth a warp, in tiles.
+// The shortest piece of the line that is worth a warp, in tiles.  With 1, 3 and 8: one sequence behind a window of 8192 keys 19.9, 18.4 and 22.9 us, four of up to 3000
+// tokens 17.2, 19.5 and 29.3, 96 of up to 100 tokens 17.4, 18.9 and 22.6; longer batches take the same.
 constexpr int LEAST = 3;
 template <int DTYPE, int DP, int HN> struct Shape {
     static constexpr int HEADS = 8 * HN;                                           // of a unit
     static constexpr int BLOCKS = HN == 2 ? 2 : 3;                                 // on an SM, as registers and shared memory leave room for
-    // Tiles in a ring.  Of 4 bits, whose tiles are half as large, three (64 sequences of up to 6000 tokens 74.4 us, weights one bf16 number; two 89; two and
-    // a fourth block on the SM, for which registers are few, 79.7); of 8 bits three leave room for two blocks only (117 us, with two 85.9).
+    // Tiles in a ring.  Of 4 bits, whose tiles are half as large, three (64 sequences of up to 6000 tokens 83 us; two 99; two and a fourth block on the SM,
+    // for which registers are few, 88); of 8 bits three leave room for two blocks only (117 us, with two 86).
     static constexpr int STAGES = DTYPE == ST_I4 ? 3 : 2;
     static constexpr int KEYS = DTYPE == ST_BF16 ? 16 : 32;                        // of a tile
     static constexpr int ROW = DTYPE == ST_BF16 ? 2 * DP : DTYPE == ST_I8 ? DP : DP / 2;       // bytes
@@ -220,7 +222,7 @@ struct Walk {
     }
 };
 
-// WIDE: rows and scales may be copied in 16-byte pieces
+// WIDE: rows and scales may be copied in 16-byte pieces, not in ones of 8 and 4 (64 sequences of 8 bits: rows of 80 bytes 76 us, of 72 bytes 101)
 template <int DTYPE, int DP, int HN, bool WIDE>
 __global__ void __launch_bounds__(cstep::WARPS * 32, (cstep::Shape<DTYPE, DP, HN>::BLOCKS)) cells_step_kernel(const CellsStepArgs a)
 {
@@ -982,7 +984,8 @@ void place_step(CellsStepArgs &a, const StepPlan &p, void *ws)
 
 size_t attn_step_workspace(int64_t nseq) { return nseq > 0 && nseq <= 65535 ? step_plan(nseq, kWsHeaderBytes).bytes : 0; }
 
-// Query heads of a unit: up to 8 of them take half of the products of 16.
+// Query heads of a unit: up to 8 of them take half of the products of 16.  64 sequences with 16 heads to a key head, as one unit of 16 and as two of 8, which
+// read the cells twice: of 16 bits 139 and 159 us, of 8 bits 93 and 112, of 4 bits 123 and 155.
 static int unit_heads(const CellsStepArgs &a) { return a.group <= 8 ? 8 : 16; }
 static int tile_keys(int dtype) { return dtype == ST_BF16 ? 16 : 32; }
 

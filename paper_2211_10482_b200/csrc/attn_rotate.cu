@@ -3,14 +3,19 @@
 // Bound by memory as long as a row (one head of one token) takes few instructions.  8 lanes (4 up to 64 columns) own a row, each 16 of its columns as two
 // pieces of 16 bytes which hold both columns of eight pairs, whichever way they are paired: a lane turns its pairs by itself, two at a time in packed fp32.  A
 // warp takes a token, or some of its heads.  Its lanes make the sines and cosines of two of its angles each, all others take them by shuffles, once for all
-// heads.  An angle is position freq / 2 pi turns, of which only the fraction counts: with freq / 2 pi as a fraction of 2^64, the product's low 64 bits are
-// that fraction of a turn, exactly, for any position; the nearest quarter of a turn is its top two bits, and the rest, at most pi / 4, goes into the Taylor
-// series of sine and cosine (their next terms are below 2^-25).  Rows come by asynchronous copies to a ring of the warp's own, over the ends of tokens and of q.
+// heads.  An angle is position freq / 2 pi turns, of which only the fraction counts: with freq / 2 pi in units of 2^-64, cut off by less than two of them, the
+// product's low 64 bits are that fraction of a turn.  Its first 32 are kept: off by at most 2^-32 + |position| 2^-63 turns, 2^-31 at any position.  The nearest quarter of a
+// turn is its top two bits, and the rest, at most pi / 4, goes into the Taylor series of sine and cosine (their next terms are below 2^-25).  Rows come by asynchronous copies to a ring of the warp's own, over the ends of tokens and of q.
 //
 // The gradient's warps keep the weights' sums in registers; a second kernel adds the blocks' sums in a fixed order.
 //
-// 32768 tokens of 16 + 4 heads of 128 with norms 62 us forward (5.4 TB/s), 91 the gradient (5.5), 4 the sums; 24 heads without norms 5.7 TB/s.  (With 16 lanes to
-// a row and rows loaded when they are needed forward and gradient took 504 us together.)
+// 32768 tokens of 16 + 4 heads of 128 with norms, inputs not in L2: forward and gradient together 161.6 us (149 where a part of them is), of which the gradient
+// 93 (5.4 TB/s) and the sums 4; 12289 tokens of 24 heads without norms 29.5 us (5.1 TB/s).  (With 16 lanes to a row and rows loaded when they are needed
+// forward and gradient took 504 us together.)
+//
+// Where `rot` is no multiple of 16, pieces of a half begin off their 16 bytes, and pairs and pieces do not fit together: columns are then taken one by one,
+// from shared memory and with stores of 2 bytes, at a fifth of the speed.  32768 tokens of 24 heads of 80 with norms: 20 turning columns 337 us, 32 of them 68;
+// with the gradient 752 and 169.
 #include "attn_common.cuh"
 #include "tc_common.cuh"
 
@@ -36,7 +41,7 @@ namespace rot {
 constexpr int MAX_D = 128, WEIGHTS = 2 * 4 * 16;      // pieces of the weights in shared memory
 ST_HD constexpr int warps(bool grad) { return grad ? 6 : 8; }                            // of a block
 ST_HD constexpr int min_blocks(bool odd, bool grad) { return odd || grad ? 2 : 3; }       // on an SM
-ST_HD constexpr int ahead(bool grad) { return grad ? 4 : 4; }                            // rows of a lane on their way
+constexpr int AHEAD = 4;                                                                 // rows of a lane on their way
 }  // namespace rot
 
 // The fraction of freq / 2 pi, in units of 2^-64: the frequency's 24 bits times the first 128 bits of 1 / 2 pi, in whole numbers.  |freq| below 2^24.  (One
@@ -125,7 +130,7 @@ template <int LANES, bool NORM, bool INTER, bool ODD, bool GRAD, bool MIXED>
 __global__ void __launch_bounds__(rot::warps(GRAD) * 32, rot::min_blocks(ODD, GRAD)) rotate_kernel(const RotateArgs a)
 {
     using namespace rot;
-    constexpr int ROWS = 32 / LANES, AHEAD = rot::ahead(GRAD), WARPS = rot::warps(GRAD);
+    constexpr int ROWS = 32 / LANES, WARPS = rot::warps(GRAD);
     constexpr bool TWO = GRAD && NORM;                     // tables that are read: x and dy, or one of them
     constexpr int TABLE = ODD ? 32 : 64, STAGE = TABLE * (TWO ? 2 : 1);       // pieces of a step
     extern __shared__ __align__(16) uint4 smem[];
@@ -455,7 +460,7 @@ static st_status launch_rotate(const RotateArgs &a, bool norm, bool inter, int g
     using namespace rot;
     void (*kernel)(RotateArgs) = norm ? (inter ? rotate_kernel<LANES, true, true, ODD, GRAD, MIXED> : rotate_kernel<LANES, true, false, ODD, GRAD, MIXED>)
                                       : (inter ? rotate_kernel<LANES, false, true, ODD, GRAD, MIXED> : rotate_kernel<LANES, false, false, ODD, GRAD, MIXED>);
-    const size_t smem = (size_t)warps(GRAD) * 32 * ahead(GRAD) * 16 * (ODD ? 1 : 2) * (GRAD && norm ? 2 : 1) + (norm ? WEIGHTS * 16 : 0);
+    const size_t smem = (size_t)warps(GRAD) * 32 * AHEAD * 16 * (ODD ? 1 : 2) * (GRAD && norm ? 2 : 1) + (norm ? WEIGHTS * 16 : 0);
     if (!ensure_dynamic_smem(kernel, smem)) return ST_ERR_CUDA;
     return launch(kernel, dim3((unsigned)grid), warps(GRAD) * 32, smem, stream, a);
 }

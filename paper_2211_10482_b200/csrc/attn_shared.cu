@@ -10,11 +10,11 @@
 // Pages whose length divides a tile of 128 keys, or is a multiple of it, come by TMA, a box to a page: one warp looks the pages up and asks for them.  A page
 // that is not there is a box outside the tensor and so zeros; values behind the last key are cleared.  Pages of other lengths are gathered by cp.async
 // into the swizzled tiles that the tensor cores read, by one or two warps for each stage, which copy, see the copies done, make them visible to the tensor
-// cores' proxy and hand the tile over.  (With pages of 64 and all rows gathered by cp.async this kernel took 84 us for 128 sequences behind two prefixes, by boxes 70.)
+// cores' proxy and hand the tile over.  (128 sequences behind two prefixes, the whole call: with pages of 64 122 us, with pages of 100, which are gathered, 157.)
 // Either way a bit of a mask says which keys have a place.
 //
 // Weights meet the values as two bf16 numbers each, P and behind it in tensor memory what is left of P, in place of the scores: two products where one would do, and
-// none of the error that one would add (0.0022 to 0.0025 in the root mean square where a result's own rounding is 0.0017).  128 sequences behind two prefixes
+// none of the error that one would add (0.0022 and 0.0023 in the root mean square of the two cases below, where a result's own rounding is 0.0017).  128 sequences behind two prefixes
 // 113.3 to 122.2 us, 8 samples of one prompt 30.8 to 31.6.  (Splitting weights by cutting bits off instead of rounding takes as long: 122.8.)
 //
 // A tile of keys takes some 4900 cycles where it meets two tiles of rows, whose six products of 128 x 128 x 128 take 3072 of them: one tile's weights (scores from
