@@ -132,3 +132,57 @@ def test_frequencies_that_are_no_numbers_or_too_large_give_none(rot, inter, norm
             assert bool(got.isnan().all())                 # a row's mean is over all of its columns
         else:
             assert bool(got[..., hit].isnan().all()) and torch.equal(got[..., ~hit], want[..., ~hit])
+
+
+# -------------------------------------------------------------------------------------- extents
+
+
+@pytest.mark.parametrize("groups,prefix,own,H,Hk,d,page", [
+    ([3], [200], [9, 0], 2, 1, 8, 16),                   # a box of 64 columns of which the table has 8
+    ([2, 2], [90, 300], [5], 4, 2, 8, 8),
+    ([5], [700], [1, 300], 6, 2, 72, 128),               # the second box of a row has 8 columns
+    ([40], [515], [2], 8, 2, 104, 512),
+    ([4], [260], [30], 4, 4, 64, 1024),                  # one page holds all
+])
+def test_shared_step_of_narrow_heads_and_long_pages(groups, prefix, own, H, Hk, d, page):
+    c, q, args, lens = shared_inputs(531, groups, prefix, own, H, Hk, d, page)
+    got = st.st_attn_shared_step(q, *c.cells, *args)
+    ok()
+    check_shared(got, c, q, groups, prefix, lens)
+
+
+def repeated(c, n, page, pages):
+    """What the first n tokens behind a table that goes through `pages` pages again and again count for: places and how often each is there."""
+    place = torch.arange(pages * page, device="cuda")
+    turns, rest = divmod(n, pages * page)
+    return (c.table[0].long()[place // page], place % page), (turns + (place < rest)).double()
+
+
+def weighted(q, k, v, times, scale):
+    """ref.attend over keys that are there several times."""
+    group = q.shape[0] // k[0].shape[1]
+    Q = q.double()[:, None]
+    (k0, k1), (v0, v1) = (tuple(z.repeat_interleave(group, 1).transpose(0, 1) for z in x) for x in (k, v))
+    x = (Q @ (k0 + k1).transpose(1, 2)) * scale + times.log()
+    p = torch.softmax(x, -1)
+    off = ref.E * scale * (Q.abs() @ (k0.abs() + k1.abs()).transpose(1, 2)).amax(-1)
+    out, size = p @ (v0 + v1), p @ (v0.abs() + v1.abs())
+    return out.squeeze(1), (ref.B * (p @ v1.abs()) + ref.B * out.abs() + (ref.F + 2 * off[..., None]) * size).squeeze(1)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+def test_steps_over_sixteen_million_tokens(bits):
+    """Pages that a table names again and again, so that positions, tiles and pieces are many and the cache is small."""
+    page, pages, n, H, Hk, d = 256, 8, (1 << 24) + 77, 4, 1, 64
+    c = Cache(541, [page * pages], Hk, d, page, bits)
+    q = normal(542, 1, H, d)
+    table = c.table[:, torch.arange((1 << 16) + 1, device="cuda") % pages].contiguous()
+    at, times = repeated(c, n, page, pages)
+    want = weighted(q[0], c.parts(0, 0, at), c.parts(1, 0, at), times, d ** -0.5)
+    got = st.st_attn_cache_step(q, *c.cells, table, ints(n), 1 << 30, 0, **c.how())
+    ok()
+    near(got[0], *want, "step")
+    if bits == 16:
+        got = st.st_attn_shared_step(q, *c.cells, table, ints(n - page * pages), c.table, ints(page * pages))
+        ok()
+        near(got[0], *want, "behind a prefix")
