@@ -17,7 +17,7 @@
 // none of the error that one would add (0.0022 and 0.0023 in the root mean square of the two cases below, where a result's own rounding is 0.0017).  128 sequences behind two prefixes
 // 113.3 to 122.2 us, 8 samples of one prompt 30.8 to 31.6.  (Splitting weights by cutting bits off instead of rounding takes as long: 122.8.)
 //
-// A tile of keys takes some 4900 cycles where it meets two tiles of rows, whose six products of 128 x 128 x 128 take 3072 of them: one tile's weights (scores from
+// A tile of keys takes some 4900 cycles where it meets two tiles of rows, whose six products of 128 x 128 x 128 take 512 each: one tile's weights (scores from
 // tensor memory, maxima, an exchange with the other half's thread, 64 exponentials) are made while the other one's products run, and in turns, as without them both tiles
 // wanted the exponentials at once and the tensor cores then (with one number to a weight 107.4 us for 114.9; with one thread to a row and no turns 112;
 // with weights handed over in quarters 113.5).
